@@ -404,6 +404,113 @@ int cvlc_decode_apply(const uint8_t* const* streams_dev, const uint64_t* stream_
                       uint32_t n_clients, double weight_total, uint64_t d, float* model_dev, float* aggregate_dev,
                       void* ws_dev, size_t ws_bytes, void* cuda_stream);
 
+/* --- where a client's local step meets the vocabulary ------------------------ */
+
+/*
+ * A client whose model speaks a vocabulary (a language model, or a classifier of many classes) meets it at two ends, and at
+ * both what it handles is sparse, as in the stream: records of (word, value) of a row of logits, and rows of the
+ * embedding table, the largest block of the update and the one of which a round touches least.  (The paper leaves
+ * the local steps open, Section III, step 2.)
+ *
+ * Types of logits, tables and their gradients.  Sums, maxima and softmax statistics are held in 32 bits or more and
+ * rounded once, to nearest.  Rows may have any stride of at least their length (in elements) and begin at any element:
+ * 16-byte alignment is faster, not required. */
+#define CVLC_F32 0u
+#define CVLC_F16 1u
+#define CVLC_BF16 2u
+
+#define CVLC_MAX_VOCAB (1u << 22)   /* words of a row of logits */
+#define CVLC_MAX_TOP 256u           /* records of a row that cvlc_top_logits lists */
+#define CVLC_MAX_RECORDS 1024u      /* records of a row that the loss takes */
+#define CVLC_DISTILL_STATS 8u       /* floats a row that the loss leaves for its gradient */
+
+/*
+ * What a client answers, in place of an update or next to it: of every row of logits the k largest, in descending
+ * order, equal ones by ascending word (zeros of either sign are equal), each with its log-probability
+ * log softmax(row / temperature).  Logits of -inf (masked words) are never listed: where fewer than k others are there, the
+ * last records are absent, word -1 with log-probability -inf.  A row with a NaN or +inf has no softmax: its records
+ * are words 0 .. k-1 with NaN.
+ *  logits_dev   rows x vocab of `dtype`, rows row_stride elements apart
+ *  ids_dev, logp_dev   rows x k, contiguous
+ * Errors: INVALID_ARG (a type, k above vocab or CVLC_MAX_TOP, vocab above CVLC_MAX_VOCAB, rows above 2^27, a stride below
+ * vocab, a temperature that is not positive and finite, a pointer that is not aligned to its type).  rows = 0 does nothing.
+ */
+int cvlc_top_logits(const void* logits_dev, uint32_t dtype, uint64_t rows, uint32_t vocab, uint64_t row_stride,
+                    uint32_t k, float temperature, int32_t* ids_dev, float* logp_dev, void* cuda_stream);
+
+/*
+ * Distillation from such answers.  With z a row of the student's logits, q = softmax(z / temperature), and
+ * p_j = the sum of exp(log-probability) over the row's records of word j (records of one word add up: lists of several
+ * clients may be joined, each with the logarithm of its weight added), P = sum p:
+ *   CVLC_REST_NONE    loss = sum_j p_j (ln p_j - ln q_j)
+ *   CVLC_REST_SCALED  the same of p / P; nothing where P = 0
+ *   CVLC_REST_BUCKET  all words that are not listed are one further outcome, of probability pr = max(0, 1 - P) for the
+ *                     teacher and qr = the sum of their q for the student: loss + pr (ln pr - ln qr).  Where the
+ *                     student may say none of them (no logit above -inf), there is no such outcome.
+ * Loss and gradient of a row are multiplied by its weight; with a weight of 0 both are 0, whatever the row holds.  The
+ * gradient is with respect to z (it holds the factor 1 / temperature; the customary temperature^2 goes into the
+ * weights).  A row whose logits are all -inf has no distribution: loss and gradient 0.  A listed word whose logit is -inf
+ * makes the loss +inf.
+ *  ids_dev, logp_dev   rows x k records, contiguous; a record of word below 0 is absent; one of word >= vocab is left
+ *                      out and reported (INVALID_ARG) in *status_dev
+ *  row_weight_dev      rows weights, or NULL: all 1
+ *  status_dev          one int32 of the caller's, 0 beforehand: the first error stays in it; or NULL
+ * cvlc_distill_loss writes loss_dev (rows) and, where stats_dev is not NULL, rows x CVLC_DISTILL_STATS floats (16-byte
+ * aligned) from which cvlc_distill_grad makes the gradient, with row weights of its own.  It has to be given the same
+ * logits and records.  cvlc_distill_step makes loss and gradient in one reading of the logits.  grad_dev: rows of
+ * `dtype`, grad_stride elements apart; it may be logits_dev itself (with the same stride), and must not overlap it otherwise.
+ * Results do not depend on the order in which blocks run.
+ * Errors: as cvlc_top_logits; k from 0 to CVLC_MAX_RECORDS.
+ */
+#define CVLC_REST_NONE 0u
+#define CVLC_REST_SCALED 1u
+#define CVLC_REST_BUCKET 2u
+typedef struct cvlc_distill {
+  const void* logits_dev;
+  uint64_t rows;
+  uint64_t row_stride;
+  uint32_t vocab;
+  uint32_t dtype;
+  const int32_t* ids_dev;
+  const float* logp_dev;
+  uint32_t k;
+  uint32_t rest;
+  float temperature;
+  uint32_t reserved;
+  const float* row_weight_dev;
+  int32_t* status_dev;
+} cvlc_distill;
+int cvlc_distill_loss(const cvlc_distill* a, float* loss_dev, float* stats_dev, void* cuda_stream);
+int cvlc_distill_grad(const cvlc_distill* a, const float* stats_dev, void* grad_dev, uint64_t grad_stride,
+                      void* cuda_stream);
+int cvlc_distill_step(const cvlc_distill* a, float* loss_dev, void* grad_dev, uint64_t grad_stride, void* cuda_stream);
+
+/*
+ * Embedding: out[i] = scale * table[tokens[i]], rounded once.  Tokens are int32 or int64 (token_bytes 4 or 8); one below
+ * 0 is padding and gives zeros; one >= vocab gives zeros and is reported (INVALID_ARG) in *status_dev (as above).
+ *  table_dev   vocab x dim of `dtype`, table_stride elements apart; out_dev: n x dim, out_stride apart, not overlapping it
+ */
+int cvlc_embed(const void* table_dev, uint32_t dtype, uint64_t vocab, uint32_t dim, uint64_t table_stride,
+               const void* tokens_dev, uint32_t token_bytes, uint64_t n, float scale, void* out_dev, uint64_t out_stride,
+               int32_t* status_dev, void* cuda_stream);
+
+/*
+ * Its gradient: update[v] = scale * sum of grad[i] over the positions i with tokens[i] = v, in fp32, added to the rows that are
+ * there (accumulate = 1; rows of words that do not occur are not touched) or with zeros for words that do not occur
+ * (accumulate = 0).  With the block of the table in the client's update vector as update_dev and the learning rate in
+ * `scale`, local steps of SGD leave U = w_0 - w_E there for cvlc_plan.  The positions of a word are added in ascending
+ * order in a fixed grouping: equal inputs give equal bits.  Padding (below 0) has no gradient; a token >= vocab has none either and
+ * is reported (INVALID_ARG) at byte 0 of the workspace (cvlc_read_status).
+ *  grad_dev     n x dim of `dtype`, grad_stride elements apart;  update_dev: vocab x dim fp32, update_stride apart,
+ *               not overlapping grad_dev
+ *  ws_dev       cvlc_embed_grad_workspace_bytes(n, dim, vocab) bytes, 256-byte aligned
+ * Errors: INVALID_ARG (as above; vocab up to 2^31 - 1, dim up to 2^20, n up to 2^31 - 1), WORKSPACE_TOO_SMALL.
+ */
+size_t cvlc_embed_grad_workspace_bytes(uint64_t n, uint32_t dim, uint64_t vocab);
+int cvlc_embed_grad(const void* tokens_dev, uint32_t token_bytes, uint64_t n, const void* grad_dev, uint32_t dtype,
+                    uint32_t dim, uint64_t grad_stride, uint64_t vocab, float scale, float* update_dev,
+                    uint64_t update_stride, int accumulate, void* ws_dev, size_t ws_bytes, void* cuda_stream);
+
 /* Waits for cuda_stream and returns the status word at byte 0 of a plan or workspace. */
 int cvlc_read_status(const void* plan_or_ws_dev, void* cuda_stream);
 
@@ -429,7 +536,8 @@ int cvlc_selftest_wait(uint64_t* word_dev, int32_t* status_dev, uint32_t max_pol
  * (all kernels when kernel_name is NULL or "", else the named one, e.g. "k_hist").  Kernel names: k_zero_words,
  * k_hist, k_plan_threshold, k_plan_fit, k_plan_tune, k_encode_init, k_select, k_select_lookback, k_rank_split, k_rank, k_rank_rest, k_sort,
  * k_pack, k_decode_prepare, k_fill_zero, k_prefetch_l2, k_decode,
- * k_noalloc_publish_status, k_selftest, k_hist_check, k_apply, k_plan_literal, k_ec_accumulate, k_pack_unframed, k_decode_unframed. */
+ * k_noalloc_publish_status, k_selftest, k_hist_check, k_apply, k_plan_literal, k_ec_accumulate, k_pack_unframed, k_decode_unframed,
+ * k_top_logits, k_distill_loss, k_distill_grad, k_distill_step, k_embed, k_token_sort, k_embed_sum, k_embed_join. */
 unsigned long long cvlc_launch_count(const char* kernel_name);
 /* Optional kernel timing: after cvlc_profile_select(name, n) the next n launches of that kernel
  * ("*" = of every kernel) are bracketed by a CUDA event pair on their own stream;

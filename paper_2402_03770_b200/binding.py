@@ -32,6 +32,13 @@ CVLC_ERR_NOT_IMPLEMENTED = 11
 CVLC_ERR_SCALE_TOO_SMALL = 12
 CVLC_ERR_PLAN_MISMATCH = 13
 
+CVLC_F32, CVLC_F16, CVLC_BF16 = 0, 1, 2
+CVLC_REST_NONE, CVLC_REST_SCALED, CVLC_REST_BUCKET = 0, 1, 2
+MAX_VOCAB = 1 << 22
+MAX_TOP = 256
+MAX_RECORDS = 1024
+DISTILL_STATS = 8
+
 CVLC_QUANT_PQ = 0
 CVLC_QUANT_QSGD = 1
 
@@ -49,7 +56,9 @@ EXPORTS = [
     "cvlc_selftest_philox", "cvlc_selftest_math", "cvlc_histogram_batch", "cvlc_plan_from_histogram_batch", "cvlc_decode_apply",
     "cvlc_decode_aggregate_noalloc", "cvlc_compress_batch", "cvlc_selftest_wait", "cvlc_plan_literal",
     "cvlc_plan_literal_workspace_bytes", "cvlc_ec_accumulate_batch", "cvlc_encode_batch_ec",
-    "cvlc_unframed_stream_capacity", "cvlc_unframed_workspace_bytes", "cvlc_encode_unframed_batch", "cvlc_decode_aggregate_unframed", "cvlc_launch_count", "cvlc_profile_select", "cvlc_profile_reset", "cvlc_profile_read",
+    "cvlc_unframed_stream_capacity", "cvlc_unframed_workspace_bytes", "cvlc_encode_unframed_batch", "cvlc_decode_aggregate_unframed",
+    "cvlc_top_logits", "cvlc_distill_loss", "cvlc_distill_grad", "cvlc_distill_step", "cvlc_embed", "cvlc_embed_grad_workspace_bytes",
+    "cvlc_embed_grad", "cvlc_launch_count", "cvlc_profile_select", "cvlc_profile_reset", "cvlc_profile_read",
 ]
 
 
@@ -77,6 +86,14 @@ class CvlcPlan(C.Structure):
 
 
 assert C.sizeof(CvlcPlan) == PLAN_BYTES
+
+
+class CvlcDistill(C.Structure):
+    _fields_ = [
+        ("logits_dev", C.c_void_p), ("rows", C.c_uint64), ("row_stride", C.c_uint64), ("vocab", C.c_uint32), ("dtype", C.c_uint32),
+        ("ids_dev", C.c_void_p), ("logp_dev", C.c_void_p), ("k", C.c_uint32), ("rest", C.c_uint32), ("temperature", C.c_float),
+        ("reserved", C.c_uint32), ("row_weight_dev", C.c_void_p), ("status_dev", C.c_void_p),
+    ]
 
 
 class CvlcError(RuntimeError):
@@ -158,6 +175,21 @@ def lib() -> C.CDLL:
     L.cvlc_decode_apply.argtypes = [vp, vp, vp, u32, f64, u64, vp, vp, vp, sz, vp]
     L.cvlc_decode_aggregate_noalloc.restype = C.c_int
     L.cvlc_decode_aggregate_noalloc.argtypes = [vp, vp, vp, u32, f64, u64, vp, C.c_int, vp, vp]
+    PD = C.POINTER(CvlcDistill)
+    L.cvlc_top_logits.restype = C.c_int
+    L.cvlc_top_logits.argtypes = [vp, u32, u64, u32, u64, u32, C.c_float, vp, vp, vp]
+    L.cvlc_distill_loss.restype = C.c_int
+    L.cvlc_distill_loss.argtypes = [PD, vp, vp, vp]
+    L.cvlc_distill_grad.restype = C.c_int
+    L.cvlc_distill_grad.argtypes = [PD, vp, vp, u64, vp]
+    L.cvlc_distill_step.restype = C.c_int
+    L.cvlc_distill_step.argtypes = [PD, vp, vp, u64, vp]
+    L.cvlc_embed.restype = C.c_int
+    L.cvlc_embed.argtypes = [vp, u32, u64, u32, u64, vp, u32, u64, C.c_float, vp, u64, vp, vp]
+    L.cvlc_embed_grad_workspace_bytes.restype = sz
+    L.cvlc_embed_grad_workspace_bytes.argtypes = [u64, u32, u64]
+    L.cvlc_embed_grad.restype = C.c_int
+    L.cvlc_embed_grad.argtypes = [vp, u32, u64, vp, u32, u32, u64, u64, C.c_float, vp, u64, C.c_int, vp, sz, vp]
     L.cvlc_read_status.restype = C.c_int
     L.cvlc_read_status.argtypes = [vp, vp]
     L.cvlc_selftest_philox.restype = C.c_int
@@ -482,6 +514,114 @@ def cvlc_decode_aggregate_noalloc(stream_ptrs: torch.Tensor, stream_bytes: torch
            "cvlc_decode_aggregate_noalloc")
 
 
+# ---- where a client's local step meets the vocabulary ----------------------------------------
+
+_DTYPES = {torch.float32: CVLC_F32, torch.float16: CVLC_F16, torch.bfloat16: CVLC_BF16}
+
+
+def _rows(t: torch.Tensor) -> Tuple[int, int]:
+    """pointer and row stride of a matrix whose rows are contiguous"""
+    assert t.dim() == 2 and t.is_cuda and t.device.index == torch.cuda.current_device()
+    assert t.shape[1] <= 1 or t.stride(1) == 1
+    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+
+
+def _here(t: Optional[torch.Tensor], dtype: torch.dtype, shape: Tuple[int, ...]) -> Optional[int]:
+    """pointer of a contiguous tensor of this type and shape on the current device"""
+    if t is None:
+        return None
+    assert t.is_cuda and t.device.index == torch.cuda.current_device() and t.is_contiguous()
+    assert t.dtype == dtype and tuple(t.shape) == shape, (t.dtype, tuple(t.shape), dtype, shape)
+    return t.data_ptr()
+
+
+def cvlc_top_logits(logits: torch.Tensor, ids: torch.Tensor, logp: torch.Tensor, temperature: float = 1.0,
+                    stream: Optional[torch.cuda.Stream] = None) -> None:
+    """The k = ids.shape[1] largest logits of every row: words into ids (int32), log-probabilities into logp (fp32)."""
+    at, stride = _rows(logits)
+    rows, vocab = logits.shape
+    shape = (rows, ids.shape[1])
+    _check(lib().cvlc_top_logits(at, _DTYPES[logits.dtype], rows, vocab, stride, shape[1], temperature, _here(ids, torch.int32, shape),
+                                 _here(logp, torch.float32, shape), _stream_handle(stream)), "cvlc_top_logits")
+
+
+def _distill(logits: torch.Tensor, ids: torch.Tensor, logp: torch.Tensor, rest: int, temperature: float,
+             row_weight: Optional[torch.Tensor], status: Optional[torch.Tensor]) -> CvlcDistill:
+    at, stride = _rows(logits)
+    rows, vocab = logits.shape
+    shape = (rows, ids.shape[1])
+    return CvlcDistill(at, rows, stride, vocab, _DTYPES[logits.dtype], _here(ids, torch.int32, shape), _here(logp, torch.float32, shape),
+                       shape[1], rest, temperature, 0, _here(row_weight, torch.float32, (rows,)), _here(status, torch.int32, (1,)))
+
+
+def _graded(logits: torch.Tensor, grad: torch.Tensor) -> Tuple[int, int]:
+    assert grad.dtype == logits.dtype and grad.shape == logits.shape
+    return _rows(grad)
+
+
+def cvlc_distill_loss(logits: torch.Tensor, ids: torch.Tensor, logp: torch.Tensor, loss: torch.Tensor,
+                      stats: Optional[torch.Tensor] = None, *, rest: int = CVLC_REST_BUCKET, temperature: float = 1.0,
+                      row_weight: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None,
+                      stream: Optional[torch.cuda.Stream] = None) -> None:
+    """loss[rows] of distilling the teacher's records (ids int32, logp fp32; rows x k) into the student's logits; stats (fp32, rows x
+    DISTILL_STATS) keeps what cvlc_distill_grad needs."""
+    a = _distill(logits, ids, logp, rest, temperature, row_weight, status)
+    rows = logits.shape[0]
+    _check(lib().cvlc_distill_loss(C.byref(a), _here(loss, torch.float32, (rows,)), _here(stats, torch.float32, (rows, DISTILL_STATS)),
+                                   _stream_handle(stream)), "cvlc_distill_loss")
+
+
+def cvlc_distill_grad(logits: torch.Tensor, ids: torch.Tensor, logp: torch.Tensor, stats: torch.Tensor, grad: torch.Tensor, *,
+                      rest: int = CVLC_REST_BUCKET, temperature: float = 1.0, row_weight: Optional[torch.Tensor] = None,
+                      status: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> None:
+    """grad (as logits, or logits itself) of the sum of row_weight * loss; the other arguments as in the call that filled stats."""
+    a = _distill(logits, ids, logp, rest, temperature, row_weight, status)
+    g, stride = _graded(logits, grad)
+    _check(lib().cvlc_distill_grad(C.byref(a), _here(stats, torch.float32, (logits.shape[0], DISTILL_STATS)), g, stride,
+                                   _stream_handle(stream)), "cvlc_distill_grad")
+
+
+def cvlc_distill_step(logits: torch.Tensor, ids: torch.Tensor, logp: torch.Tensor, loss: torch.Tensor, grad: torch.Tensor, *,
+                      rest: int = CVLC_REST_BUCKET, temperature: float = 1.0, row_weight: Optional[torch.Tensor] = None,
+                      status: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> None:
+    """cvlc_distill_loss and cvlc_distill_grad in one reading of the logits"""
+    a = _distill(logits, ids, logp, rest, temperature, row_weight, status)
+    g, stride = _graded(logits, grad)
+    _check(lib().cvlc_distill_step(C.byref(a), _here(loss, torch.float32, (logits.shape[0],)), g, stride, _stream_handle(stream)),
+           "cvlc_distill_step")
+
+
+def _token_bytes(tokens: torch.Tensor) -> int:
+    assert tokens.dtype in (torch.int32, torch.int64) and tokens.dim() == 1
+    return tokens.element_size()
+
+
+def cvlc_embed(table: torch.Tensor, tokens: torch.Tensor, out: torch.Tensor, scale: float = 1.0, status: Optional[torch.Tensor] = None,
+               stream: Optional[torch.cuda.Stream] = None) -> None:
+    """out[i] = scale * table[tokens[i]]; tokens (int32 or int64) below 0 are padding and give zeros."""
+    at, stride = _rows(table)
+    o, out_stride = _rows(out)
+    n, (vocab, dim) = tokens.numel(), table.shape
+    assert out.dtype == table.dtype and tuple(out.shape) == (n, dim)
+    _check(lib().cvlc_embed(at, _DTYPES[table.dtype], vocab, dim, stride, _here(tokens, tokens.dtype, (n,)), _token_bytes(tokens), n, scale, o,
+                            out_stride, _here(status, torch.int32, (1,)), _stream_handle(stream)), "cvlc_embed")
+
+
+def cvlc_embed_grad_workspace_bytes(n: int, dim: int, vocab: int) -> int:
+    return int(lib().cvlc_embed_grad_workspace_bytes(int(n), int(dim), int(vocab)))
+
+
+def cvlc_embed_grad(tokens: torch.Tensor, grad: torch.Tensor, update: torch.Tensor, ws: torch.Tensor, scale: float = 1.0,
+                    accumulate: bool = False, stream: Optional[torch.cuda.Stream] = None) -> None:
+    """update[v] (fp32, vocab x dim) = (or += with accumulate) scale * the sum of grad[i] over the positions with tokens[i] = v."""
+    g, stride = _rows(grad)
+    u, update_stride = _rows(update)
+    n, (vocab, dim) = tokens.numel(), update.shape
+    assert update.dtype == torch.float32 and tuple(grad.shape) == (n, dim)
+    _check(lib().cvlc_embed_grad(_here(tokens, tokens.dtype, (n,)), _token_bytes(tokens), n, g, _DTYPES[grad.dtype], dim, stride, vocab, scale, u,
+                                 update_stride, 1 if accumulate else 0, _ptr(ws), _nbytes(ws), _stream_handle(stream)), "cvlc_embed_grad")
+
+
 def cvlc_read_status(plan_or_ws: torch.Tensor, stream: Optional[torch.cuda.Stream] = None) -> int:
     return int(lib().cvlc_read_status(_ptr(plan_or_ws), _stream_handle(stream)))
 
@@ -515,7 +655,8 @@ def cvlc_profile_reset() -> None:
 
 KERNEL_NAMES = ["k_zero_words", "k_client", "k_hist", "k_plan_threshold", "k_plan_fit", "k_plan_tune", "k_encode_init", "k_select",
                 "k_select_lookback", "k_rank_split", "k_rank", "k_rank_rest", "k_sort", "k_pack", "k_decode_prepare", "k_fill_zero",
-                "k_prefetch_l2", "k_decode", "k_noalloc_publish_status", "k_selftest", "k_hist_check", "k_apply", "k_plan_literal", "k_ec_accumulate", "k_pack_unframed", "k_decode_unframed"]
+                "k_prefetch_l2", "k_decode", "k_noalloc_publish_status", "k_selftest", "k_hist_check", "k_apply", "k_plan_literal", "k_ec_accumulate", "k_pack_unframed", "k_decode_unframed",
+                "k_top_logits", "k_distill_loss", "k_distill_grad", "k_distill_step", "k_embed", "k_token_sort", "k_embed_sum", "k_embed_join"]
 
 
 def cvlc_profile_read(kernel_name: str = "*"):

@@ -8,7 +8,7 @@
 
 #include <mutex>
 
-#include "cvlc_common.cuh"
+#include "cvlc_vocab.cuh"
 
 using namespace cvlc;
 
@@ -150,6 +150,60 @@ size_t plan_ws_bytes_of(uint64_t d, uint32_t n) { return plan_ws_bytes(make_part
 bool pack_fits(const Shape& S) {
   return 4 * ((size_t)S.packet_bits / 8 + 16 + (S.quantizer == CVLC_QUANT_QSGD ? (size_t)S.cap[1] * 8 : 0)) <= kPackSharedMax;
 }
+
+size_t element_bytes(uint32_t dtype) { return dtype == CVLC_F32 ? 4 : dtype == CVLC_F16 || dtype == CVLC_BF16 ? 2 : 0; }
+
+// rows of logits: `rows` of `vocab` elements, `stride` apart; without rows nothing is behind any pointer
+bool logits_ok(const void* at, uint32_t dtype, uint64_t rows, uint32_t vocab, uint64_t stride, float temperature) {
+  const size_t size = element_bytes(dtype);
+  return size && (rows == 0 || aligned(at, size)) && rows <= (1ull << 27) && vocab >= 1 && vocab <= CVLC_MAX_VOCAB && stride >= vocab &&
+         stride <= (1ull << 32) && temperature > 0.f && temperature < INFINITY;
+}
+
+int distill_args(const cvlc_distill* a, DistillArgs* d) {
+  if (!a || !logits_ok(a->logits_dev, a->dtype, a->rows, a->vocab, a->row_stride, a->temperature)) return CVLC_ERR_INVALID_ARG;
+  if (a->k > CVLC_MAX_RECORDS || a->rest > CVLC_REST_BUCKET || (a->rows && a->k && (!aligned(a->ids_dev, 4) || !aligned(a->logp_dev, 4)))) return CVLC_ERR_INVALID_ARG;
+  if ((a->row_weight_dev && !aligned(a->row_weight_dev, 4)) || (a->status_dev && !aligned(a->status_dev, 4))) return CVLC_ERR_INVALID_ARG;
+  memset(d, 0, sizeof *d);
+  d->logits = a->logits_dev;
+  d->rows = a->rows;
+  d->row_stride = a->row_stride;
+  d->vocab = a->vocab;
+  d->k = a->k;
+  d->rest = a->rest;
+  d->temperature = a->temperature;
+  d->ids = a->ids_dev;
+  d->logp = a->logp_dev;
+  d->row_weight = a->row_weight_dev;
+  d->status = a->status_dev;
+  return CVLC_OK;
+}
+
+// the gradient's rows: in the logits' place, or nowhere near them
+int distill_grad_args(const cvlc_distill* a, void* grad, uint64_t stride, DistillArgs* d) {
+  const size_t size = element_bytes(a->dtype);
+  const uintptr_t z = reinterpret_cast<uintptr_t>(a->logits_dev), g = reinterpret_cast<uintptr_t>(grad);
+  if ((a->rows && !aligned(grad, size)) || stride < a->vocab || stride > (1ull << 32)) return CVLC_ERR_INVALID_ARG;
+  if (a->rows && !(g == z && stride == a->row_stride)) {
+    const uint64_t zn = ((a->rows - 1) * a->row_stride + a->vocab) * size, gn = ((a->rows - 1) * stride + a->vocab) * size;
+    if (g < z + zn && z < g + gn) return CVLC_ERR_INVALID_ARG;
+  }
+  d->grad = grad;
+  d->grad_stride = stride;
+  return CVLC_OK;
+}
+
+int run_distill(const cvlc_distill* a, const DistillArgs& d, DistillKind kind, void* cuda_stream) {
+  if (a->rows == 0) return CVLC_OK;
+  return launch_distill(d, a->dtype, kind, static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess ? CVLC_OK : CVLC_ERR_CUDA;
+}
+
+// tokens, and the shape of the table's rows
+bool embed_ok(uint32_t dtype, uint64_t vocab, uint32_t dim, const void* tokens, uint32_t token_bytes, uint64_t n) {
+  return element_bytes(dtype) && vocab >= 1 && vocab < (1ull << 31) && dim >= 1 && dim <= (1u << 20) && (token_bytes == 4 || token_bytes == 8) &&
+         n < (1ull << 31) && (n == 0 || aligned(tokens, token_bytes));
+}
+bool rows_ok(const void* at, size_t size, uint32_t dim, uint64_t stride) { return aligned(at, size) && stride >= dim && stride <= (1ull << 32); }
 
 }  // namespace
 
@@ -597,6 +651,73 @@ int cvlc_decode_apply(const uint8_t* const* streams_dev, const uint64_t* stream_
   return launch_apply(model_dev, aggregate_dev, d, ws_dev, static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess
              ? CVLC_OK
              : CVLC_ERR_CUDA;
+}
+
+int cvlc_top_logits(const void* logits_dev, uint32_t dtype, uint64_t rows, uint32_t vocab, uint64_t row_stride, uint32_t k,
+                    float temperature, int32_t* ids_dev, float* logp_dev, void* cuda_stream) {
+  if (!logits_ok(logits_dev, dtype, rows, vocab, row_stride, temperature) || k < 1 || k > CVLC_MAX_TOP || k > vocab) return CVLC_ERR_INVALID_ARG;
+  if (rows == 0) return CVLC_OK;
+  if (!aligned(ids_dev, 4) || !aligned(logp_dev, 4)) return CVLC_ERR_INVALID_ARG;
+  const TopArgs a = {logits_dev, rows, row_stride, vocab, k, temperature, ids_dev, logp_dev};
+  return launch_top_logits(a, dtype, static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess ? CVLC_OK : CVLC_ERR_CUDA;
+}
+
+int cvlc_distill_loss(const cvlc_distill* a, float* loss_dev, float* stats_dev, void* cuda_stream) {
+  DistillArgs d;
+  const int rc = distill_args(a, &d);
+  if (rc != CVLC_OK) return rc;
+  if (a->rows && (!aligned(loss_dev, 4) || (stats_dev && !aligned(stats_dev, 16)))) return CVLC_ERR_INVALID_ARG;
+  d.loss = loss_dev;
+  d.stats = stats_dev;
+  return run_distill(a, d, kDistillLoss, cuda_stream);
+}
+
+int cvlc_distill_grad(const cvlc_distill* a, const float* stats_dev, void* grad_dev, uint64_t grad_stride, void* cuda_stream) {
+  DistillArgs d;
+  int rc = distill_args(a, &d);
+  if (rc == CVLC_OK) rc = distill_grad_args(a, grad_dev, grad_stride, &d);
+  if (rc != CVLC_OK) return rc;
+  if (a->rows && !aligned(stats_dev, 16)) return CVLC_ERR_INVALID_ARG;
+  d.stats = const_cast<float*>(stats_dev);
+  return run_distill(a, d, kDistillGrad, cuda_stream);
+}
+
+int cvlc_distill_step(const cvlc_distill* a, float* loss_dev, void* grad_dev, uint64_t grad_stride, void* cuda_stream) {
+  DistillArgs d;
+  int rc = distill_args(a, &d);
+  if (rc == CVLC_OK) rc = distill_grad_args(a, grad_dev, grad_stride, &d);
+  if (rc != CVLC_OK) return rc;
+  if (a->rows && !aligned(loss_dev, 4)) return CVLC_ERR_INVALID_ARG;
+  d.loss = loss_dev;
+  return run_distill(a, d, kDistillStep, cuda_stream);
+}
+
+int cvlc_embed(const void* table_dev, uint32_t dtype, uint64_t vocab, uint32_t dim, uint64_t table_stride, const void* tokens_dev,
+               uint32_t token_bytes, uint64_t n, float scale, void* out_dev, uint64_t out_stride, int32_t* status_dev, void* cuda_stream) {
+  if (!embed_ok(dtype, vocab, dim, tokens_dev, token_bytes, n)) return CVLC_ERR_INVALID_ARG;
+  const size_t size = element_bytes(dtype);
+  if (!rows_ok(table_dev, size, dim, table_stride) || (n && !rows_ok(out_dev, size, dim, out_stride)) || (status_dev && !aligned(status_dev, 4)))
+    return CVLC_ERR_INVALID_ARG;
+  if (n == 0) return CVLC_OK;
+  const EmbedArgs a = {table_dev, vocab, table_stride, n, out_stride, dim, token_bytes, tokens_dev, scale, out_dev, status_dev};
+  return launch_embed(a, dtype, static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess ? CVLC_OK : CVLC_ERR_CUDA;
+}
+
+size_t cvlc_embed_grad_workspace_bytes(uint64_t n, uint32_t dim, uint64_t vocab) {
+  if (vocab < 1 || vocab >= (1ull << 31) || dim < 1 || dim > (1u << 20) || n >= (1ull << 31)) return 0;
+  return embed_grad_ws_bytes(n, dim);
+}
+
+int cvlc_embed_grad(const void* tokens_dev, uint32_t token_bytes, uint64_t n, const void* grad_dev, uint32_t dtype, uint32_t dim,
+                    uint64_t grad_stride, uint64_t vocab, float scale, float* update_dev, uint64_t update_stride, int accumulate,
+                    void* ws_dev, size_t ws_bytes, void* cuda_stream) {
+  if (!embed_ok(dtype, vocab, dim, tokens_dev, token_bytes, n)) return CVLC_ERR_INVALID_ARG;
+  if ((n && !rows_ok(grad_dev, element_bytes(dtype), dim, grad_stride)) || !rows_ok(update_dev, 4, dim, update_stride) ||
+      (accumulate != 0 && accumulate != 1) || !aligned(ws_dev, 256))
+    return CVLC_ERR_INVALID_ARG;
+  if (ws_bytes < embed_grad_ws_bytes(n, dim)) return CVLC_ERR_WORKSPACE_TOO_SMALL;
+  const EmbedGradArgs a = {tokens_dev, grad_dev, vocab, n, grad_stride, update_stride, dim, token_bytes, scale, update_dev, accumulate, ws_dev};
+  return launch_embed_grad(a, dtype, static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess ? CVLC_OK : CVLC_ERR_CUDA;
 }
 
 int cvlc_read_status(const void* plan_or_ws_dev, void* cuda_stream) {

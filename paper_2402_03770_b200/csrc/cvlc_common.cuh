@@ -367,7 +367,8 @@ CVLC_HD constexpr size_t dec_ws_bytes(uint32_t n) { return align256(dec_off_meta
 enum KernelId {
   kKZeroWords = 0, kKClient, kKHist, kKPlanThreshold, kKPlanFit, kKPlanTune, kKEncodeInit, kKSelect, kKSelectLookback, kKRankSplit, kKRank,
   kKRankRest, kKSort, kKPack, kKDecodePrepare, kKFillZero, kKPrefetchL2, kKDecode, kKNoallocStatus, kKSelftest, kKHistCheck, kKApply,
-  kKPlanLiteral, kKEcAccumulate, kKPackUnframed, kKDecodeUnframed, kNumKernelIds
+  kKPlanLiteral, kKEcAccumulate, kKPackUnframed, kKDecodeUnframed, kKTopLogits, kKDistillLoss,
+  kKDistillGrad, kKDistillStep, kKEmbed, kKTokenSort, kKEmbedSum, kKEmbedJoin, kNumKernelIds
 };
 
 // Called around every kernel launch.  Counts launches; when a kernel has been selected with

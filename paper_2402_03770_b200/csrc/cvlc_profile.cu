@@ -10,7 +10,8 @@ namespace {
 const char* const kKernelNames[kNumKernelIds] = {
     "k_zero_words", "k_client", "k_hist", "k_plan_threshold", "k_plan_fit", "k_plan_tune", "k_encode_init", "k_select", "k_select_lookback", "k_rank_split",
     "k_rank", "k_rank_rest", "k_sort", "k_pack", "k_decode_prepare", "k_fill_zero", "k_prefetch_l2", "k_decode", "k_noalloc_publish_status",
-    "k_selftest", "k_hist_check", "k_apply", "k_plan_literal", "k_ec_accumulate", "k_pack_unframed", "k_decode_unframed"};
+    "k_selftest", "k_hist_check", "k_apply", "k_plan_literal", "k_ec_accumulate", "k_pack_unframed", "k_decode_unframed",
+    "k_top_logits", "k_distill_loss", "k_distill_grad", "k_distill_step", "k_embed", "k_token_sort", "k_embed_sum", "k_embed_join"};
 
 std::atomic<unsigned long long> g_launches[kNumKernelIds];
 std::atomic<int> g_prof_kernel{-1};  // kernel id being timed; kNumKernelIds = every kernel; -1 = off

@@ -1,0 +1,118 @@
+"""Top logits, distillation and the embedding from their definitions, in 64 bits on the CPU, and what the kernels' 32-bit arithmetic may
+be off by."""
+import math
+
+import torch
+
+NONE, SCALED, BUCKET = 0, 1, 2
+U = 2.0 ** -24  # half a step of fp32, relative
+
+# ln of a row's sum of exponentials.  A term's exponent (z - m) log2(e) / temperature is off by three roundings (difference, constant,
+# product), U each, relative to it; a term of weight 2^-a counts a 2^-a times that, so what the row's terms can add up to is at
+# most their average exponent, below log2(vocab) <= 22: 22 * 3 * ln 2 = 46 U.  The exponential itself is off by 2^-22 = 4 U, the sum by one U
+# for every addition on the way: 8 of a vector, 8 vectors or the batches before, 5 of a warp, 15 warps, 7 blocks, twice that
+# where sums of two maxima are joined: 80 U.  The gradient of a row of more than 262,144 words adds its further batches.
+LN = 150 * U
+
+
+def half_step(dtype):
+    return torch.finfo(dtype).eps / 2
+
+
+def tiny(dtype):
+    """half the distance of the smallest numbers, or what 2^x flushes to zero"""
+    return max(torch.finfo(dtype).smallest_normal * torch.finfo(dtype).eps / 2, 2.0 ** -126)
+
+
+def from_largest(z):
+    """z less its row's largest value, so that lowest values of a type keep their differences (an empty row: as it is)"""
+    m = z.amax(-1, keepdim=True)
+    return z - torch.where(m > -math.inf, m, 0.0)
+
+
+def top(logits, k, temperature):
+    z = logits.double().cpu()
+    order = torch.sort(z + 0.0, dim=1, descending=True, stable=True)
+    v, ids = order.values[:, :k], order.indices[:, :k].to(torch.int32)
+    x = from_largest(z) / temperature
+    logp = x.gather(1, ids.long()) - torch.logsumexp(x, dim=1, keepdim=True)
+    gone = v == -math.inf
+    ids = torch.where(gone, -1, ids)
+    logp = torch.where(gone, -math.inf, logp)
+    spoiled = ~(z < math.inf).all(dim=1, keepdim=True)
+    ids = torch.where(spoiled, torch.arange(k, dtype=torch.int32), ids)
+    logp = torch.where(spoiled, math.nan, logp)
+    logp = logp.float().double()  # what is below fp32's range is -inf
+    return ids, logp, torch.where(gone, 0.0, LN + logp.abs() * 2 * U)
+
+
+def distill(logits, ids, logp, rest, temperature, weight=None):
+    """loss, gradient, and how far each may be off before it is rounded to the logits' type"""
+    z, ids, lp = logits.double().cpu(), ids.cpu().long(), logp.double().cpu()
+    rows, vocab = z.shape
+    loss, tol_loss = torch.zeros(rows, dtype=torch.float64), torch.zeros(rows, dtype=torch.float64)
+    grad, tol_grad = torch.zeros_like(z), torch.zeros_like(z)
+    for r in range(rows):
+        w = 1.0 if weight is None else float(weight[r])
+        if w == 0.0 or not bool((z[r] > -math.inf).any() | torch.isnan(z[r]).any()):
+            continue
+        x = from_largest(z[r]) / temperature
+        lq = x - torch.logsumexp(x, 0)
+        q = lq.exp()
+        p = torch.zeros(vocab, dtype=torch.float64)
+        named = torch.zeros(vocab, dtype=torch.bool)
+        for i, l in zip(ids[r].tolist(), lp[r].tolist()):
+            if 0 <= i < vocab:
+                p[i] += math.exp(l)
+                named[i] = True
+        mass, left = p.sum(), 0.0
+        if rest == SCALED:
+            if mass == 0:
+                continue
+            p, mass = p / mass, torch.ones((), dtype=torch.float64)
+        on = p > 0
+        L = (p[on] * (p[on].log() - lq[on])).sum()
+        far = (x.max() - x).clamp(max=200.0) * 1.4427 * 3 * U + 8 * U  # of exp((z - reference) / temperature)
+        pull = q * 0.0
+        if rest == BUCKET and bool((z[r][~named] > -math.inf).any()):
+            left = max(0.0, 1.0 - float(mass))
+            lqr = torch.logsumexp(lq[~named], 0)
+            if left > 0:
+                L = L + left * (math.log(left) - lqr)
+            pull = torch.where(named, 0.0, left * (lq - lqr).exp())
+        b = mass + left
+        loss[r], grad[r] = w * L, (b * q - pull - p) * w / temperature
+        tol_loss[r] = abs(w) * (LN * (float(mass) + 2 * left) + 4 * U * abs(L))
+        tol_grad[r] = abs(w) / temperature * ((b * q + pull) * (LN + far + 8 * U) + p * 4 * U)
+    return loss, grad, tol_loss, tol_grad
+
+
+def assert_near(got, want, tol, dtype=torch.float32, what=""):
+    """equal where the definition is not finite; else within tol, rounded to dtype"""
+    got, want = got.double().cpu(), want.double()
+    assert got.shape == want.shape
+    odd = ~torch.isfinite(want)
+    assert torch.equal(torch.isnan(got[odd]), torch.isnan(want[odd])), what
+    inf = torch.isinf(want)
+    assert torch.equal(got[inf], want[inf]), what
+    off = (got - want).abs()[~odd]
+    tol = torch.as_tensor(tol).expand(want.shape)[~odd]
+    most = tol * (1 + half_step(dtype)) + want[~odd].abs() * half_step(dtype) + tiny(dtype)
+    bad = ~(off <= most)
+    assert not bad.any(), (what, int(bad.sum()), float((off / most).max()))
+
+
+def embed_grad(tokens, grad, vocab, scale, update=None):
+    """the table's gradient, and how far fp32 sums of the same terms may be off"""
+    t, g = tokens.cpu().long(), grad.double().cpu()
+    keep = (t >= 0) & (t < vocab)
+    out = torch.zeros(vocab, g.shape[1], dtype=torch.float64)
+    out.index_add_(0, t[keep], g[keep])
+    size = torch.zeros_like(out).index_add_(0, t[keep], g[keep].abs())
+    count = torch.bincount(t[keep], minlength=vocab).double()[:, None]
+    tol = abs(scale) * size * (count + 2) * U
+    out = out * scale
+    if update is not None:
+        out = out + update.double().cpu()
+        tol = torch.where(count > 0, tol + out.abs() * 2 * U, 0.0)
+    return out, tol
