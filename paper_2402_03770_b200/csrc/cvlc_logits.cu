@@ -82,10 +82,47 @@ __device__ __forceinline__ MaxSum join(const MaxSum& a, const MaxSum& b, float c
   const float m = fmaxf(a.max, b.max), ref = finite_ref(m);
   return {m, a.sum * exp2_fast((a.max - ref) * c2) + b.sum * exp2_fast((b.max - ref) * c2)};
 }
-__device__ __forceinline__ MaxSum warp_join(MaxSum a, float c2) {
+// over the lanes of a warp: the maximum first, then every sum is moved to it once
+__device__ __forceinline__ MaxSum warp_join(const MaxSum& a, float c2) {
+  float m = a.max;
 #pragma unroll
-  for (int o = 16; o; o >>= 1) a = join(a, {__shfl_xor_sync(kFull, a.max, o), __shfl_xor_sync(kFull, a.sum, o)}, c2);
-  return a;
+  for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(kFull, m, o));
+  float s = a.sum * exp2_fast((a.max - finite_ref(m)) * c2);
+#pragma unroll
+  for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(kFull, s, o);
+  return {m, s};
+}
+template <class V>
+__device__ __forceinline__ V warp_sum(V v) {
+#pragma unroll
+  for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(kFull, v, o);
+  return v;
+}
+// over what the first `n` lanes read from an array of the warps
+__device__ __forceinline__ MaxSum join_warps(const MaxSum* of_warp, uint32_t n, float c2) {
+  const uint32_t lane = threadIdx.x & 31;
+  return warp_join(lane < n ? of_warp[lane] : MaxSum{-CUDART_INF_F, 0.f}, c2);
+}
+
+// floats in the order of unsigned numbers, zeros of either sign alike
+__device__ __forceinline__ uint32_t order_of(float v) {
+  const uint32_t b = __float_as_uint(v + 0.f);
+  return b & 0x80000000u ? ~b : b | 0x80000000u;
+}
+__device__ __forceinline__ float value_of(uint32_t o) { return __uint_as_float(o & 0x80000000u ? o & 0x7FFFFFFFu : ~o); }
+constexpr uint32_t kOrderNegInf = 0x007FFFFFu;  // order_of(-inf)
+
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }
+
+// the block's vectors from `base` on, NV of a thread
+template <class T, int NV>
+__device__ __forceinline__ void load_batch(const Row<T>& R, uint32_t share, uint32_t base, uint4 (&raw)[NV]) {
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    const uint32_t i = base + threadIdx.x + j * blockDim.x;
+    raw[j] = R.load(i < share ? R.vec(i) : R.vecs);
+  }
 }
 
 // The differences z - max are taken before the scaling by log2(e) / temperature: with rows masked by the type's lowest value, or far
@@ -124,37 +161,10 @@ __device__ __forceinline__ void add_batch(const uint4 (&raw)[NV], float c2, MaxS
 // A block marks the listed words of its share in a bitmap in shared memory, where a second record of a word is noticed too.
 // The teacher's sums are a few numbers a row and are held in 64 bits: what a list leaves over is often a small difference from one.
 
-struct Said {  // listed words: their exponentials, and the sums of p, p ln p and p (z - all.max)
-  MaxSum all;
-  double mass, ent, cross;
-};
-// what p (z - a) has to gain to be p (z - b), a at most b; a = -inf: it is -inf already, or there is no mass
-__device__ __forceinline__ double moved(double mass, float a, float b) {
-  return a == -CUDART_INF_F || a == b ? 0.0 : mass * ((double)a - (double)b);
-}
-__device__ __forceinline__ Said join(const Said& a, const Said& b, float c2) {
-  const MaxSum all = join(a.all, b.all, c2);
-  return {all, a.mass + b.mass, a.ent + b.ent, (a.cross + moved(a.mass, a.all.max, all.max)) + (b.cross + moved(b.mass, b.all.max, all.max))};
-}
-__device__ __forceinline__ Said warp_join(Said a, float c2) {
-#pragma unroll
-  for (int o = 16; o; o >>= 1) {
-    const Said b = {{__shfl_xor_sync(kFull, a.all.max, o), __shfl_xor_sync(kFull, a.all.sum, o)},
-                    __shfl_xor_sync(kFull, a.mass, o), __shfl_xor_sync(kFull, a.ent, o), __shfl_xor_sync(kFull, a.cross, o)};
-    a = join(a, b, c2);
-  }
-  return a;
-}
-// one listed word of probability p with ln p, and its logit
-__device__ __forceinline__ Said said_of(double p, double ln_p, float z) {
-  const bool masked = z == -CUDART_INF_F;
-  return {{z, masked ? 0.f : 1.f}, p, p != 0.0 ? p * ln_p : 0.0, masked && p != 0.0 ? -p * CUDART_INF : 0.0};
-}
 struct Part {  // a block's share of a row
-  MaxSum rest;  // unlisted words
-  Said said;
+  MaxSum rest, said;        // unlisted and listed words
+  double mass, ent, cross;  // listed words: the sums of p, p ln p and p (z - said.max)
 };
-__device__ __forceinline__ Part join(const Part& a, const Part& b, float c2) { return {join(a.rest, b.rest, c2), join(a.said, b.said, c2)}; }
 struct Whole {  // what the row's gradient needs; kept for it between loss and gradient
   float ref, a;         // unlisted words: a exp((z - ref) it)
   float max, inv_sum;   // q = exp((z - max) it) inv_sum
@@ -162,39 +172,57 @@ struct Whole {  // what the row's gradient needs; kept for it between loss and g
 };
 static_assert(sizeof(Whole) <= 4 * CVLC_DISTILL_STATS, "a row's place in the buffer");
 
-__device__ __forceinline__ Whole whole_row(const Part* parts, uint32_t blocks, uint32_t rest, float temperature, float c2, double* loss) {
-  Part p = parts[0];
-  for (uint32_t r = 1; r < blocks; ++r) p = join(p, parts[r], c2);
-  const MaxSum un = p.rest;
-  const double mass = p.said.mass;
-  const MaxSum all = join(un, p.said.all, c2);
-  if (all.max == -CUDART_INF_F && all.sum == 0.f) {  // every word is masked: no distribution, no loss
-    *loss = 0.0;
-    return {0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+struct Sums {  // a row's parts joined
+  MaxSum rest, said, all;
+  double mass, left;  // left: what the bucket holds
+  bool empty;         // every word is masked: no distribution
+};
+__device__ __forceinline__ Sums sums_of(const Part* parts, uint32_t blocks, uint32_t rest, float c2) {
+  Sums s = {parts[0].rest, parts[0].said, {}, parts[0].mass, 0.0, false};
+  for (uint32_t r = 1; r < blocks; ++r) {
+    s.rest = join(s.rest, parts[r].rest, c2);
+    s.said = join(s.said, parts[r].said, c2);
+    s.mass += parts[r].mass;
   }
-  const double it = 1.0 / (double)temperature;
-  const double ln_sum = log((double)all.sum), cross = p.said.cross + moved(mass, p.said.all.max, all.max);
+  s.all = join(s.rest, s.said, c2);
+  s.empty = s.all.max == -CUDART_INF_F && s.all.sum == 0.f;
+  // without a word that it could stand for there is no bucket
+  const bool some = !(s.rest.max == -CUDART_INF_F && s.rest.sum == 0.f);
+  s.left = rest == CVLC_REST_BUCKET && some && s.mass < 1.0 ? 1.0 - s.mass : 0.0;
+  return s;
+}
+__device__ __forceinline__ Whole whole_row(const Sums& s, uint32_t rest, float c2) {
+  if (s.empty) return {0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
   Whole w;
-  w.max = all.max;
-  w.inv_sum = 1.f / all.sum;
-  double b = mass, c = 1.0, left = 0.0;
-  *loss = p.said.ent - cross * it + mass * ln_sum;
+  w.max = s.all.max;
+  w.inv_sum = 1.f / s.all.sum;
+  w.b = (float)(s.mass + s.left);
+  w.c = 1.f;
   if (rest == CVLC_REST_SCALED) {
-    b = mass > 0.0 ? 1.0 : mass;  // (a NaN stays one)
-    c = mass > 0.0 ? 1.0 / mass : mass;
-    *loss = mass > 0.0 ? *loss * c - log(mass) : mass;
+    w.b = s.mass > 0.0 ? 1.f : (float)s.mass;  // (a NaN stays one)
+    w.c = s.mass > 0.0 ? (float)(1.0 / s.mass) : (float)s.mass;
   }
-  const bool some = !(un.max == -CUDART_INF_F && un.sum == 0.f);  // else the list holds every word that the student may say
-  if (rest == CVLC_REST_BUCKET && some) {
-    left = mass < 1.0 ? 1.0 - mass : 0.0;
-    b = mass + left;
-    if (left > 0.0) *loss += left * (log(left) - (((double)un.max - (double)all.max) * it + log((double)un.sum) - ln_sum));
-  }
-  w.b = (float)b;
-  w.c = (float)c;
-  w.ref = some ? un.max : 0.f;
-  w.a = some ? (float)(b * (double)(exp2_fast((un.max - all.max) * c2) * w.inv_sum) - (left > 0.0 ? left / (double)un.sum : 0.0)) : 0.f;
+  const bool some = !(s.rest.max == -CUDART_INF_F && s.rest.sum == 0.f);
+  w.ref = some ? s.rest.max : 0.f;
+  w.a = some ? w.b * (exp2_fast((s.rest.max - s.all.max) * c2) * w.inv_sum) - (float)s.left / s.rest.sum : 0.f;
   return w;
+}
+// what p (z - a) has to gain to be p (z - b), a at most b; a = -inf: it is -inf already, or there is no mass
+__device__ __forceinline__ double moved(double mass, float a, float b) {
+  return a == -CUDART_INF_F || a == b ? 0.0 : mass * ((double)a - (double)b);
+}
+__device__ double loss_of(const Sums& s, const Part* parts, uint32_t blocks, uint32_t rest, float temperature) {
+  if (s.empty) return 0.0;
+  double ent = 0.0, cross = 0.0;
+  for (uint32_t r = 0; r < blocks; ++r) {
+    ent += parts[r].ent;
+    cross += parts[r].cross + moved(parts[r].mass, parts[r].said.max, s.all.max);
+  }
+  const double it = 1.0 / (double)temperature, ln_sum = log((double)s.all.sum);
+  double loss = ent - cross * it + s.mass * ln_sum;
+  if (rest == CVLC_REST_SCALED) loss = s.mass > 0.0 ? loss / s.mass - log(s.mass) : s.mass;
+  if (s.left > 0.0) loss += s.left * (log(s.left) - (((double)s.rest.max - (double)s.all.max) * it + log((double)s.rest.sum) - ln_sum));
+  return loss;
 }
 
 // bits of the listed words of the block's vector i
@@ -203,18 +231,21 @@ __device__ __forceinline__ uint32_t listed_of(const uint8_t* marks, uint32_t i) 
   return kPerVec<T> == 8 ? marks[i] : (marks[i >> 1] >> ((i & 1) * 4)) & 15u;
 }
 
+// The loss goes through its share a batch ahead (2 x NV vectors of a thread in registers); the step keeps its batch for the gradient, and
+// reads again what lies behind the first batch, if the row is longer than its cluster keeps.
 template <class T, int NV, DistillKind KIND>
 __global__ void __launch_bounds__(kRowThreads, 2) k_distill(DistillArgs a, uint32_t log_blocks, uint32_t share_most) {
   extern __shared__ __align__(16) unsigned char dyn[];
   __shared__ Part parts[kMaxClusterBlocks];
-  __shared__ Part of_warp[kRowThreads / 32];
-  __shared__ Whole whole;
-  const uint32_t nt = blockDim.x, tid = threadIdx.x, blocks = 1u << log_blocks;
+  __shared__ MaxSum of_warp[kRowThreads / 32];
+  __shared__ Part said_of_warp[kRowThreads / 32];
+  __shared__ uint32_t said_top;
+  const uint32_t nt = blockDim.x, tid = threadIdx.x, blocks = 1u << log_blocks, lane = tid & 31, warp = tid >> 5;
   const uint32_t rank = blockIdx.x & (blocks - 1);
   const uint64_t row = blockIdx.x >> log_blocks;
   const Row<T> R(a.logits, row, a.row_stride, a.vocab, log_blocks, rank);
   const float weight = a.row_weight ? a.row_weight[row] : 1.f;
-  const float c2 = (float)((double)1.4426950408889634074 / (double)a.temperature);
+  const float c2 = a.c2;
   const uint32_t share = R.share();
 
   uint8_t* const marks = dyn;
@@ -227,17 +258,11 @@ __global__ void __launch_bounds__(kRowThreads, 2) k_distill(DistillArgs a, uint3
   const bool idle = weight == 0.f && !(KIND == kDistillLoss && a.stats);
 
   uint4 raw[NV];
+  if (!idle) load_batch<T, NV>(R, share, 0, raw);
+  if (KIND != kDistillGrad && blocks > 1) cluster_arrive();  // waited for before another block's shared memory is written
   if (!idle) {
-#pragma unroll
-    for (int j = 0; j < NV; ++j) {
-      const uint32_t i = tid + j * nt;
-      raw[j] = R.load(i < share ? R.vec(i) : R.vecs);
-    }
-  }
-  cg::cluster_group cluster = cg::this_cluster();
-  if (KIND != kDistillGrad && blocks > 1) cluster.sync();  // the other blocks have begun: their shared memory may be written
-  if (!idle) {
-    for (uint32_t i = tid; i < mark_bytes / 4; i += nt) reinterpret_cast<uint32_t*>(marks)[i] = 0;
+    for (uint32_t i = tid; i < mark_bytes / 16; i += nt) reinterpret_cast<uint4*>(marks)[i] = make_uint4(0, 0, 0, 0);
+    if (tid == 0) said_top = 0;
     __syncthreads();
     bool twice = false;
     for (uint32_t i = tid; i < a.k; i += nt) {
@@ -249,13 +274,16 @@ __global__ void __launch_bounds__(kRowThreads, 2) k_distill(DistillArgs a, uint3
         logit[i] = to_float(R.at[id]);
         const uint32_t bit = 1u << (p & 31);
         twice |= (atomicOr(reinterpret_cast<uint32_t*>(marks) + (p >> 5), bit) & bit) != 0;
+        if (KIND != kDistillGrad) atomicMax(&said_top, order_of(logit[i]));
       }
       at[i] = p;
       prob[i] = a.logp[row * a.k + i];
     }
     twice = __syncthreads_or(twice);
     // p of every word, summed in the order of its records
-    Part mine = {{-CUDART_INF_F, 0.f}, {{-CUDART_INF_F, 0.f}, 0.0, 0.0, 0.0}};
+    const float top = said_top ? value_of(said_top) : -CUDART_INF_F;
+    float sum = 0.f;
+    double mass = 0.0, ent = 0.0, cross = 0.0;
     for (uint32_t i = tid; i < a.k; i += nt) {
       double p = -1.0;
       if (at[i] >= 0) {
@@ -270,66 +298,99 @@ __global__ void __launch_bounds__(kRowThreads, 2) k_distill(DistillArgs a, uint3
             for (uint32_t o = i + 1; o < a.k; ++o)
               if (at[o] == here) p += exp((double)a.logp[row * a.k + o]), merged = true;
         }
-        if (KIND != kDistillGrad && !(p < 0.0)) mine.said = join(mine.said, said_of(p, merged ? log(p) : lp, logit[i]), c2);
+        if (KIND != kDistillGrad && !(p < 0.0)) {
+          mass += p;
+          if (p != 0.0) {
+            ent += p * (merged ? log(p) : lp);
+            cross += p * ((double)logit[i] - (double)finite_ref(top));
+          }
+          sum += exp2_fast((logit[i] - finite_ref(top)) * c2);
+        }
       }
       prob[i] = (float)p;  // only this thread reads its own
     }
-    if (KIND == kDistillGrad) {
-      if (tid == 0) whole = *reinterpret_cast<const Whole*>(a.stats + row * CVLC_DISTILL_STATS);
-    } else {
-      for (uint32_t base = 0; base < share; base += NV * nt) {
-        if (base) {
-#pragma unroll
-          for (int j = 0; j < NV; ++j) {
-            const uint32_t i = base + tid + j * nt;
-            raw[j] = R.load(i < share ? R.vec(i) : R.vecs);
-          }
-        }
+    if (KIND != kDistillGrad) {
+      if (warp * 32 < a.k) {
+        sum = warp_sum(sum), mass = warp_sum(mass), ent = warp_sum(ent), cross = warp_sum(cross);
+        if (lane == 0) said_of_warp[warp] = {{}, {top, sum}, mass, ent, cross};
+      }
+      MaxSum mine = {-CUDART_INF_F, 0.f};
+      for (uint32_t base = 0;;) {
+        const uint32_t next = base + NV * nt;
+        uint4 ahead[NV];
+        if (KIND == kDistillLoss && next < share) load_batch<T, NV>(R, share, next, ahead);
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
           const uint32_t i = base + tid + j * nt;
           if (i < share)
             if (const uint32_t bits = listed_of<T>(marks, i)) drop_elements<T>(raw[j], bits);
         }
-        add_batch<T, NV>(raw, c2, mine.rest);
+        add_batch<T, NV>(raw, c2, mine);
+        if (next >= share) break;
+        base = next;
+        if (KIND == kDistillLoss) {
+#pragma unroll
+          for (int j = 0; j < NV; ++j) raw[j] = ahead[j];
+        } else {
+          load_batch<T, NV>(R, share, base, raw);
+        }
       }
-      mine.rest = warp_join(mine.rest, c2);
-      mine.said = warp_join(mine.said, c2);
-      if ((tid & 31) == 0) of_warp[tid >> 5] = mine;
+      mine = warp_join(mine, c2);
+      if (lane == 0) of_warp[warp] = mine;
       __syncthreads();
-      if (tid < blocks) {  // thread r hands the block's sums to block r
-        Part p = of_warp[0];
-        for (uint32_t w = 1; w < nt / 32; ++w) p = join(p, of_warp[w], c2);
-        *(blocks > 1 ? cluster.map_shared_rank(&parts[rank], tid) : &parts[rank]) = p;
+      if (warp == 0) {
+        Part p = {join_warps(of_warp, nt / 32, c2), {top, 0.f}, 0.0, 0.0, 0.0};
+        const uint32_t with = min(nt / 32, (a.k + 31) / 32);  // warps that had records
+        for (uint32_t w = 0; w < with; ++w) {
+          p.said.sum += said_of_warp[w].said.sum;
+          p.mass += said_of_warp[w].mass, p.ent += said_of_warp[w].ent, p.cross += said_of_warp[w].cross;
+        }
+        if (blocks == 1) {
+          if (lane == 0) parts[0] = p;
+        } else {
+          cluster_wait();
+          if (lane < blocks) *cg::this_cluster().map_shared_rank(&parts[rank], lane) = p;
+        }
+      } else if (blocks > 1) {
+        cluster_wait();
       }
     }
+  } else if (KIND != kDistillGrad && blocks > 1) {
+    cluster_wait();
   }
-  if (KIND != kDistillGrad && blocks > 1) cluster.sync();
-  if (KIND != kDistillGrad && tid == 0) {
-    double loss = 0.0;
-    if (!idle) whole = whole_row(parts, blocks, a.rest, a.temperature, c2, &loss);
-    if (rank == 0) {
-      a.loss[row] = weight == 0.f ? 0.f : (float)((double)weight * loss);
-      if (KIND == kDistillLoss && a.stats) *reinterpret_cast<Whole*>(a.stats + row * CVLC_DISTILL_STATS) = whole;
+  if (KIND != kDistillGrad) {
+    if (blocks > 1) {
+      cluster_arrive();
+      cluster_wait();
+    } else {
+      __syncthreads();
     }
   }
-  if (KIND == kDistillLoss) return;
-  __syncthreads();
+  Whole w = {};
+  if (KIND == kDistillGrad) {
+    if (!idle) w = *reinterpret_cast<const Whole*>(a.stats + row * CVLC_DISTILL_STATS);
+  } else if (KIND == kDistillLoss) {
+    if (tid == 0 && rank == 0) {
+      double loss = 0.0;
+      if (!idle) {
+        const Sums s = sums_of(parts, blocks, a.rest, c2);
+        loss = loss_of(s, parts, blocks, a.rest, a.temperature);
+        if (a.stats) *reinterpret_cast<Whole*>(a.stats + row * CVLC_DISTILL_STATS) = whole_row(s, a.rest, c2);
+      }
+      a.loss[row] = weight == 0.f ? 0.f : (float)((double)weight * loss);
+    }
+    return;
+  } else if (!idle) {
+    w = whole_row(sums_of(parts, blocks, a.rest, c2), a.rest, c2);
+  }
 
   // the gradient, a vector at a time; where logits and gradient lie differently against 16 bytes, by elements
   T* const g = static_cast<T*>(a.grad) + row * a.grad_stride;
   const bool alike = ((reinterpret_cast<uintptr_t>(g) ^ reinterpret_cast<uintptr_t>(R.at)) & 15) == 0;
-  const Whole w = idle ? Whole{} : whole;
   const float scale = idle ? 0.f : weight / a.temperature;
   const float ca = w.a * scale;
   for (uint32_t base = 0; base < share; base += NV * nt) {
-    if (!idle && share > NV * nt) {
-#pragma unroll
-      for (int j = 0; j < NV; ++j) {
-        const uint32_t i = base + tid + j * nt;
-        raw[j] = R.load(i < share ? R.vec(i) : R.vecs);
-      }
-    }
+    if (!idle && (KIND == kDistillGrad ? base > 0 : share > NV * nt)) load_batch<T, NV>(R, share, base, raw);
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
       const uint32_t i = base + tid + j * nt;
@@ -347,7 +408,7 @@ __global__ void __launch_bounds__(kRowThreads, 2) k_distill(DistillArgs a, uint3
       }
       const int word = R.word(v);
       if (alike && R.whole(v)) {
-        *reinterpret_cast<uint4*>(g + word) = narrow<T>(f);
+        __stcs(reinterpret_cast<uint4*>(g + word), narrow<T>(f));
       } else {
 #pragma unroll
         for (int e = 0; e < kPerVec<T>; ++e)
@@ -355,14 +416,20 @@ __global__ void __launch_bounds__(kRowThreads, 2) k_distill(DistillArgs a, uint3
       }
     }
   }
-  if (idle) return;
-  __syncthreads();  // the listed words' gradients replace what the vectors hold in their places
-  const float cb = w.b * scale, cc = w.c * scale;
-  for (uint32_t i = tid; i < a.k; i += nt)
-    if (at[i] >= 0 && !(prob[i] < 0.f)) {
-      const float q = exp2_fast((logit[i] - w.max) * c2) * w.inv_sum;
-      g[a.ids[row * a.k + i]] = from_float<T>(cb * q - cc * prob[i]);
-    }
+  if (!idle) {
+    __syncthreads();  // the listed words' gradients replace what the vectors hold in their places
+    const float cb = w.b * scale, cc = w.c * scale;
+    for (uint32_t i = tid; i < a.k; i += nt)
+      if (at[i] >= 0 && !(prob[i] < 0.f)) {
+        const float q = exp2_fast((logit[i] - w.max) * c2) * w.inv_sum;
+        g[a.ids[row * a.k + i]] = from_float<T>(cb * q - cc * prob[i]);
+      }
+  }
+  // the loss last: its logarithms take as long as a store
+  if (KIND == kDistillStep && rank == 0 && tid == nt - 1) {
+    const double loss = idle ? 0.0 : loss_of(sums_of(parts, blocks, a.rest, c2), parts, blocks, a.rest, a.temperature);
+    a.loss[row] = weight == 0.f ? 0.f : (float)((double)weight * loss);
+  }
 }
 
 // how a call's rows are cut: blocks of a cluster for each, threads of a block
@@ -370,14 +437,19 @@ struct Cut {
   uint32_t log_blocks, threads, share;  // share: most vectors of a block
 };
 
-Cut cut_rows(uint64_t rows, uint32_t vocab, uint32_t per_vec, uint32_t nv) {
-  const uint32_t vecs = vocab / per_vec + 2, tiles = (vecs + 31) / 32;
+// `keep`: most vectors a thread keeps, where the second half works from them (0: it does not).  Blocks of a cluster: as many as keep the row,
+// and, where rows are few, as many as give every SM two blocks.
+Cut cut_rows(const void* logits, uint64_t stride, uint64_t rows, uint32_t vocab, uint32_t size, uint32_t nv, uint32_t keep) {
+  const uint32_t per_vec = 16 / size;
+  const bool even = (reinterpret_cast<uintptr_t>(logits) & 15) == 0 && stride * size % 16 == 0;  // every row begins with a vector
+  const uint32_t vecs = (vocab + per_vec - 1) / per_vec + (even ? 0 : 1), tiles = (vecs + 31) / 32;
   Cut c = {0, 0, 0};
-  while (c.log_blocks < 3 && ((tiles + (1u << c.log_blocks) - 1) >> c.log_blocks) * 32 > nv * kRowThreads) ++c.log_blocks;
+  const auto share = [&] { return ((tiles + (1u << c.log_blocks) - 1) >> c.log_blocks) * 32; };
+  if (keep)
+    while (c.log_blocks < 3 && share() > keep * kRowThreads) ++c.log_blocks;
   while (c.log_blocks < 3 && (rows << c.log_blocks) < 2 * kNumSM && (vecs >> c.log_blocks) >= 512) ++c.log_blocks;
-  c.share = ((tiles + (1u << c.log_blocks) - 1) >> c.log_blocks) * 32;
-  uint32_t t = (c.share + nv - 1) / nv;
-  t = (t + 31) & ~31u;
+  c.share = share();
+  uint32_t t = ((c.share + nv - 1) / nv + 31) & ~31u;
   c.threads = t < 64 ? 64 : (t > kRowThreads ? kRowThreads : t);
   return c;
 }
@@ -407,12 +479,15 @@ cudaError_t launch_rows(int id, void (*kernel)(Params...), uint64_t rows, const 
 
 template <class T, DistillKind KIND>
 cudaError_t distill_typed(const DistillArgs& a, cudaStream_t st) {
-  constexpr int NV = 8;
-  const Cut c = cut_rows(a.rows, a.vocab, kPerVec<T>, NV);
+  constexpr int NV = KIND == kDistillStep ? 8 : 4;
+  const Cut c = cut_rows(a.logits, a.row_stride, a.rows, a.vocab, sizeof(T), NV, KIND == kDistillStep ? NV : 0);
   const size_t smem = ((c.share * kPerVec<T> / 8 + 15) & ~15u) + (size_t)a.k * 12;
   return launch_rows(KIND == kDistillLoss ? kKDistillLoss : KIND == kDistillGrad ? kKDistillGrad : kKDistillStep, k_distill<T, NV, KIND>, a.rows, c,
                      KIND != kDistillGrad, smem, st, a, c.log_blocks, c.share);
 }
+// log2(e) / temperature, rounded once
+float scale_of(float temperature) { return (float)(1.4426950408889634074 / (double)temperature); }
+
 template <class T>
 cudaError_t distill_kind(const DistillArgs& a, DistillKind kind, cudaStream_t st) {
   switch (kind) {
@@ -425,20 +500,15 @@ cudaError_t distill_kind(const DistillArgs& a, DistillKind kind, cudaStream_t st
 // ---- top logits --------------------------------------------------------------------------------
 //
 // The k largest logits of a row, in order, equal ones by ascending word; each with its log-probability.  Of the elements
-// a thread has loaded, only the largest is looked at first: with `blocks` blocks a row, the ceil(k / blocks)-th largest of a block's
-// thread maxima has that many elements at or above it, so the smallest of the blocks' bounds has at least k in the row, and
-// hardly more (a thread rarely holds two).  What lies at or above it goes to the first block and is ranked there by (value, word).
-// Rows with more such elements than the lists hold (whole rows of equal logits) are selected digit by digit instead.
+// a thread has loaded, only the largest is looked at first: the k-th largest of the block's thread maxima has at least k elements at or above
+// it, and hardly more (a thread rarely holds two).  One block per row goes through it batch by batch, raises that bound as it goes
+// (after 1, 2, 4, .. batches and the last) and lists what reaches it: about 3 k elements, of which the last bound leaves little more
+// than k.  Those are ranked by (value, word).  Several blocks per row (few rows): the smallest of their bounds for k / blocks each
+// serves all of them, and they list from what they have kept.  Rows with more elements at the bound than the lists hold (whole rows
+// of equal logits) are selected digit by digit instead.
 
 constexpr uint32_t kTopList = 2048;  // candidates of a row
 
-// floats in the order of unsigned numbers, zeros of either sign alike
-__device__ __forceinline__ uint32_t order_of(float v) {
-  const uint32_t b = __float_as_uint(v + 0.f);
-  return b & 0x80000000u ? ~b : b | 0x80000000u;
-}
-__device__ __forceinline__ float value_of(uint32_t o) { return __uint_as_float(o & 0x80000000u ? o & 0x7FFFFFFFu : ~o); }
-constexpr uint32_t kOrderNegInf = 0x007FFFFFu;  // order_of(-inf); what is not above it is never listed
 __device__ __forceinline__ unsigned long long candidate(uint32_t order, uint32_t word) {
   return ((unsigned long long)order << 32) | (uint32_t)~word;
 }
@@ -448,114 +518,119 @@ struct TopPart {
   uint32_t bound;
 };
 
+// The largest bound from `lo` on that `want` of the block's threads reach with theirs (`lo` if it is none, or finer than 2^12 apart)
+__device__ __forceinline__ uint32_t raise_bound(uint32_t top, uint32_t want, uint32_t lo, uint32_t* largest) {
+  const uint32_t of_warp = __reduce_max_sync(kFull, top);
+  if ((threadIdx.x & 31) == 0) atomicMax(largest, of_warp);
+  uint32_t n = __syncthreads_count(top >= lo);
+  if (n < want) return lo;
+  uint32_t hi = *largest;
+  __syncthreads();  // all have read it: the next call adds to it
+  while (hi > lo && hi - lo > 4096) {
+    const uint32_t mid = lo + (hi - lo) / 2;
+    n = __syncthreads_count(top >= mid);
+    if (n >= want) lo = mid;
+    else hi = mid - 1;
+    if (n == want) break;
+  }
+  return lo;
+}
+
+// Elements from `least` on (a candidate: value and word) of a batch, into a list of `room`
+template <class T, int NV>
+__device__ __forceinline__ void list_batch(const Row<T>& R, const uint4 (&raw)[NV], uint32_t base, unsigned long long least, uint32_t* count,
+                                           unsigned long long* to, uint32_t room) {
+  const float floor_value = value_of((uint32_t)(least >> 32));
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    if (!(vec_max<T>(raw[j]) >= floor_value)) continue;
+    float f[kPerVec<T>];
+    widen<T>(raw[j], f);
+    const int word = R.word(R.vec(base + threadIdx.x + j * blockDim.x));
+#pragma unroll
+    for (int e = 0; e < kPerVec<T>; ++e) {
+      if (!(f[e] >= floor_value)) continue;
+      const unsigned long long c = candidate(order_of(f[e]), (uint32_t)(word + e));
+      if (c < least) continue;
+      const uint32_t n = atomicAdd(count, 1u);
+      if (n < room) to[n] = c;
+    }
+  }
+}
+
 template <class T, int NV>
 __global__ void __launch_bounds__(kRowThreads, 2) k_top_logits(TopArgs a, uint32_t log_blocks) {
-  __shared__ unsigned long long list[kTopList];    // in the first block: a stretch for every block
-  __shared__ unsigned long long packed[kTopList];  // the same without gaps
+  __shared__ __align__(16) unsigned long long list[kTopList];    // in the first block: a stretch for every block
+  __shared__ __align__(16) unsigned long long packed[kTopList];  // the same without gaps
   __shared__ TopPart parts[kMaxClusterBlocks];
   __shared__ MaxSum of_warp[kRowThreads / 32];
   __shared__ uint32_t counts[kMaxClusterBlocks];
   __shared__ uint32_t hist[256];
-  __shared__ uint32_t mine, picked, above;
-  __shared__ MaxSum of_block;
-  const uint32_t nt = blockDim.x, tid = threadIdx.x, blocks = 1u << log_blocks;
+  __shared__ uint32_t mine, picked, above, largest, kept;
+  const uint32_t nt = blockDim.x, tid = threadIdx.x, blocks = 1u << log_blocks, lane = tid & 31, warp_id = tid >> 5;
   const uint32_t rank = blockIdx.x & (blocks - 1);
   const uint64_t row = blockIdx.x >> log_blocks;
   const Row<T> R(a.logits, row, a.row_stride, a.vocab, log_blocks, rank);
-  const float c2 = (float)((double)1.4426950408889634074 / (double)a.temperature);
-  const uint32_t share = R.share();
+  const float c2 = a.c2;
+  const uint32_t share = R.share(), step = NV * nt, batches = (share + step - 1) / step;
+  const uint32_t stretch = kTopList >> log_blocks;
   cg::cluster_group cluster = cg::this_cluster();
 
   uint4 raw[NV];
-#pragma unroll
-  for (int j = 0; j < NV; ++j) {
-    const uint32_t i = tid + j * nt;
-    raw[j] = R.load(i < share ? R.vec(i) : R.vecs);
-  }
-  if (tid == 0) mine = 0;
-  if (blocks > 1) cluster.sync();
+  load_batch<T, NV>(R, share, 0, raw);
+  if (blocks > 1) cluster_arrive();  // waited for before another block's shared memory is written
+  if (tid == 0) mine = largest = kept = 0;
+  __syncthreads();
 
   MaxSum acc = {-CUDART_INF_F, 0.f};
-  for (uint32_t base = 0; base < share; base += NV * nt) {
-    if (base) {
-#pragma unroll
-      for (int j = 0; j < NV; ++j) {
-        const uint32_t i = base + tid + j * nt;
-        raw[j] = R.load(i < share ? R.vec(i) : R.vecs);
-      }
-    }
-    add_batch<T, NV>(raw, c2, acc);
-  }
-  const uint32_t top = order_of(acc.max);
-  const MaxSum warp = warp_join(acc, c2);
-  if ((tid & 31) == 0) of_warp[tid >> 5] = warp;
-  __syncthreads();
-  if (tid == 0) {
-    MaxSum s = of_warp[0];
-    for (uint32_t w = 1; w < nt / 32; ++w) s = join(s, of_warp[w], c2);
-    of_block = s;
-  }
-  __syncthreads();
-  // the largest bound that `want` threads reach, by halving
+  uint32_t bound = kOrderNegInf + 1;
   const uint32_t want = (a.k + blocks - 1) >> log_blocks;
-  uint32_t lo = kOrderNegInf + 1, hi = order_of(of_block.max);
-  if ((uint32_t)__syncthreads_count(top >= lo) < want) hi = lo;
-  while (lo < hi) {
-    const uint32_t mid = lo + (hi - lo + 1) / 2;
-    if ((uint32_t)__syncthreads_count(top >= mid) >= want) lo = mid;
-    else hi = mid - 1;
+  for (uint32_t b = 0;;) {
+    uint4 ahead[NV];
+    if (b + 1 < batches) load_batch<T, NV>(R, share, (b + 1) * step, ahead);
+    add_batch<T, NV>(raw, c2, acc);
+    if (b + 1 == batches || (blocks == 1 && (b & (b + 1)) == 0)) bound = raise_bound(order_of(acc.max), want, bound, &largest);
+    if (blocks == 1) list_batch<T, NV>(R, raw, b * step, (unsigned long long)bound << 32, &mine, list, stretch);
+    if (++b >= batches) break;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) raw[j] = ahead[j];
   }
-  if (tid < blocks) *(blocks > 1 ? cluster.map_shared_rank(&parts[rank], tid) : &parts[rank]) = {of_block, lo};
-  if (blocks > 1) cluster.sync();
-  else __syncthreads();
-  uint32_t bound = parts[0].bound;
-  MaxSum all = parts[0].all;
-  for (uint32_t r = 1; r < blocks; ++r) {
-    bound = min(bound, parts[r].bound);
-    all = join(all, parts[r].all, c2);
-  }
-  const bool spoiled = !(all.sum < CUDART_INF_F);  // a NaN or +inf among the logits: there is no softmax
-  const uint32_t stretch = kTopList >> log_blocks;
-
-  // elements from `least` on (a candidate: value and word) into the first block's list
-  auto gather = [&](unsigned long long least) {
+  const MaxSum warp = warp_join(acc, c2);
+  if (lane == 0) of_warp[warp_id] = warp;
+  __syncthreads();
+  MaxSum all = join_warps(of_warp, nt / 32, c2);
+  auto relist = [&](unsigned long long least) {  // several blocks, or a second time
     unsigned long long* const to = (blocks > 1 ? cluster.map_shared_rank(list, 0) : list) + rank * stretch;
-    const float floor_value = value_of((uint32_t)(least >> 32));
-    for (uint32_t base = 0; base < share; base += NV * nt) {
-      if (share > NV * nt) {
-#pragma unroll
-        for (int j = 0; j < NV; ++j) {
-          const uint32_t i = base + tid + j * nt;
-          raw[j] = R.load(i < share ? R.vec(i) : R.vecs);
-        }
-      }
-#pragma unroll
-      for (int j = 0; j < NV; ++j) {
-        if (!(vec_max<T>(raw[j]) >= floor_value)) continue;
-        const uint32_t i = base + tid + j * nt;
-        float f[kPerVec<T>];
-        widen<T>(raw[j], f);
-        const int word = R.word(R.vec(i));
-#pragma unroll
-        for (int e = 0; e < kPerVec<T>; ++e) {
-          const unsigned long long c = candidate(order_of(f[e]), (uint32_t)(word + e));
-          if (f[e] >= floor_value && c >= least) {
-            const uint32_t n = atomicAdd(&mine, 1u);
-            if (n < stretch) to[n] = c;
-          }
-        }
-      }
+    for (uint32_t b = 0; b < batches; ++b) {
+      if (batches > 1) load_batch<T, NV>(R, share, b * step, raw);
+      list_batch<T, NV>(R, raw, b * step, least, &mine, to, stretch);
     }
     __syncthreads();
     if (tid < blocks) *(blocks > 1 ? cluster.map_shared_rank(&counts[rank], tid) : &counts[rank]) = mine;
     if (blocks > 1) cluster.sync();
     else __syncthreads();
   };
-  bool overflow = false;
-  if (!spoiled) {
-    gather((unsigned long long)bound << 32);
-    for (uint32_t r = 0; r < blocks; ++r) overflow |= counts[r] > stretch;
+  bool spoiled;  // a NaN or +inf among the logits: there is no softmax
+  if (blocks == 1) {
+    spoiled = !(all.sum < CUDART_INF_F);
+    if (tid == 0) counts[0] = mine;
+    __syncthreads();
+  } else {
+    cluster_wait();
+    if (tid < blocks) *cluster.map_shared_rank(&parts[rank], tid) = {all, bound};
+    cluster.sync();
+    bound = parts[0].bound;
+    all = parts[0].all;
+    for (uint32_t r = 1; r < blocks; ++r) {
+      bound = min(bound, parts[r].bound);
+      all = join(all, parts[r].all, c2);
+    }
+    spoiled = !(all.sum < CUDART_INF_F);
+    if (!spoiled) relist((unsigned long long)bound << 32);
   }
+  bool overflow = false;
+  if (!spoiled)
+    for (uint32_t r = 0; r < blocks; ++r) overflow |= counts[r] > stretch;
   if (overflow) {
     // the k-th largest candidate, eight bits at a time
     unsigned long long prefix = 0;
@@ -564,19 +639,13 @@ __global__ void __launch_bounds__(kRowThreads, 2) k_top_logits(TopArgs a, uint32
       for (uint32_t i = tid; i < 256; i += nt) hist[i] = 0;
       __syncthreads();
       uint32_t last = 0, run = 0;  // equal digits in a row are counted at once
-      for (uint32_t base = 0; base < share; base += NV * nt) {
-        if (share > NV * nt) {
-#pragma unroll
-          for (int j = 0; j < NV; ++j) {
-            const uint32_t i = base + tid + j * nt;
-            raw[j] = R.load(i < share ? R.vec(i) : R.vecs);
-          }
-        }
+      for (uint32_t b = 0; b < batches; ++b) {
+        if (batches > 1) load_batch<T, NV>(R, share, b * step, raw);
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
           float f[kPerVec<T>];
           widen<T>(raw[j], f);
-          const int word = R.word(R.vec(base + tid + j * nt));
+          const int word = R.word(R.vec(b * step + tid + j * nt));
 #pragma unroll
           for (int e = 0; e < kPerVec<T>; ++e) {
             if (!(f[e] > -CUDART_INF_F)) continue;
@@ -624,7 +693,8 @@ __global__ void __launch_bounds__(kRowThreads, 2) k_top_logits(TopArgs a, uint32
     }
     if (tid == 0) mine = 0;
     __syncthreads();
-    gather(prefix);
+    relist(prefix);
+    bound = (uint32_t)(prefix >> 32);
   }
 
   if (rank != 0) return;
@@ -635,22 +705,45 @@ __global__ void __launch_bounds__(kRowThreads, 2) k_top_logits(TopArgs a, uint32
     }
     return;
   }
-  uint32_t n = 0;
+  // what the last bound leaves, in any order
   for (uint32_t r = 0; r < blocks; ++r) {
     const uint32_t c = counts[r];
-    for (uint32_t i = tid; i < c; i += nt) packed[n + i] = list[r * stretch + i];
-    n += c;
+    for (uint32_t i = tid; i < c; i += nt) {
+      const unsigned long long v = list[r * stretch + i];
+      if ((uint32_t)(v >> 32) >= bound) packed[atomicAdd(&kept, 1u)] = v;
+    }
   }
   __syncthreads();
+  const uint32_t n = kept;
   const double it = 1.0 / (double)a.temperature, ln_sum = log((double)all.sum);
-  for (uint32_t i = tid; i < n; i += nt) {
-    const unsigned long long c = packed[i];
-    uint32_t larger = 0;
-    for (uint32_t o = 0; o < n; ++o) larger += packed[o] > c;
-    if (larger < a.k) {
-      a.ids[row * a.k + larger] = (int32_t)~(uint32_t)c;
-      a.logp[row * a.k + larger] = (float)(((double)value_of((uint32_t)(c >> 32)) - (double)all.max) * it - ln_sum);
+  auto put = [&](uint32_t at, unsigned long long c) {
+    a.ids[row * a.k + at] = (int32_t)~(uint32_t)c;
+    a.logp[row * a.k + at] = (float)(((double)value_of((uint32_t)(c >> 32)) - (double)all.max) * it - ln_sum);
+  };
+  if (n <= nt) {  // one for each thread: its rank is the number of larger ones
+    const unsigned long long c = tid < n ? packed[tid] : 0;
+    uint32_t larger = 0, o = 0;
+    for (; o + 2 <= n; o += 2) {
+      const ulonglong2 p = *reinterpret_cast<const ulonglong2*>(packed + o);
+      larger += (p.x > c) + (p.y > c);
     }
+    if (o < n) larger += packed[o] > c;
+    if (tid < n && larger < a.k) put(larger, c);
+  } else {  // sorted in pairs, the largest first
+    uint32_t size = 2;
+    while (size < n) size *= 2;
+    for (uint32_t i = n + tid; i < size; i += nt) packed[i] = 0;
+    __syncthreads();
+    for (uint32_t length = 2; length <= size; length *= 2)
+      for (uint32_t apart = length / 2; apart; apart /= 2) {
+        for (uint32_t i = tid; i < size / 2; i += nt) {
+          const uint32_t x = i / apart * 2 * apart + i % apart, y = x + apart;
+          const unsigned long long p = packed[x], q = packed[y];
+          if ((p < q) == ((x & length) == 0)) packed[x] = q, packed[y] = p;
+        }
+        __syncthreads();
+      }
+    for (uint32_t i = tid; i < a.k && i < n; i += nt) put(i, packed[i]);
   }
   for (uint32_t i = n + tid; i < a.k; i += nt) {  // fewer words than records: the others are masked
     a.ids[row * a.k + i] = -1;
@@ -660,20 +753,26 @@ __global__ void __launch_bounds__(kRowThreads, 2) k_top_logits(TopArgs a, uint32
 
 template <class T>
 cudaError_t top_typed(const TopArgs& a, cudaStream_t st) {
-  constexpr int NV = 8;
-  const Cut c = cut_rows(a.rows, a.vocab, kPerVec<T>, NV);
+  constexpr int NV = 4;
+  Cut c = cut_rows(a.logits, a.row_stride, a.rows, a.vocab, sizeof(T), NV, 0);
+  // the bound is the better the more threads the row's elements are spread over
+  while (c.threads < kRowThreads && c.threads < 2 * (a.k >> c.log_blocks) && c.threads < c.share) c.threads += 32;
   return launch_rows(kKTopLogits, k_top_logits<T, NV>, a.rows, c, true, 0, st, a, c.log_blocks);
 }
 
 }  // namespace
 
-cudaError_t launch_top_logits(const TopArgs& a, uint32_t dtype, cudaStream_t st) {
+cudaError_t launch_top_logits(const TopArgs& args, uint32_t dtype, cudaStream_t st) {
+  TopArgs a = args;
+  a.c2 = scale_of(a.temperature);
   if (dtype == CVLC_F32) return top_typed<float>(a, st);
   if (dtype == CVLC_F16) return top_typed<__half>(a, st);
   return top_typed<__nv_bfloat16>(a, st);
 }
 
-cudaError_t launch_distill(const DistillArgs& a, uint32_t dtype, DistillKind kind, cudaStream_t st) {
+cudaError_t launch_distill(const DistillArgs& args, uint32_t dtype, DistillKind kind, cudaStream_t st) {
+  DistillArgs a = args;
+  a.c2 = scale_of(a.temperature);
   if (dtype == CVLC_F32) return distill_kind<float>(a, kind, st);
   if (dtype == CVLC_F16) return distill_kind<__half>(a, kind, st);
   return distill_kind<__nv_bfloat16>(a, kind, st);

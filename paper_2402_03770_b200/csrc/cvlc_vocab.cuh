@@ -23,6 +23,7 @@ struct TopArgs {
   float temperature;
   int32_t* ids;
   float* logp;
+  float c2;  // log2(e) / temperature
 };
 cudaError_t launch_top_logits(const TopArgs& a, uint32_t dtype, cudaStream_t st);
 
@@ -38,6 +39,7 @@ struct DistillArgs {
   float* loss;              // the loss and the step write it
   float* stats;             // the loss writes it (or nullptr), the gradient reads it
   void* grad;               // the gradient and the step write it
+  float c2;                 // log2(e) / temperature
 };
 enum DistillKind { kDistillLoss, kDistillGrad, kDistillStep };
 cudaError_t launch_distill(const DistillArgs& a, uint32_t dtype, DistillKind kind, cudaStream_t st);
