@@ -16,28 +16,33 @@ constexpr int kRowThreads = 512;  // most threads of a block
 
 // ---- a row, cut into vectors and dealt to the blocks of a cluster --------------------------
 // Vectors are aligned to 16 bytes in memory, so a row's first and last one may hold elements of other rows or none at all: those
-// two are loaded and stored by elements.  Tiles of 32 vectors (a warp's load) go to the blocks in turn.  Vocabularies are often
-// sorted by frequency: contiguous shares would leave the large logits to one block.
+// two are loaded and stored by elements.  Tiles of 32 vectors (a warp's load) go to the warps of the cluster's blocks in turn, the blocks
+// first: vocabularies are often sorted by frequency, and contiguous shares would leave the large logits to one block.  A thread's
+// i-th vector is then vector first + i * apart of the row.
 template <class T>
 struct Row {
-  const T* at;        // element 0
-  uint32_t lead;      // elements of vector 0 that lie before it
+  const T* at;                 // word 0
+  const uint4* from;           // vector 0
+  uint32_t lead;               // elements of vector 0 that lie before word 0
   uint32_t vocab, vecs;
   uint32_t log_blocks, rank;
+  uint32_t first, apart;       // of the thread
+  uint32_t whole_from, wholes; // vectors whose elements are all the row's
 
   __device__ __forceinline__ Row(const void* logits, uint64_t row, uint64_t stride, uint32_t vocab_, uint32_t log_blocks_, uint32_t rank_)
       : at(static_cast<const T*>(logits) + row * stride), vocab(vocab_), log_blocks(log_blocks_), rank(rank_) {
     lead = (uint32_t)((reinterpret_cast<uintptr_t>(at) & 15) / sizeof(T));
+    from = reinterpret_cast<const uint4*>(reinterpret_cast<uintptr_t>(at) & ~(uintptr_t)15);
     vecs = (lead + vocab + kPerVec<T> - 1) / kPerVec<T>;
+    whole_from = lead ? 1 : 0;
+    const uint32_t whole_to = (lead + vocab) / kPerVec<T>;
+    wholes = whole_to > whole_from ? whole_to - whole_from : 0;
+    first = ((((threadIdx.x >> 5) << log_blocks) | rank) << 5) | (threadIdx.x & 31);
+    apart = ((blockDim.x >> 5) << log_blocks) << 5;
   }
-  // vectors of this block, in whole tiles
-  __device__ __forceinline__ uint32_t share() const {
-    const uint32_t tiles = (vecs + 31) >> 5, blocks = 1u << log_blocks;
-    return ((tiles + blocks - 1 - rank) >> log_blocks) << 5;
-  }
-  // the block's i-th vector among the row's
-  __device__ __forceinline__ uint32_t vec(uint32_t i) const { return ((((i >> 5) << log_blocks) | rank) << 5) | (i & 31); }
-  // where this block has word j: the place among its elements, or -1
+  // vectors that a thread of this block has at most
+  __device__ __forceinline__ uint32_t rounds() const { return (vecs + apart - 1) / apart; }
+  // where this block has word j: thread + block size * round, in elements, or -1
   __device__ __forceinline__ int place(uint32_t j) const {
     const uint32_t e = j + lead, v = e / kPerVec<T>, tile = v >> 5;
     if ((tile & ((1u << log_blocks) - 1)) != rank) return -1;
@@ -45,19 +50,46 @@ struct Row {
   }
   // first word of a vector; below zero in the row's first one
   __device__ __forceinline__ int word(uint32_t v) const { return (int)(v * kPerVec<T>) - (int)lead; }
-  __device__ __forceinline__ bool whole(uint32_t v) const {
+  __device__ __forceinline__ bool whole(uint32_t v) const { return v - whole_from < wholes; }
+  __device__ __forceinline__ bool ragged() const { return wholes != vecs; }
+  __device__ uint4 load_elements(uint32_t v) const {
     const int w = word(v);
-    return w >= 0 && w + kPerVec<T> <= (int)vocab;
-  }
-  __device__ __forceinline__ uint4 load(uint32_t v) const {
-    const int w = word(v);
-    if (whole(v)) return __ldcs(reinterpret_cast<const uint4*>(at + w));
     float f[kPerVec<T>];
 #pragma unroll
     for (int e = 0; e < kPerVec<T>; ++e) f[e] = (w + e >= 0 && w + e < (int)vocab) ? to_float(at[w + e]) : -CUDART_INF_F;
     return narrow<T>(f);
   }
 };
+
+// all elements minus infinity
+template <class T>
+__device__ __forceinline__ uint4 nothing() {
+  constexpr uint32_t w = sizeof(T) == 4 ? 0xFF800000u : std::is_same<T, __half>::value ? 0xFC00FC00u : 0xFF80FF80u;
+  return make_uint4(w, w, w, w);
+}
+
+// rounds `from` .. from + NV - 1 of the thread; what lies behind the row is minus infinity
+template <class T, int NV>
+__device__ __forceinline__ void load_batch(const Row<T>& R, uint32_t from, uint4 (&raw)[NV]) {
+  const uint32_t v0 = R.first + from * R.apart;
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    raw[j] = nothing<T>();
+    if (R.whole(v0 + j * R.apart)) raw[j] = __ldcs(R.from + v0 + j * R.apart);
+  }
+  if (R.ragged()) {  // the first and the last vector
+    const uint32_t last = R.vecs - 1;
+    const bool mine_first = !R.whole(0) && v0 == 0;
+    const bool mine_last = !R.whole(last) && last && last >= v0 && (last - v0) % R.apart == 0 && (last - v0) / R.apart < NV;
+    if (mine_first) raw[0] = R.load_elements(0);
+    if (mine_last) {
+      const uint4 r = R.load_elements(last);
+#pragma unroll
+      for (int j = 0; j < NV; ++j)
+        if (v0 + j * R.apart == last) raw[j] = r;
+    }
+  }
+}
 
 // largest element of a vector; NaN only where all are
 template <class T>
@@ -112,18 +144,13 @@ __device__ __forceinline__ uint32_t order_of(float v) {
 __device__ __forceinline__ float value_of(uint32_t o) { return __uint_as_float(o & 0x80000000u ? o & 0x7FFFFFFFu : ~o); }
 constexpr uint32_t kOrderNegInf = 0x007FFFFFu;  // order_of(-inf)
 
-__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release;" ::: "memory"); }
-__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }
-
-// the block's vectors from `base` on, NV of a thread
-template <class T, int NV>
-__device__ __forceinline__ void load_batch(const Row<T>& R, uint32_t share, uint32_t base, uint4 (&raw)[NV]) {
-#pragma unroll
-  for (int j = 0; j < NV; ++j) {
-    const uint32_t i = base + threadIdx.x + j * blockDim.x;
-    raw[j] = R.load(i < share ? R.vec(i) : R.vecs);
-  }
+// `publish`: what the thread has written is seen by who waits
+template <bool publish>
+__device__ __forceinline__ void cluster_arrive() {
+  if (publish) asm volatile("barrier.cluster.arrive.release;" ::: "memory");
+  else asm volatile("barrier.cluster.arrive.relaxed;" ::: "memory");
 }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }
 
 // The differences z - max are taken before the scaling by log2(e) / temperature: with rows masked by the type's lowest value, or far
 // from zero, the product alone would overflow or lose the difference.
@@ -133,17 +160,19 @@ __device__ __forceinline__ void add_batch(const uint4 (&raw)[NV], float c2, MaxS
 #pragma unroll
   for (int j = 0; j < NV; ++j) m = fmaxf(m, vec_max<T>(raw[j]));
   const float ref = finite_ref(m);
-  float sum = acc.sum * exp2_fast((acc.max - ref) * c2);
+  const float2 less = make_float2(-ref, -ref), by = make_float2(c2, c2);
+  float2 sum = make_float2(acc.sum * exp2_fast((acc.max - ref) * c2), 0.f);
 #pragma unroll
   for (int j = 0; j < NV; ++j) {
     float f[kPerVec<T>];
     widen<T>(raw[j], f);
-    float part = 0.f;
 #pragma unroll
-    for (int e = 0; e < kPerVec<T>; ++e) part += exp2_fast((f[e] - ref) * c2);
-    sum += part;
+    for (int e = 0; e < kPerVec<T>; e += 2) {
+      const float2 x = mul2(add2(make_float2(f[e], f[e + 1]), less), by);
+      sum = add2(sum, make_float2(exp2_fast(x.x), exp2_fast(x.y)));
+    }
   }
-  acc = {m, sum};
+  acc = {m, sum.x + sum.y};
 }
 
 // ---- distillation ---------------------------------------------------------------------------
@@ -234,22 +263,22 @@ __device__ __forceinline__ uint32_t listed_of(const uint8_t* marks, uint32_t i) 
 // The loss goes through its share a batch ahead (2 x NV vectors of a thread in registers); the step keeps its batch for the gradient, and
 // reads again what lies behind the first batch, if the row is longer than its cluster keeps.
 template <class T, int NV, DistillKind KIND>
-__global__ void __launch_bounds__(kRowThreads, 2) k_distill(DistillArgs a, uint32_t log_blocks, uint32_t share_most) {
+__global__ void __launch_bounds__(kRowThreads, 2) k_distill(DistillArgs a, uint32_t log_blocks, uint32_t mark_bytes) {
   extern __shared__ __align__(16) unsigned char dyn[];
   __shared__ Part parts[kMaxClusterBlocks];
   __shared__ MaxSum of_warp[kRowThreads / 32];
   __shared__ Part said_of_warp[kRowThreads / 32];
   __shared__ uint32_t said_top;
+  __shared__ Whole whole;
   const uint32_t nt = blockDim.x, tid = threadIdx.x, blocks = 1u << log_blocks, lane = tid & 31, warp = tid >> 5;
   const uint32_t rank = blockIdx.x & (blocks - 1);
   const uint64_t row = blockIdx.x >> log_blocks;
   const Row<T> R(a.logits, row, a.row_stride, a.vocab, log_blocks, rank);
   const float weight = a.row_weight ? a.row_weight[row] : 1.f;
   const float c2 = a.c2;
-  const uint32_t share = R.share();
+  const uint32_t rounds = R.rounds();
 
   uint8_t* const marks = dyn;
-  const uint32_t mark_bytes = (share_most * kPerVec<T> / 8 + 15) & ~15u;
   int* const at = reinterpret_cast<int*>(dyn + mark_bytes);  // places of the records in the block's share, or -1
   float* const prob = reinterpret_cast<float*>(at + a.k);    // their probabilities; -1: counted with an earlier record of the word
   float* const logit = prob + a.k;                           // the student's logits of their words
@@ -258,8 +287,8 @@ __global__ void __launch_bounds__(kRowThreads, 2) k_distill(DistillArgs a, uint3
   const bool idle = weight == 0.f && !(KIND == kDistillLoss && a.stats);
 
   uint4 raw[NV];
-  if (!idle) load_batch<T, NV>(R, share, 0, raw);
-  if (KIND != kDistillGrad && blocks > 1) cluster_arrive();  // waited for before another block's shared memory is written
+  if (!idle) load_batch<T, NV>(R, 0, raw);
+  if (KIND != kDistillGrad && blocks > 1) cluster_arrive<false>();  // waited for before another block's shared memory is written
   if (!idle) {
     for (uint32_t i = tid; i < mark_bytes / 16; i += nt) reinterpret_cast<uint4*>(marks)[i] = make_uint4(0, 0, 0, 0);
     if (tid == 0) said_top = 0;
@@ -315,24 +344,21 @@ __global__ void __launch_bounds__(kRowThreads, 2) k_distill(DistillArgs a, uint3
         if (lane == 0) said_of_warp[warp] = {{}, {top, sum}, mass, ent, cross};
       }
       MaxSum mine = {-CUDART_INF_F, 0.f};
-      for (uint32_t base = 0;;) {
-        const uint32_t next = base + NV * nt;
+      for (uint32_t from = 0;;) {
         uint4 ahead[NV];
-        if (KIND == kDistillLoss && next < share) load_batch<T, NV>(R, share, next, ahead);
+        if (KIND == kDistillLoss && from + NV < rounds) load_batch<T, NV>(R, from + NV, ahead);
 #pragma unroll
-        for (int j = 0; j < NV; ++j) {
-          const uint32_t i = base + tid + j * nt;
-          if (i < share)
-            if (const uint32_t bits = listed_of<T>(marks, i)) drop_elements<T>(raw[j], bits);
-        }
+        for (int j = 0; j < NV; ++j)
+          if (from + j < rounds)
+            if (const uint32_t bits = listed_of<T>(marks, tid + (from + j) * nt)) drop_elements<T>(raw[j], bits);
         add_batch<T, NV>(raw, c2, mine);
-        if (next >= share) break;
-        base = next;
+        from += NV;
+        if (from >= rounds) break;
         if (KIND == kDistillLoss) {
 #pragma unroll
           for (int j = 0; j < NV; ++j) raw[j] = ahead[j];
         } else {
-          load_batch<T, NV>(R, share, base, raw);
+          load_batch<T, NV>(R, from, raw);
         }
       }
       mine = warp_join(mine, c2);
@@ -350,21 +376,20 @@ __global__ void __launch_bounds__(kRowThreads, 2) k_distill(DistillArgs a, uint3
         } else {
           cluster_wait();
           if (lane < blocks) *cg::this_cluster().map_shared_rank(&parts[rank], lane) = p;
+          cluster_arrive<true>();
         }
       } else if (blocks > 1) {
         cluster_wait();
+        cluster_arrive<false>();
       }
     }
   } else if (KIND != kDistillGrad && blocks > 1) {
     cluster_wait();
+    cluster_arrive<false>();
   }
   if (KIND != kDistillGrad) {
-    if (blocks > 1) {
-      cluster_arrive();
-      cluster_wait();
-    } else {
-      __syncthreads();
-    }
+    if (blocks > 1) cluster_wait();
+    else __syncthreads();
   }
   Whole w = {};
   if (KIND == kDistillGrad) {
@@ -381,7 +406,12 @@ __global__ void __launch_bounds__(kRowThreads, 2) k_distill(DistillArgs a, uint3
     }
     return;
   } else if (!idle) {
-    w = whole_row(sums_of(parts, blocks, a.rest, c2), a.rest, c2);
+    if (warp == 0) {
+      const Whole mine = whole_row(sums_of(parts, blocks, a.rest, c2), a.rest, c2);
+      if (lane == 0) whole = mine;
+    }
+    __syncthreads();
+    w = whole;
   }
 
   // the gradient, a vector at a time; where logits and gradient lie differently against 16 bytes, by elements
@@ -389,30 +419,37 @@ __global__ void __launch_bounds__(kRowThreads, 2) k_distill(DistillArgs a, uint3
   const bool alike = ((reinterpret_cast<uintptr_t>(g) ^ reinterpret_cast<uintptr_t>(R.at)) & 15) == 0;
   const float scale = idle ? 0.f : weight / a.temperature;
   const float ca = w.a * scale;
-  for (uint32_t base = 0; base < share; base += NV * nt) {
-    if (!idle && (KIND == kDistillGrad ? base > 0 : share > NV * nt)) load_batch<T, NV>(R, share, base, raw);
+  for (uint32_t from = 0; from < rounds; from += NV) {
+    if (!idle && (KIND == kDistillGrad ? from > 0 : rounds > NV)) load_batch<T, NV>(R, from, raw);
+    const uint32_t v0 = R.first + from * R.apart;
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
-      const uint32_t i = base + tid + j * nt;
-      if (i >= share) continue;
-      const uint32_t v = R.vec(i);
-      if (v >= R.vecs) continue;
       float f[kPerVec<T>];
-      if (idle) {
+      widen<T>(raw[j], f);
 #pragma unroll
-        for (int e = 0; e < kPerVec<T>; ++e) f[e] = 0.f;
-      } else {
-        widen<T>(raw[j], f);
-#pragma unroll
-        for (int e = 0; e < kPerVec<T>; ++e) f[e] = ca * exp2_fast((f[e] - w.ref) * c2);
+      for (int e = 0; e < kPerVec<T>; e += 2) {
+        const float2 x = mul2(add2(make_float2(f[e], f[e + 1]), make_float2(-w.ref, -w.ref)), make_float2(c2, c2));
+        const float2 y = mul2(make_float2(exp2_fast(x.x), exp2_fast(x.y)), make_float2(ca, ca));
+        f[e] = y.x, f[e + 1] = y.y;
       }
-      const int word = R.word(v);
-      if (alike && R.whole(v)) {
-        __stcs(reinterpret_cast<uint4*>(g + word), narrow<T>(f));
-      } else {
+      raw[j] = idle ? make_uint4(0, 0, 0, 0) : narrow<T>(f);
+    }
+    uint4* const to = reinterpret_cast<uint4*>(g - R.lead);
+    if (alike) {
+#pragma unroll
+      for (int j = 0; j < NV; ++j)
+        if (R.whole(v0 + j * R.apart)) __stcs(to + v0 + j * R.apart, raw[j]);
+    }
+    if (!alike || R.ragged()) {
+#pragma unroll
+      for (int j = 0; j < NV; ++j) {
+        const uint32_t v = v0 + j * R.apart;
+        if (v >= R.vecs || (alike && R.whole(v))) continue;
+        const int word = R.word(v);
+        const T* const elements = reinterpret_cast<const T*>(&raw[j]);
 #pragma unroll
         for (int e = 0; e < kPerVec<T>; ++e)
-          if (word + e >= 0 && word + e < (int)R.vocab) g[word + e] = from_float<T>(f[e]);
+          if (word + e >= 0 && word + e < (int)R.vocab) g[word + e] = elements[e];
       }
     }
   }
@@ -434,7 +471,7 @@ __global__ void __launch_bounds__(kRowThreads, 2) k_distill(DistillArgs a, uint3
 
 // how a call's rows are cut: blocks of a cluster for each, threads of a block
 struct Cut {
-  uint32_t log_blocks, threads, share;  // share: most vectors of a block
+  uint32_t log_blocks, threads, rounds;  // rounds: vectors of a thread at most
 };
 
 // `keep`: most vectors a thread keeps, where the second half works from them (0: it does not).  Blocks of a cluster: as many as keep the row,
@@ -448,9 +485,9 @@ Cut cut_rows(const void* logits, uint64_t stride, uint64_t rows, uint32_t vocab,
   if (keep)
     while (c.log_blocks < 3 && share() > keep * kRowThreads) ++c.log_blocks;
   while (c.log_blocks < 3 && (rows << c.log_blocks) < 2 * kNumSM && (vecs >> c.log_blocks) >= 512) ++c.log_blocks;
-  c.share = share();
-  uint32_t t = ((c.share + nv - 1) / nv + 31) & ~31u;
+  const uint32_t t = ((share() + nv - 1) / nv + 31) & ~31u;
   c.threads = t < 64 ? 64 : (t > kRowThreads ? kRowThreads : t);
+  c.rounds = (share() + c.threads - 1) / c.threads;
   return c;
 }
 
@@ -481,9 +518,10 @@ template <class T, DistillKind KIND>
 cudaError_t distill_typed(const DistillArgs& a, cudaStream_t st) {
   constexpr int NV = KIND == kDistillStep ? 8 : 4;
   const Cut c = cut_rows(a.logits, a.row_stride, a.rows, a.vocab, sizeof(T), NV, KIND == kDistillStep ? NV : 0);
-  const size_t smem = ((c.share * kPerVec<T> / 8 + 15) & ~15u) + (size_t)a.k * 12;
+  const uint32_t mark_bytes = (c.rounds * c.threads * kPerVec<T> / 8 + 15) & ~15u;  // a bit for every element of a block
+  const size_t smem = mark_bytes + (size_t)a.k * 12;
   return launch_rows(KIND == kDistillLoss ? kKDistillLoss : KIND == kDistillGrad ? kKDistillGrad : kKDistillStep, k_distill<T, NV, KIND>, a.rows, c,
-                     KIND != kDistillGrad, smem, st, a, c.log_blocks, c.share);
+                     KIND != kDistillGrad, smem, st, a, c.log_blocks, mark_bytes);
 }
 // log2(e) / temperature, rounded once
 float scale_of(float temperature) { return (float)(1.4426950408889634074 / (double)temperature); }
@@ -538,7 +576,7 @@ __device__ __forceinline__ uint32_t raise_bound(uint32_t top, uint32_t want, uin
 
 // Elements from `least` on (a candidate: value and word) of a batch, into a list of `room`
 template <class T, int NV>
-__device__ __forceinline__ void list_batch(const Row<T>& R, const uint4 (&raw)[NV], uint32_t base, unsigned long long least, uint32_t* count,
+__device__ __forceinline__ void list_batch(const Row<T>& R, const uint4 (&raw)[NV], uint32_t from, unsigned long long least, uint32_t* count,
                                            unsigned long long* to, uint32_t room) {
   const float floor_value = value_of((uint32_t)(least >> 32));
 #pragma unroll
@@ -546,7 +584,7 @@ __device__ __forceinline__ void list_batch(const Row<T>& R, const uint4 (&raw)[N
     if (!(vec_max<T>(raw[j]) >= floor_value)) continue;
     float f[kPerVec<T>];
     widen<T>(raw[j], f);
-    const int word = R.word(R.vec(base + threadIdx.x + j * blockDim.x));
+    const int word = R.word(R.first + (from + j) * R.apart);
 #pragma unroll
     for (int e = 0; e < kPerVec<T>; ++e) {
       if (!(f[e] >= floor_value)) continue;
@@ -572,13 +610,13 @@ __global__ void __launch_bounds__(kRowThreads, 2) k_top_logits(TopArgs a, uint32
   const uint64_t row = blockIdx.x >> log_blocks;
   const Row<T> R(a.logits, row, a.row_stride, a.vocab, log_blocks, rank);
   const float c2 = a.c2;
-  const uint32_t share = R.share(), step = NV * nt, batches = (share + step - 1) / step;
+  const uint32_t batches = (R.rounds() + NV - 1) / NV;
   const uint32_t stretch = kTopList >> log_blocks;
   cg::cluster_group cluster = cg::this_cluster();
 
   uint4 raw[NV];
-  load_batch<T, NV>(R, share, 0, raw);
-  if (blocks > 1) cluster_arrive();  // waited for before another block's shared memory is written
+  load_batch<T, NV>(R, 0, raw);
+  if (blocks > 1) cluster_arrive<false>();  // waited for before another block's shared memory is written
   if (tid == 0) mine = largest = kept = 0;
   __syncthreads();
 
@@ -587,10 +625,10 @@ __global__ void __launch_bounds__(kRowThreads, 2) k_top_logits(TopArgs a, uint32
   const uint32_t want = (a.k + blocks - 1) >> log_blocks;
   for (uint32_t b = 0;;) {
     uint4 ahead[NV];
-    if (b + 1 < batches) load_batch<T, NV>(R, share, (b + 1) * step, ahead);
+    if (b + 1 < batches) load_batch<T, NV>(R, (b + 1) * NV, ahead);
     add_batch<T, NV>(raw, c2, acc);
     if (b + 1 == batches || (blocks == 1 && (b & (b + 1)) == 0)) bound = raise_bound(order_of(acc.max), want, bound, &largest);
-    if (blocks == 1) list_batch<T, NV>(R, raw, b * step, (unsigned long long)bound << 32, &mine, list, stretch);
+    if (blocks == 1) list_batch<T, NV>(R, raw, b * NV, (unsigned long long)bound << 32, &mine, list, stretch);
     if (++b >= batches) break;
 #pragma unroll
     for (int j = 0; j < NV; ++j) raw[j] = ahead[j];
@@ -602,8 +640,8 @@ __global__ void __launch_bounds__(kRowThreads, 2) k_top_logits(TopArgs a, uint32
   auto relist = [&](unsigned long long least) {  // several blocks, or a second time
     unsigned long long* const to = (blocks > 1 ? cluster.map_shared_rank(list, 0) : list) + rank * stretch;
     for (uint32_t b = 0; b < batches; ++b) {
-      if (batches > 1) load_batch<T, NV>(R, share, b * step, raw);
-      list_batch<T, NV>(R, raw, b * step, least, &mine, to, stretch);
+      if (batches > 1) load_batch<T, NV>(R, b * NV, raw);
+      list_batch<T, NV>(R, raw, b * NV, least, &mine, to, stretch);
     }
     __syncthreads();
     if (tid < blocks) *(blocks > 1 ? cluster.map_shared_rank(&counts[rank], tid) : &counts[rank]) = mine;
@@ -640,12 +678,12 @@ __global__ void __launch_bounds__(kRowThreads, 2) k_top_logits(TopArgs a, uint32
       __syncthreads();
       uint32_t last = 0, run = 0;  // equal digits in a row are counted at once
       for (uint32_t b = 0; b < batches; ++b) {
-        if (batches > 1) load_batch<T, NV>(R, share, b * step, raw);
+        if (batches > 1) load_batch<T, NV>(R, b * NV, raw);
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
           float f[kPerVec<T>];
           widen<T>(raw[j], f);
-          const int word = R.word(R.vec(b * step + tid + j * nt));
+          const int word = R.word(R.first + (b * NV + j) * R.apart);
 #pragma unroll
           for (int e = 0; e < kPerVec<T>; ++e) {
             if (!(f[e] > -CUDART_INF_F)) continue;
@@ -756,7 +794,11 @@ cudaError_t top_typed(const TopArgs& a, cudaStream_t st) {
   constexpr int NV = 4;
   Cut c = cut_rows(a.logits, a.row_stride, a.rows, a.vocab, sizeof(T), NV, 0);
   // the bound is the better the more threads the row's elements are spread over
-  while (c.threads < kRowThreads && c.threads < 2 * (a.k >> c.log_blocks) && c.threads < c.share) c.threads += 32;
+  while (c.threads < kRowThreads && c.threads < 2 * (a.k >> c.log_blocks) && c.rounds > 1) {
+    const uint32_t held = c.rounds * c.threads;
+    c.threads += 32;
+    c.rounds = (held + c.threads - 1) / c.threads;
+  }
   return launch_rows(kKTopLogits, k_top_logits<T, NV>, a.rows, c, true, 0, st, a, c.log_blocks);
 }
 
