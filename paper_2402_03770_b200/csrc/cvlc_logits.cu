@@ -201,17 +201,47 @@ struct Whole {  // what the row's gradient needs; kept for it between loss and g
 };
 static_assert(sizeof(Whole) <= 4 * CVLC_DISTILL_STATS, "a row's place in the buffer");
 
+// e^x to 2^-36 relative, which is far below what the rounding of x to fp32 leaves of it: x = n ln 2 + r, and the Taylor series of e^r
+// (|r| <= 0.35: 0.35^11 / 11! = 2^-42).  A third of the instructions of the library's.
+__device__ __forceinline__ double exp_of(float x) {
+  if (!(x > -600.f)) return x == x ? 0.0 : (double)x;
+  if (x > 600.f) return exp((double)x);
+  const double n = rint((double)x * 1.4426950408889634074), r = fma(n, -0.693147180559945309417, (double)x);
+  double y = 1.0 / 3628800.0;
+  y = fma(y, r, 1.0 / 362880.0);
+  y = fma(y, r, 1.0 / 40320.0);
+  y = fma(y, r, 1.0 / 5040.0);
+  y = fma(y, r, 1.0 / 720.0);
+  y = fma(y, r, 1.0 / 120.0);
+  y = fma(y, r, 1.0 / 24.0);
+  y = fma(y, r, 1.0 / 6.0);
+  y = fma(y, r, 0.5);
+  y = fma(y, r, 1.0);
+  y = fma(y, r, 1.0);
+  return __hiloint2double(__double2hiint(y) + ((int)n << 20), __double2loint(y));  // |n| < 870: the exponent stays a normal one's
+}
+
+// what p (z - a) has to gain to be p (z - b), a at most b; a = -inf: it is -inf already, or there is no mass
+__device__ __forceinline__ double moved(double mass, float a, float b) {
+  return a == -CUDART_INF_F || a == b ? 0.0 : mass * ((double)a - (double)b);
+}
+
 struct Sums {  // a row's parts joined
   MaxSum rest, said, all;
   double mass, left;  // left: what the bucket holds
   bool empty;         // every word is masked: no distribution
 };
+// by a warp: a lane for each part
 __device__ __forceinline__ Sums sums_of(const Part* parts, uint32_t blocks, uint32_t rest, float c2) {
-  Sums s = {parts[0].rest, parts[0].said, {}, parts[0].mass, 0.0, false};
-  for (uint32_t r = 1; r < blocks; ++r) {
-    s.rest = join(s.rest, parts[r].rest, c2);
-    s.said = join(s.said, parts[r].said, c2);
-    s.mass += parts[r].mass;
+  const uint32_t lane = threadIdx.x & 31;
+  Sums s = {{-CUDART_INF_F, 0.f}, {-CUDART_INF_F, 0.f}, {}, 0.0, 0.0, false};
+  if (lane < blocks) s.rest = parts[lane].rest, s.said = parts[lane].said, s.mass = parts[lane].mass;
+  for (uint32_t o = 1; o < blocks; o *= 2) {
+    const MaxSum rest_o = {__shfl_xor_sync(kFull, s.rest.max, o), __shfl_xor_sync(kFull, s.rest.sum, o)};
+    const MaxSum said_o = {__shfl_xor_sync(kFull, s.said.max, o), __shfl_xor_sync(kFull, s.said.sum, o)};
+    s.mass += __shfl_xor_sync(kFull, s.mass, o);
+    s.rest = join(s.rest, rest_o, c2);
+    s.said = join(s.said, said_o, c2);
   }
   s.all = join(s.rest, s.said, c2);
   s.empty = s.all.max == -CUDART_INF_F && s.all.sum == 0.f;
@@ -224,22 +254,19 @@ __device__ __forceinline__ Whole whole_row(const Sums& s, uint32_t rest, float c
   if (s.empty) return {0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
   Whole w;
   w.max = s.all.max;
-  w.inv_sum = 1.f / s.all.sum;
+  w.inv_sum = __frcp_rn(s.all.sum);
   w.b = (float)(s.mass + s.left);
   w.c = 1.f;
   if (rest == CVLC_REST_SCALED) {
     w.b = s.mass > 0.0 ? 1.f : (float)s.mass;  // (a NaN stays one)
-    w.c = s.mass > 0.0 ? (float)(1.0 / s.mass) : (float)s.mass;
+    w.c = s.mass > 0.0 ? __frcp_rn((float)s.mass) : (float)s.mass;
   }
   const bool some = !(s.rest.max == -CUDART_INF_F && s.rest.sum == 0.f);
   w.ref = some ? s.rest.max : 0.f;
-  w.a = some ? w.b * (exp2_fast((s.rest.max - s.all.max) * c2) * w.inv_sum) - (float)s.left / s.rest.sum : 0.f;
+  w.a = some ? w.b * (exp2_fast((s.rest.max - s.all.max) * c2) * w.inv_sum) - (float)s.left * __frcp_rn(s.rest.sum) : 0.f;
   return w;
 }
-// what p (z - a) has to gain to be p (z - b), a at most b; a = -inf: it is -inf already, or there is no mass
-__device__ __forceinline__ double moved(double mass, float a, float b) {
-  return a == -CUDART_INF_F || a == b ? 0.0 : mass * ((double)a - (double)b);
-}
+// by one thread
 __device__ double loss_of(const Sums& s, const Part* parts, uint32_t blocks, uint32_t rest, float temperature) {
   if (s.empty) return 0.0;
   double ent = 0.0, cross = 0.0;
@@ -254,6 +281,101 @@ __device__ double loss_of(const Sums& s, const Part* parts, uint32_t blocks, uin
   return loss;
 }
 
+// ---- a row's records, as a block sees them ----
+// The words' places are marked as soon as the records are there, for the pass over the logits; what the teacher says of them is summed
+// while the logits are on their way, and what the student says of them when they have come.
+struct Records {
+  int* at;        // places of the records in the block's share, or -1
+  float* prob;    // their probabilities; below 0: counted with an earlier record of the word
+  float* logit;   // the student's logits of their words
+  double mass, ent;
+
+  __device__ __forceinline__ Records(unsigned char* shared, uint32_t k)
+      : at(reinterpret_cast<int*>(shared)), prob(reinterpret_cast<float*>(at + k)), logit(prob + k), mass(0.0), ent(0.0) {}
+  // the first record of a thread, and its word's logit
+  int id;
+  float logp, z;
+
+  __device__ __forceinline__ void fetch(const DistillArgs& a, uint64_t row) {
+    id = -1;
+    logp = 0.f;
+    if (threadIdx.x < a.k) {
+      id = a.ids[row * a.k + threadIdx.x];
+      logp = a.logp[row * a.k + threadIdx.x];
+    }
+  }
+  // true: a word of this thread is marked twice.  marks: cleared before, a barrier between
+  template <class T>
+  __device__ __forceinline__ bool mark(const DistillArgs& a, uint64_t row, const Row<T>& R, uint32_t* marks) {
+    bool twice = false;
+    for (uint32_t i = threadIdx.x; i < a.k; i += blockDim.x) {
+      if (i != threadIdx.x) id = a.ids[row * a.k + i], logp = a.logp[row * a.k + i];
+      int p = -1;
+      float v = 0.f;
+      if (id >= 0 && (uint32_t)id >= a.vocab) {
+        if (a.status) set_status(a.status, CVLC_ERR_INVALID_ARG);
+      } else if (id >= 0 && (p = R.place((uint32_t)id)) >= 0) {
+        v = to_float(R.at[id]);
+        const uint32_t bit = 1u << (p & 31);
+        twice |= (atomicOr(marks + (p >> 5), bit) & bit) != 0;
+      }
+      at[i] = p;
+      prob[i] = logp;
+      if (i == threadIdx.x) z = v;
+      else logit[i] = v;
+    }
+    return twice;
+  }
+  // p of every word, summed in the order of its records; behind the barrier that follows mark()
+  template <bool SUMS>
+  __device__ __forceinline__ void teacher(const DistillArgs& a, uint64_t row, bool twice) {
+    for (uint32_t i = threadIdx.x; i < a.k; i += blockDim.x) {
+      double p = -1.0;
+      if (at[i] >= 0) {
+        const float lp = prob[i];
+        p = exp_of(lp);
+        bool merged = false;
+        if (twice) {
+          const int here = at[i];
+          for (uint32_t o = 0; o < i; ++o)
+            if (at[o] == here) p = -1.0;
+          if (p >= 0.0)
+            for (uint32_t o = i + 1; o < a.k; ++o)
+              if (at[o] == here) p += exp_of(a.logp[row * a.k + o]), merged = true;
+        }
+        if (SUMS && !(p < 0.0)) {
+          mass += p;
+          if (p != 0.0) ent += p * (merged ? log(p) : (double)lp);
+        }
+      }
+      prob[i] = p > 0.0 ? fmaxf((float)p, 1e-45f) : (float)p;  // (above 0 stays so; only this thread reads its own)
+    }
+  }
+  // the sums of the warp's records; every lane has them
+  __device__ __forceinline__ Part student(const DistillArgs& a, float c2) {
+    if (threadIdx.x < a.k) logit[threadIdx.x] = z;
+    Part p = {{}, {-CUDART_INF_F, 0.f}, 0.0, 0.0, 0.0};
+    for (uint32_t i = threadIdx.x; i < a.k; i += blockDim.x)
+      if (at[i] >= 0 && !(prob[i] < 0.f)) p.said.max = fmaxf(p.said.max, logit[i]);
+#pragma unroll
+    for (int o = 16; o; o >>= 1) p.said.max = fmaxf(p.said.max, __shfl_xor_sync(kFull, p.said.max, o));
+    const float ref = finite_ref(p.said.max);
+    for (uint32_t i = threadIdx.x; i < a.k; i += blockDim.x)
+      if (at[i] >= 0 && !(prob[i] < 0.f)) {
+        p.said.sum += exp2_fast((logit[i] - ref) * c2);
+        if (prob[i] != 0.f) p.cross += (double)prob[i] * ((double)logit[i] - (double)ref);
+      }
+    p.said.sum = warp_sum(p.said.sum), p.cross = warp_sum(p.cross), p.mass = warp_sum(mass), p.ent = warp_sum(ent);
+    return p;
+  }
+};
+__device__ __forceinline__ void add_said(Part& p, const Part& o, float c2) {
+  const MaxSum all = join(p.said, o.said, c2);
+  p.cross = p.cross + moved(p.mass, p.said.max, all.max) + o.cross + moved(o.mass, o.said.max, all.max);
+  p.said = all;
+  p.mass += o.mass, p.ent += o.ent;
+}
+
 // bits of the listed words of the block's vector i
 template <class T>
 __device__ __forceinline__ uint32_t listed_of(const uint8_t* marks, uint32_t i) {
@@ -264,11 +386,10 @@ __device__ __forceinline__ uint32_t listed_of(const uint8_t* marks, uint32_t i) 
 // reads again what lies behind the first batch, if the row is longer than its cluster keeps.
 template <class T, int NV, DistillKind KIND>
 __global__ void __launch_bounds__(kRowThreads, 2) k_distill(DistillArgs a, uint32_t log_blocks, uint32_t mark_bytes) {
-  extern __shared__ __align__(16) unsigned char dyn[];
+  extern __shared__ __align__(128) unsigned char dyn[];
   __shared__ Part parts[kMaxClusterBlocks];
   __shared__ MaxSum of_warp[kRowThreads / 32];
   __shared__ Part said_of_warp[kRowThreads / 32];
-  __shared__ uint32_t said_top;
   __shared__ Whole whole;
   const uint32_t nt = blockDim.x, tid = threadIdx.x, blocks = 1u << log_blocks, lane = tid & 31, warp = tid >> 5;
   const uint32_t rank = blockIdx.x & (blocks - 1);
@@ -279,70 +400,25 @@ __global__ void __launch_bounds__(kRowThreads, 2) k_distill(DistillArgs a, uint3
   const uint32_t rounds = R.rounds();
 
   uint8_t* const marks = dyn;
-  int* const at = reinterpret_cast<int*>(dyn + mark_bytes);  // places of the records in the block's share, or -1
-  float* const prob = reinterpret_cast<float*>(at + a.k);    // their probabilities; -1: counted with an earlier record of the word
-  float* const logit = prob + a.k;                           // the student's logits of their words
+  Records S(dyn + mark_bytes, a.k);
 
   // a row that counts for nothing is not looked at (but for what a later gradient may ask for)
   const bool idle = weight == 0.f && !(KIND == kDistillLoss && a.stats);
 
   uint4 raw[NV];
-  if (!idle) load_batch<T, NV>(R, 0, raw);
+  if (!idle) {
+    S.fetch(a, row);
+    load_batch<T, NV>(R, 0, raw);
+  }
   if (KIND != kDistillGrad && blocks > 1) cluster_arrive<false>();  // waited for before another block's shared memory is written
   if (!idle) {
     for (uint32_t i = tid; i < mark_bytes / 16; i += nt) reinterpret_cast<uint4*>(marks)[i] = make_uint4(0, 0, 0, 0);
-    if (tid == 0) said_top = 0;
     __syncthreads();
-    bool twice = false;
-    for (uint32_t i = tid; i < a.k; i += nt) {
-      const int id = a.ids[row * a.k + i];
-      int p = -1;
-      if (id >= 0 && (uint32_t)id >= a.vocab) {
-        if (a.status) set_status(a.status, CVLC_ERR_INVALID_ARG);
-      } else if (id >= 0 && (p = R.place((uint32_t)id)) >= 0) {
-        logit[i] = to_float(R.at[id]);
-        const uint32_t bit = 1u << (p & 31);
-        twice |= (atomicOr(reinterpret_cast<uint32_t*>(marks) + (p >> 5), bit) & bit) != 0;
-        if (KIND != kDistillGrad) atomicMax(&said_top, order_of(logit[i]));
-      }
-      at[i] = p;
-      prob[i] = a.logp[row * a.k + i];
-    }
-    twice = __syncthreads_or(twice);
-    // p of every word, summed in the order of its records
-    const float top = said_top ? value_of(said_top) : -CUDART_INF_F;
-    float sum = 0.f;
-    double mass = 0.0, ent = 0.0, cross = 0.0;
-    for (uint32_t i = tid; i < a.k; i += nt) {
-      double p = -1.0;
-      if (at[i] >= 0) {
-        const double lp = (double)prob[i];
-        p = exp(lp);
-        bool merged = false;
-        if (twice) {
-          const int here = at[i];
-          for (uint32_t o = 0; o < i; ++o)
-            if (at[o] == here) p = -1.0;
-          if (p >= 0.0)
-            for (uint32_t o = i + 1; o < a.k; ++o)
-              if (at[o] == here) p += exp((double)a.logp[row * a.k + o]), merged = true;
-        }
-        if (KIND != kDistillGrad && !(p < 0.0)) {
-          mass += p;
-          if (p != 0.0) {
-            ent += p * (merged ? log(p) : lp);
-            cross += p * ((double)logit[i] - (double)finite_ref(top));
-          }
-          sum += exp2_fast((logit[i] - finite_ref(top)) * c2);
-        }
-      }
-      prob[i] = (float)p;  // only this thread reads its own
-    }
-    if (KIND != kDistillGrad) {
-      if (warp * 32 < a.k) {
-        sum = warp_sum(sum), mass = warp_sum(mass), ent = warp_sum(ent), cross = warp_sum(cross);
-        if (lane == 0) said_of_warp[warp] = {{}, {top, sum}, mass, ent, cross};
-      }
+    const bool twice = __syncthreads_or(S.mark<T>(a, row, R, reinterpret_cast<uint32_t*>(marks)));
+    S.teacher<KIND != kDistillGrad>(a, row, twice);
+    if (KIND == kDistillGrad) {
+      if (tid < a.k) S.logit[tid] = S.z;
+    } else {
       MaxSum mine = {-CUDART_INF_F, 0.f};
       for (uint32_t from = 0;;) {
         uint4 ahead[NV];
@@ -363,14 +439,16 @@ __global__ void __launch_bounds__(kRowThreads, 2) k_distill(DistillArgs a, uint3
       }
       mine = warp_join(mine, c2);
       if (lane == 0) of_warp[warp] = mine;
+      if (warp * 32 < a.k) {
+        const Part p = S.student(a, c2);
+        if (lane == 0) said_of_warp[warp] = p;
+      }
       __syncthreads();
       if (warp == 0) {
-        Part p = {join_warps(of_warp, nt / 32, c2), {top, 0.f}, 0.0, 0.0, 0.0};
-        const uint32_t with = min(nt / 32, (a.k + 31) / 32);  // warps that had records
-        for (uint32_t w = 0; w < with; ++w) {
-          p.said.sum += said_of_warp[w].said.sum;
-          p.mass += said_of_warp[w].mass, p.ent += said_of_warp[w].ent, p.cross += said_of_warp[w].cross;
-        }
+        Part p = {{}, {-CUDART_INF_F, 0.f}, 0.0, 0.0, 0.0};
+        const uint32_t with = min(nt / 32, (a.k + 31) / 32);  // warps that have records
+        for (uint32_t w = 0; w < with; ++w) add_said(p, said_of_warp[w], c2);
+        p.rest = join_warps(of_warp, nt / 32, c2);
         if (blocks == 1) {
           if (lane == 0) parts[0] = p;
         } else {
@@ -395,15 +473,14 @@ __global__ void __launch_bounds__(kRowThreads, 2) k_distill(DistillArgs a, uint3
   if (KIND == kDistillGrad) {
     if (!idle) w = *reinterpret_cast<const Whole*>(a.stats + row * CVLC_DISTILL_STATS);
   } else if (KIND == kDistillLoss) {
-    if (tid == 0 && rank == 0) {
-      double loss = 0.0;
-      if (!idle) {
-        const Sums s = sums_of(parts, blocks, a.rest, c2);
-        loss = loss_of(s, parts, blocks, a.rest, a.temperature);
-        if (a.stats) *reinterpret_cast<Whole*>(a.stats + row * CVLC_DISTILL_STATS) = whole_row(s, a.rest, c2);
-      }
-      a.loss[row] = weight == 0.f ? 0.f : (float)((double)weight * loss);
+    if (warp != 0 || rank != 0) return;
+    double loss = 0.0;
+    if (!idle) {
+      const Sums s = sums_of(parts, blocks, a.rest, c2);
+      if (lane == 0) loss = loss_of(s, parts, blocks, a.rest, a.temperature);
+      if (lane == 0 && a.stats) *reinterpret_cast<Whole*>(a.stats + row * CVLC_DISTILL_STATS) = whole_row(s, a.rest, c2);
     }
+    if (lane == 0) a.loss[row] = weight == 0.f ? 0.f : (float)((double)weight * loss);
     return;
   } else if (!idle) {
     if (warp == 0) {
@@ -457,15 +534,431 @@ __global__ void __launch_bounds__(kRowThreads, 2) k_distill(DistillArgs a, uint3
     __syncthreads();  // the listed words' gradients replace what the vectors hold in their places
     const float cb = w.b * scale, cc = w.c * scale;
     for (uint32_t i = tid; i < a.k; i += nt)
-      if (at[i] >= 0 && !(prob[i] < 0.f)) {
-        const float q = exp2_fast((logit[i] - w.max) * c2) * w.inv_sum;
-        g[a.ids[row * a.k + i]] = from_float<T>(cb * q - cc * prob[i]);
+      if (S.at[i] >= 0 && !(S.prob[i] < 0.f)) {
+        const float q = exp2_fast((S.logit[i] - w.max) * c2) * w.inv_sum;
+        g[a.ids[row * a.k + i]] = from_float<T>(cb * q - cc * S.prob[i]);
       }
   }
   // the loss last: its logarithms take as long as a store
-  if (KIND == kDistillStep && rank == 0 && tid == nt - 1) {
-    const double loss = idle ? 0.0 : loss_of(sums_of(parts, blocks, a.rest, c2), parts, blocks, a.rest, a.temperature);
-    a.loss[row] = weight == 0.f ? 0.f : (float)((double)weight * loss);
+  if (KIND == kDistillStep && rank == 0 && warp == 0) {
+    double loss = 0.0;
+    if (!idle) {
+      const Sums s = sums_of(parts, blocks, a.rest, c2);
+      if (lane == 0) loss = loss_of(s, parts, blocks, a.rest, a.temperature);
+    }
+    if (lane == 0) a.loss[row] = weight == 0.f ? 0.f : (float)((double)weight * loss);
+  }
+}
+
+// ---- many long rows: a block goes from row to row ----
+//
+// Everything that a row needs beside its elements (records, sums, logarithms) takes a block about as long as reading 64 KB does, whoever does
+// it.  So where rows are many it is done by warps of their own, beside the pass over the elements: a row's records are prepared while
+// the row before it is passed over, and its loss, its listed words and its ragged ends are finished while the row behind it is.  One
+// thread copies the rows through a ring of stages in shared memory (cp.async.bulk), one thread's pair of vectors a stage; the step
+// copies every row twice, the second time out of the L2 cache, which holds the 296 rows on their way (76 MB at 131,072 words of 16
+// bits).  Keeping the row in the cluster's registers instead costs every block of the cluster all of the above:
+// 4096 x 131072 bf16 750 us.
+constexpr int kStreamWarps = 16, kSideWarps = 3;  // and one that copies: twenty warps leave each of two blocks 48 registers a thread
+constexpr int kStreamLanes = kStreamWarps * 32, kSideLanes = kSideWarps * 32;
+constexpr int kStreamBlock = kStreamLanes + kSideLanes + 32;
+constexpr int kStageVecs = 2 * kStreamLanes;  // vectors of a stage: 16 KB
+constexpr int kStagesMost = 8;
+constexpr size_t kStreamShared = 110 * 1024;  // of a block, two of which share an SM
+
+struct RowAt {  // where a row lies
+  const unsigned char* from;  // vector 0
+  uint32_t lead, vecs, whole_from, wholes;
+};
+template <class T>
+__device__ __forceinline__ RowAt row_at(const DistillArgs& a, uint64_t row) {
+  const T* const at = static_cast<const T*>(a.logits) + row * a.row_stride;
+  RowAt r;
+  r.lead = (uint32_t)((reinterpret_cast<uintptr_t>(at) & 15) / sizeof(T));
+  r.from = reinterpret_cast<const unsigned char*>(reinterpret_cast<uintptr_t>(at) & ~(uintptr_t)15);
+  r.vecs = (r.lead + a.vocab + kPerVec<T> - 1) / kPerVec<T>;
+  r.whole_from = r.lead ? 1 : 0;
+  const uint32_t whole_to = (r.lead + a.vocab) / kPerVec<T>;
+  r.wholes = whole_to > r.whole_from ? whole_to - r.whole_from : 0;
+  return r;
+}
+
+__device__ __forceinline__ uint32_t shared_at(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ void bar_init(uint64_t* b, uint32_t n) { asm volatile("mbarrier.init.shared.b64 [%0], %1;" ::"r"(shared_at(b)), "r"(n)); }
+__device__ __forceinline__ void bar_arrive(uint64_t* b) { asm volatile("mbarrier.arrive.shared.b64 _, [%0];" ::"r"(shared_at(b)) : "memory"); }
+__device__ __forceinline__ void bar_expect(uint64_t* b, uint32_t bytes) {
+  asm volatile("mbarrier.arrive.expect_tx.shared.b64 _, [%0], %1;" ::"r"(shared_at(b)), "r"(bytes) : "memory");
+}
+// Bounded: a wait that runs out clears `ok`, and later ones try once.
+__device__ __forceinline__ void bar_wait(uint64_t* b, uint32_t parity, bool& ok) {
+  uint32_t done = 0;
+  for (uint32_t tries = ok ? 1u << 22 : 1u; tries && !done; --tries)
+    asm volatile("{.reg .pred p;\n mbarrier.try_wait.parity.shared.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;}"
+                 : "=r"(done)
+                 : "r"(shared_at(b)), "r"(parity)
+                 : "memory");
+  if (!done) ok = false;
+}
+// A warp has read its part of a stage.  The copy that fills the stage next writes it by another path than the loads take: the loads
+// have to be over before the copying thread hears of it, and the arrival alone does not see to that.
+__device__ __forceinline__ void release_stage(uint64_t* b) {
+  asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  __syncwarp();
+  if ((threadIdx.x & 31) == 0) bar_arrive(b);
+}
+// named barriers among some of a block's warps
+template <int N>
+__device__ __forceinline__ void some_sync(int id) { asm volatile("bar.sync %0, %1;" ::"r"(id), "n"(N) : "memory"); }
+template <int N>
+__device__ __forceinline__ void some_arrive(int id) { asm volatile("bar.arrive %0, %1;" ::"r"(id), "n"(N) : "memory"); }
+template <int N>
+__device__ __forceinline__ bool some_or(int id, bool v) {
+  uint32_t r;
+  asm volatile("{.reg .pred p, q;\n setp.ne.u32 p, %1, 0;\n bar.red.or.pred q, %2, %3, p;\n selp.u32 %0, 1, 0, q;}" : "=r"(r) : "r"((uint32_t)v), "r"(id), "n"(N) : "memory");
+  return r != 0;
+}
+enum { kBarSide = 1, kBarStream = 2, kBarReady = 3, kBarDone = 5 };  // the last two: one for each of two rows
+
+struct RowSide {  // what the side warps know of a row
+  MaxSum said, ends;        // listed words; unlisted ones in the ragged ends
+  double mass, ent, cross;  // as in Part
+  float left, b_left, b, c; // left of the bucket, if there is one; b with and without it; c
+  MaxSum rest[kStreamWarps];
+};
+
+// The row's numbers, by a whole warp
+__device__ __forceinline__ Whole whole_of(const RowSide& s, float c2, MaxSum* rest_out, MaxSum* all_out, float* left_out) {
+  const uint32_t lane = threadIdx.x & 31;
+  const MaxSum mine = lane < kStreamWarps ? s.rest[lane] : lane == kStreamWarps ? s.ends : MaxSum{-CUDART_INF_F, 0.f};
+  const MaxSum rest = warp_join(mine, c2);
+  const MaxSum all = join(rest, s.said, c2);
+  const bool some = !(rest.max == -CUDART_INF_F && rest.sum == 0.f);  // without a word that it could stand for there is no bucket
+  const float left = some ? s.left : 0.f;
+  *rest_out = rest, *all_out = all, *left_out = left;
+  if (all.max == -CUDART_INF_F && all.sum == 0.f) return {0.f, 0.f, 0.f, 0.f, 0.f, 0.f};  // every word is masked
+  Whole w;
+  w.max = all.max;
+  w.inv_sum = __frcp_rn(all.sum);
+  w.b = some ? s.b_left : s.b;
+  w.c = s.c;
+  w.ref = some ? rest.max : 0.f;
+  w.a = some ? w.b * (exp2_fast((rest.max - all.max) * c2) * w.inv_sum) - left * __frcp_rn(rest.sum) : 0.f;
+  return w;
+}
+
+template <class T, DistillKind KIND>
+__global__ void __launch_bounds__(kStreamBlock, 2) k_distill_stream(DistillArgs a, uint32_t stages, uint32_t mark_bytes) {
+  extern __shared__ __align__(128) unsigned char dyn[];
+  __shared__ uint64_t full[kStagesMost], empty[kStagesMost];
+  __shared__ RowSide sides[2];
+  __shared__ Part of_side[kSideWarps];
+  constexpr int E = kPerVec<T>;
+  const uint32_t tid = threadIdx.x, lane = tid & 31;
+  const float c2 = a.c2;
+  uint4* const ring = reinterpret_cast<uint4*>(dyn);
+  uint8_t* const marks_of[2] = {dyn + (size_t)stages * kStageVecs * 16, dyn + (size_t)stages * kStageVecs * 16 + mark_bytes};
+  int* const records = reinterpret_cast<int*>(dyn + (size_t)stages * kStageVecs * 16 + 2 * mark_bytes);  // [2][3][k]
+  constexpr int kPasses = KIND == kDistillStep ? 2 : 1;
+  const auto idle_row = [&](uint64_t row) { return a.row_weight && a.row_weight[row] == 0.f && !(KIND == kDistillLoss && a.stats); };
+
+  if (tid == 0) {
+    for (uint32_t i = 0; i < stages; ++i) bar_init(&full[i], 1), bar_init(&empty[i], kStreamWarps);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  for (uint32_t i = tid; i < mark_bytes / 8; i += kStreamBlock) reinterpret_cast<uint4*>(marks_of[0])[i] = make_uint4(0, 0, 0, 0);
+  __syncthreads();
+
+  bool ok = true;
+  if (tid >= kStreamLanes + kSideLanes) {
+    // ---- the copying thread ----
+    if (lane == 0) {
+      uint64_t again;  // the second reading is the last
+      asm("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(again));
+      uint32_t stage = 0, phase = 0;
+      for (uint64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+        if (idle_row(row)) continue;
+        const RowAt R = row_at<T>(a, row);
+        for (int pass = 0; pass < kPasses; ++pass)
+          for (uint32_t v = 0; v < R.wholes; v += kStageVecs) {
+            bar_wait(&empty[stage], phase ^ 1, ok);
+            const uint32_t bytes = min(R.wholes - v, (uint32_t)kStageVecs) * 16;
+            bar_expect(&full[stage], bytes);
+            const unsigned char* const src = R.from + ((size_t)R.whole_from + v) * 16;
+            if (pass == kPasses - 1)
+              asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1], %2, [%3], %4;" ::"r"(
+                               shared_at(ring + (size_t)stage * kStageVecs)),
+                           "l"(src), "r"(bytes), "r"(shared_at(&full[stage])), "l"(again)
+                           : "memory");
+            else
+              asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(
+                               shared_at(ring + (size_t)stage * kStageVecs)),
+                           "l"(src), "r"(bytes), "r"(shared_at(&full[stage]))
+                           : "memory");
+            if (++stage == stages) stage = 0, phase ^= 1;
+          }
+      }
+      // no copy is left on its way, even where a wait ran out
+      bool last = true;
+      for (uint32_t i = 0; i < stages; ++i) {
+        bar_wait(&empty[stage], phase ^ 1, last);
+        if (++stage == stages) stage = 0, phase ^= 1;
+      }
+      if (!(ok && last) && a.status) set_status(a.status, CVLC_ERR_DEVICE_TIMEOUT);
+    }
+    return;
+  }
+
+  if (tid >= kStreamLanes) {
+    // ---- the side warps: records, ragged ends, losses ----
+    const uint32_t t = tid - kStreamLanes, side = t >> 5;
+    struct Ends {
+      int word;  // of the lane, or -1
+      float z;
+    };
+    // words of the vectors that are not whole: of the first one and, behind them, of the last one
+    const auto end_word = [&](const RowAt& R) {
+      if (side != 0 || lane >= 2 * E) return -1;
+      const uint32_t last = R.vecs - 1;
+      const bool first_ragged = R.whole_from > 0 || R.wholes == 0, last_ragged = last > 0 && last >= R.whole_from + R.wholes;
+      const int w = lane < E ? (int)lane - (int)R.lead : (int)(last * E + lane - E) - (int)R.lead;
+      return (lane < E ? first_ragged : last_ragged) && w >= 0 && w < (int)a.vocab ? w : -1;
+    };
+    const auto prepare = [&](uint64_t row, uint32_t buf) {
+      some_sync<kSideLanes>(kBarSide);  // the row before the last one is finished, its marks cleared
+      const RowAt R = row_at<T>(a, row);
+      const T* const z = reinterpret_cast<const T*>(R.from) + R.lead;
+      uint8_t* const marks = marks_of[buf];
+      int* const at = records + buf * 3 * a.k;
+      float* const prob = reinterpret_cast<float*>(at + a.k);
+      float* const logit = prob + a.k;
+      bool twice = false;
+      const int end = end_word(R);
+      const float end_z = end >= 0 ? to_float(z[end]) : -CUDART_INF_F;
+      for (uint32_t i = t; i < a.k; i += kSideLanes) {
+        const int id = a.ids[row * a.k + i];
+        prob[i] = a.logp[row * a.k + i];
+        int p = -1;
+        if (id >= 0 && (uint32_t)id >= a.vocab) {
+          if (a.status) set_status(a.status, CVLC_ERR_INVALID_ARG);
+        } else if (id >= 0) {
+          p = id + (int)R.lead;
+          logit[i] = to_float(z[id]);
+          const uint32_t bit = 1u << (p & 31);
+          twice |= (atomicOr(reinterpret_cast<uint32_t*>(marks) + (p >> 5), bit) & bit) != 0;
+        }
+        at[i] = p;
+      }
+      twice = some_or<kSideLanes>(kBarSide, twice);
+      Part mine = {{-CUDART_INF_F, 0.f}, {-CUDART_INF_F, 0.f}, 0.0, 0.0, 0.0};
+      for (uint32_t i = t; i < a.k; i += kSideLanes) {
+        const int here = at[i];
+        double p = -1.0;
+        if (here >= 0) {
+          const float lp = prob[i];
+          p = exp_of(lp);
+          bool merged = false;
+          if (twice) {
+            for (uint32_t o = 0; o < i; ++o)
+              if (at[o] == here) p = -1.0;
+            if (p >= 0.0)
+              for (uint32_t o = i + 1; o < a.k; ++o)
+                if (at[o] == here) p += exp_of(a.logp[row * a.k + o]), merged = true;
+          }
+          if (KIND != kDistillGrad && !(p < 0.0)) {
+            mine.mass += p;
+            if (p != 0.0) mine.ent += p * (merged ? log(p) : (double)lp);
+            mine.said.max = fmaxf(mine.said.max, logit[i]);
+          }
+        }
+        prob[i] = p > 0.0 ? fmaxf((float)p, 1e-45f) : (float)p;  // (above 0 stays so; only this thread reads its own)
+      }
+      if (KIND != kDistillGrad) {
+#pragma unroll
+        for (int o = 16; o; o >>= 1) mine.said.max = fmaxf(mine.said.max, __shfl_xor_sync(kFull, mine.said.max, o));
+        const float ref = finite_ref(mine.said.max);
+        for (uint32_t i = t; i < a.k; i += kSideLanes)
+          if (at[i] >= 0 && !(prob[i] < 0.f)) {
+            mine.said.sum += exp2_fast((logit[i] - ref) * c2);
+            if (prob[i] != 0.f) mine.cross += (double)prob[i] * ((double)logit[i] - (double)ref);
+          }
+        mine.said.sum = warp_sum(mine.said.sum), mine.mass = warp_sum(mine.mass), mine.ent = warp_sum(mine.ent), mine.cross = warp_sum(mine.cross);
+        if (side == 0) {
+          const bool listed = end >= 0 && (marks[(end + R.lead) >> 3] >> ((end + R.lead) & 7) & 1);
+          const float e = listed ? -CUDART_INF_F : end_z;
+          mine.rest = warp_join(MaxSum{e, e == -CUDART_INF_F ? 0.f : e == e ? 1.f : e}, c2);
+        }
+        if (lane == 0) of_side[side] = mine;
+        some_sync<kSideLanes>(kBarSide);
+        if (t == 0) {
+          Part p = of_side[0];
+          for (int w = 1; w < kSideWarps; ++w) add_said(p, of_side[w], c2);
+          RowSide& s = sides[buf];
+          s.said = p.said, s.ends = p.rest;
+          s.mass = p.mass, s.ent = p.ent, s.cross = p.cross;
+          const double left = a.rest == CVLC_REST_BUCKET && p.mass < 1.0 ? 1.0 - p.mass : 0.0;
+          s.left = (float)left;
+          s.b_left = (float)(p.mass + left), s.b = (float)p.mass, s.c = 1.f;
+          if (a.rest == CVLC_REST_SCALED) {
+            s.b = s.b_left = p.mass > 0.0 ? 1.f : (float)p.mass;  // (a NaN stays one)
+            s.c = p.mass > 0.0 ? __frcp_rn((float)p.mass) : (float)p.mass;
+          }
+        }
+      }
+      __threadfence_block();
+      some_arrive<kStreamLanes + kSideLanes>(kBarReady + buf);
+    };
+    const auto finish = [&](uint64_t row, uint32_t buf) {
+      some_sync<kStreamLanes + kSideLanes>(kBarDone + buf);
+      const RowAt R = row_at<T>(a, row);
+      const float weight = a.row_weight ? a.row_weight[row] : 1.f;
+      uint8_t* const marks = marks_of[buf];
+      int* const at = records + buf * 3 * a.k;
+      float* const prob = reinterpret_cast<float*>(at + a.k);
+      float* const logit = prob + a.k;
+      Whole w;
+      if (KIND == kDistillGrad) {
+        w = *reinterpret_cast<const Whole*>(a.stats + row * CVLC_DISTILL_STATS);
+      } else {
+        RowSide& s = sides[buf];
+        MaxSum rest, all;
+        float left;
+        w = whole_of(s, c2, &rest, &all, &left);
+        if (t == 0) {
+          double loss = 0.0;
+          if (!(all.max == -CUDART_INF_F && all.sum == 0.f)) {
+            const double it = 1.0 / (double)a.temperature, ln_sum = log((double)all.sum);
+            loss = s.ent - (s.cross + moved(s.mass, s.said.max, all.max)) * it + s.mass * ln_sum;
+            if (a.rest == CVLC_REST_SCALED) loss = s.mass > 0.0 ? loss / s.mass - log(s.mass) : s.mass;
+            if (left > 0.f) {
+              const double l = 1.0 - s.mass;
+              loss += l * (log(l) - (((double)rest.max - (double)all.max) * it + log((double)rest.sum) - ln_sum));
+            }
+          }
+          a.loss[row] = weight == 0.f ? 0.f : (float)((double)weight * loss);
+          if (KIND == kDistillLoss && a.stats) *reinterpret_cast<Whole*>(a.stats + row * CVLC_DISTILL_STATS) = w;
+        }
+      }
+      T* const g = static_cast<T*>(a.grad) + row * a.grad_stride;
+      const float scale = weight / a.temperature;
+      if (KIND != kDistillLoss) {
+        const int end = end_word(R);
+        if (end >= 0 && !(marks[(end + R.lead) >> 3] >> ((end + R.lead) & 7) & 1)) {
+          const float z = to_float((reinterpret_cast<const T*>(R.from) + R.lead)[end]);
+          g[end] = from_float<T>(w.a * scale * exp2_fast((z - w.ref) * c2));
+        }
+        for (uint32_t i = t; i < a.k; i += kSideLanes)
+          if (at[i] >= 0 && !(prob[i] < 0.f)) {
+            const float q = exp2_fast((logit[i] - w.max) * c2) * w.inv_sum;
+            g[at[i] - (int)R.lead] = from_float<T>(w.b * scale * q - w.c * scale * prob[i]);
+          }
+        some_sync<kSideLanes>(kBarSide);  // the ends' marks have been read
+      }
+      for (uint32_t i = t; i < a.k; i += kSideLanes)
+        if (at[i] >= 0) reinterpret_cast<uint32_t*>(marks)[at[i] >> 5] = 0;
+    };
+    uint64_t before = ~0ull;
+    uint32_t buf = 0;
+    for (uint64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+      if (idle_row(row)) {
+        if (KIND != kDistillGrad && t == 0) a.loss[row] = 0.f;
+        continue;
+      }
+      prepare(row, buf);
+      if (before != ~0ull) finish(before, buf ^ 1);
+      before = row;
+      buf ^= 1;
+    }
+    if (before != ~0ull) finish(before, buf ^ 1);
+    return;
+  }
+
+  // ---- the pass over the elements ----
+  uint32_t stage = 0, phase = 0, buf = 0;
+  for (uint64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+    const RowAt R = row_at<T>(a, row);
+    T* const g = static_cast<T*>(a.grad) + row * a.grad_stride;
+    if (idle_row(row)) {
+      if (KIND != kDistillLoss)
+        for (uint32_t j = tid; j < a.vocab; j += kStreamLanes) g[j] = from_float<T>(0.f);
+      continue;
+    }
+    some_sync<kStreamLanes + kSideLanes>(kBarReady + buf);
+    const uint8_t* const marks = marks_of[buf];
+    Whole w = {};
+    if (KIND != kDistillGrad) {
+      MaxSum acc = {-CUDART_INF_F, 0.f};
+      for (uint32_t v = 0; v < R.wholes; v += kStageVecs) {
+        bar_wait(&full[stage], phase, ok);
+        uint4 raw[2];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const uint32_t i = v + tid + j * kStreamLanes;
+          raw[j] = i < R.wholes ? ring[(size_t)stage * kStageVecs + tid + j * kStreamLanes] : nothing<T>();
+        }
+        release_stage(&empty[stage]);
+        if (++stage == stages) stage = 0, phase ^= 1;
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const uint32_t i = v + tid + j * kStreamLanes;
+          if (i < R.wholes)
+            if (const uint32_t bits = listed_of<T>(marks, R.whole_from + i)) drop_elements<T>(raw[j], bits);
+        }
+        add_batch<T, 2>(raw, c2, acc);
+      }
+      acc = warp_join(acc, c2);
+      if (lane == 0) sides[buf].rest[tid >> 5] = acc;
+      __syncwarp();
+    }
+    if (KIND == kDistillLoss) {
+      __threadfence_block();
+      some_arrive<kStreamLanes + kSideLanes>(kBarDone + buf);
+      buf ^= 1;
+      continue;
+    }
+    if (KIND == kDistillStep) {
+      some_sync<kStreamLanes>(kBarStream);
+      MaxSum rest, all;
+      float left;
+      w = whole_of(sides[buf], c2, &rest, &all, &left);
+    } else {
+      w = *reinterpret_cast<const Whole*>(a.stats + row * CVLC_DISTILL_STATS);
+    }
+    const float ca = w.a * ((a.row_weight ? a.row_weight[row] : 1.f) / a.temperature);
+    unsigned char* const to = reinterpret_cast<unsigned char*>(g) + (int)(R.whole_from * 16) - (int)(R.lead * sizeof(T));  // of the first whole vector
+    const bool alike = (reinterpret_cast<uintptr_t>(to) & 15) == 0;
+    for (uint32_t v = 0; v < R.wholes; v += kStageVecs) {
+      bar_wait(&full[stage], phase, ok);
+      uint4 raw[2];
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const uint32_t i = v + tid + j * kStreamLanes;
+        raw[j] = i < R.wholes ? ring[(size_t)stage * kStageVecs + tid + j * kStreamLanes] : nothing<T>();
+      }
+      release_stage(&empty[stage]);
+      if (++stage == stages) stage = 0, phase ^= 1;
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const uint32_t i = v + tid + j * kStreamLanes;
+        float f[E];
+        widen<T>(raw[j], f);
+#pragma unroll
+        for (int e = 0; e < E; e += 2) {
+          const float2 x = mul2(add2(make_float2(f[e], f[e + 1]), make_float2(-w.ref, -w.ref)), make_float2(c2, c2));
+          const float2 y = mul2(make_float2(exp2_fast(x.x), exp2_fast(x.y)), make_float2(ca, ca));
+          f[e] = y.x, f[e + 1] = y.y;
+        }
+        if (i >= R.wholes) continue;
+        if (alike) {
+          __stcs(reinterpret_cast<uint4*>(to) + i, narrow<T>(f));
+        } else {
+#pragma unroll
+          for (int e = 0; e < E; ++e) reinterpret_cast<T*>(to)[(size_t)i * E + e] = from_float<T>(f[e]);
+        }
+      }
+    }
+    __threadfence_block();
+    some_arrive<kStreamLanes + kSideLanes>(kBarDone + buf);  // the listed words' gradients replace what stands in their places
+    buf ^= 1;
   }
 }
 
@@ -516,6 +1009,21 @@ cudaError_t launch_rows(int id, void (*kernel)(Params...), uint64_t rows, const 
 
 template <class T, DistillKind KIND>
 cudaError_t distill_typed(const DistillArgs& a, cudaStream_t st) {
+  // many long rows: two blocks an SM go from row to row, where two rows' marks and three stages fit
+  const uint32_t mark_row = (a.vocab + 2 * kPerVec<T> + 127) / 128 * 16;
+  const size_t beside = 2 * (size_t)mark_row + (size_t)a.k * 24;
+  if (a.rows >= kNumSM && (uint64_t)a.vocab * sizeof(T) >= 2 * kStageVecs * 16 && beside + 3 * kStageVecs * 16 <= kStreamShared) {
+    const uint32_t fit = (uint32_t)((kStreamShared - beside) / (kStageVecs * 16));
+    const uint32_t stages = fit < kStagesMost ? fit : kStagesMost;
+    const size_t smem = (size_t)stages * kStageVecs * 16 + beside;
+    void (*const kernel)(DistillArgs, uint32_t, uint32_t) = k_distill_stream<T, KIND>;
+    const cudaError_t e = allow_shared(kernel, smem);
+    if (e != cudaSuccess) return e;
+    const uint64_t grid = a.rows < 2 * kNumSM ? a.rows : 2 * kNumSM;
+    launch_kernel(KIND == kDistillLoss ? kKDistillLoss : KIND == kDistillGrad ? kKDistillGrad : kKDistillStep, kernel, dim3((unsigned)grid),
+                  dim3(kStreamBlock), smem, st, false, a, stages, mark_row);
+    return cudaGetLastError();
+  }
   constexpr int NV = KIND == kDistillStep ? 8 : 4;
   const Cut c = cut_rows(a.logits, a.row_stride, a.rows, a.vocab, sizeof(T), NV, KIND == kDistillStep ? NV : 0);
   const uint32_t mark_bytes = (c.rounds * c.threads * kPerVec<T> / 8 + 15) & ~15u;  // a bit for every element of a block

@@ -285,6 +285,51 @@ def test_distill_of_more_words_than_a_cluster_keeps(rest):
 
 
 @pytest.mark.parametrize("rest", [R.NONE, R.SCALED, R.BUCKET])
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("kind,lists,lead,pad", [("normal", "top", 0, 0), ("normal", "twice", 1, 1), ("masked", "absent", 3, 2), ("lowest", "any", 0, 8),
+                                                 ("front", "twice", 5, 0), ("far", "top", 0, 3)])
+def test_distill_of_many_long_rows(rest, dtype, kind, lists, lead, pad):
+    """more rows than blocks, each of several stages; some without weight, in a row and apart"""
+    B = binding()
+    rows, vocab = 610, 35000 // torch.finfo(dtype).bits * 16 + 7
+    z, flat = logits_of(rows, vocab, dtype, seed=vocab, kind=kind, pad=pad, lead=lead)
+    ids, lp = records(z, 70, 1.5, seed=3, kind=lists)
+    weight = torch.rand(rows, generator=torch.Generator().manual_seed(1))
+    weight[torch.rand(rows, generator=torch.Generator().manual_seed(2)) < 0.2] = 0.0
+    weight[297:305] = 0.0
+    check_distill(B, z, flat, ids, lp, rest, 1.5, weight.cuda() if lists != "top" else None)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("k", [0, 1, 1024])
+def test_distill_of_many_long_rows_records(dtype, k):
+    B = binding()
+    z, flat = logits_of(160, 40000, dtype, seed=k, lead=2)
+    if k:
+        ids, lp = records(z, k, 1.0, seed=3, kind="any")
+        ids[5], ids[6, 1:] = 39999, ids[6, :1]
+    else:
+        ids, lp = torch.zeros(160, 0, dtype=torch.int32, device="cuda"), torch.zeros(160, 0, device="cuda")
+    check_distill(B, z, flat, ids, lp, R.BUCKET, 1.0)
+
+
+def test_distill_spoiled_among_many_long_rows():
+    B = binding()
+    z, _ = logits_of(310, 20000, torch.bfloat16, seed=2)
+    clean = z.clone()
+    z[1, 100] = math.nan
+    z[297] = math.inf
+    ids, lp = records(clean, 20, 1.0, seed=1)
+    loss, g, ref, h = torch.zeros(310, device="cuda"), torch.zeros_like(z), torch.zeros(310, device="cuda"), torch.zeros_like(z)
+    B.cvlc_distill_step(z, ids, lp, loss, g)
+    B.cvlc_distill_step(clean, ids, lp, ref, h)
+    assert torch.isnan(loss[[1, 297]]).all() and torch.isnan(g[[1, 297]]).all()
+    keep = torch.ones(310, dtype=torch.bool)
+    keep[[1, 297]] = False
+    assert torch.equal(loss[keep.cuda()], ref[keep.cuda()]) and torch.equal(g[keep.cuda()], h[keep.cuda()])
+
+
+@pytest.mark.parametrize("rest", [R.NONE, R.SCALED, R.BUCKET])
 def test_distill_gradient_by_differences(rest):
     """the gradient against differences of the loss in 64 bits, by central differences of step h: off by h^2 / 6 times a third derivative
     below 2 (|w| / tau^3) and by twice the loss's rounding over 2 h"""

@@ -1,5 +1,5 @@
-"""Top logits, distillation and the embedding from their definitions, in 64 bits on the CPU, and what the kernels' 32-bit arithmetic may
-be off by."""
+"""Top logits, distillation and the embedding from their definitions, in 64 bits with plain tensor operations, and what the kernels' 32-bit
+arithmetic may be off by."""
 import math
 
 import torch
@@ -48,43 +48,41 @@ def top(logits, k, temperature):
 
 def distill(logits, ids, logp, rest, temperature, weight=None):
     """loss, gradient, and how far each may be off before it is rounded to the logits' type"""
-    z, ids, lp = logits.double().cpu(), ids.cpu().long(), logp.double().cpu()
+    few = max(1, (1 << 24) // logits.shape[1])
+    parts = [_distill_rows(logits[i:i + few], ids[i:i + few], logp[i:i + few], rest, temperature,
+                           None if weight is None else weight[i:i + few]) for i in range(0, logits.shape[0], few)]
+    return tuple(torch.cat(p).cpu() for p in zip(*parts))
+
+
+def _distill_rows(logits, ids, logp, rest, temperature, weight):
+    z, ids, lp = logits.double(), ids.long(), logp.double()
     rows, vocab = z.shape
-    loss, tol_loss = torch.zeros(rows, dtype=torch.float64), torch.zeros(rows, dtype=torch.float64)
-    grad, tol_grad = torch.zeros_like(z), torch.zeros_like(z)
-    for r in range(rows):
-        w = 1.0 if weight is None else float(weight[r])
-        if w == 0.0 or not bool((z[r] > -math.inf).any() | torch.isnan(z[r]).any()):
-            continue
-        x = from_largest(z[r]) / temperature
-        lq = x - torch.logsumexp(x, 0)
-        q = lq.exp()
-        p = torch.zeros(vocab, dtype=torch.float64)
-        named = torch.zeros(vocab, dtype=torch.bool)
-        for i, l in zip(ids[r].tolist(), lp[r].tolist()):
-            if 0 <= i < vocab:
-                p[i] += math.exp(l)
-                named[i] = True
-        mass, left = p.sum(), 0.0
-        if rest == SCALED:
-            if mass == 0:
-                continue
-            p, mass = p / mass, torch.ones((), dtype=torch.float64)
-        on = p > 0
-        L = (p[on] * (p[on].log() - lq[on])).sum()
-        far = (x.max() - x).clamp(max=200.0) * 1.4427 * 3 * U + 8 * U  # of exp((z - reference) / temperature)
-        pull = q * 0.0
-        if rest == BUCKET and bool((z[r][~named] > -math.inf).any()):
-            left = max(0.0, 1.0 - float(mass))
-            lqr = torch.logsumexp(lq[~named], 0)
-            if left > 0:
-                L = L + left * (math.log(left) - lqr)
-            pull = torch.where(named, 0.0, left * (lq - lqr).exp())
-        b = mass + left
-        loss[r], grad[r] = w * L, (b * q - pull - p) * w / temperature
-        tol_loss[r] = abs(w) * (LN * (float(mass) + 2 * left) + 4 * U * abs(L))
-        tol_grad[r] = abs(w) / temperature * ((b * q + pull) * (LN + far + 8 * U) + p * 4 * U)
-    return loss, grad, tol_loss, tol_grad
+    x = from_largest(z) / temperature
+    lq = x - torch.logsumexp(x, 1, keepdim=True)
+    q = lq.exp()
+    at = torch.where((ids >= 0) & (ids < vocab), ids, vocab)  # one more column takes what is left out
+    p = torch.zeros(rows, vocab + 1, dtype=torch.float64, device=z.device).scatter_add_(1, at, lp.exp())[:, :vocab]
+    named = torch.zeros(rows, vocab + 1, dtype=torch.bool, device=z.device).scatter_(1, at, True)[:, :vocab]
+    mass = p.sum(1, keepdim=True)
+    if rest == SCALED:
+        p = torch.where(mass == 0, 0.0, p / mass)
+        mass = torch.where(mass == 0, 0.0, torch.ones_like(mass))
+    L = torch.where(p == 0, 0.0, p * (p.log() - lq)).sum(1, keepdim=True)
+    far = (x.amax(1, keepdim=True) - x).clamp(max=200.0) * 1.4427 * 3 * U + 8 * U  # of exp((z - reference) / temperature)
+    left, pull = torch.zeros_like(mass), torch.zeros_like(q)
+    if rest == BUCKET:
+        some = (~named & ~(z == -math.inf)).any(1, keepdim=True)
+        left = torch.where(some, (1.0 - mass).clamp(min=0.0), 0.0)
+        lqr = torch.logsumexp(torch.where(named, -math.inf, lq), 1, keepdim=True)
+        L = L + torch.where(left > 0, left * (left.log() - lqr), 0.0)
+        pull = torch.where(named | (left == 0), 0.0, left * (lq - lqr).exp())
+    b = mass + left
+    w = torch.ones_like(mass) if weight is None else weight.double()[:, None]
+    counts = (w != 0) & ~(z == -math.inf).all(1, keepdim=True)  # else nothing
+    out = (w * L, (b * q - pull - p) * w / temperature, abs(w) * (LN * (mass + 2 * left) + 4 * U * abs(L)),
+           abs(w) / temperature * ((b * q + pull) * (LN + far + 8 * U) + p * 4 * U))
+    out = [torch.where(counts, o, 0.0) for o in out]
+    return out[0][:, 0], out[1], out[2][:, 0], out[3]
 
 
 def assert_near(got, want, tol, dtype=torch.float32, what=""):
