@@ -617,7 +617,57 @@ __device__ __forceinline__ bool some_or(int id, bool v) {
   asm volatile("{.reg .pred p, q;\n setp.ne.u32 p, %1, 0;\n bar.red.or.pred q, %2, %3, p;\n selp.u32 %0, 1, 0, q;}" : "=r"(r) : "r"((uint32_t)v), "r"(id), "n"(N) : "memory");
   return r != 0;
 }
+template <int N>
+__device__ __forceinline__ uint32_t some_count(int id, bool v) {
+  uint32_t r;
+  asm volatile("{.reg .pred p;\n setp.ne.u32 p, %1, 0;\n bar.red.popc.u32 %0, %2, %3, p;}" : "=r"(r) : "r"((uint32_t)v), "r"(id), "n"(N) : "memory");
+  return r;
+}
 enum { kBarSide = 1, kBarStream = 2, kBarReady = 3, kBarDone = 5 };  // the last two: one for each of two rows
+
+// The copying thread: the whole vectors of the block's rows through the ring, every row PASSES times; false: a wait has run out.  The last
+// reading of a row leaves nothing in the L2 cache.
+template <class T, int PASSES, class F>
+__device__ bool copy_rows(const DistillArgs& a, uint64_t rows, uint4* ring, uint32_t stages, uint64_t* full, uint64_t* empty, F&& skip) {
+  uint64_t once;
+  asm("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(once));
+  uint32_t stage = 0, phase = 0;
+  bool ok = true;
+  for (uint64_t row = blockIdx.x; row < rows; row += gridDim.x) {
+    if (skip(row)) continue;
+    const RowAt R = row_at<T>(a, row);
+    for (int pass = 0; pass < PASSES; ++pass)
+      for (uint32_t v = 0; v < R.wholes; v += kStageVecs) {
+        bar_wait(&empty[stage], phase ^ 1, ok);
+        const uint32_t bytes = min(R.wholes - v, (uint32_t)kStageVecs) * 16;
+        bar_expect(&full[stage], bytes);
+        const unsigned char* const src = R.from + ((size_t)R.whole_from + v) * 16;
+        const uint32_t to = shared_at(ring + (size_t)stage * kStageVecs), bar = shared_at(&full[stage]);
+        if (pass == PASSES - 1)
+          asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1], %2, [%3], %4;" ::"r"(to), "l"(src),
+                       "r"(bytes), "r"(bar), "l"(once)
+                       : "memory");
+        else
+          asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(to), "l"(src), "r"(bytes), "r"(bar)
+                       : "memory");
+        if (++stage == stages) stage = 0, phase ^= 1;
+      }
+  }
+  bool last = true;  // no copy is left on its way, even where a wait has run out
+  for (uint32_t i = 0; i < stages; ++i) {
+    bar_wait(&empty[stage], phase ^ 1, last);
+    if (++stage == stages) stage = 0, phase ^= 1;
+  }
+  return ok && last;
+}
+// word of a row's i-th element beside its whole vectors (E of the first vector, then E of the last one), or -1
+template <int E>
+__device__ __forceinline__ int end_word(const RowAt& R, uint32_t vocab, uint32_t i) {
+  const uint32_t last = R.vecs - 1;
+  if (i >= 2 * E || !(i < E ? R.whole_from > 0 || R.wholes == 0 : last > 0 && last >= R.whole_from + R.wholes)) return -1;
+  const int w = i < E ? (int)i - (int)R.lead : (int)(last * E + i - E) - (int)R.lead;
+  return w >= 0 && w < (int)vocab ? w : -1;
+}
 
 struct RowSide {  // what the side warps know of a row
   MaxSum said, ends;        // listed words; unlisted ones in the ragged ends
@@ -658,7 +708,6 @@ __global__ void __launch_bounds__(kStreamBlock, 2) k_distill_stream(DistillArgs 
   uint4* const ring = reinterpret_cast<uint4*>(dyn);
   uint8_t* const marks_of[2] = {dyn + (size_t)stages * kStageVecs * 16, dyn + (size_t)stages * kStageVecs * 16 + mark_bytes};
   int* const records = reinterpret_cast<int*>(dyn + (size_t)stages * kStageVecs * 16 + 2 * mark_bytes);  // [2][3][k]
-  constexpr int kPasses = KIND == kDistillStep ? 2 : 1;
   const auto idle_row = [&](uint64_t row) { return a.row_weight && a.row_weight[row] == 0.f && !(KIND == kDistillLoss && a.stats); };
 
   if (tid == 0) {
@@ -670,59 +719,15 @@ __global__ void __launch_bounds__(kStreamBlock, 2) k_distill_stream(DistillArgs 
 
   bool ok = true;
   if (tid >= kStreamLanes + kSideLanes) {
-    // ---- the copying thread ----
-    if (lane == 0) {
-      uint64_t again;  // the second reading is the last
-      asm("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(again));
-      uint32_t stage = 0, phase = 0;
-      for (uint64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
-        if (idle_row(row)) continue;
-        const RowAt R = row_at<T>(a, row);
-        for (int pass = 0; pass < kPasses; ++pass)
-          for (uint32_t v = 0; v < R.wholes; v += kStageVecs) {
-            bar_wait(&empty[stage], phase ^ 1, ok);
-            const uint32_t bytes = min(R.wholes - v, (uint32_t)kStageVecs) * 16;
-            bar_expect(&full[stage], bytes);
-            const unsigned char* const src = R.from + ((size_t)R.whole_from + v) * 16;
-            if (pass == kPasses - 1)
-              asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1], %2, [%3], %4;" ::"r"(
-                               shared_at(ring + (size_t)stage * kStageVecs)),
-                           "l"(src), "r"(bytes), "r"(shared_at(&full[stage])), "l"(again)
-                           : "memory");
-            else
-              asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(
-                               shared_at(ring + (size_t)stage * kStageVecs)),
-                           "l"(src), "r"(bytes), "r"(shared_at(&full[stage]))
-                           : "memory");
-            if (++stage == stages) stage = 0, phase ^= 1;
-          }
-      }
-      // no copy is left on its way, even where a wait ran out
-      bool last = true;
-      for (uint32_t i = 0; i < stages; ++i) {
-        bar_wait(&empty[stage], phase ^ 1, last);
-        if (++stage == stages) stage = 0, phase ^= 1;
-      }
-      if (!(ok && last) && a.status) set_status(a.status, CVLC_ERR_DEVICE_TIMEOUT);
-    }
+    if (lane == 0 && !copy_rows<T, KIND == kDistillStep ? 2 : 1>(a, a.rows, ring, stages, full, empty, idle_row) && a.status)
+      set_status(a.status, CVLC_ERR_DEVICE_TIMEOUT);
     return;
   }
 
   if (tid >= kStreamLanes) {
     // ---- the side warps: records, ragged ends, losses ----
     const uint32_t t = tid - kStreamLanes, side = t >> 5;
-    struct Ends {
-      int word;  // of the lane, or -1
-      float z;
-    };
-    // words of the vectors that are not whole: of the first one and, behind them, of the last one
-    const auto end_word = [&](const RowAt& R) {
-      if (side != 0 || lane >= 2 * E) return -1;
-      const uint32_t last = R.vecs - 1;
-      const bool first_ragged = R.whole_from > 0 || R.wholes == 0, last_ragged = last > 0 && last >= R.whole_from + R.wholes;
-      const int w = lane < E ? (int)lane - (int)R.lead : (int)(last * E + lane - E) - (int)R.lead;
-      return (lane < E ? first_ragged : last_ragged) && w >= 0 && w < (int)a.vocab ? w : -1;
-    };
+    const auto end_of = [&](const RowAt& R) { return side == 0 ? end_word<E>(R, a.vocab, lane) : -1; };
     const auto prepare = [&](uint64_t row, uint32_t buf) {
       some_sync<kSideLanes>(kBarSide);  // the row before the last one is finished, its marks cleared
       const RowAt R = row_at<T>(a, row);
@@ -732,7 +737,7 @@ __global__ void __launch_bounds__(kStreamBlock, 2) k_distill_stream(DistillArgs 
       float* const prob = reinterpret_cast<float*>(at + a.k);
       float* const logit = prob + a.k;
       bool twice = false;
-      const int end = end_word(R);
+      const int end = end_of(R);
       const float end_z = end >= 0 ? to_float(z[end]) : -CUDART_INF_F;
       for (uint32_t i = t; i < a.k; i += kSideLanes) {
         const int id = a.ids[row * a.k + i];
@@ -841,7 +846,7 @@ __global__ void __launch_bounds__(kStreamBlock, 2) k_distill_stream(DistillArgs 
       T* const g = static_cast<T*>(a.grad) + row * a.grad_stride;
       const float scale = weight / a.temperature;
       if (KIND != kDistillLoss) {
-        const int end = end_word(R);
+        const int end = end_of(R);
         if (end >= 0 && !(marks[(end + R.lead) >> 3] >> ((end + R.lead) & 7) & 1)) {
           const float z = to_float((reinterpret_cast<const T*>(R.from) + R.lead)[end]);
           g[end] = from_float<T>(w.a * scale * exp2_fast((z - w.ref) * c2));
@@ -905,6 +910,7 @@ __global__ void __launch_bounds__(kStreamBlock, 2) k_distill_stream(DistillArgs 
         }
         add_batch<T, 2>(raw, c2, acc);
       }
+      if (!ok) acc.sum = CUDART_NAN_F;  // a wait has run out: the row is void
       acc = warp_join(acc, c2);
       if (lane == 0) sides[buf].rest[tid >> 5] = acc;
       __syncwarp();
@@ -1007,21 +1013,24 @@ cudaError_t launch_rows(int id, void (*kernel)(Params...), uint64_t rows, const 
   return e != cudaSuccess ? e : last;
 }
 
+// where blocks go from row to row: rows enough for all SMs, and long enough for a few stages each
+bool streamed(uint64_t rows, uint64_t bytes) { return rows >= kNumSM && bytes >= 2 * kStageVecs * 16; }
+unsigned stream_grid(uint64_t rows) { return (unsigned)(rows < 2 * kNumSM ? rows : 2 * kNumSM); }
+
 template <class T, DistillKind KIND>
 cudaError_t distill_typed(const DistillArgs& a, cudaStream_t st) {
   // many long rows: two blocks an SM go from row to row, where two rows' marks and three stages fit
   const uint32_t mark_row = (a.vocab + 2 * kPerVec<T> + 127) / 128 * 16;
   const size_t beside = 2 * (size_t)mark_row + (size_t)a.k * 24;
-  if (a.rows >= kNumSM && (uint64_t)a.vocab * sizeof(T) >= 2 * kStageVecs * 16 && beside + 3 * kStageVecs * 16 <= kStreamShared) {
+  if (streamed(a.rows, (uint64_t)a.vocab * sizeof(T)) && beside + 3 * kStageVecs * 16 <= kStreamShared) {
     const uint32_t fit = (uint32_t)((kStreamShared - beside) / (kStageVecs * 16));
     const uint32_t stages = fit < kStagesMost ? fit : kStagesMost;
     const size_t smem = (size_t)stages * kStageVecs * 16 + beside;
     void (*const kernel)(DistillArgs, uint32_t, uint32_t) = k_distill_stream<T, KIND>;
     const cudaError_t e = allow_shared(kernel, smem);
     if (e != cudaSuccess) return e;
-    const uint64_t grid = a.rows < 2 * kNumSM ? a.rows : 2 * kNumSM;
-    launch_kernel(KIND == kDistillLoss ? kKDistillLoss : KIND == kDistillGrad ? kKDistillGrad : kKDistillStep, kernel, dim3((unsigned)grid),
-                  dim3(kStreamBlock), smem, st, false, a, stages, mark_row);
+    launch_kernel(KIND == kDistillLoss ? kKDistillLoss : KIND == kDistillGrad ? kKDistillGrad : kKDistillStep, kernel,
+                  dim3(stream_grid(a.rows)), dim3(kStreamBlock), smem, st, false, a, stages, mark_row);
     return cudaGetLastError();
   }
   constexpr int NV = KIND == kDistillStep ? 8 : 4;
@@ -1059,12 +1068,14 @@ __device__ __forceinline__ unsigned long long candidate(uint32_t order, uint32_t
   return ((unsigned long long)order << 32) | (uint32_t)~word;
 }
 
+constexpr uint32_t kBoundStep = 1u << 13;  // 2^-10 of a value: not worth another round
+
 struct TopPart {
   MaxSum all;
   uint32_t bound;
 };
 
-// The largest bound from `lo` on that `want` of the block's threads reach with theirs (`lo` if it is none, or finer than 2^12 apart)
+// The largest bound from `lo` on that `want` of the block's threads reach with theirs (`lo` if it is none), to kBoundStep
 __device__ __forceinline__ uint32_t raise_bound(uint32_t top, uint32_t want, uint32_t lo, uint32_t* largest) {
   const uint32_t of_warp = __reduce_max_sync(kFull, top);
   if ((threadIdx.x & 31) == 0) atomicMax(largest, of_warp);
@@ -1072,7 +1083,7 @@ __device__ __forceinline__ uint32_t raise_bound(uint32_t top, uint32_t want, uin
   if (n < want) return lo;
   uint32_t hi = *largest;
   __syncthreads();  // all have read it: the next call adds to it
-  while (hi > lo && hi - lo > 4096) {
+  while (hi > lo && hi - lo > kBoundStep) {
     const uint32_t mid = lo + (hi - lo) / 2;
     n = __syncthreads_count(top >= mid);
     if (n >= want) lo = mid;
@@ -1082,17 +1093,17 @@ __device__ __forceinline__ uint32_t raise_bound(uint32_t top, uint32_t want, uin
   return lo;
 }
 
-// Elements from `least` on (a candidate: value and word) of a batch, into a list of `room`
-template <class T, int NV>
-__device__ __forceinline__ void list_batch(const Row<T>& R, const uint4 (&raw)[NV], uint32_t from, unsigned long long least, uint32_t* count,
-                                           unsigned long long* to, uint32_t room) {
+// Elements from `least` on (a candidate: value and word) of some vectors, into a list of `room`; word_of(j): the first word of the j-th
+template <class T, int NV, class F>
+__device__ __forceinline__ void list_batch(const uint4 (&raw)[NV], F&& word_of, unsigned long long least, uint32_t* count, unsigned long long* to,
+                                           uint32_t room) {
   const float floor_value = value_of((uint32_t)(least >> 32));
 #pragma unroll
   for (int j = 0; j < NV; ++j) {
     if (!(vec_max<T>(raw[j]) >= floor_value)) continue;
     float f[kPerVec<T>];
     widen<T>(raw[j], f);
-    const int word = R.word(R.first + (from + j) * R.apart);
+    const int word = word_of(j);
 #pragma unroll
     for (int e = 0; e < kPerVec<T>; ++e) {
       if (!(f[e] >= floor_value)) continue;
@@ -1101,6 +1112,106 @@ __device__ __forceinline__ void list_batch(const Row<T>& R, const uint4 (&raw)[N
       const uint32_t n = atomicAdd(count, 1u);
       if (n < room) to[n] = c;
     }
+  }
+}
+
+// Digits of the candidates of some vectors that share a prefix, counted; equal ones in a row at once
+template <class T>
+struct DigitCount {
+  uint32_t* hist;
+  uint32_t last, run;
+  __device__ __forceinline__ void one(float f, uint32_t word, unsigned long long prefix, int shift) {
+    if (!(f > -CUDART_INF_F)) return;
+    const unsigned long long c = candidate(order_of(f), word);
+    if (shift < 56 && (c >> (shift + 8)) != prefix) return;
+    const uint32_t digit = (uint32_t)(c >> shift) & 255u;
+    if (run && digit != last) {
+      atomicAdd(&hist[last], run);
+      run = 0;
+    }
+    last = digit;
+    ++run;
+  }
+  __device__ __forceinline__ void vec(const uint4& raw, int word, unsigned long long prefix, int shift) {
+    float f[kPerVec<T>];
+    widen<T>(raw, f);
+#pragma unroll
+    for (int e = 0; e < kPerVec<T>; ++e) one(f[e], (uint32_t)(word + e), prefix, shift);
+  }
+  __device__ __forceinline__ void done() {
+    if (run) atomicAdd(&hist[last], run);
+  }
+};
+// The digit that holds rank `left` from the largest down, and how many lie above it; by a warp, eight digits a lane
+template <class F>
+__device__ __forceinline__ void pick_digit(F&& count_of, uint32_t left, uint32_t* picked, uint32_t* above) {
+  const uint32_t lane = threadIdx.x & 31;
+  uint32_t n[8], sum = 0;
+#pragma unroll
+  for (int d = 0; d < 8; ++d) {
+    n[d] = count_of(255 - (lane * 8 + d));
+    sum += n[d];
+  }
+  uint32_t before = sum;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const uint32_t v = __shfl_up_sync(kFull, before, o);
+    if (lane >= (uint32_t)o) before += v;
+  }
+  before -= sum;
+#pragma unroll
+  for (int d = 0; d < 8; ++d) {
+    if (before < left && left <= before + n[d]) *picked = 255 - (lane * 8 + d), *above = before;
+    before += n[d];
+  }
+}
+
+// A row's records from its candidates, whose order is any, by `nt` threads that meet at sync(): `t` is the thread's number
+template <class F>
+__device__ __forceinline__ void put_records(const TopArgs& a, uint64_t row, const MaxSum& all, unsigned long long* packed, uint32_t n, uint32_t t,
+                                            uint32_t nt, F&& sync) {
+  const double it = 1.0 / (double)a.temperature, ln_sum = log((double)all.sum);
+  auto put = [&](uint32_t at, unsigned long long c) {
+    a.ids[row * a.k + at] = (int32_t)~(uint32_t)c;
+    a.logp[row * a.k + at] = (float)(((double)value_of((uint32_t)(c >> 32)) - (double)all.max) * it - ln_sum);
+  };
+  if (n <= 4 * nt) {  // a few for each thread: a candidate's rank is the number of larger ones
+    for (uint32_t i = t; i < n; i += nt) {
+      const unsigned long long c = packed[i];
+      uint32_t larger = 0, o = 0;
+      for (; o + 2 <= n; o += 2) {
+        const ulonglong2 p = *reinterpret_cast<const ulonglong2*>(packed + o);
+        larger += (p.x > c) + (p.y > c);
+      }
+      if (o < n) larger += packed[o] > c;
+      if (larger < a.k) put(larger, c);
+    }
+  } else {  // sorted in pairs, the largest first
+    uint32_t size = 2;
+    while (size < n) size *= 2;
+    for (uint32_t i = n + t; i < size; i += nt) packed[i] = 0;
+    sync();
+    for (uint32_t length = 2; length <= size; length *= 2)
+      for (uint32_t apart = length / 2; apart; apart /= 2) {
+        for (uint32_t i = t; i < size / 2; i += nt) {
+          const uint32_t x = i / apart * 2 * apart + i % apart, y = x + apart;
+          const unsigned long long p = packed[x], q = packed[y];
+          if ((p < q) == ((x & length) == 0)) packed[x] = q, packed[y] = p;
+        }
+        sync();
+      }
+    for (uint32_t i = t; i < a.k && i < n; i += nt) put(i, packed[i]);
+  }
+  for (uint32_t i = n + t; i < a.k; i += nt) {  // fewer words than records: the others are masked
+    a.ids[row * a.k + i] = -1;
+    a.logp[row * a.k + i] = -CUDART_INF_F;
+  }
+}
+// ... of a row without a softmax
+__device__ __forceinline__ void put_spoiled(const TopArgs& a, uint64_t row, uint32_t t, uint32_t nt) {
+  for (uint32_t i = t; i < a.k; i += nt) {
+    a.ids[row * a.k + i] = (int32_t)i;
+    a.logp[row * a.k + i] = CUDART_NAN_F;
   }
 }
 
@@ -1136,7 +1247,7 @@ __global__ void __launch_bounds__(kRowThreads, 2) k_top_logits(TopArgs a, uint32
     if (b + 1 < batches) load_batch<T, NV>(R, (b + 1) * NV, ahead);
     add_batch<T, NV>(raw, c2, acc);
     if (b + 1 == batches || (blocks == 1 && (b & (b + 1)) == 0)) bound = raise_bound(order_of(acc.max), want, bound, &largest);
-    if (blocks == 1) list_batch<T, NV>(R, raw, b * NV, (unsigned long long)bound << 32, &mine, list, stretch);
+    if (blocks == 1) list_batch<T, NV>(raw, [&](int j) { return R.word(R.first + (b * NV + j) * R.apart); }, (unsigned long long)bound << 32, &mine, list, stretch);
     if (++b >= batches) break;
 #pragma unroll
     for (int j = 0; j < NV; ++j) raw[j] = ahead[j];
@@ -1149,7 +1260,7 @@ __global__ void __launch_bounds__(kRowThreads, 2) k_top_logits(TopArgs a, uint32
     unsigned long long* const to = (blocks > 1 ? cluster.map_shared_rank(list, 0) : list) + rank * stretch;
     for (uint32_t b = 0; b < batches; ++b) {
       if (batches > 1) load_batch<T, NV>(R, b * NV, raw);
-      list_batch<T, NV>(R, raw, b * NV, least, &mine, to, stretch);
+      list_batch<T, NV>(raw, [&](int j) { return R.word(R.first + (b * NV + j) * R.apart); }, least, &mine, to, stretch);
     }
     __syncthreads();
     if (tid < blocks) *(blocks > 1 ? cluster.map_shared_rank(&counts[rank], tid) : &counts[rank]) = mine;
@@ -1184,53 +1295,23 @@ __global__ void __launch_bounds__(kRowThreads, 2) k_top_logits(TopArgs a, uint32
     for (int shift = 56; shift >= 0; shift -= 8) {
       for (uint32_t i = tid; i < 256; i += nt) hist[i] = 0;
       __syncthreads();
-      uint32_t last = 0, run = 0;  // equal digits in a row are counted at once
+      DigitCount<T> digits = {hist, 0, 0};
       for (uint32_t b = 0; b < batches; ++b) {
         if (batches > 1) load_batch<T, NV>(R, b * NV, raw);
 #pragma unroll
-        for (int j = 0; j < NV; ++j) {
-          float f[kPerVec<T>];
-          widen<T>(raw[j], f);
-          const int word = R.word(R.first + (b * NV + j) * R.apart);
-#pragma unroll
-          for (int e = 0; e < kPerVec<T>; ++e) {
-            if (!(f[e] > -CUDART_INF_F)) continue;
-            const unsigned long long c = candidate(order_of(f[e]), (uint32_t)(word + e));
-            if (shift < 56 && (c >> (shift + 8)) != prefix) continue;
-            const uint32_t digit = (uint32_t)(c >> shift) & 255u;
-            if (run && digit != last) {
-              atomicAdd(&hist[last], run);
-              run = 0;
-            }
-            last = digit;
-            ++run;
-          }
-        }
+        for (int j = 0; j < NV; ++j) digits.vec(raw[j], R.word(R.first + (b * NV + j) * R.apart), prefix, shift);
       }
-      if (run) atomicAdd(&hist[last], run);
+      digits.done();
       if (blocks > 1) cluster.sync();
       else __syncthreads();
-      if (tid < 32) {  // eight digits a lane, from the largest down
-        uint32_t n[8], sum = 0;
-#pragma unroll
-        for (int d = 0; d < 8; ++d) {
-          n[d] = 0;
-          for (uint32_t r = 0; r < blocks; ++r) n[d] += (blocks > 1 ? cluster.map_shared_rank(hist, r) : hist)[255 - (tid * 8 + d)];
-          sum += n[d];
-        }
-        uint32_t before = sum;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-          const uint32_t v = __shfl_up_sync(kFull, before, o);
-          if (tid >= (uint32_t)o) before += v;
-        }
-        before -= sum;
-#pragma unroll
-        for (int d = 0; d < 8; ++d) {
-          if (before < left && left <= before + n[d]) picked = 255 - (tid * 8 + d), above = before;
-          before += n[d];
-        }
-      }
+      if (tid < 32)
+        pick_digit(
+            [&](uint32_t d) {
+              uint32_t n = 0;
+              for (uint32_t r = 0; r < blocks; ++r) n += (blocks > 1 ? cluster.map_shared_rank(hist, r) : hist)[d];
+              return n;
+            },
+            left, &picked, &above);
       __syncthreads();
       prefix = (prefix << 8) | picked;
       left -= above;
@@ -1245,10 +1326,7 @@ __global__ void __launch_bounds__(kRowThreads, 2) k_top_logits(TopArgs a, uint32
 
   if (rank != 0) return;
   if (spoiled) {
-    for (uint32_t i = tid; i < a.k; i += nt) {
-      a.ids[row * a.k + i] = (int32_t)i;
-      a.logp[row * a.k + i] = CUDART_NAN_F;
-    }
+    put_spoiled(a, row, tid, nt);
     return;
   }
   // what the last bound leaves, in any order
@@ -1260,45 +1338,175 @@ __global__ void __launch_bounds__(kRowThreads, 2) k_top_logits(TopArgs a, uint32
     }
   }
   __syncthreads();
-  const uint32_t n = kept;
-  const double it = 1.0 / (double)a.temperature, ln_sum = log((double)all.sum);
-  auto put = [&](uint32_t at, unsigned long long c) {
-    a.ids[row * a.k + at] = (int32_t)~(uint32_t)c;
-    a.logp[row * a.k + at] = (float)(((double)value_of((uint32_t)(c >> 32)) - (double)all.max) * it - ln_sum);
-  };
-  if (n <= nt) {  // one for each thread: its rank is the number of larger ones
-    const unsigned long long c = tid < n ? packed[tid] : 0;
-    uint32_t larger = 0, o = 0;
-    for (; o + 2 <= n; o += 2) {
-      const ulonglong2 p = *reinterpret_cast<const ulonglong2*>(packed + o);
-      larger += (p.x > c) + (p.y > c);
-    }
-    if (o < n) larger += packed[o] > c;
-    if (tid < n && larger < a.k) put(larger, c);
-  } else {  // sorted in pairs, the largest first
-    uint32_t size = 2;
-    while (size < n) size *= 2;
-    for (uint32_t i = n + tid; i < size; i += nt) packed[i] = 0;
-    __syncthreads();
-    for (uint32_t length = 2; length <= size; length *= 2)
-      for (uint32_t apart = length / 2; apart; apart /= 2) {
-        for (uint32_t i = tid; i < size / 2; i += nt) {
-          const uint32_t x = i / apart * 2 * apart + i % apart, y = x + apart;
-          const unsigned long long p = packed[x], q = packed[y];
-          if ((p < q) == ((x & length) == 0)) packed[x] = q, packed[y] = p;
-        }
-        __syncthreads();
-      }
-    for (uint32_t i = tid; i < a.k && i < n; i += nt) put(i, packed[i]);
+  put_records(a, row, all, packed, kept, tid, nt, [] { __syncthreads(); });
+}
+
+// Many long rows: as in k_distill_stream, a block goes from row to row, and the side warps rank what the pass over a row has listed while the
+// next row is passed over.  (2048 x 131072 bf16, k = 64: a block for every row 200 us.)
+struct RowTop {
+  MaxSum of_warp[kStreamWarps];
+  uint32_t count, bound;
+};
+template <class T>
+__global__ void __launch_bounds__(kStreamBlock, 2) k_top_stream(TopArgs a, uint32_t stages) {
+  extern __shared__ __align__(128) unsigned char dyn[];
+  __shared__ uint64_t full[kStagesMost], empty[kStagesMost];
+  __shared__ RowTop tops[2];
+  __shared__ uint32_t hist[256];
+  __shared__ uint32_t mine, picked, above, largest[2], kept;
+  constexpr int E = kPerVec<T>;
+  const uint32_t tid = threadIdx.x, lane = tid & 31;
+  const float c2 = a.c2;
+  uint4* const ring = reinterpret_cast<uint4*>(dyn);
+  unsigned long long* const lists = reinterpret_cast<unsigned long long*>(dyn + (size_t)stages * kStageVecs * 16);  // [2], then the ranking's
+  DistillArgs where = {};
+  where.logits = a.logits, where.row_stride = a.row_stride, where.vocab = a.vocab;
+
+  if (tid == 0) {
+    for (uint32_t i = 0; i < stages; ++i) bar_init(&full[i], 1), bar_init(&empty[i], kStreamWarps);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    mine = kept = 0;
   }
-  for (uint32_t i = n + tid; i < a.k; i += nt) {  // fewer words than records: the others are masked
-    a.ids[row * a.k + i] = -1;
-    a.logp[row * a.k + i] = -CUDART_INF_F;
+  __syncthreads();
+  bool ok = true;
+  if (tid >= kStreamLanes + kSideLanes) {
+    if (lane == 0) copy_rows<T, 1>(where, a.rows, ring, stages, full, empty, [](uint64_t) { return false; });
+    return;
+  }
+  if (tid >= kStreamLanes) {
+    const uint32_t t = tid - kStreamLanes;
+    unsigned long long* const packed = lists + 2 * kTopList;
+    uint32_t buf = 0;
+    some_arrive<kStreamLanes + kSideLanes>(kBarReady);
+    for (uint64_t row = blockIdx.x; row < a.rows; row += gridDim.x, buf ^= 1) {
+      if (row + gridDim.x < a.rows) some_arrive<kStreamLanes + kSideLanes>(kBarReady + (buf ^ 1));  // the next row's list is free
+      some_sync<kStreamLanes + kSideLanes>(kBarDone + buf);
+      const RowTop& s = tops[buf];
+      const MaxSum all = join_warps(s.of_warp, kStreamWarps, c2);
+      if (!(all.sum < CUDART_INF_F)) {
+        put_spoiled(a, row, t, kSideLanes);
+      } else {
+        const unsigned long long* const list = lists + buf * kTopList;
+        const uint32_t c = s.count, bound = s.bound;
+        for (uint32_t i = t; i < c; i += kSideLanes)
+          if ((uint32_t)(list[i] >> 32) >= bound) packed[atomicAdd(&kept, 1u)] = list[i];
+        some_sync<kSideLanes>(kBarSide);
+        put_records(a, row, all, packed, kept, t, kSideLanes, [] { some_sync<kSideLanes>(kBarSide); });
+        some_sync<kSideLanes>(kBarSide);
+        if (t == 0) kept = 0;
+      }
+      some_sync<kSideLanes>(kBarSide);
+    }
+    return;
+  }
+
+  uint32_t stage = 0, phase = 0, buf = 0;
+  for (uint64_t row = blockIdx.x; row < a.rows; row += gridDim.x, buf ^= 1) {
+    const RowAt R = row_at<T>(where, row);
+    const T* const z = reinterpret_cast<const T*>(R.from) + R.lead;
+    const int end = end_word<E>(R, a.vocab, tid);  // ends of the row beside its whole vectors: one for a thread
+    const float end_z = end >= 0 ? to_float(z[end]) : -CUDART_INF_F;
+    some_sync<kStreamLanes + kSideLanes>(kBarReady + buf);
+    if (tid == 0) mine = 0, largest[0] = largest[1] = 0;
+    some_sync<kStreamLanes>(kBarStream);
+    unsigned long long* const list = lists + buf * kTopList;
+    MaxSum acc = {end_z, end_z == -CUDART_INF_F ? 0.f : end_z < CUDART_INF_F ? 1.f : CUDART_NAN_F};
+    if (end_z != end_z) acc.max = -CUDART_INF_F;
+    uint32_t bound = kOrderNegInf + 1, raised = 0;
+    const uint32_t cuts = (R.wholes + kStageVecs - 1) / kStageVecs;
+    const auto list_end = [&](unsigned long long least) {
+      if (end_z > -CUDART_INF_F) {
+        const unsigned long long c = candidate(order_of(end_z), (uint32_t)end);
+        if (c >= least) {
+          const uint32_t n = atomicAdd(&mine, 1u);
+          if (n < kTopList) list[n] = c;
+        }
+      }
+    };
+    for (uint32_t b = 0; b < cuts; ++b) {
+      const uint32_t v = b * kStageVecs + tid;
+      bar_wait(&full[stage], phase, ok);
+      uint4 raw[2];
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+        raw[j] = v + j * kStreamLanes < R.wholes ? ring[(size_t)stage * kStageVecs + tid + j * kStreamLanes] : nothing<T>();
+      release_stage(&empty[stage]);
+      if (++stage == stages) stage = 0, phase ^= 1;
+      add_batch<T, 2>(raw, c2, acc);
+      if (b + 1 == cuts || (b & (b + 1)) == 0) {
+        // raise_bound() among the stream warps; two places for the largest, in turn: who writes one again has met all readers at the other
+        const uint32_t top = order_of(acc.max);
+        uint32_t* const most = &largest[raised++ & 1];
+        const uint32_t of_warp = __reduce_max_sync(kFull, top);
+        if (lane == 0) atomicMax(most, of_warp);
+        uint32_t n = some_count<kStreamLanes>(kBarStream, top >= bound);
+        if (n >= a.k) {
+          uint32_t hi = *most;
+          while (hi > bound && hi - bound > kBoundStep) {
+            const uint32_t mid = bound + (hi - bound) / 2;
+            n = some_count<kStreamLanes>(kBarStream, top >= mid);
+            if (n >= a.k) bound = mid;
+            else hi = mid - 1;
+            if (n == a.k) break;
+          }
+        }
+      }
+      list_batch<T, 2>(raw, [&](int j) { return (int)((R.whole_from + v + j * kStreamLanes) * E) - (int)R.lead; }, (unsigned long long)bound << 32,
+                       &mine, list, kTopList);
+    }
+    list_end((unsigned long long)bound << 32);
+    if (!ok) acc.sum = CUDART_NAN_F;  // a wait has run out: the row is void
+    const MaxSum warp = warp_join(acc, c2);
+    if (lane == 0) tops[buf].of_warp[tid >> 5] = warp;
+    some_sync<kStreamLanes>(kBarStream);
+    if (mine > kTopList) {
+      // the k-th largest candidate, eight bits at a time, read again from global memory
+      unsigned long long prefix = 0;
+      uint32_t left = a.k;
+      const uint4* const from = reinterpret_cast<const uint4*>(R.from) + R.whole_from;
+      for (int shift = 56; shift >= 0; shift -= 8) {
+        if (tid < 256) hist[tid] = 0;
+        some_sync<kStreamLanes>(kBarStream);
+        DigitCount<T> digits = {hist, 0, 0};
+        for (uint32_t i = tid; i < R.wholes; i += kStreamLanes)
+          digits.vec(__ldg(from + i), (int)((R.whole_from + i) * E) - (int)R.lead, prefix, shift);
+        digits.one(end_z, (uint32_t)end, prefix, shift);
+        digits.done();
+        some_sync<kStreamLanes>(kBarStream);
+        if (tid < 32) pick_digit([&](uint32_t d) { return hist[d]; }, left, &picked, &above);
+        some_sync<kStreamLanes>(kBarStream);
+        prefix = (prefix << 8) | picked;
+        left -= above;
+      }
+      some_sync<kStreamLanes>(kBarStream);
+      if (tid == 0) mine = 0;
+      some_sync<kStreamLanes>(kBarStream);
+      for (uint32_t i = tid; i < R.wholes; i += kStreamLanes) {
+        const uint4 raw[1] = {__ldg(from + i)};
+        list_batch<T, 1>(raw, [&](int) { return (int)((R.whole_from + i) * E) - (int)R.lead; }, prefix, &mine, list, kTopList);
+      }
+      list_end(prefix);
+      bound = (uint32_t)(prefix >> 32);
+      some_sync<kStreamLanes>(kBarStream);
+    }
+    if (tid == 0) tops[buf].count = min(mine, kTopList), tops[buf].bound = bound;
+    __threadfence_block();
+    some_arrive<kStreamLanes + kSideLanes>(kBarDone + buf);
   }
 }
 
 template <class T>
 cudaError_t top_typed(const TopArgs& a, cudaStream_t st) {
+  if (streamed(a.rows, (uint64_t)a.vocab * sizeof(T))) {
+    const size_t beside = 3 * kTopList * 8;
+    const uint32_t stages = (uint32_t)((kStreamShared - beside) / (kStageVecs * 16));
+    const size_t smem = (size_t)stages * kStageVecs * 16 + beside;
+    void (*const kernel)(TopArgs, uint32_t) = k_top_stream<T>;
+    const cudaError_t e = allow_shared(kernel, smem);
+    if (e != cudaSuccess) return e;
+    launch_kernel(kKTopLogits, kernel, dim3(stream_grid(a.rows)), dim3(kStreamBlock), smem, st, false, a, stages);
+    return cudaGetLastError();
+  }
   constexpr int NV = 4;
   Cut c = cut_rows(a.logits, a.row_stride, a.rows, a.vocab, sizeof(T), NV, 0);
   // the bound is the better the more threads the row's elements are spread over

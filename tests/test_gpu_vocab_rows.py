@@ -99,6 +99,18 @@ def test_top_logits_spoiled_rows(dtype):
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("kind,lead,pad,k", [("normal", 0, 0, 64), ("ties", 1, 1, 256), ("equal", 0, 3, 20), ("masked", 3, 0, 100), ("lowest", 0, 8, 256),
+                                             ("zeros", 5, 0, 33), ("far", 0, 1, 1), ("front", 1, 0, 200)])
+def test_top_logits_of_many_long_rows(dtype, kind, lead, pad, k):
+    """more rows than blocks, each of several stages"""
+    B = binding()
+    z, _ = logits_of(610, 35000 // torch.finfo(dtype).bits * 16 + 7, dtype, seed=k, kind=kind, pad=pad, lead=lead)
+    if kind == "normal":
+        z[3, 5], z[4, 7], z[300] = math.nan, math.inf, -math.inf
+    check_top(B, z, k, 0.7)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("kind", ["normal", "equal"])
 def test_top_logits_of_more_words_than_a_cluster_keeps(dtype, kind):
     B = binding()
@@ -112,13 +124,13 @@ def records(z, k, tau, seed, kind="top"):
     """a teacher near the student, and its k records; `kind`: how they are laid out"""
     g = torch.Generator().manual_seed(seed)
     rows, vocab = z.shape
-    t = torch.nan_to_num(z.double().cpu(), neginf=-40.0).clamp(-40, 40) + torch.randn(rows, vocab, generator=g)
+    t = torch.nan_to_num(z.double(), neginf=-40.0).clamp(-40, 40) + torch.randn(rows, vocab, generator=g).to(z.device)
     lp = torch.log_softmax(t / tau, 1)
     if kind == "any":  # words drawn with repetition
         ids = torch.randint(0, vocab, (rows, k), generator=g)
         lp = torch.log_softmax(torch.randn(rows, k, generator=g), 1)
     else:
-        lp, ids = torch.topk(lp, k, dim=1)
+        lp, ids = [r.cpu() for r in torch.topk(lp, k, dim=1)]
     if kind == "twice":  # two clients' lists
         ids = torch.cat([ids, ids.flip(1)], 1)
         lp = torch.cat([lp + math.log(0.25), lp.flip(1) + math.log(0.75)], 1)

@@ -49,9 +49,10 @@ def top(logits, k, temperature):
 def distill(logits, ids, logp, rest, temperature, weight=None):
     """loss, gradient, and how far each may be off before it is rounded to the logits' type"""
     few = max(1, (1 << 24) // logits.shape[1])
+    ids, logp = ids.to(logits.device), logp.to(logits.device)
     parts = [_distill_rows(logits[i:i + few], ids[i:i + few], logp[i:i + few], rest, temperature,
                            None if weight is None else weight[i:i + few]) for i in range(0, logits.shape[0], few)]
-    return tuple(torch.cat(p).cpu() for p in zip(*parts))
+    return tuple(torch.cat(p) for p in zip(*parts))
 
 
 def _distill_rows(logits, ids, logp, rest, temperature, weight):
@@ -87,14 +88,14 @@ def _distill_rows(logits, ids, logp, rest, temperature, weight):
 
 def assert_near(got, want, tol, dtype=torch.float32, what=""):
     """equal where the definition is not finite; else within tol, rounded to dtype"""
-    got, want = got.double().cpu(), want.double()
+    got, want = got.double(), want.double().to(got.device)
     assert got.shape == want.shape
     odd = ~torch.isfinite(want)
     assert torch.equal(torch.isnan(got[odd]), torch.isnan(want[odd])), what
     inf = torch.isinf(want)
     assert torch.equal(got[inf], want[inf]), what
     off = (got - want).abs()[~odd]
-    tol = torch.as_tensor(tol).expand(want.shape)[~odd]
+    tol = torch.as_tensor(tol).to(got.device).expand(want.shape)[~odd]
     most = tol * (1 + half_step(dtype)) + want[~odd].abs() * half_step(dtype) + tiny(dtype)
     bad = ~(off <= most)
     assert not bad.any(), (what, int(bad.sum()), float((off / most).max()))
