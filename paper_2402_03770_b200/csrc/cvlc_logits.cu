@@ -168,8 +168,8 @@ __device__ __forceinline__ void add_batch(const uint4 (&raw)[NV], float c2, MaxS
     widen<T>(raw[j], f);
 #pragma unroll
     for (int e = 0; e < kPerVec<T>; e += 2) {
-      const float2 x = mul2(add2(make_float2(f[e], f[e + 1]), less), by);
-      sum = add2(sum, make_float2(exp2_fast(x.x), exp2_fast(x.y)));
+      const float2 x = __fmul2_rn(__fadd2_rn(make_float2(f[e], f[e + 1]), less), by);
+      sum = __fadd2_rn(sum, make_float2(exp2_fast(x.x), exp2_fast(x.y)));
     }
   }
   acc = {m, sum.x + sum.y};
@@ -505,8 +505,8 @@ __global__ void __launch_bounds__(kRowThreads, 2) k_distill(DistillArgs a, uint3
       widen<T>(raw[j], f);
 #pragma unroll
       for (int e = 0; e < kPerVec<T>; e += 2) {
-        const float2 x = mul2(add2(make_float2(f[e], f[e + 1]), make_float2(-w.ref, -w.ref)), make_float2(c2, c2));
-        const float2 y = mul2(make_float2(exp2_fast(x.x), exp2_fast(x.y)), make_float2(ca, ca));
+        const float2 x = __fmul2_rn(__fadd2_rn(make_float2(f[e], f[e + 1]), make_float2(-w.ref, -w.ref)), make_float2(c2, c2));
+        const float2 y = __fmul2_rn(make_float2(exp2_fast(x.x), exp2_fast(x.y)), make_float2(ca, ca));
         f[e] = y.x, f[e + 1] = y.y;
       }
       raw[j] = idle ? make_uint4(0, 0, 0, 0) : narrow<T>(f);
@@ -555,14 +555,15 @@ __global__ void __launch_bounds__(kRowThreads, 2) k_distill(DistillArgs a, uint3
 // Everything that a row needs beside its elements (records, sums, logarithms) takes a block about as long as reading 64 KB does, whoever does
 // it.  So where rows are many it is done by warps of their own, beside the pass over the elements: a row's records are prepared while
 // the row before it is passed over, and its loss, its listed words and its ragged ends are finished while the row behind it is.  One
-// thread copies the rows through a ring of stages in shared memory (cp.async.bulk), one thread's pair of vectors a stage; the step
+// thread copies the rows through a ring of stages in shared memory (cp.async.bulk), four vectors of every thread a stage; the step
 // copies every row twice, the second time out of the L2 cache, which holds the 296 rows on their way (76 MB at 131,072 words of 16
 // bits).  Keeping the row in the cluster's registers instead costs every block of the cluster all of the above:
 // 4096 x 131072 bf16 750 us.
-constexpr int kStreamWarps = 16, kSideWarps = 3;  // and one that copies: twenty warps leave each of two blocks 48 registers a thread
+constexpr int kStreamWarps = 8, kSideWarps = 3;  // and one that copies
 constexpr int kStreamLanes = kStreamWarps * 32, kSideLanes = kSideWarps * 32;
 constexpr int kStreamBlock = kStreamLanes + kSideLanes + 32;
-constexpr int kStageVecs = 2 * kStreamLanes;  // vectors of a stage: 16 KB
+constexpr int kStageShare = 4;  // vectors of a thread in a stage: with two, waiting for it and giving it back were a third of the instructions
+constexpr int kStageVecs = kStageShare * kStreamLanes;  // 16 KB
 constexpr int kStagesMost = 8;
 constexpr size_t kStreamShared = 110 * 1024;  // of a block, two of which share an SM
 
@@ -589,15 +590,23 @@ __device__ __forceinline__ void bar_arrive(uint64_t* b) { asm volatile("mbarrier
 __device__ __forceinline__ void bar_expect(uint64_t* b, uint32_t bytes) {
   asm volatile("mbarrier.arrive.expect_tx.shared.b64 _, [%0], %1;" ::"r"(shared_at(b)), "r"(bytes) : "memory");
 }
+// The side warps and the copying one come first: the scheduler prefers older warps, and those of the pass over the elements always have something
+// to do (with them first, the side warps took 20 us for 2 us of work, and the rows waited).
+constexpr int kStreamFirst = kSideLanes + 32;
+__device__ __forceinline__ bool bar_try(uint64_t* b, uint32_t parity) {
+  uint32_t done;
+  asm volatile("{.reg .pred p;\n mbarrier.try_wait.parity.shared.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;}"
+               : "=r"(done)
+               : "r"(shared_at(b)), "r"(parity)
+               : "memory");
+  return done != 0;
+}
 // Bounded: a wait that runs out clears `ok`, and later ones try once.
 __device__ __forceinline__ void bar_wait(uint64_t* b, uint32_t parity, bool& ok) {
-  uint32_t done = 0;
-  for (uint32_t tries = ok ? 1u << 22 : 1u; tries && !done; --tries)
-    asm volatile("{.reg .pred p;\n mbarrier.try_wait.parity.shared.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;}"
-                 : "=r"(done)
-                 : "r"(shared_at(b)), "r"(parity)
-                 : "memory");
-  if (!done) ok = false;
+  if (bar_try(b, parity)) return;
+  for (uint32_t tries = ok ? 1u << 22 : 0u; tries; --tries)
+    if (bar_try(b, parity)) return;
+  ok = false;
 }
 // A warp has read its part of a stage.  The copy that fills the stage next writes it by another path than the loads take: the loads
 // have to be over before the copying thread hears of it, and the arrival alone does not see to that.
@@ -669,6 +678,49 @@ __device__ __forceinline__ int end_word(const RowAt& R, uint32_t vocab, uint32_t
   return w >= 0 && w < (int)vocab ? w : -1;
 }
 
+// The warp's part of a stage of the row's whole vectors from `v` on; what lies behind them is minus infinity.  Then the stage is given back.
+template <class T>
+__device__ __forceinline__ void take_stage(const uint4* ring, uint32_t& stage, uint32_t& phase, uint32_t stages, uint64_t* full, uint64_t* empty,
+                                           uint32_t v, uint32_t wholes, bool& ok, uint4 (&raw)[kStageShare]) {
+  const uint32_t tid = threadIdx.x - kStreamFirst;
+  bar_wait(&full[stage], phase, ok);
+  const uint4* const from = ring + stage * kStageVecs + tid;
+  if (v + kStageVecs <= wholes) {
+#pragma unroll
+    for (int j = 0; j < kStageShare; ++j) raw[j] = from[j * kStreamLanes];
+  } else {
+#pragma unroll
+    for (int j = 0; j < kStageShare; ++j) {
+      raw[j] = nothing<T>();
+      if (v + tid + j * kStreamLanes < wholes) raw[j] = from[j * kStreamLanes];
+    }
+  }
+  release_stage(&empty[stage]);
+  if (++stage == stages) stage = 0, phase ^= 1;
+}
+// add_batch() of vectors whose largest element is known; the sum moves only when the maximum does
+template <class T>
+__device__ __forceinline__ void add_share(const uint4 (&raw)[kStageShare], float largest, float c2, MaxSum& acc) {
+  if (largest > acc.max) {
+    acc.sum *= exp2_fast((acc.max - largest) * c2);
+    acc.max = largest;
+  }
+  const float ref = finite_ref(acc.max);
+  const float2 less = make_float2(-ref, -ref), by = make_float2(c2, c2);
+  float2 sum = make_float2(0.f, 0.f);
+#pragma unroll
+  for (int j = 0; j < kStageShare; ++j) {
+    float f[kPerVec<T>];
+    widen<T>(raw[j], f);
+#pragma unroll
+    for (int e = 0; e < kPerVec<T>; e += 2) {
+      const float2 x = __fmul2_rn(__fadd2_rn(make_float2(f[e], f[e + 1]), less), by);
+      sum = __fadd2_rn(sum, make_float2(exp2_fast(x.x), exp2_fast(x.y)));
+    }
+  }
+  acc.sum += sum.x + sum.y;
+}
+
 struct RowSide {  // what the side warps know of a row
   MaxSum said, ends;        // listed words; unlisted ones in the ragged ends
   double mass, ent, cross;  // as in Part
@@ -703,36 +755,36 @@ __global__ void __launch_bounds__(kStreamBlock, 2) k_distill_stream(DistillArgs 
   __shared__ RowSide sides[2];
   __shared__ Part of_side[kSideWarps];
   constexpr int E = kPerVec<T>;
-  const uint32_t tid = threadIdx.x, lane = tid & 31;
+  const uint32_t thread = threadIdx.x, lane = thread & 31;
   const float c2 = a.c2;
   uint4* const ring = reinterpret_cast<uint4*>(dyn);
-  uint8_t* const marks_of[2] = {dyn + (size_t)stages * kStageVecs * 16, dyn + (size_t)stages * kStageVecs * 16 + mark_bytes};
+  const auto marks_of = [&](uint32_t buf) { return dyn + stages * (kStageVecs * 16) + buf * mark_bytes; };
   int* const records = reinterpret_cast<int*>(dyn + (size_t)stages * kStageVecs * 16 + 2 * mark_bytes);  // [2][3][k]
   const auto idle_row = [&](uint64_t row) { return a.row_weight && a.row_weight[row] == 0.f && !(KIND == kDistillLoss && a.stats); };
 
-  if (tid == 0) {
+  if (thread == 0) {
     for (uint32_t i = 0; i < stages; ++i) bar_init(&full[i], 1), bar_init(&empty[i], kStreamWarps);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  for (uint32_t i = tid; i < mark_bytes / 8; i += kStreamBlock) reinterpret_cast<uint4*>(marks_of[0])[i] = make_uint4(0, 0, 0, 0);
+  for (uint32_t i = thread; i < mark_bytes / 8; i += kStreamBlock) reinterpret_cast<uint4*>(marks_of(0))[i] = make_uint4(0, 0, 0, 0);
   __syncthreads();
 
   bool ok = true;
-  if (tid >= kStreamLanes + kSideLanes) {
+  if (thread >= kSideLanes && thread < kStreamFirst) {
     if (lane == 0 && !copy_rows<T, KIND == kDistillStep ? 2 : 1>(a, a.rows, ring, stages, full, empty, idle_row) && a.status)
       set_status(a.status, CVLC_ERR_DEVICE_TIMEOUT);
     return;
   }
 
-  if (tid >= kStreamLanes) {
+  if (thread < kSideLanes) {
     // ---- the side warps: records, ragged ends, losses ----
-    const uint32_t t = tid - kStreamLanes, side = t >> 5;
+    const uint32_t t = thread, side = t >> 5;
     const auto end_of = [&](const RowAt& R) { return side == 0 ? end_word<E>(R, a.vocab, lane) : -1; };
     const auto prepare = [&](uint64_t row, uint32_t buf) {
       some_sync<kSideLanes>(kBarSide);  // the row before the last one is finished, its marks cleared
       const RowAt R = row_at<T>(a, row);
       const T* const z = reinterpret_cast<const T*>(R.from) + R.lead;
-      uint8_t* const marks = marks_of[buf];
+      uint8_t* const marks = marks_of(buf);
       int* const at = records + buf * 3 * a.k;
       float* const prob = reinterpret_cast<float*>(at + a.k);
       float* const logit = prob + a.k;
@@ -816,7 +868,7 @@ __global__ void __launch_bounds__(kStreamBlock, 2) k_distill_stream(DistillArgs 
       some_sync<kStreamLanes + kSideLanes>(kBarDone + buf);
       const RowAt R = row_at<T>(a, row);
       const float weight = a.row_weight ? a.row_weight[row] : 1.f;
-      uint8_t* const marks = marks_of[buf];
+      uint8_t* const marks = marks_of(buf);
       int* const at = records + buf * 3 * a.k;
       float* const prob = reinterpret_cast<float*>(at + a.k);
       float* const logit = prob + a.k;
@@ -878,6 +930,7 @@ __global__ void __launch_bounds__(kStreamBlock, 2) k_distill_stream(DistillArgs 
   }
 
   // ---- the pass over the elements ----
+  const uint32_t tid = thread - kStreamFirst;
   uint32_t stage = 0, phase = 0, buf = 0;
   for (uint64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
     const RowAt R = row_at<T>(a, row);
@@ -888,27 +941,27 @@ __global__ void __launch_bounds__(kStreamBlock, 2) k_distill_stream(DistillArgs 
       continue;
     }
     some_sync<kStreamLanes + kSideLanes>(kBarReady + buf);
-    const uint8_t* const marks = marks_of[buf];
+    const unsigned char* const marks = marks_of(buf);
     Whole w = {};
     if (KIND != kDistillGrad) {
       MaxSum acc = {-CUDART_INF_F, 0.f};
       for (uint32_t v = 0; v < R.wholes; v += kStageVecs) {
-        bar_wait(&full[stage], phase, ok);
-        uint4 raw[2];
+        uint4 raw[kStageShare];
+        take_stage<T>(ring, stage, phase, stages, full, empty, v, R.wholes, ok, raw);
+        uint32_t bits[kStageShare];
+        const uint32_t i = R.whole_from + v + tid;
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          const uint32_t i = v + tid + j * kStreamLanes;
-          raw[j] = i < R.wholes ? ring[(size_t)stage * kStageVecs + tid + j * kStreamLanes] : nothing<T>();
-        }
-        release_stage(&empty[stage]);
-        if (++stage == stages) stage = 0, phase ^= 1;
+        for (int j = 0; j < kStageShare; ++j)  // (behind the row no mark is set, and the room for marks ends with a whole stage)
+          bits[j] = listed_of<T>(marks, i + j * kStreamLanes);
+        if (__any_sync(kFull, bits[0] | bits[1] | bits[2] | bits[3])) {  // few do: the warp goes around it
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          const uint32_t i = v + tid + j * kStreamLanes;
-          if (i < R.wholes)
-            if (const uint32_t bits = listed_of<T>(marks, R.whole_from + i)) drop_elements<T>(raw[j], bits);
+          for (int j = 0; j < kStageShare; ++j)
+            if (bits[j]) drop_elements<T>(raw[j], bits[j]);
         }
-        add_batch<T, 2>(raw, c2, acc);
+        float largest = vec_max<T>(raw[0]);
+#pragma unroll
+        for (int j = 1; j < kStageShare; ++j) largest = fmaxf(largest, vec_max<T>(raw[j]));
+        add_share<T>(raw, largest, c2, acc);
       }
       if (!ok) acc.sum = CUDART_NAN_F;  // a wait has run out: the row is void
       acc = warp_join(acc, c2);
@@ -933,32 +986,38 @@ __global__ void __launch_bounds__(kStreamBlock, 2) k_distill_stream(DistillArgs 
     unsigned char* const to = reinterpret_cast<unsigned char*>(g) + (int)(R.whole_from * 16) - (int)(R.lead * sizeof(T));  // of the first whole vector
     const bool alike = (reinterpret_cast<uintptr_t>(to) & 15) == 0;
     for (uint32_t v = 0; v < R.wholes; v += kStageVecs) {
-      bar_wait(&full[stage], phase, ok);
-      uint4 raw[2];
+      uint4 raw[kStageShare];
+      take_stage<T>(ring, stage, phase, stages, full, empty, v, R.wholes, ok, raw);
 #pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        const uint32_t i = v + tid + j * kStreamLanes;
-        raw[j] = i < R.wholes ? ring[(size_t)stage * kStageVecs + tid + j * kStreamLanes] : nothing<T>();
-      }
-      release_stage(&empty[stage]);
-      if (++stage == stages) stage = 0, phase ^= 1;
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        const uint32_t i = v + tid + j * kStreamLanes;
+      for (int j = 0; j < kStageShare; ++j) {
         float f[E];
         widen<T>(raw[j], f);
 #pragma unroll
         for (int e = 0; e < E; e += 2) {
-          const float2 x = mul2(add2(make_float2(f[e], f[e + 1]), make_float2(-w.ref, -w.ref)), make_float2(c2, c2));
-          const float2 y = mul2(make_float2(exp2_fast(x.x), exp2_fast(x.y)), make_float2(ca, ca));
+          const float2 x = __fmul2_rn(__fadd2_rn(make_float2(f[e], f[e + 1]), make_float2(-w.ref, -w.ref)), make_float2(c2, c2));
+          const float2 y = __fmul2_rn(make_float2(exp2_fast(x.x), exp2_fast(x.y)), make_float2(ca, ca));
           f[e] = y.x, f[e + 1] = y.y;
         }
-        if (i >= R.wholes) continue;
-        if (alike) {
-          __stcs(reinterpret_cast<uint4*>(to) + i, narrow<T>(f));
+        raw[j] = narrow<T>(f);
+      }
+      const uint32_t i = v + tid;
+      if (alike) {
+        uint4* const at = reinterpret_cast<uint4*>(to) + i;
+        if (v + kStageVecs <= R.wholes) {
+#pragma unroll
+          for (int j = 0; j < kStageShare; ++j) __stcs(at + j * kStreamLanes, raw[j]);
         } else {
 #pragma unroll
-          for (int e = 0; e < E; ++e) reinterpret_cast<T*>(to)[(size_t)i * E + e] = from_float<T>(f[e]);
+          for (int j = 0; j < kStageShare; ++j)
+            if (i + j * kStreamLanes < R.wholes) __stcs(at + j * kStreamLanes, raw[j]);
+        }
+      } else {
+#pragma unroll
+        for (int j = 0; j < kStageShare; ++j) {
+          if (i + j * kStreamLanes >= R.wholes) continue;
+          const T* const elements = reinterpret_cast<const T*>(&raw[j]);
+#pragma unroll
+          for (int e = 0; e < E; ++e) reinterpret_cast<T*>(to)[(size_t)(i + j * kStreamLanes) * E + e] = elements[e];
         }
       }
     }
@@ -1020,7 +1079,7 @@ unsigned stream_grid(uint64_t rows) { return (unsigned)(rows < 2 * kNumSM ? rows
 template <class T, DistillKind KIND>
 cudaError_t distill_typed(const DistillArgs& a, cudaStream_t st) {
   // many long rows: two blocks an SM go from row to row, where two rows' marks and three stages fit
-  const uint32_t mark_row = (a.vocab + 2 * kPerVec<T> + 127) / 128 * 16;
+  const uint32_t mark_row = (a.vocab / kPerVec<T> + 2 + kStageVecs) * kPerVec<T> / 128 * 16 + 16;  // the row's, and a stage's behind it
   const size_t beside = 2 * (size_t)mark_row + (size_t)a.k * 24;
   if (streamed(a.rows, (uint64_t)a.vocab * sizeof(T)) && beside + 3 * kStageVecs * 16 <= kStreamShared) {
     const uint32_t fit = (uint32_t)((kStreamShared - beside) / (kStageVecs * 16));
@@ -1068,7 +1127,7 @@ __device__ __forceinline__ unsigned long long candidate(uint32_t order, uint32_t
   return ((unsigned long long)order << 32) | (uint32_t)~word;
 }
 
-constexpr uint32_t kBoundStep = 1u << 13;  // 2^-10 of a value: not worth another round
+constexpr uint32_t kBoundStep = 1u << 15;  // 2^-8 of a value: not worth another round
 
 struct TopPart {
   MaxSum all;
@@ -1088,26 +1147,60 @@ __device__ __forceinline__ uint32_t raise_bound(uint32_t top, uint32_t want, uin
     n = __syncthreads_count(top >= mid);
     if (n >= want) lo = mid;
     else hi = mid - 1;
-    if (n == want) break;
+    if (n >= want && n <= want + want / 8) break;
   }
   return lo;
 }
 
-// Elements from `least` on (a candidate: value and word) of some vectors, into a list of `room`; word_of(j): the first word of the j-th
+// element e of a vector, widened
+template <class T>
+__device__ __forceinline__ float element_of(const uint4& raw, uint32_t e) {
+  const uint32_t i = sizeof(T) == 4 ? e : e >> 1;
+  const uint32_t w = i & 2 ? (i & 1 ? raw.w : raw.z) : (i & 1 ? raw.y : raw.x);
+  if constexpr (sizeof(T) == 4) return __uint_as_float(w);
+  const uint16_t h = (uint16_t)(e & 1 ? w >> 16 : w);
+  T v;
+  memcpy(&v, &h, 2);
+  return to_float(v);
+}
+// bit e: element e of a vector is at least `least`
+template <class T>
+__device__ __forceinline__ uint32_t reaching(const uint4& raw, float least) {
+  const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
+  uint32_t bits = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (sizeof(T) == 4) {
+      bits |= __uint_as_float(w[i]) >= least ? 1u << i : 0u;
+    } else {  // against the smallest number of the type that is not below `least`
+      uint32_t m;
+      if constexpr (std::is_same<T, __half>::value) {
+        __half2 h;
+        memcpy(&h, &w[i], 4);
+        m = __hge2_mask(h, __half2half2(__float2half_ru(least)));
+      } else {
+        __nv_bfloat162 h;
+        memcpy(&h, &w[i], 4);
+        m = __hge2_mask(h, __bfloat162bfloat162(__float2bfloat16_ru(least)));
+      }
+      bits |= (m & 0x10001u) << (2 * i);  // the upper one 16 bits above its place
+    }
+  }
+  return sizeof(T) == 4 ? bits : (bits & 0xFFu) | (bits >> 15);
+}
+// Elements from `least` on (a candidate: value and word) of some vectors, into a list of `room`; word_of(j): the first word of the j-th.
+// Few threads have any, and hardly one more than one: they find theirs one by one.
 template <class T, int NV, class F>
 __device__ __forceinline__ void list_batch(const uint4 (&raw)[NV], F&& word_of, unsigned long long least, uint32_t* count, unsigned long long* to,
                                            uint32_t room) {
   const float floor_value = value_of((uint32_t)(least >> 32));
 #pragma unroll
   for (int j = 0; j < NV; ++j) {
-    if (!(vec_max<T>(raw[j]) >= floor_value)) continue;
-    float f[kPerVec<T>];
-    widen<T>(raw[j], f);
-    const int word = word_of(j);
-#pragma unroll
-    for (int e = 0; e < kPerVec<T>; ++e) {
-      if (!(f[e] >= floor_value)) continue;
-      const unsigned long long c = candidate(order_of(f[e]), (uint32_t)(word + e));
+    const bool any = vec_max<T>(raw[j]) >= floor_value;
+    if (!any) continue;
+    for (uint32_t bits = reaching<T>(raw[j], floor_value); bits; bits &= bits - 1) {
+      const uint32_t e = __ffs(bits) - 1;
+      const unsigned long long c = candidate(order_of(element_of<T>(raw[j], e)), (uint32_t)(word_of(j) + (int)e));
       if (c < least) continue;
       const uint32_t n = atomicAdd(count, 1u);
       if (n < room) to[n] = c;
@@ -1170,20 +1263,25 @@ __device__ __forceinline__ void pick_digit(F&& count_of, uint32_t left, uint32_t
 template <class F>
 __device__ __forceinline__ void put_records(const TopArgs& a, uint64_t row, const MaxSum& all, unsigned long long* packed, uint32_t n, uint32_t t,
                                             uint32_t nt, F&& sync) {
-  const double it = 1.0 / (double)a.temperature, ln_sum = log((double)all.sum);
+  const float it = 1.f / a.temperature, ln_sum = logf(all.sum);
   auto put = [&](uint32_t at, unsigned long long c) {
     a.ids[row * a.k + at] = (int32_t)~(uint32_t)c;
-    a.logp[row * a.k + at] = (float)(((double)value_of((uint32_t)(c >> 32)) - (double)all.max) * it - ln_sum);
+    a.logp[row * a.k + at] = (value_of((uint32_t)(c >> 32)) - all.max) * it - ln_sum;
   };
   if (n <= 4 * nt) {  // a few for each thread: a candidate's rank is the number of larger ones
+    const uint32_t even = (n + 7) & ~7u;
+    if (t < even - n) packed[n + t] = 0;
+    sync();
     for (uint32_t i = t; i < n; i += nt) {
       const unsigned long long c = packed[i];
-      uint32_t larger = 0, o = 0;
-      for (; o + 2 <= n; o += 2) {
-        const ulonglong2 p = *reinterpret_cast<const ulonglong2*>(packed + o);
-        larger += (p.x > c) + (p.y > c);
+      uint32_t larger = 0;
+      for (uint32_t o = 0; o < even; o += 8) {
+        ulonglong2 p[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) p[q] = *reinterpret_cast<const ulonglong2*>(packed + o + 2 * q);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) larger += (p[q].x > c) + (p[q].y > c);
       }
-      if (o < n) larger += packed[o] > c;
       if (larger < a.k) put(larger, c);
     }
   } else {  // sorted in pairs, the largest first
@@ -1353,28 +1451,29 @@ __global__ void __launch_bounds__(kStreamBlock, 2) k_top_stream(TopArgs a, uint3
   __shared__ uint64_t full[kStagesMost], empty[kStagesMost];
   __shared__ RowTop tops[2];
   __shared__ uint32_t hist[256];
-  __shared__ uint32_t mine, picked, above, largest[2], kept;
+  static_assert(kStreamLanes == 256, "a bin for each thread");
+  __shared__ uint32_t mine, picked, above, largest, smallest, kept;
   constexpr int E = kPerVec<T>;
-  const uint32_t tid = threadIdx.x, lane = tid & 31;
+  const uint32_t thread = threadIdx.x, lane = thread & 31;
   const float c2 = a.c2;
   uint4* const ring = reinterpret_cast<uint4*>(dyn);
   unsigned long long* const lists = reinterpret_cast<unsigned long long*>(dyn + (size_t)stages * kStageVecs * 16);  // [2], then the ranking's
   DistillArgs where = {};
   where.logits = a.logits, where.row_stride = a.row_stride, where.vocab = a.vocab;
 
-  if (tid == 0) {
+  if (thread == 0) {
     for (uint32_t i = 0; i < stages; ++i) bar_init(&full[i], 1), bar_init(&empty[i], kStreamWarps);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     mine = kept = 0;
   }
   __syncthreads();
   bool ok = true;
-  if (tid >= kStreamLanes + kSideLanes) {
+  if (thread >= kSideLanes && thread < kStreamFirst) {
     if (lane == 0) copy_rows<T, 1>(where, a.rows, ring, stages, full, empty, [](uint64_t) { return false; });
     return;
   }
-  if (tid >= kStreamLanes) {
-    const uint32_t t = tid - kStreamLanes;
+  if (thread < kSideLanes) {
+    const uint32_t t = thread;
     unsigned long long* const packed = lists + 2 * kTopList;
     uint32_t buf = 0;
     some_arrive<kStreamLanes + kSideLanes>(kBarReady);
@@ -1400,6 +1499,7 @@ __global__ void __launch_bounds__(kStreamBlock, 2) k_top_stream(TopArgs a, uint3
     return;
   }
 
+  const uint32_t tid = thread - kStreamFirst;
   uint32_t stage = 0, phase = 0, buf = 0;
   for (uint64_t row = blockIdx.x; row < a.rows; row += gridDim.x, buf ^= 1) {
     const RowAt R = row_at<T>(where, row);
@@ -1407,12 +1507,16 @@ __global__ void __launch_bounds__(kStreamBlock, 2) k_top_stream(TopArgs a, uint3
     const int end = end_word<E>(R, a.vocab, tid);  // ends of the row beside its whole vectors: one for a thread
     const float end_z = end >= 0 ? to_float(z[end]) : -CUDART_INF_F;
     some_sync<kStreamLanes + kSideLanes>(kBarReady + buf);
-    if (tid == 0) mine = 0, largest[0] = largest[1] = 0;
+    if (tid == 0) mine = 0, largest = 0, smallest = 0xFFFFFFFFu;
+    hist[tid] = 0;
     some_sync<kStreamLanes>(kBarStream);
     unsigned long long* const list = lists + buf * kTopList;
     MaxSum acc = {end_z, end_z == -CUDART_INF_F ? 0.f : end_z < CUDART_INF_F ? 1.f : CUDART_NAN_F};
     if (end_z != end_z) acc.max = -CUDART_INF_F;
-    uint32_t bound = kOrderNegInf + 1, raised = 0;
+    // after 1, 4, 16, .. stages, which lists about 7 k elements; after 1, 2, 4, .. where that could be too many
+    const uint32_t often = a.k <= 96 ? 4 : 2;
+    float top[2] = {-CUDART_INF_F, -CUDART_INF_F};  // the thread's largest, of every other vector
+    uint32_t bound = kOrderNegInf + 1, next_raise = 0;
     const uint32_t cuts = (R.wholes + kStageVecs - 1) / kStageVecs;
     const auto list_end = [&](unsigned long long least) {
       if (end_z > -CUDART_INF_F) {
@@ -1424,35 +1528,45 @@ __global__ void __launch_bounds__(kStreamBlock, 2) k_top_stream(TopArgs a, uint3
       }
     };
     for (uint32_t b = 0; b < cuts; ++b) {
-      const uint32_t v = b * kStageVecs + tid;
-      bar_wait(&full[stage], phase, ok);
-      uint4 raw[2];
+      uint4 raw[kStageShare];
+      take_stage<T>(ring, stage, phase, stages, full, empty, b * kStageVecs, R.wholes, ok, raw);
+      float halves[2] = {vec_max<T>(raw[0]), vec_max<T>(raw[1])};
 #pragma unroll
-      for (int j = 0; j < 2; ++j)
-        raw[j] = v + j * kStreamLanes < R.wholes ? ring[(size_t)stage * kStageVecs + tid + j * kStreamLanes] : nothing<T>();
-      release_stage(&empty[stage]);
-      if (++stage == stages) stage = 0, phase ^= 1;
-      add_batch<T, 2>(raw, c2, acc);
-      if (b + 1 == cuts || (b & (b + 1)) == 0) {
-        // raise_bound() among the stream warps; two places for the largest, in turn: who writes one again has met all readers at the other
-        const uint32_t top = order_of(acc.max);
-        uint32_t* const most = &largest[raised++ & 1];
-        const uint32_t of_warp = __reduce_max_sync(kFull, top);
-        if (lane == 0) atomicMax(most, of_warp);
-        uint32_t n = some_count<kStreamLanes>(kBarStream, top >= bound);
-        if (n >= a.k) {
-          uint32_t hi = *most;
-          while (hi > bound && hi - bound > kBoundStep) {
-            const uint32_t mid = bound + (hi - bound) / 2;
-            n = some_count<kStreamLanes>(kBarStream, top >= mid);
-            if (n >= a.k) bound = mid;
-            else hi = mid - 1;
-            if (n == a.k) break;
+      for (int j = 2; j < kStageShare; ++j) halves[j & 1] = fmaxf(halves[j & 1], vec_max<T>(raw[j]));
+      top[0] = fmaxf(top[0], halves[0]), top[1] = fmaxf(top[1], halves[1]);
+      const float top_of = fmaxf(halves[0], halves[1]);
+      add_share<T>(raw, top_of, c2, acc);
+      if (b + 1 == cuts || b == next_raise) {
+        // The bound is raised by a histogram of the threads' maxima (two of a thread) between the last bound (at first: the smallest of
+        // them) and the largest
+        next_raise = next_raise * often + often - 1;
+        const uint32_t mine_of[2] = {order_of(top[0]), order_of(top[1])};
+        const uint32_t most = __reduce_max_sync(kFull, max(mine_of[0], mine_of[1])), least = __reduce_min_sync(kFull, min(mine_of[0], mine_of[1]));
+        if (lane == 0) atomicMax(&largest, most), atomicMin(&smallest, least);
+        some_sync<kStreamLanes>(kBarStream);
+        uint32_t lo = b ? bound : max(smallest, kOrderNegInf + 1), hi = largest, left = a.k;
+        while (true) {
+          const uint32_t shift = hi > lo ? max(24 - __clz(hi - lo), 0) : 0;
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+            if (mine_of[h] >= lo && mine_of[h] <= hi) atomicAdd(&hist[(mine_of[h] - lo) >> shift], 1u);
+          some_sync<kStreamLanes>(kBarStream);
+          if (tid < 32) {
+            if (tid == 0) picked = 0, above = 0;  // fewer than k: the lowest bin
+            __syncwarp();
+            pick_digit([&](uint32_t d) { const uint32_t n = hist[d]; hist[d] = 0; return n; }, left, &picked, &above);
           }
+          some_sync<kStreamLanes>(kBarStream);
+          lo += picked << shift;
+          if (shift <= 17) break;
+          hi = lo + ((1u << shift) - 1), left -= above;  // a bin of more than 1 / 64 of an octave: its own histogram
         }
+        bound = lo;
       }
-      list_batch<T, 2>(raw, [&](int j) { return (int)((R.whole_from + v + j * kStreamLanes) * E) - (int)R.lead; }, (unsigned long long)bound << 32,
-                       &mine, list, kTopList);
+      if (__any_sync(kFull, top_of >= value_of(bound))) {  // few do: the warp goes around it
+        const int word = (int)((R.whole_from + b * kStageVecs + tid) * E) - (int)R.lead;
+        list_batch<T, kStageShare>(raw, [&](int j) { return word + j * kStreamLanes * E; }, (unsigned long long)bound << 32, &mine, list, kTopList);
+      }
     }
     list_end((unsigned long long)bound << 32);
     if (!ok) acc.sum = CUDART_NAN_F;  // a wait has run out: the row is void
@@ -1465,7 +1579,7 @@ __global__ void __launch_bounds__(kStreamBlock, 2) k_top_stream(TopArgs a, uint3
       uint32_t left = a.k;
       const uint4* const from = reinterpret_cast<const uint4*>(R.from) + R.whole_from;
       for (int shift = 56; shift >= 0; shift -= 8) {
-        if (tid < 256) hist[tid] = 0;
+        hist[tid] = 0;
         some_sync<kStreamLanes>(kBarStream);
         DigitCount<T> digits = {hist, 0, 0};
         for (uint32_t i = tid; i < R.wholes; i += kStreamLanes)
