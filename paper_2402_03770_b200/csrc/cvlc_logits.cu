@@ -281,6 +281,34 @@ __device__ double loss_of(const Sums& s, const Part* parts, uint32_t blocks, uin
   return loss;
 }
 
+// Records in shared memory come in fours of 16: the places of the row's words are padded with -2.
+__device__ __forceinline__ uint32_t padded(uint32_t k) { return (k + 15) & ~15u; }
+// What record i says of its word, where a word may have several: the sum over its records in their order, by the first of them; below 0
+// for the others.  ln_p: its logarithm.
+__device__ __forceinline__ double said_by(const int* at, const float* logp, uint32_t k, uint32_t i, double* ln_p) {
+  const int here = at[i];
+  double p = exp_of(logp[i]);
+  *ln_p = (double)logp[i];
+  bool merged = false;
+  for (uint32_t o = 0; o < k; o += 16) {
+    const int4* const q = reinterpret_cast<const int4*>(at + o);
+    uint32_t same = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int4 v = q[j];
+      same |= (v.x == here ? 1u : 0u) << (4 * j) | (v.y == here ? 2u : 0u) << (4 * j) | (v.z == here ? 4u : 0u) << (4 * j) |
+              (v.w == here ? 8u : 0u) << (4 * j);
+    }
+    if (i >= o && i < o + 16) same &= ~(1u << (i - o));
+    if (!same) continue;
+    if (o + __ffs(same) - 1 < i) return -1.0;
+    for (; same; same &= same - 1) p += exp_of(logp[o + __ffs(same) - 1]);
+    merged = true;
+  }
+  if (merged) *ln_p = log(p);
+  return p;
+}
+
 // ---- a row's records, as a block sees them ----
 // The words' places are marked as soon as the records are there, for the pass over the logits; what the teacher says of them is summed
 // while the logits are on their way, and what the student says of them when they have come.
@@ -288,10 +316,11 @@ struct Records {
   int* at;        // places of the records in the block's share, or -1
   float* prob;    // their probabilities; below 0: counted with an earlier record of the word
   float* logit;   // the student's logits of their words
+  float* said;    // the records' log-probabilities
   double mass, ent;
 
   __device__ __forceinline__ Records(unsigned char* shared, uint32_t k)
-      : at(reinterpret_cast<int*>(shared)), prob(reinterpret_cast<float*>(at + k)), logit(prob + k), mass(0.0), ent(0.0) {}
+      : at(reinterpret_cast<int*>(shared)), prob(reinterpret_cast<float*>(at + padded(k))), logit(prob + k), said(logit + k), mass(0.0), ent(0.0) {}
   // the first record of a thread, and its word's logit
   int id;
   float logp, z;
@@ -320,32 +349,24 @@ struct Records {
         twice |= (atomicOr(marks + (p >> 5), bit) & bit) != 0;
       }
       at[i] = p;
-      prob[i] = logp;
+      said[i] = logp;
       if (i == threadIdx.x) z = v;
       else logit[i] = v;
     }
+    if (threadIdx.x < padded(a.k) - a.k) at[a.k + threadIdx.x] = -2;
     return twice;
   }
   // p of every word, summed in the order of its records; behind the barrier that follows mark()
   template <bool SUMS>
-  __device__ __forceinline__ void teacher(const DistillArgs& a, uint64_t row, bool twice) {
+  __device__ __forceinline__ void teacher(const DistillArgs& a, bool twice) {
     for (uint32_t i = threadIdx.x; i < a.k; i += blockDim.x) {
-      double p = -1.0;
+      double p = -1.0, ln_p = 0.0;
       if (at[i] >= 0) {
-        const float lp = prob[i];
-        p = exp_of(lp);
-        bool merged = false;
-        if (twice) {
-          const int here = at[i];
-          for (uint32_t o = 0; o < i; ++o)
-            if (at[o] == here) p = -1.0;
-          if (p >= 0.0)
-            for (uint32_t o = i + 1; o < a.k; ++o)
-              if (at[o] == here) p += exp_of(a.logp[row * a.k + o]), merged = true;
-        }
+        if (twice) p = said_by(at, said, a.k, i, &ln_p);
+        else ln_p = (double)said[i], p = exp_of(said[i]);
         if (SUMS && !(p < 0.0)) {
           mass += p;
-          if (p != 0.0) ent += p * (merged ? log(p) : (double)lp);
+          if (p != 0.0) ent += p * ln_p;
         }
       }
       prob[i] = p > 0.0 ? fmaxf((float)p, 1e-45f) : (float)p;  // (above 0 stays so; only this thread reads its own)
@@ -415,7 +436,7 @@ __global__ void __launch_bounds__(kRowThreads, 2) k_distill(DistillArgs a, uint3
     for (uint32_t i = tid; i < mark_bytes / 16; i += nt) reinterpret_cast<uint4*>(marks)[i] = make_uint4(0, 0, 0, 0);
     __syncthreads();
     const bool twice = __syncthreads_or(S.mark<T>(a, row, R, reinterpret_cast<uint32_t*>(marks)));
-    S.teacher<KIND != kDistillGrad>(a, row, twice);
+    S.teacher<KIND != kDistillGrad>(a, twice);
     if (KIND == kDistillGrad) {
       if (tid < a.k) S.logit[tid] = S.z;
     } else {
@@ -555,9 +576,9 @@ __global__ void __launch_bounds__(kRowThreads, 2) k_distill(DistillArgs a, uint3
 // Everything that a row needs beside its elements (records, sums, logarithms) takes a block about as long as reading 64 KB does, whoever does
 // it.  So where rows are many it is done by warps of their own, beside the pass over the elements: a row's records are prepared while
 // the row before it is passed over, and its loss, its listed words and its ragged ends are finished while the row behind it is.  One
-// thread copies the rows through a ring of stages in shared memory (cp.async.bulk), four vectors of every thread a stage; the step
-// copies every row twice, the second time out of the L2 cache, which holds the 296 rows on their way (76 MB at 131,072 words of 16
-// bits).  Keeping the row in the cluster's registers instead costs every block of the cluster all of the above:
+// thread copies the rows through a ring of stages in shared memory (cp.async.bulk), four vectors of every thread a stage.  The step passes over
+// every row twice, at first over what the ring still holds of it, then over what it has to copy once more, most of which is in the L2 cache
+// (the 296 rows on their way are 76 MB at 131,072 words of 16 bits).  Keeping the row in the cluster's registers instead costs every block of the cluster all of the above:
 // 4096 x 131072 bf16 750 us.
 constexpr int kStreamWarps = 8, kSideWarps = 3;  // and one that copies
 constexpr int kStreamLanes = kStreamWarps * 32, kSideLanes = kSideWarps * 32;
@@ -634,8 +655,13 @@ __device__ __forceinline__ uint32_t some_count(int id, bool v) {
 }
 enum { kBarSide = 1, kBarStream = 2, kBarReady = 3, kBarDone = 5 };  // the last two: one for each of two rows
 
-// The copying thread: the whole vectors of the block's rows through the ring, every row PASSES times; false: a wait has run out.  The last
-// reading of a row leaves nothing in the L2 cache.
+// of a row's whole vectors, those that the ring no longer holds when it has passed
+__device__ __forceinline__ uint32_t copied_again(uint32_t wholes, uint32_t stages) {
+  const uint32_t cuts = (wholes + kStageVecs - 1) / kStageVecs;
+  return cuts > stages ? (cuts - stages) * kStageVecs : 0;
+}
+// The copying thread: the whole vectors of the block's rows through the ring; with two passes all but what the ring still holds of the row a
+// second time.  False: a wait has run out.  The last reading of a row leaves nothing in the L2 cache.
 template <class T, int PASSES, class F>
 __device__ bool copy_rows(const DistillArgs& a, uint64_t rows, uint4* ring, uint32_t stages, uint64_t* full, uint64_t* empty, F&& skip) {
   uint64_t once;
@@ -645,14 +671,16 @@ __device__ bool copy_rows(const DistillArgs& a, uint64_t rows, uint4* ring, uint
   for (uint64_t row = blockIdx.x; row < rows; row += gridDim.x) {
     if (skip(row)) continue;
     const RowAt R = row_at<T>(a, row);
-    for (int pass = 0; pass < PASSES; ++pass)
-      for (uint32_t v = 0; v < R.wholes; v += kStageVecs) {
+    for (int pass = 0; pass < PASSES; ++pass) {
+      const uint32_t to_copy = pass == 0 ? R.wholes : copied_again(R.wholes, stages);
+      const bool once_more = pass + 1 < PASSES;
+      for (uint32_t v = 0; v < to_copy; v += kStageVecs) {
         bar_wait(&empty[stage], phase ^ 1, ok);
         const uint32_t bytes = min(R.wholes - v, (uint32_t)kStageVecs) * 16;
         bar_expect(&full[stage], bytes);
         const unsigned char* const src = R.from + ((size_t)R.whole_from + v) * 16;
         const uint32_t to = shared_at(ring + (size_t)stage * kStageVecs), bar = shared_at(&full[stage]);
-        if (pass == PASSES - 1)
+        if (!once_more || v >= copied_again(R.wholes, stages))
           asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1], %2, [%3], %4;" ::"r"(to), "l"(src),
                        "r"(bytes), "r"(bar), "l"(once)
                        : "memory");
@@ -661,6 +689,7 @@ __device__ bool copy_rows(const DistillArgs& a, uint64_t rows, uint4* ring, uint
                        : "memory");
         if (++stage == stages) stage = 0, phase ^= 1;
       }
+    }
   }
   bool last = true;  // no copy is left on its way, even where a wait has run out
   for (uint32_t i = 0; i < stages; ++i) {
@@ -678,12 +707,10 @@ __device__ __forceinline__ int end_word(const RowAt& R, uint32_t vocab, uint32_t
   return w >= 0 && w < (int)vocab ? w : -1;
 }
 
-// The warp's part of a stage of the row's whole vectors from `v` on; what lies behind them is minus infinity.  Then the stage is given back.
+// The warp's part of a stage that holds the row's whole vectors from `v` on; what lies behind them is minus infinity.
 template <class T>
-__device__ __forceinline__ void take_stage(const uint4* ring, uint32_t& stage, uint32_t& phase, uint32_t stages, uint64_t* full, uint64_t* empty,
-                                           uint32_t v, uint32_t wholes, bool& ok, uint4 (&raw)[kStageShare]) {
+__device__ __forceinline__ void read_stage(const uint4* ring, uint32_t stage, uint32_t v, uint32_t wholes, uint4 (&raw)[kStageShare]) {
   const uint32_t tid = threadIdx.x - kStreamFirst;
-  bar_wait(&full[stage], phase, ok);
   const uint4* const from = ring + stage * kStageVecs + tid;
   if (v + kStageVecs <= wholes) {
 #pragma unroll
@@ -695,7 +722,14 @@ __device__ __forceinline__ void take_stage(const uint4* ring, uint32_t& stage, u
       if (v + tid + j * kStreamLanes < wholes) raw[j] = from[j * kStreamLanes];
     }
   }
-  release_stage(&empty[stage]);
+}
+// ... of the next stage of the ring, which is then given back, unless it is to be read once more
+template <class T>
+__device__ __forceinline__ void take_stage(const uint4* ring, uint32_t& stage, uint32_t& phase, uint32_t stages, uint64_t* full, uint64_t* empty,
+                                           uint32_t v, uint32_t wholes, bool& ok, uint4 (&raw)[kStageShare], bool keep = false) {
+  bar_wait(&full[stage], phase, ok);
+  read_stage<T>(ring, stage, v, wholes, raw);
+  if (!keep) release_stage(&empty[stage]);
   if (++stage == stages) stage = 0, phase ^= 1;
 }
 // add_batch() of vectors whose largest element is known; the sum moves only when the maximum does
@@ -748,6 +782,16 @@ __device__ __forceinline__ Whole whole_of(const RowSide& s, float c2, MaxSum* re
   return w;
 }
 
+// thread `t` of `nt` writes its part of a row of zeros
+template <class T>
+__device__ __forceinline__ void zero_row(T* g, uint32_t vocab, uint32_t t, uint32_t nt) {
+  const uint32_t lead = (uint32_t)(-(reinterpret_cast<uintptr_t>(g) / sizeof(T)) & (kPerVec<T> - 1)), front = min(lead, vocab);
+  const uint32_t vecs = (vocab - front) / kPerVec<T>, back = front + vecs * kPerVec<T>;
+  if (t < front) g[t] = from_float<T>(0.f);
+  for (uint32_t v = t; v < vecs; v += nt) __stcs(reinterpret_cast<uint4*>(g + front) + v, make_uint4(0, 0, 0, 0));
+  if (back + t < vocab) g[back + t] = from_float<T>(0.f);
+}
+
 template <class T, DistillKind KIND>
 __global__ void __launch_bounds__(kStreamBlock, 2) k_distill_stream(DistillArgs a, uint32_t stages, uint32_t mark_bytes) {
   extern __shared__ __align__(128) unsigned char dyn[];
@@ -759,7 +803,9 @@ __global__ void __launch_bounds__(kStreamBlock, 2) k_distill_stream(DistillArgs 
   const float c2 = a.c2;
   uint4* const ring = reinterpret_cast<uint4*>(dyn);
   const auto marks_of = [&](uint32_t buf) { return dyn + stages * (kStageVecs * 16) + buf * mark_bytes; };
-  int* const records = reinterpret_cast<int*>(dyn + (size_t)stages * kStageVecs * 16 + 2 * mark_bytes);  // [2][3][k]
+  const auto places_of = [&](uint32_t buf) {  // of two rows: places, then what Records has
+    return reinterpret_cast<int*>(dyn + stages * (kStageVecs * 16) + 2 * mark_bytes) + buf * 4 * padded(a.k);
+  };
   const auto idle_row = [&](uint64_t row) { return a.row_weight && a.row_weight[row] == 0.f && !(KIND == kDistillLoss && a.stats); };
 
   if (thread == 0) {
@@ -785,15 +831,16 @@ __global__ void __launch_bounds__(kStreamBlock, 2) k_distill_stream(DistillArgs 
       const RowAt R = row_at<T>(a, row);
       const T* const z = reinterpret_cast<const T*>(R.from) + R.lead;
       uint8_t* const marks = marks_of(buf);
-      int* const at = records + buf * 3 * a.k;
-      float* const prob = reinterpret_cast<float*>(at + a.k);
+      int* const at = places_of(buf);
+      float* const prob = reinterpret_cast<float*>(at + padded(a.k));
       float* const logit = prob + a.k;
+      float* const said = logit + a.k;
       bool twice = false;
       const int end = end_of(R);
       const float end_z = end >= 0 ? to_float(z[end]) : -CUDART_INF_F;
       for (uint32_t i = t; i < a.k; i += kSideLanes) {
         const int id = a.ids[row * a.k + i];
-        prob[i] = a.logp[row * a.k + i];
+        said[i] = a.logp[row * a.k + i];
         int p = -1;
         if (id >= 0 && (uint32_t)id >= a.vocab) {
           if (a.status) set_status(a.status, CVLC_ERR_INVALID_ARG);
@@ -805,25 +852,17 @@ __global__ void __launch_bounds__(kStreamBlock, 2) k_distill_stream(DistillArgs 
         }
         at[i] = p;
       }
+      if (t < padded(a.k) - a.k) at[a.k + t] = -2;
       twice = some_or<kSideLanes>(kBarSide, twice);
       Part mine = {{-CUDART_INF_F, 0.f}, {-CUDART_INF_F, 0.f}, 0.0, 0.0, 0.0};
       for (uint32_t i = t; i < a.k; i += kSideLanes) {
-        const int here = at[i];
-        double p = -1.0;
-        if (here >= 0) {
-          const float lp = prob[i];
-          p = exp_of(lp);
-          bool merged = false;
-          if (twice) {
-            for (uint32_t o = 0; o < i; ++o)
-              if (at[o] == here) p = -1.0;
-            if (p >= 0.0)
-              for (uint32_t o = i + 1; o < a.k; ++o)
-                if (at[o] == here) p += exp_of(a.logp[row * a.k + o]), merged = true;
-          }
+        double p = -1.0, ln_p = 0.0;
+        if (at[i] >= 0) {
+          if (twice) p = said_by(at, said, a.k, i, &ln_p);
+          else ln_p = (double)said[i], p = exp_of(said[i]);
           if (KIND != kDistillGrad && !(p < 0.0)) {
             mine.mass += p;
-            if (p != 0.0) mine.ent += p * (merged ? log(p) : (double)lp);
+            if (p != 0.0) mine.ent += p * ln_p;
             mine.said.max = fmaxf(mine.said.max, logit[i]);
           }
         }
@@ -869,8 +908,8 @@ __global__ void __launch_bounds__(kStreamBlock, 2) k_distill_stream(DistillArgs 
       const RowAt R = row_at<T>(a, row);
       const float weight = a.row_weight ? a.row_weight[row] : 1.f;
       uint8_t* const marks = marks_of(buf);
-      int* const at = records + buf * 3 * a.k;
-      float* const prob = reinterpret_cast<float*>(at + a.k);
+      int* const at = places_of(buf);
+      float* const prob = reinterpret_cast<float*>(at + padded(a.k));
       float* const logit = prob + a.k;
       Whole w;
       if (KIND == kDistillGrad) {
@@ -936,18 +975,18 @@ __global__ void __launch_bounds__(kStreamBlock, 2) k_distill_stream(DistillArgs 
     const RowAt R = row_at<T>(a, row);
     T* const g = static_cast<T*>(a.grad) + row * a.grad_stride;
     if (idle_row(row)) {
-      if (KIND != kDistillLoss)
-        for (uint32_t j = tid; j < a.vocab; j += kStreamLanes) g[j] = from_float<T>(0.f);
+      if (KIND != kDistillLoss) zero_row<T>(g, a.vocab, tid, kStreamLanes);
       continue;
     }
     some_sync<kStreamLanes + kSideLanes>(kBarReady + buf);
     const unsigned char* const marks = marks_of(buf);
+    const uint32_t again = copied_again(R.wholes, stages);  // from here on the ring still holds the row for the second pass
     Whole w = {};
     if (KIND != kDistillGrad) {
       MaxSum acc = {-CUDART_INF_F, 0.f};
       for (uint32_t v = 0; v < R.wholes; v += kStageVecs) {
         uint4 raw[kStageShare];
-        take_stage<T>(ring, stage, phase, stages, full, empty, v, R.wholes, ok, raw);
+        take_stage<T>(ring, stage, phase, stages, full, empty, v, R.wholes, ok, raw, KIND == kDistillStep && v >= again);
         uint32_t bits[kStageShare];
         const uint32_t i = R.whole_from + v + tid;
 #pragma unroll
@@ -985,9 +1024,20 @@ __global__ void __launch_bounds__(kStreamBlock, 2) k_distill_stream(DistillArgs 
     const float ca = w.a * ((a.row_weight ? a.row_weight[row] : 1.f) / a.temperature);
     unsigned char* const to = reinterpret_cast<unsigned char*>(g) + (int)(R.whole_from * 16) - (int)(R.lead * sizeof(T));  // of the first whole vector
     const bool alike = (reinterpret_cast<uintptr_t>(to) & 15) == 0;
-    for (uint32_t v = 0; v < R.wholes; v += kStageVecs) {
+    const uint32_t cuts = (R.wholes + kStageVecs - 1) / kStageVecs, kept = cuts - again / kStageVecs;
+    uint32_t held = stage + (stage < kept ? stages : 0) - kept;  // the step: the stage of the first that is held
+    for (uint32_t cut = 0; cut < cuts; ++cut) {  // what is held, then the row's beginning
       uint4 raw[kStageShare];
-      take_stage<T>(ring, stage, phase, stages, full, empty, v, R.wholes, ok, raw);
+      uint32_t v;
+      if (KIND == kDistillStep && cut < kept) {
+        v = again + cut * kStageVecs;
+        read_stage<T>(ring, held, v, R.wholes, raw);
+        release_stage(&empty[held]);
+        if (++held == stages) held = 0;
+      } else {
+        v = (KIND == kDistillStep ? cut - kept : cut) * kStageVecs;
+        take_stage<T>(ring, stage, phase, stages, full, empty, v, R.wholes, ok, raw);
+      }
 #pragma unroll
       for (int j = 0; j < kStageShare; ++j) {
         float f[E];
@@ -1080,7 +1130,7 @@ template <class T, DistillKind KIND>
 cudaError_t distill_typed(const DistillArgs& a, cudaStream_t st) {
   // many long rows: two blocks an SM go from row to row, where two rows' marks and three stages fit
   const uint32_t mark_row = (a.vocab / kPerVec<T> + 2 + kStageVecs) * kPerVec<T> / 128 * 16 + 16;  // the row's, and a stage's behind it
-  const size_t beside = 2 * (size_t)mark_row + (size_t)a.k * 24;
+  const size_t beside = 2 * ((size_t)mark_row + ((size_t)a.k + 15) / 16 * 16 * 16);
   if (streamed(a.rows, (uint64_t)a.vocab * sizeof(T)) && beside + 3 * kStageVecs * 16 <= kStreamShared) {
     const uint32_t fit = (uint32_t)((kStreamShared - beside) / (kStageVecs * 16));
     const uint32_t stages = fit < kStagesMost ? fit : kStagesMost;
@@ -1095,7 +1145,7 @@ cudaError_t distill_typed(const DistillArgs& a, cudaStream_t st) {
   constexpr int NV = KIND == kDistillStep ? 8 : 4;
   const Cut c = cut_rows(a.logits, a.row_stride, a.rows, a.vocab, sizeof(T), NV, KIND == kDistillStep ? NV : 0);
   const uint32_t mark_bytes = (c.rounds * c.threads * kPerVec<T> / 8 + 15) & ~15u;  // a bit for every element of a block
-  const size_t smem = mark_bytes + (size_t)a.k * 12;
+  const size_t smem = mark_bytes + ((size_t)a.k + 15) * 16;
   return launch_rows(KIND == kDistillLoss ? kKDistillLoss : KIND == kDistillGrad ? kKDistillGrad : kKDistillStep, k_distill<T, NV, KIND>, a.rows, c,
                      KIND != kDistillGrad, smem, st, a, c.log_blocks, mark_bytes);
 }
