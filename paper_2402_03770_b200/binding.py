@@ -519,44 +519,52 @@ def cvlc_decode_aggregate_noalloc(stream_ptrs: torch.Tensor, stream_bytes: torch
 _DTYPES = {torch.float32: CVLC_F32, torch.float16: CVLC_F16, torch.bfloat16: CVLC_BF16}
 
 
-def _rows(t: torch.Tensor) -> Tuple[int, int]:
+_device = torch._C._cuda_getDevice if hasattr(torch._C, "_cuda_getDevice") else torch.cuda.current_device
+
+
+def _rows(t: torch.Tensor, device: int) -> Tuple[int, int]:
     """pointer and row stride of a matrix whose rows are contiguous"""
-    assert t.dim() == 2 and t.is_cuda and t.device.index == torch.cuda.current_device()
-    assert t.shape[1] <= 1 or t.stride(1) == 1
-    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+    (rows, cols), (stride, step) = t.shape, t.stride()
+    assert t.get_device() == device and (step == 1 or cols <= 1)
+    return t.data_ptr(), stride if rows > 1 else max(stride, cols)
 
 
-def _here(t: Optional[torch.Tensor], dtype: torch.dtype, shape: Tuple[int, ...]) -> Optional[int]:
-    """pointer of a contiguous tensor of this type and shape on the current device"""
+def _here(t: Optional[torch.Tensor], dtype: torch.dtype, shape: Tuple[int, ...], device: int) -> Optional[int]:
+    """pointer of a contiguous tensor of this type and shape on the device"""
     if t is None:
         return None
-    assert t.is_cuda and t.device.index == torch.cuda.current_device() and t.is_contiguous()
-    assert t.dtype == dtype and tuple(t.shape) == shape, (t.dtype, tuple(t.shape), dtype, shape)
+    assert t.dtype == dtype and t.shape == shape and t.get_device() == device and t.is_contiguous(), (t.dtype, t.shape, t.device, dtype, shape)
     return t.data_ptr()
+
+
+def _stream_on(stream: Optional[torch.cuda.Stream], device: int) -> int:
+    return _raw_stream(device) if stream is None and _raw_stream is not None else _stream_handle(stream)
 
 
 def cvlc_top_logits(logits: torch.Tensor, ids: torch.Tensor, logp: torch.Tensor, temperature: float = 1.0,
                     stream: Optional[torch.cuda.Stream] = None) -> None:
     """The k = ids.shape[1] largest logits of every row: words into ids (int32), log-probabilities into logp (fp32)."""
-    at, stride = _rows(logits)
+    device = _device()
+    at, stride = _rows(logits, device)
     rows, vocab = logits.shape
     shape = (rows, ids.shape[1])
-    _check(lib().cvlc_top_logits(at, _DTYPES[logits.dtype], rows, vocab, stride, shape[1], temperature, _here(ids, torch.int32, shape),
-                                 _here(logp, torch.float32, shape), _stream_handle(stream)), "cvlc_top_logits")
+    _check(lib().cvlc_top_logits(at, _DTYPES[logits.dtype], rows, vocab, stride, shape[1], temperature, _here(ids, torch.int32, shape, device),
+                                 _here(logp, torch.float32, shape, device), _stream_on(stream, device)), "cvlc_top_logits")
 
 
 def _distill(logits: torch.Tensor, ids: torch.Tensor, logp: torch.Tensor, rest: int, temperature: float,
-             row_weight: Optional[torch.Tensor], status: Optional[torch.Tensor]) -> CvlcDistill:
-    at, stride = _rows(logits)
+             row_weight: Optional[torch.Tensor], status: Optional[torch.Tensor], device: int) -> CvlcDistill:
+    at, stride = _rows(logits, device)
     rows, vocab = logits.shape
     shape = (rows, ids.shape[1])
-    return CvlcDistill(at, rows, stride, vocab, _DTYPES[logits.dtype], _here(ids, torch.int32, shape), _here(logp, torch.float32, shape),
-                       shape[1], rest, temperature, 0, _here(row_weight, torch.float32, (rows,)), _here(status, torch.int32, (1,)))
+    return CvlcDistill(at, rows, stride, vocab, _DTYPES[logits.dtype], _here(ids, torch.int32, shape, device),
+                       _here(logp, torch.float32, shape, device), shape[1], rest, temperature, 0,
+                       _here(row_weight, torch.float32, (rows,), device), _here(status, torch.int32, (1,), device))
 
 
-def _graded(logits: torch.Tensor, grad: torch.Tensor) -> Tuple[int, int]:
+def _graded(logits: torch.Tensor, grad: torch.Tensor, device: int) -> Tuple[int, int]:
     assert grad.dtype == logits.dtype and grad.shape == logits.shape
-    return _rows(grad)
+    return _rows(grad, device)
 
 
 def cvlc_distill_loss(logits: torch.Tensor, ids: torch.Tensor, logp: torch.Tensor, loss: torch.Tensor,
@@ -565,29 +573,31 @@ def cvlc_distill_loss(logits: torch.Tensor, ids: torch.Tensor, logp: torch.Tenso
                       stream: Optional[torch.cuda.Stream] = None) -> None:
     """loss[rows] of distilling the teacher's records (ids int32, logp fp32; rows x k) into the student's logits; stats (fp32, rows x
     DISTILL_STATS) keeps what cvlc_distill_grad needs."""
-    a = _distill(logits, ids, logp, rest, temperature, row_weight, status)
-    rows = logits.shape[0]
-    _check(lib().cvlc_distill_loss(C.byref(a), _here(loss, torch.float32, (rows,)), _here(stats, torch.float32, (rows, DISTILL_STATS)),
-                                   _stream_handle(stream)), "cvlc_distill_loss")
+    device = _device()
+    a = _distill(logits, ids, logp, rest, temperature, row_weight, status, device)
+    _check(lib().cvlc_distill_loss(C.byref(a), _here(loss, torch.float32, (a.rows,), device),
+                                   _here(stats, torch.float32, (a.rows, DISTILL_STATS), device), _stream_on(stream, device)), "cvlc_distill_loss")
 
 
 def cvlc_distill_grad(logits: torch.Tensor, ids: torch.Tensor, logp: torch.Tensor, stats: torch.Tensor, grad: torch.Tensor, *,
                       rest: int = CVLC_REST_BUCKET, temperature: float = 1.0, row_weight: Optional[torch.Tensor] = None,
                       status: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> None:
     """grad (as logits, or logits itself) of the sum of row_weight * loss; the other arguments as in the call that filled stats."""
-    a = _distill(logits, ids, logp, rest, temperature, row_weight, status)
-    g, stride = _graded(logits, grad)
-    _check(lib().cvlc_distill_grad(C.byref(a), _here(stats, torch.float32, (logits.shape[0], DISTILL_STATS)), g, stride,
-                                   _stream_handle(stream)), "cvlc_distill_grad")
+    device = _device()
+    a = _distill(logits, ids, logp, rest, temperature, row_weight, status, device)
+    g, stride = _graded(logits, grad, device)
+    _check(lib().cvlc_distill_grad(C.byref(a), _here(stats, torch.float32, (a.rows, DISTILL_STATS), device), g, stride,
+                                   _stream_on(stream, device)), "cvlc_distill_grad")
 
 
 def cvlc_distill_step(logits: torch.Tensor, ids: torch.Tensor, logp: torch.Tensor, loss: torch.Tensor, grad: torch.Tensor, *,
                       rest: int = CVLC_REST_BUCKET, temperature: float = 1.0, row_weight: Optional[torch.Tensor] = None,
                       status: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> None:
     """cvlc_distill_loss and cvlc_distill_grad in one reading of the logits"""
-    a = _distill(logits, ids, logp, rest, temperature, row_weight, status)
-    g, stride = _graded(logits, grad)
-    _check(lib().cvlc_distill_step(C.byref(a), _here(loss, torch.float32, (logits.shape[0],)), g, stride, _stream_handle(stream)),
+    device = _device()
+    a = _distill(logits, ids, logp, rest, temperature, row_weight, status, device)
+    g, stride = _graded(logits, grad, device)
+    _check(lib().cvlc_distill_step(C.byref(a), _here(loss, torch.float32, (a.rows,), device), g, stride, _stream_on(stream, device)),
            "cvlc_distill_step")
 
 
@@ -599,12 +609,13 @@ def _token_bytes(tokens: torch.Tensor) -> int:
 def cvlc_embed(table: torch.Tensor, tokens: torch.Tensor, out: torch.Tensor, scale: float = 1.0, status: Optional[torch.Tensor] = None,
                stream: Optional[torch.cuda.Stream] = None) -> None:
     """out[i] = scale * table[tokens[i]]; tokens (int32 or int64) below 0 are padding and give zeros."""
-    at, stride = _rows(table)
-    o, out_stride = _rows(out)
+    device = _device()
+    at, stride = _rows(table, device)
+    o, out_stride = _rows(out, device)
     n, (vocab, dim) = tokens.numel(), table.shape
-    assert out.dtype == table.dtype and tuple(out.shape) == (n, dim)
-    _check(lib().cvlc_embed(at, _DTYPES[table.dtype], vocab, dim, stride, _here(tokens, tokens.dtype, (n,)), _token_bytes(tokens), n, scale, o,
-                            out_stride, _here(status, torch.int32, (1,)), _stream_handle(stream)), "cvlc_embed")
+    assert out.dtype == table.dtype and out.shape == (n, dim)
+    _check(lib().cvlc_embed(at, _DTYPES[table.dtype], vocab, dim, stride, _here(tokens, tokens.dtype, (n,), device), _token_bytes(tokens), n,
+                            scale, o, out_stride, _here(status, torch.int32, (1,), device), _stream_on(stream, device)), "cvlc_embed")
 
 
 def cvlc_embed_grad_workspace_bytes(n: int, dim: int, vocab: int) -> int:
@@ -614,12 +625,13 @@ def cvlc_embed_grad_workspace_bytes(n: int, dim: int, vocab: int) -> int:
 def cvlc_embed_grad(tokens: torch.Tensor, grad: torch.Tensor, update: torch.Tensor, ws: torch.Tensor, scale: float = 1.0,
                     accumulate: bool = False, stream: Optional[torch.cuda.Stream] = None) -> None:
     """update[v] (fp32, vocab x dim) = (or += with accumulate) scale * the sum of grad[i] over the positions with tokens[i] = v."""
-    g, stride = _rows(grad)
-    u, update_stride = _rows(update)
+    device = _device()
+    g, stride = _rows(grad, device)
+    u, update_stride = _rows(update, device)
     n, (vocab, dim) = tokens.numel(), update.shape
-    assert update.dtype == torch.float32 and tuple(grad.shape) == (n, dim)
-    _check(lib().cvlc_embed_grad(_here(tokens, tokens.dtype, (n,)), _token_bytes(tokens), n, g, _DTYPES[grad.dtype], dim, stride, vocab, scale, u,
-                                 update_stride, 1 if accumulate else 0, _ptr(ws), _nbytes(ws), _stream_handle(stream)), "cvlc_embed_grad")
+    assert update.dtype == torch.float32 and grad.shape == (n, dim)
+    _check(lib().cvlc_embed_grad(_here(tokens, tokens.dtype, (n,), device), _token_bytes(tokens), n, g, _DTYPES[grad.dtype], dim, stride, vocab,
+                                 scale, u, update_stride, 1 if accumulate else 0, _ptr(ws), _nbytes(ws), _stream_on(stream, device)), "cvlc_embed_grad")
 
 
 def cvlc_read_status(plan_or_ws: torch.Tensor, stream: Optional[torch.cuda.Stream] = None) -> int:

@@ -4,6 +4,8 @@
 // writing each word's row once, and what a word has in several chunks is joined by a last kernel.
 #include <cooperative_groups.h>
 
+#include <algorithm>
+
 #include "cvlc_vocab.cuh"
 
 namespace cg = cooperative_groups;
@@ -22,46 +24,44 @@ constexpr int kLookupRows = 4;  // tokens of a thread: that many independent loa
 
 // A block has blockDim.x columns (vectors of a row) by blockDim.y groups of kLookupRows tokens.
 template <class T, bool VEC>
-__global__ void __launch_bounds__(kLookupThreads) k_embed(EmbedArgs a) {
+__global__ void __launch_bounds__(kLookupThreads, 6) k_embed(EmbedArgs a) {
   constexpr int E = VEC ? kPerVec<T> : 1;
+  constexpr uint32_t kPadding = 0xFFFFFFFFu;
   const uint32_t cols = a.dim / E;
   const uint64_t first = ((uint64_t)blockIdx.x * blockDim.y + threadIdx.y) * kLookupRows;
   const T* const table = static_cast<const T*>(a.table);
-  T* const out = static_cast<T*>(a.out);
-  int64_t t[kLookupRows];
+  T* const out = static_cast<T*>(a.out) + first * a.out_stride;
+  const uint32_t rows = first < a.n ? (uint32_t)min((uint64_t)kLookupRows, a.n - first) : 0;
+  uint32_t word[kLookupRows];
+  bool outside = false;
 #pragma unroll
   for (int r = 0; r < kLookupRows; ++r) {
-    t[r] = first + r < a.n ? token_at(a.tokens, a.token_bytes, first + r) : -1;
-    if (t[r] >= (int64_t)a.vocab) {
-      if (a.status && threadIdx.x == 0 && blockIdx.y == 0) set_status(a.status, CVLC_ERR_INVALID_ARG);
-      t[r] = -1;
-    }
+    const int64_t t = r < rows ? token_at(a.tokens, a.token_bytes, first + r) : -1;
+    word[r] = t >= 0 && t < (int64_t)a.vocab ? (uint32_t)t : kPadding;
+    outside |= t >= (int64_t)a.vocab;
   }
+  if (outside && a.status) set_status(a.status, CVLC_ERR_INVALID_ARG);
   for (uint32_t c = blockIdx.y * blockDim.x + threadIdx.x; c < cols; c += gridDim.y * blockDim.x) {
     if constexpr (VEC) {
-      uint4 raw[kLookupRows] = {};
-#pragma unroll
-      for (int r = 0; r < kLookupRows; ++r)
-        if (t[r] >= 0) raw[r] = __ldg(reinterpret_cast<const uint4*>(table + (uint64_t)t[r] * a.table_stride) + c);
+      uint4 raw[kLookupRows];
 #pragma unroll
       for (int r = 0; r < kLookupRows; ++r) {
-        if (first + r >= a.n) break;
+        raw[r] = make_uint4(0, 0, 0, 0);
+        if (word[r] != kPadding) raw[r] = __ldg(reinterpret_cast<const uint4*>(table + word[r] * a.table_stride) + c);
+      }
+#pragma unroll
+      for (int r = 0; r < kLookupRows; ++r) {
+        if (r >= rows) break;
         float f[E];
-        if (t[r] >= 0) {
-          widen<T>(raw[r], f);
+        widen<T>(raw[r], f);
 #pragma unroll
-          for (int e = 0; e < E; ++e) f[e] *= a.scale;
-        } else {
-#pragma unroll
-          for (int e = 0; e < E; ++e) f[e] = 0.f;
-        }
-        __stcs(reinterpret_cast<uint4*>(out + (first + r) * a.out_stride) + c, narrow<T>(f));
+        for (int e = 0; e < E; ++e) f[e] = word[r] != kPadding ? f[e] * a.scale : 0.f;
+        __stcs(reinterpret_cast<uint4*>(out + r * a.out_stride) + c, narrow<T>(f));
       }
     } else {
 #pragma unroll
       for (int r = 0; r < kLookupRows; ++r)
-        if (first + r < a.n)
-          out[(first + r) * a.out_stride + c] = from_float<T>(t[r] >= 0 ? to_float(table[(uint64_t)t[r] * a.table_stride + c]) * a.scale : 0.f);
+        if (r < rows) out[r * a.out_stride + c] = from_float<T>(word[r] != kPadding ? to_float(table[word[r] * a.table_stride + c]) * a.scale : 0.f);
     }
   }
 }
@@ -73,6 +73,7 @@ constexpr int kTokenThreads = 1024;
 constexpr int kTokenWarps = kTokenThreads / 32;
 constexpr int kTokenDigits = 512;
 constexpr size_t kTokenShared = (size_t)kTokenWarps * kTokenDigits * 4;
+constexpr int kSortAhead = 4;  // loads of a thread in flight
 
 CVLC_HD inline size_t eg_off_a() { return 256; }
 CVLC_HD inline size_t eg_off_b(uint64_t n) { return align256(eg_off_a() + n * 8); }
@@ -86,131 +87,261 @@ uint32_t chunk_of(uint64_t n) {
   return (uint32_t)c;
 }
 
+// What the sort's launch does besides, where the table is written out: zeros for the rows of words that do not occur.  A block has a range of
+// rows; it looks through all tokens for those that occur, unless they are so many that writing zeros to all rows is less.
+constexpr uint64_t kMarkedTokens = 1u << 18;
+__device__ __forceinline__ void zero_absent(const EmbedGradArgs& a, uint32_t block, uint32_t blocks, uint32_t* marks, uint32_t mark_words) {
+  const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const uint64_t per = (a.vocab + blocks - 1) / blocks, begin = block * per, end = begin + per < a.vocab ? begin + per : a.vocab;
+  if (begin >= end) return;
+  const bool marked = a.n <= kMarkedTokens && end - begin <= (uint64_t)mark_words * 32;
+  if (marked) {
+    for (uint32_t i = tid; i < (uint32_t)(end - begin + 31) / 32; i += blockDim.x) marks[i] = 0;
+    __syncthreads();
+    for (uint64_t i = tid; i < a.n; i += 8 * kTokenThreads) {
+      int64_t t[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) t[j] = i + j * kTokenThreads < a.n ? token_at(a.tokens, a.token_bytes, i + j * kTokenThreads) - (int64_t)begin : -1;
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (t[j] >= 0 && t[j] < (int64_t)(end - begin)) atomicOr(&marks[t[j] >> 5], 1u << (t[j] & 31));
+    }
+    __syncthreads();
+  }
+  const bool vec = a.dim % 4 == 0 && a.update_stride % 4 == 0 && (reinterpret_cast<uintptr_t>(a.update) & 15) == 0;
+  for (uint64_t row = begin + warp; row < end; row += blockDim.x / 32) {
+    const uint32_t r = (uint32_t)(row - begin);
+    if (marked && (marks[r >> 5] >> (r & 31) & 1)) continue;
+    float* const u = a.update + row * a.update_stride;
+    if (vec) {
+      for (uint32_t c = lane; c < a.dim / 4; c += 32) __stcs(reinterpret_cast<float4*>(u) + c, make_float4(0.f, 0.f, 0.f, 0.f));
+    } else {
+      for (uint32_t c = lane; c < a.dim; c += 32) u[c] = 0.f;
+    }
+  }
+}
+
+// word << 32 | position; a token that stands for nothing is word `vocab`
+__device__ __forceinline__ unsigned long long sort_item(const EmbedGradArgs& a, uint64_t i, bool& outside) {
+  const int64_t t = token_at(a.tokens, a.token_bytes, i);
+  outside |= t >= (int64_t)a.vocab;
+  return ((unsigned long long)(t >= 0 && t < (int64_t)a.vocab ? (uint32_t)t : (uint32_t)a.vocab) << 32) | (uint32_t)i;
+}
+// the lanes of `active` with this lane's digit of `bits` bits
+__device__ __forceinline__ uint32_t peers_of(uint32_t digit, uint32_t bits, uint32_t active) {
+  uint32_t m = active;
+#pragma unroll
+  for (uint32_t b = 0; b < 9; ++b) {
+    if (b >= bits) break;
+    const uint32_t own = 0u - ((digit >> b) & 1u);
+    m &= ~(__ballot_sync(kFull, own) ^ own);
+  }
+  return m;
+}
+// Exclusive scan over the first 2^n threads' values, n at most 10, by a block of 1024 threads
+__device__ __forceinline__ uint32_t block_scan(uint32_t v, uint32_t* scan) {
+  const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  uint32_t inc = v;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const uint32_t u = __shfl_up_sync(kFull, inc, o);
+    if (lane >= (uint32_t)o) inc += u;
+  }
+  if (lane == 31) scan[warp] = inc;
+  __syncthreads();
+  if (warp == 0) {
+    uint32_t s = scan[lane];
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const uint32_t u = __shfl_up_sync(kFull, s, o);
+      if (lane >= (uint32_t)o) s += u;
+    }
+    scan[lane] = s;
+  }
+  __syncthreads();
+  return inc - v + (warp ? scan[warp - 1] : 0);
+}
+
+// A warp's next 32 items to their places: what the digits before, the blocks, groups and warps before have (`base`, `mine`), and the lanes before
+__device__ __forceinline__ void place_items(unsigned long long it, bool in, uint32_t shift, uint32_t bits, uint32_t* mine, const uint32_t* base,
+                                            unsigned long long* to) {
+  const uint32_t lane = threadIdx.x & 31, digit = (uint32_t)(it >> shift) & ((1u << bits) - 1);
+  const uint32_t peers = peers_of(digit, bits, __ballot_sync(kFull, in));
+  const uint32_t place = in ? mine[digit] : 0;
+  __syncwarp();
+  if (in) {
+    to[base[digit] + place + __popc(peers & ((1u << lane) - 1))] = it;
+    if (lane == (uint32_t)__ffs(peers) - 1) mine[digit] = place + __popc(peers);
+  }
+  __syncwarp();
+}
+
+// Up to 2048 positions: one block holds them, in registers while they are counted and in shared memory from pass to pass.  (The cluster
+// needs two of its barriers a pass, with everything written to memory behind each; but with 8192 positions one block takes twice its time.)
+constexpr int kBlockItems = 2;
+constexpr uint64_t kBlockSort = (uint64_t)kBlockItems * kTokenThreads;
+template <int ITEMS>
+__device__ void sort_in_block(const EmbedGradArgs& a, uint32_t bits, uint32_t passes, uint32_t* counts, unsigned long long* held, uint32_t* group_base,
+                              uint32_t* scan) {
+  const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, n = (uint32_t)a.n;
+  int32_t* const status = static_cast<int32_t*>(a.ws);
+  if (tid == 0) *status = 0;
+  __syncthreads();
+  const uint32_t begin = warp * ITEMS * 32;
+  const uint32_t per = (bits + passes - 1) / passes, digits = 1u << per, mask = digits - 1;
+  const uint32_t groups = kTokenThreads / digits < kTokenWarps ? kTokenThreads / digits : kTokenWarps, group_warps = kTokenWarps / groups;
+  uint32_t* const mine = counts + warp * digits;
+  unsigned long long it[ITEMS];
+  bool outside = false;
+#pragma unroll
+  for (int j = 0; j < ITEMS; ++j) it[j] = begin + 32 * j + lane < n ? sort_item(a, begin + 32 * j + lane, outside) : 0;
+  if (outside) set_status(status, CVLC_ERR_INVALID_ARG);
+  unsigned long long* const out = reinterpret_cast<unsigned long long*>(static_cast<unsigned char*>(a.ws) + eg_off_a());
+  for (uint32_t pass = 0; pass < passes; ++pass) {
+    const uint32_t shift = 32 + pass * per;
+    for (uint32_t d = lane; d < digits; d += 32) mine[d] = 0;
+    __syncwarp();
+#pragma unroll
+    for (int j = 0; j < ITEMS; ++j)
+      if (begin + 32 * j + lane < n) atomicAdd(&mine[(uint32_t)(it[j] >> shift) & mask], 1u);
+    __syncthreads();
+    if (tid < groups * digits) {  // over a group's warps
+      const uint32_t d = tid & mask, first = tid / digits * group_warps;
+      uint32_t sum = 0;
+      for (uint32_t w = first; w < first + group_warps; ++w) {
+        const uint32_t c = counts[w * digits + d];
+        counts[w * digits + d] = sum;
+        sum += c;
+      }
+      group_base[tid] = sum;
+    }
+    __syncthreads();
+    uint32_t sum = 0;
+    if (tid < digits)
+      for (uint32_t g = 0; g < groups; ++g) {
+        const uint32_t c = group_base[g * digits + tid];
+        group_base[g * digits + tid] = sum;
+        sum += c;
+      }
+    const uint32_t at = block_scan(sum, scan);
+    if (tid < digits)
+      for (uint32_t g = 0; g < groups; ++g) group_base[g * digits + tid] += at;
+    __syncthreads();
+    const bool last = pass + 1 == passes;
+#pragma unroll
+    for (int j = 0; j < ITEMS; ++j) place_items(it[j], begin + 32 * j + lane < n, shift, per, mine, group_base + warp / group_warps * digits, last ? out : held);
+    if (last) break;
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < ITEMS; ++j)
+      if (begin + 32 * j + lane < n) it[j] = held[begin + 32 * j + lane];
+    __syncthreads();
+  }
+}
+
 // Stable radix sort by digits of up to nine bits, by one cluster.  Every warp has a stretch of the positions, in order; it counts its
-// digits, the counts are scanned over warps and blocks for every digit, and the warp walks its stretch again, giving each position its
-// place.  Tokens that stand for nothing (below zero, or outside the table) sort behind all words as word `vocab`.
-// The other clusters of the launch, if any, write the table's zeros meanwhile.
+// digits (in any order), the counts are scanned over warps (in groups, side by side) and blocks for every digit, and the warp walks its stretch again, giving
+// each position its place.  Tokens that stand for nothing (below zero, or outside the table) sort behind all words as word `vocab`.
 __global__ void __launch_bounds__(kTokenThreads, 1) k_token_sort(EmbedGradArgs a, uint32_t bits, uint32_t passes, uint32_t blocks) {
   extern __shared__ uint32_t counts[];  // [warp][digit]
   __shared__ uint32_t totals[kMaxClusterBlocks][kTokenDigits];
+  __shared__ uint32_t group_base[kTokenThreads];  // [group][digit]
   __shared__ uint32_t scan[kTokenWarps];
   cg::cluster_group cluster = cg::this_cluster();
+  if (blocks == 1 && blockIdx.x == 0) {
+    unsigned long long* const held = reinterpret_cast<unsigned long long*>(counts + kTokenWarps * kTokenDigits);
+    sort_in_block<kBlockItems>(a, bits, passes, counts, held, group_base, scan);
+    return;
+  }
   if (blockIdx.x >= blocks) {
-    const uint64_t first = (uint64_t)(blockIdx.x - blocks) * kTokenThreads + threadIdx.x, stride = (uint64_t)(gridDim.x - blocks) * kTokenThreads;
-    if (a.update_stride == a.dim && (reinterpret_cast<uintptr_t>(a.update) & 15) == 0) {
-      zero_fill(a.update, a.vocab * a.dim, first, stride);
-    } else {
-      for (uint64_t i = first; i < a.vocab * a.dim; i += stride) a.update[i / a.dim * a.update_stride + i % a.dim] = 0.f;
-    }
+    zero_absent(a, blockIdx.x - blocks, gridDim.x - blocks, counts, kTokenShared / 4);
     return;
   }
   const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, rank = blockIdx.x;
   int32_t* const status = static_cast<int32_t*>(a.ws);
   if (rank == 0 && tid == 0) *status = 0;
-  if (blocks > 1) cluster.sync();
-  else __syncthreads();
-  const uint64_t stretch = ((a.n + (uint64_t)blocks * kTokenThreads - 1) / ((uint64_t)blocks * kTokenThreads)) * 32;
+  cluster.sync();
+  const uint64_t stretch = ((uint32_t)a.n / (blocks * kTokenThreads) + 1) * 32;
   const uint64_t begin = ((uint64_t)rank * kTokenWarps + warp) * stretch;
   const uint64_t end = begin + stretch < a.n ? begin + stretch : a.n;
   unsigned long long* const buf[2] = {reinterpret_cast<unsigned long long*>(static_cast<unsigned char*>(a.ws) + eg_off_a()),
                                       reinterpret_cast<unsigned long long*>(static_cast<unsigned char*>(a.ws) + eg_off_b(a.n))};
-  uint32_t* const mine = counts + warp * kTokenDigits;
-  const uint32_t per = (bits + passes - 1) / passes, mask = (1u << per) - 1;
+  const uint32_t per = (bits + passes - 1) / passes, digits = 1u << per, mask = digits - 1;
+  // groups of warps whose counts of a digit one thread adds up: 1024 threads, a digit and a group each
+  const uint32_t groups = kTokenThreads / digits < kTokenWarps ? kTokenThreads / digits : kTokenWarps, group_warps = kTokenWarps / groups;
+  uint32_t* const mine = counts + warp * digits;
+  const uint32_t* const my_base = group_base + warp / group_warps * digits;
   // the first pass reads the tokens, the last one writes the first buffer
   for (uint32_t pass = 0; pass < passes; ++pass) {
     const uint32_t shift = 32 + pass * per;
     unsigned long long* const to = buf[(passes - 1 - pass) & 1];
     const unsigned long long* const from = buf[(passes - pass) & 1];
-    auto item = [&](uint64_t i) -> unsigned long long {
-      if (pass) return __ldcg(from + i);
-      const int64_t t = token_at(a.tokens, a.token_bytes, i);
-      if (t >= (int64_t)a.vocab) set_status(status, CVLC_ERR_INVALID_ARG);
-      return ((unsigned long long)(t >= 0 && t < (int64_t)a.vocab ? (uint32_t)t : (uint32_t)a.vocab) << 32) | (uint32_t)i;
-    };
-    // lanes with the same digit
-    auto peers_of = [&](uint32_t digit, uint32_t active) {
-      uint32_t m = active;
-      for (uint32_t b = 0; b < per; ++b) {
-        const uint32_t v = __ballot_sync(kFull, (digit >> b) & 1);
-        m &= (digit >> b) & 1 ? v : ~v;
-      }
-      return m;
-    };
-    for (uint32_t d = lane; d < kTokenDigits; d += 32) mine[d] = 0;
+    bool outside = false;
+    auto item = [&](uint64_t i) { return pass ? __ldcg(from + i) : sort_item(a, i, outside); };
+    for (uint32_t d = lane; d < digits; d += 32) mine[d] = 0;
     __syncwarp();
-    for (uint64_t base = begin; base < end; base += 32) {
-      const bool in = base + lane < end;
-      const uint32_t active = __ballot_sync(kFull, in);
-      const uint32_t digit = in ? (uint32_t)(item(base + lane) >> shift) & mask : 0;
-      const uint32_t peers = peers_of(digit, active);
-      if (in && lane == (uint32_t)__ffs(peers) - 1) mine[digit] += __popc(peers);
-      __syncwarp();
+    for (uint64_t base = begin; base < end; base += 32 * kSortAhead) {
+      unsigned long long it[kSortAhead];
+#pragma unroll
+      for (int j = 0; j < kSortAhead; ++j) it[j] = base + 32 * j + lane < end ? item(base + 32 * j + lane) : 0;
+#pragma unroll
+      for (int j = 0; j < kSortAhead; ++j)
+        if (base + 32 * j + lane < end) atomicAdd(&mine[(uint32_t)(it[j] >> shift) & mask], 1u);
     }
+    if (outside) set_status(status, CVLC_ERR_INVALID_ARG);
     __syncthreads();
-    for (uint32_t d = tid; d < kTokenDigits; d += kTokenThreads) {  // over the block's warps
+    for (uint32_t i = tid; i < groups * digits; i += kTokenThreads) {  // over a group's warps
+      const uint32_t d = i & mask, first = i / digits * group_warps;
       uint32_t sum = 0;
-      for (int w = 0; w < kTokenWarps; ++w) {
-        const uint32_t c = counts[w * kTokenDigits + d];
-        counts[w * kTokenDigits + d] = sum;
+      for (uint32_t w = first; w < first + group_warps; ++w) {
+        const uint32_t c = counts[w * digits + d];
+        counts[w * digits + d] = sum;
         sum += c;
       }
-      for (uint32_t r = 0; r < blocks; ++r) (blocks > 1 ? cluster.map_shared_rank(totals[rank], r) : totals[rank])[d] = sum;
+      group_base[i] = sum;
     }
-    if (blocks > 1) cluster.sync();
-    else __syncthreads();
+    __syncthreads();
+    if (tid < digits) {  // over the groups
+      uint32_t sum = 0;
+      for (uint32_t g = 0; g < groups; ++g) {
+        const uint32_t c = group_base[g * digits + tid];
+        group_base[g * digits + tid] = sum;
+        sum += c;
+      }
+      for (uint32_t r = 0; r < blocks; ++r) cluster.map_shared_rank(totals[rank], r)[tid] = sum;
+    }
+    cluster.sync();
     {  // over the digits, then over the blocks before this one
       uint32_t sum = 0, before = 0;
-      if (tid < kTokenDigits)
+      if (tid < digits)
         for (uint32_t r = 0; r < blocks; ++r) {
           if (r < rank) before += totals[r][tid];
           sum += totals[r][tid];
         }
-      uint32_t inc = sum;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const uint32_t v = __shfl_up_sync(kFull, inc, o);
-        if (lane >= (uint32_t)o) inc += v;
-      }
-      if (lane == 31) scan[warp] = inc;
-      __syncthreads();
-      if (warp == 0) {
-        uint32_t s = scan[lane];
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-          const uint32_t v = __shfl_up_sync(kFull, s, o);
-          if (lane >= (uint32_t)o) s += v;
-        }
-        scan[lane] = s;
-      }
-      __syncthreads();
-      if (tid < kTokenDigits) {
-        const uint32_t at = inc - sum + (warp ? scan[warp - 1] : 0) + before;
-        for (int w = 0; w < kTokenWarps; ++w) counts[w * kTokenDigits + tid] += at;
+      const uint32_t at = block_scan(sum, scan) + before;
+      if (tid < digits) {
+        for (uint32_t g = 0; g < groups; ++g) group_base[g * digits + tid] += at;
       }
       __syncthreads();
     }
-    for (uint64_t base = begin; base < end; base += 32) {
-      const bool in = base + lane < end;
-      const uint32_t active = __ballot_sync(kFull, in);
-      const unsigned long long it = in ? item(base + lane) : 0;
-      const uint32_t digit = in ? (uint32_t)(it >> shift) & mask : 0;
-      const uint32_t peers = peers_of(digit, active);
-      const uint32_t place = in ? mine[digit] : 0;
-      __syncwarp();
-      if (in) {
-        to[place + __popc(peers & ((1u << lane) - 1))] = it;
-        if (lane == (uint32_t)__ffs(peers) - 1) mine[digit] = place + __popc(peers);
+    for (uint64_t base = begin; base < end; base += 32 * kSortAhead) {
+      unsigned long long it[kSortAhead];
+#pragma unroll
+      for (int j = 0; j < kSortAhead; ++j) it[j] = base + 32 * j + lane < end ? item(base + 32 * j + lane) : 0;
+#pragma unroll
+      for (int j = 0; j < kSortAhead; ++j) {
+        if (base + 32 * j >= end) break;
+        place_items(it[j], base + 32 * j + lane < end, shift, per, mine, my_base, to);
       }
-      __syncwarp();
     }
-    if (blocks > 1) cluster.sync();
-    else __syncthreads();
+    cluster.sync();
   }
 }
 
 // ---- the gradient: sums ------------------------------------------------------------------------------
 constexpr int kSumThreads = 128;
-constexpr int kSumAhead = 8;  // rows whose loads a thread has in flight
+constexpr int kSumAhead = 8;   // rows whose loads a thread has in flight
+constexpr int kJoinAhead = 8;  // and pieces
 
 struct Sorted {
   const unsigned long long* at;
@@ -220,21 +351,42 @@ struct Sorted {
   __device__ __forceinline__ uint32_t word(uint64_t i) const { return i < n ? (uint32_t)(__ldg(at + i) >> 32) : vocab; }
 };
 
+// A word's row, or a part of it.  Added by reductions in memory, which nothing waits for: a row is added to once in a kernel, so they
+// have no order (reading the row first took k_embed_sum 22 us where it now takes 9).
 template <int E>
 __device__ __forceinline__ void put_row(const EmbedGradArgs& a, uint32_t word, uint32_t col, const float (&acc)[E]) {
   float* const u = a.update + (uint64_t)word * a.update_stride + (uint64_t)col * E;
   if constexpr (E == 1) {
-    u[0] = a.accumulate ? u[0] + a.scale * acc[0] : a.scale * acc[0];
+    if (a.accumulate) atomicAdd(u, a.scale * acc[0]);
+    else u[0] = a.scale * acc[0];
   } else {
 #pragma unroll
-    for (int q = 0; q < E / 4; ++q) {
-      float4* const p = reinterpret_cast<float4*>(u) + q;
-      float4 v = make_float4(a.scale * acc[4 * q], a.scale * acc[4 * q + 1], a.scale * acc[4 * q + 2], a.scale * acc[4 * q + 3]);
-      if (a.accumulate) {
-        const float4 o = *p;
-        v.x += o.x, v.y += o.y, v.z += o.z, v.w += o.w;
-      }
-      *p = v;
+    for (int q = 0; q < E; q += 4) {
+      const float4 v = make_float4(a.scale * acc[q], a.scale * acc[q + 1], a.scale * acc[q + 2], a.scale * acc[q + 3]);
+      if (a.accumulate) asm volatile("red.global.add.v4.f32 [%0], {%1, %2, %3, %4};" ::"l"(u + q), "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w) : "memory");
+      else __stcs(reinterpret_cast<float4*>(u + q), v);
+    }
+  }
+}
+
+template <int E>
+__device__ __forceinline__ void put_piece(float* p, const float (&v)[E]) {
+  if constexpr (E == 1) {
+    p[0] = v[0];
+  } else {
+#pragma unroll
+    for (int e = 0; e < E; e += 4) *reinterpret_cast<float4*>(p + e) = make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]);
+  }
+}
+template <int E>
+__device__ __forceinline__ void get_piece(const float* p, float (&v)[E]) {
+  if constexpr (E == 1) {
+    v[0] = p[0];
+  } else {
+#pragma unroll
+    for (int e = 0; e < E; e += 4) {
+      const float4 q = *reinterpret_cast<const float4*>(p + e);
+      v[e] = q.x, v[e + 1] = q.y, v[e + 2] = q.z, v[e + 3] = q.w;
     }
   }
 }
@@ -263,31 +415,34 @@ __global__ void __launch_bounds__(kSumThreads) k_embed_sum(EmbedGradArgs a, uint
   for (int e = 0; e < E; ++e) acc[e] = 0.f;
   bool begun_before = before == words[0];
   for (uint32_t i = 0; i < chunk; i += kSumAhead) {
-    float f[kSumAhead][E];
-    if constexpr (VEC) {
-      uint4 raw[kSumAhead] = {};
+    uint4 raw[VEC ? kSumAhead : 1] = {};
+    float one[VEC ? 1 : kSumAhead];
 #pragma unroll
-      for (int r = 0; r < kSumAhead; ++r)
-        if (words[i + r] != S.vocab) raw[r] = __ldcs(reinterpret_cast<const uint4*>(grad + (uint64_t)where[i + r] * a.grad_stride));
-#pragma unroll
-      for (int r = 0; r < kSumAhead; ++r) widen<T>(raw[r], f[r]);
-    } else {
-#pragma unroll
-      for (int r = 0; r < kSumAhead; ++r) f[r][0] = words[i + r] == S.vocab ? 0.f : to_float(grad[(uint64_t)where[i + r] * a.grad_stride]);
+    for (int r = 0; r < kSumAhead; ++r) {
+      const T* const from = grad + (uint64_t)where[i + r] * a.grad_stride;
+      if constexpr (VEC) {
+        if (words[i + r] != S.vocab) raw[r] = __ldcs(reinterpret_cast<const uint4*>(from));
+      } else {
+        one[r] = words[i + r] == S.vocab ? 0.f : to_float(*from);
+      }
     }
 #pragma unroll
     for (int r = 0; r < kSumAhead; ++r) {
       const uint32_t w = words[i + r];
       if (w == S.vocab) return;  // behind the last word
+      if constexpr (VEC) {
+        float f[E];
+        widen<T>(raw[r], f);
 #pragma unroll
-      for (int e = 0; e < E; ++e) acc[e] += f[r][e];
+        for (int e = 0; e < E; ++e) acc[e] += f[e];
+      } else {
+        acc[0] += one[r];
+      }
       const bool last = i + r + 1 == chunk;
       const uint32_t next = last ? after : words[i + r + 1];
       if (next == w && !last) continue;
       if (begun_before || next == w) {
-        float* const p = pieces + ((uint64_t)blockIdx.x * 2 + (begun_before ? 0 : 1)) * a.dim + (uint64_t)col * E;
-#pragma unroll
-        for (int e = 0; e < E; ++e) p[e] = acc[e];
+        put_piece<E>(pieces + ((uint64_t)blockIdx.x * 2 + (begun_before ? 0 : 1)) * a.dim + (uint64_t)col * E, acc);
       } else {
         put_row<E>(a, w, col, acc);
       }
@@ -308,22 +463,26 @@ __global__ void __launch_bounds__(kSumThreads) k_embed_join(EmbedGradArgs a, uin
   if (w == S.vocab || S.word(next) != w) return;
   if (first && S.word(first - 1) == w) return;  // it began earlier
   const uint32_t col = blockIdx.y * kSumThreads + threadIdx.x;
-  if (col >= a.dim / E) return;
-  uint64_t lo = next, hi = a.n;  // the first place behind the word
-  while (lo < hi) {
-    const uint64_t mid = lo + (hi - lo) / 2;
-    if (S.word(mid) == w) lo = mid + 1;
-    else hi = mid;
+  uint64_t last = c + 1;  // the last chunk that begins with the word, 32 chunks at a time
+  for (;; last += 32) {
+    const uint32_t more = __ballot_sync(kFull, S.word((last + 1 + (threadIdx.x & 31)) * chunk) == w);
+    if (more != kFull) {
+      last += __ffs(~more) - 1;
+      break;
+    }
   }
-  const uint64_t last = (lo - 1) / chunk;
+  if (col >= a.dim / E) return;
   float acc[E];
-  const float* p = pieces + (c * 2 + 1) * a.dim + (uint64_t)col * E;
+  get_piece<E>(pieces + (c * 2 + 1) * a.dim + (uint64_t)col * E, acc);
+  for (uint64_t o = c + 1; o <= last; o += kJoinAhead) {
+    float f[kJoinAhead][E];
 #pragma unroll
-  for (int e = 0; e < E; ++e) acc[e] = p[e];
-  for (uint64_t o = c + 1; o <= last; ++o) {
-    p = pieces + o * 2 * a.dim + (uint64_t)col * E;
+    for (int j = 0; j < kJoinAhead; ++j) get_piece<E>(pieces + (o + j <= last ? o + j : last) * 2 * a.dim + (uint64_t)col * E, f[j]);
 #pragma unroll
-    for (int e = 0; e < E; ++e) acc[e] += p[e];
+    for (int j = 0; j < kJoinAhead; ++j)
+      if (o + j <= last)
+#pragma unroll
+        for (int e = 0; e < E; ++e) acc[e] += f[j][e];
   }
   put_row<E>(a, w, col, acc);
 }
@@ -361,19 +520,53 @@ cudaError_t embed_grad_typed(const EmbedGradArgs& a, cudaStream_t st) {
   return cudaGetLastError();
 }
 
+// clusters of the sort that the current device runs at once, asked for once per device
+uint32_t clusters_at_once() {
+  static OncePerDevice once;
+  static std::atomic<int> known[64];
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 2;
+  const cudaError_t e = once_per_device(once, [&] {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(kNumSM / kMaxClusterBlocks * kMaxClusterBlocks);
+    cfg.blockDim = dim3(kTokenThreads);
+    cfg.dynamicSmemBytes = kTokenShared;
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = kMaxClusterBlocks;
+    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    int n = 0;
+    const cudaError_t r = cudaOccupancyMaxActiveClusters(&n, k_token_sort, &cfg);
+    if (r == cudaSuccess) known[dev].store(n < 2 ? 2 : n, std::memory_order_relaxed);
+    return r;
+  });
+  return e == cudaSuccess ? (uint32_t)known[dev].load(std::memory_order_relaxed) : 2;
+}
+
 cudaError_t launch_token_sort(const EmbedGradArgs& a, cudaStream_t st) {
   uint32_t bits = 1;
   while ((a.vocab >> bits) != 0) ++bits;  // words 0 .. vocab
   const uint32_t passes = (bits + 8) / 9;
-  const uint32_t blocks = a.n <= 2 * kTokenThreads ? 1 : kMaxClusterBlocks;
-  const cudaError_t allowed = allow_shared(k_token_sort, kTokenShared);
+  const uint32_t blocks = a.n <= kBlockSort ? 1 : kMaxClusterBlocks;
+  const size_t smem = kTokenShared + (blocks == 1 ? (a.n < kTokenThreads ? kTokenThreads : a.n) * 8 : 0);
+  const cudaError_t allowed = allow_shared(k_token_sort, kTokenShared + kBlockSort * 8);
   if (allowed != cudaSuccess) return allowed;
   LaunchScope ls(kKTokenSort, st);
   cudaLaunchConfig_t cfg = {};
-  const uint32_t fill = a.accumulate ? 0 : (fill_grid(a.vocab * a.dim, 4 * kTokenThreads, kNumSM) + blocks - 1) / blocks * blocks;
+  // blocks beside those of the sort that write zeros: as many whole clusters as run at once, since a second round of them would double the time
+  uint32_t fill = 0;
+  if (!a.accumulate) {
+    fill = fill_grid(a.vocab * a.dim, 4 * kTokenThreads, kNumSM - 1);
+    if (blocks > 1) {
+      const uint32_t most = (clusters_at_once() - 1) * blocks;
+      fill = std::min((fill + blocks - 1) / blocks * blocks, most);
+    }
+  }
   cfg.gridDim = dim3(blocks + fill);
   cfg.blockDim = dim3(kTokenThreads);
-  cfg.dynamicSmemBytes = kTokenShared;
+  cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
   cudaLaunchAttribute attr;
   attr.id = cudaLaunchAttributeClusterDimension;
