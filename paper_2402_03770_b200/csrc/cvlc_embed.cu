@@ -22,46 +22,93 @@ __device__ __forceinline__ int64_t token_at(const void* tokens, uint32_t token_b
 constexpr int kLookupThreads = 256;
 constexpr int kLookupRows = 4;  // tokens of a thread: that many independent loads
 
-// A block has blockDim.x columns (vectors of a row) by blockDim.y groups of kLookupRows tokens.
+// A block has blockDim.x columns (vectors of a row) by blockDim.y groups of kLookupRows tokens, and goes from groups to groups: the next ones'
+// tokens are on their way while this one's rows are.  (A block for every group, which has to wait for its tokens first: 32768 rows of 8 KB
+// 76 us.)
 template <class T, bool VEC>
 __global__ void __launch_bounds__(kLookupThreads, 6) k_embed(EmbedArgs a) {
   constexpr int E = VEC ? kPerVec<T> : 1;
   constexpr uint32_t kPadding = 0xFFFFFFFFu;
   const uint32_t cols = a.dim / E;
-  const uint64_t first = ((uint64_t)blockIdx.x * blockDim.y + threadIdx.y) * kLookupRows;
   const T* const table = static_cast<const T*>(a.table);
-  T* const out = static_cast<T*>(a.out) + first * a.out_stride;
-  const uint32_t rows = first < a.n ? (uint32_t)min((uint64_t)kLookupRows, a.n - first) : 0;
-  uint32_t word[kLookupRows];
+  const uint64_t step = (uint64_t)gridDim.x * blockDim.y * kLookupRows;
+  uint64_t first = ((uint64_t)blockIdx.x * blockDim.y + threadIdx.y) * kLookupRows;
   bool outside = false;
+  uint32_t word[kLookupRows], next[kLookupRows];
+  const auto fetch = [&](uint64_t from, uint32_t (&w)[kLookupRows]) {
 #pragma unroll
-  for (int r = 0; r < kLookupRows; ++r) {
-    const int64_t t = r < rows ? token_at(a.tokens, a.token_bytes, first + r) : -1;
-    word[r] = t >= 0 && t < (int64_t)a.vocab ? (uint32_t)t : kPadding;
-    outside |= t >= (int64_t)a.vocab;
+    for (int r = 0; r < kLookupRows; ++r) {
+      const int64_t t = from + r < a.n ? token_at(a.tokens, a.token_bytes, from + r) : -1;
+      w[r] = t >= 0 && t < (int64_t)a.vocab ? (uint32_t)t : kPadding;
+      outside |= t >= (int64_t)a.vocab;
+    }
+  };
+  fetch(first, word);
+  for (; first < a.n; first += step) {
+    fetch(first + step, next);
+    T* const out = static_cast<T*>(a.out) + first * a.out_stride;
+    const uint32_t rows = (uint32_t)min((uint64_t)kLookupRows, a.n - first);
+    for (uint32_t c = blockIdx.y * blockDim.x + threadIdx.x; c < cols; c += gridDim.y * blockDim.x) {
+      if constexpr (VEC) {
+        uint4 raw[kLookupRows];
+#pragma unroll
+        for (int r = 0; r < kLookupRows; ++r) {
+          raw[r] = make_uint4(0, 0, 0, 0);
+          if (word[r] != kPadding) raw[r] = __ldg(reinterpret_cast<const uint4*>(table + word[r] * a.table_stride) + c);
+        }
+#pragma unroll
+        for (int r = 0; r < kLookupRows; ++r) {
+          if (r >= rows) break;
+          float f[E];
+          widen<T>(raw[r], f);
+#pragma unroll
+          for (int e = 0; e < E; ++e) f[e] = word[r] != kPadding ? f[e] * a.scale : 0.f;
+          __stcs(reinterpret_cast<uint4*>(out + r * a.out_stride) + c, narrow<T>(f));
+        }
+      } else {
+#pragma unroll
+        for (int r = 0; r < kLookupRows; ++r)
+          if (r < rows) out[r * a.out_stride + c] = from_float<T>(word[r] != kPadding ? to_float(table[word[r] * a.table_stride + c]) * a.scale : 0.f);
+      }
+    }
+#pragma unroll
+    for (int r = 0; r < kLookupRows; ++r) word[r] = next[r];
   }
   if (outside && a.status) set_status(a.status, CVLC_ERR_INVALID_ARG);
-  for (uint32_t c = blockIdx.y * blockDim.x + threadIdx.x; c < cols; c += gridDim.y * blockDim.x) {
-    if constexpr (VEC) {
-      uint4 raw[kLookupRows];
+}
+
+// Long rows: a warp for a row, kLookupWide vectors of a lane on their way, and the next row's token.
+constexpr int kLookupWide = 8;
+template <class T>
+__global__ void __launch_bounds__(kLookupThreads, 4) k_embed_wide(EmbedArgs a) {
+  constexpr int E = kPerVec<T>;
+  const uint32_t cols = a.dim / E, lane = threadIdx.x & 31;
+  const uint64_t step = (uint64_t)gridDim.x * (kLookupThreads / 32);
+  uint64_t row = (uint64_t)blockIdx.x * (kLookupThreads / 32) + (threadIdx.x >> 5);
+  int64_t next = row < a.n ? token_at(a.tokens, a.token_bytes, row) : -1;
+  for (; row < a.n; row += step) {
+    const int64_t word = next;
+    next = row + step < a.n ? token_at(a.tokens, a.token_bytes, row + step) : -1;
+    const bool there = word >= 0 && word < (int64_t)a.vocab;
+    if (word >= (int64_t)a.vocab && a.status) set_status(a.status, CVLC_ERR_INVALID_ARG);
+    const uint4* const from = reinterpret_cast<const uint4*>(static_cast<const T*>(a.table) + (there ? (uint64_t)word : 0) * a.table_stride);
+    uint4* const to = reinterpret_cast<uint4*>(static_cast<T*>(a.out) + row * a.out_stride);
+    for (uint32_t c = lane; c < cols; c += 32 * kLookupWide) {
+      uint4 raw[kLookupWide];
 #pragma unroll
-      for (int r = 0; r < kLookupRows; ++r) {
-        raw[r] = make_uint4(0, 0, 0, 0);
-        if (word[r] != kPadding) raw[r] = __ldg(reinterpret_cast<const uint4*>(table + word[r] * a.table_stride) + c);
+      for (int j = 0; j < kLookupWide; ++j) {
+        raw[j] = make_uint4(0, 0, 0, 0);
+        if (there && c + 32 * j < cols) raw[j] = __ldg(from + c + 32 * j);
       }
 #pragma unroll
-      for (int r = 0; r < kLookupRows; ++r) {
-        if (r >= rows) break;
+      for (int j = 0; j < kLookupWide; ++j) {
+        if (c + 32 * j >= cols) break;
         float f[E];
-        widen<T>(raw[r], f);
+        widen<T>(raw[j], f);
 #pragma unroll
-        for (int e = 0; e < E; ++e) f[e] = word[r] != kPadding ? f[e] * a.scale : 0.f;
-        __stcs(reinterpret_cast<uint4*>(out + r * a.out_stride) + c, narrow<T>(f));
+        for (int e = 0; e < E; ++e) f[e] = there ? f[e] * a.scale : 0.f;
+        __stcs(to + c + 32 * j, narrow<T>(f));
       }
-    } else {
-#pragma unroll
-      for (int r = 0; r < kLookupRows; ++r)
-        if (r < rows) out[r * a.out_stride + c] = from_float<T>(word[r] != kPadding ? to_float(table[word[r] * a.table_stride + c]) * a.scale : 0.f);
     }
   }
 }
@@ -496,9 +543,14 @@ cudaError_t embed_typed(const EmbedArgs& a, cudaStream_t st) {
   while (x < kLookupThreads && x < cols) x *= 2;
   const dim3 block(x, kLookupThreads / x);
   const uint64_t rows = (uint64_t)block.y * kLookupRows;
-  const uint64_t gx = (a.n + rows - 1) / rows;
-  uint64_t gy = (cols + x - 1) / x;
-  if (gy > 65535) gy = 65535;
+  const uint64_t resident = 6 * kNumSM;
+  const uint64_t gy = std::min<uint64_t>((cols + x - 1) / x, resident);
+  const uint64_t gx = std::min((a.n + rows - 1) / rows, (resident + gy - 1) / gy);
+  if (vec && cols >= 128) {
+    const uint64_t blocks = (a.n + kLookupThreads / 32 - 1) / (kLookupThreads / 32);
+    launch_kernel(kKEmbed, k_embed_wide<T>, dim3((unsigned)std::min<uint64_t>(blocks, 4 * kNumSM)), dim3(kLookupThreads), 0, st, false, a);
+    return cudaGetLastError();
+  }
   void (*const kernel)(EmbedArgs) = vec ? k_embed<T, true> : k_embed<T, false>;
   launch_kernel(kKEmbed, kernel, dim3((unsigned)gx, (unsigned)gy), block, 0, st, false, a);
   return cudaGetLastError();
