@@ -1240,22 +1240,24 @@ __device__ __forceinline__ uint32_t reaching(const uint4& raw, float least) {
 }
 // Elements from `least` on (a candidate: value and word) of some vectors, into a list of `room`; word_of(j): the first word of the j-th.
 // Few threads have any, and hardly one more than one: they find theirs one by one.
+template <class T, class F>
+__device__ __forceinline__ void list_vec(const uint4& raw, F&& word_of, unsigned long long least, float floor_value, uint32_t* count,
+                                         unsigned long long* to, uint32_t room) {
+  for (uint32_t bits = reaching<T>(raw, floor_value); bits; bits &= bits - 1) {
+    const uint32_t e = __ffs(bits) - 1;
+    const unsigned long long c = candidate(order_of(element_of<T>(raw, e)), (uint32_t)(word_of() + (int)e));
+    if (c < least) continue;
+    const uint32_t n = atomicAdd(count, 1u);
+    if (n < room) to[n] = c;
+  }
+}
 template <class T, int NV, class F>
 __device__ __forceinline__ void list_batch(const uint4 (&raw)[NV], F&& word_of, unsigned long long least, uint32_t* count, unsigned long long* to,
                                            uint32_t room) {
   const float floor_value = value_of((uint32_t)(least >> 32));
 #pragma unroll
-  for (int j = 0; j < NV; ++j) {
-    const bool any = vec_max<T>(raw[j]) >= floor_value;
-    if (!any) continue;
-    for (uint32_t bits = reaching<T>(raw[j], floor_value); bits; bits &= bits - 1) {
-      const uint32_t e = __ffs(bits) - 1;
-      const unsigned long long c = candidate(order_of(element_of<T>(raw[j], e)), (uint32_t)(word_of(j) + (int)e));
-      if (c < least) continue;
-      const uint32_t n = atomicAdd(count, 1u);
-      if (n < room) to[n] = c;
-    }
-  }
+  for (int j = 0; j < NV; ++j)
+    if (vec_max<T>(raw[j]) >= floor_value) list_vec<T>(raw[j], [&] { return word_of(j); }, least, floor_value, count, to, room);
 }
 
 // Digits of the candidates of some vectors that share a prefix, counted; equal ones in a row at once
@@ -1491,6 +1493,9 @@ __global__ void __launch_bounds__(kRowThreads, 2) k_top_logits(TopArgs a, uint32
 
 // Many long rows: as in k_distill_stream, a block goes from row to row, and the side warps rank what the pass over a row has listed while the
 // next row is passed over.  (2048 x 131072 bf16, k = 64: a block for every row 200 us.)
+// What the pass lists is whole vectors, each with its largest element: for a thread of a warp that alone has found one, the elements
+// would take many instructions of the whole warp.  The side warps read those again that the last bound leaves.
+constexpr uint32_t kEndWord = 0x80000000u;  // a listed word, not a vector
 struct RowTop {
   MaxSum of_warp[kStreamWarps];
   uint32_t count, bound;
@@ -1502,6 +1507,7 @@ __global__ void __launch_bounds__(kStreamBlock, 2) k_top_stream(TopArgs a, uint3
   __shared__ RowTop tops[2];
   __shared__ uint32_t hist[256];
   static_assert(kStreamLanes == 256, "a bin for each thread");
+  __shared__ uint32_t side_hist[256], side_picked, side_above;
   __shared__ uint32_t mine, picked, above, largest, smallest, kept;
   constexpr int E = kPerVec<T>;
   const uint32_t thread = threadIdx.x, lane = thread & 31;
@@ -1537,9 +1543,55 @@ __global__ void __launch_bounds__(kStreamBlock, 2) k_top_stream(TopArgs a, uint3
       } else {
         const unsigned long long* const list = lists + buf * kTopList;
         const uint32_t c = s.count, bound = s.bound;
-        for (uint32_t i = t; i < c; i += kSideLanes)
-          if ((uint32_t)(list[i] >> 32) >= bound) packed[atomicAdd(&kept, 1u)] = list[i];
-        some_sync<kSideLanes>(kBarSide);
+        const RowAt R = row_at<T>(where, row);
+        const uint4* const from = reinterpret_cast<const uint4*>(R.from) + R.whole_from;
+        // f(value, word) of every listed element
+        const auto each = [&](auto&& f) {
+          for (uint32_t i = t; i < c; i += kSideLanes) {
+            const uint32_t order = (uint32_t)(list[i] >> 32), id = (uint32_t)list[i];
+            if (order < bound) continue;
+            if (id & kEndWord) {
+              f(value_of(order), id & ~kEndWord);
+            } else {
+              float v[E];
+              widen<T>(__ldg(from + id), v);
+              const int word = (int)((R.whole_from + id) * E) - (int)R.lead;
+#pragma unroll
+              for (int e = 0; e < E; ++e) f(v[e], (uint32_t)(word + e));
+            }
+          }
+        };
+        const auto keep = [&](unsigned long long least) {
+          each([&](float v, uint32_t word) {
+            if (!(v >= value_of((uint32_t)(least >> 32)))) return;
+            const unsigned long long x = candidate(order_of(v), word);
+            if (x < least) return;
+            const uint32_t n = atomicAdd(&kept, 1u);
+            if (n < kTopList) packed[n] = x;
+          });
+          some_sync<kSideLanes>(kBarSide);
+        };
+        keep((unsigned long long)bound << 32);
+        if (kept > kTopList) {  // equal elements in many of the vectors: the k-th largest among them, eight bits at a time
+          unsigned long long prefix = 0;
+          uint32_t left = a.k;
+          for (int shift = 56; shift >= 0; shift -= 8) {
+            for (uint32_t i = t; i < 256; i += kSideLanes) side_hist[i] = 0;
+            some_sync<kSideLanes>(kBarSide);
+            DigitCount<T> digits = {side_hist, 0, 0};
+            each([&](float v, uint32_t word) { digits.one(v, word, prefix, shift); });
+            digits.done();
+            some_sync<kSideLanes>(kBarSide);
+            if (t < 32) pick_digit([&](uint32_t d) { return side_hist[d]; }, left, &side_picked, &side_above);
+            some_sync<kSideLanes>(kBarSide);
+            prefix = (prefix << 8) | side_picked;
+            left -= side_above;
+          }
+          some_sync<kSideLanes>(kBarSide);
+          if (t == 0) kept = 0;
+          some_sync<kSideLanes>(kBarSide);
+          keep(prefix);
+        }
         put_records(a, row, all, packed, kept, t, kSideLanes, [] { some_sync<kSideLanes>(kBarSide); });
         some_sync<kSideLanes>(kBarSide);
         if (t == 0) kept = 0;
@@ -1568,23 +1620,17 @@ __global__ void __launch_bounds__(kStreamBlock, 2) k_top_stream(TopArgs a, uint3
     float top[2] = {-CUDART_INF_F, -CUDART_INF_F};  // the thread's largest, of every other vector
     uint32_t bound = kOrderNegInf + 1, next_raise = 0;
     const uint32_t cuts = (R.wholes + kStageVecs - 1) / kStageVecs;
-    const auto list_end = [&](unsigned long long least) {
-      if (end_z > -CUDART_INF_F) {
-        const unsigned long long c = candidate(order_of(end_z), (uint32_t)end);
-        if (c >= least) {
-          const uint32_t n = atomicAdd(&mine, 1u);
-          if (n < kTopList) list[n] = c;
-        }
-      }
+    const auto note = [&](uint32_t order, uint32_t id) {
+      const uint32_t n = atomicAdd(&mine, 1u);
+      if (n < kTopList) list[n] = (unsigned long long)order << 32 | id;
     };
     for (uint32_t b = 0; b < cuts; ++b) {
       uint4 raw[kStageShare];
       take_stage<T>(ring, stage, phase, stages, full, empty, b * kStageVecs, R.wholes, ok, raw);
-      float halves[2] = {vec_max<T>(raw[0]), vec_max<T>(raw[1])};
+      float largest_of[kStageShare];
 #pragma unroll
-      for (int j = 2; j < kStageShare; ++j) halves[j & 1] = fmaxf(halves[j & 1], vec_max<T>(raw[j]));
-      top[0] = fmaxf(top[0], halves[0]), top[1] = fmaxf(top[1], halves[1]);
-      const float top_of = fmaxf(halves[0], halves[1]);
+      for (int j = 0; j < kStageShare; ++j) largest_of[j] = vec_max<T>(raw[j]), top[j & 1] = fmaxf(top[j & 1], largest_of[j]);
+      const float top_of = fmaxf(fmaxf(largest_of[0], largest_of[1]), fmaxf(largest_of[2], largest_of[3]));
       add_share<T>(raw, top_of, c2, acc);
       if (b + 1 == cuts || b == next_raise) {
         // The bound is raised by a histogram of the threads' maxima (two of a thread) between the last bound (at first: the smallest of
@@ -1613,12 +1659,14 @@ __global__ void __launch_bounds__(kStreamBlock, 2) k_top_stream(TopArgs a, uint3
         }
         bound = lo;
       }
-      if (__any_sync(kFull, top_of >= value_of(bound))) {  // few do: the warp goes around it
-        const int word = (int)((R.whole_from + b * kStageVecs + tid) * E) - (int)R.lead;
-        list_batch<T, kStageShare>(raw, [&](int j) { return word + j * kStreamLanes * E; }, (unsigned long long)bound << 32, &mine, list, kTopList);
+      const float floor_value = value_of(bound);
+      if (__any_sync(kFull, top_of >= floor_value)) {  // the warp goes around what none of its threads has
+#pragma unroll
+        for (int j = 0; j < kStageShare; ++j)
+          if (largest_of[j] >= floor_value) note(order_of(largest_of[j]), b * kStageVecs + tid + j * kStreamLanes);
       }
     }
-    list_end((unsigned long long)bound << 32);
+    if (end_z >= value_of(bound)) note(order_of(end_z), kEndWord | (uint32_t)end);
     if (!ok) acc.sum = CUDART_NAN_F;  // a wait has run out: the row is void
     const MaxSum warp = warp_join(acc, c2);
     if (lane == 0) tops[buf].of_warp[tid >> 5] = warp;
@@ -1645,11 +1693,17 @@ __global__ void __launch_bounds__(kStreamBlock, 2) k_top_stream(TopArgs a, uint3
       some_sync<kStreamLanes>(kBarStream);
       if (tid == 0) mine = 0;
       some_sync<kStreamLanes>(kBarStream);
+      // its k candidates stand in the list as words
+      const float floor_value = value_of((uint32_t)(prefix >> 32));
       for (uint32_t i = tid; i < R.wholes; i += kStreamLanes) {
-        const uint4 raw[1] = {__ldg(from + i)};
-        list_batch<T, 1>(raw, [&](int) { return (int)((R.whole_from + i) * E) - (int)R.lead; }, prefix, &mine, list, kTopList);
+        const uint4 raw = __ldg(from + i);
+        const int word = (int)((R.whole_from + i) * E) - (int)R.lead;
+        for (uint32_t bits = reaching<T>(raw, floor_value); bits; bits &= bits - 1) {
+          const uint32_t e = __ffs(bits) - 1, order = order_of(element_of<T>(raw, e));
+          if (candidate(order, (uint32_t)(word + (int)e)) >= prefix) note(order, kEndWord | (uint32_t)(word + (int)e));
+        }
       }
-      list_end(prefix);
+      if (end_z > -CUDART_INF_F && candidate(order_of(end_z), (uint32_t)end) >= prefix) note(order_of(end_z), kEndWord | (uint32_t)end);
       bound = (uint32_t)(prefix >> 32);
       some_sync<kStreamLanes>(kBarStream);
     }

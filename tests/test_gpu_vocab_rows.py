@@ -43,6 +43,9 @@ def logits_of(rows, vocab, dtype, seed, kind="normal", pad=0, lead=0):
         z = torch.where(torch.rand(rows, vocab, generator=g) < 0.5, 0.0, -0.0)
     elif kind == "far":
         z = z + 3.0e4 * (1 if dtype == torch.float16 else 1e3)
+    elif kind == "crowd":  # many equal ones at the top, in few 16 bytes
+        z = z.round().clamp(max=2)
+        z[:, 100:100 + min(12000, vocab // 3)] = 5
     elif kind == "front":  # the large ones lie together
         z[:, :max(1, vocab // 50)] += 30
     return rows_of(z.to(dtype), dtype, pad, lead)
@@ -100,7 +103,7 @@ def test_top_logits_spoiled_rows(dtype):
 
 @pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("kind,lead,pad,k", [("normal", 0, 0, 64), ("ties", 1, 1, 256), ("equal", 0, 3, 20), ("masked", 3, 0, 100), ("lowest", 0, 8, 256),
-                                             ("zeros", 5, 0, 33), ("far", 0, 1, 1), ("front", 1, 0, 200)])
+                                             ("zeros", 5, 0, 33), ("far", 0, 1, 1), ("front", 1, 0, 200), ("crowd", 1, 1, 256), ("crowd", 0, 0, 3)])
 def test_top_logits_of_many_long_rows(dtype, kind, lead, pad, k):
     """more rows than blocks, each of several stages"""
     B = binding()
