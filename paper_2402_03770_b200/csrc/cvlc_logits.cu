@@ -1542,7 +1542,25 @@ __global__ void __launch_bounds__(kStreamBlock, 2) k_top_stream(TopArgs a, uint3
         put_spoiled(a, row, t, kSideLanes);
       } else {
         const unsigned long long* const list = lists + buf * kTopList;
-        const uint32_t c = s.count, bound = s.bound;
+        const uint32_t c = s.count;
+        uint32_t bound = s.bound;
+        if (c > a.k) {  // the k-th largest of what is listed, to a bin, is the last bound
+          for (uint32_t i = t; i < 256; i += kSideLanes) side_hist[i] = 0;
+          some_sync<kSideLanes>(kBarSide);
+          const uint32_t hi = max(order_of(all.max), bound), shift = hi > bound ? max(24 - __clz(hi - bound), 0) : 0;
+          for (uint32_t i = t; i < c; i += kSideLanes) {
+            const uint32_t order = (uint32_t)(list[i] >> 32);
+            if (order >= bound) atomicAdd(&side_hist[min((order - bound) >> shift, 255u)], 1u);
+          }
+          some_sync<kSideLanes>(kBarSide);
+          if (t < 32) {
+            if (t == 0) side_picked = 0;
+            __syncwarp();
+            pick_digit([&](uint32_t d) { return side_hist[d]; }, a.k, &side_picked, &side_above);
+          }
+          some_sync<kSideLanes>(kBarSide);
+          bound += side_picked << shift;
+        }
         const RowAt R = row_at<T>(where, row);
         const uint4* const from = reinterpret_cast<const uint4*>(R.from) + R.whole_from;
         // f(value, word) of every listed element
@@ -1615,7 +1633,7 @@ __global__ void __launch_bounds__(kStreamBlock, 2) k_top_stream(TopArgs a, uint3
     unsigned long long* const list = lists + buf * kTopList;
     MaxSum acc = {end_z, end_z == -CUDART_INF_F ? 0.f : end_z < CUDART_INF_F ? 1.f : CUDART_NAN_F};
     if (end_z != end_z) acc.max = -CUDART_INF_F;
-    // after 1, 4, 16, .. stages, which lists about 7 k elements; after 1, 2, 4, .. where that could be too many
+    // after 1, 4, 16, .. stages, which lists about 7 k vectors; after 1, 2, 4, .. where that could be too many
     const uint32_t often = a.k <= 96 ? 4 : 2;
     float top[2] = {-CUDART_INF_F, -CUDART_INF_F};  // the thread's largest, of every other vector
     uint32_t bound = kOrderNegInf + 1, next_raise = 0;
@@ -1632,7 +1650,7 @@ __global__ void __launch_bounds__(kStreamBlock, 2) k_top_stream(TopArgs a, uint3
       for (int j = 0; j < kStageShare; ++j) largest_of[j] = vec_max<T>(raw[j]), top[j & 1] = fmaxf(top[j & 1], largest_of[j]);
       const float top_of = fmaxf(fmaxf(largest_of[0], largest_of[1]), fmaxf(largest_of[2], largest_of[3]));
       add_share<T>(raw, top_of, c2, acc);
-      if (b + 1 == cuts || b == next_raise) {
+      if (b == next_raise && b + 1 < cuts) {
         // The bound is raised by a histogram of the threads' maxima (two of a thread) between the last bound (at first: the smallest of
         // them) and the largest
         next_raise = next_raise * often + often - 1;
@@ -1654,8 +1672,8 @@ __global__ void __launch_bounds__(kStreamBlock, 2) k_top_stream(TopArgs a, uint3
           }
           some_sync<kStreamLanes>(kBarStream);
           lo += picked << shift;
-          if (shift <= 17) break;
-          hi = lo + ((1u << shift) - 1), left -= above;  // a bin of more than 1 / 64 of an octave: its own histogram
+          if (shift <= 18) break;
+          hi = lo + ((1u << shift) - 1), left -= above;  // a bin of more than 1 / 32 of an octave: its own histogram
         }
         bound = lo;
       }
