@@ -603,7 +603,8 @@ cudaError_t launch_token_sort(const EmbedGradArgs& a, cudaStream_t st) {
   const uint32_t passes = (bits + 8) / 9;
   const uint32_t blocks = a.n <= kBlockSort ? 1 : kMaxClusterBlocks;
   const size_t smem = kTokenShared + (blocks == 1 ? (a.n < kTokenThreads ? kTokenThreads : a.n) * 8 : 0);
-  const cudaError_t allowed = allow_shared(k_token_sort, kTokenShared + kBlockSort * 8);
+  static OncePerDevice once;
+  const cudaError_t allowed = once_per_device(once, [] { return allow_shared(k_token_sort, kTokenShared + kBlockSort * 8); });
   if (allowed != cudaSuccess) return allowed;
   LaunchScope ls(kKTokenSort, st);
   cudaLaunchConfig_t cfg = {};

@@ -1080,7 +1080,9 @@ __global__ void __launch_bounds__(kStreamBlock, 2) k_distill_stream(DistillArgs 
 // how a call's rows are cut: blocks of a cluster for each, threads of a block
 struct Cut {
   uint32_t log_blocks, threads, rounds;  // rounds: vectors of a thread at most
+  bool few;                              // kFewVecs vectors of a thread hold the block's share
 };
+constexpr int kFewVecs = 2;  // short shares have more threads instead, each of which is done sooner
 
 // `keep`: most vectors a thread keeps, where the second half works from them (0: it does not).  Blocks of a cluster: as many as keep the row,
 // and, where rows are few, as many as give every SM two blocks.
@@ -1088,11 +1090,13 @@ Cut cut_rows(const void* logits, uint64_t stride, uint64_t rows, uint32_t vocab,
   const uint32_t per_vec = 16 / size;
   const bool even = (reinterpret_cast<uintptr_t>(logits) & 15) == 0 && stride * size % 16 == 0;  // every row begins with a vector
   const uint32_t vecs = (vocab + per_vec - 1) / per_vec + (even ? 0 : 1), tiles = (vecs + 31) / 32;
-  Cut c = {0, 0, 0};
+  Cut c = {0, 0, 0, false};
   const auto share = [&] { return ((tiles + (1u << c.log_blocks) - 1) >> c.log_blocks) * 32; };
   if (keep)
     while (c.log_blocks < 3 && share() > keep * kRowThreads) ++c.log_blocks;
   while (c.log_blocks < 3 && (rows << c.log_blocks) < 2 * kNumSM && (vecs >> c.log_blocks) >= 512) ++c.log_blocks;
+  c.few = share() <= kFewVecs * kRowThreads;
+  if (c.few) nv = kFewVecs;
   const uint32_t t = ((share() + nv - 1) / nv + 31) & ~31u;
   c.threads = t < 64 ? 64 : (t > kRowThreads ? kRowThreads : t);
   c.rounds = (share() + c.threads - 1) / c.threads;
@@ -1136,7 +1140,8 @@ cudaError_t distill_typed(const DistillArgs& a, cudaStream_t st) {
     const uint32_t stages = fit < kStagesMost ? fit : kStagesMost;
     const size_t smem = (size_t)stages * kStageVecs * 16 + beside;
     void (*const kernel)(DistillArgs, uint32_t, uint32_t) = k_distill_stream<T, KIND>;
-    const cudaError_t e = allow_shared(kernel, smem);
+    static OncePerDevice once;
+    const cudaError_t e = once_per_device(once, [&] { return allow_shared(kernel, kStreamShared); });
     if (e != cudaSuccess) return e;
     launch_kernel(KIND == kDistillLoss ? kKDistillLoss : KIND == kDistillGrad ? kKDistillGrad : kKDistillStep, kernel,
                   dim3(stream_grid(a.rows)), dim3(kStreamBlock), smem, st, false, a, stages, mark_row);
@@ -1146,7 +1151,8 @@ cudaError_t distill_typed(const DistillArgs& a, cudaStream_t st) {
   const Cut c = cut_rows(a.logits, a.row_stride, a.rows, a.vocab, sizeof(T), NV, KIND == kDistillStep ? NV : 0);
   const uint32_t mark_bytes = (c.rounds * c.threads * kPerVec<T> / 8 + 15) & ~15u;  // a bit for every element of a block
   const size_t smem = mark_bytes + ((size_t)a.k + 15) * 16;
-  return launch_rows(KIND == kDistillLoss ? kKDistillLoss : KIND == kDistillGrad ? kKDistillGrad : kKDistillStep, k_distill<T, NV, KIND>, a.rows, c,
+  void (*const kernel)(DistillArgs, uint32_t, uint32_t) = c.few ? k_distill<T, kFewVecs, KIND> : k_distill<T, NV, KIND>;
+  return launch_rows(KIND == kDistillLoss ? kKDistillLoss : KIND == kDistillGrad ? kKDistillGrad : kKDistillStep, kernel, a.rows, c,
                      KIND != kDistillGrad, smem, st, a, c.log_blocks, mark_bytes);
 }
 // log2(e) / temperature, rounded once
@@ -1738,7 +1744,8 @@ cudaError_t top_typed(const TopArgs& a, cudaStream_t st) {
     const uint32_t stages = (uint32_t)((kStreamShared - beside) / (kStageVecs * 16));
     const size_t smem = (size_t)stages * kStageVecs * 16 + beside;
     void (*const kernel)(TopArgs, uint32_t) = k_top_stream<T>;
-    const cudaError_t e = allow_shared(kernel, smem);
+    static OncePerDevice once;
+    const cudaError_t e = once_per_device(once, [&] { return allow_shared(kernel, kStreamShared); });
     if (e != cudaSuccess) return e;
     launch_kernel(kKTopLogits, kernel, dim3(stream_grid(a.rows)), dim3(kStreamBlock), smem, st, false, a, stages);
     return cudaGetLastError();
@@ -1751,7 +1758,8 @@ cudaError_t top_typed(const TopArgs& a, cudaStream_t st) {
     c.threads += 32;
     c.rounds = (held + c.threads - 1) / c.threads;
   }
-  return launch_rows(kKTopLogits, k_top_logits<T, NV>, a.rows, c, true, 0, st, a, c.log_blocks);
+  void (*const kernel)(TopArgs, uint32_t) = c.few ? k_top_logits<T, kFewVecs> : k_top_logits<T, NV>;
+  return launch_rows(kKTopLogits, kernel, a.rows, c, true, 0, st, a, c.log_blocks);
 }
 
 }  // namespace
