@@ -221,6 +221,14 @@ __device__ __forceinline__ double exp_of(float x) {
   return __hiloint2double(__double2hiint(y) + ((int)n << 20), __double2loint(y));  // |n| < 870: the exponent stays a normal one's
 }
 
+// ln x to 2^-36: the fp32 logarithm, corrected by what its exponential leaves of x
+__device__ __forceinline__ double ln_of(double x) {
+  if (!(x > 1e-30 && x < 1e30)) return log(x);
+  const float y = logf((float)x);
+  const double r = fma(x, exp_of(-y), -1.0);
+  return (double)y + r * (1.0 - 0.5 * r);
+}
+
 // what p (z - a) has to gain to be p (z - b), a at most b; a = -inf: it is -inf already, or there is no mass
 __device__ __forceinline__ double moved(double mass, float a, float b) {
   return a == -CUDART_INF_F || a == b ? 0.0 : mass * ((double)a - (double)b);
@@ -274,23 +282,23 @@ __device__ double loss_of(const Sums& s, const Part* parts, uint32_t blocks, uin
     ent += parts[r].ent;
     cross += parts[r].cross + moved(parts[r].mass, parts[r].said.max, s.all.max);
   }
-  const double it = 1.0 / (double)temperature, ln_sum = log((double)s.all.sum);
+  const double it = 1.0 / (double)temperature, ln_sum = ln_of((double)s.all.sum);
   double loss = ent - cross * it + s.mass * ln_sum;
-  if (rest == CVLC_REST_SCALED) loss = s.mass > 0.0 ? loss / s.mass - log(s.mass) : s.mass;
-  if (s.left > 0.0) loss += s.left * (log(s.left) - (((double)s.rest.max - (double)s.all.max) * it + log((double)s.rest.sum) - ln_sum));
+  if (rest == CVLC_REST_SCALED) loss = s.mass > 0.0 ? loss / s.mass - ln_of(s.mass) : s.mass;
+  if (s.left > 0.0) loss += s.left * (ln_of(s.left) - (((double)s.rest.max - (double)s.all.max) * it + ln_of((double)s.rest.sum) - ln_sum));
   return loss;
 }
 
-// Records in shared memory come in fours of 16: the places of the row's words are padded with -2.
-__device__ __forceinline__ uint32_t padded(uint32_t k) { return (k + 15) & ~15u; }
-// What record i says of its word, where a word may have several: the sum over its records in their order, by the first of them; below 0
-// for the others.  ln_p: its logarithm.
-__device__ __forceinline__ double said_by(const int* at, const float* logp, uint32_t k, uint32_t i, double* ln_p) {
+// Records in shared memory: doubles first, then the places of the row's words, padded with -2 to whole sixteens.
+__device__ __host__ __forceinline__ uint32_t padded(uint32_t k) { return (k + 15) & ~15u; }
+__device__ __host__ __forceinline__ size_t records_bytes(uint32_t k) { return (size_t)padded(k) * (8 + 4 * 4); }
+// What record i says of its word, where a word may have several: the sum over its records (`alone`: what each says by itself) in their
+// order, by the first of them; below 0 for the others.  ln_p: its logarithm.
+__device__ __forceinline__ double said_by(const int* at, const double* alone, const float* logp, uint32_t k, uint32_t i, double* ln_p) {
   const int here = at[i];
-  double p = exp_of(logp[i]);
-  *ln_p = (double)logp[i];
-  bool merged = false;
-  for (uint32_t o = 0; o < k; o += 16) {
+  double p = alone[i];
+  bool merged = false, first = true;
+  for (uint32_t o = 0; o < k && first; o += 16) {
     const int4* const q = reinterpret_cast<const int4*>(at + o);
     uint32_t same = 0;
 #pragma unroll
@@ -300,13 +308,14 @@ __device__ __forceinline__ double said_by(const int* at, const float* logp, uint
               (v.w == here ? 8u : 0u) << (4 * j);
     }
     if (i >= o && i < o + 16) same &= ~(1u << (i - o));
-    if (!same) continue;
-    if (o + __ffs(same) - 1 < i) return -1.0;
-    for (; same; same &= same - 1) p += exp_of(logp[o + __ffs(same) - 1]);
-    merged = true;
+    for (; same; same &= same - 1) {
+      const uint32_t other = o + __ffs(same) - 1;
+      first &= other > i;
+      p += alone[other], merged = true;
+    }
   }
-  if (merged) *ln_p = log(p);
-  return p;
+  *ln_p = merged ? ln_of(p) : (double)logp[i];
+  return first ? p : -1.0;
 }
 
 // ---- a row's records, as a block sees them ----
@@ -317,10 +326,14 @@ struct Records {
   float* prob;    // their probabilities; below 0: counted with an earlier record of the word
   float* logit;   // the student's logits of their words
   float* said;    // the records' log-probabilities
+  double* alone;  // their exponentials
   double mass, ent;
 
   __device__ __forceinline__ Records(unsigned char* shared, uint32_t k)
-      : at(reinterpret_cast<int*>(shared)), prob(reinterpret_cast<float*>(at + padded(k))), logit(prob + k), said(logit + k), mass(0.0), ent(0.0) {}
+      : alone(reinterpret_cast<double*>(shared)), mass(0.0), ent(0.0) {
+    at = reinterpret_cast<int*>(alone + padded(k));
+    prob = reinterpret_cast<float*>(at + padded(k)), logit = prob + padded(k), said = logit + padded(k);
+  }
   // the first record of a thread, and its word's logit
   int id;
   float logp, z;
@@ -359,10 +372,14 @@ struct Records {
   // p of every word, summed in the order of its records; behind the barrier that follows mark()
   template <bool SUMS>
   __device__ __forceinline__ void teacher(const DistillArgs& a, bool twice) {
+    if (twice) {
+      for (uint32_t i = threadIdx.x; i < a.k; i += blockDim.x) alone[i] = exp_of(said[i]);
+      __syncthreads();
+    }
     for (uint32_t i = threadIdx.x; i < a.k; i += blockDim.x) {
       double p = -1.0, ln_p = 0.0;
       if (at[i] >= 0) {
-        if (twice) p = said_by(at, said, a.k, i, &ln_p);
+        if (twice) p = said_by(at, alone, said, a.k, i, &ln_p);
         else ln_p = (double)said[i], p = exp_of(said[i]);
         if (SUMS && !(p < 0.0)) {
           mass += p;
@@ -583,6 +600,7 @@ __global__ void __launch_bounds__(kRowThreads, 2) k_distill(DistillArgs a, uint3
 constexpr int kStreamWarps = 8, kSideWarps = 3;  // and one that copies
 constexpr int kStreamLanes = kStreamWarps * 32, kSideLanes = kSideWarps * 32;
 constexpr int kStreamBlock = kStreamLanes + kSideLanes + 32;
+constexpr int kRecordsAhead = 4;  // records of a side thread whose loads are on their way
 constexpr int kStageShare = 4;  // vectors of a thread in a stage: with two, waiting for it and giving it back were a third of the instructions
 constexpr int kStageVecs = kStageShare * kStreamLanes;  // 16 KB
 constexpr int kStagesMost = 8;
@@ -667,9 +685,11 @@ __device__ bool copy_rows(const DistillArgs& a, uint64_t rows, uint4* ring, uint
   uint64_t once;
   asm("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(once));
   uint32_t stage = 0, phase = 0;
-  bool ok = true;
+  bool ok = true, skip_next = skip(blockIdx.x);
   for (uint64_t row = blockIdx.x; row < rows; row += gridDim.x) {
-    if (skip(row)) continue;
+    const bool skipped = skip_next;
+    skip_next = skip(row + gridDim.x);  // known before it is needed
+    if (skipped) continue;
     const RowAt R = row_at<T>(a, row);
     for (int pass = 0; pass < PASSES; ++pass) {
       const uint32_t to_copy = pass == 0 ? R.wholes : copied_again(R.wholes, stages);
@@ -803,10 +823,11 @@ __global__ void __launch_bounds__(kStreamBlock, 2) k_distill_stream(DistillArgs 
   const float c2 = a.c2;
   uint4* const ring = reinterpret_cast<uint4*>(dyn);
   const auto marks_of = [&](uint32_t buf) { return dyn + stages * (kStageVecs * 16) + buf * mark_bytes; };
-  const auto places_of = [&](uint32_t buf) {  // of two rows: places, then what Records has
-    return reinterpret_cast<int*>(dyn + stages * (kStageVecs * 16) + 2 * mark_bytes) + buf * 4 * padded(a.k);
+  const auto records_of = [&](uint32_t buf) {  // of two rows, as in Records
+    return reinterpret_cast<double*>(dyn + stages * (kStageVecs * 16) + 2 * mark_bytes + buf * (uint32_t)records_bytes(a.k));
   };
-  const auto idle_row = [&](uint64_t row) { return a.row_weight && a.row_weight[row] == 0.f && !(KIND == kDistillLoss && a.stats); };
+  const auto weight_of = [&](uint64_t row) { return !a.row_weight ? 1.f : row < a.rows ? a.row_weight[row] : 0.f; };
+  const bool all_rows = KIND == kDistillLoss && a.stats;  // a later gradient may ask for rows that count for nothing
 
   if (thread == 0) {
     for (uint32_t i = 0; i < stages; ++i) bar_init(&full[i], 1), bar_init(&empty[i], kStreamWarps);
@@ -817,7 +838,7 @@ __global__ void __launch_bounds__(kStreamBlock, 2) k_distill_stream(DistillArgs 
 
   bool ok = true;
   if (thread >= kSideLanes && thread < kStreamFirst) {
-    if (lane == 0 && !copy_rows<T, KIND == kDistillStep ? 2 : 1>(a, a.rows, ring, stages, full, empty, idle_row) && a.status)
+    if (lane == 0 && !copy_rows<T, KIND == kDistillStep ? 2 : 1>(a, a.rows, ring, stages, full, empty, [&](uint64_t row) { return !all_rows && weight_of(row) == 0.f; }) && a.status)
       set_status(a.status, CVLC_ERR_DEVICE_TIMEOUT);
     return;
   }
@@ -826,39 +847,76 @@ __global__ void __launch_bounds__(kStreamBlock, 2) k_distill_stream(DistillArgs 
     // ---- the side warps: records, ragged ends, losses ----
     const uint32_t t = thread, side = t >> 5;
     const auto end_of = [&](const RowAt& R) { return side == 0 ? end_word<E>(R, a.vocab, lane) : -1; };
-    const auto prepare = [&](uint64_t row, uint32_t buf) {
+    // A row's records begin with loads that depend on each other: the first record of a thread is fetched while an earlier row is worked on,
+    // and its word's logit after it.
+    struct First {
+      int id, end;
+      float logp, z, end_z;
+    };
+    const auto fetch = [&](uint64_t row, First& f) {
+      f.id = -1, f.logp = 0.f;
+      if (row < a.rows && t < a.k) f.id = a.ids[row * a.k + t], f.logp = a.logp[row * a.k + t];
+    };
+    const auto fetch_logits = [&](uint64_t row, First& f) {
+      if (row >= a.rows) return;
+      const RowAt R = row_at<T>(a, row);
+      const T* const z = reinterpret_cast<const T*>(R.from) + R.lead;
+      f.end = end_of(R);
+      f.end_z = f.end >= 0 ? to_float(z[f.end]) : -CUDART_INF_F;
+      f.z = f.id >= 0 && (uint32_t)f.id < a.vocab ? to_float(z[f.id]) : 0.f;
+    };
+    const auto prepare = [&](uint64_t row, uint32_t buf, const First& first) {
       some_sync<kSideLanes>(kBarSide);  // the row before the last one is finished, its marks cleared
       const RowAt R = row_at<T>(a, row);
       const T* const z = reinterpret_cast<const T*>(R.from) + R.lead;
       uint8_t* const marks = marks_of(buf);
-      int* const at = places_of(buf);
+      double* const alone = records_of(buf);
+      int* const at = reinterpret_cast<int*>(alone + padded(a.k));
       float* const prob = reinterpret_cast<float*>(at + padded(a.k));
-      float* const logit = prob + a.k;
-      float* const said = logit + a.k;
+      float* const logit = prob + padded(a.k);
+      float* const said = logit + padded(a.k);
       bool twice = false;
-      const int end = end_of(R);
-      const float end_z = end >= 0 ? to_float(z[end]) : -CUDART_INF_F;
-      for (uint32_t i = t; i < a.k; i += kSideLanes) {
-        const int id = a.ids[row * a.k + i];
-        said[i] = a.logp[row * a.k + i];
-        int p = -1;
-        if (id >= 0 && (uint32_t)id >= a.vocab) {
-          if (a.status) set_status(a.status, CVLC_ERR_INVALID_ARG);
-        } else if (id >= 0) {
-          p = id + (int)R.lead;
-          logit[i] = to_float(z[id]);
-          const uint32_t bit = 1u << (p & 31);
-          twice |= (atomicOr(reinterpret_cast<uint32_t*>(marks) + (p >> 5), bit) & bit) != 0;
+      const int end = first.end;
+      const float end_z = first.end_z;
+      for (uint32_t base = t; base < a.k; base += kRecordsAhead * kSideLanes) {  // a few records of a thread at once: their loads are far
+        int ids[kRecordsAhead];
+        float lps[kRecordsAhead], zs[kRecordsAhead];
+#pragma unroll
+        for (int j = 0; j < kRecordsAhead; ++j) {
+          const uint32_t i = base + j * kSideLanes;
+          const bool fetched = i == t;
+          ids[j] = fetched ? first.id : i < a.k ? a.ids[row * a.k + i] : -1;
+          lps[j] = fetched ? first.logp : i < a.k ? a.logp[row * a.k + i] : 0.f;
         }
-        at[i] = p;
+#pragma unroll
+        for (int j = 0; j < kRecordsAhead; ++j)
+          zs[j] = base + j * kSideLanes == t ? first.z : ids[j] >= 0 && (uint32_t)ids[j] < a.vocab ? to_float(z[ids[j]]) : 0.f;
+#pragma unroll
+        for (int j = 0; j < kRecordsAhead; ++j) {
+          const uint32_t i = base + j * kSideLanes;
+          if (i >= a.k) break;
+          int p = -1;
+          if (ids[j] >= 0 && (uint32_t)ids[j] >= a.vocab) {
+            if (a.status) set_status(a.status, CVLC_ERR_INVALID_ARG);
+          } else if (ids[j] >= 0) {
+            p = ids[j] + (int)R.lead;
+            const uint32_t bit = 1u << (p & 31);
+            twice |= (atomicOr(reinterpret_cast<uint32_t*>(marks) + (p >> 5), bit) & bit) != 0;
+          }
+          at[i] = p, said[i] = lps[j], logit[i] = zs[j];
+        }
       }
       if (t < padded(a.k) - a.k) at[a.k + t] = -2;
       twice = some_or<kSideLanes>(kBarSide, twice);
       Part mine = {{-CUDART_INF_F, 0.f}, {-CUDART_INF_F, 0.f}, 0.0, 0.0, 0.0};
+      if (twice) {
+        for (uint32_t i = t; i < a.k; i += kSideLanes) alone[i] = exp_of(said[i]);
+        some_sync<kSideLanes>(kBarSide);
+      }
       for (uint32_t i = t; i < a.k; i += kSideLanes) {
         double p = -1.0, ln_p = 0.0;
         if (at[i] >= 0) {
-          if (twice) p = said_by(at, said, a.k, i, &ln_p);
+          if (twice) p = said_by(at, alone, said, a.k, i, &ln_p);
           else ln_p = (double)said[i], p = exp_of(said[i]);
           if (KIND != kDistillGrad && !(p < 0.0)) {
             mine.mass += p;
@@ -908,9 +966,9 @@ __global__ void __launch_bounds__(kStreamBlock, 2) k_distill_stream(DistillArgs 
       const RowAt R = row_at<T>(a, row);
       const float weight = a.row_weight ? a.row_weight[row] : 1.f;
       uint8_t* const marks = marks_of(buf);
-      int* const at = places_of(buf);
+      int* const at = reinterpret_cast<int*>(records_of(buf) + padded(a.k));
       float* const prob = reinterpret_cast<float*>(at + padded(a.k));
-      float* const logit = prob + a.k;
+      float* const logit = prob + padded(a.k);
       Whole w;
       if (KIND == kDistillGrad) {
         w = *reinterpret_cast<const Whole*>(a.stats + row * CVLC_DISTILL_STATS);
@@ -922,12 +980,12 @@ __global__ void __launch_bounds__(kStreamBlock, 2) k_distill_stream(DistillArgs 
         if (t == 0) {
           double loss = 0.0;
           if (!(all.max == -CUDART_INF_F && all.sum == 0.f)) {
-            const double it = 1.0 / (double)a.temperature, ln_sum = log((double)all.sum);
+            const double it = 1.0 / (double)a.temperature, ln_sum = ln_of((double)all.sum);
             loss = s.ent - (s.cross + moved(s.mass, s.said.max, all.max)) * it + s.mass * ln_sum;
-            if (a.rest == CVLC_REST_SCALED) loss = s.mass > 0.0 ? loss / s.mass - log(s.mass) : s.mass;
+            if (a.rest == CVLC_REST_SCALED) loss = s.mass > 0.0 ? loss / s.mass - ln_of(s.mass) : s.mass;
             if (left > 0.f) {
               const double l = 1.0 - s.mass;
-              loss += l * (log(l) - (((double)rest.max - (double)all.max) * it + log((double)rest.sum) - ln_sum));
+              loss += l * (ln_of(l) - (((double)rest.max - (double)all.max) * it + ln_of((double)rest.sum) - ln_sum));
             }
           }
           a.loss[row] = weight == 0.f ? 0.f : (float)((double)weight * loss);
@@ -952,16 +1010,24 @@ __global__ void __launch_bounds__(kStreamBlock, 2) k_distill_stream(DistillArgs 
       for (uint32_t i = t; i < a.k; i += kSideLanes)
         if (at[i] >= 0) reinterpret_cast<uint32_t*>(marks)[at[i] >> 5] = 0;
     };
-    uint64_t before = ~0ull;
-    uint32_t buf = 0;
-    for (uint64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
-      if (idle_row(row)) {
+    // the next row that counts, whose loss is 0 where it does not
+    const auto counting = [&](uint64_t row) {
+      for (; row < a.rows && !all_rows && weight_of(row) == 0.f; row += gridDim.x)
         if (KIND != kDistillGrad && t == 0) a.loss[row] = 0.f;
-        continue;
-      }
-      prepare(row, buf);
+      return row;
+    };
+    uint64_t before = ~0ull, row = counting(blockIdx.x);
+    uint32_t buf = 0;
+    First first, next;
+    fetch(row, first);
+    fetch_logits(row, first);
+    while (row < a.rows) {
+      const uint64_t after = counting(row + gridDim.x);
+      fetch(after, next);
+      prepare(row, buf, first);
+      fetch_logits(after, next);
       if (before != ~0ull) finish(before, buf ^ 1);
-      before = row;
+      before = row, row = after, first = next;
       buf ^= 1;
     }
     if (before != ~0ull) finish(before, buf ^ 1);
@@ -971,10 +1037,13 @@ __global__ void __launch_bounds__(kStreamBlock, 2) k_distill_stream(DistillArgs 
   // ---- the pass over the elements ----
   const uint32_t tid = thread - kStreamFirst;
   uint32_t stage = 0, phase = 0, buf = 0;
+  float next_weight = weight_of(blockIdx.x);
   for (uint64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+    const float weight = next_weight;
+    next_weight = weight_of(row + gridDim.x);
     const RowAt R = row_at<T>(a, row);
     T* const g = static_cast<T*>(a.grad) + row * a.grad_stride;
-    if (idle_row(row)) {
+    if (!all_rows && weight == 0.f) {
       if (KIND != kDistillLoss) zero_row<T>(g, a.vocab, tid, kStreamLanes);
       continue;
     }
@@ -1021,7 +1090,7 @@ __global__ void __launch_bounds__(kStreamBlock, 2) k_distill_stream(DistillArgs 
     } else {
       w = *reinterpret_cast<const Whole*>(a.stats + row * CVLC_DISTILL_STATS);
     }
-    const float ca = w.a * ((a.row_weight ? a.row_weight[row] : 1.f) / a.temperature);
+    const float ca = w.a * (weight / a.temperature);
     unsigned char* const to = reinterpret_cast<unsigned char*>(g) + (int)(R.whole_from * 16) - (int)(R.lead * sizeof(T));  // of the first whole vector
     const bool alike = (reinterpret_cast<uintptr_t>(to) & 15) == 0;
     const uint32_t cuts = (R.wholes + kStageVecs - 1) / kStageVecs, kept = cuts - again / kStageVecs;
@@ -1134,7 +1203,7 @@ template <class T, DistillKind KIND>
 cudaError_t distill_typed(const DistillArgs& a, cudaStream_t st) {
   // many long rows: two blocks an SM go from row to row, where two rows' marks and three stages fit
   const uint32_t mark_row = (a.vocab / kPerVec<T> + 2 + kStageVecs) * kPerVec<T> / 128 * 16 + 16;  // the row's, and a stage's behind it
-  const size_t beside = 2 * ((size_t)mark_row + ((size_t)a.k + 15) / 16 * 16 * 16);
+  const size_t beside = 2 * ((size_t)mark_row + records_bytes(a.k));
   if (streamed(a.rows, (uint64_t)a.vocab * sizeof(T)) && beside + 3 * kStageVecs * 16 <= kStreamShared) {
     const uint32_t fit = (uint32_t)((kStreamShared - beside) / (kStageVecs * 16));
     const uint32_t stages = fit < kStagesMost ? fit : kStagesMost;
@@ -1150,7 +1219,7 @@ cudaError_t distill_typed(const DistillArgs& a, cudaStream_t st) {
   constexpr int NV = KIND == kDistillStep ? 8 : 4;
   const Cut c = cut_rows(a.logits, a.row_stride, a.rows, a.vocab, sizeof(T), NV, KIND == kDistillStep ? NV : 0);
   const uint32_t mark_bytes = (c.rounds * c.threads * kPerVec<T> / 8 + 15) & ~15u;  // a bit for every element of a block
-  const size_t smem = mark_bytes + ((size_t)a.k + 15) * 16;
+  const size_t smem = mark_bytes + records_bytes(a.k);
   void (*const kernel)(DistillArgs, uint32_t, uint32_t) = c.few ? k_distill<T, kFewVecs, KIND> : k_distill<T, NV, KIND>;
   return launch_rows(KIND == kDistillLoss ? kKDistillLoss : KIND == kDistillGrad ? kKDistillGrad : kKDistillStep, kernel, a.rows, c,
                      KIND != kDistillGrad, smem, st, a, c.log_blocks, mark_bytes);
