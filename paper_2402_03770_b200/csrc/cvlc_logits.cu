@@ -597,9 +597,10 @@ __global__ void __launch_bounds__(kRowThreads, 2) k_distill(DistillArgs a, uint3
 // every row twice, at first over what the ring still holds of it, then over what it has to copy once more, most of which is in the L2 cache
 // (the 296 rows on their way are 76 MB at 131,072 words of 16 bits).  Keeping the row in the cluster's registers instead costs every block of the cluster all of the above:
 // 4096 x 131072 bf16 750 us.
-constexpr int kStreamWarps = 8, kSideWarps = 3;  // and one that copies
+constexpr int kStreamWarps = 8, kSideWarps = 4;  // and one that copies
 constexpr int kStreamLanes = kStreamWarps * 32, kSideLanes = kSideWarps * 32;
 constexpr int kStreamBlock = kStreamLanes + kSideLanes + 32;
+constexpr int kPrepWarps = kSideWarps - 1, kPrepLanes = kPrepWarps * 32;  // distillation: the side warp that is left has the losses
 constexpr int kRecordsAhead = 4;  // records of a side thread whose loads are on their way
 constexpr int kStageShare = 4;  // vectors of a thread in a stage: with two, waiting for it and giving it back were a third of the instructions
 constexpr int kStageVecs = kStageShare * kStreamLanes;  // 16 KB
@@ -671,7 +672,7 @@ __device__ __forceinline__ uint32_t some_count(int id, bool v) {
   asm volatile("{.reg .pred p;\n setp.ne.u32 p, %1, 0;\n bar.red.popc.u32 %0, %2, %3, p;}" : "=r"(r) : "r"((uint32_t)v), "r"(id), "n"(N) : "memory");
   return r;
 }
-enum { kBarSide = 1, kBarStream = 2, kBarReady = 3, kBarDone = 5 };  // the last two: one for each of two rows
+enum { kBarSide = 1, kBarStream = 2, kBarReady = 3, kBarDone = 5, kBarLoss = 7 };  // from kBarReady on: one for each of two rows
 
 // of a row's whole vectors, those that the ring no longer holds when it has passed
 __device__ __forceinline__ uint32_t copied_again(uint32_t wholes, uint32_t stages) {
@@ -817,7 +818,7 @@ __global__ void __launch_bounds__(kStreamBlock, 2) k_distill_stream(DistillArgs 
   extern __shared__ __align__(128) unsigned char dyn[];
   __shared__ uint64_t full[kStagesMost], empty[kStagesMost];
   __shared__ RowSide sides[2];
-  __shared__ Part of_side[kSideWarps];
+  __shared__ Part of_side[kPrepWarps];
   constexpr int E = kPerVec<T>;
   const uint32_t thread = threadIdx.x, lane = thread & 31;
   const float c2 = a.c2;
@@ -865,8 +866,8 @@ __global__ void __launch_bounds__(kStreamBlock, 2) k_distill_stream(DistillArgs 
       f.end_z = f.end >= 0 ? to_float(z[f.end]) : -CUDART_INF_F;
       f.z = f.id >= 0 && (uint32_t)f.id < a.vocab ? to_float(z[f.id]) : 0.f;
     };
-    const auto prepare = [&](uint64_t row, uint32_t buf, const First& first) {
-      some_sync<kSideLanes>(kBarSide);  // the row before the last one is finished, its marks cleared
+    const auto prepare = [&](uint64_t row, uint32_t buf, const First& first, bool again) {
+      some_sync<kPrepLanes>(kBarSide);  // the row before the last one is finished, its marks cleared
       const RowAt R = row_at<T>(a, row);
       const T* const z = reinterpret_cast<const T*>(R.from) + R.lead;
       uint8_t* const marks = marks_of(buf);
@@ -878,22 +879,22 @@ __global__ void __launch_bounds__(kStreamBlock, 2) k_distill_stream(DistillArgs 
       bool twice = false;
       const int end = first.end;
       const float end_z = first.end_z;
-      for (uint32_t base = t; base < a.k; base += kRecordsAhead * kSideLanes) {  // a few records of a thread at once: their loads are far
+      for (uint32_t base = t; base < a.k; base += kRecordsAhead * kPrepLanes) {  // a few records of a thread at once: their loads are far
         int ids[kRecordsAhead];
         float lps[kRecordsAhead], zs[kRecordsAhead];
 #pragma unroll
         for (int j = 0; j < kRecordsAhead; ++j) {
-          const uint32_t i = base + j * kSideLanes;
+          const uint32_t i = base + j * kPrepLanes;
           const bool fetched = i == t;
           ids[j] = fetched ? first.id : i < a.k ? a.ids[row * a.k + i] : -1;
           lps[j] = fetched ? first.logp : i < a.k ? a.logp[row * a.k + i] : 0.f;
         }
 #pragma unroll
         for (int j = 0; j < kRecordsAhead; ++j)
-          zs[j] = base + j * kSideLanes == t ? first.z : ids[j] >= 0 && (uint32_t)ids[j] < a.vocab ? to_float(z[ids[j]]) : 0.f;
+          zs[j] = base + j * kPrepLanes == t ? first.z : ids[j] >= 0 && (uint32_t)ids[j] < a.vocab ? to_float(z[ids[j]]) : 0.f;
 #pragma unroll
         for (int j = 0; j < kRecordsAhead; ++j) {
-          const uint32_t i = base + j * kSideLanes;
+          const uint32_t i = base + j * kPrepLanes;
           if (i >= a.k) break;
           int p = -1;
           if (ids[j] >= 0 && (uint32_t)ids[j] >= a.vocab) {
@@ -907,13 +908,13 @@ __global__ void __launch_bounds__(kStreamBlock, 2) k_distill_stream(DistillArgs 
         }
       }
       if (t < padded(a.k) - a.k) at[a.k + t] = -2;
-      twice = some_or<kSideLanes>(kBarSide, twice);
+      twice = some_or<kPrepLanes>(kBarSide, twice);
       Part mine = {{-CUDART_INF_F, 0.f}, {-CUDART_INF_F, 0.f}, 0.0, 0.0, 0.0};
       if (twice) {
-        for (uint32_t i = t; i < a.k; i += kSideLanes) alone[i] = exp_of(said[i]);
-        some_sync<kSideLanes>(kBarSide);
+        for (uint32_t i = t; i < a.k; i += kPrepLanes) alone[i] = exp_of(said[i]);
+        some_sync<kPrepLanes>(kBarSide);
       }
-      for (uint32_t i = t; i < a.k; i += kSideLanes) {
+      for (uint32_t i = t; i < a.k; i += kPrepLanes) {
         double p = -1.0, ln_p = 0.0;
         if (at[i] >= 0) {
           if (twice) p = said_by(at, alone, said, a.k, i, &ln_p);
@@ -930,7 +931,7 @@ __global__ void __launch_bounds__(kStreamBlock, 2) k_distill_stream(DistillArgs 
 #pragma unroll
         for (int o = 16; o; o >>= 1) mine.said.max = fmaxf(mine.said.max, __shfl_xor_sync(kFull, mine.said.max, o));
         const float ref = finite_ref(mine.said.max);
-        for (uint32_t i = t; i < a.k; i += kSideLanes)
+        for (uint32_t i = t; i < a.k; i += kPrepLanes)
           if (at[i] >= 0 && !(prob[i] < 0.f)) {
             mine.said.sum += exp2_fast((logit[i] - ref) * c2);
             if (prob[i] != 0.f) mine.cross += (double)prob[i] * ((double)logit[i] - (double)ref);
@@ -942,10 +943,11 @@ __global__ void __launch_bounds__(kStreamBlock, 2) k_distill_stream(DistillArgs 
           mine.rest = warp_join(MaxSum{e, e == -CUDART_INF_F ? 0.f : e == e ? 1.f : e}, c2);
         }
         if (lane == 0) of_side[side] = mine;
-        some_sync<kSideLanes>(kBarSide);
+        if (again) some_sync<kSideLanes>(kBarLoss + buf);  // the loss of the row before the last one is done
+        some_sync<kPrepLanes>(kBarSide);
         if (t == 0) {
           Part p = of_side[0];
-          for (int w = 1; w < kSideWarps; ++w) add_said(p, of_side[w], c2);
+          for (int w = 1; w < kPrepWarps; ++w) add_said(p, of_side[w], c2);
           RowSide& s = sides[buf];
           s.said = p.said, s.ends = p.rest;
           s.mass = p.mass, s.ent = p.ent, s.cross = p.cross;
@@ -959,7 +961,7 @@ __global__ void __launch_bounds__(kStreamBlock, 2) k_distill_stream(DistillArgs 
         }
       }
       __threadfence_block();
-      some_arrive<kStreamLanes + kSideLanes>(kBarReady + buf);
+      some_arrive<kStreamLanes + kPrepLanes>(kBarReady + buf);
     };
     const auto finish = [&](uint64_t row, uint32_t buf) {
       some_sync<kStreamLanes + kSideLanes>(kBarDone + buf);
@@ -973,11 +975,51 @@ __global__ void __launch_bounds__(kStreamBlock, 2) k_distill_stream(DistillArgs 
       if (KIND == kDistillGrad) {
         w = *reinterpret_cast<const Whole*>(a.stats + row * CVLC_DISTILL_STATS);
       } else {
-        RowSide& s = sides[buf];
         MaxSum rest, all;
         float left;
-        w = whole_of(s, c2, &rest, &all, &left);
-        if (t == 0) {
+        if (KIND == kDistillStep) w = whole_of(sides[buf], c2, &rest, &all, &left);
+      }
+      T* const g = static_cast<T*>(a.grad) + row * a.grad_stride;
+      const float scale = weight / a.temperature;
+      if (KIND != kDistillLoss) {
+        const int end = end_of(R);
+        if (end >= 0 && !(marks[(end + R.lead) >> 3] >> ((end + R.lead) & 7) & 1)) {
+          const float z = to_float((reinterpret_cast<const T*>(R.from) + R.lead)[end]);
+          g[end] = from_float<T>(w.a * scale * exp2_fast((z - w.ref) * c2));
+        }
+        for (uint32_t i = t; i < a.k; i += kPrepLanes)
+          if (at[i] >= 0 && !(prob[i] < 0.f)) {
+            const float q = exp2_fast((logit[i] - w.max) * c2) * w.inv_sum;
+            g[at[i] - (int)R.lead] = from_float<T>(w.b * scale * q - w.c * scale * prob[i]);
+          }
+        some_sync<kPrepLanes>(kBarSide);  // the ends' marks have been read
+      }
+      for (uint32_t i = t; i < a.k; i += kPrepLanes)
+        if (at[i] >= 0) reinterpret_cast<uint32_t*>(marks)[at[i] >> 5] = 0;
+    };
+    // the next row that counts, whose loss is 0 where it does not
+    const auto counting = [&](uint64_t row) {
+      for (; row < a.rows && !all_rows && weight_of(row) == 0.f; row += gridDim.x)
+        if (KIND != kDistillGrad && t == 0) a.loss[row] = 0.f;
+      return row;
+    };
+    if (side == kPrepWarps) {
+      // ---- the losses: their logarithms in 64 bits take a lane as long as the records take the others ----
+      if (KIND == kDistillGrad) {  // (it has none, but the barriers count it)
+        uint32_t buf = 0;
+        for (uint64_t row = counting(blockIdx.x); row < a.rows; row = counting(row + gridDim.x), buf ^= 1)
+          some_sync<kStreamLanes + kSideLanes>(kBarDone + buf);
+        return;
+      }
+      uint32_t buf = 0;
+      for (uint64_t row = counting(blockIdx.x); row < a.rows; row = counting(row + gridDim.x), buf ^= 1) {
+        const float weight = weight_of(row);
+        some_sync<kStreamLanes + kSideLanes>(kBarDone + buf);
+        const RowSide& s = sides[buf];
+        MaxSum rest, all;
+        float left;
+        const Whole w = whole_of(s, c2, &rest, &all, &left);
+        if (lane == 0) {
           double loss = 0.0;
           if (!(all.max == -CUDART_INF_F && all.sum == 0.f)) {
             const double it = 1.0 / (double)a.temperature, ln_sum = ln_of((double)all.sum);
@@ -991,46 +1033,29 @@ __global__ void __launch_bounds__(kStreamBlock, 2) k_distill_stream(DistillArgs 
           a.loss[row] = weight == 0.f ? 0.f : (float)((double)weight * loss);
           if (KIND == kDistillLoss && a.stats) *reinterpret_cast<Whole*>(a.stats + row * CVLC_DISTILL_STATS) = w;
         }
+        __syncwarp();
+        some_arrive<kSideLanes>(kBarLoss + buf);  // the row's sums have been read
       }
-      T* const g = static_cast<T*>(a.grad) + row * a.grad_stride;
-      const float scale = weight / a.temperature;
-      if (KIND != kDistillLoss) {
-        const int end = end_of(R);
-        if (end >= 0 && !(marks[(end + R.lead) >> 3] >> ((end + R.lead) & 7) & 1)) {
-          const float z = to_float((reinterpret_cast<const T*>(R.from) + R.lead)[end]);
-          g[end] = from_float<T>(w.a * scale * exp2_fast((z - w.ref) * c2));
-        }
-        for (uint32_t i = t; i < a.k; i += kSideLanes)
-          if (at[i] >= 0 && !(prob[i] < 0.f)) {
-            const float q = exp2_fast((logit[i] - w.max) * c2) * w.inv_sum;
-            g[at[i] - (int)R.lead] = from_float<T>(w.b * scale * q - w.c * scale * prob[i]);
-          }
-        some_sync<kSideLanes>(kBarSide);  // the ends' marks have been read
-      }
-      for (uint32_t i = t; i < a.k; i += kSideLanes)
-        if (at[i] >= 0) reinterpret_cast<uint32_t*>(marks)[at[i] >> 5] = 0;
-    };
-    // the next row that counts, whose loss is 0 where it does not
-    const auto counting = [&](uint64_t row) {
-      for (; row < a.rows && !all_rows && weight_of(row) == 0.f; row += gridDim.x)
-        if (KIND != kDistillGrad && t == 0) a.loss[row] = 0.f;
-      return row;
-    };
+      return;
+    }
     uint64_t before = ~0ull, row = counting(blockIdx.x);
-    uint32_t buf = 0;
+    uint32_t buf = 0, prepared = 0;
     First first, next;
     fetch(row, first);
     fetch_logits(row, first);
     while (row < a.rows) {
       const uint64_t after = counting(row + gridDim.x);
       fetch(after, next);
-      prepare(row, buf, first);
+      prepare(row, buf, first, prepared >= 2);
+      ++prepared;
       fetch_logits(after, next);
       if (before != ~0ull) finish(before, buf ^ 1);
       before = row, row = after, first = next;
       buf ^= 1;
     }
     if (before != ~0ull) finish(before, buf ^ 1);
+    if (KIND != kDistillGrad)
+      for (uint32_t i = 0; i < min(prepared, 2u); ++i) some_sync<kSideLanes>(kBarLoss + ((prepared - 1 - i) & 1));  // no barrier is left half full
     return;
   }
 
@@ -1047,7 +1072,7 @@ __global__ void __launch_bounds__(kStreamBlock, 2) k_distill_stream(DistillArgs 
       if (KIND != kDistillLoss) zero_row<T>(g, a.vocab, tid, kStreamLanes);
       continue;
     }
-    some_sync<kStreamLanes + kSideLanes>(kBarReady + buf);
+    some_sync<kStreamLanes + kPrepLanes>(kBarReady + buf);
     const unsigned char* const marks = marks_of(buf);
     const uint32_t again = copied_again(R.wholes, stages);  // from here on the ring still holds the row for the second pass
     Whole w = {};
@@ -1195,8 +1220,10 @@ cudaError_t launch_rows(int id, void (*kernel)(Params...), uint64_t rows, const 
   return e != cudaSuccess ? e : last;
 }
 
-// where blocks go from row to row: rows enough for all SMs, and long enough for a few stages each
-bool streamed(uint64_t rows, uint64_t bytes) { return rows >= kNumSM && bytes >= 2 * kStageVecs * 16; }
+// Where blocks go from row to row: rows of a few stages each, and so many that a cluster for each of fewer would be slower.  Both sides, us
+// (rows of one kernel / of the other): step of 131,072 words bf16, 64 rows 23 / 17, 100 rows 25 / 31, 333 rows 50 / 74; of 32,000 words, 64 rows
+// 11 / 9, 100 rows 12 / 15, 1000 rows 43 / 53; of 9000 words, 1000 rows 28 / 22, 4000 rows 98 / 62.
+bool streamed(uint64_t rows, uint64_t bytes) { return bytes >= 2 * kStageVecs * 16 && (rows >= kNumSM || (rows >= 80 && bytes >= 3 * kStageVecs * 16)); }
 unsigned stream_grid(uint64_t rows) { return (unsigned)(rows < 2 * kNumSM ? rows : 2 * kNumSM); }
 
 template <class T, DistillKind KIND>
