@@ -17,7 +17,7 @@
  *    and only enqueues kernels on `cuda_stream` (a cudaStream_t passed as void*;
  *    NULL = the legacy default stream).
  *  - State the library keeps in the process, all of it outside the data path: per-device
- *    flags saying that kernel attributes have been set; two CUDA events per device used by
+ *    flags saying that kernel attributes have been set, and how many clusters of the token sort run at once; two CUDA events per device used by
  *    cvlc_compress_batch to order its two streams; the launch counters and, while
  *    cvlc_profile_select is active, the profiling events; the built-in scratch of
  *    cvlc_decode_aggregate_noalloc and its cached device address.  cvlc_set_device changes
@@ -433,7 +433,7 @@ int cvlc_decode_apply(const uint8_t* const* streams_dev, const uint64_t* stream_
  *  logits_dev   rows x vocab of `dtype`, rows row_stride elements apart
  *  ids_dev, logp_dev   rows x k, contiguous
  * Errors: INVALID_ARG (a type, k above vocab or CVLC_MAX_TOP, vocab above CVLC_MAX_VOCAB, rows above 2^27, a stride below
- * vocab, a temperature that is not positive and finite, a pointer that is not aligned to its type).  rows = 0 does nothing.
+ * vocab, a temperature outside 1e-6 .. 1e6, a pointer that is not aligned to its type).  rows = 0 does nothing.
  */
 int cvlc_top_logits(const void* logits_dev, uint32_t dtype, uint64_t rows, uint32_t vocab, uint64_t row_stride,
                     uint32_t k, float temperature, int32_t* ids_dev, float* logp_dev, void* cuda_stream);

@@ -157,7 +157,7 @@ size_t element_bytes(uint32_t dtype) { return dtype == CVLC_F32 ? 4 : dtype == C
 bool logits_ok(const void* at, uint32_t dtype, uint64_t rows, uint32_t vocab, uint64_t stride, float temperature) {
   const size_t size = element_bytes(dtype);
   return size && (rows == 0 || aligned(at, size)) && rows <= (1ull << 27) && vocab >= 1 && vocab <= CVLC_MAX_VOCAB && stride >= vocab &&
-         stride <= (1ull << 32) && temperature > 0.f && temperature < INFINITY;
+         stride <= (1ull << 32) && temperature >= 1e-6f && temperature <= 1e6f;
 }
 
 int distill_args(const cvlc_distill* a, DistillArgs* d) {

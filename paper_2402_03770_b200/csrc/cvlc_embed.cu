@@ -134,32 +134,35 @@ uint32_t chunk_of(uint64_t n) {
   return (uint32_t)c;
 }
 
-// What the sort's launch does besides, where the table is written out: zeros for the rows of words that do not occur.  A block has a range of
-// rows; it looks through all tokens for those that occur, unless they are so many that writing zeros to all rows is less.
+// What the sort's launch does besides, where the table is written out: zeros for the rows of words that do not occur.  The blocks have the
+// rows in turn (the words that occur are often the first ones); a block looks through all tokens for those of its rows, unless they are so
+// many that writing zeros to all rows is less.
 constexpr uint64_t kMarkedTokens = 1u << 18;
 __device__ __forceinline__ void zero_absent(const EmbedGradArgs& a, uint32_t block, uint32_t blocks, uint32_t* marks, uint32_t mark_words) {
-  const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const uint64_t per = (a.vocab + blocks - 1) / blocks, begin = block * per, end = begin + per < a.vocab ? begin + per : a.vocab;
-  if (begin >= end) return;
-  const bool marked = a.n <= kMarkedTokens && end - begin <= (uint64_t)mark_words * 32;
+  const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, vocab = (uint32_t)a.vocab;
+  if (block >= vocab) return;
+  const uint32_t rows = (vocab - 1 - block) / blocks + 1;  // row i of the block: block + i * blocks
+  const bool marked = a.n <= kMarkedTokens && rows <= mark_words * 32;
   if (marked) {
-    for (uint32_t i = tid; i < (uint32_t)(end - begin + 31) / 32; i += blockDim.x) marks[i] = 0;
+    for (uint32_t i = tid; i < (rows + 31) / 32; i += blockDim.x) marks[i] = 0;
     __syncthreads();
     for (uint64_t i = tid; i < a.n; i += 8 * kTokenThreads) {
       int64_t t[8];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) t[j] = i + j * kTokenThreads < a.n ? token_at(a.tokens, a.token_bytes, i + j * kTokenThreads) - (int64_t)begin : -1;
+      for (int j = 0; j < 8; ++j) t[j] = i + j * kTokenThreads < a.n ? token_at(a.tokens, a.token_bytes, i + j * kTokenThreads) : -1;
 #pragma unroll
-      for (int j = 0; j < 8; ++j)
-        if (t[j] >= 0 && t[j] < (int64_t)(end - begin)) atomicOr(&marks[t[j] >> 5], 1u << (t[j] & 31));
+      for (int j = 0; j < 8; ++j) {
+        if (t[j] < 0 || t[j] >= (int64_t)vocab) continue;
+        const uint32_t row = (uint32_t)t[j] / blocks;
+        if ((uint32_t)t[j] - row * blocks == block) atomicOr(&marks[row >> 5], 1u << (row & 31));
+      }
     }
     __syncthreads();
   }
   const bool vec = a.dim % 4 == 0 && a.update_stride % 4 == 0 && (reinterpret_cast<uintptr_t>(a.update) & 15) == 0;
-  for (uint64_t row = begin + warp; row < end; row += blockDim.x / 32) {
-    const uint32_t r = (uint32_t)(row - begin);
+  for (uint32_t r = warp; r < rows; r += kTokenWarps) {
     if (marked && (marks[r >> 5] >> (r & 31) & 1)) continue;
-    float* const u = a.update + row * a.update_stride;
+    float* const u = a.update + ((uint64_t)r * blocks + block) * a.update_stride;
     if (vec) {
       for (uint32_t c = lane; c < a.dim / 4; c += 32) __stcs(reinterpret_cast<float4*>(u) + c, make_float4(0.f, 0.f, 0.f, 0.f));
     } else {
@@ -399,7 +402,7 @@ struct Sorted {
 };
 
 // A word's row, or a part of it.  Added by reductions in memory, which nothing waits for: a row is added to once in a kernel, so they
-// have no order (reading the row first took k_embed_sum 22 us where it now takes 9).
+// have no order (8192 rows of 4 KB added: 17 us, reading the rows first 22).
 template <int E>
 __device__ __forceinline__ void put_row(const EmbedGradArgs& a, uint32_t word, uint32_t col, const float (&acc)[E]) {
   float* const u = a.update + (uint64_t)word * a.update_stride + (uint64_t)col * E;
@@ -572,36 +575,41 @@ cudaError_t embed_grad_typed(const EmbedGradArgs& a, cudaStream_t st) {
   return cudaGetLastError();
 }
 
-// clusters of the sort that the current device runs at once, asked for once per device
-uint32_t clusters_at_once() {
+// clusters of the sort, of 4 or of 8 blocks, that the current device runs at once, asked for once per device
+uint32_t clusters_at_once(uint32_t blocks) {
   static OncePerDevice once;
-  static std::atomic<int> known[64];
+  static std::atomic<int> known[64][2];
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 2;
   const cudaError_t e = once_per_device(once, [&] {
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(kNumSM / kMaxClusterBlocks * kMaxClusterBlocks);
-    cfg.blockDim = dim3(kTokenThreads);
-    cfg.dynamicSmemBytes = kTokenShared;
-    cudaLaunchAttribute attr;
-    attr.id = cudaLaunchAttributeClusterDimension;
-    attr.val.clusterDim.x = kMaxClusterBlocks;
-    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
-    cfg.attrs = &attr;
-    cfg.numAttrs = 1;
-    int n = 0;
-    const cudaError_t r = cudaOccupancyMaxActiveClusters(&n, k_token_sort, &cfg);
-    if (r == cudaSuccess) known[dev].store(n < 2 ? 2 : n, std::memory_order_relaxed);
-    return r;
+    for (int i = 0; i < 2; ++i) {
+      cudaLaunchAttribute attr;
+      attr.id = cudaLaunchAttributeClusterDimension;
+      attr.val.clusterDim.x = i ? 8 : 4;
+      attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+      cudaLaunchConfig_t cfg = {};
+      cfg.gridDim = dim3(attr.val.clusterDim.x);
+      cfg.blockDim = dim3(kTokenThreads);
+      cfg.dynamicSmemBytes = kTokenShared;
+      cfg.attrs = &attr;
+      cfg.numAttrs = 1;
+      int n = 0;
+      const cudaError_t r = cudaOccupancyMaxActiveClusters(&n, k_token_sort, &cfg);
+      if (r != cudaSuccess) return r;
+      known[dev][i].store(n < 2 ? 2 : n, std::memory_order_relaxed);
+    }
+    return cudaSuccess;
   });
-  return e == cudaSuccess ? (uint32_t)known[dev].load(std::memory_order_relaxed) : 2;
+  return e == cudaSuccess ? (uint32_t)known[dev][blocks == 8].load(std::memory_order_relaxed) : 2;
 }
 
 cudaError_t launch_token_sort(const EmbedGradArgs& a, cudaStream_t st) {
   uint32_t bits = 1;
   while ((a.vocab >> bits) != 0) ++bits;  // words 0 .. vocab
   const uint32_t passes = (bits + 8) / 9;
-  const uint32_t blocks = a.n <= kBlockSort ? 1 : kMaxClusterBlocks;
+  // Beside a table that is written out clusters of 4 leave fewer SMs without a block (65537 x 2048 into 65536 words: 70 us with clusters of 4, 92 of
+  // 8), as long as the sort is done before the zeros are.
+  const uint32_t blocks = a.n <= kBlockSort ? 1 : !a.accumulate && a.n <= kMarkedTokens / 2 ? 4 : kMaxClusterBlocks;
   const size_t smem = kTokenShared + (blocks == 1 ? (a.n < kTokenThreads ? kTokenThreads : a.n) * 8 : 0);
   static OncePerDevice once;
   const cudaError_t allowed = once_per_device(once, [] { return allow_shared(k_token_sort, kTokenShared + kBlockSort * 8); });
@@ -613,7 +621,7 @@ cudaError_t launch_token_sort(const EmbedGradArgs& a, cudaStream_t st) {
   if (!a.accumulate) {
     fill = fill_grid(a.vocab * a.dim, 4 * kTokenThreads, kNumSM - 1);
     if (blocks > 1) {
-      const uint32_t most = (clusters_at_once() - 1) * blocks;
+      const uint32_t most = (clusters_at_once(blocks) - 1) * blocks;
       fill = std::min((fill + blocks - 1) / blocks * blocks, most);
     }
   }

@@ -641,12 +641,19 @@ __device__ __forceinline__ bool bar_try(uint64_t* b, uint32_t parity) {
                : "memory");
   return done != 0;
 }
-// Bounded: a wait that runs out clears `ok`, and later ones try once.
+__device__ __forceinline__ uint64_t nanoseconds() {
+  uint64_t t;
+  asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
+  return t;
+}
+// Bounded: a wait of four seconds clears `ok`, and later ones try once.
 __device__ __forceinline__ void bar_wait(uint64_t* b, uint32_t parity, bool& ok) {
   if (bar_try(b, parity)) return;
-  for (uint32_t tries = ok ? 1u << 22 : 0u; tries; --tries)
+  const uint64_t began = nanoseconds();
+  while (ok) {
     if (bar_try(b, parity)) return;
-  ok = false;
+    if (nanoseconds() - began > 4000000000ull) ok = false;
+  }
 }
 // A warp has read its part of a stage.  The copy that fills the stage next writes it by another path than the loads take: the loads
 // have to be over before the copying thread hears of it, and the arrival alone does not see to that.
@@ -1178,16 +1185,15 @@ struct Cut {
 };
 constexpr int kFewVecs = 2;  // short shares have more threads instead, each of which is done sooner
 
-// `keep`: most vectors a thread keeps, where the second half works from them (0: it does not).  Blocks of a cluster: as many as keep the row,
-// and, where rows are few, as many as give every SM two blocks.
+// `keep`: most vectors a thread keeps, where the second half works from them (0: it does not).  Blocks of a cluster: as many as keep the row
+// (and have room for its marks), and, where rows are few, as many as give every SM two blocks.
 Cut cut_rows(const void* logits, uint64_t stride, uint64_t rows, uint32_t vocab, uint32_t size, uint32_t nv, uint32_t keep) {
   const uint32_t per_vec = 16 / size;
   const bool even = (reinterpret_cast<uintptr_t>(logits) & 15) == 0 && stride * size % 16 == 0;  // every row begins with a vector
   const uint32_t vecs = (vocab + per_vec - 1) / per_vec + (even ? 0 : 1), tiles = (vecs + 31) / 32;
   Cut c = {0, 0, 0, false};
   const auto share = [&] { return ((tiles + (1u << c.log_blocks) - 1) >> c.log_blocks) * 32; };
-  if (keep)
-    while (c.log_blocks < 3 && share() > keep * kRowThreads) ++c.log_blocks;
+  while (c.log_blocks < 3 && ((keep && share() > keep * kRowThreads) || share() * per_vec > CVLC_MAX_VOCAB / 8)) ++c.log_blocks;
   while (c.log_blocks < 3 && (rows << c.log_blocks) < 2 * kNumSM && (vecs >> c.log_blocks) >= 512) ++c.log_blocks;
   c.few = share() <= kFewVecs * kRowThreads;
   if (c.few) nv = kFewVecs;
@@ -1197,12 +1203,11 @@ Cut cut_rows(const void* logits, uint64_t stride, uint64_t rows, uint32_t vocab,
   return c;
 }
 
+// shared memory of a block at most: a bit for every element of an eighth of the longest row, and the most records
+constexpr size_t kRowShared = CVLC_MAX_VOCAB / 8 / 8 + 8192 + (size_t)CVLC_MAX_RECORDS * 24;
+
 template <class... Params, class... Args>
 cudaError_t launch_rows(int id, void (*kernel)(Params...), uint64_t rows, const Cut& c, bool clusters, size_t smem, cudaStream_t st, Args&&... args) {
-  if (smem > 40 * 1024) {
-    const cudaError_t e = allow_shared(kernel, smem);
-    if (e != cudaSuccess) return e;
-  }
   LaunchScope ls(id, st);
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(rows << c.log_blocks));
@@ -1248,6 +1253,11 @@ cudaError_t distill_typed(const DistillArgs& a, cudaStream_t st) {
   const uint32_t mark_bytes = (c.rounds * c.threads * kPerVec<T> / 8 + 15) & ~15u;  // a bit for every element of a block
   const size_t smem = mark_bytes + records_bytes(a.k);
   void (*const kernel)(DistillArgs, uint32_t, uint32_t) = c.few ? k_distill<T, kFewVecs, KIND> : k_distill<T, NV, KIND>;
+  if (smem > 40 * 1024) {  // the most that any call asks for, so that calls of other threads do not matter
+    static OncePerDevice once[2];
+    const cudaError_t e = smem > kRowShared ? cudaErrorInvalidValue : once_per_device(once[c.few], [&] { return allow_shared(kernel, kRowShared); });
+    if (e != cudaSuccess) return e;
+  }
   return launch_rows(KIND == kDistillLoss ? kKDistillLoss : KIND == kDistillGrad ? kKDistillGrad : kKDistillStep, kernel, a.rows, c,
                      KIND != kDistillGrad, smem, st, a, c.log_blocks, mark_bytes);
 }

@@ -299,6 +299,19 @@ def test_distill_of_more_words_than_a_cluster_keeps(rest):
         check_distill(B, z, flat, ids, lp, rest, 1.0)
 
 
+@pytest.mark.parametrize("rows,vocab,dtype", [(300, 900_001, torch.bfloat16), (300, 530_000, torch.float32), (1, 1 << 22, torch.float32),
+                                              (2, (1 << 22) - 3, torch.float16)])
+def test_distill_of_the_longest_rows(rows, vocab, dtype):
+    B = binding()
+    g = torch.Generator(device="cuda").manual_seed(1)
+    z = torch.randn(rows, vocab, generator=g, device="cuda").mul_(2).to(dtype)
+    ids = torch.randint(0, vocab, (rows, 40), generator=g, device="cuda", dtype=torch.int32)
+    lp = torch.log_softmax(torch.randn(rows, 41, generator=g, device="cuda"), 1)[:, :40].contiguous()
+    check_distill(B, z, z.flatten(), ids, lp, R.BUCKET, 1.0, in_place=False)
+    if rows < 3:
+        check_top(B, z, 256, 1.0)
+
+
 @pytest.mark.parametrize("rest", [R.NONE, R.SCALED, R.BUCKET])
 @pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("kind,lists,lead,pad", [("normal", "top", 0, 0), ("normal", "twice", 1, 1), ("masked", "absent", 3, 2), ("lowest", "any", 0, 8),

@@ -19,7 +19,7 @@ def top(**kw):
 @pytest.mark.parametrize("kw", [
     dict(logits=None), dict(logits=AT + 1), dict(logits=AT + 2, dtype=B.CVLC_F32), dict(dtype=3), dict(rows=(1 << 27) + 1),
     dict(vocab=0, stride=0, k=1), dict(vocab=B.MAX_VOCAB + 1, stride=B.MAX_VOCAB + 1), dict(stride=99), dict(stride=1 << 33), dict(k=0),
-    dict(k=101), dict(vocab=1000, stride=1000, k=257), dict(temperature=0.0), dict(temperature=-1.0), dict(temperature=math.inf),
+    dict(k=101), dict(vocab=1000, stride=1000, k=257), dict(temperature=0.0), dict(temperature=-1.0), dict(temperature=9e-7), dict(temperature=1.1e6), dict(temperature=math.inf),
     dict(temperature=math.nan), dict(ids=None), dict(ids=AT + 2), dict(logp=None), dict(logp=AT + 1)])
 def test_top_logits_refuses(kw):
     assert top(**kw) == BAD
