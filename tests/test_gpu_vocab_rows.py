@@ -379,12 +379,13 @@ def test_distill_gradient_by_differences(rest):
 
 # ---- how they are called -------------------------------------------------------------------------
 
-def test_rows_on_another_stream_and_in_a_graph():
+@pytest.mark.parametrize("rows,vocab", [(20, 9001), (310, 20001)])
+def test_rows_on_another_stream_and_in_a_graph(rows, vocab):
     B = binding()
-    z, _ = logits_of(20, 9001, torch.bfloat16, seed=4)
+    z, _ = logits_of(rows, vocab, torch.bfloat16, seed=4)
     side = torch.cuda.Stream()
-    ids, lp = torch.zeros(20, 40, dtype=torch.int32, device="cuda"), torch.zeros(20, 40, device="cuda")
-    loss, g = torch.zeros(20, device="cuda"), torch.zeros_like(z)
+    ids, lp = torch.zeros(rows, 40, dtype=torch.int32, device="cuda"), torch.zeros(rows, 40, device="cuda")
+    loss, g = torch.zeros(rows, device="cuda"), torch.zeros_like(z)
     torch.cuda.synchronize()
     B.cvlc_top_logits(z, ids, lp, stream=side)
     B.cvlc_distill_step(z, ids, lp, loss, g, stream=side)
@@ -400,11 +401,58 @@ def test_rows_on_another_stream_and_in_a_graph():
         graph.replay()
         for t, w in zip((ids, lp, loss, g), want):
             assert torch.equal(t, w)
-    other, _ = logits_of(20, 9001, torch.bfloat16, seed=5)
+    other, _ = logits_of(rows, vocab, torch.bfloat16, seed=5)
     z.copy_(other)
     graph.replay()
     check_ids, _, _ = R.top(z, 40, 1.0)
     assert torch.equal(ids.cpu(), check_ids)
+
+
+def test_two_calls_at_once():
+    """two streams, each with rows for all SMs: equal bits to one after the other"""
+    B = binding()
+    zs = [logits_of(330, 20000, torch.bfloat16, seed=s)[0] for s in (1, 2)]
+    recs = [records(z, 30, 1.0, seed=4) for z in zs]
+    loss, g = [torch.zeros(330, device="cuda") for _ in zs], [torch.zeros_like(z) for z in zs]
+    for i in (0, 1):
+        B.cvlc_distill_step(zs[i], *recs[i], loss[i], g[i])
+    want = [t.clone() for t in loss + g]
+    streams = [torch.cuda.Stream() for _ in zs]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for i in (0, 1):
+            B.cvlc_distill_step(zs[i], *recs[i], loss[i], g[i], stream=streams[i])
+    torch.cuda.synchronize()
+    for t, w in zip(loss + g, want):
+        assert torch.equal(t, w)
+
+
+@pytest.mark.parametrize("rows,vocab", [(6, 3000), (310, 18000)])
+def test_gradient_with_weights_of_its_own(rows, vocab):
+    """what the loss keeps holds for every row, also for those that its own weights left out"""
+    B = binding()
+    z, _ = logits_of(rows, vocab, torch.float32, seed=8)
+    ids, lp = records(z, 25, 1.0, seed=4)
+    early = torch.zeros(rows, device="cuda")
+    early[::2] = 1.0
+    late = torch.rand(rows, generator=torch.Generator().manual_seed(2)).cuda()
+    late[3] = 0.0
+    loss, stats, g = torch.zeros(rows, device="cuda"), torch.zeros(rows, B.DISTILL_STATS, device="cuda"), torch.ones_like(z)
+    B.cvlc_distill_loss(z, ids, lp, loss, stats, row_weight=early)
+    assert (loss[1::2] == 0).all()
+    B.cvlc_distill_grad(z, ids, lp, stats, g, row_weight=late)
+    _, want, _, tol = R.distill(z, ids, lp, R.BUCKET, 1.0, late)
+    R.assert_near(g, want, tol)
+
+
+def test_no_rows():
+    B = binding()
+    z, ids, lp = torch.zeros(0, 100, device="cuda"), torch.zeros(0, 5, dtype=torch.int32, device="cuda"), torch.zeros(0, 5, device="cuda")
+    loss, stats, g = torch.zeros(0, device="cuda"), torch.zeros(0, B.DISTILL_STATS, device="cuda"), torch.zeros(0, 100, device="cuda")
+    B.cvlc_top_logits(z, ids, lp)
+    B.cvlc_distill_loss(z, ids, lp, loss, stats)
+    B.cvlc_distill_grad(z, ids, lp, stats, g)
+    B.cvlc_distill_step(z, ids, lp, loss, g)
 
 
 def test_launches_are_counted():
