@@ -23,8 +23,8 @@ constexpr int kLookupThreads = 256;
 constexpr int kLookupRows = 4;  // tokens of a thread: that many independent loads
 
 // A block has blockDim.x columns (vectors of a row) by blockDim.y groups of kLookupRows tokens, and goes from groups to groups: the next ones'
-// tokens are on their way while this one's rows are.  (A block for every group, which has to wait for its tokens first: 32768 rows of 8 KB
-// 76 us.)
+// tokens are on their way while this one's rows are.  The rows' reads bound it, or the launch: 300 x 768 32-bit values 8 us a call, 30000 rows
+// of 128 bytes 6 us, in a graph.  (A block for every group, which has to wait for its tokens first: 32768 rows of 8 KB 80 us, this form 76.)
 template <class T, bool VEC>
 __global__ void __launch_bounds__(kLookupThreads, 6) k_embed(EmbedArgs a) {
   constexpr int E = VEC ? kPerVec<T> : 1;
@@ -77,7 +77,8 @@ __global__ void __launch_bounds__(kLookupThreads, 6) k_embed(EmbedArgs a) {
   if (outside && a.status) set_status(a.status, CVLC_ERR_INVALID_ARG);
 }
 
-// Long rows: a warp for a row, kLookupWide vectors of a lane on their way, and the next row's token.
+// Long rows, of 128 vectors or more: a warp for a row, kLookupWide vectors of a lane on their way, and the next row's token.  Memory bounds it: 32768
+// rows of 8 KB (24000 of them different) 71 us, 79% of the copy bandwidth, k_embed 76.
 constexpr int kLookupWide = 8;
 template <class T>
 __global__ void __launch_bounds__(kLookupThreads, 4) k_embed_wide(EmbedArgs a) {
@@ -289,7 +290,10 @@ __device__ void sort_in_block(const EmbedGradArgs& a, uint32_t bits, uint32_t pa
   }
 }
 
-// Stable radix sort by digits of up to nine bits, by one cluster.  Every warp has a stretch of the positions, in order; it counts its
+// Stable radix sort by digits of up to nine bits, by one cluster.  What bounds it is its chain of passes, each of two walks and two cluster
+// barriers, on eight SMs: 8192 tokens of 32000 words 18 us with the launch.  The zeros of the launch's other blocks hide it where the table is
+// large (65537 tokens beside 512 MB of table: 88 us, the time of the zeros alone).  Clusters of 4 leave the zeros more SMs and the sort
+// fewer: 17308 tokens beside 22 MB 31 us for the whole gradient, with 8 27; beside 512 MB 180 and 180.  Every warp has a stretch of the positions, in order; it counts its
 // digits (in any order), the counts are scanned over warps (in groups, side by side) and blocks for every digit, and the warp walks its stretch again, giving
 // each position its place.  Tokens that stand for nothing (below zero, or outside the table) sort behind all words as word `vocab`.
 __global__ void __launch_bounds__(kTokenThreads, 1) k_token_sort(EmbedGradArgs a, uint32_t bits, uint32_t passes, uint32_t blocks) {
@@ -390,6 +394,7 @@ __global__ void __launch_bounds__(kTokenThreads, 1) k_token_sort(EmbedGradArgs a
 
 // ---- the gradient: sums ------------------------------------------------------------------------------
 constexpr int kSumThreads = 128;
+constexpr uint32_t kSumPlaces = 1024;  // positions of a block
 constexpr int kSumAhead = 8;   // rows whose loads a thread has in flight
 constexpr int kJoinAhead = 8;  // and pieces
 
@@ -441,23 +446,29 @@ __device__ __forceinline__ void get_piece(const float* p, float (&v)[E]) {
   }
 }
 
-// Block (chunk, slice of the columns).  A word whose positions all lie in the chunk gets its row; the piece of one that began in an
-// earlier chunk goes to the chunk's first place in `pieces`, that of one that begins here and goes on to the second.
+// Block (chunks, slice of the columns): kSumThreads / `width` chunks, `width` columns, so that short rows leave no thread idle (100000 rows of 64 32-bit
+// values, the whole gradient: 60 us with a chunk a block, 54 so).  Memory bounds it: 65537 rows of 4 KB 87 us, 8192 rows of 2 KB, added,
+// 17.  A word whose positions all lie in the chunk gets its row;
+// the piece of one that began in an earlier chunk goes to the chunk's first place in `pieces`, that of one that begins here and goes
+// on to the second.
 template <class T, bool VEC>
-__global__ void __launch_bounds__(kSumThreads) k_embed_sum(EmbedGradArgs a, uint32_t chunk, float* pieces) {
+__global__ void __launch_bounds__(kSumThreads) k_embed_sum(EmbedGradArgs a, uint32_t chunk, uint32_t width, float* pieces) {
   constexpr int E = VEC ? kPerVec<T> : 1;
-  __shared__ uint32_t words[kChunkMost], where[kChunkMost];
+  __shared__ uint32_t words_of[kSumPlaces], where_of[kSumPlaces];
   pdl_enter();
   const Sorted S = {reinterpret_cast<const unsigned long long*>(static_cast<unsigned char*>(a.ws) + eg_off_a()), a.n, (uint32_t)a.vocab};
-  const uint64_t first = (uint64_t)blockIdx.x * chunk;
-  for (uint32_t i = threadIdx.x; i < chunk; i += kSumThreads) {
-    const unsigned long long it = first + i < a.n ? __ldg(S.at + first + i) : (unsigned long long)a.vocab << 32;
-    words[i] = (uint32_t)(it >> 32);
-    where[i] = (uint32_t)it;
+  const uint32_t here = kSumThreads / width, mine = threadIdx.x / width;
+  for (uint32_t i = threadIdx.x; i < here * chunk; i += kSumThreads) {
+    const uint64_t at = (uint64_t)blockIdx.x * here * chunk + i;
+    const unsigned long long it = at < a.n ? __ldg(S.at + at) : (unsigned long long)a.vocab << 32;
+    words_of[i] = (uint32_t)(it >> 32);
+    where_of[i] = (uint32_t)it;
   }
+  const uint64_t c = (uint64_t)blockIdx.x * here + mine, first = c * chunk;
+  const uint32_t *const words = words_of + mine * chunk, *const where = where_of + mine * chunk;
   const uint32_t before = first ? S.word(first - 1) : S.vocab, after = S.word(first + chunk);
   __syncthreads();
-  const uint32_t cols = a.dim / E, col = blockIdx.y * kSumThreads + threadIdx.x;
+  const uint32_t cols = a.dim / E, col = blockIdx.y * width + threadIdx.x % width;
   if (col >= cols || words[0] == S.vocab) return;
   const T* const grad = static_cast<const T*>(a.grad) + (uint64_t)col * E;
   float acc[E];
@@ -492,7 +503,7 @@ __global__ void __launch_bounds__(kSumThreads) k_embed_sum(EmbedGradArgs a, uint
       const uint32_t next = last ? after : words[i + r + 1];
       if (next == w && !last) continue;
       if (begun_before || next == w) {
-        put_piece<E>(pieces + ((uint64_t)blockIdx.x * 2 + (begun_before ? 0 : 1)) * a.dim + (uint64_t)col * E, acc);
+        put_piece<E>(pieces + (c * 2 + (begun_before ? 0 : 1)) * a.dim + (uint64_t)col * E, acc);
       } else {
         put_row<E>(a, w, col, acc);
       }
@@ -503,7 +514,10 @@ __global__ void __launch_bounds__(kSumThreads) k_embed_sum(EmbedGradArgs a, uint
   }
 }
 
-// The word that begins in a chunk and goes on behind it: its pieces, in order
+// The word that begins in a chunk and goes on behind it: its pieces, in order.  Latency bounds it: the launch, and the chain of a word that has many
+// chunks (8192 tokens 8.6 us, 65537 13).  Four groups of threads for a quarter of the pieces each make every block large, and the blocks of
+// the words that do not go on cost more than the chains save (65537 x 2048: 181 us for the whole gradient, so 172; 26336 positions of 616 words
+// 87 and 68).
 template <int E>
 __global__ void __launch_bounds__(kSumThreads) k_embed_join(EmbedGradArgs a, uint32_t chunk, const float* pieces) {
   pdl_enter();
@@ -567,49 +581,48 @@ cudaError_t embed_grad_typed(const EmbedGradArgs& a, cudaStream_t st) {
   const bool vec = (reinterpret_cast<uintptr_t>(a.grad) & 15) == 0 && (reinterpret_cast<uintptr_t>(a.update) & 15) == 0 &&
                    a.dim % kPerVec<T> == 0 && a.grad_stride % kPerVec<T> == 0 && a.update_stride % 4 == 0;
   const uint32_t E = vec ? kPerVec<T> : 1;
-  const dim3 grid((unsigned)chunks, (a.dim / E + kSumThreads - 1) / kSumThreads);
-  void (*const sum)(EmbedGradArgs, uint32_t, float*) = vec ? k_embed_sum<T, true> : k_embed_sum<T, false>;
+  const uint32_t cols = a.dim / E;
+  uint32_t width = kSumThreads;  // columns of a block; short rows leave room for several chunks
+  while (width > 4 && width / 2 >= cols && kSumThreads / (width / 2) * chunk <= kSumPlaces) width /= 2;
+  const uint32_t here = kSumThreads / width;
+  void (*const sum)(EmbedGradArgs, uint32_t, uint32_t, float*) = vec ? k_embed_sum<T, true> : k_embed_sum<T, false>;
   void (*const join)(EmbedGradArgs, uint32_t, const float*) = vec ? k_embed_join<kPerVec<T>> : k_embed_join<1>;
-  launch_kernel(kKEmbedSum, sum, grid, dim3(kSumThreads), 0, st, true, a, chunk, pieces);
-  launch_kernel(kKEmbedJoin, join, grid, dim3(kSumThreads), 0, st, true, a, chunk, pieces);
+  launch_kernel(kKEmbedSum, sum, dim3((unsigned)((chunks + here - 1) / here), (cols + width - 1) / width), dim3(kSumThreads), 0, st, true, a, chunk, width,
+                pieces);
+  launch_kernel(kKEmbedJoin, join, dim3((unsigned)chunks, (cols + kSumThreads - 1) / kSumThreads), dim3(kSumThreads), 0, st, true, a, chunk, pieces);
   return cudaGetLastError();
 }
 
-// clusters of the sort, of 4 or of 8 blocks, that the current device runs at once, asked for once per device
-uint32_t clusters_at_once(uint32_t blocks) {
+// clusters of the sort that the current device runs at once, asked for once per device
+uint32_t clusters_at_once() {
   static OncePerDevice once;
-  static std::atomic<int> known[64][2];
+  static std::atomic<int> known[64];
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 2;
   const cudaError_t e = once_per_device(once, [&] {
-    for (int i = 0; i < 2; ++i) {
-      cudaLaunchAttribute attr;
-      attr.id = cudaLaunchAttributeClusterDimension;
-      attr.val.clusterDim.x = i ? 8 : 4;
-      attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
-      cudaLaunchConfig_t cfg = {};
-      cfg.gridDim = dim3(attr.val.clusterDim.x);
-      cfg.blockDim = dim3(kTokenThreads);
-      cfg.dynamicSmemBytes = kTokenShared;
-      cfg.attrs = &attr;
-      cfg.numAttrs = 1;
-      int n = 0;
-      const cudaError_t r = cudaOccupancyMaxActiveClusters(&n, k_token_sort, &cfg);
-      if (r != cudaSuccess) return r;
-      known[dev][i].store(n < 2 ? 2 : n, std::memory_order_relaxed);
-    }
-    return cudaSuccess;
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = kMaxClusterBlocks;
+    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(kMaxClusterBlocks);
+    cfg.blockDim = dim3(kTokenThreads);
+    cfg.dynamicSmemBytes = kTokenShared;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    int n = 0;
+    const cudaError_t r = cudaOccupancyMaxActiveClusters(&n, k_token_sort, &cfg);
+    if (r == cudaSuccess) known[dev].store(n < 2 ? 2 : n, std::memory_order_relaxed);
+    return r;
   });
-  return e == cudaSuccess ? (uint32_t)known[dev][blocks == 8].load(std::memory_order_relaxed) : 2;
+  return e == cudaSuccess ? (uint32_t)known[dev].load(std::memory_order_relaxed) : 2;
 }
 
 cudaError_t launch_token_sort(const EmbedGradArgs& a, cudaStream_t st) {
   uint32_t bits = 1;
   while ((a.vocab >> bits) != 0) ++bits;  // words 0 .. vocab
   const uint32_t passes = (bits + 8) / 9;
-  // Beside a table that is written out clusters of 4 leave fewer SMs without a block (65537 x 2048 into 65536 words: 70 us with clusters of 4, 92 of
-  // 8), as long as the sort is done before the zeros are.
-  const uint32_t blocks = a.n <= kBlockSort ? 1 : !a.accumulate && a.n <= kMarkedTokens / 2 ? 4 : kMaxClusterBlocks;
+  const uint32_t blocks = a.n <= kBlockSort ? 1 : kMaxClusterBlocks;
   const size_t smem = kTokenShared + (blocks == 1 ? (a.n < kTokenThreads ? kTokenThreads : a.n) * 8 : 0);
   static OncePerDevice once;
   const cudaError_t allowed = once_per_device(once, [] { return allow_shared(k_token_sort, kTokenShared + kBlockSort * 8); });
@@ -621,7 +634,7 @@ cudaError_t launch_token_sort(const EmbedGradArgs& a, cudaStream_t st) {
   if (!a.accumulate) {
     fill = fill_grid(a.vocab * a.dim, 4 * kTokenThreads, kNumSM - 1);
     if (blocks > 1) {
-      const uint32_t most = (clusters_at_once(blocks) - 1) * blocks;
+      const uint32_t most = (clusters_at_once() - 1) * blocks;
       fill = std::min((fill + blocks - 1) / blocks * blocks, most);
     }
   }
