@@ -1,7 +1,11 @@
 // Rows of logits: what a client or a teacher answers (the top logits of every row) and distillation from such answers, the loss
-// and its gradient.  A row's softmax needs its maximum and its sum of exponentials before anything can be written, so a row is
-// cut over the blocks of a cluster, every thread keeps the 16-byte vectors that it has loaded in registers, the blocks exchange a
-// few numbers through the cluster's shared memory, and the second half works from the registers: the logits are read once.
+// and its gradient.  All are bound by the reading of the logits (0.5 to 3 operations a byte, none of which a matrix instruction does) and, where
+// rows are few or short, by the chain of load, maximum, sum, exchange and store.  A row's softmax needs its maximum and its sum of
+// exponentials before anything can be written.
+// Few or short rows: a row is cut over the blocks of a cluster, every thread keeps the 16-byte vectors that it has loaded in registers, the
+// blocks exchange a few numbers through the cluster's shared memory, and the second half works from the registers: the logits are read once.
+// Many long rows: two blocks an SM go from row to row, and what a row needs beside its elements is done by warps of their own.
+// streamed() says which, with both sides' times.
 #include <cooperative_groups.h>
 
 #include "cvlc_vocab.cuh"
@@ -1122,7 +1126,7 @@ __global__ void __launch_bounds__(kStreamBlock, 2) k_distill_stream(DistillArgs 
     } else {
       w = *reinterpret_cast<const Whole*>(a.stats + row * CVLC_DISTILL_STATS);
     }
-    const float ca = w.a * (weight / a.temperature);
+    float ca = w.a * (weight / a.temperature);
     unsigned char* const to = reinterpret_cast<unsigned char*>(g) + (int)(R.whole_from * 16) - (int)(R.lead * sizeof(T));  // of the first whole vector
     const bool alike = (reinterpret_cast<uintptr_t>(to) & 15) == 0;
     const uint32_t cuts = (R.wholes + kStageVecs - 1) / kStageVecs, kept = cuts - again / kStageVecs;
@@ -1139,6 +1143,7 @@ __global__ void __launch_bounds__(kStreamBlock, 2) k_distill_stream(DistillArgs 
         v = (KIND == kDistillStep ? cut - kept : cut) * kStageVecs;
         take_stage<T>(ring, stage, phase, stages, full, empty, v, R.wholes, ok, raw);
       }
+      if (!ok) ca = CUDART_NAN_F;
 #pragma unroll
       for (int j = 0; j < kStageShare; ++j) {
         float f[E];

@@ -130,6 +130,35 @@ def test_embed_grad_of_many_tokens(kind):
     check_grad(B, tokens_of(150_001, 70_000, kind, True), g, 70_000, 1.0, True)
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("kind", ["zipf", "few"])
+@pytest.mark.parametrize("dim", [1, 8, 17, 32, 64, 200])
+def test_embed_grad_of_many_short_rows(dim, kind, dtype):
+    """several chunks in a block, the last of which has no position"""
+    B = binding()
+    for n, vocab in ((70_001, 5000), (33_000, 400)):
+        g, _ = matrix(n, dim, dtype, 8)
+        check_grad(B, tokens_of(n, vocab, kind, False), g, vocab, 1.0, kind == "few")
+
+
+def test_embed_of_rows_far_apart():
+    """rows behind 2^32 elements, by their strides"""
+    B = binding()
+    stride = (1 << 31) + 16
+    flat = torch.empty(2 * stride + 1024, dtype=torch.bfloat16, device="cuda")
+    table, out = flat.as_strided((3, 256), (stride, 1)), flat.as_strided((3, 200), (stride, 1), 512)
+    table.copy_(torch.randn(3, 256, generator=torch.Generator().manual_seed(1)))
+    t = torch.tensor([2, 0, 2], device="cuda")
+    B.cvlc_embed(table[:, :200], t, out)
+    assert torch.equal(out, table[t, :200])
+    far = flat.as_strided((3, 256), (stride, 1), 768)
+    far.copy_(table)
+    got = torch.empty(3, 256, dtype=torch.bfloat16, device="cuda")
+    B.cvlc_embed(far, t, got)
+    assert torch.equal(got, table[t])
+    check_grad(B, t, far, 3, 1.0, False)
+
+
 def test_embed_grad_of_a_wide_row():
     B = binding()
     g, _ = matrix(40, 8192, torch.float16, 8)

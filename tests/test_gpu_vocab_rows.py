@@ -445,6 +445,27 @@ def test_gradient_with_weights_of_its_own(rows, vocab):
     R.assert_near(g, want, tol)
 
 
+@pytest.mark.parametrize("rows,vocab,stride", [(3, 5003, (1 << 31) + 5), (3, 140001, (1 << 31) + 8), (160, 20001, 27_000_003)])
+def test_rows_far_apart(rows, vocab, stride):
+    """rows behind 2^32 elements, by their strides"""
+    B = binding()
+    flat = torch.empty((rows - 1) * stride + vocab + 8, dtype=torch.bfloat16, device="cuda")
+    z = flat.as_strided((rows, vocab), (stride, 1), 3)
+    z.copy_(torch.randn(rows, vocab, generator=torch.Generator().manual_seed(rows)) * 3)
+    check_top(B, z, 40, 0.7)
+    ids, lp = records(z, 40, 1.0, seed=2)
+    want, want_g, tol, tol_g = R.distill(z, ids, lp, R.BUCKET, 1.0)
+    loss, stats = torch.zeros(rows, device="cuda"), torch.zeros(rows, B.DISTILL_STATS, device="cuda")
+    B.cvlc_distill_loss(z, ids, lp, loss, stats)
+    R.assert_near(loss, want, tol)
+    g = torch.zeros_like(z.contiguous())
+    B.cvlc_distill_grad(z, ids, lp, stats, g)
+    R.assert_near(g, want_g, tol_g, z.dtype)
+    B.cvlc_distill_step(z, ids, lp, loss, z)  # in the logits' place
+    R.assert_near(loss, want, tol)
+    R.assert_near(z, want_g, tol_g, z.dtype)
+
+
 def test_no_rows():
     B = binding()
     z, ids, lp = torch.zeros(0, 100, device="cuda"), torch.zeros(0, 5, dtype=torch.int32, device="cuda"), torch.zeros(0, 5, device="cuda")
