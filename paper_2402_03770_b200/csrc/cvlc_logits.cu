@@ -424,6 +424,7 @@ __device__ __forceinline__ uint32_t listed_of(const uint8_t* marks, uint32_t i) 
   return kPerVec<T> == 8 ? marks[i] : (marks[i >> 1] >> ((i & 1) * 4)) & 15u;
 }
 
+// Latency bounds it: 16 rows of 32,000 words 10 us a call, 64 of 131,072 17.
 // The loss goes through its share a batch ahead (2 x NV vectors of a thread in registers); the step keeps its batch for the gradient, and
 // reads again what lies behind the first batch, if the row is longer than its cluster keeps.
 template <class T, int NV, DistillKind KIND>
@@ -600,7 +601,9 @@ __global__ void __launch_bounds__(kRowThreads, 2) k_distill(DistillArgs a, uint3
 // thread copies the rows through a ring of stages in shared memory (cp.async.bulk), four vectors of every thread a stage.  The step passes over
 // every row twice, at first over what the ring still holds of it, then over what it has to copy once more, most of which is in the L2 cache
 // (the 296 rows on their way are 76 MB at 131,072 words of 16 bits).  Keeping the row in the cluster's registers instead costs every block of the cluster all of the above:
-// 4096 x 131072 bf16 750 us.
+// 4096 x 131072 bf16 750 us, so 415 to 452 (of 329 at the copy bandwidth; warm, and with cold caches); the loss 192 to 214 (of 165).  The pass is a
+// chain of load, maximum, exponential and sum in 16 warps an SM: without the exponentials the loss takes 156 us.  More warps for it leave
+// too few registers and stages (ten 211, twelve 243).
 constexpr int kStreamWarps = 8, kSideWarps = 4;  // and one that copies
 constexpr int kStreamLanes = kStreamWarps * 32, kSideLanes = kSideWarps * 32;
 constexpr int kStreamBlock = kStreamLanes + kSideLanes + 32;
@@ -1609,7 +1612,8 @@ __global__ void __launch_bounds__(kRowThreads, 2) k_top_logits(TopArgs a, uint32
 }
 
 // Many long rows: as in k_distill_stream, a block goes from row to row, and the side warps rank what the pass over a row has listed while the
-// next row is passed over.  (2048 x 131072 bf16, k = 64: a block for every row 200 us.)
+// next row is passed over.  (2048 x 131072 bf16, k = 64: a block for every row 200 us, so 139; 82 at the copy bandwidth, 113 without the
+// exponentials.)
 // What the pass lists is whole vectors, each with its largest element: for a thread of a warp that alone has found one, the elements
 // would take many instructions of the whole warp.  The side warps read those again that the last bound leaves.
 constexpr uint32_t kEndWord = 0x80000000u;  // a listed word, not a vector
