@@ -443,7 +443,8 @@ int cvlc_top_logits(const void* logits_dev, uint32_t dtype, uint64_t rows, uint3
  * p_j = the sum of exp(log-probability) over the row's records of word j (records of one word add up: lists of several
  * clients may be joined, each with the logarithm of its weight added), P = sum p:
  *   CVLC_REST_NONE    loss = sum_j p_j (ln p_j - ln q_j)
- *   CVLC_REST_SCALED  the same of p / P; nothing where P = 0
+ *   CVLC_REST_SCALED  the same of p / P, whatever P is: log-probabilities that all move by one number change nothing.  Nothing
+ *                     where no record is above -inf
  *   CVLC_REST_BUCKET  all words that are not listed are one further outcome, of probability pr = max(0, 1 - P) for the
  *                     teacher and qr = the sum of their q for the student: loss + pr (ln pr - ln qr).  Where the
  *                     student may say none of them (no logit above -inf), there is no such outcome.

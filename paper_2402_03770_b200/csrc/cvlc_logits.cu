@@ -128,6 +128,11 @@ __device__ __forceinline__ MaxSum warp_join(const MaxSum& a, float c2) {
   for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(kFull, s, o);
   return {m, s};
 }
+__device__ __forceinline__ float warp_max(float v) {
+#pragma unroll
+  for (int o = 16; o; o >>= 1) v = fmaxf(v, __shfl_xor_sync(kFull, v, o));
+  return v;
+}
 template <class V>
 __device__ __forceinline__ V warp_sum(V v) {
 #pragma unroll
@@ -193,6 +198,8 @@ __device__ __forceinline__ void add_batch(const uint4 (&raw)[NV], float c2, MaxS
 //   it exp((z_j - r) it) A,  A = (P + pr) exp((r - m) it) / s - pr / s_r.
 // A block marks the listed words of its share in a bitmap in shared memory, where a second record of a word is noticed too.
 // The teacher's sums are a few numbers a row and are held in 64 bits: what a list leaves over is often a small difference from one.
+// SCALED does not change when all of a row's log-probabilities move by one number, so its p are taken relative to the largest of them:
+// a list of any mass, however far below (or above) what a number holds, then has P from 1 to k.
 
 struct Part {  // a block's share of a row
   MaxSum rest, said;        // unlisted and listed words
@@ -206,11 +213,11 @@ struct Whole {  // what the row's gradient needs; kept for it between loss and g
 static_assert(sizeof(Whole) <= 4 * CVLC_DISTILL_STATS, "a row's place in the buffer");
 
 // e^x to 2^-36 relative, which is far below what the rounding of x to fp32 leaves of it: x = n ln 2 + r, and the Taylor series of e^r
-// (|r| <= 0.35: 0.35^11 / 11! = 2^-42).  A third of the instructions of the library's.
-__device__ __forceinline__ double exp_of(float x) {
-  if (!(x > -600.f)) return x == x ? 0.0 : (double)x;
-  if (x > 600.f) return exp((double)x);
-  const double n = rint((double)x * 1.4426950408889634074), r = fma(n, -0.693147180559945309417, (double)x);
+// (|r| <= 0.35: 0.35^11 / 11! = 2^-42).
+__device__ __forceinline__ double exp_of(double x) {
+  if (!(x > -600.0)) return x == x ? 0.0 : x;
+  if (x > 600.0) return exp(x);
+  const double n = rint(x * 1.4426950408889634074), r = fma(n, -0.693147180559945309417, x);
   double y = 1.0 / 3628800.0;
   y = fma(y, r, 1.0 / 362880.0);
   y = fma(y, r, 1.0 / 40320.0);
@@ -229,7 +236,7 @@ __device__ __forceinline__ double exp_of(float x) {
 __device__ __forceinline__ double ln_of(double x) {
   if (!(x > 1e-30 && x < 1e30)) return log(x);
   const float y = logf((float)x);
-  const double r = fma(x, exp_of(-y), -1.0);
+  const double r = fma(x, exp_of((double)-y), -1.0);
   return (double)y + r * (1.0 - 0.5 * r);
 }
 
@@ -297,8 +304,8 @@ __device__ double loss_of(const Sums& s, const Part* parts, uint32_t blocks, uin
 __device__ __host__ __forceinline__ uint32_t padded(uint32_t k) { return (k + 15) & ~15u; }
 __device__ __host__ __forceinline__ size_t records_bytes(uint32_t k) { return (size_t)padded(k) * (8 + 4 * 4); }
 // What record i says of its word, where a word may have several: the sum over its records (`alone`: what each says by itself) in their
-// order, by the first of them; below 0 for the others.  ln_p: its logarithm.
-__device__ __forceinline__ double said_by(const int* at, const double* alone, const float* logp, uint32_t k, uint32_t i, double* ln_p) {
+// order, by the first of them; below 0 for the others.  ln_p: its logarithm, `ln_alone` where the word has no other record.
+__device__ __forceinline__ double said_by(const int* at, const double* alone, double ln_alone, uint32_t k, uint32_t i, double* ln_p) {
   const int here = at[i];
   double p = alone[i];
   bool merged = false, first = true;
@@ -318,9 +325,11 @@ __device__ __forceinline__ double said_by(const int* at, const double* alone, co
       p += alone[other], merged = true;
     }
   }
-  *ln_p = merged ? ln_of(p) : (double)logp[i];
+  *ln_p = merged ? ln_of(p) : ln_alone;
   return first ? p : -1.0;
 }
+// what all of a row's log-probabilities are taken relative to, their largest being `top`
+__device__ __forceinline__ double said_from(uint32_t rest, float top) { return rest == CVLC_REST_SCALED && top > -CUDART_INF_F ? (double)top : 0.0; }
 
 // ---- a row's records, as a block sees them ----
 // The words' places are marked as soon as the records are there, for the pass over the logits; what the teacher says of them is summed
@@ -350,20 +359,25 @@ struct Records {
       logp = a.logp[row * a.k + threadIdx.x];
     }
   }
-  // true: a word of this thread is marked twice.  marks: cleared before, a barrier between
+  // true: a word of this thread is marked twice.  marks: cleared before, a barrier between.  top_of_warp: the largest log-probability that
+  // the warp has seen of all the row's words, whichever block has them
   template <class T>
-  __device__ __forceinline__ bool mark(const DistillArgs& a, uint64_t row, const Row<T>& R, uint32_t* marks) {
+  __device__ __forceinline__ bool mark(const DistillArgs& a, uint64_t row, const Row<T>& R, uint32_t* marks, float* top_of_warp) {
     bool twice = false;
+    float top = -CUDART_INF_F;
     for (uint32_t i = threadIdx.x; i < a.k; i += blockDim.x) {
       if (i != threadIdx.x) id = a.ids[row * a.k + i], logp = a.logp[row * a.k + i];
       int p = -1;
       float v = 0.f;
       if (id >= 0 && (uint32_t)id >= a.vocab) {
         if (a.status) set_status(a.status, CVLC_ERR_INVALID_ARG);
-      } else if (id >= 0 && (p = R.place((uint32_t)id)) >= 0) {
-        v = to_float(R.at[id]);
-        const uint32_t bit = 1u << (p & 31);
-        twice |= (atomicOr(marks + (p >> 5), bit) & bit) != 0;
+      } else if (id >= 0) {
+        top = fmaxf(top, logp);
+        if ((p = R.place((uint32_t)id)) >= 0) {
+          v = to_float(R.at[id]);
+          const uint32_t bit = 1u << (p & 31);
+          twice |= (atomicOr(marks + (p >> 5), bit) & bit) != 0;
+        }
       }
       at[i] = p;
       said[i] = logp;
@@ -371,20 +385,28 @@ struct Records {
       else logit[i] = v;
     }
     if (threadIdx.x < padded(a.k) - a.k) at[a.k + threadIdx.x] = -2;
+    if (a.rest == CVLC_REST_SCALED) {
+      top = warp_max(top);
+      if ((threadIdx.x & 31) == 0) top_of_warp[threadIdx.x >> 5] = top;
+    }
     return twice;
   }
   // p of every word, summed in the order of its records; behind the barrier that follows mark()
   template <bool SUMS>
-  __device__ __forceinline__ void teacher(const DistillArgs& a, bool twice) {
+  __device__ __forceinline__ void teacher(const DistillArgs& a, bool twice, const float* top_of_warp) {
+    float top = -CUDART_INF_F;
+    if (a.rest == CVLC_REST_SCALED)
+      for (uint32_t w = 0; w < blockDim.x / 32; ++w) top = fmaxf(top, top_of_warp[w]);
+    const double from = said_from(a.rest, top);
     if (twice) {
-      for (uint32_t i = threadIdx.x; i < a.k; i += blockDim.x) alone[i] = exp_of(said[i]);
+      for (uint32_t i = threadIdx.x; i < a.k; i += blockDim.x) alone[i] = exp_of((double)said[i] - from);
       __syncthreads();
     }
     for (uint32_t i = threadIdx.x; i < a.k; i += blockDim.x) {
-      double p = -1.0, ln_p = 0.0;
+      double p = -1.0, ln_p = (double)said[i] - from;
       if (at[i] >= 0) {
-        if (twice) p = said_by(at, alone, said, a.k, i, &ln_p);
-        else ln_p = (double)said[i], p = exp_of(said[i]);
+        if (twice) p = said_by(at, alone, ln_p, a.k, i, &ln_p);
+        else p = exp_of(ln_p);
         if (SUMS && !(p < 0.0)) {
           mass += p;
           if (p != 0.0) ent += p * ln_p;
@@ -433,6 +455,7 @@ __global__ void __launch_bounds__(kRowThreads, 2) k_distill(DistillArgs a, uint3
   __shared__ Part parts[kMaxClusterBlocks];
   __shared__ MaxSum of_warp[kRowThreads / 32];
   __shared__ Part said_of_warp[kRowThreads / 32];
+  __shared__ float top_of_warp[kRowThreads / 32];
   __shared__ Whole whole;
   const uint32_t nt = blockDim.x, tid = threadIdx.x, blocks = 1u << log_blocks, lane = tid & 31, warp = tid >> 5;
   const uint32_t rank = blockIdx.x & (blocks - 1);
@@ -457,8 +480,8 @@ __global__ void __launch_bounds__(kRowThreads, 2) k_distill(DistillArgs a, uint3
   if (!idle) {
     for (uint32_t i = tid; i < mark_bytes / 16; i += nt) reinterpret_cast<uint4*>(marks)[i] = make_uint4(0, 0, 0, 0);
     __syncthreads();
-    const bool twice = __syncthreads_or(S.mark<T>(a, row, R, reinterpret_cast<uint32_t*>(marks)));
-    S.teacher<KIND != kDistillGrad>(a, twice);
+    const bool twice = __syncthreads_or(S.mark<T>(a, row, R, reinterpret_cast<uint32_t*>(marks), top_of_warp));
+    S.teacher<KIND != kDistillGrad>(a, twice, top_of_warp);
     if (KIND == kDistillGrad) {
       if (tid < a.k) S.logit[tid] = S.z;
     } else {
@@ -833,6 +856,7 @@ __global__ void __launch_bounds__(kStreamBlock, 2) k_distill_stream(DistillArgs 
   __shared__ uint64_t full[kStagesMost], empty[kStagesMost];
   __shared__ RowSide sides[2];
   __shared__ Part of_side[kPrepWarps];
+  __shared__ float top_of_side[kPrepWarps];
   constexpr int E = kPerVec<T>;
   const uint32_t thread = threadIdx.x, lane = thread & 31;
   const float c2 = a.c2;
@@ -891,6 +915,7 @@ __global__ void __launch_bounds__(kStreamBlock, 2) k_distill_stream(DistillArgs 
       float* const logit = prob + padded(a.k);
       float* const said = logit + padded(a.k);
       bool twice = false;
+      float top = -CUDART_INF_F;
       const int end = first.end;
       const float end_z = first.end_z;
       for (uint32_t base = t; base < a.k; base += kRecordsAhead * kPrepLanes) {  // a few records of a thread at once: their loads are far
@@ -915,6 +940,7 @@ __global__ void __launch_bounds__(kStreamBlock, 2) k_distill_stream(DistillArgs 
             if (a.status) set_status(a.status, CVLC_ERR_INVALID_ARG);
           } else if (ids[j] >= 0) {
             p = ids[j] + (int)R.lead;
+            top = fmaxf(top, lps[j]);
             const uint32_t bit = 1u << (p & 31);
             twice |= (atomicOr(reinterpret_cast<uint32_t*>(marks) + (p >> 5), bit) & bit) != 0;
           }
@@ -922,17 +948,24 @@ __global__ void __launch_bounds__(kStreamBlock, 2) k_distill_stream(DistillArgs 
         }
       }
       if (t < padded(a.k) - a.k) at[a.k + t] = -2;
+      if (a.rest == CVLC_REST_SCALED) {
+        top = warp_max(top);
+        if (lane == 0) top_of_side[side] = top;  // (the last row's were read before this row's first barrier)
+      }
       twice = some_or<kPrepLanes>(kBarSide, twice);
+      if (a.rest == CVLC_REST_SCALED)
+        for (int w = 0; w < kPrepWarps; ++w) top = fmaxf(top, top_of_side[w]);
+      const double from = said_from(a.rest, top);
       Part mine = {{-CUDART_INF_F, 0.f}, {-CUDART_INF_F, 0.f}, 0.0, 0.0, 0.0};
       if (twice) {
-        for (uint32_t i = t; i < a.k; i += kPrepLanes) alone[i] = exp_of(said[i]);
+        for (uint32_t i = t; i < a.k; i += kPrepLanes) alone[i] = exp_of((double)said[i] - from);
         some_sync<kPrepLanes>(kBarSide);
       }
       for (uint32_t i = t; i < a.k; i += kPrepLanes) {
-        double p = -1.0, ln_p = 0.0;
+        double p = -1.0, ln_p = (double)said[i] - from;
         if (at[i] >= 0) {
-          if (twice) p = said_by(at, alone, said, a.k, i, &ln_p);
-          else ln_p = (double)said[i], p = exp_of(said[i]);
+          if (twice) p = said_by(at, alone, ln_p, a.k, i, &ln_p);
+          else p = exp_of(ln_p);
           if (KIND != kDistillGrad && !(p < 0.0)) {
             mine.mass += p;
             if (p != 0.0) mine.ent += p * ln_p;

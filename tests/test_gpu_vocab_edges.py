@@ -1,0 +1,68 @@
+"""Rows of logits at the ends of what the definitions allow: lists of any mass, temperatures, values and sizes far apart."""
+import math
+
+import pytest
+import torch
+
+import vocab_ref as R
+from test_gpu_vocab_rows import binding, check_top, logits_of, records, rows_of
+
+pytestmark = pytest.mark.gpu
+DTYPES = [torch.bfloat16, torch.float16, torch.float32]
+FORMS = [(4, 6001), (160, 36007)]  # rows cut over a cluster; more long rows than blocks, which go from row to row
+
+
+def moved_to_one(ids, lp, vocab):
+    """log-probabilities less their row's largest: SCALED stays what it is"""
+    there = (ids >= 0) & (ids < vocab)
+    top = torch.where(there, lp.double(), -math.inf).amax(1, keepdim=True)
+    return torch.where(there, lp.double() - torch.where(top > -math.inf, top, 0.0), -math.inf)
+
+
+def check(B, z, ids, lp, rest, tau, weight, want):
+    """the loss, the gradient behind it and both in one call against loss, gradient and what each may be off by"""
+    loss64, grad64, tol, tol_g = want
+    loss64, grad64 = loss64.float().double(), grad64.float().double()  # what is beyond fp32's range is infinite
+    rows, vocab = z.shape
+    how = dict(rest=rest, temperature=tau, row_weight=weight)
+    loss, stats = torch.full((rows,), 5.0, device="cuda"), torch.zeros(rows, B.DISTILL_STATS, device="cuda")
+    B.cvlc_distill_loss(z, ids, lp, loss, stats, **how)
+    R.assert_near(loss, loss64, tol, what="loss")
+    g, _ = rows_of(torch.zeros(rows, vocab), z.dtype, pad=3, lead=2)
+    B.cvlc_distill_grad(z, ids, lp, stats, g, **how)
+    R.assert_near(g, grad64, tol_g, z.dtype, "grad")
+    loss.fill_(5.0)
+    h = torch.zeros_like(z)
+    B.cvlc_distill_step(z, ids, lp, loss, h, **how)
+    R.assert_near(loss, loss64, tol, what="step loss")
+    R.assert_near(h, grad64, tol_g, z.dtype, "step grad")
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("rows,vocab", FORMS)
+@pytest.mark.parametrize("kind", ["top", "twice", "absent"])
+@pytest.mark.parametrize("by", [-88.0, -95.0, -110.0, -300.0, -800.0, -1e5, 90.0, 900.0])
+def test_scaled_lists_of_any_mass(dtype, rows, vocab, kind, by):
+    """p / P does not change when a list's weight does, whatever a number holds of p and P"""
+    B = binding()
+    z, _ = logits_of(rows, vocab, dtype, seed=vocab, pad=1, lead=1)
+    ids, lp = records(z, 30, 1.5, seed=7, kind=kind)
+    lp += by
+    weight = torch.ones(rows, device="cuda")
+    weight[2] = 0.0
+    check(B, z, ids, lp, R.SCALED, 1.5, weight, R.distill(z, ids, moved_to_one(ids, lp, vocab), R.SCALED, 1.5, weight))
+
+
+@pytest.mark.parametrize("rows,vocab", FORMS)
+def test_scaled_lists_with_a_word_outside(rows, vocab):
+    """what is left out has no part in the list's mass"""
+    B = binding()
+    z, _ = logits_of(rows, vocab, torch.float32, seed=3)
+    ids, lp = records(z, 20, 1.0, seed=7)
+    lp -= 400.0
+    ids[1, 0], lp[1, 0] = vocab, 0.0
+    ids[2, 3], lp[2, 3] = -1, 50.0
+    lp[3] = -math.inf  # no mass: nothing
+    want = R.distill(z, ids, moved_to_one(ids, lp, vocab), R.SCALED, 1.0)
+    assert want[0][3] == 0 and (want[1][3] == 0).all()
+    check(B, z, ids, lp, R.SCALED, 1.0, None, want)
