@@ -304,7 +304,8 @@ __device__ double loss_of(const Sums& s, const Part* parts, uint32_t blocks, uin
 __device__ __host__ __forceinline__ uint32_t padded(uint32_t k) { return (k + 15) & ~15u; }
 __device__ __host__ __forceinline__ size_t records_bytes(uint32_t k) { return (size_t)padded(k) * (8 + 4 * 4); }
 // What record i says of its word, where a word may have several: the sum over its records (`alone`: what each says by itself) in their
-// order, by the first of them; below 0 for the others.  ln_p: its logarithm, `ln_alone` where the word has no other record.
+// order, by the first of them; below 0 for the others, which read nothing but their own (the first may already have put the sum
+// in its place).  ln_p: its logarithm, `ln_alone` where the word has no other record.
 __device__ __forceinline__ double said_by(const int* at, const double* alone, double ln_alone, uint32_t k, uint32_t i, double* ln_p) {
   const int here = at[i];
   double p = alone[i];
@@ -319,13 +320,13 @@ __device__ __forceinline__ double said_by(const int* at, const double* alone, do
               (v.w == here ? 8u : 0u) << (4 * j);
     }
     if (i >= o && i < o + 16) same &= ~(1u << (i - o));
-    for (; same; same &= same - 1) {
+    for (; same && first; same &= same - 1) {  // the lowest first
       const uint32_t other = o + __ffs(same) - 1;
-      first &= other > i;
-      p += alone[other], merged = true;
+      first = other > i;
+      if (first) p += alone[other], merged = true;
     }
   }
-  *ln_p = merged ? ln_of(p) : ln_alone;
+  *ln_p = merged && first ? ln_of(p) : ln_alone;
   return first ? p : -1.0;
 }
 // what all of a row's log-probabilities are taken relative to, their largest being `top`
@@ -339,7 +340,7 @@ struct Records {
   float* prob;    // their probabilities; below 0: counted with an earlier record of the word
   float* logit;   // the student's logits of their words
   float* said;    // the records' log-probabilities
-  double* alone;  // their exponentials
+  double* alone;  // their exponentials; then, for the first record of a word, the word's probability
   double mass, ent;
 
   __device__ __forceinline__ Records(unsigned char* shared, uint32_t k)
@@ -408,11 +409,12 @@ struct Records {
         if (twice) p = said_by(at, alone, ln_p, a.k, i, &ln_p);
         else p = exp_of(ln_p);
         if (SUMS && !(p < 0.0)) {
+          alone[i] = p;
           mass += p;
           if (p != 0.0) ent += p * ln_p;
         }
       }
-      prob[i] = p > 0.0 ? fmaxf((float)p, 1e-45f) : (float)p;  // (above 0 stays so; only this thread reads its own)
+      prob[i] = (float)p;  // (only this thread reads its own)
     }
   }
   // the sums of the warp's records; every lane has them
@@ -427,7 +429,7 @@ struct Records {
     for (uint32_t i = threadIdx.x; i < a.k; i += blockDim.x)
       if (at[i] >= 0 && !(prob[i] < 0.f)) {
         p.said.sum += exp2_fast((logit[i] - ref) * c2);
-        if (prob[i] != 0.f) p.cross += (double)prob[i] * ((double)logit[i] - (double)ref);
+        if (alone[i] != 0.0) p.cross += alone[i] * ((double)logit[i] - (double)ref);  // (the logit may be far enough for any p above 0)
       }
     p.said.sum = warp_sum(p.said.sum), p.cross = warp_sum(p.cross), p.mass = warp_sum(mass), p.ent = warp_sum(ent);
     return p;
@@ -967,12 +969,13 @@ __global__ void __launch_bounds__(kStreamBlock, 2) k_distill_stream(DistillArgs 
           if (twice) p = said_by(at, alone, ln_p, a.k, i, &ln_p);
           else p = exp_of(ln_p);
           if (KIND != kDistillGrad && !(p < 0.0)) {
+            alone[i] = p;
             mine.mass += p;
             if (p != 0.0) mine.ent += p * ln_p;
             mine.said.max = fmaxf(mine.said.max, logit[i]);
           }
         }
-        prob[i] = p > 0.0 ? fmaxf((float)p, 1e-45f) : (float)p;  // (above 0 stays so; only this thread reads its own)
+        prob[i] = (float)p;  // (only this thread reads its own)
       }
       if (KIND != kDistillGrad) {
 #pragma unroll
@@ -981,7 +984,7 @@ __global__ void __launch_bounds__(kStreamBlock, 2) k_distill_stream(DistillArgs 
         for (uint32_t i = t; i < a.k; i += kPrepLanes)
           if (at[i] >= 0 && !(prob[i] < 0.f)) {
             mine.said.sum += exp2_fast((logit[i] - ref) * c2);
-            if (prob[i] != 0.f) mine.cross += (double)prob[i] * ((double)logit[i] - (double)ref);
+            if (alone[i] != 0.0) mine.cross += alone[i] * ((double)logit[i] - (double)ref);
           }
         mine.said.sum = warp_sum(mine.said.sum), mine.mass = warp_sum(mine.mass), mine.ent = warp_sum(mine.ent), mine.cross = warp_sum(mine.cross);
         if (side == 0) {

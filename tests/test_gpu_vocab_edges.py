@@ -66,3 +66,19 @@ def test_scaled_lists_with_a_word_outside(rows, vocab):
     want = R.distill(z, ids, moved_to_one(ids, lp, vocab), R.SCALED, 1.0)
     assert want[0][3] == 0 and (want[1][3] == 0).all()
     check(B, z, ids, lp, R.SCALED, 1.0, None, want)
+
+
+@pytest.mark.parametrize("rest", [R.NONE, R.SCALED, R.BUCKET])
+@pytest.mark.parametrize("rows,vocab", FORMS)
+def test_rare_words_far_from_the_student(rest, rows, vocab):
+    """a probability below fp32's smallest number counts where the word's logit is as far away"""
+    B = binding()
+    tau = 1e-6
+    z, _ = logits_of(rows, vocab, torch.float32, seed=3)
+    z.div_(1e7)
+    ids = torch.arange(1, 9, dtype=torch.int32, device="cuda").repeat(rows, 1) * 37
+    lp = torch.tensor([-1.0, -2.0, -2.5, -90.0, -100.0, -106.0, -110.0, -110.5], device="cuda").repeat(rows, 1)
+    for i in (3, 4, 5, 6, 7):
+        z[i % rows, int(ids[0, i])] = torch.finfo(torch.float32).min
+    weight = torch.full((rows,), tau, device="cuda")
+    check(B, z, ids, lp, rest, tau, weight, R.distill(z, ids, lp, rest, tau, weight))
