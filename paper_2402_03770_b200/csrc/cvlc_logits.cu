@@ -215,7 +215,7 @@ static_assert(sizeof(Whole) <= 4 * CVLC_DISTILL_STATS, "a row's place in the buf
 // e^x to 2^-36 relative, which is far below what the rounding of x to fp32 leaves of it: x = n ln 2 + r, and the Taylor series of e^r
 // (|r| <= 0.35: 0.35^11 / 11! = 2^-42).
 __device__ __forceinline__ double exp_of(double x) {
-  if (!(x > -600.0)) return x == x ? 0.0 : x;
+  if (!(x > -600.0)) return x > -(double)CUDART_INF_F ? fmax(exp(x), 4.9e-324) : x == x ? 0.0 : x;  // of a number it is above 0
   if (x > 600.0) return exp(x);
   const double n = rint(x * 1.4426950408889634074), r = fma(n, -0.693147180559945309417, x);
   double y = 1.0 / 3628800.0;

@@ -82,3 +82,20 @@ def test_rare_words_far_from_the_student(rest, rows, vocab):
         z[i % rows, int(ids[0, i])] = torch.finfo(torch.float32).min
     weight = torch.full((rows,), tau, device="cuda")
     check(B, z, ids, lp, rest, tau, weight, R.distill(z, ids, lp, rest, tau, weight))
+
+
+@pytest.mark.parametrize("rest", [R.NONE, R.SCALED, R.BUCKET])
+@pytest.mark.parametrize("rows,vocab", FORMS)
+def test_a_masked_word_listed_at_any_probability(rest, rows, vocab):
+    """its loss is infinite as long as its log-probability is a number"""
+    B = binding()
+    z, _ = logits_of(rows, vocab, torch.float32, seed=3)
+    ids, lp = records(z, 20, 1.0, seed=1)
+    z.scatter_(1, ids[:, 5:6].long(), -math.inf)
+    lp[0, 5], lp[1, 5], lp[2, 5], lp[3, 5] = -601.0, -740.0, -1e30, -math.inf
+    loss, g = torch.zeros(rows, device="cuda"), torch.zeros_like(z)
+    for call in (lambda: B.cvlc_distill_loss(z, ids, lp, loss, rest=rest), lambda: B.cvlc_distill_step(z, ids, lp, loss, g, rest=rest)):
+        loss.zero_()
+        call()
+        assert (loss[:3] == math.inf).all() and (loss[4:] == math.inf).all() and torch.isfinite(loss[3])
+    assert torch.isfinite(g).all()
