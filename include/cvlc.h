@@ -504,7 +504,8 @@ int cvlc_embed(const void* table_dev, uint32_t dtype, uint64_t vocab, uint32_t d
  * is reported (INVALID_ARG) at byte 0 of the workspace (cvlc_read_status).
  *  grad_dev     n x dim of `dtype`, grad_stride elements apart;  update_dev: vocab x dim fp32, update_stride apart,
  *               not overlapping grad_dev
- *  ws_dev       cvlc_embed_grad_workspace_bytes(n, dim, vocab) bytes, 256-byte aligned
+ *  ws_dev       cvlc_embed_grad_workspace_bytes(n, dim, vocab) bytes, 256-byte aligned; what serves a call serves every one of
+ *               no more tokens, columns and words
  * Errors: INVALID_ARG (as above; vocab up to 2^31 - 1, dim up to 2^20, n up to 2^31 - 1), WORKSPACE_TOO_SMALL.
  */
 size_t cvlc_embed_grad_workspace_bytes(uint64_t n, uint32_t dim, uint64_t vocab);

@@ -116,7 +116,7 @@ __global__ void __launch_bounds__(kLookupThreads, 4) k_embed_wide(EmbedArgs a) {
 
 // ---- the gradient: positions sorted by word ------------------------------------------------------
 //
-// Workspace: [0] status | [256] uint64[n] (word << 32 | position) | uint64[n] | float[chunks][2][dim] pieces of words at a chunk's ends
+// Workspace: [0] status | [256] uint64[n] (word << 32 | position) | uint64[n] | float[chunks_most][2][dim] pieces of words at a chunk's ends
 constexpr int kTokenThreads = 1024;
 constexpr int kTokenWarps = kTokenThreads / 32;
 constexpr int kTokenDigits = 512;
@@ -128,11 +128,16 @@ CVLC_HD inline size_t eg_off_b(uint64_t n) { return align256(eg_off_a() + n * 8)
 CVLC_HD inline size_t eg_off_pieces(uint64_t n) { return align256(eg_off_b(n) + n * 8); }
 
 // Positions of a chunk
-constexpr uint32_t kChunkMost = 512;
+constexpr uint32_t kChunkLeast = 16, kChunkMost = 512, kChunksWanted = 2048;
 uint32_t chunk_of(uint64_t n) {
-  uint64_t c = 16;
-  while (c < kChunkMost && (n + c - 1) / c > 2048) c *= 2;
+  uint64_t c = kChunkLeast;
+  while (c < kChunkMost && (n + c - 1) / c > kChunksWanted) c *= 2;
   return (uint32_t)c;
+}
+// The most chunks that n positions or fewer have: a longer chunk is taken from some number of positions on, and a workspace
+// serves every call that is not larger than the one that it was made for.
+uint64_t chunks_most(uint64_t n) {
+  return std::max(std::min<uint64_t>((n + kChunkLeast - 1) / kChunkLeast, kChunksWanted), (n + kChunkMost - 1) / kChunkMost);
 }
 
 // What the sort's launch does besides, where the table is written out: zeros for the rows of words that do not occur.  The blocks have the
@@ -656,8 +661,7 @@ cudaError_t launch_token_sort(const EmbedGradArgs& a, cudaStream_t st) {
 }  // namespace
 
 size_t embed_grad_ws_bytes(uint64_t n, uint32_t dim) {
-  const uint32_t chunk = chunk_of(n);
-  return align256(eg_off_pieces(n) + (n + chunk - 1) / chunk * 2 * dim * 4);
+  return align256(eg_off_pieces(n) + chunks_most(n) * 2 * dim * 4);
 }
 
 cudaError_t launch_embed(const EmbedArgs& a, uint32_t dtype, cudaStream_t st) {
