@@ -460,7 +460,9 @@ int cvlc_top_logits(const void* logits_dev, uint32_t dtype, uint64_t rows, uint3
  * aligned) from which cvlc_distill_grad makes the gradient, with row weights of its own.  It has to be given the same
  * logits and records.  cvlc_distill_step makes loss and gradient in one reading of the logits.  grad_dev: rows of
  * `dtype`, grad_stride elements apart; it may be logits_dev itself (with the same stride), and must not overlap it otherwise.
- * Results do not depend on the order in which blocks run.
+ * Results do not depend on the order in which blocks run.  Waits inside the kernels are bounded (four seconds, for copies that take microseconds):
+ * should one run out, CVLC_ERR_DEVICE_TIMEOUT goes to *status_dev and the rows that were not finished hold NaN (in
+ * cvlc_top_logits: the records of a row without a softmax).
  * Errors: as cvlc_top_logits; k from 0 to CVLC_MAX_RECORDS.
  */
 #define CVLC_REST_NONE 0u
@@ -533,6 +535,13 @@ int cvlc_selftest_math(const double* in_dev, uint64_t n, double* log2_out_dev, d
  * published yet") with a limit of max_polls (1 .. 2^20): when the wait runs out the kernel writes
  * CVLC_ERR_DEVICE_TIMEOUT to *status_dev (if that still holds 0) and returns.  Nothing hangs. */
 int cvlc_selftest_wait(uint64_t* word_dev, int32_t* status_dev, uint32_t max_polls, void* cuda_stream);
+
+/* The ring of two stages of 4096 floats through which rows of logits are copied, run on one row of `stages` (1 .. 256) stages with a limit of
+ * limit_us (up to a second) for every wait.  give_back = 1: every stage is given back when it has come.  0: none is: the copies
+ * stop behind the second stage, the wait for a free one runs out, CVLC_ERR_DEVICE_TIMEOUT goes to *status_dev (if that
+ * still holds 0) and the kernel returns.  seen_dev: the 8192 floats that the ring holds at the end.  Nothing hangs. */
+int cvlc_selftest_ring(const float* row_dev, uint32_t stages, int give_back, uint32_t limit_us, int32_t* status_dev, float* seen_dev,
+                       void* cuda_stream);
 
 /* Launch accounting: number of kernels this library has launched in this process
  * (all kernels when kernel_name is NULL or "", else the named one, e.g. "k_hist").  Kernel names: k_zero_words,

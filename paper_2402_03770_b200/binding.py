@@ -54,7 +54,7 @@ EXPORTS = [
     "cvlc_plan", "cvlc_plan_fixed", "cvlc_encode", "cvlc_plan_batch_workspace_bytes",
     "cvlc_encode_batch_workspace_bytes", "cvlc_plan_batch", "cvlc_encode_batch", "cvlc_decode_aggregate", "cvlc_read_status",
     "cvlc_selftest_philox", "cvlc_selftest_math", "cvlc_histogram_batch", "cvlc_plan_from_histogram_batch", "cvlc_decode_apply",
-    "cvlc_decode_aggregate_noalloc", "cvlc_compress_batch", "cvlc_selftest_wait", "cvlc_plan_literal",
+    "cvlc_decode_aggregate_noalloc", "cvlc_compress_batch", "cvlc_selftest_wait", "cvlc_selftest_ring", "cvlc_plan_literal",
     "cvlc_plan_literal_workspace_bytes", "cvlc_ec_accumulate_batch", "cvlc_encode_batch_ec",
     "cvlc_unframed_stream_capacity", "cvlc_unframed_workspace_bytes", "cvlc_encode_unframed_batch", "cvlc_decode_aggregate_unframed",
     "cvlc_top_logits", "cvlc_distill_loss", "cvlc_distill_grad", "cvlc_distill_step", "cvlc_embed", "cvlc_embed_grad_workspace_bytes",
@@ -165,6 +165,8 @@ def lib() -> C.CDLL:
     L.cvlc_decode_aggregate_unframed.argtypes = [vp, vp, vp, u32, f64, u64, vp, C.c_int, vp, sz, vp]
     L.cvlc_selftest_wait.restype = C.c_int
     L.cvlc_selftest_wait.argtypes = [vp, vp, u32, vp]
+    L.cvlc_selftest_ring.restype = C.c_int
+    L.cvlc_selftest_ring.argtypes = [vp, u32, C.c_int, u32, vp, vp, vp]
     L.cvlc_decode_aggregate.restype = C.c_int
     L.cvlc_decode_aggregate.argtypes = [vp, vp, vp, u32, f64, u64, vp, C.c_int, vp, sz, vp]
     L.cvlc_histogram_batch.restype = C.c_int
@@ -451,6 +453,13 @@ def cvlc_selftest_wait(word: torch.Tensor, status: torch.Tensor, max_polls: int,
                        stream: Optional[torch.cuda.Stream] = None) -> None:
     assert word.element_size() == 8 and status.dtype == torch.int32
     _check(lib().cvlc_selftest_wait(_ptr(word), _ptr(status), int(max_polls), _stream_handle(stream)), "cvlc_selftest_wait")
+
+
+def cvlc_selftest_ring(row: torch.Tensor, give_back: bool, limit_us: int, status: torch.Tensor, seen: torch.Tensor,
+                       stream: Optional[torch.cuda.Stream] = None) -> None:
+    assert row.dtype == seen.dtype == torch.float32 and status.dtype == torch.int32 and row.numel() % 4096 == 0 and seen.numel() >= 8192
+    _check(lib().cvlc_selftest_ring(_ptr(row), row.numel() // 4096, 1 if give_back else 0, int(limit_us), _ptr(status), _ptr(seen),
+                                    _stream_handle(stream)), "cvlc_selftest_ring")
 
 
 def cvlc_decode_aggregate(stream_ptrs: torch.Tensor, stream_bytes: torch.Tensor, weights: torch.Tensor,

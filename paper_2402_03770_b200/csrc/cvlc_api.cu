@@ -737,6 +737,16 @@ int cvlc_selftest_wait(uint64_t* word_dev, int32_t* status_dev, uint32_t max_pol
              : CVLC_ERR_CUDA;
 }
 
+int cvlc_selftest_ring(const float* row_dev, uint32_t stages, int give_back, uint32_t limit_us, int32_t* status_dev, float* seen_dev,
+                       void* cuda_stream) {
+  if (!aligned(row_dev, 16) || !aligned(seen_dev, 16) || !aligned(status_dev, 4) || stages < 1 || stages > 256 || limit_us > 1000000u)
+    return CVLC_ERR_INVALID_ARG;
+  return launch_selftest_ring(row_dev, stages, give_back, (uint64_t)limit_us * 1000, status_dev, seen_dev, static_cast<cudaStream_t>(cuda_stream)) ==
+                 cudaSuccess
+             ? CVLC_OK
+             : CVLC_ERR_CUDA;
+}
+
 int cvlc_selftest_philox(uint64_t seed, uint32_t client_id, uint32_t round, uint64_t first, uint64_t n, uint32_t* out_dev,
                          void* cuda_stream) {
   if (!aligned(out_dev, 4)) return CVLC_ERR_INVALID_ARG;

@@ -678,21 +678,37 @@ __device__ __forceinline__ uint64_t nanoseconds() {
   asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
   return t;
 }
-// Bounded: a wait of four seconds clears `ok`, and later ones try once.
-__device__ __forceinline__ void bar_wait(uint64_t* b, uint32_t parity, bool& ok) {
-  if (bar_try(b, parity)) return;
+// What a block's waits share.  They are bounded: one that runs out sets `gone` and reports it, and then no role of the block waits for
+// another any more, nothing further is copied and no stage is given back, so that a stage that may still be read is never written.  The
+// rows that are not finished then are void.
+constexpr uint64_t kWaitMost = 4000000000ull;  // nanoseconds
+constexpr uint32_t kLateTries = 256;           // behind that: the time also runs while the block does not (another process has the GPU)
+struct Waits {
+  uint32_t* gone;   // in shared memory, 0 at first
+  int32_t* status;  // or nullptr
+  uint64_t most;
+  __device__ __forceinline__ bool over() const { return *static_cast<volatile uint32_t*>(gone) != 0; }
+};
+// true: the phase is complete
+__device__ __forceinline__ bool bar_wait(uint64_t* b, uint32_t parity, const Waits& w) {
+  if (bar_try(b, parity)) return true;
   const uint64_t began = nanoseconds();
-  while (ok) {
-    if (bar_try(b, parity)) return;
-    if (nanoseconds() - began > 4000000000ull) ok = false;
+  for (uint32_t late = 0; !w.over();) {
+    if (bar_try(b, parity)) return true;
+    if (nanoseconds() - began > w.most && ++late > kLateTries) {
+      *static_cast<volatile uint32_t*>(w.gone) = 1;
+      if (w.status) set_status(w.status, CVLC_ERR_DEVICE_TIMEOUT);
+    }
   }
+  return false;
 }
 // A warp has read its part of a stage.  The copy that fills the stage next writes it by another path than the loads take: the loads
-// have to be over before the copying thread hears of it, and the arrival alone does not see to that.
-__device__ __forceinline__ void release_stage(uint64_t* b) {
+// have to be over before the copying thread hears of it, and the arrival alone does not see to that.  `ok`: none of the thread's waits has run
+// out; those of a warp may differ in that, so all meet.
+__device__ __forceinline__ void release_stage(uint64_t* b, bool ok) {
   asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   __syncwarp();
-  if ((threadIdx.x & 31) == 0) bar_arrive(b);
+  if ((threadIdx.x & 31) == 0 && ok) bar_arrive(b);
 }
 // named barriers among some of a block's warps
 template <int N>
@@ -719,23 +735,24 @@ __device__ __forceinline__ uint32_t copied_again(uint32_t wholes, uint32_t stage
   return cuts > stages ? (cuts - stages) * kStageVecs : 0;
 }
 // The copying thread: the whole vectors of the block's rows through the ring; with two passes all but what the ring still holds of the row a
-// second time.  False: a wait has run out.  The last reading of a row leaves nothing in the L2 cache.
+// second time.  The last reading of a row leaves nothing in the L2 cache.
 template <class T, int PASSES, class F>
-__device__ bool copy_rows(const DistillArgs& a, uint64_t rows, uint4* ring, uint32_t stages, uint64_t* full, uint64_t* empty, F&& skip) {
+__device__ void copy_rows(const DistillArgs& a, uint64_t rows, uint4* ring, uint32_t stages, uint64_t* full, uint64_t* empty, const Waits& waits, F&& skip) {
   uint64_t once;
   asm("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(once));
   uint32_t stage = 0, phase = 0;
   bool ok = true, skip_next = skip(blockIdx.x);
-  for (uint64_t row = blockIdx.x; row < rows; row += gridDim.x) {
+  for (uint64_t row = blockIdx.x; ok && row < rows; row += gridDim.x) {
     const bool skipped = skip_next;
     skip_next = skip(row + gridDim.x);  // known before it is needed
     if (skipped) continue;
     const RowAt R = row_at<T>(a, row);
-    for (int pass = 0; pass < PASSES; ++pass) {
+    for (int pass = 0; ok && pass < PASSES; ++pass) {
       const uint32_t to_copy = pass == 0 ? R.wholes : copied_again(R.wholes, stages);
       const bool once_more = pass + 1 < PASSES;
       for (uint32_t v = 0; v < to_copy; v += kStageVecs) {
-        bar_wait(&empty[stage], phase ^ 1, ok);
+        ok = bar_wait(&empty[stage], phase ^ 1, waits);
+        if (!ok) break;
         const uint32_t bytes = min(R.wholes - v, (uint32_t)kStageVecs) * 16;
         bar_expect(&full[stage], bytes);
         const unsigned char* const src = R.from + ((size_t)R.whole_from + v) * 16;
@@ -751,12 +768,19 @@ __device__ bool copy_rows(const DistillArgs& a, uint64_t rows, uint4* ring, uint
       }
     }
   }
-  bool last = true;  // no copy is left on its way, even where a wait has run out
-  for (uint32_t i = 0; i < stages; ++i) {
-    bar_wait(&empty[stage], phase ^ 1, last);
+  // no copy is left on its way: all stages have been given back, or, where that is not waited for any more, have been filled
+  const uint32_t next = stage, next_phase = phase;
+  for (uint32_t i = 0; ok && i < stages; ++i) {
+    ok = bar_wait(&empty[stage], phase ^ 1, waits);
     if (++stage == stages) stage = 0, phase ^= 1;
   }
-  return ok && last;
+  if (ok) return;
+  uint32_t alone = 0;
+  stage = next, phase = next_phase;
+  for (uint32_t i = 0; i < stages; ++i) {  // (of a stage that has never been filled the phase before the first is complete)
+    (void)bar_wait(&full[stage], phase ^ 1, Waits{&alone, nullptr, waits.most});
+    if (++stage == stages) stage = 0, phase ^= 1;
+  }
 }
 // word of a row's i-th element beside its whole vectors (E of the first vector, then E of the last one), or -1
 template <int E>
@@ -786,10 +810,10 @@ __device__ __forceinline__ void read_stage(const uint4* ring, uint32_t stage, ui
 // ... of the next stage of the ring, which is then given back, unless it is to be read once more
 template <class T>
 __device__ __forceinline__ void take_stage(const uint4* ring, uint32_t& stage, uint32_t& phase, uint32_t stages, uint64_t* full, uint64_t* empty,
-                                           uint32_t v, uint32_t wholes, bool& ok, uint4 (&raw)[kStageShare], bool keep = false) {
-  bar_wait(&full[stage], phase, ok);
+                                           uint32_t v, uint32_t wholes, const Waits& waits, bool& ok, uint4 (&raw)[kStageShare], bool keep = false) {
+  if (ok) ok = bar_wait(&full[stage], phase, waits);
   read_stage<T>(ring, stage, v, wholes, raw);
-  if (!keep) release_stage(&empty[stage]);
+  if (!keep) release_stage(&empty[stage], ok);
   if (++stage == stages) stage = 0, phase ^= 1;
 }
 // add_batch() of vectors whose largest element is known; the sum moves only when the maximum does
@@ -859,6 +883,7 @@ __global__ void __launch_bounds__(kStreamBlock, 2) k_distill_stream(DistillArgs 
   __shared__ RowSide sides[2];
   __shared__ Part of_side[kPrepWarps];
   __shared__ float top_of_side[kPrepWarps];
+  __shared__ uint32_t gone;
   constexpr int E = kPerVec<T>;
   const uint32_t thread = threadIdx.x, lane = thread & 31;
   const float c2 = a.c2;
@@ -869,8 +894,10 @@ __global__ void __launch_bounds__(kStreamBlock, 2) k_distill_stream(DistillArgs 
   };
   const auto weight_of = [&](uint64_t row) { return !a.row_weight ? 1.f : row < a.rows ? a.row_weight[row] : 0.f; };
   const bool all_rows = KIND == kDistillLoss && a.stats;  // a later gradient may ask for rows that count for nothing
+  const Waits waits = {&gone, a.status, kWaitMost};
 
   if (thread == 0) {
+    gone = 0;
     for (uint32_t i = 0; i < stages; ++i) bar_init(&full[i], 1), bar_init(&empty[i], kStreamWarps);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -879,8 +906,8 @@ __global__ void __launch_bounds__(kStreamBlock, 2) k_distill_stream(DistillArgs 
 
   bool ok = true;
   if (thread >= kSideLanes && thread < kStreamFirst) {
-    if (lane == 0 && !copy_rows<T, KIND == kDistillStep ? 2 : 1>(a, a.rows, ring, stages, full, empty, [&](uint64_t row) { return !all_rows && weight_of(row) == 0.f; }) && a.status)
-      set_status(a.status, CVLC_ERR_DEVICE_TIMEOUT);
+    if (lane == 0)
+      copy_rows<T, KIND == kDistillStep ? 2 : 1>(a, a.rows, ring, stages, full, empty, waits, [&](uint64_t row) { return !all_rows && weight_of(row) == 0.f; });
     return;
   }
 
@@ -1032,6 +1059,7 @@ __global__ void __launch_bounds__(kStreamBlock, 2) k_distill_stream(DistillArgs 
       T* const g = static_cast<T*>(a.grad) + row * a.grad_stride;
       const float scale = weight / a.temperature;
       if (KIND != kDistillLoss) {
+        if (waits.over()) w.a = w.b = CUDART_NAN_F;
         const int end = end_of(R);
         if (end >= 0 && !(marks[(end + R.lead) >> 3] >> ((end + R.lead) & 7) & 1)) {
           const float z = to_float((reinterpret_cast<const T*>(R.from) + R.lead)[end]);
@@ -1080,6 +1108,7 @@ __global__ void __launch_bounds__(kStreamBlock, 2) k_distill_stream(DistillArgs 
               loss += l * (ln_of(l) - (((double)rest.max - (double)all.max) * it + ln_of((double)rest.sum) - ln_sum));
             }
           }
+          if (waits.over()) loss = CUDART_NAN;
           a.loss[row] = weight == 0.f ? 0.f : (float)((double)weight * loss);
           if (KIND == kDistillLoss && a.stats) *reinterpret_cast<Whole*>(a.stats + row * CVLC_DISTILL_STATS) = w;
         }
@@ -1130,7 +1159,7 @@ __global__ void __launch_bounds__(kStreamBlock, 2) k_distill_stream(DistillArgs 
       MaxSum acc = {-CUDART_INF_F, 0.f};
       for (uint32_t v = 0; v < R.wholes; v += kStageVecs) {
         uint4 raw[kStageShare];
-        take_stage<T>(ring, stage, phase, stages, full, empty, v, R.wholes, ok, raw, KIND == kDistillStep && v >= again);
+        take_stage<T>(ring, stage, phase, stages, full, empty, v, R.wholes, waits, ok, raw, KIND == kDistillStep && v >= again);
         uint32_t bits[kStageShare];
         const uint32_t i = R.whole_from + v + tid;
 #pragma unroll
@@ -1176,11 +1205,11 @@ __global__ void __launch_bounds__(kStreamBlock, 2) k_distill_stream(DistillArgs 
       if (KIND == kDistillStep && cut < kept) {
         v = again + cut * kStageVecs;
         read_stage<T>(ring, held, v, R.wholes, raw);
-        release_stage(&empty[held]);
+        release_stage(&empty[held], ok);
         if (++held == stages) held = 0;
       } else {
         v = (KIND == kDistillStep ? cut - kept : cut) * kStageVecs;
-        take_stage<T>(ring, stage, phase, stages, full, empty, v, R.wholes, ok, raw);
+        take_stage<T>(ring, stage, phase, stages, full, empty, v, R.wholes, waits, ok, raw);
       }
       if (!ok) ca = CUDART_NAN_F;
 #pragma unroll
@@ -1665,7 +1694,7 @@ __global__ void __launch_bounds__(kStreamBlock, 2) k_top_stream(TopArgs a, uint3
   __shared__ uint32_t hist[256];
   static_assert(kStreamLanes == 256, "a bin for each thread");
   __shared__ uint32_t side_hist[256], side_picked, side_above;
-  __shared__ uint32_t mine, picked, above, largest, smallest, kept;
+  __shared__ uint32_t mine, picked, above, largest, smallest, kept, gone;
   constexpr int E = kPerVec<T>;
   const uint32_t thread = threadIdx.x, lane = thread & 31;
   const float c2 = a.c2;
@@ -1673,16 +1702,17 @@ __global__ void __launch_bounds__(kStreamBlock, 2) k_top_stream(TopArgs a, uint3
   unsigned long long* const lists = reinterpret_cast<unsigned long long*>(dyn + (size_t)stages * kStageVecs * 16);  // [2], then the ranking's
   DistillArgs where = {};
   where.logits = a.logits, where.row_stride = a.row_stride, where.vocab = a.vocab;
+  const Waits waits = {&gone, nullptr, kWaitMost};
 
   if (thread == 0) {
     for (uint32_t i = 0; i < stages; ++i) bar_init(&full[i], 1), bar_init(&empty[i], kStreamWarps);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-    mine = kept = 0;
+    mine = kept = gone = 0;
   }
   __syncthreads();
   bool ok = true;
   if (thread >= kSideLanes && thread < kStreamFirst) {
-    if (lane == 0) copy_rows<T, 1>(where, a.rows, ring, stages, full, empty, [](uint64_t) { return false; });
+    if (lane == 0) copy_rows<T, 1>(where, a.rows, ring, stages, full, empty, waits, [](uint64_t) { return false; });
     return;
   }
   if (thread < kSideLanes) {
@@ -1801,7 +1831,7 @@ __global__ void __launch_bounds__(kStreamBlock, 2) k_top_stream(TopArgs a, uint3
     };
     for (uint32_t b = 0; b < cuts; ++b) {
       uint4 raw[kStageShare];
-      take_stage<T>(ring, stage, phase, stages, full, empty, b * kStageVecs, R.wholes, ok, raw);
+      take_stage<T>(ring, stage, phase, stages, full, empty, b * kStageVecs, R.wholes, waits, ok, raw);
       float largest_of[kStageShare];
 #pragma unroll
       for (int j = 0; j < kStageShare; ++j) largest_of[j] = vec_max<T>(raw[j]), top[j & 1] = fmaxf(top[j & 1], largest_of[j]);
@@ -1888,6 +1918,34 @@ __global__ void __launch_bounds__(kStreamBlock, 2) k_top_stream(TopArgs a, uint3
   }
 }
 
+// The ring alone, one block: `give_back`: a thread takes the row's stages and gives them back; else none is given back, and the copies stop
+// when the wait for one has run out.  seen: what the stages hold then.
+constexpr uint32_t kSelftestStages = 2;
+__global__ void k_selftest_ring(DistillArgs a, int32_t* status, uint64_t most, int give_back, uint4* seen) {
+  extern __shared__ __align__(128) unsigned char dyn[];
+  __shared__ uint64_t full[kSelftestStages], empty[kSelftestStages];
+  __shared__ uint32_t gone;
+  uint4* const ring = reinterpret_cast<uint4*>(dyn);
+  const Waits waits = {&gone, status, most};
+  if (threadIdx.x == 0) {
+    gone = 0;
+    for (uint32_t i = 0; i < kSelftestStages; ++i) bar_init(&full[i], 1), bar_init(&empty[i], 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  __syncthreads();
+  if (threadIdx.x == 0) copy_rows<float, 1>(a, 1, ring, kSelftestStages, full, empty, waits, [](uint64_t) { return false; });
+  if (threadIdx.x >= 32 && threadIdx.x < 64) {
+    const uint32_t cuts = a.vocab / (kStageVecs * kPerVec<float>);
+    bool ok = true;
+    for (uint32_t c = 0; c < cuts; ++c) {
+      if (ok) ok = bar_wait(&full[c % kSelftestStages], c / kSelftestStages & 1, waits);
+      release_stage(&empty[c % kSelftestStages], ok && give_back);
+    }
+  }
+  __syncthreads();
+  for (uint32_t i = threadIdx.x; i < kSelftestStages * kStageVecs; i += blockDim.x) seen[i] = ring[i];
+}
+
 template <class T>
 cudaError_t top_typed(const TopArgs& a, cudaStream_t st) {
   if (streamed(a.rows, (uint64_t)a.vocab * sizeof(T))) {
@@ -1914,6 +1972,14 @@ cudaError_t top_typed(const TopArgs& a, cudaStream_t st) {
 }
 
 }  // namespace
+
+cudaError_t launch_selftest_ring(const float* row, uint32_t cuts, int give_back, uint64_t most, int32_t* status, float* seen, cudaStream_t st) {
+  DistillArgs a = {};
+  a.logits = row, a.rows = 1, a.vocab = cuts * kStageVecs * kPerVec<float>, a.row_stride = a.vocab;
+  LaunchScope ls(kKSelftest, st);
+  k_selftest_ring<<<1, 64, kSelftestStages * kStageVecs * 16, st>>>(a, status, most, give_back, reinterpret_cast<uint4*>(seen));
+  return cudaGetLastError();
+}
 
 cudaError_t launch_top_logits(const TopArgs& args, uint32_t dtype, cudaStream_t st) {
   TopArgs a = args;

@@ -43,6 +43,7 @@ struct DistillArgs {
 };
 enum DistillKind { kDistillLoss, kDistillGrad, kDistillStep };
 cudaError_t launch_distill(const DistillArgs& a, uint32_t dtype, DistillKind kind, cudaStream_t st);
+cudaError_t launch_selftest_ring(const float* row, uint32_t cuts, int give_back, uint64_t most, int32_t* status, float* seen, cudaStream_t st);
 
 struct EmbedArgs {
   const void* table;
