@@ -678,37 +678,57 @@ __device__ __forceinline__ uint64_t nanoseconds() {
   asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
   return t;
 }
-// What a block's waits share.  They are bounded: one that runs out sets `gone` and reports it, and then no role of the block waits for
-// another any more, nothing further is copied and no stage is given back, so that a stage that may still be read is never written.  The
-// rows that are not finished then are void.
+// What a block's waits share.  They are bounded.  When one has run out, the copying thread stops, by its own wait or because it is told, and
+// who has waited for a copy goes on only then, without waiting any more: so a stage that may still be read is never written, whoever
+// gives it back.  The rows that are not finished are void.
 constexpr uint64_t kWaitMost = 4000000000ull;  // nanoseconds
-constexpr uint32_t kLateTries = 256;           // behind that: the time also runs while the block does not (another process has the GPU)
+constexpr int kLateTries = 256;                // behind that: the time also runs while the block does not (another process has the GPU)
 struct Waits {
-  uint32_t* gone;   // in shared memory, 0 at first
-  int32_t* status;  // or nullptr
+  uint32_t *gone, *stopped;  // in shared memory, 0 at first: a wait has run out; nothing will be copied any more
+  int32_t* status;           // or nullptr
   uint64_t most;
   __device__ __forceinline__ bool over() const { return *static_cast<volatile uint32_t*>(gone) != 0; }
+  __device__ __forceinline__ void stop() const { *static_cast<volatile uint32_t*>(stopped) = 1; }
 };
-// true: the phase is complete
-__device__ __forceinline__ bool bar_wait(uint64_t* b, uint32_t parity, const Waits& w) {
+// The time is over; false: the wait has run out
+__device__ __forceinline__ bool wait_late(uint64_t* b, uint32_t parity, Waits w, bool copies) {
+  for (int i = 0; i < kLateTries; ++i)
+    if (bar_try(b, parity)) return true;
+  *static_cast<volatile uint32_t*>(w.gone) = 1;
+  if (w.status) set_status(w.status, CVLC_ERR_DEVICE_TIMEOUT);
+  const uint64_t began = nanoseconds();
+  while (!copies && !*static_cast<volatile uint32_t*>(w.stopped) && nanoseconds() - began < 2 * w.most) {
+  }
+  return false;
+}
+// Clears `ok` when it runs out; later ones try once.
+__device__ __forceinline__ void bar_wait(uint64_t* b, uint32_t parity, const Waits& w, bool& ok) {
+  if (bar_try(b, parity)) return;
+  const uint64_t began = nanoseconds();
+  while (ok) {
+    if (bar_try(b, parity)) return;
+    if (nanoseconds() - began > w.most) {
+      ok = wait_late(b, parity, w, false);
+      return;
+    }
+  }
+}
+// ... of the copying thread, which also stops when another's has
+__device__ __forceinline__ bool copy_wait(uint64_t* b, uint32_t parity, const Waits& w) {
   if (bar_try(b, parity)) return true;
   const uint64_t began = nanoseconds();
-  for (uint32_t late = 0; !w.over();) {
+  while (!w.over()) {
     if (bar_try(b, parity)) return true;
-    if (nanoseconds() - began > w.most && ++late > kLateTries) {
-      *static_cast<volatile uint32_t*>(w.gone) = 1;
-      if (w.status) set_status(w.status, CVLC_ERR_DEVICE_TIMEOUT);
-    }
+    if (nanoseconds() - began > w.most) return wait_late(b, parity, w, true);
   }
   return false;
 }
 // A warp has read its part of a stage.  The copy that fills the stage next writes it by another path than the loads take: the loads
-// have to be over before the copying thread hears of it, and the arrival alone does not see to that.  `ok`: none of the thread's waits has run
-// out; those of a warp may differ in that, so all meet.
-__device__ __forceinline__ void release_stage(uint64_t* b, bool ok) {
+// have to be over before the copying thread hears of it, and the arrival alone does not see to that.
+__device__ __forceinline__ void release_stage(uint64_t* b) {
   asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   __syncwarp();
-  if ((threadIdx.x & 31) == 0 && ok) bar_arrive(b);
+  if ((threadIdx.x & 31) == 0) bar_arrive(b);
 }
 // named barriers among some of a block's warps
 template <int N>
@@ -751,7 +771,7 @@ __device__ void copy_rows(const DistillArgs& a, uint64_t rows, uint4* ring, uint
       const uint32_t to_copy = pass == 0 ? R.wholes : copied_again(R.wholes, stages);
       const bool once_more = pass + 1 < PASSES;
       for (uint32_t v = 0; v < to_copy; v += kStageVecs) {
-        ok = bar_wait(&empty[stage], phase ^ 1, waits);
+        ok = copy_wait(&empty[stage], phase ^ 1, waits);
         if (!ok) break;
         const uint32_t bytes = min(R.wholes - v, (uint32_t)kStageVecs) * 16;
         bar_expect(&full[stage], bytes);
@@ -768,17 +788,18 @@ __device__ void copy_rows(const DistillArgs& a, uint64_t rows, uint4* ring, uint
       }
     }
   }
-  // no copy is left on its way: all stages have been given back, or, where that is not waited for any more, have been filled
+  // no copy is left on its way: all stages have been given back, or, where a wait has run out, have been filled
   const uint32_t next = stage, next_phase = phase;
   for (uint32_t i = 0; ok && i < stages; ++i) {
-    ok = bar_wait(&empty[stage], phase ^ 1, waits);
+    ok = copy_wait(&empty[stage], phase ^ 1, waits);
     if (++stage == stages) stage = 0, phase ^= 1;
   }
   if (ok) return;
+  waits.stop();
   uint32_t alone = 0;
   stage = next, phase = next_phase;
   for (uint32_t i = 0; i < stages; ++i) {  // (of a stage that has never been filled the phase before the first is complete)
-    (void)bar_wait(&full[stage], phase ^ 1, Waits{&alone, nullptr, waits.most});
+    (void)copy_wait(&full[stage], phase ^ 1, Waits{&alone, nullptr, nullptr, waits.most});
     if (++stage == stages) stage = 0, phase ^= 1;
   }
 }
@@ -811,9 +832,9 @@ __device__ __forceinline__ void read_stage(const uint4* ring, uint32_t stage, ui
 template <class T>
 __device__ __forceinline__ void take_stage(const uint4* ring, uint32_t& stage, uint32_t& phase, uint32_t stages, uint64_t* full, uint64_t* empty,
                                            uint32_t v, uint32_t wholes, const Waits& waits, bool& ok, uint4 (&raw)[kStageShare], bool keep = false) {
-  if (ok) ok = bar_wait(&full[stage], phase, waits);
+  bar_wait(&full[stage], phase, waits, ok);
   read_stage<T>(ring, stage, v, wholes, raw);
-  if (!keep) release_stage(&empty[stage], ok);
+  if (!keep) release_stage(&empty[stage]);
   if (++stage == stages) stage = 0, phase ^= 1;
 }
 // add_batch() of vectors whose largest element is known; the sum moves only when the maximum does
@@ -883,7 +904,7 @@ __global__ void __launch_bounds__(kStreamBlock, 2) k_distill_stream(DistillArgs 
   __shared__ RowSide sides[2];
   __shared__ Part of_side[kPrepWarps];
   __shared__ float top_of_side[kPrepWarps];
-  __shared__ uint32_t gone;
+  __shared__ uint32_t gone, stopped;
   constexpr int E = kPerVec<T>;
   const uint32_t thread = threadIdx.x, lane = thread & 31;
   const float c2 = a.c2;
@@ -894,10 +915,10 @@ __global__ void __launch_bounds__(kStreamBlock, 2) k_distill_stream(DistillArgs 
   };
   const auto weight_of = [&](uint64_t row) { return !a.row_weight ? 1.f : row < a.rows ? a.row_weight[row] : 0.f; };
   const bool all_rows = KIND == kDistillLoss && a.stats;  // a later gradient may ask for rows that count for nothing
-  const Waits waits = {&gone, a.status, kWaitMost};
+  const Waits waits = {&gone, &stopped, a.status, kWaitMost};
 
   if (thread == 0) {
-    gone = 0;
+    gone = stopped = 0;
     for (uint32_t i = 0; i < stages; ++i) bar_init(&full[i], 1), bar_init(&empty[i], kStreamWarps);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -1205,7 +1226,7 @@ __global__ void __launch_bounds__(kStreamBlock, 2) k_distill_stream(DistillArgs 
       if (KIND == kDistillStep && cut < kept) {
         v = again + cut * kStageVecs;
         read_stage<T>(ring, held, v, R.wholes, raw);
-        release_stage(&empty[held], ok);
+        release_stage(&empty[held]);
         if (++held == stages) held = 0;
       } else {
         v = (KIND == kDistillStep ? cut - kept : cut) * kStageVecs;
@@ -1694,7 +1715,7 @@ __global__ void __launch_bounds__(kStreamBlock, 2) k_top_stream(TopArgs a, uint3
   __shared__ uint32_t hist[256];
   static_assert(kStreamLanes == 256, "a bin for each thread");
   __shared__ uint32_t side_hist[256], side_picked, side_above;
-  __shared__ uint32_t mine, picked, above, largest, smallest, kept, gone;
+  __shared__ uint32_t mine, picked, above, largest, smallest, kept, gone, stopped;
   constexpr int E = kPerVec<T>;
   const uint32_t thread = threadIdx.x, lane = thread & 31;
   const float c2 = a.c2;
@@ -1702,12 +1723,12 @@ __global__ void __launch_bounds__(kStreamBlock, 2) k_top_stream(TopArgs a, uint3
   unsigned long long* const lists = reinterpret_cast<unsigned long long*>(dyn + (size_t)stages * kStageVecs * 16);  // [2], then the ranking's
   DistillArgs where = {};
   where.logits = a.logits, where.row_stride = a.row_stride, where.vocab = a.vocab;
-  const Waits waits = {&gone, nullptr, kWaitMost};
+  const Waits waits = {&gone, &stopped, nullptr, kWaitMost};
 
   if (thread == 0) {
     for (uint32_t i = 0; i < stages; ++i) bar_init(&full[i], 1), bar_init(&empty[i], kStreamWarps);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-    mine = kept = gone = 0;
+    mine = kept = gone = stopped = 0;
   }
   __syncthreads();
   bool ok = true;
@@ -1924,11 +1945,11 @@ constexpr uint32_t kSelftestStages = 2;
 __global__ void k_selftest_ring(DistillArgs a, int32_t* status, uint64_t most, int give_back, uint4* seen) {
   extern __shared__ __align__(128) unsigned char dyn[];
   __shared__ uint64_t full[kSelftestStages], empty[kSelftestStages];
-  __shared__ uint32_t gone;
+  __shared__ uint32_t gone, stopped;
   uint4* const ring = reinterpret_cast<uint4*>(dyn);
-  const Waits waits = {&gone, status, most};
+  const Waits waits = {&gone, &stopped, status, most};
   if (threadIdx.x == 0) {
-    gone = 0;
+    gone = stopped = 0;
     for (uint32_t i = 0; i < kSelftestStages; ++i) bar_init(&full[i], 1), bar_init(&empty[i], 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -1938,8 +1959,8 @@ __global__ void k_selftest_ring(DistillArgs a, int32_t* status, uint64_t most, i
     const uint32_t cuts = a.vocab / (kStageVecs * kPerVec<float>);
     bool ok = true;
     for (uint32_t c = 0; c < cuts; ++c) {
-      if (ok) ok = bar_wait(&full[c % kSelftestStages], c / kSelftestStages & 1, waits);
-      release_stage(&empty[c % kSelftestStages], ok && give_back);
+      bar_wait(&full[c % kSelftestStages], c / kSelftestStages & 1, waits, ok);
+      if (give_back) release_stage(&empty[c % kSelftestStages]);
     }
   }
   __syncthreads();
