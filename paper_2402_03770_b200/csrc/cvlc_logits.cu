@@ -163,14 +163,16 @@ __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.w
 
 // The differences z - max are taken before the scaling by log2(e) / temperature: with rows masked by the type's lowest value, or far
 // from zero, the product alone would overflow or lose the difference.
+// A batch has a sum of its own, which is added to those before it with what the addition rounds off kept in `low`: a thread has up to 64
+// batches, and equal terms round the same way (one running sum over rows of 2^22 words was off by up to 470 half steps of fp32).
 template <class T, int NV>
-__device__ __forceinline__ void add_batch(const uint4 (&raw)[NV], float c2, MaxSum& acc) {
+__device__ __forceinline__ void add_batch(const uint4 (&raw)[NV], float c2, MaxSum& acc, float& low) {
   float m = acc.max;
 #pragma unroll
   for (int j = 0; j < NV; ++j) m = fmaxf(m, vec_max<T>(raw[j]));
   const float ref = finite_ref(m);
   const float2 less = make_float2(-ref, -ref), by = make_float2(c2, c2);
-  float2 sum = make_float2(acc.sum * exp2_fast((acc.max - ref) * c2), 0.f);
+  float2 sum = make_float2(0.f, 0.f);
 #pragma unroll
   for (int j = 0; j < NV; ++j) {
     float f[kPerVec<T>];
@@ -181,7 +183,9 @@ __device__ __forceinline__ void add_batch(const uint4 (&raw)[NV], float c2, MaxS
       sum = __fadd2_rn(sum, make_float2(exp2_fast(x.x), exp2_fast(x.y)));
     }
   }
-  acc = {m, sum.x + sum.y};
+  const float moved = exp2_fast((acc.max - ref) * c2), before = acc.sum * moved, batch = sum.x + sum.y;
+  acc = {m, before + batch};
+  low = low * moved + (before > batch ? batch - (acc.sum - before) : before - (acc.sum - batch));
 }
 
 // ---- distillation ---------------------------------------------------------------------------
@@ -488,6 +492,7 @@ __global__ void __launch_bounds__(kRowThreads, 2) k_distill(DistillArgs a, uint3
       if (tid < a.k) S.logit[tid] = S.z;
     } else {
       MaxSum mine = {-CUDART_INF_F, 0.f};
+      float low = 0.f;
       for (uint32_t from = 0;;) {
         uint4 ahead[NV];
         if (KIND == kDistillLoss && from + NV < rounds) load_batch<T, NV>(R, from + NV, ahead);
@@ -495,7 +500,7 @@ __global__ void __launch_bounds__(kRowThreads, 2) k_distill(DistillArgs a, uint3
         for (int j = 0; j < NV; ++j)
           if (from + j < rounds)
             if (const uint32_t bits = listed_of<T>(marks, tid + (from + j) * nt)) drop_elements<T>(raw[j], bits);
-        add_batch<T, NV>(raw, c2, mine);
+        add_batch<T, NV>(raw, c2, mine, low);
         from += NV;
         if (from >= rounds) break;
         if (KIND == kDistillLoss) {
@@ -505,6 +510,7 @@ __global__ void __launch_bounds__(kRowThreads, 2) k_distill(DistillArgs a, uint3
           load_batch<T, NV>(R, from, raw);
         }
       }
+      mine.sum += low;
       mine = warp_join(mine, c2);
       if (lane == 0) of_warp[warp] = mine;
       if (warp * 32 < a.k) {
@@ -1596,18 +1602,20 @@ __global__ void __launch_bounds__(kRowThreads, 2) k_top_logits(TopArgs a, uint32
   __syncthreads();
 
   MaxSum acc = {-CUDART_INF_F, 0.f};
+  float low = 0.f;
   uint32_t bound = kOrderNegInf + 1;
   const uint32_t want = (a.k + blocks - 1) >> log_blocks;
   for (uint32_t b = 0;;) {
     uint4 ahead[NV];
     if (b + 1 < batches) load_batch<T, NV>(R, (b + 1) * NV, ahead);
-    add_batch<T, NV>(raw, c2, acc);
+    add_batch<T, NV>(raw, c2, acc, low);
     if (b + 1 == batches || (blocks == 1 && (b & (b + 1)) == 0)) bound = raise_bound(order_of(acc.max), want, bound, &largest);
     if (blocks == 1) list_batch<T, NV>(raw, [&](int j) { return R.word(R.first + (b * NV + j) * R.apart); }, (unsigned long long)bound << 32, &mine, list, stretch);
     if (++b >= batches) break;
 #pragma unroll
     for (int j = 0; j < NV; ++j) raw[j] = ahead[j];
   }
+  acc.sum += low;
   const MaxSum warp = warp_join(acc, c2);
   if (lane == 0) of_warp[warp_id] = warp;
   __syncthreads();
@@ -1702,12 +1710,15 @@ __global__ void __launch_bounds__(kRowThreads, 2) k_top_logits(TopArgs a, uint32
 // exponentials.)
 // What the pass lists is whole vectors, each with its largest element: for a thread of a warp that alone has found one, the elements
 // would take many instructions of the whole warp.  The side warps read those again that the last bound leaves.
+constexpr uint32_t kSumStages = 32;
 constexpr uint32_t kEndWord = 0x80000000u;  // a listed word, not a vector
 struct RowTop {
   MaxSum of_warp[kStreamWarps];
   uint32_t count, bound;
 };
-template <class T>
+// LONG: sums of kSumStages stages at a time, since equal terms round the same way (one sum of 1024 stages was off by up to 982 half steps of
+// fp32).  Rows of fewer stages do without: 2048 x 131072 bf16 137 us, so 141.
+template <class T, bool LONG>
 __global__ void __launch_bounds__(kStreamBlock, 2) k_top_stream(TopArgs a, uint32_t stages) {
   extern __shared__ __align__(128) unsigned char dyn[];
   __shared__ uint64_t full[kStagesMost], empty[kStagesMost];
@@ -1846,6 +1857,7 @@ __global__ void __launch_bounds__(kStreamBlock, 2) k_top_stream(TopArgs a, uint3
     float top[2] = {-CUDART_INF_F, -CUDART_INF_F};  // the thread's largest, of every other vector
     uint32_t bound = kOrderNegInf + 1, next_raise = 0;
     const uint32_t cuts = (R.wholes + kStageVecs - 1) / kStageVecs;
+    MaxSum earlier = {-CUDART_INF_F, 0.f};
     const auto note = [&](uint32_t order, uint32_t id) {
       const uint32_t n = atomicAdd(&mine, 1u);
       if (n < kTopList) list[n] = (unsigned long long)order << 32 | id;
@@ -1858,6 +1870,10 @@ __global__ void __launch_bounds__(kStreamBlock, 2) k_top_stream(TopArgs a, uint3
       for (int j = 0; j < kStageShare; ++j) largest_of[j] = vec_max<T>(raw[j]), top[j & 1] = fmaxf(top[j & 1], largest_of[j]);
       const float top_of = fmaxf(fmaxf(largest_of[0], largest_of[1]), fmaxf(largest_of[2], largest_of[3]));
       add_share<T>(raw, top_of, c2, acc);
+      if (LONG && (b + 1) % kSumStages == 0) {
+        earlier = join(earlier, acc, c2);
+        acc.sum = 0.f;
+      }
       if (b == next_raise && b + 1 < cuts) {
         // The bound is raised by a histogram of the threads' maxima (two of a thread) between the last bound (at first: the smallest of
         // them) and the largest
@@ -1894,6 +1910,7 @@ __global__ void __launch_bounds__(kStreamBlock, 2) k_top_stream(TopArgs a, uint3
     }
     if (end_z >= value_of(bound)) note(order_of(end_z), kEndWord | (uint32_t)end);
     if (!ok) acc.sum = CUDART_NAN_F;  // a wait has run out: the row is void
+    if (LONG) acc = join(earlier, acc, c2);
     const MaxSum warp = warp_join(acc, c2);
     if (lane == 0) tops[buf].of_warp[tid >> 5] = warp;
     some_sync<kStreamLanes>(kBarStream);
@@ -1973,9 +1990,10 @@ cudaError_t top_typed(const TopArgs& a, cudaStream_t st) {
     const size_t beside = 3 * kTopList * 8;
     const uint32_t stages = (uint32_t)((kStreamShared - beside) / (kStageVecs * 16));
     const size_t smem = (size_t)stages * kStageVecs * 16 + beside;
-    void (*const kernel)(TopArgs, uint32_t) = k_top_stream<T>;
-    static OncePerDevice once;
-    const cudaError_t e = once_per_device(once, [&] { return allow_shared(kernel, kStreamShared); });
+    const bool more = (uint64_t)a.vocab * sizeof(T) > (uint64_t)kSumStages * kStageVecs * 16;
+    void (*const kernel)(TopArgs, uint32_t) = more ? k_top_stream<T, true> : k_top_stream<T, false>;
+    static OncePerDevice once[2];
+    const cudaError_t e = once_per_device(once[more], [&] { return allow_shared(kernel, kStreamShared); });
     if (e != cudaSuccess) return e;
     launch_kernel(kKTopLogits, kernel, dim3(stream_grid(a.rows)), dim3(kStreamBlock), smem, st, false, a, stages);
     return cudaGetLastError();

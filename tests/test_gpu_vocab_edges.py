@@ -99,3 +99,29 @@ def test_a_masked_word_listed_at_any_probability(rest, rows, vocab):
         call()
         assert (loss[:3] == math.inf).all() and (loss[4:] == math.inf).all() and torch.isfinite(loss[3])
     assert torch.isfinite(g).all()
+
+
+@pytest.mark.parametrize("rows,vocab,dtype", [(80, 1 << 22, torch.float32), (39, 1 << 22, torch.float32), (39, (1 << 22) - 5, torch.bfloat16),
+                                              (160, 100_003, torch.float32)])
+def test_sums_of_many_equal_terms(rows, vocab, dtype):
+    """all logits of a row but the first ones, of which every thread has some, are the same, so that additions round alike.  A term's exponent v log2(e) is off by three roundings, twice
+    where sums of two maxima meet (6 |v| U), each power of two by 4 U and a product, and the sum by one for every addition that a term goes
+    through: at most 16 of a batch or stage, 32 of the stages that are summed together, 32 of those sums, 5 + 5 of warps and 3 of blocks.
+    The logarithm and its difference from the logit are rounded last."""
+    B = binding()
+    v = -0.25 * (torch.arange(rows, device="cuda") % 39 + 1)
+    z = v[:, None].to(dtype).expand(rows, vocab).contiguous()
+    first = min(32768, vocab // 4)
+    z[:, :first] = 0.0
+    ids, logp = torch.ones(rows, 1, dtype=torch.int32, device="cuda"), torch.zeros(rows, 1, device="cuda")
+    B.cvlc_top_logits(z, ids, logp)
+    assert (ids == 0).all()
+    ln = torch.log(first + (vocab - first) * torch.exp(v.double()))
+    tol = (6 * v.double().abs() + 10 + 93) * R.U
+    R.assert_near(logp[:, 0], -ln, tol + 2 * R.U * ln)
+    loss = torch.zeros(rows, device="cuda")
+    B.cvlc_distill_loss(z, ids, torch.zeros_like(logp), loss, rest=R.NONE)
+    R.assert_near(loss, ln, tol + 2 * R.U * ln)
+    g = torch.zeros_like(z)
+    B.cvlc_distill_step(z, ids, torch.zeros_like(logp), loss, g, rest=R.NONE)
+    R.assert_near(loss, ln, tol + 2 * R.U * ln)
