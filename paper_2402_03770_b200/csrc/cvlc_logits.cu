@@ -1523,14 +1523,17 @@ __device__ __forceinline__ void pick_digit(F&& count_of, uint32_t left, uint32_t
   }
 }
 
-// A row's records from its candidates, whose order is any, by `nt` threads that meet at sync(): `t` is the thread's number
+// A row's records from its candidates, whose order is any, by `nt` threads that meet at sync(): `t` is the thread's number.  A record's
+// log-probability has two roundings, of the difference and of the result (at a low temperature it is a large number), and is made of halves:
+// at a high temperature the difference of two logits may be beyond the type's range and it not.
 template <class F>
 __device__ __forceinline__ void put_records(const TopArgs& a, uint64_t row, const MaxSum& all, unsigned long long* packed, uint32_t n, uint32_t t,
                                             uint32_t nt, F&& sync) {
-  const float it = 1.f / a.temperature, ln_sum = logf(all.sum);
+  const float ln_sum = logf(all.sum), half_max = 0.5f * all.max;
   auto put = [&](uint32_t at, unsigned long long c) {
     a.ids[row * a.k + at] = (int32_t)~(uint32_t)c;
-    a.logp[row * a.k + at] = (value_of((uint32_t)(c >> 32)) - all.max) * it - ln_sum;
+    const float half = 0.5f * value_of((uint32_t)(c >> 32)) - half_max;
+    a.logp[row * a.k + at] = __fmaf_rn(half, a.twice_it, __fmaf_rn(half, a.twice_it_rest, -ln_sum));
   };
   if (n <= 4 * nt) {  // a few for each thread: a candidate's rank is the number of larger ones
     const uint32_t even = (n + 7) & ~7u;
@@ -2023,6 +2026,9 @@ cudaError_t launch_selftest_ring(const float* row, uint32_t cuts, int give_back,
 cudaError_t launch_top_logits(const TopArgs& args, uint32_t dtype, cudaStream_t st) {
   TopArgs a = args;
   a.c2 = scale_of(a.temperature);
+  const double twice_it = 2.0 / (double)a.temperature;
+  a.twice_it = (float)twice_it;
+  a.twice_it_rest = (float)(twice_it - (double)a.twice_it);
   if (dtype == CVLC_F32) return top_typed<float>(a, st);
   if (dtype == CVLC_F16) return top_typed<__half>(a, st);
   return top_typed<__nv_bfloat16>(a, st);

@@ -23,7 +23,8 @@ struct TopArgs {
   float temperature;
   int32_t* ids;
   float* logp;
-  float c2;  // log2(e) / temperature
+  float c2;                       // log2(e) / temperature
+  float twice_it, twice_it_rest;  // 2 / temperature, in two numbers
 };
 cudaError_t launch_top_logits(const TopArgs& a, uint32_t dtype, cudaStream_t st);
 

@@ -23,6 +23,11 @@ def check(B, z, ids, lp, rest, tau, weight, want):
     """the loss, the gradient behind it and both in one call against loss, gradient and what each may be off by"""
     loss64, grad64, tol, tol_g = want
     loss64, grad64 = loss64.float().double(), grad64.float().double()  # what is beyond fp32's range is infinite
+    # an exponential below 2^-126 is 0, and the gradient is that times up to twice |weight| / temperature (the student's share and the bucket's)
+    # the bucket's share is one less a sum whose terms have relative errors of 2^-36 (their definition in 64 bits has 2^-53): what is left of
+    # a list that holds nearly everything is off by that much of one
+    per = (1.0 if weight is None else weight.double().abs()[:, None]) / tau
+    tol_g = tol_g + (2 * 2.0 ** -126 + (2.0 ** -36 if rest == R.BUCKET else 0.0)) * per
     rows, vocab = z.shape
     how = dict(rest=rest, temperature=tau, row_weight=weight)
     loss, stats = torch.full((rows,), 5.0, device="cuda"), torch.zeros(rows, B.DISTILL_STATS, device="cuda")
@@ -125,3 +130,46 @@ def test_sums_of_many_equal_terms(rows, vocab, dtype):
     g = torch.zeros_like(z)
     B.cvlc_distill_step(z, ids, torch.zeros_like(logp), loss, g, rest=R.NONE)
     R.assert_near(loss, ln, tol + 2 * R.U * ln)
+
+
+TEMPERATURES = [1e-6, 1e-3, 1e3, 1e6]
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("rows,vocab", FORMS)
+@pytest.mark.parametrize("kind", ["normal", "lowest", "masked", "ties"])
+@pytest.mark.parametrize("tau", TEMPERATURES)
+def test_top_logits_at_the_ends_of_the_temperature(dtype, rows, vocab, kind, tau):
+    B = binding()
+    z, _ = logits_of(rows, vocab, dtype, seed=vocab, kind=kind, pad=1)
+    check_top(B, z, 60, tau)
+
+
+@pytest.mark.parametrize("rest", [R.NONE, R.SCALED, R.BUCKET])
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("rows,vocab", FORMS)
+@pytest.mark.parametrize("kind,lists", [("normal", "top"), ("lowest", "top"), ("lowest", "any"), ("masked", "top"), ("normal", "twice")])
+@pytest.mark.parametrize("tau", TEMPERATURES)
+def test_distill_at_the_ends_of_the_temperature(rest, dtype, rows, vocab, kind, lists, tau):
+    """with weights of the temperature, which keep the gradient in the type's range, and without"""
+    B = binding()
+    z, _ = logits_of(rows, vocab, dtype, seed=vocab, kind=kind, pad=1, lead=1)
+    ids, lp = records(z, 40, tau, seed=3, kind=lists)
+    seen = lp if rest != R.SCALED else moved_to_one(ids, lp, vocab)
+    weight = torch.full((rows,), tau, device="cuda")
+    check(B, z, ids, lp, rest, tau, weight, R.distill(z, ids, seen, rest, tau, weight))
+    if dtype != torch.float16:
+        check(B, z, ids, lp, rest, tau, None, R.distill(z, ids, seen, rest, tau))
+
+
+@pytest.mark.parametrize("rows,vocab", FORMS)
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_top_logits_of_rows_wider_than_the_type(rows, vocab, dtype):
+    """differences beyond the type's range, which a high temperature brings back"""
+    B = binding()
+    z, _ = logits_of(rows, vocab, dtype, seed=vocab)
+    z[:, ::7] = torch.finfo(dtype).min
+    z[:, 5] = torch.finfo(dtype).max
+    z[:, 200:] = torch.finfo(dtype).min  # fewer than k others
+    check_top(B, z, 256, 1e6)
+    check_top(B, z, 256, 1.0)
