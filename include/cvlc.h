@@ -459,7 +459,8 @@ int cvlc_top_logits(const void* logits_dev, uint32_t dtype, uint64_t rows, uint3
  * cvlc_distill_loss writes loss_dev (rows) and, where stats_dev is not NULL, rows x CVLC_DISTILL_STATS floats (16-byte
  * aligned) from which cvlc_distill_grad makes the gradient, with row weights of its own.  It has to be given the same
  * logits and records.  cvlc_distill_step makes loss and gradient in one reading of the logits.  grad_dev: rows of
- * `dtype`, grad_stride elements apart; it may be logits_dev itself (with the same stride), and must not overlap it otherwise.
+ * `dtype`, grad_stride elements apart; it may be logits_dev itself (with the same stride), or lie between the logits' rows (with the
+ * same stride), and must not overlap it otherwise.
  * Results do not depend on the order in which blocks run.  Waits inside the kernels are bounded (four seconds, for copies that take microseconds):
  * should one run out, CVLC_ERR_DEVICE_TIMEOUT goes to *status_dev and the rows that were not finished hold NaN (in
  * cvlc_top_logits: the records of a row without a softmax).

@@ -179,14 +179,17 @@ int distill_args(const cvlc_distill* a, DistillArgs* d) {
   return CVLC_OK;
 }
 
-// the gradient's rows: in the logits' place, or nowhere near them
+// the gradient's rows: in the logits' place, or apart from them (beside them, where the rows of both are equally far from each other)
 int distill_grad_args(const cvlc_distill* a, void* grad, uint64_t stride, DistillArgs* d) {
   const size_t size = element_bytes(a->dtype);
   const uintptr_t z = reinterpret_cast<uintptr_t>(a->logits_dev), g = reinterpret_cast<uintptr_t>(grad);
   if ((a->rows && !aligned(grad, size)) || stride < a->vocab || stride > (1ull << 32)) return CVLC_ERR_INVALID_ARG;
-  if (a->rows && !(g == z && stride == a->row_stride)) {
-    const uint64_t zn = ((a->rows - 1) * a->row_stride + a->vocab) * size, gn = ((a->rows - 1) * stride + a->vocab) * size;
-    if (g < z + zn && z < g + gn) return CVLC_ERR_INVALID_ARG;
+  const bool alike = stride == a->row_stride || a->rows == 1;  // of a single row no stride is used
+  if (a->rows && !(g == z && alike)) {
+    const uint64_t row = a->vocab * size, zn = (a->rows - 1) * a->row_stride * size + row, gn = (a->rows - 1) * stride * size + row;
+    const uint64_t between = (g > z ? g - z : z - g) % (stride * size);  // from a row of one to the next of the other; the rest of the stride back
+    const bool beside = alike && a->rows > 1 && between >= row && stride * size - between >= row;
+    if (g < z + zn && z < g + gn && !beside) return CVLC_ERR_INVALID_ARG;
   }
   d->grad = grad;
   d->grad_stride = stride;

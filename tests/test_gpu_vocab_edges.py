@@ -173,3 +173,39 @@ def test_top_logits_of_rows_wider_than_the_type(rows, vocab, dtype):
     z[:, 200:] = torch.finfo(dtype).min  # fewer than k others
     check_top(B, z, 256, 1e6)
     check_top(B, z, 256, 1.0)
+
+
+@pytest.mark.parametrize("rows,vocab", FORMS)
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("gap,first", [(0, "logits"), (3, "logits"), (5, "grad")])
+def test_gradient_between_the_rows_of_the_logits(rows, vocab, dtype, gap, first):
+    B = binding()
+    both = torch.full((rows, 2 * vocab + 2 * gap), 7.0, dtype=dtype, device="cuda")
+    a, b = both[:, :vocab], both[:, vocab + gap:2 * vocab + gap]
+    z, g = (a, b) if first == "logits" else (b, a)
+    z.copy_(logits_of(rows, vocab, dtype, seed=vocab)[0])
+    ids, lp = records(z, 30, 1.0, seed=7)
+    copy = both.clone()  # logits that lie alike against 16 bytes, whose sums are grouped alike
+    apart = copy[:, :vocab] if first == "logits" else copy[:, vocab + gap:2 * vocab + gap]
+    want, want_g = torch.zeros(rows, device="cuda"), torch.zeros(rows, vocab, dtype=dtype, device="cuda")
+    B.cvlc_distill_step(apart, ids, lp, want, want_g)
+    loss, stats = torch.zeros(rows, device="cuda"), torch.zeros(rows, B.DISTILL_STATS, device="cuda")
+    B.cvlc_distill_step(z, ids, lp, loss, g)
+    assert torch.equal(loss, want) and torch.equal(g, want_g) and torch.equal(z, apart)
+    g.zero_()
+    B.cvlc_distill_loss(z, ids, lp, loss, stats)
+    B.cvlc_distill_grad(z, ids, lp, stats, g)
+    B.cvlc_distill_grad(apart, ids, lp, stats, want_g)
+    assert torch.equal(g, want_g) and torch.equal(z, apart)
+    assert (both[:, vocab:vocab + gap] == 7).all() and (both[:, 2 * vocab + gap:] == 7).all()
+
+
+def test_one_row_in_the_logits_place_whatever_the_strides():
+    B = binding()
+    flat = torch.randn(4096, generator=torch.Generator().manual_seed(1)).cuda()
+    z, g = flat.as_strided((1, 500), (2000, 1)), flat.as_strided((1, 500), (700, 1))
+    ids, lp = records(z, 9, 1.0, seed=7)
+    loss, want, want_g = torch.zeros(1, device="cuda"), torch.zeros(1, device="cuda"), torch.zeros(1, 500, device="cuda")
+    B.cvlc_distill_step(z, ids, lp, want, want_g)
+    B.cvlc_distill_step(z, ids, lp, loss, g)
+    assert torch.equal(loss, want) and torch.equal(g, want_g)
