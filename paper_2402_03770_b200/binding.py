@@ -638,7 +638,7 @@ def cvlc_embed_grad(tokens: torch.Tensor, grad: torch.Tensor, update: torch.Tens
     g, stride = _rows(grad, device)
     u, update_stride = _rows(update, device)
     n, (vocab, dim) = tokens.numel(), update.shape
-    assert update.dtype == torch.float32 and grad.shape == (n, dim)
+    assert update.dtype == torch.float32 and grad.shape == (n, dim) and ws.get_device() == device
     _check(lib().cvlc_embed_grad(_here(tokens, tokens.dtype, (n,), device), _token_bytes(tokens), n, g, _DTYPES[grad.dtype], dim, stride, vocab,
                                  scale, u, update_stride, 1 if accumulate else 0, _ptr(ws), _nbytes(ws), _stream_on(stream, device)), "cvlc_embed_grad")
 
