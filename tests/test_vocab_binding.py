@@ -10,10 +10,10 @@ class On:
     is_cuda = True
 
     def __init__(self, device, dtype, *shape):
-        self.device_index, self.dtype, self.shape = device, dtype, shape
+        self.device, self.dtype, self.shape = device, dtype, shape
 
     def get_device(self):
-        return self.device_index
+        return self.device
 
     def dim(self):
         return len(self.shape)
