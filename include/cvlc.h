@@ -451,14 +451,15 @@ int cvlc_top_logits(const void* logits_dev, uint32_t dtype, uint64_t rows, uint3
  * Loss and gradient of a row are multiplied by its weight; with a weight of 0 both are 0, whatever the row holds.  The
  * gradient is with respect to z (it holds the factor 1 / temperature; the customary temperature^2 goes into the
  * weights).  A row whose logits are all -inf has no distribution: loss and gradient 0.  A listed word whose logit is -inf
- * makes the loss +inf.
+ * makes the loss +inf.  The records of a row that counts for nothing (weight 0) may go unread, and what is wrong with them unreported.
+ * A student's probability below 2^-126 of the largest counts as 0 in the gradient; the bucket's pr is off by up to 2^-36.
  *  ids_dev, logp_dev   rows x k records, contiguous; a record of word below 0 is absent; one of word >= vocab is left
  *                      out and reported (INVALID_ARG) in *status_dev
  *  row_weight_dev      rows weights, or NULL: all 1
  *  status_dev          one int32 of the caller's, 0 beforehand: the first error stays in it; or NULL
  * cvlc_distill_loss writes loss_dev (rows) and, where stats_dev is not NULL, rows x CVLC_DISTILL_STATS floats (16-byte
  * aligned) from which cvlc_distill_grad makes the gradient, with row weights of its own.  It has to be given the same
- * logits and records.  cvlc_distill_step makes loss and gradient in one reading of the logits.  grad_dev: rows of
+ * logits, records, temperature and treatment of the rest.  cvlc_distill_step makes loss and gradient in one reading of the logits.  grad_dev: rows of
  * `dtype`, grad_stride elements apart; it may be logits_dev itself (with the same stride), or lie between the logits' rows (with the
  * same stride), and must not overlap it otherwise.
  * Results do not depend on the order in which blocks run.  Waits inside the kernels are bounded (four seconds, for copies that take microseconds):
@@ -501,7 +502,8 @@ int cvlc_embed(const void* table_dev, uint32_t dtype, uint64_t vocab, uint32_t d
 /*
  * Its gradient: update[v] = scale * sum of grad[i] over the positions i with tokens[i] = v, in fp32, added to the rows that are
  * there (accumulate = 1; rows of words that do not occur are not touched) or with zeros for words that do not occur
- * (accumulate = 0).  With the block of the table in the client's update vector as update_dev and the learning rate in
+ * (accumulate = 0).  Adding takes fp32 numbers below 2^-126 for 0 (what is there, what is added and their sum); writing out does
+ * not.  With the block of the table in the client's update vector as update_dev and the learning rate in
  * `scale`, local steps of SGD leave U = w_0 - w_E there for cvlc_plan.  The positions of a word are added in ascending
  * order in a fixed grouping: equal inputs give equal bits.  Padding (below 0) has no gradient; a token >= vocab has none either and
  * is reported (INVALID_ARG) at byte 0 of the workspace (cvlc_read_status).

@@ -78,7 +78,8 @@ __global__ void __launch_bounds__(kLookupThreads, 6) k_embed(EmbedArgs a) {
 }
 
 // Long rows, of 128 vectors or more: a warp for a row, kLookupWide vectors of a lane on their way, and the next row's token.  Memory bounds it: 32768
-// rows of 8 KB (24000 of them different) 71 us, 79% of the copy bandwidth, k_embed 76.
+// rows of 8 KB (24000 of them different) 71 us, 79% of the copy bandwidth, k_embed 76.  Few rows are bound by the rounds of their one warp: in a
+// graph, one row of 8 KB 2.2 us (16-bit) and one of 32 KB 4.4, where the shortest rows take 1.7.
 constexpr int kLookupWide = 8;
 template <class T>
 __global__ void __launch_bounds__(kLookupThreads, 4) k_embed_wide(EmbedArgs a) {
@@ -297,7 +298,8 @@ __device__ void sort_in_block(const EmbedGradArgs& a, uint32_t bits, uint32_t pa
 
 // Stable radix sort by digits of up to nine bits, by one cluster.  What bounds it is its chain of passes, each of two walks and two cluster
 // barriers, on eight SMs: 8192 tokens of 32000 words 18 us with the launch.  The zeros of the launch's other blocks hide it where the table is
-// large (65537 tokens beside 512 MB of table: 88 us, the time of the zeros alone).  Clusters of 4 leave the zeros more SMs and the sort
+// large (65537 tokens beside 512 MB of table: 88 us, which 112 blocks take for 345 MB of zeros; being clusters as well, they leave 28
+// SMs without a block, and a plain fill of all 512 MB takes 76).  Clusters of 4 leave the zeros more SMs and the sort
 // fewer: 17308 tokens beside 22 MB 31 us for the whole gradient, with 8 27; beside 512 MB 180 and 180.  Every warp has a stretch of the positions, in order; it counts its
 // digits (in any order), the counts are scanned over warps (in groups, side by side) and blocks for every digit, and the warp walks its stretch again, giving
 // each position its place.  Tokens that stand for nothing (below zero, or outside the table) sort behind all words as word `vocab`.
@@ -412,7 +414,7 @@ struct Sorted {
 };
 
 // A word's row, or a part of it.  Added by reductions in memory, which nothing waits for: a row is added to once in a kernel, so they
-// have no order (8192 rows of 4 KB added: 17 us, reading the rows first 22).
+// have no order (8192 rows of 4 KB added: 17 us, reading the rows first 22).  They take subnormal numbers for 0.
 template <int E>
 __device__ __forceinline__ void put_row(const EmbedGradArgs& a, uint32_t word, uint32_t col, const float (&acc)[E]) {
   float* const u = a.update + (uint64_t)word * a.update_stride + (uint64_t)col * E;

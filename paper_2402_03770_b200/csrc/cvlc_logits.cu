@@ -635,7 +635,7 @@ __global__ void __launch_bounds__(kRowThreads, 2) k_distill(DistillArgs a, uint3
 // thread copies the rows through a ring of stages in shared memory (cp.async.bulk), four vectors of every thread a stage.  The step passes over
 // every row twice, at first over what the ring still holds of it, then over what it has to copy once more, most of which is in the L2 cache
 // (the 296 rows on their way are 76 MB at 131,072 words of 16 bits).  Keeping the row in the cluster's registers instead costs every block of the cluster all of the above:
-// 4096 x 131072 bf16 750 us, so 415 to 452 (of 329 at the copy bandwidth; warm, and with cold caches); the loss 192 to 214 (of 165).  The pass is a
+// 4096 x 131072 bf16 750 us, so 430 to 455 (of 332 at the copy bandwidth; from box to box); the loss 200 to 215 (of 166).  The pass is a
 // chain of load, maximum, exponential and sum in 16 warps an SM: without the exponentials the loss takes 156 us.  More warps for it leave
 // too few registers and stages (ten 211, twelve 243).
 constexpr int kStreamWarps = 8, kSideWarps = 4;  // and one that copies
