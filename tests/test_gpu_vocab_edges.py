@@ -209,3 +209,17 @@ def test_one_row_in_the_logits_place_whatever_the_strides():
     B.cvlc_distill_step(z, ids, lp, want, want_g)
     B.cvlc_distill_step(z, ids, lp, loss, g)
     assert torch.equal(loss, want) and torch.equal(g, want_g)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("kind,lead,pad,k", [("normal", 0, 0, 64), ("ties", 1, 1, 256), ("crowd", 3, 0, 100), ("masked", 0, 2, 7), ("front masked", 5, 1, 96)])
+def test_top_logits_of_many_rows_of_many_stages(dtype, kind, lead, pad, k):
+    """more than 32 stages a row, which are summed 32 at a time; with the front masked the list of what reaches the bound overflows"""
+    B = binding()
+    rows, vocab = 82, 140_003 if dtype == torch.float32 else 270_005
+    z, _ = logits_of(rows, vocab, dtype, seed=k, kind="normal" if kind == "front masked" else kind, lead=lead, pad=pad)
+    if kind == "front masked":
+        z[:, :vocab // 4] = -math.inf
+    if kind == "normal":
+        z[3, 5], z[4, vocab - 1], z[5] = math.nan, math.inf, -math.inf
+    check_top(B, z, k, 0.7)
