@@ -518,6 +518,75 @@ int cvlc_embed_grad(const void* tokens_dev, uint32_t token_bytes, uint64_t n, co
                     uint32_t dim, uint64_t grad_stride, uint64_t vocab, float scale, float* update_dev,
                     uint64_t update_stride, int accumulate, void* ws_dev, size_t ws_bytes, void* cuda_stream);
 
+/* --- the optimiser of a local step, and of the server ------------------------- */
+
+/*
+ * AdamW over many tensors at once.  With g = grad_scale * clip * grad, t the number of the step (from 1 on):
+ *   m = beta1 m + (1 - beta1) g        v = beta2 v + (1 - beta2) g^2
+ *   param -= lr (weight_decay param + (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps))
+ * in fp32, param rounded once to its type.  Between cvlc_embed_grad and cvlc_plan it is the client's local step; at
+ * the parameter server, with the aggregate of cvlc_decode_aggregate as the gradient, the adaptive form of the model step of cvlc_decode_apply.
+ *  param_dtype, grad_dtype   any of the three types; copy_dtype: CVLC_F16 or CVLC_BF16, for tensors with a copy_dev
+ *  state_bits   32: m_dev and v_dev are n fp32 each, scale_dev is not used.  8: n bytes each, m in e4m3, v in e5m2 (the OCP
+ *               types), and for every CVLC_STATE_BLOCK consecutive values, the last ones of a tensor fewer, two floats in scale_dev (m's and
+ *               v's, 8-byte aligned): a state is its byte's value times its scale, the largest of a block at 448 or
+ *               57344 (a block whose largest is below 2^-100 is held as zeros).  Bytes are rounded up or down with the probability that keeps the average, by the random
+ *               bits of Philox4x32-10 with counter (value / 4, its upper half, number of the tensor in the call, t) and
+ *               key `seed`, word value % 4, the lower half for m, the upper one for v; a v above 0 stays above 0.  All zeros are the
+ *               states before the first step.
+ *  copy_dev     n values of copy_dtype, rounded from the new param, or NULL
+ *  lr_dev, step_dev   device words in place of values that a captured graph would hold: lr is multiplied by *lr_dev, t is *step_dev; or NULL
+ *  norm_dev     clip = min(1, max_norm / *norm_dev) (cvlc_grad_norm's, with the same grad_scale); NULL: clip = 1.  If it is
+ *               not finite the call changes nothing and reports NONFINITE_INPUT in *status_dev (one int32 of the caller's, or NULL)
+ * Tensors may begin at any element (16-byte alignment of all of a tensor's arrays, or the same misalignment with states of 32
+ * bits, is faster), must not overlap, and are left alone where n = 0.  Equal inputs give equal bits.
+ * Errors: INVALID_ARG (types, bits, a pointer that is not aligned to its type, n above 2^40 in all, betas outside [0, 1), eps below
+ * 1e-30, a step of 0 where it counts, max_norm that is not above 0, numbers that are not finite).
+ */
+#define CVLC_STATE_BLOCK 256u
+typedef struct cvlc_adamw_tensor {
+  uint64_t n;
+  const void* grad_dev;
+  void* param_dev;
+  void* m_dev;
+  void* v_dev;
+  float* scale_dev;
+  void* copy_dev;
+  float lr; /* multiplies the call's */
+  float weight_decay;
+} cvlc_adamw_tensor;
+typedef struct cvlc_adamw_args {
+  uint32_t param_dtype;
+  uint32_t grad_dtype;
+  uint32_t copy_dtype;
+  uint32_t state_bits;
+  double lr;
+  double beta1;
+  double beta2;
+  double eps;
+  uint64_t seed;
+  uint32_t step;
+  float grad_scale;
+  float max_norm;
+  uint32_t reserved;
+  const float* norm_dev;
+  const float* lr_dev;
+  const uint32_t* step_dev;
+  int32_t* status_dev;
+} cvlc_adamw_args;
+int cvlc_adamw(const cvlc_adamw_tensor* tensors, uint32_t n_tensors, const cvlc_adamw_args* a, void* cuda_stream);
+
+/*
+ * The norm of all gradients together, *norm_dev = |grad_scale| sqrt(sum grad^2), for cvlc_adamw's clipping: squares in fp32 (a value above 1.8e19 makes it
+ * infinite, one below 1e-23 counts for nothing), their sums in 64 bits, in an order that does not change.  Only n and grad_dev of the tensors are
+ * read; they may overlap.
+ *  ws_dev   cvlc_grad_norm_workspace_bytes(n_tensors) bytes, 256-byte aligned
+ * Errors: INVALID_ARG, WORKSPACE_TOO_SMALL.
+ */
+size_t cvlc_grad_norm_workspace_bytes(uint32_t n_tensors);
+int cvlc_grad_norm(const cvlc_adamw_tensor* tensors, uint32_t n_tensors, uint32_t grad_dtype, float grad_scale, float* norm_dev,
+                   void* ws_dev, size_t ws_bytes, void* cuda_stream);
+
 /* Waits for cuda_stream and returns the status word at byte 0 of a plan or workspace. */
 int cvlc_read_status(const void* plan_or_ws_dev, void* cuda_stream);
 
@@ -551,7 +620,8 @@ int cvlc_selftest_ring(const float* row_dev, uint32_t stages, int give_back, uin
  * k_hist, k_plan_threshold, k_plan_fit, k_plan_tune, k_encode_init, k_select, k_select_lookback, k_rank_split, k_rank, k_rank_rest, k_sort,
  * k_pack, k_decode_prepare, k_fill_zero, k_prefetch_l2, k_decode,
  * k_noalloc_publish_status, k_selftest, k_hist_check, k_apply, k_plan_literal, k_ec_accumulate, k_pack_unframed, k_decode_unframed,
- * k_top_logits, k_distill_loss, k_distill_grad, k_distill_step, k_embed, k_token_sort, k_embed_sum, k_embed_join. */
+ * k_top_logits, k_distill_loss, k_distill_grad, k_distill_step, k_embed, k_token_sort, k_embed_sum, k_embed_join,
+ * k_adamw, k_norm_parts, k_norm_join. */
 unsigned long long cvlc_launch_count(const char* kernel_name);
 /* Optional kernel timing: after cvlc_profile_select(name, n) the next n launches of that kernel
  * ("*" = of every kernel) are bracketed by a CUDA event pair on their own stream;

@@ -38,6 +38,7 @@ MAX_VOCAB = 1 << 22
 MAX_TOP = 256
 MAX_RECORDS = 1024
 DISTILL_STATS = 8
+STATE_BLOCK = 256
 
 CVLC_QUANT_PQ = 0
 CVLC_QUANT_QSGD = 1
@@ -58,7 +59,7 @@ EXPORTS = [
     "cvlc_plan_literal_workspace_bytes", "cvlc_ec_accumulate_batch", "cvlc_encode_batch_ec",
     "cvlc_unframed_stream_capacity", "cvlc_unframed_workspace_bytes", "cvlc_encode_unframed_batch", "cvlc_decode_aggregate_unframed",
     "cvlc_top_logits", "cvlc_distill_loss", "cvlc_distill_grad", "cvlc_distill_step", "cvlc_embed", "cvlc_embed_grad_workspace_bytes",
-    "cvlc_embed_grad", "cvlc_launch_count", "cvlc_profile_select", "cvlc_profile_reset", "cvlc_profile_read",
+    "cvlc_embed_grad", "cvlc_adamw", "cvlc_grad_norm", "cvlc_grad_norm_workspace_bytes", "cvlc_launch_count", "cvlc_profile_select", "cvlc_profile_reset", "cvlc_profile_read",
 ]
 
 
@@ -93,6 +94,22 @@ class CvlcDistill(C.Structure):
         ("logits_dev", C.c_void_p), ("rows", C.c_uint64), ("row_stride", C.c_uint64), ("vocab", C.c_uint32), ("dtype", C.c_uint32),
         ("ids_dev", C.c_void_p), ("logp_dev", C.c_void_p), ("k", C.c_uint32), ("rest", C.c_uint32), ("temperature", C.c_float),
         ("reserved", C.c_uint32), ("row_weight_dev", C.c_void_p), ("status_dev", C.c_void_p),
+    ]
+
+
+class CvlcAdamwTensor(C.Structure):
+    _fields_ = [
+        ("n", C.c_uint64), ("grad_dev", C.c_void_p), ("param_dev", C.c_void_p), ("m_dev", C.c_void_p), ("v_dev", C.c_void_p),
+        ("scale_dev", C.c_void_p), ("copy_dev", C.c_void_p), ("lr", C.c_float), ("weight_decay", C.c_float),
+    ]
+
+
+class CvlcAdamwArgs(C.Structure):
+    _fields_ = [
+        ("param_dtype", C.c_uint32), ("grad_dtype", C.c_uint32), ("copy_dtype", C.c_uint32), ("state_bits", C.c_uint32),
+        ("lr", C.c_double), ("beta1", C.c_double), ("beta2", C.c_double), ("eps", C.c_double), ("seed", C.c_uint64),
+        ("step", C.c_uint32), ("grad_scale", C.c_float), ("max_norm", C.c_float), ("reserved", C.c_uint32),
+        ("norm_dev", C.c_void_p), ("lr_dev", C.c_void_p), ("step_dev", C.c_void_p), ("status_dev", C.c_void_p),
     ]
 
 
@@ -192,6 +209,13 @@ def lib() -> C.CDLL:
     L.cvlc_embed_grad_workspace_bytes.argtypes = [u64, u32, u64]
     L.cvlc_embed_grad.restype = C.c_int
     L.cvlc_embed_grad.argtypes = [vp, u32, u64, vp, u32, u32, u64, u64, C.c_float, vp, u64, C.c_int, vp, sz, vp]
+    PT = C.POINTER(CvlcAdamwTensor)
+    L.cvlc_adamw.restype = C.c_int
+    L.cvlc_adamw.argtypes = [PT, u32, C.POINTER(CvlcAdamwArgs), vp]
+    L.cvlc_grad_norm_workspace_bytes.restype = sz
+    L.cvlc_grad_norm_workspace_bytes.argtypes = [u32]
+    L.cvlc_grad_norm.restype = C.c_int
+    L.cvlc_grad_norm.argtypes = [PT, u32, u32, C.c_float, vp, vp, sz, vp]
     L.cvlc_read_status.restype = C.c_int
     L.cvlc_read_status.argtypes = [vp, vp]
     L.cvlc_selftest_philox.restype = C.c_int
@@ -643,6 +667,76 @@ def cvlc_embed_grad(tokens: torch.Tensor, grad: torch.Tensor, update: torch.Tens
                                  scale, u, update_stride, 1 if accumulate else 0, _ptr(ws), _nbytes(ws), _stream_on(stream, device)), "cvlc_embed_grad")
 
 
+class AdamwTensors:
+    """The tensors of cvlc_adamw and cvlc_grad_norm, made once for all steps: gradients, and for the step weights, states and, with states of
+    8 bits (m in e4m3, v in e5m2, uint8 or those types), scales of shape (blocks of STATE_BLOCK values, 2).  Tensors are contiguous and stay where
+    they are.  lr (a multiple of the call's) and weight_decay: one number, or one for each."""
+
+    def __init__(self, grads: Sequence[torch.Tensor], params: Optional[Sequence[torch.Tensor]] = None, m: Optional[Sequence[torch.Tensor]] = None,
+                 v: Optional[Sequence[torch.Tensor]] = None, scales: Optional[Sequence[torch.Tensor]] = None,
+                 copies: Optional[Sequence[Optional[torch.Tensor]]] = None, lr=1.0, weight_decay=0.0):
+        self.n = n = len(grads)
+        self._keep = [list(x) for x in (grads, params, m, v, scales, copies) if x is not None]
+        self.device = grads[0].get_device() if n else _device()
+        self.step = params is not None
+        self.array = (CvlcAdamwTensor * max(n, 1))()
+        self.grad_dtype = _DTYPES[grads[0].dtype] if n else CVLC_F32
+        self.param_dtype = _DTYPES[params[0].dtype] if n and self.step else CVLC_F32
+        self.state_bits = 32 if scales is None else 8
+        self.copy_dtype = next((_DTYPES[x.dtype] for x in copies or () if x is not None), CVLC_BF16)
+
+        def at(x: Optional[torch.Tensor], size: int, dtype: int) -> Optional[int]:
+            if x is None:
+                return None
+            assert x.numel() == size and x.is_contiguous() and x.get_device() == self.device and _DTYPES[x.dtype] == dtype, (x.shape, x.dtype, x.device)
+            return x.data_ptr()
+
+        def state(x: torch.Tensor, size: int, float8: torch.dtype) -> int:
+            if self.state_bits == 32:
+                return at(x, size, CVLC_F32)
+            assert x.dtype in (torch.uint8, float8) and x.numel() == size and x.is_contiguous() and x.get_device() == self.device, (x.shape, x.dtype)
+            return x.data_ptr()
+
+        for i, (t, g) in enumerate(zip(self.array, grads)):
+            t.n = size = g.numel()
+            t.grad_dev = at(g, size, self.grad_dtype)
+            t.lr = lr if isinstance(lr, (int, float)) else lr[i]
+            t.weight_decay = (weight_decay if isinstance(weight_decay, (int, float)) else weight_decay[i]) if weight_decay is not None else 0.0
+            if self.step:
+                t.param_dev = at(params[i], size, self.param_dtype)
+                t.m_dev, t.v_dev = state(m[i], size, torch.float8_e4m3fn), state(v[i], size, torch.float8_e5m2)
+                if scales is not None:
+                    t.scale_dev = at(scales[i], 2 * ((size + STATE_BLOCK - 1) // STATE_BLOCK), CVLC_F32)
+                if copies is not None:
+                    t.copy_dev = at(copies[i], size, self.copy_dtype)
+
+
+def cvlc_adamw(tensors: AdamwTensors, *, lr: float, step: int, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8, grad_scale: float = 1.0,
+               norm: Optional[torch.Tensor] = None, max_norm: float = 1.0, seed: int = 0, lr_dev: Optional[torch.Tensor] = None,
+               step_dev: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> None:
+    """One AdamW step; norm (fp32, one value): clip by it to max_norm; lr_dev (fp32) multiplies lr and step_dev (int32) replaces step, for
+    captured graphs."""
+    device = _device()
+    assert tensors.step and (tensors.device == device or tensors.n == 0)
+    a = CvlcAdamwArgs(tensors.param_dtype, tensors.grad_dtype, tensors.copy_dtype, tensors.state_bits, lr, beta1, beta2, eps, seed, step, grad_scale,
+                      max_norm, 0, _here(norm, torch.float32, (1,), device), _here(lr_dev, torch.float32, (1,), device),
+                      _here(step_dev, torch.int32, (1,), device), _here(status, torch.int32, (1,), device))
+    _check(lib().cvlc_adamw(tensors.array, tensors.n, C.byref(a), _stream_on(stream, device)), "cvlc_adamw")
+
+
+def cvlc_grad_norm_workspace_bytes(tensors: AdamwTensors) -> int:
+    return int(lib().cvlc_grad_norm_workspace_bytes(tensors.n))
+
+
+def cvlc_grad_norm(tensors: AdamwTensors, norm: torch.Tensor, ws: torch.Tensor, grad_scale: float = 1.0,
+                   stream: Optional[torch.cuda.Stream] = None) -> None:
+    """norm (fp32, one value) of grad_scale times all gradients"""
+    device = _device()
+    assert (tensors.device == device or tensors.n == 0) and ws.get_device() == device
+    _check(lib().cvlc_grad_norm(tensors.array, tensors.n, tensors.grad_dtype, grad_scale, _here(norm, torch.float32, (1,), device), _ptr(ws), _nbytes(ws),
+                                _stream_on(stream, device)), "cvlc_grad_norm")
+
+
 def cvlc_read_status(plan_or_ws: torch.Tensor, stream: Optional[torch.cuda.Stream] = None) -> int:
     return int(lib().cvlc_read_status(_ptr(plan_or_ws), _stream_handle(stream)))
 
@@ -677,7 +771,8 @@ def cvlc_profile_reset() -> None:
 KERNEL_NAMES = ["k_zero_words", "k_client", "k_hist", "k_plan_threshold", "k_plan_fit", "k_plan_tune", "k_encode_init", "k_select",
                 "k_select_lookback", "k_rank_split", "k_rank", "k_rank_rest", "k_sort", "k_pack", "k_decode_prepare", "k_fill_zero",
                 "k_prefetch_l2", "k_decode", "k_noalloc_publish_status", "k_selftest", "k_hist_check", "k_apply", "k_plan_literal", "k_ec_accumulate", "k_pack_unframed", "k_decode_unframed",
-                "k_top_logits", "k_distill_loss", "k_distill_grad", "k_distill_step", "k_embed", "k_token_sort", "k_embed_sum", "k_embed_join"]
+                "k_top_logits", "k_distill_loss", "k_distill_grad", "k_distill_step", "k_embed", "k_token_sort", "k_embed_sum", "k_embed_join",
+                "k_adamw", "k_norm_parts", "k_norm_join"]
 
 
 def cvlc_profile_read(kernel_name: str = "*"):

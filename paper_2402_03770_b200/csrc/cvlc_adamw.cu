@@ -1,0 +1,412 @@
+// AdamW over many tensors at once, with states in fp32 or in 8 bits, and the norm of their gradients.
+//
+// m = b1 m + (1 - b1) g,  v = b2 v + (1 - b2) g^2,  p -= lr (wd p + (m / (1 - b1^t)) / (sqrt(v / (1 - b2^t)) + eps))
+//
+// Nothing is used twice, so the step is bounded by what it moves: 30 bytes a value with fp32 weights and states, bf16 gradients and a bf16
+// copy, 16 with states of 8 bits.  All tensors go in one launch: their descriptors are a parameter of the kernel, a block finds its tensor by
+// the number of its first chunk.  A warp has 256 values at a time, 8 consecutive ones a lane: the values that share a scale, so that their
+// largest is found by one reduction of a warp and the states are read and written once.
+#include "cvlc_common.cuh"
+#include "cvlc_vocab.cuh"
+
+namespace cvlc {
+namespace {
+
+constexpr int kBlock = CVLC_STATE_BLOCK;  // values of a warp at a time, and of a scale
+constexpr int kPer = kBlock / 32;         // consecutive ones of a lane
+constexpr int kThreads = 256, kWarps = kThreads / 32;
+constexpr uint32_t kNormChunks = 16 * kNumSM;  // of the norm, at most, and one more for every tensor
+
+// Which of a tensor's arrays can be read and written by vectors.  fp32 states have no blocks of their own, so that their tensors are cut where the
+// weights' addresses are multiples of 32 bytes: `lead` values before the first are not there.
+enum : uint32_t { kVecParam = 1, kVecGrad = 2, kVecM = 4, kVecV = 8, kVecCopy = 16 };
+struct TensorDesc {
+  uint64_t n;
+  const void* grad;
+  void *param, *m, *v, *copy;
+  float2* scale;
+  float lr, decay;
+  uint32_t first;  // its first chunk
+  uint16_t vec, lead;
+};
+struct StepScalars {
+  float lr, b1, b1r, b2, b2r, eps, ic1, ic2, grad_scale, max_norm;
+  double beta1, beta2;
+  const float *norm, *lr_dev;
+  const uint32_t* step_dev;
+  uint64_t seed;
+  uint32_t step, chunk;  // blocks of values in a chunk
+  uint32_t param_dtype, grad_dtype, copy_dtype;
+  uint32_t tensor0;  // number of the first tensor of this launch
+  int32_t* status;
+};
+// Launch parameters cost the host what they hold (24 KB about 3 us), so there are three capacities.
+constexpr uint32_t kFew = 8, kSome = 64, kMany = 440;
+template <uint32_t CAP>
+struct TensorList {
+  uint32_t n, chunks;
+  StepScalars s;
+  TensorDesc t[CAP];
+};
+static_assert(sizeof(TensorList<kMany>) <= 32764, "launch parameters");
+
+template <uint32_t CAP>
+__device__ __forceinline__ uint32_t tensor_of(const TensorList<CAP>& L, uint32_t chunk) {
+  uint32_t lo = 0, hi = L.n;  // the last one whose first chunk is not behind it
+  while (hi - lo > 1) {
+    const uint32_t mid = (lo + hi) / 2;
+    if (L.t[mid].first <= chunk) lo = mid; else hi = mid;
+  }
+  return lo;
+}
+
+// eight values from `at` on; those outside of [0, n) are 0 and are not touched
+template <class T>
+__device__ __forceinline__ void load8(const void* base, int64_t at, uint64_t n, bool vec, float (&x)[kPer]) {
+  const T* p = static_cast<const T*>(base) + at;
+  if (vec && at >= 0 && (uint64_t)at + kPer <= n) {
+    constexpr int per = kPerVec<T>;
+#pragma unroll
+    for (int i = 0; i < kPer / per; ++i) {
+      float y[per];
+      widen<T>(__ldcs(reinterpret_cast<const uint4*>(p) + i), y);
+#pragma unroll
+      for (int k = 0; k < per; ++k) x[i * per + k] = y[k];
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) x[i] = (uint64_t)(at + i) < n ? to_float(p[i]) : 0.0f;
+  }
+}
+template <class T>
+__device__ __forceinline__ void store8(void* base, int64_t at, uint64_t n, bool vec, const float (&x)[kPer]) {
+  T* p = static_cast<T*>(base) + at;
+  if (vec && at >= 0 && (uint64_t)at + kPer <= n) {
+    constexpr int per = kPerVec<T>;
+#pragma unroll
+    for (int i = 0; i < kPer / per; ++i) {
+      float y[per];
+#pragma unroll
+      for (int k = 0; k < per; ++k) y[k] = x[i * per + k];
+      __stcs(reinterpret_cast<uint4*>(p) + i, narrow<T>(y));
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < kPer; ++i)
+      if ((uint64_t)(at + i) < n) p[i] = from_float<T>(x[i]);
+  }
+}
+__device__ __forceinline__ void load8(uint32_t dtype, const void* base, int64_t at, uint64_t n, bool vec, float (&x)[kPer]) {
+  if (dtype == CVLC_F32) load8<float>(base, at, n, vec, x);
+  else if (dtype == CVLC_F16) load8<__half>(base, at, n, vec, x);
+  else load8<__nv_bfloat16>(base, at, n, vec, x);
+}
+__device__ __forceinline__ void store8(uint32_t dtype, void* base, int64_t at, uint64_t n, bool vec, const float (&x)[kPer]) {
+  if (dtype == CVLC_F32) store8<float>(base, at, n, vec, x);
+  else if (dtype == CVLC_F16) store8<__half>(base, at, n, vec, x);
+  else store8<__nv_bfloat16>(base, at, n, vec, x);
+}
+__device__ __forceinline__ uint2 load_bytes(const void* base, int64_t at, uint64_t n, bool vec) {
+  const uint8_t* p = static_cast<const uint8_t*>(base) + at;
+  if (vec && (uint64_t)at + kPer <= n) return __ldcs(reinterpret_cast<const uint2*>(p));
+  uint32_t w[2] = {0, 0};
+#pragma unroll
+  for (int i = 0; i < kPer; ++i)
+    if ((uint64_t)(at + i) < n) w[i / 4] |= (uint32_t)p[i] << (8 * (i & 3));
+  return make_uint2(w[0], w[1]);
+}
+__device__ __forceinline__ void store_bytes(void* base, int64_t at, uint64_t n, bool vec, const uint32_t (&w)[2]) {
+  uint8_t* p = static_cast<uint8_t*>(base) + at;
+  if (vec && (uint64_t)at + kPer <= n) {
+    __stcs(reinterpret_cast<uint2*>(p), make_uint2(w[0], w[1]));
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < kPer; ++i)
+    if ((uint64_t)(at + i) < n) p[i] = (uint8_t)(w[i / 4] >> (8 * (i & 3)));
+}
+
+// ---- 8-bit states --------------------------------------------------------------------------
+// m is held in e4m3 (largest value 448), v in e5m2 (57344), relative to the largest value of the block of 256.  A float's bits are linear
+// between two neighbouring values of the short type, so rounding up with the probability of what is cut off is adding random bits below the cut.
+// Rounding to nearest would not do: an average that moves by a thousandth a step never leaves a value whose neighbours are an eighth away.
+template <int MANTISSA, int BIAS>
+__device__ __forceinline__ uint32_t to_float8(float y, uint32_t random16) {
+  constexpr int cut = 23 - MANTISSA;
+  constexpr float lowest = MANTISSA == 3 ? 0x1p-6f : 0x1p-14f;  // below it the steps stay as they are: a float of that size added has the same ones
+  const bool small = y < lowest;
+  const uint32_t bits = __float_as_uint(small ? y + lowest : y) + (random16 << (cut - 16)) + (1u << (cut - 17));
+  return (bits >> cut) - ((uint32_t)(127 - BIAS) << MANTISSA) - (small ? 1u << MANTISSA : 0u);
+}
+template <int MANTISSA, int BIAS>
+__device__ __forceinline__ float from_float8(uint32_t code) {  // of 7 bits
+  // as a float's subnormal or normal number of another bias; the product with a power of two is exact
+  return __uint_as_float(code << (23 - MANTISSA)) * (BIAS == 7 ? 0x1p120f : 0x1p112f);
+}
+constexpr float kLeast = 0x1p-100f;  // a block whose largest value is below this is held as zeros
+
+template <bool EIGHT, uint32_t CAP>
+__global__ void __launch_bounds__(kThreads) k_adamw(const __grid_constant__ TensorList<CAP> L) {
+  const StepScalars& s = L.s;
+  __shared__ float corrections[2];
+  float ic1 = s.ic1, ic2 = s.ic2;
+  uint32_t step = s.step;
+  if (s.step_dev) {
+    step = *s.step_dev;
+    if (threadIdx.x == 0) {
+      double p1 = 1.0, p2 = 1.0, q1 = s.beta1, q2 = s.beta2;
+      for (uint32_t k = step; k; k >>= 1) {
+        if (k & 1) p1 *= q1, p2 *= q2;
+        q1 *= q1, q2 *= q2;
+      }
+      corrections[0] = (float)(1.0 / (1.0 - p1)), corrections[1] = (float)(1.0 / (1.0 - p2));
+    }
+    __syncthreads();
+    ic1 = corrections[0], ic2 = corrections[1];
+  }
+  float scale = s.grad_scale;
+  if (s.norm) {
+    const float norm = *s.norm;
+    if (!(norm < CUDART_INF_F)) {  // nothing is to be learnt from such gradients
+      if (s.status && blockIdx.x == 0 && threadIdx.x == 0) set_status(s.status, CVLC_ERR_NONFINITE_INPUT);
+      return;
+    }
+    scale *= norm > s.max_norm ? s.max_norm / norm : 1.0f;
+  }
+  const uint32_t index = tensor_of(L, blockIdx.x);
+  const TensorDesc& t = L.t[index];
+  const float lr = (s.lr_dev ? s.lr * *s.lr_dev : s.lr) * t.lr;
+  const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x & 31;
+  const uint64_t blocks = (t.n + t.lead + kBlock - 1) / kBlock;
+  uint64_t block = (uint64_t)(blockIdx.x - t.first) * s.chunk + warp;
+  const uint64_t end = min(blocks, (uint64_t)(blockIdx.x - t.first + 1) * s.chunk);
+  for (; block < end; block += kWarps) {
+    const int64_t at = (int64_t)(block * kBlock + lane * kPer) - t.lead;
+    float p[kPer], g[kPer], m[kPer], v[kPer];
+    load8(s.param_dtype, t.param, at, t.n, t.vec & kVecParam, p);
+    load8(s.grad_dtype, t.grad, at, t.n, t.vec & kVecGrad, g);
+    if (EIGHT) {
+      const uint2 cm = load_bytes(t.m, at, t.n, t.vec & kVecM), cv = load_bytes(t.v, at, t.n, t.vec & kVecV);
+      const float2 sc = __ldcs(t.scale + block);
+      const uint32_t wm[2] = {cm.x, cm.y}, wv[2] = {cv.x, cv.y};
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) {
+        const uint32_t a = wm[i / 4] >> (8 * (i & 3)), b = wv[i / 4] >> (8 * (i & 3));
+        m[i] = __uint_as_float(__float_as_uint(from_float8<3, 7>(a & 127)) | (a & 128) << 24) * sc.x;
+        v[i] = from_float8<2, 15>(b & 127) * sc.y;
+      }
+    } else {
+      load8<float>(t.m, at, t.n, t.vec & kVecM, m);
+      load8<float>(t.v, at, t.n, t.vec & kVecV, v);
+    }
+    uint32_t am = 0, av = 0;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      // every product and sum is rounded by itself, in this order: what an 8-bit state becomes is then a function of its inputs' bits
+      const float x = g[i] * scale;
+      m[i] = s.b1 * m[i] + s.b1r * x;
+      v[i] = s.b2 * v[i] + s.b2r * (x * x);
+      am = max(am, __float_as_uint(m[i]) & 0x7FFFFFFFu), av = max(av, __float_as_uint(v[i]) & 0x7FFFFFFFu);
+      float root;
+      asm("sqrt.approx.f32 %0, %1;" : "=f"(root) : "f"(v[i] * ic2));
+      p[i] -= lr * (t.decay * p[i] + __fdividef(m[i] * ic1, root + s.eps));
+    }
+    store8(s.param_dtype, t.param, at, t.n, t.vec & kVecParam, p);
+    if (t.copy) {  // of the weights as they are held
+      if (s.param_dtype != CVLC_F32)
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) p[i] = s.param_dtype == CVLC_F16 ? to_float(from_float<__half>(p[i])) : to_float(from_float<__nv_bfloat16>(p[i]));
+      if (s.copy_dtype == CVLC_F16) store8<__half>(t.copy, at, t.n, t.vec & kVecCopy, p);
+      else store8<__nv_bfloat16>(t.copy, at, t.n, t.vec & kVecCopy, p);
+    }
+    if (EIGHT) {
+      const float a = __uint_as_float(__reduce_max_sync(kFull, am)), b = __uint_as_float(__reduce_max_sync(kFull, av));
+      const float ia = a >= kLeast ? 448.0f * (1.0f / a) : 0.0f, ib = b >= kLeast ? 57344.0f * (1.0f / b) : 0.0f;
+      const uint64_t quad = (uint64_t)at / 4;
+      uint32_t wm[2] = {0, 0}, wv[2] = {0, 0};
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const uint4 r = philox4x32_10(make_uint4((uint32_t)(quad + h), (uint32_t)((quad + h) >> 32), s.tensor0 + index, step),
+                                      make_uint2((uint32_t)s.seed, (uint32_t)(s.seed >> 32)));
+        const uint32_t word[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float x = m[4 * h + i], y = fminf(v[4 * h + i] * ib, 57344.0f);
+          uint32_t c = to_float8<3, 7>(fminf(fabsf(x) * ia, 448.0f), word[i] & 0xFFFF);
+          if (c) c |= __float_as_uint(x) >> 31 << 7;
+          uint32_t d = to_float8<2, 15>(y, word[i] >> 16);
+          // a second moment that is there never becomes 0: the step would divide by eps alone
+          if (y > 0.0f) d = max(d, 1u); else d = 0;
+          wm[h] |= (c & 255) << (8 * i), wv[h] |= (d & 127) << (8 * i);
+        }
+      }
+      store_bytes(t.m, at, t.n, t.vec & kVecM, wm);
+      store_bytes(t.v, at, t.n, t.vec & kVecV, wv);
+      // 0 for a block of zeros; what is not a number stays that
+      if (lane == 0) __stcs(t.scale + block, make_float2(a < kLeast ? 0.0f : a * (1.0f / 448.0f), b < kLeast ? 0.0f : b * (1.0f / 57344.0f)));
+    } else {
+      store8<float>(t.m, at, t.n, t.vec & kVecM, m);
+      store8<float>(t.v, at, t.n, t.vec & kVecV, v);
+    }
+  }
+}
+
+// ---- norm ----------------------------------------------------------------------------------
+// Squares of a lane's 8 values in 32 bits, their sums in 64: the result is right to a rounding and does not depend on the order of blocks.
+__device__ __forceinline__ double sum_of_block(double x, double* shared) {
+#pragma unroll
+  for (int d = 16; d; d /= 2) x += __shfl_xor_sync(kFull, x, d);
+  if ((threadIdx.x & 31) == 0) shared[threadIdx.x / 32] = x;
+  __syncthreads();
+  x = 0.0;
+  for (int i = 0; i < (int)blockDim.x / 32; ++i) x += shared[i];
+  return x;
+}
+template <uint32_t CAP>
+__global__ void __launch_bounds__(kThreads) k_norm_parts(const __grid_constant__ TensorList<CAP> L, double* parts) {
+  __shared__ double shared[kWarps];
+  const StepScalars& s = L.s;
+  const TensorDesc& t = L.t[tensor_of(L, blockIdx.x)];
+  const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x & 31, chunk = blockIdx.x - t.first;
+  const uint64_t blocks = (t.n + t.lead + kBlock - 1) / kBlock, begin = (uint64_t)chunk * s.chunk;
+  const uint32_t mine = (uint32_t)min((uint64_t)s.chunk, blocks - begin);  // blocks of values of this block of threads
+  const int64_t from = (int64_t)(begin * kBlock + lane * kPer) - t.lead;
+  constexpr int kAhead = 4;  // loads of a thread that are on their way together
+  double sum = 0.0;
+  for (uint32_t b = warp; b < mine; b += kAhead * kWarps) {
+    float g[kAhead][kPer];
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      const uint32_t at = b + k * kWarps;
+      load8(s.grad_dtype, t.grad, from + (int64_t)at * kBlock, at < mine ? t.n : 0, t.vec & kVecGrad, g[k]);
+    }
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      float q = 0.0f;
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) q = fmaf(g[k][i], g[k][i], q);
+      sum += (double)q;
+    }
+  }
+  sum = sum_of_block(sum, shared);
+  if (threadIdx.x == 0) parts[blockIdx.x] = sum;
+}
+__global__ void __launch_bounds__(1024) k_norm_join(const double* parts, uint32_t n, float grad_scale, float* norm) {
+  __shared__ double shared[32];
+  pdl_enter();
+  double sum = 0.0;
+  for (uint32_t i = threadIdx.x; i < n; i += blockDim.x) sum += parts[i];
+  sum = sum_of_block(sum, shared);
+  if (threadIdx.x == 0) *norm = (float)(sqrt(sum) * fabs((double)grad_scale));
+}
+
+// ---- launching -----------------------------------------------------------------------------
+
+// Blocks of values in a chunk, the work of a block of threads: short ones where there is little to do, so that all SMs have some, longer ones
+// so that finding the tensor does not count.
+uint64_t blocks_of(const cvlc_adamw_tensor* t, uint32_t n) {
+  uint64_t blocks = 0;
+  for (uint32_t i = 0; i < n; ++i) blocks += (t[i].n + kPer + kBlock - 1) / kBlock;
+  return blocks;
+}
+uint32_t step_chunk(uint64_t blocks) {
+  uint32_t chunk = kWarps;
+  while (chunk < 4 * kWarps && blocks / (2 * chunk) >= 8 * kNumSM) chunk *= 2;
+  return chunk;
+}
+uint32_t norm_chunk(uint64_t blocks) {
+  uint32_t chunk = kWarps;
+  while (chunk < 4 * kWarps && blocks / (2 * chunk) >= 2 * kNumSM) chunk *= 2;
+  while (blocks / chunk >= kNormChunks) chunk *= 2;
+  return chunk;
+}
+uint32_t misplaced(const void* p, size_t size, uint32_t per) { return (uint32_t)(reinterpret_cast<uintptr_t>(p) / size % per); }
+
+TensorDesc describe(const cvlc_adamw_tensor& t, const StepScalars& s, uint32_t bits, bool norm) {
+  auto bytes = [](uint32_t dtype) { return dtype == CVLC_F32 ? (size_t)4 : (size_t)2; };
+  TensorDesc d = {};
+  d.n = t.n, d.grad = t.grad_dev;
+  const size_t size_g = bytes(s.grad_dtype);
+  if (norm) {
+    d.lead = (uint16_t)misplaced(t.grad_dev, size_g, kPer);
+    d.vec = kVecGrad;
+    return d;
+  }
+  d.param = t.param_dev, d.m = t.m_dev, d.v = t.v_dev, d.scale = reinterpret_cast<float2*>(t.scale_dev), d.copy = t.copy_dev;
+  d.lr = t.lr, d.decay = t.weight_decay;
+  const size_t size_p = bytes(s.param_dtype), size_s = bits == 8 ? 1 : 4;
+  if (bits != 8) d.lead = (uint16_t)misplaced(t.param_dev, size_p, kPer);
+  auto fits = [&](const void* p, size_t size, size_t vector) { return (reinterpret_cast<uintptr_t>(p) + vector * 64 - d.lead * size) % vector == 0; };
+  d.vec = (fits(t.param_dev, size_p, 16) ? kVecParam : 0) | (fits(t.grad_dev, size_g, 16) ? kVecGrad : 0) |
+          (fits(t.m_dev, size_s, bits == 8 ? 8 : 16) ? kVecM : 0) | (fits(t.v_dev, size_s, bits == 8 ? 8 : 16) ? kVecV : 0) |
+          (fits(t.copy_dev, 2, 16) ? kVecCopy : 0);
+  return d;
+}
+
+// Calls f with the descriptors of at most CAP tensors from `at` on; false behind the last one
+template <uint32_t CAP, class F>
+cudaError_t with_list(const cvlc_adamw_tensor* t, uint32_t n, const StepScalars& s, uint32_t bits, bool norm, uint32_t tensor0, F&& f) {
+  TensorList<CAP> L;
+  L.s = s;
+  L.s.tensor0 = tensor0;
+  L.n = 0, L.chunks = 0;
+  for (uint32_t i = 0; i < n; ++i) {
+    TensorDesc& d = L.t[L.n++];
+    d = describe(t[i], s, bits, norm);
+    d.first = L.chunks;
+    const uint64_t blocks = (d.n + d.lead + kBlock - 1) / kBlock;
+    L.chunks += (uint32_t)((blocks + s.chunk - 1) / s.chunk);
+  }
+  if (L.chunks == 0) return cudaSuccess;
+  f(L);
+  return cudaGetLastError();
+}
+template <class F>
+cudaError_t by_lists(const cvlc_adamw_tensor* t, uint32_t n, const StepScalars& s, uint32_t bits, bool norm, F&& f) {
+  for (uint32_t at = 0; at < n;) {
+    const uint32_t left = n - at, now = left < kMany ? left : kMany;
+    const cudaError_t e = now <= kFew    ? with_list<kFew>(t + at, now, s, bits, norm, at, f)
+                          : now <= kSome ? with_list<kSome>(t + at, now, s, bits, norm, at, f)
+                                         : with_list<kMany>(t + at, now, s, bits, norm, at, f);
+    if (e != cudaSuccess) return e;
+    at += now;
+  }
+  return cudaSuccess;
+}
+template <uint32_t CAP>
+void run_step(const TensorList<CAP>& L, uint32_t bits, cudaStream_t st) {
+  if (bits == 8) launch_kernel(kKAdamw, k_adamw<true, CAP>, dim3(L.chunks), dim3(kThreads), 0, st, false, L);
+  else launch_kernel(kKAdamw, k_adamw<false, CAP>, dim3(L.chunks), dim3(kThreads), 0, st, false, L);
+}
+
+}  // namespace
+
+cudaError_t launch_adamw(const cvlc_adamw_tensor* t, uint32_t n, const cvlc_adamw_args& a, cudaStream_t st) {
+  StepScalars s = {};
+  s.lr = (float)a.lr, s.b1 = (float)a.beta1, s.b1r = (float)(1.0 - a.beta1), s.b2 = (float)a.beta2, s.b2r = (float)(1.0 - a.beta2), s.eps = (float)a.eps;
+  s.beta1 = a.beta1, s.beta2 = a.beta2;
+  s.ic1 = (float)(1.0 / (1.0 - pow(a.beta1, (double)a.step))), s.ic2 = (float)(1.0 / (1.0 - pow(a.beta2, (double)a.step)));
+  s.grad_scale = a.grad_scale, s.max_norm = a.max_norm, s.norm = a.norm_dev, s.lr_dev = a.lr_dev, s.step_dev = a.step_dev, s.seed = a.seed, s.step = a.step;
+  s.param_dtype = a.param_dtype, s.grad_dtype = a.grad_dtype, s.copy_dtype = a.copy_dtype, s.status = a.status_dev;
+  s.chunk = step_chunk(blocks_of(t, n));
+  return by_lists(t, n, s, a.state_bits, false, [&](const auto& L) { run_step(L, a.state_bits, st); });
+}
+
+size_t norm_ws_bytes(uint32_t n) { return align256(((size_t)kNormChunks + n) * sizeof(double)); }
+
+cudaError_t launch_grad_norm(const cvlc_adamw_tensor* t, uint32_t n, uint32_t dtype, float grad_scale, float* norm, void* ws, cudaStream_t st) {
+  StepScalars s = {};
+  s.grad_dtype = dtype;
+  s.chunk = norm_chunk(blocks_of(t, n));
+  double* parts = static_cast<double*>(ws);
+  uint32_t made = 0;
+  const cudaError_t e = by_lists(t, n, s, 32, true, [&](const auto& L) {
+    launch_kernel(kKNormParts, k_norm_parts<sizeof(L.t) / sizeof(L.t[0])>, dim3(L.chunks), dim3(kThreads), 0, st, false, L, parts + made);
+    made += L.chunks;
+  });
+  if (e != cudaSuccess) return e;
+  launch_kernel(kKNormJoin, k_norm_join, dim3(1), dim3(made > 256 ? 1024 : 256), 0, st, made != 0, parts, made, grad_scale, norm);
+  return cudaGetLastError();
+}
+
+}  // namespace cvlc

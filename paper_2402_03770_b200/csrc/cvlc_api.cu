@@ -208,6 +208,28 @@ bool embed_ok(uint32_t dtype, uint64_t vocab, uint32_t dim, const void* tokens, 
 }
 bool rows_ok(const void* at, size_t size, uint32_t dim, uint64_t stride) { return aligned(at, size) && stride >= dim && stride <= (1ull << 32); }
 
+constexpr uint64_t kMostValues = 1ull << 40;  // of all tensors of a call
+bool add_values(uint64_t n, uint64_t* total) {
+  if (n > kMostValues || *total + n > kMostValues) return false;
+  *total += n;
+  return true;
+}
+bool adamw_ok(const cvlc_adamw_args& a) {
+  return element_bytes(a.param_dtype) && element_bytes(a.grad_dtype) && (a.state_bits == 8 || a.state_bits == 32) && std::isfinite(a.lr) &&
+         std::fabs(a.lr) < 1e38 && a.beta1 >= 0.0 && a.beta1 < 1.0 && a.beta2 >= 0.0 && a.beta2 < 1.0 && a.eps >= 1e-30 && a.eps < 1e38 &&
+         (a.step_dev || a.step >= 1) && std::isfinite(a.grad_scale) && (!a.norm_dev || a.max_norm > 0.0f) &&
+         (!a.norm_dev || aligned(a.norm_dev, 4)) && (!a.lr_dev || aligned(a.lr_dev, 4)) && (!a.step_dev || aligned(a.step_dev, 4)) &&
+         (!a.status_dev || aligned(a.status_dev, 4));
+}
+bool adamw_tensor_ok(const cvlc_adamw_tensor& t, const cvlc_adamw_args& a, uint64_t* total) {
+  if (!add_values(t.n, total) || !std::isfinite(t.lr) || !std::isfinite(t.weight_decay)) return false;
+  if (t.n == 0) return true;
+  const size_t state = a.state_bits == 8 ? 1 : 4;
+  return aligned(t.param_dev, element_bytes(a.param_dtype)) && aligned(t.grad_dev, element_bytes(a.grad_dtype)) && aligned(t.m_dev, state) &&
+         aligned(t.v_dev, state) && (a.state_bits == 32 || aligned(t.scale_dev, 8)) &&
+         (!t.copy_dev || (a.copy_dtype != CVLC_F32 && element_bytes(a.copy_dtype) && aligned(t.copy_dev, 2)));
+}
+
 }  // namespace
 
 extern "C" {
@@ -721,6 +743,29 @@ int cvlc_embed_grad(const void* tokens_dev, uint32_t token_bytes, uint64_t n, co
   if (ws_bytes < embed_grad_ws_bytes(n, dim)) return CVLC_ERR_WORKSPACE_TOO_SMALL;
   const EmbedGradArgs a = {tokens_dev, grad_dev, vocab, n, grad_stride, update_stride, dim, token_bytes, scale, update_dev, accumulate, ws_dev};
   return launch_embed_grad(a, dtype, static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess ? CVLC_OK : CVLC_ERR_CUDA;
+}
+
+int cvlc_adamw(const cvlc_adamw_tensor* tensors, uint32_t n_tensors, const cvlc_adamw_args* a, void* cuda_stream) {
+  if (!a || (n_tensors && !tensors) || !adamw_ok(*a)) return CVLC_ERR_INVALID_ARG;
+  uint64_t total = 0;
+  for (uint32_t i = 0; i < n_tensors; ++i)
+    if (!adamw_tensor_ok(tensors[i], *a, &total)) return CVLC_ERR_INVALID_ARG;
+  return launch_adamw(tensors, n_tensors, *a, static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess ? CVLC_OK : CVLC_ERR_CUDA;
+}
+
+size_t cvlc_grad_norm_workspace_bytes(uint32_t n_tensors) { return norm_ws_bytes(n_tensors ? n_tensors : 1); }
+
+int cvlc_grad_norm(const cvlc_adamw_tensor* tensors, uint32_t n_tensors, uint32_t grad_dtype, float grad_scale, float* norm_dev,
+                   void* ws_dev, size_t ws_bytes, void* cuda_stream) {
+  const size_t size = element_bytes(grad_dtype);
+  if (!size || (n_tensors && !tensors) || !std::isfinite(grad_scale) || !aligned(norm_dev, 4) || !aligned(ws_dev, 256)) return CVLC_ERR_INVALID_ARG;
+  uint64_t total = 0;
+  for (uint32_t i = 0; i < n_tensors; ++i)
+    if (!add_values(tensors[i].n, &total) || (tensors[i].n && !aligned(tensors[i].grad_dev, size))) return CVLC_ERR_INVALID_ARG;
+  if (ws_bytes < cvlc_grad_norm_workspace_bytes(n_tensors)) return CVLC_ERR_WORKSPACE_TOO_SMALL;
+  return launch_grad_norm(tensors, n_tensors, grad_dtype, grad_scale, norm_dev, ws_dev, static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess
+             ? CVLC_OK
+             : CVLC_ERR_CUDA;
 }
 
 int cvlc_read_status(const void* plan_or_ws_dev, void* cuda_stream) {

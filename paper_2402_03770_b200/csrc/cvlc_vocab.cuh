@@ -1,5 +1,5 @@
-// The two ends of a client's local step at which the vocabulary is: rows of logits (top logits, distillation) and rows of the
-// embedding table (lookup, gradient).  What their kernels share: element types and 16-byte vectors of them.
+// The two ends of a client's local step at which the vocabulary is, rows of logits (top logits, distillation) and rows of the
+// embedding table (lookup, gradient), and the optimiser behind it.  What their kernels share: element types and 16-byte vectors of them.
 #pragma once
 
 #include <cuda_bf16.h>
@@ -69,6 +69,10 @@ struct EmbedGradArgs {
 };
 cudaError_t launch_embed_grad(const EmbedGradArgs& a, uint32_t dtype, cudaStream_t st);
 size_t embed_grad_ws_bytes(uint64_t n, uint32_t dim);
+
+cudaError_t launch_adamw(const cvlc_adamw_tensor* tensors, uint32_t n, const cvlc_adamw_args& a, cudaStream_t st);
+size_t norm_ws_bytes(uint32_t n);
+cudaError_t launch_grad_norm(const cvlc_adamw_tensor* tensors, uint32_t n, uint32_t dtype, float grad_scale, float* norm, void* ws, cudaStream_t st);
 
 #ifdef __CUDACC__
 

@@ -1,0 +1,73 @@
+"""What the optimiser's entry points refuse, without a GPU: every check is made before anything is launched."""
+import ctypes as C
+import math
+
+import pytest
+
+from paper_2402_03770_b200 import binding as B
+
+BAD = B.CVLC_ERR_INVALID_ARG
+AT = 1 << 20  # an address that nothing reads
+
+
+def args(**kw):
+    a = dict(param_dtype=B.CVLC_F32, grad_dtype=B.CVLC_F32, copy_dtype=B.CVLC_BF16, state_bits=32, lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, seed=0, step=1,
+             grad_scale=1.0, max_norm=1.0, reserved=0, norm_dev=None, lr_dev=None, step_dev=None, status_dev=None)
+    a.update(kw)
+    return B.CvlcAdamwArgs(**a)
+
+
+def tensor(**kw):
+    a = dict(n=10, grad_dev=AT, param_dev=AT, m_dev=AT, v_dev=AT, scale_dev=None, copy_dev=None, lr=1.0, weight_decay=0.0)
+    a.update(kw)
+    return B.CvlcAdamwTensor(**a)
+
+
+def step(tensors, a):
+    return B.lib().cvlc_adamw((B.CvlcAdamwTensor * max(1, len(tensors)))(*tensors), len(tensors), C.byref(a), None)
+
+
+@pytest.mark.parametrize("kw", [
+    dict(param_dtype=3), dict(grad_dtype=9), dict(state_bits=16), dict(lr=math.nan), dict(lr=math.inf), dict(lr=1e39), dict(beta1=1.0), dict(beta1=-0.1),
+    dict(beta2=1.0), dict(beta2=math.nan), dict(eps=0.0), dict(eps=-1.0), dict(eps=1e-31), dict(eps=math.inf), dict(step=0), dict(grad_scale=math.inf),
+    dict(norm_dev=AT, max_norm=0.0), dict(norm_dev=AT, max_norm=math.nan), dict(norm_dev=AT + 2), dict(lr_dev=AT + 1), dict(step_dev=AT + 2),
+    dict(status_dev=AT + 2)])
+def test_adamw_refuses(kw):
+    assert step([tensor(scale_dev=AT)], args(**kw)) == BAD
+
+
+@pytest.mark.parametrize("kw,a", [
+    (dict(n=(1 << 40) + 1), {}), (dict(grad_dev=None), {}), (dict(param_dev=None), {}), (dict(m_dev=None), {}), (dict(v_dev=None), {}), (dict(grad_dev=AT + 2), {}),
+    (dict(param_dev=AT + 1), dict(param_dtype=B.CVLC_BF16)), (dict(m_dev=AT + 2), {}), (dict(scale_dev=None), dict(state_bits=8)),
+    (dict(scale_dev=AT + 4), dict(state_bits=8)), (dict(copy_dev=AT + 1), {}), (dict(copy_dev=AT), dict(copy_dtype=B.CVLC_F32)), (dict(lr=math.nan), {}),
+    (dict(weight_decay=math.inf), {})])
+def test_adamw_refuses_tensors(kw, a):
+    assert step([tensor(), tensor(**kw)], args(**a)) == BAD
+
+
+def test_nothing_to_do():
+    assert step([], args()) == B.CVLC_OK
+    assert step([tensor(n=0, grad_dev=None, param_dev=None, m_dev=None, v_dev=None)], args()) == B.CVLC_OK
+    assert B.lib().cvlc_adamw(None, 1, C.byref(args()), None) == BAD and B.lib().cvlc_adamw(None, 0, None, None) == BAD
+
+
+def test_all_tensors_count():
+    assert step([tensor(n=1 << 39), tensor(n=(1 << 39) + 1)], args()) == BAD
+
+
+@pytest.mark.parametrize("kw", [dict(dtype=3), dict(scale=math.nan), dict(norm=None), dict(norm=AT + 2), dict(ws=None), dict(ws=AT + 128)])
+def test_norm_refuses(kw):
+    a = dict(dtype=B.CVLC_F32, scale=1.0, norm=AT, ws=AT)
+    a.update(kw)
+    t = tensor()
+    assert B.lib().cvlc_grad_norm(C.byref(t), 1, a["dtype"], a["scale"], a["norm"], a["ws"], 1 << 20, None) == BAD
+
+
+def test_norm_workspace():
+    need = B.lib().cvlc_grad_norm_workspace_bytes(1)
+    assert need > 0 and need % 256 == 0 and B.lib().cvlc_grad_norm_workspace_bytes(2000) > need and B.lib().cvlc_grad_norm_workspace_bytes(0) == need
+    t = tensor()
+    assert B.lib().cvlc_grad_norm(C.byref(t), 1, 0, 1.0, AT, AT, need - 1, None) == B.CVLC_ERR_WORKSPACE_TOO_SMALL
+    t = tensor(grad_dev=AT + 2)
+    assert B.lib().cvlc_grad_norm(C.byref(t), 1, 0, 1.0, AT, AT, need, None) == BAD
+    assert C.sizeof(B.CvlcAdamwTensor) == 64 and C.sizeof(B.CvlcAdamwArgs) == 104
