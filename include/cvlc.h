@@ -518,6 +518,50 @@ int cvlc_embed_grad(const void* tokens_dev, uint32_t token_bytes, uint64_t n, co
                     uint32_t dim, uint64_t grad_stride, uint64_t vocab, float scale, float* update_dev,
                     uint64_t update_stride, int accumulate, void* ws_dev, size_t ws_bytes, void* cuda_stream);
 
+/*
+ * The training loss of such a model: softmax cross entropy of hidden states against the head, the matrix whose rows are the words (the
+ * embedding table itself, or one of its own), without ever holding the logits.  With z = scale hidden_t . head_v,
+ *   loss_t = row_weight_t (ln sum_v exp(z_tv) - z_t,target)
+ * and, for cvlc_head_step, the gradients of the sum of all losses, d_hidden and d_head, in the operands' type.
+ * A target below 0 is none, and a row without one, or of weight 0, counts for nothing, whatever it holds: its loss, its gradient and
+ * its part of d_head are 0.  A target >= vocab is treated as none and reported (INVALID_ARG) in *status_dev (one int32 of the caller's,
+ * 0 beforehand; or NULL).  An infinite or NaN logit makes the row's loss, and what the row has a part in, not finite.
+ * The products are made by the tensor cores: operands in 16 bits (CVLC_F16 or CVLC_BF16; there is no product of fp32), sums in fp32.  A logit's
+ * gradient, row_weight (softmax - one for the target), is rounded to the operands' type (in fp16 times a power of two that keeps the largest row_weight at
+ * 2^15), as the operand of the two products that follow; d_hidden and d_head are rounded once more.
+ *  hidden_dev   rows x dim, hidden_stride elements apart; head_dev: vocab x dim, head_stride apart.  Rows that begin on 16 bytes are
+ *               read where they are, others are copied first
+ *  targets_dev  rows words of int32 or int64 (token_bytes 4 or 8);  row_weight_dev: rows fp32, or NULL: all 1
+ *  pieces       cvlc_head_step makes the gradients of so many pieces of the vocabulary (or fewer: a piece has at least 256 words) one behind the other; the workspace holds rows x
+ *               vocab / pieces values of 16 bits
+ *  d_hidden_dev, d_head_dev   as hidden and head, of strides of their own; they must not overlap hidden, head or each other
+ *  ws_dev       cvlc_head_workspace_bytes(a, graded) bytes (graded: 0 for cvlc_head_loss, 1 for cvlc_head_step), 256-byte aligned
+ * Results do not depend on the order in which blocks run.  Waits inside the kernels are bounded (four seconds): should one run out,
+ * CVLC_ERR_DEVICE_TIMEOUT goes to *status_dev, and losses and d_hidden are NaN, d_head undefined.
+ * Errors: INVALID_ARG (dtype, vocab from 1 to CVLC_MAX_VOCAB, dim from 1 to 65536, rows above 2^24, a stride below dim or above 2^32, a scale that
+ * is not finite, pieces of 0, alignment, overlap), WORKSPACE_TOO_SMALL.  rows = 0 writes zeros to d_head.
+ */
+typedef struct cvlc_head {
+  const void* hidden_dev;
+  const void* head_dev;
+  const void* targets_dev;
+  const float* row_weight_dev;
+  int32_t* status_dev;
+  uint64_t rows;
+  uint64_t hidden_stride;
+  uint64_t head_stride;
+  uint32_t vocab;
+  uint32_t dim;
+  uint32_t dtype;
+  uint32_t token_bytes;
+  float scale;
+  uint32_t pieces;
+} cvlc_head;
+size_t cvlc_head_workspace_bytes(const cvlc_head* a, int graded);
+int cvlc_head_loss(const cvlc_head* a, float* loss_dev, void* ws_dev, size_t ws_bytes, void* cuda_stream);
+int cvlc_head_step(const cvlc_head* a, float* loss_dev, void* d_hidden_dev, uint64_t d_hidden_stride, void* d_head_dev,
+                   uint64_t d_head_stride, void* ws_dev, size_t ws_bytes, void* cuda_stream);
+
 /* --- the optimiser of a local step, and of the server ------------------------- */
 
 /*
@@ -621,7 +665,8 @@ int cvlc_selftest_ring(const float* row_dev, uint32_t stages, int give_back, uin
  * k_pack, k_decode_prepare, k_fill_zero, k_prefetch_l2, k_decode,
  * k_noalloc_publish_status, k_selftest, k_hist_check, k_apply, k_plan_literal, k_ec_accumulate, k_pack_unframed, k_decode_unframed,
  * k_top_logits, k_distill_loss, k_distill_grad, k_distill_step, k_embed, k_token_sort, k_embed_sum, k_embed_join,
- * k_adamw, k_norm_parts, k_norm_join. */
+ * k_adamw, k_norm_parts, k_norm_join,
+ * k_head_begin, k_head_align, k_head_stats, k_head_rows, k_head_probs, k_head_parts, k_head_grad, k_head_join. */
 unsigned long long cvlc_launch_count(const char* kernel_name);
 /* Optional kernel timing: after cvlc_profile_select(name, n) the next n launches of that kernel
  * ("*" = of every kernel) are bracketed by a CUDA event pair on their own stream;

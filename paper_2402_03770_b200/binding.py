@@ -59,7 +59,8 @@ EXPORTS = [
     "cvlc_plan_literal_workspace_bytes", "cvlc_ec_accumulate_batch", "cvlc_encode_batch_ec",
     "cvlc_unframed_stream_capacity", "cvlc_unframed_workspace_bytes", "cvlc_encode_unframed_batch", "cvlc_decode_aggregate_unframed",
     "cvlc_top_logits", "cvlc_distill_loss", "cvlc_distill_grad", "cvlc_distill_step", "cvlc_embed", "cvlc_embed_grad_workspace_bytes",
-    "cvlc_embed_grad", "cvlc_adamw", "cvlc_grad_norm", "cvlc_grad_norm_workspace_bytes", "cvlc_launch_count", "cvlc_profile_select", "cvlc_profile_reset", "cvlc_profile_read",
+    "cvlc_embed_grad", "cvlc_adamw", "cvlc_grad_norm", "cvlc_grad_norm_workspace_bytes",
+    "cvlc_head_workspace_bytes", "cvlc_head_loss", "cvlc_head_step", "cvlc_launch_count", "cvlc_profile_select", "cvlc_profile_reset", "cvlc_profile_read",
 ]
 
 
@@ -94,6 +95,14 @@ class CvlcDistill(C.Structure):
         ("logits_dev", C.c_void_p), ("rows", C.c_uint64), ("row_stride", C.c_uint64), ("vocab", C.c_uint32), ("dtype", C.c_uint32),
         ("ids_dev", C.c_void_p), ("logp_dev", C.c_void_p), ("k", C.c_uint32), ("rest", C.c_uint32), ("temperature", C.c_float),
         ("reserved", C.c_uint32), ("row_weight_dev", C.c_void_p), ("status_dev", C.c_void_p),
+    ]
+
+
+class CvlcHead(C.Structure):
+    _fields_ = [
+        ("hidden_dev", C.c_void_p), ("head_dev", C.c_void_p), ("targets_dev", C.c_void_p), ("row_weight_dev", C.c_void_p), ("status_dev", C.c_void_p),
+        ("rows", C.c_uint64), ("hidden_stride", C.c_uint64), ("head_stride", C.c_uint64), ("vocab", C.c_uint32), ("dim", C.c_uint32),
+        ("dtype", C.c_uint32), ("token_bytes", C.c_uint32), ("scale", C.c_float), ("pieces", C.c_uint32),
     ]
 
 
@@ -209,6 +218,13 @@ def lib() -> C.CDLL:
     L.cvlc_embed_grad_workspace_bytes.argtypes = [u64, u32, u64]
     L.cvlc_embed_grad.restype = C.c_int
     L.cvlc_embed_grad.argtypes = [vp, u32, u64, vp, u32, u32, u64, u64, C.c_float, vp, u64, C.c_int, vp, sz, vp]
+    PH = C.POINTER(CvlcHead)
+    L.cvlc_head_workspace_bytes.restype = sz
+    L.cvlc_head_workspace_bytes.argtypes = [PH, C.c_int]
+    L.cvlc_head_loss.restype = C.c_int
+    L.cvlc_head_loss.argtypes = [PH, vp, vp, sz, vp]
+    L.cvlc_head_step.restype = C.c_int
+    L.cvlc_head_step.argtypes = [PH, vp, vp, u64, vp, u64, vp, sz, vp]
     PT = C.POINTER(CvlcAdamwTensor)
     L.cvlc_adamw.restype = C.c_int
     L.cvlc_adamw.argtypes = [PT, u32, C.POINTER(CvlcAdamwArgs), vp]
@@ -667,6 +683,45 @@ def cvlc_embed_grad(tokens: torch.Tensor, grad: torch.Tensor, update: torch.Tens
                                  scale, u, update_stride, 1 if accumulate else 0, _ptr(ws), _nbytes(ws), _stream_on(stream, device)), "cvlc_embed_grad")
 
 
+def _head(hidden: torch.Tensor, head: torch.Tensor, targets: Optional[torch.Tensor], scale: float, row_weight: Optional[torch.Tensor],
+          pieces: int, status: Optional[torch.Tensor], device: int) -> CvlcHead:
+    h, hidden_stride = _rows(hidden, device)
+    w, head_stride = _rows(head, device)
+    (rows, dim), vocab = hidden.shape, head.shape[0]
+    assert head.shape[1] == dim and head.dtype == hidden.dtype
+    t = None if targets is None else _here(targets, targets.dtype, (rows,), device)
+    return CvlcHead(h, w, t, _here(row_weight, torch.float32, (rows,), device), _here(status, torch.int32, (1,), device), rows, hidden_stride, head_stride,
+                    vocab, dim, _DTYPES[hidden.dtype], 4 if targets is None else _token_bytes(targets), scale, pieces)
+
+
+def cvlc_head_workspace_bytes(hidden: torch.Tensor, head: torch.Tensor, pieces: int = 1) -> int:
+    """for cvlc_head_step with so many pieces of the vocabulary; 0: for cvlc_head_loss"""
+    a = _head(hidden, head, None, 1.0, None, max(pieces, 1), None, hidden.get_device())
+    return int(lib().cvlc_head_workspace_bytes(C.byref(a), 1 if pieces else 0))
+
+
+def cvlc_head_loss(hidden: torch.Tensor, head: torch.Tensor, targets: torch.Tensor, loss: torch.Tensor, ws: torch.Tensor, *, scale: float = 1.0,
+                   row_weight: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> None:
+    """loss[rows] = row_weight * cross entropy of softmax(scale * hidden @ head.T) at targets (int32 or int64; below 0: none)."""
+    device = _device()
+    a = _head(hidden, head, targets, scale, row_weight, 1, status, device)
+    assert ws.get_device() == device
+    _check(lib().cvlc_head_loss(C.byref(a), _here(loss, torch.float32, (a.rows,), device), _ptr(ws), _nbytes(ws), _stream_on(stream, device)), "cvlc_head_loss")
+
+
+def cvlc_head_step(hidden: torch.Tensor, head: torch.Tensor, targets: torch.Tensor, loss: torch.Tensor, d_hidden: torch.Tensor, d_head: torch.Tensor,
+                   ws: torch.Tensor, *, scale: float = 1.0, row_weight: Optional[torch.Tensor] = None, pieces: int = 1,
+                   status: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> None:
+    """cvlc_head_loss, and the gradients of the sum of the losses: d_hidden (as hidden) and d_head (as head)."""
+    device = _device()
+    a = _head(hidden, head, targets, scale, row_weight, pieces, status, device)
+    assert ws.get_device() == device and d_hidden.shape == hidden.shape and d_head.shape == head.shape
+    assert d_hidden.dtype == hidden.dtype and d_head.dtype == head.dtype
+    (dh, dh_stride), (dw, dw_stride) = _rows(d_hidden, device), _rows(d_head, device)
+    _check(lib().cvlc_head_step(C.byref(a), _here(loss, torch.float32, (a.rows,), device), dh, dh_stride, dw, dw_stride, _ptr(ws), _nbytes(ws),
+                                _stream_on(stream, device)), "cvlc_head_step")
+
+
 class AdamwTensors:
     """The tensors of cvlc_adamw and cvlc_grad_norm, made once for all steps: gradients, and for the step weights, states and, with states of
     8 bits (m in e4m3, v in e5m2, uint8 or those types), scales of shape (blocks of STATE_BLOCK values, 2).  Tensors are contiguous and stay where
@@ -772,7 +827,8 @@ KERNEL_NAMES = ["k_zero_words", "k_client", "k_hist", "k_plan_threshold", "k_pla
                 "k_select_lookback", "k_rank_split", "k_rank", "k_rank_rest", "k_sort", "k_pack", "k_decode_prepare", "k_fill_zero",
                 "k_prefetch_l2", "k_decode", "k_noalloc_publish_status", "k_selftest", "k_hist_check", "k_apply", "k_plan_literal", "k_ec_accumulate", "k_pack_unframed", "k_decode_unframed",
                 "k_top_logits", "k_distill_loss", "k_distill_grad", "k_distill_step", "k_embed", "k_token_sort", "k_embed_sum", "k_embed_join",
-                "k_adamw", "k_norm_parts", "k_norm_join"]
+                "k_adamw", "k_norm_parts", "k_norm_join",
+                "k_head_begin", "k_head_align", "k_head_stats", "k_head_rows", "k_head_probs", "k_head_parts", "k_head_grad", "k_head_join"]
 
 
 def cvlc_profile_read(kernel_name: str = "*"):

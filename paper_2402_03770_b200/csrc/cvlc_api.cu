@@ -208,6 +208,25 @@ bool embed_ok(uint32_t dtype, uint64_t vocab, uint32_t dim, const void* tokens, 
 }
 bool rows_ok(const void* at, size_t size, uint32_t dim, uint64_t stride) { return aligned(at, size) && stride >= dim && stride <= (1ull << 32); }
 
+// sizes and types of a head: what its workspace depends on
+bool head_shape_ok(const cvlc_head& a) {
+  return element_bytes(a.dtype) == 2 && a.vocab >= 1 && a.vocab <= CVLC_MAX_VOCAB && a.dim >= 1 && a.dim <= 65536 && a.rows <= (1ull << 24) && a.pieces >= 1 &&
+         a.hidden_stride >= a.dim && a.hidden_stride <= (1ull << 32) && a.head_stride >= a.dim && a.head_stride <= (1ull << 32);
+}
+bool head_ok(const cvlc_head& a) {
+  return head_shape_ok(a) && std::isfinite(a.scale) && (a.token_bytes == 4 || a.token_bytes == 8) && aligned(a.head_dev, 2) &&
+         (a.rows == 0 || (aligned(a.hidden_dev, 2) && aligned(a.targets_dev, a.token_bytes))) && (!a.row_weight_dev || aligned(a.row_weight_dev, 4)) &&
+         (!a.status_dev || aligned(a.status_dev, 4));
+}
+// rows of two matrices that have no byte in common: apart, or beside each other in rows of the same stride
+bool rows_apart(const void* p, uint64_t p_rows, uint64_t p_stride, const void* q, uint64_t q_rows, uint64_t q_stride, uint64_t row) {
+  if (p_rows == 0 || q_rows == 0) return true;
+  const uintptr_t x = reinterpret_cast<uintptr_t>(p), y = reinterpret_cast<uintptr_t>(q);
+  if (x >= y + (q_rows - 1) * q_stride + row || y >= x + (p_rows - 1) * p_stride + row) return true;
+  const uint64_t between = (x > y ? x - y : y - x) % p_stride;
+  return p_stride == q_stride && between >= row && p_stride - between >= row;
+}
+
 constexpr uint64_t kMostValues = 1ull << 40;  // of all tensors of a call
 bool add_values(uint64_t n, uint64_t* total) {
   if (n > kMostValues || *total + n > kMostValues) return false;
@@ -743,6 +762,36 @@ int cvlc_embed_grad(const void* tokens_dev, uint32_t token_bytes, uint64_t n, co
   if (ws_bytes < embed_grad_ws_bytes(n, dim)) return CVLC_ERR_WORKSPACE_TOO_SMALL;
   const EmbedGradArgs a = {tokens_dev, grad_dev, vocab, n, grad_stride, update_stride, dim, token_bytes, scale, update_dev, accumulate, ws_dev};
   return launch_embed_grad(a, dtype, static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess ? CVLC_OK : CVLC_ERR_CUDA;
+}
+
+size_t cvlc_head_workspace_bytes(const cvlc_head* a, int graded) {
+  return a && head_shape_ok(*a) ? head_ws_bytes(*a, graded ? a->pieces : 0) : 0;
+}
+
+int cvlc_head_loss(const cvlc_head* a, float* loss_dev, void* ws_dev, size_t ws_bytes, void* cuda_stream) {
+  if (!a || !head_ok(*a)) return CVLC_ERR_INVALID_ARG;
+  if (a->rows == 0) return CVLC_OK;
+  if (!aligned(loss_dev, 4) || !aligned(ws_dev, 256)) return CVLC_ERR_INVALID_ARG;
+  if (ws_bytes < head_ws_bytes(*a, 0)) return CVLC_ERR_WORKSPACE_TOO_SMALL;
+  return launch_head(*a, 0, loss_dev, nullptr, 0, nullptr, 0, ws_dev, static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess ? CVLC_OK : CVLC_ERR_CUDA;
+}
+
+int cvlc_head_step(const cvlc_head* a, float* loss_dev, void* d_hidden_dev, uint64_t d_hidden_stride, void* d_head_dev,
+                   uint64_t d_head_stride, void* ws_dev, size_t ws_bytes, void* cuda_stream) {
+  if (!a || !head_ok(*a) || !rows_ok(d_head_dev, 2, a->dim, d_head_stride)) return CVLC_ERR_INVALID_ARG;
+  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  const uint64_t row = (uint64_t)a->dim * 2;
+  if (a->rows == 0)
+    return cudaMemset2DAsync(d_head_dev, d_head_stride * 2, 0, row, a->vocab, st) == cudaSuccess ? CVLC_OK : CVLC_ERR_CUDA;
+  if (!rows_ok(d_hidden_dev, 2, a->dim, d_hidden_stride) || !aligned(loss_dev, 4) || !aligned(ws_dev, 256)) return CVLC_ERR_INVALID_ARG;
+  if (!rows_apart(a->hidden_dev, a->rows, a->hidden_stride * 2, d_hidden_dev, a->rows, d_hidden_stride * 2, row) ||
+      !rows_apart(a->hidden_dev, a->rows, a->hidden_stride * 2, d_head_dev, a->vocab, d_head_stride * 2, row) ||
+      !rows_apart(a->head_dev, a->vocab, a->head_stride * 2, d_hidden_dev, a->rows, d_hidden_stride * 2, row) ||
+      !rows_apart(a->head_dev, a->vocab, a->head_stride * 2, d_head_dev, a->vocab, d_head_stride * 2, row) ||
+      !rows_apart(d_hidden_dev, a->rows, d_hidden_stride * 2, d_head_dev, a->vocab, d_head_stride * 2, row))
+    return CVLC_ERR_INVALID_ARG;
+  if (ws_bytes < head_ws_bytes(*a, a->pieces)) return CVLC_ERR_WORKSPACE_TOO_SMALL;
+  return launch_head(*a, a->pieces, loss_dev, d_hidden_dev, d_hidden_stride, d_head_dev, d_head_stride, ws_dev, st) == cudaSuccess ? CVLC_OK : CVLC_ERR_CUDA;
 }
 
 int cvlc_adamw(const cvlc_adamw_tensor* tensors, uint32_t n_tensors, const cvlc_adamw_args* a, void* cuda_stream) {

@@ -368,7 +368,8 @@ enum KernelId {
   kKZeroWords = 0, kKClient, kKHist, kKPlanThreshold, kKPlanFit, kKPlanTune, kKEncodeInit, kKSelect, kKSelectLookback, kKRankSplit, kKRank,
   kKRankRest, kKSort, kKPack, kKDecodePrepare, kKFillZero, kKPrefetchL2, kKDecode, kKNoallocStatus, kKSelftest, kKHistCheck, kKApply,
   kKPlanLiteral, kKEcAccumulate, kKPackUnframed, kKDecodeUnframed, kKTopLogits, kKDistillLoss,
-  kKDistillGrad, kKDistillStep, kKEmbed, kKTokenSort, kKEmbedSum, kKEmbedJoin, kKAdamw, kKNormParts, kKNormJoin, kNumKernelIds
+  kKDistillGrad, kKDistillStep, kKEmbed, kKTokenSort, kKEmbedSum, kKEmbedJoin, kKAdamw, kKNormParts, kKNormJoin,
+  kKHeadBegin, kKHeadAlign, kKHeadStats, kKHeadRows, kKHeadProbs, kKHeadParts, kKHeadGrad, kKHeadJoin, kNumKernelIds
 };
 
 // Called around every kernel launch.  Counts launches; when a kernel has been selected with

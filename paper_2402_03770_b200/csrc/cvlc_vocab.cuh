@@ -70,6 +70,10 @@ struct EmbedGradArgs {
 cudaError_t launch_embed_grad(const EmbedGradArgs& a, uint32_t dtype, cudaStream_t st);
 size_t embed_grad_ws_bytes(uint64_t n, uint32_t dim);
 
+size_t head_ws_bytes(const cvlc_head& a, uint32_t pieces);
+cudaError_t launch_head(const cvlc_head& a, uint32_t pieces, float* loss, void* d_hidden, uint64_t d_hidden_stride, void* d_head, uint64_t d_head_stride, void* ws,
+                        cudaStream_t st);  // pieces = 0: the loss alone
+
 cudaError_t launch_adamw(const cvlc_adamw_tensor* tensors, uint32_t n, const cvlc_adamw_args& a, cudaStream_t st);
 size_t norm_ws_bytes(uint32_t n);
 cudaError_t launch_grad_norm(const cvlc_adamw_tensor* tensors, uint32_t n, uint32_t dtype, float grad_scale, float* norm, void* ws, cudaStream_t st);

@@ -1,0 +1,203 @@
+"""Cross entropy against a head and its gradients, at the sizes where tiles, pieces and alignment end."""
+import math
+
+import pytest
+import torch
+
+import head_ref as R
+from paper_2402_03770_b200 import binding as B
+
+pytestmark = pytest.mark.gpu
+BF, HF = torch.bfloat16, torch.float16
+
+
+def padded(x, pad, shift=0):
+    rows, cols = x.shape
+    room = torch.zeros(rows * (cols + pad) + shift + 16, dtype=x.dtype, device="cuda")
+    at = room[shift:shift + rows * (cols + pad)].view(rows, cols + pad)[:, :cols]
+    return at.copy_(x)
+
+
+def make(rows, dim, vocab, dtype=BF, pad=0, shift=0, seed=1, width=2.0, wide=True):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    head = padded((torch.randn(vocab, dim, generator=g, device="cuda") * (width / math.sqrt(dim))).to(dtype), pad, shift)
+    t = torch.randint(0, vocab, (rows,), generator=g, device="cuda")
+    lean = torch.rand(rows, 1, generator=g, device="cuda") * 2
+    hidden = padded((torch.randn(rows, dim, generator=g, device="cuda") + lean * head[t].float()).to(dtype), pad, shift)
+    return hidden, head, t if wide else t.int()
+
+
+def space(hidden, head, pieces):
+    ws = B.alloc_bytes(B.cvlc_head_workspace_bytes(hidden, head, pieces), torch.device("cuda"))
+    return ws.fill_(255)
+
+
+def run(hidden, head, targets, scale=1.0, weight=None, pieces=1, pad=0, shift=0, status=None):
+    rows, vocab = hidden.shape[0], head.shape[0]
+    loss, alone = torch.full((rows,), 7.0, device="cuda"), torch.full((rows,), 7.0, device="cuda")
+    dh, dw = (padded(torch.full_like(x, 7.0), pad, shift) for x in (hidden, head))
+    B.cvlc_head_loss(hidden, head, targets, alone, space(hidden, head, 0), scale=scale, row_weight=weight, status=status)
+    B.cvlc_head_step(hidden, head, targets, loss, dh, dw, space(hidden, head, pieces), scale=scale, row_weight=weight, pieces=pieces, status=status)
+    torch.cuda.synchronize()
+    return alone, loss, dh, dw
+
+
+def check(hidden, head, targets, scale=1.0, weight=None, **how):
+    alone, loss, dh, dw = run(hidden, head, targets, scale, weight, **how)
+    R.check(loss, dh, dw, hidden, head, targets, scale, weight)
+    R.check(alone, None, None, hidden, head, targets, scale, weight)
+    return loss, dh, dw
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("rows,dim,vocab", [(128, 64, 256), (1, 64, 256), (129, 64, 256), (128, 128, 256), (128, 64, 257), (300, 200, 1000)])
+def test_first(dtype, rows, dim, vocab):
+    check(*make(rows, dim, vocab, dtype))
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("rows", [1, 2, 16, 127, 257])
+@pytest.mark.parametrize("dim", [1, 8, 63, 65, 264])
+@pytest.mark.parametrize("vocab", [1, 2, 10, 255, 513, 1003])
+def test_sizes(dtype, rows, dim, vocab):
+    check(*make(rows, dim, vocab, dtype, seed=rows + dim + vocab, wide=rows % 2 == 0))
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("dim,pad,shift", [(64, 8, 0), (64, 0, 8), (64, 0, 1), (64, 3, 0), (65, 0, 0), (63, 1, 0), (200, 5, 3), (7, 1, 2)])
+def test_strides(dtype, dim, pad, shift):
+    check(*make(200, dim, 700, dtype, pad, shift), pad=pad, shift=shift)
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("vocab", [300, 2000, 2304])
+@pytest.mark.parametrize("pieces", [2, 3, 8, 1000])
+def test_pieces(dtype, vocab, pieces):
+    check(*make(150, 96, vocab, dtype), pieces=pieces)
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("pieces", [1, 3])
+def test_weights_masks_and_scale(dtype, pieces):
+    hidden, head, t = make(333, 72, 1500, dtype)
+    g = torch.Generator(device="cuda").manual_seed(5)
+    weight = torch.rand(333, generator=g, device="cuda") * 1e-3 - 2e-4
+    weight[::7] = 0
+    t[::5] = -1
+    t[3] = -(1 << 40)
+    hidden[0] = float("nan")   # weight 0
+    hidden[5] = float("inf")   # no target
+    loss, dh, dw = check(hidden, head, t, scale=0.7, weight=weight, pieces=pieces)
+    assert not bool(dh[::7].any()) and not bool(dh[::5].any()) and not bool(loss[::5].any())
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+def test_all_rows_count_for_nothing(dtype):
+    hidden, head, t = make(40, 64, 300, dtype)
+    alone, loss, dh, dw = run(hidden, head, torch.full_like(t, -1))
+    assert not any(bool(x.any()) for x in (alone, loss, dh, dw))
+    alone, loss, dh, dw = run(hidden, head, t, weight=torch.zeros(40, device="cuda"))
+    assert not any(bool(x.any()) for x in (alone, loss, dh, dw))
+
+
+def test_no_rows():
+    hidden, head, t = make(4, 64, 300)
+    dw = torch.ones(300, 72, dtype=BF, device="cuda")
+    ws = B.alloc_bytes(256, torch.device("cuda"))
+    B.cvlc_head_step(hidden[:0], head, t[:0], torch.zeros(0, device="cuda"), hidden[:0].clone(), dw[:, :64], ws)
+    assert not bool(dw[:, :64].any()) and bool((dw[:, 64:] == 1).all())
+
+
+@pytest.mark.parametrize("pieces", [1, 2])
+def test_words_that_are_not_there_are_reported(pieces):
+    hidden, head, t = make(200, 64, 600)
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    check(hidden, head, t, pieces=pieces, status=status)
+    assert status.item() == 0
+    t[7], t[100] = 600, 1 << 33
+    check(hidden, head, t, pieces=pieces, status=status)
+    assert status.item() == B.CVLC_ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("pieces", [1, 2])
+def test_far_logits(dtype, pieces):
+    """rows whose target is far below or above all others: losses of hundreds, and of next to nothing"""
+    hidden, head, t = make(256, 64, 800, dtype, width=8.0)
+    hidden[:64] = (-20 * head[t[:64]].float()).to(dtype)
+    hidden[64:128] = (3 * head[t[64:128]].float()).to(dtype)
+    hidden[128:192] *= 12
+    loss, _, _ = check(hidden, head, t, pieces=pieces)
+    assert float(loss.max()) > 500 and 0 < float(loss[64:128].max()) and float(loss.min()) < 1e-30
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+def test_not_finite(dtype):
+    hidden, head, t = make(140, 64, 500, dtype)
+    good = [x.clone() for x in run(hidden, head, t)]
+    hidden[3, 5] = float("nan")
+    alone, loss, dh, dw = run(hidden, head, t)
+    others = torch.arange(140, device="cuda") != 3
+    assert bool(torch.isnan(loss[3])) and bool(torch.isnan(alone[3])) and bool(torch.isnan(dh[3]).all()) and bool(torch.isnan(dw).all(dim=1).all())
+    assert torch.equal(loss[others], good[1][others]) and torch.equal(dh[others], good[2][others])
+
+
+def test_same_bits_again_and_streams():
+    a, b = make(300, 128, 3000, seed=1), make(200, 128, 2000, seed=2)
+    first, second = run(*a), run(*b)
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    outs = []
+    for (h, w, t), st in zip((a, b), streams):
+        o = [torch.zeros(h.shape[0], device="cuda"), torch.zeros_like(h), torch.zeros_like(w), space(h, w, 1)]
+        outs.append(o)
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for (h, w, t), st, o in zip((a, b), streams, outs):
+            B.cvlc_head_step(h, w, t, o[0], o[1], o[2], o[3], stream=st)
+    torch.cuda.synchronize()
+    for o, x in zip(outs, (first, second)):
+        assert all(torch.equal(p, q) for p, q in zip(o[:3], x[1:]))
+
+
+def test_graph():
+    hidden, head, t = make(130, 64, 900)
+    loss, dh, dw, ws = torch.zeros(130, device="cuda"), torch.zeros_like(hidden), torch.zeros_like(head), space(hidden, head, 2)
+    stream = torch.cuda.Stream()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        B.cvlc_head_step(hidden, head, t, loss, dh, dw, ws, pieces=2, stream=stream)
+    for seed in (3, 4):
+        for x, y in zip((hidden, head, t), make(130, 64, 900, seed=seed)):
+            x.copy_(y)
+        graph.replay()
+        torch.cuda.synchronize()
+        want = run(hidden, head, t, pieces=2)
+        assert torch.equal(loss, want[1]) and torch.equal(dh, want[2]) and torch.equal(dw, want[3])
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("rows,dim,vocab,pieces", [(1000, 512, 20000, 1), (2500, 384, 9000, 3), (5, 1024, 50021, 1), (4097, 64, 1000, 1), (20000, 72, 130, 1)])
+def test_larger(dtype, rows, dim, vocab, pieces):
+    check(*make(rows, dim, vocab, dtype, seed=rows), pieces=pieces)
+
+
+def test_gradients_by_differences():
+    """the loss's own change along a straight way is the gradient's product with it: by the trapezium rule, of the gradients at both ends (the two ends
+    are rounded to the type, so that the point they were made from is not halfway between them)"""
+    hidden, head, t = make(64, 64, 400)
+    weight = torch.rand(64, device="cuda")
+    g = torch.Generator(device="cuda").manual_seed(9)
+    for x, at in ((hidden, 2), (head, 3)):
+        way = torch.randn(x.shape, generator=g, device="cuda") * 2.0 ** -4
+        up, down = (x.float() + way).to(BF), (x.float() - way).to(BF)
+        moved = (up.double() - down.double())
+        a = run(*((up, head) if x is hidden else (hidden, up)), t, scale=1.3, weight=weight)
+        b = run(*((down, head) if x is hidden else (hidden, down)), t, scale=1.3, weight=weight)
+        terms = moved * (a[at].double() + b[at].double()) / 2
+        predicted = float(terms.sum())
+        # what the rule leaves out (a twelfth of the third derivative, times the cube of the way) by the definition in 64 bits; the rest is the
+        # gradients' rounding: 2^-8 of each of the terms
+        e, f = (R.step(*((y, head) if x is hidden else (hidden, y)), t, 1.3, weight)[0] for y in (up, down))
+        name = "d_hidden" if x is hidden else "d_head"
+        left_out = float((e["loss"] - f["loss"]).sum() - (moved * (e[name] + f[name]) / 2).sum())
+        assert abs(float(a[1].double().sum() - b[1].double().sum()) - predicted - left_out) <= 2.0 ** -8 * float(terms.norm()) * 3
