@@ -37,15 +37,30 @@ namespace {
 constexpr float kLog2E = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 // ---- the products --------------------------------------------------------------------------
-// A block has a tile of 128 rows by 256 columns: one thread copies operands (a ring of stages of 64 values of the sum), one issues the
-// products, eight warps read a finished tile from the tensor memory while the next one is made in its other half.
+// A block has a tile of 128 rows by 256 columns, a pair of blocks one of 256 by 256: one thread copies operands (a ring of stages of 64 values of the
+// sum), one issues the products, eight warps read a finished tile from the tensor memory while the next one is made in its other half.
 constexpr uint32_t kTileM = 128, kTileN = 256, kTileK = 64;
 constexpr int kThreads = 384, kOutWarps = 8;
 constexpr uint32_t kBytesA = kTileM * kTileK * 2, kBytesB = kTileN * kTileK * 2;
-constexpr int kStages = 4;
-constexpr size_t kGemmShared = kStages * (kBytesA + kBytesB) + 1024;
+template <int CG>
+constexpr int kStages = CG == 2 ? 6 : 4;
+template <int CG>
+constexpr uint32_t kStageBytes = kBytesA + kBytesB / CG;  // of one block
+template <int CG>
+constexpr size_t kGemmShared = kStages<CG> * kStageBytes<CG> + 1024;
 
-enum Epilogue { kStats, kProbs, kParts, kGrad };
+struct Header {  // at the beginning of the workspace
+  float up, down;         // fp16: a power of two that brings weights to at most 1, times 2^15, and its inverse
+  uint32_t wild;          // some row is
+  uint32_t late[kNumSM];  // a block of the products has given up
+};
+__device__ __forceinline__ bool any_late(const Header* h) {  // asked by all threads of a block
+  uint32_t x = 0;
+  for (uint32_t i = threadIdx.x; i < kNumSM; i += blockDim.x) x |= h->late[i];
+  return __syncthreads_or((int)x) != 0;
+}
+
+enum Epilogue { kStats, kKeep, kProbs, kParts, kGrad };
 struct Product {
   CUtensorMap a, b;
   uint32_t m, n, k_blocks;               // rows, columns, steps of 64 of the sum
@@ -62,17 +77,27 @@ struct Product {
   uint64_t ldo, split_stride;
   uint32_t add, wide;                    // added to what is there; rows of `out` by vectors of 32 bytes
   const float* alpha_dev;                // or nullptr; multiplies alpha
-  int32_t *late, *status;
+  const uint32_t* skip;                  // or nullptr; where it is 0 nothing is to be done
+  const uint32_t* wild;                  // or nullptr; of 256 rows each: 0 where they are left out
+  Header* header;
+  int32_t* status;
+  uint32_t first;                        // of the call's products
 };
+__device__ __forceinline__ bool left_out(const Product& g, uint32_t w) {
+  if (!g.wild) return false;
+  const uint32_t t = w % (g.tiles_m * g.tiles_n), tm = g.m_first ? t % g.tiles_m : t / g.tiles_n;
+  return g.wild[tm] == 0;  // a pair's tile, or the only one
+}
 
 struct Work {
   uint32_t m0, n0, k_from, k_to, split;
 };
+template <int CG>
 __device__ __forceinline__ Work work_of(const Product& g, uint32_t w) {
   const uint32_t tiles = g.tiles_m * g.tiles_n, split = w / tiles, t = w - split * tiles;
   const uint32_t tm = g.m_first ? t % g.tiles_m : t / g.tiles_n, tn = g.m_first ? t / g.tiles_m : t % g.tiles_n;
   Work r;
-  r.m0 = tm * kTileM, r.n0 = tn * kTileN, r.split = split;
+  r.m0 = (tm * CG + pair_rank<CG>()) * kTileM, r.n0 = tn * kTileN, r.split = split;
   r.k_from = (uint32_t)((uint64_t)g.k_blocks * split / g.splits), r.k_to = (uint32_t)((uint64_t)g.k_blocks * (split + 1) / g.splits);
   return r;
 }
@@ -132,6 +157,44 @@ __device__ __forceinline__ void finish_tile(const Product& g, const Work& w, uin
       for (int i = 0; i < 32; ++i) s += exp2_fast(v[i] - from);
       sum = fmaf(sum, exp2_fast(most - from), s);
       most = m;
+    }
+    if (there && w.n0 + half * 128 < g.n) g.stats[(uint64_t)(w.n0 / 128 + half) * g.stats_stride + row] = make_float2(most, sum);
+  } else if constexpr (EPI == kKeep) {
+    // relative to the target's own value, known from before: what is kept needs no second look.  A row of which some word is more than 2^60 times as likely as
+    // the target is wild and gets a second turn, relative to its maximum.
+    const float from = there ? g.at_target[row] : CUDART_INF_F;
+    const int64_t target = there ? target_of(g.targets, g.token_bytes, row) : -1;
+    T* const out = static_cast<T*>(g.out) + (uint64_t)row * g.ldo;
+    float most = -CUDART_INF_F, sum = 0.0f;
+    for (int c = 0; c < 4; ++c) {
+      const uint32_t col = w.n0 + half * 128 + c * 32;
+      if (col >= g.n) break;
+      tensor_load(tensor + c * 32, v);
+      tensor_loaded(v);
+#pragma unroll
+      for (int i = 0; i < 32; ++i) v[i] = fmaf(v[i], g.k2, -from);
+      const bool mine = target >= col && target < (int64_t)col + 32;
+      if (g.n - col < 32 || __any_sync(kFull, mine)) {
+#pragma unroll
+        for (int i = 0; i < 32; ++i)
+          if (col + i >= g.n || (mine && target == (int64_t)col + i)) v[i] = -CUDART_INF_F;
+      }
+#pragma unroll
+      for (int i = 0; i < 32; ++i) most = fmaxf(most, v[i]), v[i] = exp2_fast(v[i]);
+      float s[4] = {v[0], v[1], v[2], v[3]};
+#pragma unroll
+      for (int i = 4; i < 32; ++i) s[i & 3] += v[i];
+      sum += (s[0] + s[1]) + (s[2] + s[3]);
+      if (there) {
+        const bool counts = from != CUDART_INF_F;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          uint32_t p[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) p[i] = counts ? pack2<T>(v[16 * h + 2 * i], v[16 * h + 2 * i + 1]) : 0u;
+          store_sector(out + col + 16 * h, p);
+        }
+      }
     }
     if (there && w.n0 + half * 128 < g.n) g.stats[(uint64_t)(w.n0 / 128 + half) * g.stats_stride + row] = make_float2(most, sum);
   } else if constexpr (EPI == kProbs) {
@@ -216,145 +279,146 @@ __device__ __forceinline__ void finish_tile(const Product& g, const Work& w, uin
   }
 }
 
-template <int EPI, bool A_ROWS, bool B_ROWS, class T>
+template <int EPI, bool A_ROWS, bool B_ROWS, class T, int CG>
 __global__ void __launch_bounds__(kThreads, 1) k_head_product(const __grid_constant__ Product g) {
+  constexpr int stages = kStages<CG>;
   extern __shared__ uint8_t dynamic[];
-  __shared__ uint64_t full[kStages], empty[kStages], made[2], taken[2], over;
+  __shared__ uint64_t full[stages], empty[stages], made[2], taken[2], over;
   __shared__ uint32_t tensor_at, late;
   __shared__ uint32_t turn[EPI == kGrad ? kOutWarps * 32 * 17 : 1];
-  const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x & 31;
+  const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x & 31, rank = pair_rank<CG>();
   const uint32_t ring = (smem_at(dynamic) + 1023) & ~1023u;
   if (threadIdx.x == 0) {
-    for (int i = 0; i < kStages; ++i) mbar_init(full + i, 1), mbar_init(empty + i, 1);
-    for (int i = 0; i < 2; ++i) mbar_init(made + i, 1), mbar_init(taken + i, kOutWarps);
+    for (int i = 0; i < stages; ++i) mbar_init(full + i, 1), mbar_init(empty + i, 1);
+    for (int i = 0; i < 2; ++i) mbar_init(made + i, 1), mbar_init(taken + i, CG * kOutWarps);
     mbar_init(&over, 1);
     late = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  if (warp == 2) tensor_alloc<1>(&tensor_at);
+  if (warp == 2) tensor_alloc<CG>(&tensor_at);
   tensor_before();
   __syncthreads();
+  pair_sync<CG>();
   tensor_after();
-  const uint32_t tensor = tensor_at, items = g.tiles_m * g.tiles_n * g.splits;
+  const uint32_t tensor = tensor_at, first = blockIdx.x / CG, apart = gridDim.x / CG;
   pdl_enter();
+  const uint32_t items = g.skip && *g.skip == 0 ? 0 : g.tiles_m * g.tiles_n * g.splits;
   bool ok = true;
   if (warp == 0 && lane == 0) {
     uint32_t s = 0, phase = 0, issued = 0;
-    for (uint32_t w = blockIdx.x; ok && w < items; w += gridDim.x) {
-      const Work r = work_of(g, w);
+    for (uint32_t w = first; ok && w < items; w += apart) {
+      if (left_out(g, w)) continue;
+      const Work r = work_of<CG>(g, w);
       for (uint32_t k = r.k_from; k < r.k_to; ++k) {
         if (!(ok = mbar_wait(empty + s, phase ^ 1, &late))) break;
-        mbar_expect(full + s, kBytesA + kBytesB);
-        const uint32_t a = ring + s * (kBytesA + kBytesB), b = a + kBytesA, bar = smem_at(full + s);
+        if (rank == 0) mbar_expect(full + s, CG * kStageBytes<CG>);
+        const uint32_t a = ring + s * kStageBytes<CG>, b = a + kBytesA, bar = leader_at<CG>(smem_at(full + s)), n0 = r.n0 + rank * (kTileN / CG);
         if constexpr (A_ROWS) {
 #pragma unroll
-          for (uint32_t i = 0; i < kTileM / 64; ++i) load_tile<1>(g.a, a + i * kTileBytes64, bar, r.m0 + 64 * i, k * kTileK);
+          for (uint32_t i = 0; i < kTileM / 64; ++i) load_tile<CG>(g.a, a + i * kTileBytes64, bar, r.m0 + 64 * i, k * kTileK);
         } else {
-          load_tile<1>(g.a, a, bar, k * kTileK, r.m0);
+          load_tile<CG>(g.a, a, bar, k * kTileK, r.m0);
         }
         if constexpr (B_ROWS) {
 #pragma unroll
-          for (uint32_t i = 0; i < kTileN / 64; ++i) load_tile<1>(g.b, b + i * kTileBytes64, bar, r.n0 + 64 * i, k * kTileK);
+          for (uint32_t i = 0; i < kTileN / CG / 64; ++i) load_tile<CG>(g.b, b + i * kTileBytes64, bar, n0 + 64 * i, k * kTileK);
         } else {
-          load_tile<1>(g.b, b, bar, k * kTileK, r.n0);
+          load_tile<CG>(g.b, b, bar, k * kTileK, n0);
         }
         ++issued;
-        if (++s == kStages) s = 0, phase ^= 1;
+        if (++s == stages) s = 0, phase ^= 1;
       }
     }
-    if (!ok) {  // copies that are on their way end before the block does
+    if (!ok && rank == 0) {  // copies that are on their way, the other block's among them, end before the blocks do
       uint32_t none = 0;
-      for (uint32_t i = 0; i < (issued < kStages ? issued : kStages); ++i) {
-        if (s == 0) s = kStages, phase ^= 1;
+      for (uint32_t i = 0; i < (issued < stages ? issued : stages); ++i) {
+        if (s == 0) s = stages, phase ^= 1;
         --s;
         mbar_wait(full + s, phase, &none, kMostWait / 4);
       }
     }
-  } else if (warp == 1 && lane == 0) {
-    constexpr uint32_t kind = product_kind(std::is_same<T, __nv_bfloat16>::value, A_ROWS, B_ROWS, kTileM, kTileN);
+  } else if (warp == 1 && lane == 0 && rank == 0) {
+    constexpr uint32_t kind = product_kind(std::is_same<T, __nv_bfloat16>::value, A_ROWS, B_ROWS, CG * kTileM, kTileN);
     uint32_t s = 0, phase = 0, turn_of = 0;
     bool any = false;
-    for (uint32_t w = blockIdx.x; ok && w < items; w += gridDim.x, ++turn_of) {
-      const Work r = work_of(g, w);
+    for (uint32_t w = first; ok && w < items; w += apart) {
+      if (left_out(g, w)) continue;
+      const Work r = work_of<CG>(g, w);
       const uint32_t half = turn_of & 1;
       if (!(ok = mbar_wait(taken + half, (turn_of / 2 & 1) ^ 1, &late))) break;
       tensor_after();
       for (uint32_t k = r.k_from; k < r.k_to; ++k) {
         if (!(ok = mbar_wait(full + s, phase, &late))) break;
         tensor_after();
-        const uint32_t a = ring + s * (kBytesA + kBytesB), b = a + kBytesA;
+        const uint32_t a = ring + s * kStageBytes<CG>, b = a + kBytesA;
 #pragma unroll
         for (uint32_t i = 0; i < kTileK / 16; ++i)
-          multiply<1>(tensor + half * kTileN, operand<A_ROWS>(a + i * kStepBytes<A_ROWS>), operand<B_ROWS>(b + i * kStepBytes<B_ROWS>), kind,
-                      k != r.k_from || i != 0);
-        commit<1>(empty + s);
+          multiply<CG>(tensor + half * kTileN, operand<A_ROWS>(a + i * kStepBytes<A_ROWS>), operand<B_ROWS>(b + i * kStepBytes<B_ROWS>), kind,
+                       k != r.k_from || i != 0);
+        commit<CG>(empty + s);
         any = true;
-        if (++s == kStages) s = 0, phase ^= 1;
+        if (++s == stages) s = 0, phase ^= 1;
       }
-      if (ok) commit<1>(made + half);
+      if (ok) commit<CG>(made + half);
+      ++turn_of;
     }
     if (!ok && any) {
       uint32_t none = 0;
-      commit<1>(&over);
+      commit<CG>(&over);
       mbar_wait(&over, 0, &none, kMostWait / 4);
     }
   } else if (warp >= 4) {
     const uint32_t half_tile = (warp - 4) / 4, quarter = warp & 3;
     uint32_t turn_of = 0;
-    for (uint32_t w = blockIdx.x; w < items; w += gridDim.x, ++turn_of) {
-      const Work r = work_of(g, w);
+    for (uint32_t w = first; w < items; w += apart) {
+      if (left_out(g, w)) continue;
+      const Work r = work_of<CG>(g, w);
       const uint32_t half = turn_of & 1;
       if (!(ok = __all_sync(kFull, mbar_wait(made + half, turn_of / 2 & 1, &late)))) break;
       tensor_after();
       finish_tile<EPI, T>(g, r, tensor + half * kTileN + half_tile * 128 + (quarter * 32 << 16), half_tile, quarter, lane, turn + (EPI == kGrad ? (warp - 4) * 32 * 17 : 0));
       tensor_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive(taken + half);
+      if (lane == 0) mbar_arrive_leader<CG>(taken + half);
+      ++turn_of;
     }
   }
   __syncwarp();
   tensor_before();
   __syncthreads();
+  pair_sync<CG>();
   tensor_after();
-  if (warp == 2) tensor_free<1>(tensor);
-  if (threadIdx.x == 0 && late) {
-    *g.late = 1;
-    if (g.status) set_status(g.status, CVLC_ERR_DEVICE_TIMEOUT);
+  if (warp == 2) tensor_free<CG>(tensor);
+  if (threadIdx.x == 0) {
+    for (uint32_t i = blockIdx.x; i < kNumSM; i += gridDim.x) {
+      if (g.first) g.header->late[i] = late;  // nobody has written here
+      else if (late) g.header->late[i] = 1;
+    }
+    if (late && g.status) set_status(g.status, CVLC_ERR_DEVICE_TIMEOUT);
   }
 }
 
 // ---- what is around them -------------------------------------------------------------------
 
-struct Header {  // at the beginning of the workspace
-  int32_t late;
-  uint32_t largest;  // bits of the largest weight's size
-  float up, down;    // a power of two that brings weights to at most 1, times 2^15 (fp16), and its inverse
-};
-
-// One block: what the call's kernels share
-__global__ void __launch_bounds__(1024) k_head_begin(Header* h, const float* weight, const void* targets, uint32_t token_bytes, uint64_t rows, uint32_t vocab,
-                                                     int half, int32_t* status) {
+// One block, fp16 only: the power of two by which G is held.  fp16 holds 2^-24 to 2^16; G, at most the largest weight in size, is held at most 2^15.
+__global__ void __launch_bounds__(1024) k_head_begin(Header* h, const float* weight, const void* targets, uint32_t token_bytes, uint64_t rows, uint32_t vocab) {
+  pdl_enter();
   __shared__ uint32_t most;
   if (threadIdx.x == 0) most = 0;
   __syncthreads();
   uint32_t m = 0;
-  bool beyond = false;
-  for (uint64_t i = threadIdx.x; i < rows; i += blockDim.x) {
-    const int64_t t = target_of(targets, token_bytes, i);
-    if (t >= (int64_t)vocab) beyond = true;
-    if (weight && t >= 0 && t < (int64_t)vocab) {
+  if (weight) {
+    for (uint64_t i = threadIdx.x; i < rows; i += blockDim.x) {
+      const int64_t t = target_of(targets, token_bytes, i);
       const uint32_t w = __float_as_uint(weight[i]) & 0x7FFFFFFFu;
-      if (w < 0x7F800000u) m = max(m, w);
+      if (t >= 0 && t < (int64_t)vocab && w < 0x7F800000u) m = max(m, w);
     }
+    m = __reduce_max_sync(kFull, m);
+    if ((threadIdx.x & 31) == 0) atomicMax(&most, m);
+    __syncthreads();
   }
-  if (beyond && status) set_status(status, CVLC_ERR_INVALID_ARG);
-  m = __reduce_max_sync(kFull, m);
-  if ((threadIdx.x & 31) == 0) atomicMax(&most, m);
-  __syncthreads();
   if (threadIdx.x == 0) {
-    h->late = 0;
-    // fp16 holds 2^-24 to 2^16: G, at most the largest weight in size, is held times a power of two that makes it at most 2^15
-    const int e = !half ? 0 : weight ? (most ? min(max((int)(most >> 23) - 126, -100), 100) : 0) - 15 : -15;
+    const int e = (weight && most ? min(max((int)(most >> 23) - 126, -100), 100) : 0) - 15;
     h->up = exp2f((float)-e), h->down = exp2f((float)e);
   }
 }
@@ -363,6 +427,7 @@ __global__ void __launch_bounds__(1024) k_head_begin(Header* h, const float* wei
 // in the products of others' gradients.
 __global__ void __launch_bounds__(256) k_head_align(const uint16_t* from, uint64_t from_stride, uint16_t* to, uint64_t to_stride, uint64_t rows, uint32_t dim,
                                                     const void* targets, uint32_t token_bytes, uint32_t vocab, const float* weight) {
+  pdl_enter();
   const uint64_t row = (uint64_t)blockIdx.x * 8 + threadIdx.x / 32;
   const uint32_t lane = threadIdx.x & 31;
   if (row >= rows) return;
@@ -390,57 +455,189 @@ __global__ void __launch_bounds__(256) k_head_align(const uint16_t* from, uint64
   }
 }
 
+// z of every row's target, in log2; +inf where the row counts for nothing.  A warp a row.
+struct TargetArgs {
+  const void *hidden, *head, *targets;
+  uint64_t hidden_ld, head_ld, rows;
+  uint32_t dim, vocab, token_bytes, blocks_wild;
+  const float* weight;
+  float* at_target;
+  float k2;
+  uint32_t* wild;
+  Header* header;
+};
+__global__ void __launch_bounds__(256) k_head_target(const TargetArgs a) {
+  pdl_enter();
+  const uint64_t row = (uint64_t)blockIdx.x * 8 + threadIdx.x / 32;
+  const uint32_t lane = threadIdx.x & 31;
+  if (blockIdx.x == 0 && threadIdx.x == 0) a.header->wild = 0;
+  for (uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x; i < a.blocks_wild; i += (uint64_t)gridDim.x * 256) a.wild[i] = 0;
+  if (row >= a.rows) return;
+  const int64_t t = target_of(a.targets, a.token_bytes, row);
+  if (t < 0 || t >= (int64_t)a.vocab || (a.weight && a.weight[row] == 0.0f)) {
+    if (lane == 0) a.at_target[row] = CUDART_INF_F;
+    return;
+  }
+  const __nv_bfloat16* const h = static_cast<const __nv_bfloat16*>(a.hidden) + row * a.hidden_ld;
+  const __nv_bfloat16* const w = static_cast<const __nv_bfloat16*>(a.head) + (uint64_t)t * a.head_ld;
+  float sum = 0.0f;
+  for (uint32_t i = lane * 8; i < a.dim; i += 256) {
+    if (i + 8 <= a.dim) {
+      float x[8], y[8];
+      widen<__nv_bfloat16>(__ldg(reinterpret_cast<const uint4*>(h + i)), x);
+      widen<__nv_bfloat16>(__ldg(reinterpret_cast<const uint4*>(w + i)), y);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) sum = fmaf(x[k], y[k], sum);
+    } else {
+      for (uint32_t k = i; k < a.dim; ++k) sum = fmaf(to_float(h[k]), to_float(w[k]), sum);
+    }
+  }
+#pragma unroll
+  for (int d = 16; d; d /= 2) sum += __shfl_xor_sync(kFull, sum, d);
+  sum *= a.k2;
+  if (lane == 0) a.at_target[row] = sum < CUDART_INF_F ? sum : CUDART_NAN_F;
+}
+
+constexpr float kWild = 60.0f;
+constexpr uint32_t kWildRows = 2 * kTileM;  // that get a second turn together
 struct RowsArgs {
   const float2* stats;
   uint64_t stats_stride;
   uint32_t slots, token_bytes, vocab;
-  const float* at_target;
+  float* at_target;
   const void* targets;
   const float* weight;
   float* loss;
   float4* row;  // or nullptr
-  const Header* header;
+  Header* header;
   uint64_t rows;
+  int32_t* status;
+  uint32_t half;  // fp16
+  // where the exponentials are kept:
+  __nv_bfloat16* kept;
+  uint64_t ldg, hidden_ld, scaled_ld;
+  const __nv_bfloat16* hidden;
+  __nv_bfloat16* scaled;  // hidden states times their rows' factor
+  float *factor, *raised;  // raised: by how much a row's second reference is above its target, 0: not at all
+  uint32_t* wild;
+  uint32_t dim, second;
 };
-// A row's parts joined: 32 rows a block, eight threads a row.
-// Sums relative to the largest; that of the words other than the target (o) is kept apart, so that 1 - q and a small loss ln(1 + o) keep their accuracy.
-__global__ void __launch_bounds__(256) k_head_rows(const RowsArgs a) {
-  pdl_enter();
-  __shared__ float2 part[8][32];
-  const uint32_t lane = threadIdx.x & 31, group = threadIdx.x / 32;
-  const uint64_t row = (uint64_t)blockIdx.x * 32 + lane;
+constexpr uint32_t kRowsOf = 8, kGroups = 32;  // rows of a block, threads of a row
+
+// The parts of a block's rows joined, by thread (group, row)
+__device__ __forceinline__ float2 join_parts(const RowsArgs& a, uint64_t row, uint32_t group, bool relative, float2 (*part)[kRowsOf]) {
   float m = -CUDART_INF_F, s = 0.0f;
   if (row < a.rows) {
 #pragma unroll 4
-    for (uint32_t i = group; i < a.slots; i += 8) {
+    for (uint32_t i = group; i < a.slots; i += kGroups) {
       const float2 x = a.stats[(uint64_t)i * a.stats_stride + row];
-      const float n = fmaxf(m, x.x), from = n == -CUDART_INF_F ? 0.0f : n;
-      s = s * exp2f(m - from) + x.y * exp2f(x.x - from);
+      const float n = fmaxf(m, x.x);
+      if (relative) {  // each to its own maximum
+        const float from = n == -CUDART_INF_F ? 0.0f : n;
+        s = s * exp2f(m - from) + x.y * exp2f(x.x - from);
+      } else {
+        s += x.y;
+      }
       m = n;
     }
   }
-  part[group][lane] = make_float2(m, s);
+  part[group][threadIdx.x % kRowsOf] = make_float2(m, s);
   __syncthreads();
+  return make_float2(m, s);
+}
+
+// A row's parts joined.  Sums relative to the largest; that of the words other than the target (o) is kept apart, so that 1 - q and a small loss
+// ln(1 + o) keep their accuracy.
+__global__ void __launch_bounds__(256) k_head_rows(const RowsArgs a) {
+  pdl_enter();
+  __shared__ float2 part[kGroups][kRowsOf];
+  const uint32_t group = threadIdx.x / kRowsOf, lane = threadIdx.x % kRowsOf;
+  const uint64_t row = (uint64_t)blockIdx.x * kRowsOf + lane;
+  const bool late = any_late(a.header);
+  join_parts(a, row, group, true, part);
   if (group || row >= a.rows) return;
   const int64_t target = target_of(a.targets, a.token_bytes, row);
   const float weight = a.weight ? a.weight[row] : 1.0f;
+  if (target >= (int64_t)a.vocab && a.status) set_status(a.status, CVLC_ERR_INVALID_ARG);
   if (target < 0 || target >= (int64_t)a.vocab || weight == 0.0f) {
-    a.loss[row] = a.header->late ? CUDART_NAN_F : 0.0f;
+    a.loss[row] = late ? CUDART_NAN_F : 0.0f;
     if (a.row) a.row[row] = make_float4(0, 0, 0, 0);
     return;
   }
   const float zt = a.at_target[row];
   float most = zt;
-  for (int i = 0; i < 8; ++i) most = fmaxf(most, part[i][lane].x);
+  for (uint32_t i = 0; i < kGroups; ++i) most = fmaxf(most, part[i][lane].x);
   double others = 0.0;
-  for (int i = 0; i < 8; ++i)
+  for (uint32_t i = 0; i < kGroups; ++i)
     if (part[i][lane].x != -CUDART_INF_F || part[i][lane].y != 0.0f) others += (double)(part[i][lane].y * exp2f(part[i][lane].x - most));
   const float o = (float)others, right = exp2f(zt - most), total = right + o;
   const float loss = most == zt ? log1pf(o) : logf(total) + (most - zt) * kLn2;
-  a.loss[row] = a.header->late ? CUDART_NAN_F : weight * loss;
+  a.loss[row] = late ? CUDART_NAN_F : weight * loss;
   if (a.row) {
-    const float w = weight * a.header->up;
+    const float w = a.half ? weight * a.header->up : weight;
     a.row[row] = make_float4(most + log2f(total), w, -(o / total) * w, 0.0f);
+  }
+}
+
+// The same where the exponentials are kept, relative to the target's (to the row's maximum in a second turn): of G = weight exp(z - from) / total the
+// factor goes into the hidden states, row by row, and the target's own value, - o, to its place.
+__global__ void __launch_bounds__(256) k_head_rows_kept(const RowsArgs a) {
+  pdl_enter();
+  __shared__ float2 part[kGroups][kRowsOf];
+  __shared__ float factors[kRowsOf];
+  if (a.second && a.header->wild == 0) return;
+  if (a.second && a.wild[(uint64_t)blockIdx.x * kRowsOf / kWildRows] == 0) return;
+  const uint32_t group = threadIdx.x / kRowsOf, lane = threadIdx.x % kRowsOf;
+  const uint64_t row = (uint64_t)blockIdx.x * kRowsOf + lane;
+  const bool late = any_late(a.header);
+  join_parts(a, row, group, false, part);
+  if (group == 0 && row < a.rows) {
+    const int64_t target = target_of(a.targets, a.token_bytes, row);
+    const float weight = a.weight ? a.weight[row] : 1.0f;
+    if (target >= (int64_t)a.vocab && a.status) set_status(a.status, CVLC_ERR_INVALID_ARG);
+    float factor = 0.0f, loss = 0.0f;
+    if (target >= 0 && target < (int64_t)a.vocab && weight != 0.0f) {
+      float most = -CUDART_INF_F;
+      double others = 0.0;
+      for (uint32_t i = 0; i < kGroups; ++i) most = fmaxf(most, part[i][lane].x), others += (double)part[i][lane].y;
+      const float o = (float)others;
+      const float raised = a.second ? a.raised[row] : 0.0f, right = exp2f(-raised), total = right + o;
+      loss = weight * (raised == 0.0f ? log1pf(o) : logf(total) + raised * kLn2);
+      factor = weight / total;
+      a.kept[row * a.ldg + target] = __float2bfloat16_rn(-o);
+      if (!a.second) {
+        const bool wild = most > kWild && most < CUDART_INF_F;
+        a.raised[row] = wild ? most : 0.0f;
+        if (wild) {
+          a.at_target[row] += most;
+          a.wild[row / kWildRows] = 1;
+          a.header->wild = 1;
+        }
+      }
+    }
+    a.loss[row] = late ? CUDART_NAN_F : loss;
+    factors[lane] = factor;
+  }
+  __syncthreads();
+  const uint64_t row0 = (uint64_t)blockIdx.x * kRowsOf;
+  const uint32_t warp = threadIdx.x / 32;
+  if (row0 + warp >= a.rows) return;
+  const float f = factors[warp];
+  if ((threadIdx.x & 31) == 0) a.factor[row0 + warp] = f;
+  const __nv_bfloat16* const h = a.hidden + (row0 + warp) * a.hidden_ld;
+  __nv_bfloat16* const to = a.scaled + (row0 + warp) * a.scaled_ld;
+  for (uint32_t i = (threadIdx.x & 31) * 8; i < a.dim; i += 256) {
+    float x[8] = {};
+    if (f != 0.0f) {  // else the row may hold anything
+      if (i + 8 <= a.dim) {
+        widen<__nv_bfloat16>(__ldg(reinterpret_cast<const uint4*>(h + i)), x);
+      } else {
+        for (uint32_t k = 0; i + k < a.dim; ++k) x[k] = to_float(h[i + k]);
+      }
+#pragma unroll
+      for (int k = 0; k < 8; ++k) x[k] *= f;
+    }
+    *reinterpret_cast<uint4*>(to + i) = narrow<__nv_bfloat16>(x);
   }
 }
 
@@ -450,17 +647,19 @@ struct JoinArgs {
   uint32_t splits, dim;
   uint64_t rows;
   float alpha;
+  const float *factor, *down;  // of a row; of all; or nullptr
   const Header* header;
   void* out;
 };
 template <class T>
 __global__ void __launch_bounds__(256) k_head_join(const JoinArgs a) {
   pdl_enter();
-  const float alpha = a.header->late ? CUDART_NAN_F : a.alpha * a.header->down;
+  const bool late = any_late(a.header);
   const uint32_t per = (a.dim + 3) / 4;
   const uint64_t i = (uint64_t)blockIdx.x * blockDim.x + threadIdx.x, row = i / per;
   const uint32_t col = (uint32_t)(i - row * per) * 4;
   if (row >= a.rows) return;
+  const float alpha = late ? CUDART_NAN_F : a.alpha * (a.factor ? a.factor[row] : a.down ? *a.down : 1.0f);
   float4 s = make_float4(0, 0, 0, 0);
   for (uint32_t k = 0; k < a.splits; ++k) {
     const float4 x = *reinterpret_cast<const float4*>(a.parts + k * a.split_stride + row * a.ldp + col);
@@ -475,134 +674,242 @@ __global__ void __launch_bounds__(256) k_head_join(const JoinArgs a) {
 
 // ---- layout and launching --------------------------------------------------------------------
 
-struct HeadLayout {
-  bool copy_hidden, copy_head;
-  uint64_t ld;  // of copies
-  uint32_t piece, pieces;  // words
-  uint64_t ldg, ldp, stats_stride;
-  uint32_t splits;
-  size_t off_hidden, off_head, off_stats, off_target, off_row, off_g, off_parts, total;
-};
 bool on16(const void* p, uint64_t stride) { return reinterpret_cast<uintptr_t>(p) % 16 == 0 && stride % 8 == 0; }
 uint32_t tiles(uint64_t n, uint32_t tile) { return (uint32_t)((n + tile - 1) / tile); }
+// Up to 128 rows a block has them all; above, a pair of blocks reads half as much of the other operand.
+bool by_pairs(uint64_t m) { return m > kTileM; }
+uint32_t tiles_m(uint64_t m) { return tiles(m, by_pairs(m) ? 2 * kTileM : kTileM); }
 
 // In how many parts a sum is cut: as many as leave the SMs the least to do one behind the other (a part more costs its reading and writing).
-uint32_t splits_of(uint32_t tiles_all, uint32_t k_blocks) {
+uint32_t splits_of(uint64_t m, uint64_t n, uint32_t k_blocks) {
+  const uint64_t all = (uint64_t)tiles_m(m) * tiles(n, kTileN), at_once = by_pairs(m) ? kNumSM / 2 : kNumSM;
   uint32_t best = 1;
   double cost = 1e30;
   for (uint32_t s = 1; s <= 32 && s * 8 <= (k_blocks > 8 ? k_blocks : 8); ++s) {
-    const double c = (double)((tiles_all * s + kNumSM - 1) / kNumSM) / s * k_blocks + 2.0 * s;
+    const double c = (double)((all * s + at_once - 1) / at_once) / s * k_blocks + 2.0 * s;
     if (c < cost * 0.98) cost = c, best = s;
   }
   return best;
 }
 
+struct HeadLayout {
+  bool keep, copy_hidden, copy_head;
+  uint64_t ld;             // of copies
+  uint32_t piece, pieces;  // words
+  uint64_t ldg, ldp, stats_stride;
+  uint32_t splits, blocks_wild;
+  size_t off_hidden, off_head, off_scaled, off_stats, off_target, off_row, off_factor, off_raised, off_wild, off_g, off_parts, total;
+};
 HeadLayout head_layout(const cvlc_head& a, uint32_t pieces) {
   HeadLayout L = {};
-  L.copy_hidden = pieces || !on16(a.hidden_dev, a.hidden_stride), L.copy_head = !on16(a.head_dev, a.head_stride);
+  if (pieces) {
+    L.piece = tiles((a.vocab + pieces - 1) / pieces, kTileN) * kTileN;
+    L.pieces = tiles(a.vocab, L.piece);
+    if (L.pieces == 1) L.piece = a.vocab;
+  }
+  // bf16 has fp32's range: the exponentials are kept from the first time.  fp16 has not, and with several pieces there is no room for them.
+  L.keep = L.pieces == 1 && a.dtype == CVLC_BF16;
+  L.copy_hidden = (pieces && !L.keep) || !on16(a.hidden_dev, a.hidden_stride), L.copy_head = !on16(a.head_dev, a.head_stride);
   L.ld = (a.dim + 7) / 8 * 8;
   L.stats_stride = (a.rows + 31) / 32 * 32;
-  size_t at = 256;
+  size_t at = align256(sizeof(Header));
   auto take = [&](size_t bytes) { const size_t from = at; at = align256(at + bytes); return from; };
   L.off_hidden = take(L.copy_hidden ? a.rows * L.ld * 2 : 0);
   L.off_head = take(L.copy_head ? a.vocab * L.ld * 2 : 0);
   L.off_stats = take((size_t)tiles(a.vocab, 128) * L.stats_stride * 8);
   L.off_target = take(a.rows * 4);
   if (pieces) {
-    L.piece = tiles((a.vocab + pieces - 1) / pieces, kTileN) * kTileN;
-    L.pieces = tiles(a.vocab, L.piece);
-    if (L.pieces == 1) L.piece = a.vocab;
-    L.ldg = (L.piece + 31) / 32 * 32;
+    L.ldg = (uint64_t)tiles(L.piece, 32) * 32;
     L.ldp = (a.dim + 31) / 32 * 32;
-    L.splits = splits_of(tiles(a.rows, kTileM) * tiles(a.dim, kTileN), tiles(L.piece, kTileK));
-    L.off_row = take(a.rows * 16);
+    L.splits = splits_of(a.rows, a.dim, tiles(L.piece, kTileK));
     L.off_g = take(a.rows * L.ldg * 2);
     L.off_parts = take((size_t)L.splits * a.rows * L.ldp * 4);
+    if (L.keep) {
+      L.blocks_wild = tiles(a.rows, kWildRows);
+      L.off_scaled = take(a.rows * L.ld * 2);
+      L.off_factor = take(a.rows * 4);
+      L.off_raised = take(a.rows * 4);
+      L.off_wild = take(L.blocks_wild * 4);
+    } else {
+      L.off_row = take(a.rows * 16);
+    }
   }
   L.total = at;
   return L;
 }
 
-template <int EPI, bool A_ROWS, bool B_ROWS, class T>
-cudaError_t run_product(int id, Product& g, cudaStream_t st) {
+template <int EPI, bool A_ROWS, bool B_ROWS, class T, int CG>
+cudaError_t run_product_of(int id, Product& g, cudaStream_t st, bool overlap) {
   static OncePerDevice once;
-  const cudaError_t e = once_per_device(once, [] { return allow_shared(k_head_product<EPI, A_ROWS, B_ROWS, T>, kGemmShared); });
+  const cudaError_t e = once_per_device(once, [] { return allow_shared(k_head_product<EPI, A_ROWS, B_ROWS, T, CG>, kGemmShared<CG>); });
   if (e != cudaSuccess) return e;
-  g.tiles_m = tiles(g.m, kTileM), g.tiles_n = tiles(g.n, kTileN);
+  const uint64_t items = (uint64_t)g.tiles_m * g.tiles_n * g.splits;
+  LaunchScope ls(id, st);
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((uint32_t)(items * CG < kNumSM ? items * CG : kNumSM));
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = kGemmShared<CG>;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = CG, attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = overlap ? 2 : 1;
+  (void)cudaLaunchKernelEx(&cfg, k_head_product<EPI, A_ROWS, B_ROWS, T, CG>, static_cast<Product>(g));
+  return cudaGetLastError();
+}
+struct Operand {
+  const void* at;
+  uint64_t cols, rows, ld;
+};
+// D = A B^T, sums along the operands' columns, or along their rows (ROWS)
+template <int EPI, bool A_ROWS, bool B_ROWS, class T>
+cudaError_t run_product(int id, Product& g, const Operand& a, const Operand& b, cudaStream_t st, bool overlap) {
+  constexpr bool bf16 = std::is_same<T, __nv_bfloat16>::value;
+  const bool pairs = by_pairs(g.m);
+  g.tiles_m = tiles_m(g.m), g.tiles_n = tiles(g.n, kTileN);
   // the operand with more tiles is read once, the other one's stay in the L2 cache
   g.m_first = g.tiles_m <= g.tiles_n;
-  const uint64_t items = (uint64_t)g.tiles_m * g.tiles_n * g.splits;
-  launch_kernel(id, k_head_product<EPI, A_ROWS, B_ROWS, T>, dim3((uint32_t)(items < kNumSM ? items : kNumSM)), dim3(kThreads), kGemmShared, st, true, g);
-  return cudaGetLastError();
+  if (!make_tensor_map(&g.a, a.at, bf16, a.cols, a.rows, a.ld, 64, A_ROWS ? kTileK : kTileM) ||
+      !make_tensor_map(&g.b, b.at, bf16, b.cols, b.rows, b.ld, 64, B_ROWS ? kTileK : kTileN / (pairs ? 2 : 1)))
+    return cudaErrorUnknown;
+  return pairs ? run_product_of<EPI, A_ROWS, B_ROWS, T, 2>(id, g, st, overlap) : run_product_of<EPI, A_ROWS, B_ROWS, T, 1>(id, g, st, overlap);
 }
+
+struct Gradients {
+  void* d_hidden;
+  uint64_t d_hidden_stride;
+  void* d_head;
+  uint64_t d_head_stride;
+};
 
 template <class T>
-cudaError_t run_head(const cvlc_head& a, uint32_t pieces, float* loss, void* d_hidden, uint64_t d_hidden_stride, void* d_head, uint64_t d_head_stride,
-                     void* ws, cudaStream_t st) {
-  constexpr bool bf16 = std::is_same<T, __nv_bfloat16>::value;
-  const HeadLayout L = head_layout(a, pieces);
-  uint8_t* const base = static_cast<uint8_t*>(ws);
-  Header* const header = reinterpret_cast<Header*>(base);
-  launch_kernel(kKHeadBegin, k_head_begin, dim3(1), dim3(a.rows > 256 ? 1024 : 256), 0, st, false, header, a.row_weight_dev, a.targets_dev, a.token_bytes,
-                a.rows, a.vocab, bf16 ? 0 : 1, a.status_dev);
-  const void *hidden = a.hidden_dev, *head = a.head_dev;
-  uint64_t hidden_ld = a.hidden_stride, head_ld = a.head_stride;
-  auto copy = [&](const void*& x, uint64_t& ld, uint64_t rows, size_t off, const void* targets) {
-    launch_kernel(kKHeadAlign, k_head_align, dim3(tiles(rows, 8)), dim3(256), 0, st, false, static_cast<const uint16_t*>(x), ld,
-                  reinterpret_cast<uint16_t*>(base + off), L.ld, rows, a.dim, targets, a.token_bytes, a.vocab, a.row_weight_dev);
-    x = base + off, ld = L.ld;
-  };
-  if (L.copy_hidden) copy(hidden, hidden_ld, a.rows, L.off_hidden, a.targets_dev);
-  if (L.copy_head) copy(head, head_ld, a.vocab, L.off_head, nullptr);
+struct HeadRun {
+  const cvlc_head& a;
+  const HeadLayout L;
+  uint8_t* const base;
+  const cudaStream_t st;
+  Header* const header;
+  Operand hidden, head;
+  bool behind = false;  // some kernel of the call is in front
+  cudaError_t error = cudaSuccess;
 
-  Product p = {};
-  p.m = (uint32_t)a.rows, p.n = a.vocab, p.k_blocks = tiles(a.dim, kTileK), p.splits = 1;
-  p.k2 = a.scale * kLog2E, p.targets = a.targets_dev, p.token_bytes = a.token_bytes;
-  p.stats = reinterpret_cast<float2*>(base + L.off_stats), p.stats_stride = L.stats_stride, p.at_target = reinterpret_cast<float*>(base + L.off_target);
-  p.late = &header->late, p.status = a.status_dev;
-  if (!make_tensor_map(&p.a, hidden, bf16, a.dim, a.rows, hidden_ld, kTileK, kTileM) || !make_tensor_map(&p.b, head, bf16, a.dim, a.vocab, head_ld, kTileK, kTileN))
-    return cudaErrorUnknown;
-  cudaError_t e = run_product<kStats, false, false, T>(kKHeadStats, p, st);
-  if (e != cudaSuccess) return e;
-  RowsArgs r = {};
-  r.stats = p.stats, r.stats_stride = L.stats_stride, r.slots = tiles(a.vocab, 128), r.token_bytes = a.token_bytes, r.vocab = a.vocab;
-  r.at_target = p.at_target, r.targets = a.targets_dev, r.weight = a.row_weight_dev, r.loss = loss, r.header = header, r.rows = a.rows;
-  r.row = pieces ? reinterpret_cast<float4*>(base + L.off_row) : nullptr;
-  launch_kernel(kKHeadRows, k_head_rows, dim3(tiles(a.rows, 32)), dim3(256), 0, st, true, r);
-  if (!pieces) return cudaGetLastError();
-
-  T* const G = reinterpret_cast<T*>(base + L.off_g);
-  for (uint32_t i = 0; i < L.pieces; ++i) {
-    const uint32_t from = i * L.piece, words = i + 1 < L.pieces ? L.piece : a.vocab - from;
-    const T* const head_piece = static_cast<const T*>(head) + (uint64_t)from * head_ld;
-    Product q = p;
-    q.n = words, q.col0 = from, q.row = r.row, q.out = G, q.ldo = L.ldg;
-    if (!make_tensor_map(&q.b, head_piece, bf16, a.dim, words, head_ld, kTileK, kTileN)) return cudaErrorUnknown;
-    if ((e = run_product<kProbs, false, false, T>(kKHeadProbs, q, st)) != cudaSuccess) return e;
-    q = Product{};
-    q.late = p.late, q.status = p.status;
-    q.m = (uint32_t)a.rows, q.n = a.dim, q.k_blocks = tiles(words, kTileK);
-    q.splits = L.splits <= q.k_blocks ? L.splits : q.k_blocks;
-    q.out = base + L.off_parts, q.ldo = L.ldp, q.split_stride = a.rows * L.ldp, q.add = i != 0;
-    if (!make_tensor_map(&q.a, G, bf16, words, a.rows, L.ldg, kTileK, kTileM) || !make_tensor_map(&q.b, head_piece, bf16, a.dim, words, head_ld, 64, kTileK))
-      return cudaErrorUnknown;
-    if ((e = run_product<kParts, false, true, T>(kKHeadParts, q, st)) != cudaSuccess) return e;
-    q = Product{};
-    q.late = p.late, q.status = p.status;
-    q.m = words, q.n = a.dim, q.k_blocks = tiles(a.rows, kTileK), q.splits = 1;
-    T* const out = static_cast<T*>(d_head) + (uint64_t)from * d_head_stride;
-    q.out = out, q.ldo = d_head_stride, q.wide = reinterpret_cast<uintptr_t>(out) % 32 == 0 && d_head_stride % 16 == 0;
-    q.alpha = a.scale, q.alpha_dev = &header->down;
-    if (!make_tensor_map(&q.a, G, bf16, words, a.rows, L.ldg, 64, kTileK) || !make_tensor_map(&q.b, hidden, bf16, a.dim, a.rows, hidden_ld, 64, kTileK))
-      return cudaErrorUnknown;
-    if ((e = run_product<kGrad, true, true, T>(kKHeadGrad, q, st)) != cudaSuccess) return e;
+  HeadRun(const cvlc_head& a_, uint32_t pieces, void* ws, cudaStream_t st_)
+      : a(a_), L(head_layout(a_, pieces)), base(static_cast<uint8_t*>(ws)), st(st_), header(static_cast<Header*>(ws)),
+        hidden{a_.hidden_dev, a_.dim, a_.rows, a_.hidden_stride}, head{a_.head_dev, a_.dim, a_.vocab, a_.head_stride} {}
+  template <class P>
+  P* at(size_t off) const { return reinterpret_cast<P*>(base + off); }
+  template <class... Params, class... Args>
+  void launch(int id, void (*kernel)(Params...), uint32_t grid, uint32_t threads, Args&&... args) {
+    launch_kernel(id, kernel, dim3(grid), dim3(threads), 0, st, behind, args...);
+    behind = true;
   }
-  JoinArgs j = {};
-  j.parts = reinterpret_cast<const float*>(base + L.off_parts), j.split_stride = a.rows * L.ldp, j.ldp = L.ldp, j.ldo = d_hidden_stride;
-  j.splits = L.splits, j.dim = a.dim, j.rows = a.rows, j.alpha = a.scale, j.header = header, j.out = d_hidden;
-  launch_kernel(kKHeadJoin, k_head_join<T>, dim3((uint32_t)((a.rows * ((a.dim + 3) / 4) + 255) / 256)), dim3(256), 0, st, true, j);
-  return cudaGetLastError();
-}
+  Product product() const {
+    Product p = {};
+    p.splits = 1, p.alpha = a.scale, p.k2 = a.scale * kLog2E, p.targets = a.targets_dev, p.token_bytes = a.token_bytes;
+    p.stats = at<float2>(L.off_stats), p.stats_stride = L.stats_stride, p.at_target = at<float>(L.off_target);
+    p.header = header, p.status = a.status_dev;
+    return p;
+  }
+  template <int EPI, bool A_ROWS, bool B_ROWS>
+  void multiply(int id, Product& p, const Operand& x, const Operand& y) {
+    if (error == cudaSuccess) error = run_product<EPI, A_ROWS, B_ROWS, T>(id, p, x, y, st, behind);
+    behind = true;
+  }
+  void copy(Operand& x, size_t off, const void* targets) {
+    launch(kKHeadAlign, k_head_align, tiles(x.rows, 8), 256, static_cast<const uint16_t*>(x.at), x.ld, at<uint16_t>(off), L.ld, x.rows, a.dim, targets,
+           a.token_bytes, a.vocab, a.row_weight_dev);
+    x.at = base + off, x.ld = L.ld;
+  }
+  RowsArgs rows(float* loss) const {
+    RowsArgs r = {};
+    r.stats = at<float2>(L.off_stats), r.stats_stride = L.stats_stride, r.slots = tiles(a.vocab, 128), r.token_bytes = a.token_bytes, r.vocab = a.vocab;
+    r.at_target = at<float>(L.off_target), r.targets = a.targets_dev, r.weight = a.row_weight_dev, r.loss = loss, r.header = header, r.rows = a.rows;
+    r.status = a.status_dev;
+    return r;
+  }
+  uint32_t row_blocks() const { return tiles(a.rows, kRowsOf); }
+
+  void logits_once(float* loss, bool graded) {
+    Product p = product();
+    p.m = (uint32_t)a.rows, p.n = a.vocab, p.k_blocks = tiles(a.dim, kTileK), p.first = 1;
+    multiply<kStats, false, false>(kKHeadStats, p, hidden, head);
+    RowsArgs r = rows(loss);
+    r.row = graded ? at<float4>(L.off_row) : nullptr, r.half = std::is_same<T, __half>::value;
+    launch(kKHeadRows, k_head_rows, row_blocks(), 256, r);
+  }
+  // the part of a piece of the words in both gradients
+  void gradients(uint32_t from, uint32_t words, const Operand& hidden_scaled, const Gradients& to, const float* down) {
+    const Operand g = {base + L.off_g, words, a.rows, L.ldg}, piece = {static_cast<const T*>(head.at) + (uint64_t)from * head.ld, a.dim, words, head.ld};
+    Product p = product();
+    p.m = (uint32_t)a.rows, p.n = a.dim, p.k_blocks = tiles(words, kTileK);
+    p.splits = L.splits <= p.k_blocks ? L.splits : p.k_blocks;
+    p.out = base + L.off_parts, p.ldo = L.ldp, p.split_stride = a.rows * L.ldp, p.add = from != 0;
+    multiply<kParts, false, true>(kKHeadParts, p, g, piece);
+    p = product();
+    p.m = words, p.n = a.dim, p.k_blocks = tiles(a.rows, kTileK);
+    T* const out = static_cast<T*>(to.d_head) + (uint64_t)from * to.d_head_stride;
+    p.out = out, p.ldo = to.d_head_stride, p.wide = reinterpret_cast<uintptr_t>(out) % 32 == 0 && to.d_head_stride % 16 == 0;
+    p.alpha_dev = down;
+    multiply<kGrad, true, true>(kKHeadGrad, p, g, hidden_scaled);
+  }
+  void join(const Gradients& to, const float* factor, const float* down) {
+    JoinArgs j = {};
+    j.parts = at<float>(L.off_parts), j.split_stride = a.rows * L.ldp, j.ldp = L.ldp, j.ldo = to.d_hidden_stride;
+    j.splits = L.splits, j.dim = a.dim, j.rows = a.rows, j.alpha = a.scale, j.factor = factor, j.down = down, j.header = header, j.out = to.d_hidden;
+    launch(kKHeadJoin, k_head_join<T>, (uint32_t)((a.rows * ((a.dim + 3) / 4) + 255) / 256), 256, j);
+  }
+  void run_kept(float* loss, const Gradients& to) {
+    TargetArgs t = {};
+    t.hidden = hidden.at, t.head = head.at, t.targets = a.targets_dev, t.hidden_ld = hidden.ld, t.head_ld = head.ld, t.rows = a.rows, t.dim = a.dim;
+    t.vocab = a.vocab, t.token_bytes = a.token_bytes, t.blocks_wild = L.blocks_wild, t.weight = a.row_weight_dev, t.at_target = at<float>(L.off_target);
+    t.k2 = a.scale * kLog2E, t.wild = at<uint32_t>(L.off_wild), t.header = header;
+    launch(kKHeadTarget, k_head_target, tiles(a.rows, 8), 256, t);
+    for (uint32_t turn = 0; turn < 2; ++turn) {
+      Product p = product();
+      p.m = (uint32_t)a.rows, p.n = a.vocab, p.k_blocks = tiles(a.dim, kTileK), p.first = turn == 0;
+      p.out = base + L.off_g, p.ldo = L.ldg;
+      if (turn) p.skip = &header->wild, p.wild = t.wild;
+      if constexpr (std::is_same<T, __nv_bfloat16>::value) multiply<kKeep, false, false>(kKHeadKeep, p, hidden, head);
+      RowsArgs r = rows(loss);
+      r.kept = at<__nv_bfloat16>(L.off_g), r.ldg = L.ldg, r.hidden = static_cast<const __nv_bfloat16*>(hidden.at), r.hidden_ld = hidden.ld;
+      r.scaled = at<__nv_bfloat16>(L.off_scaled), r.scaled_ld = L.ld, r.factor = at<float>(L.off_factor), r.raised = at<float>(L.off_raised), r.wild = t.wild;
+      r.dim = a.dim, r.second = turn;
+      launch(kKHeadRows, k_head_rows_kept, row_blocks(), 256, r);
+    }
+    gradients(0, a.vocab, {base + L.off_scaled, a.dim, a.rows, L.ld}, to, nullptr);
+    join(to, at<float>(L.off_factor), nullptr);
+  }
+  void run_pieces(float* loss, const Gradients& to) {
+    const bool half = std::is_same<T, __half>::value;
+    if (half) launch(kKHeadBegin, k_head_begin, 1, a.rows > 256 ? 1024 : 256, header, a.row_weight_dev, a.targets_dev, a.token_bytes, a.rows, a.vocab);
+    copy(hidden, L.off_hidden, a.targets_dev);
+    if (L.copy_head) copy(head, L.off_head, nullptr);
+    logits_once(loss, true);
+    const float* const down = half ? &header->down : nullptr;
+    for (uint32_t i = 0; i < L.pieces; ++i) {
+      const uint32_t from = i * L.piece, words = i + 1 < L.pieces ? L.piece : a.vocab - from;
+      Product p = product();
+      p.m = (uint32_t)a.rows, p.n = words, p.k_blocks = tiles(a.dim, kTileK), p.col0 = from, p.row = at<float4>(L.off_row);
+      p.out = base + L.off_g, p.ldo = L.ldg;
+      multiply<kProbs, false, false>(kKHeadProbs, p, hidden, {static_cast<const T*>(head.at) + (uint64_t)from * head.ld, a.dim, words, head.ld});
+      gradients(from, words, hidden, to, down);
+    }
+    join(to, nullptr, down);
+  }
+  cudaError_t run(float* loss, const Gradients* to) {
+    if (!to || L.keep) {
+      if (L.copy_hidden) copy(hidden, L.off_hidden, nullptr);
+      if (L.copy_head) copy(head, L.off_head, nullptr);
+    }
+    if (!to) logits_once(loss, false);
+    else if (L.keep) run_kept(loss, *to);
+    else run_pieces(loss, *to);
+    return error != cudaSuccess ? error : cudaGetLastError();
+  }
+};
 
 }  // namespace
 
@@ -610,8 +917,9 @@ size_t head_ws_bytes(const cvlc_head& a, uint32_t pieces) { return head_layout(a
 
 cudaError_t launch_head(const cvlc_head& a, uint32_t pieces, float* loss, void* d_hidden, uint64_t d_hidden_stride, void* d_head, uint64_t d_head_stride, void* ws,
                         cudaStream_t st) {
-  if (a.dtype == CVLC_F16) return run_head<__half>(a, pieces, loss, d_hidden, d_hidden_stride, d_head, d_head_stride, ws, st);
-  return run_head<__nv_bfloat16>(a, pieces, loss, d_hidden, d_hidden_stride, d_head, d_head_stride, ws, st);
+  const Gradients g = {d_hidden, d_hidden_stride, d_head, d_head_stride};
+  if (a.dtype == CVLC_F16) return HeadRun<__half>(a, pieces, ws, st).run(loss, pieces ? &g : nullptr);
+  return HeadRun<__nv_bfloat16>(a, pieces, ws, st).run(loss, pieces ? &g : nullptr);
 }
 
 }  // namespace cvlc

@@ -15,14 +15,38 @@ bool make_tensor_map(CUtensorMap* map, const void* base, bool bf16, uint64_t col
 #ifdef __CUDACC__
 
 __device__ __forceinline__ uint32_t smem_at(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
-// the same place in the shared memory of the cluster's first block (the bit that tells the two blocks of a pair apart is cleared)
-__device__ __forceinline__ uint32_t leader_at(uint32_t at) { return at & 0xFEFFFFFFu; }
+// Two blocks of a cluster (CG = 2) make a tile of twice the rows together: each copies its half of both operands, the first one, the leader, issues the
+// products of both, and what the leader waits for is reported to its barriers.  The same place in the leader's shared memory:
+template <int CG>
+__device__ __forceinline__ uint32_t leader_at(uint32_t at) {
+  if constexpr (CG == 1) return at;
+  uint32_t r;
+  asm("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(r) : "r"(at));
+  return r;
+}
+template <int CG>
+__device__ __forceinline__ uint32_t pair_rank() {
+  if constexpr (CG == 1) return 0;
+  uint32_t r;
+  asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+template <int CG>
+__device__ __forceinline__ void pair_sync() {  // of all threads
+  if constexpr (CG == 1) __syncthreads();
+  else asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
 
 __device__ __forceinline__ void mbar_init(uint64_t* b, uint32_t n) { asm volatile("mbarrier.init.shared.b64 [%0], %1;" ::"r"(smem_at(b)), "r"(n)); }
 __device__ __forceinline__ void mbar_expect(uint64_t* b, uint32_t bytes) {
   asm volatile("mbarrier.arrive.expect_tx.shared.b64 _, [%0], %1;" ::"r"(smem_at(b)), "r"(bytes) : "memory");
 }
 __device__ __forceinline__ void mbar_arrive(uint64_t* b) { asm volatile("mbarrier.arrive.shared.b64 _, [%0];" ::"r"(smem_at(b)) : "memory"); }
+template <int CG>
+__device__ __forceinline__ void mbar_arrive_leader(uint64_t* b) {
+  if constexpr (CG == 1) mbar_arrive(b);
+  else asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(leader_at<CG>(smem_at(b))) : "memory");
+}
 __device__ __forceinline__ bool mbar_try(uint64_t* b, uint32_t parity) {
   uint32_t done;
   asm volatile("{.reg .pred p;\n mbarrier.try_wait.parity.shared.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;}"
@@ -54,11 +78,12 @@ __device__ __forceinline__ bool mbar_wait(uint64_t* b, uint32_t parity, uint32_t
 }
 
 // ---- copies --------------------------------------------------------------------------------
+// `bar`: the leader's
 template <int CG>
 __device__ __forceinline__ void load_tile(const CUtensorMap& map, uint32_t to, uint32_t bar, uint32_t x, uint32_t y) {
   if constexpr (CG == 2)
     asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];" ::"r"(to),
-                 "l"(&map), "r"(leader_at(bar)), "r"(x), "r"(y)
+                 "l"(&map), "r"(bar), "r"(x), "r"(y)
                  : "memory");
   else
     asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];" ::"r"(to), "l"(&map), "r"(bar),

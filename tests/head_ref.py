@@ -13,8 +13,9 @@ def sums(n, size):
     return size * 2 * U * (n / 16 + 8)
 
 
-def step(hidden, head, targets, scale=1.0, weight=None):
-    """loss, d_hidden, d_head; the largest error of each before it is rounded to the operands' type, and its root mean square (the rounding of G to
+def step(hidden, head, targets, scale=1.0, weight=None, kept=False):
+    """kept: the exponentials are kept in 16 bits and their rows' factors go into the hidden states, which are rounded too for the head's gradient.
+    loss, d_hidden, d_head; the largest error of each before it is rounded to the operands' type, and its root mean square (the rounding of G to
     16 bits is off by a third of a half step, squared, on average)"""
     h, w = hidden.double(), head.double()
     rows, vocab, dim = h.shape[0], w.shape[0], h.shape[1]
@@ -47,9 +48,13 @@ def step(hidden, head, targets, scale=1.0, weight=None):
     out = {"loss": loss, "d_hidden": G @ w * scale, "d_head": G.T @ h * scale}
     aw, ah = w.abs(), h.abs()
     tol["d_hidden"] = abs(scale) * ((off + cut) @ aw + sums(vocab, G.abs() @ aw)) + out["d_hidden"].abs() * 4 * U
-    tol["d_head"] = abs(scale) * ((off + cut).T @ ah + sums(rows, G.abs().T @ ah)) + out["d_head"].abs() * 4 * U
+    if kept:
+        cut_head, square = cut + G.abs() * u * 1.01, cut.square() + (G.abs() * u).square()
+    else:
+        cut_head, square = cut, cut.square()
+    tol["d_head"] = abs(scale) * ((off + cut_head).T @ ah + sums(rows, G.abs().T @ ah)) + out["d_head"].abs() * 4 * U
     mean = {"d_hidden": abs(scale) * ((off @ aw + sums(vocab, G.abs() @ aw)).square() + (cut.square() / 3) @ w.square()).sqrt(),
-            "d_head": abs(scale) * ((off.T @ ah + sums(rows, G.abs().T @ ah)).square() + (cut.square().T / 3) @ h.square()).sqrt()}
+            "d_head": abs(scale) * ((off.T @ ah + sums(rows, G.abs().T @ ah)).square() + (square.T / 3) @ h.square()).sqrt()}
     return out, tol, mean
 
 
@@ -64,8 +69,10 @@ def assert_near(got, want, tol, what="", mean=None):
         assert float(err.norm()) <= 1.5 * float(mean.norm()), (what, float(err.norm() / mean.norm()))
 
 
-def check(loss, d_hidden, d_head, hidden, head, targets, scale=1.0, weight=None):
-    want, tol, mean = step(hidden, head, targets, scale, weight)
+def check(loss, d_hidden, d_head, hidden, head, targets, scale=1.0, weight=None, pieces=1):
+    vocab = head.shape[0]
+    kept = hidden.dtype == torch.bfloat16 and vocab <= (-(-vocab // pieces) + 255) // 256 * 256
+    want, tol, mean = step(hidden, head, targets, scale, weight, kept)
     assert_near(loss, want["loss"], tol["loss"] * 1.01 + want["loss"].abs() * U, "loss")
     for name, got in (("d_hidden", d_hidden), ("d_head", d_head)):
         if got is None:

@@ -44,7 +44,7 @@ def run(hidden, head, targets, scale=1.0, weight=None, pieces=1, pad=0, shift=0,
 
 def check(hidden, head, targets, scale=1.0, weight=None, **how):
     alone, loss, dh, dw = run(hidden, head, targets, scale, weight, **how)
-    R.check(loss, dh, dw, hidden, head, targets, scale, weight)
+    R.check(loss, dh, dw, hidden, head, targets, scale, weight, how.get("pieces", 1))
     R.check(alone, None, None, hidden, head, targets, scale, weight)
     return loss, dh, dw
 
@@ -129,6 +129,25 @@ def test_far_logits(dtype, pieces):
     hidden[128:192] *= 12
     loss, _, _ = check(hidden, head, t, pieces=pieces)
     assert float(loss.max()) > 500 and 0 < float(loss[64:128].max()) and float(loss.min()) < 1e-30
+
+
+@pytest.mark.parametrize("rows", [3, 128, 129, 700])
+def test_rows_far_above_their_target(rows):
+    """some word 2^60 times and more as likely as the target, in single rows, next to others of the same tiles and of others"""
+    hidden, head, t = make(rows, 64, 800, width=8.0)
+    weight = torch.rand(rows, device="cuda")
+    for i in {0, rows // 2, rows - 1}:
+        hidden[i] = (-25 * head[t[i]].float()).to(BF)
+    loss, _, _ = check(hidden, head, t, scale=0.9, weight=weight)
+    assert int((loss > 60 * weight).sum()) >= 1
+    t[0] = -1
+    check(hidden, head, t, scale=0.9, weight=weight)
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("scale", [0.0, -1.5])
+def test_any_scale(dtype, scale):
+    check(*make(200, 64, 700, dtype), scale=scale)
 
 
 @pytest.mark.parametrize("dtype", [BF, HF])
