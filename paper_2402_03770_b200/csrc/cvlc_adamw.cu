@@ -15,7 +15,7 @@ namespace {
 constexpr int kBlock = CVLC_STATE_BLOCK;  // values of a warp at a time, and of a scale
 constexpr int kPer = kBlock / 32;         // consecutive ones of a lane
 constexpr int kThreads = 256, kWarps = kThreads / 32;
-constexpr uint32_t kNormChunks = 16 * kNumSM;  // of the norm, at most, and one more for every tensor
+constexpr uint32_t kNormChunks = 64 * kNumSM;  // of the norm, at most, and one more for every tensor
 
 // Which of a tensor's arrays can be read and written by vectors.  fp32 states have no blocks of their own, so that their tensors are cut where the
 // weights' addresses are multiples of 32 bytes: `lead` values before the first are not there.
@@ -60,28 +60,52 @@ __device__ __forceinline__ uint32_t tensor_of(const TensorList<CAP>& L, uint32_t
   return lo;
 }
 
-// eight values from `at` on; those outside of [0, n) are 0 and are not touched
-template <class T>
-__device__ __forceinline__ void load8(const void* base, int64_t at, uint64_t n, bool vec, float (&x)[kPer]) {
-  const T* p = static_cast<const T*>(base) + at;
-  if (vec && at >= 0 && (uint64_t)at + kPer <= n) {
-    constexpr int per = kPerVec<T>;
+// Eight values from `at` on, in two steps, so that the loads of all arrays are on their way before the first value is used.  Those outside of [0, n) are 0
+// and are not touched.
+struct Raw {
+  uint4 a, b;  // b: of fp32 only
+};
+__device__ __forceinline__ uint4 scalars16(const uint16_t* p, int64_t at, uint64_t n) {
+  uint32_t x[kPer];
 #pragma unroll
-    for (int i = 0; i < kPer / per; ++i) {
-      float y[per];
-      widen<T>(__ldcs(reinterpret_cast<const uint4*>(p) + i), y);
+  for (int i = 0; i < kPer; ++i) x[i] = (uint64_t)(at + i) < n ? p[i] : 0u;
+  return make_uint4(x[0] | x[1] << 16, x[2] | x[3] << 16, x[4] | x[5] << 16, x[6] | x[7] << 16);
+}
+__device__ __forceinline__ Raw fetch8(bool f32, const void* base, int64_t at, uint64_t n, bool vec) {
+  Raw r;
+  if (f32) {
+    const uint32_t* const p = static_cast<const uint32_t*>(base) + at;
+    if (vec) {
+      r.a = __ldcs(reinterpret_cast<const uint4*>(p)), r.b = __ldcs(reinterpret_cast<const uint4*>(p) + 1);
+    } else {
+      uint32_t x[kPer];
 #pragma unroll
-      for (int k = 0; k < per; ++k) x[i * per + k] = y[k];
+      for (int i = 0; i < kPer; ++i) x[i] = (uint64_t)(at + i) < n ? p[i] : 0u;
+      r.a = make_uint4(x[0], x[1], x[2], x[3]), r.b = make_uint4(x[4], x[5], x[6], x[7]);
     }
   } else {
+    const uint16_t* const p = static_cast<const uint16_t*>(base) + at;
+    r.a = vec ? __ldcs(reinterpret_cast<const uint4*>(p)) : scalars16(p, at, n);
+    r.b = make_uint4(0, 0, 0, 0);
+  }
+  return r;
+}
+__device__ __forceinline__ void widen8(uint32_t dtype, const Raw& r, float (&x)[kPer]) {
+  if (dtype == CVLC_F32) {
+    float y[4], z[4];
+    widen<float>(r.a, y), widen<float>(r.b, z);
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) x[i] = (uint64_t)(at + i) < n ? to_float(p[i]) : 0.0f;
+    for (int i = 0; i < 4; ++i) x[i] = y[i], x[4 + i] = z[i];
+  } else if (dtype == CVLC_F16) {
+    widen<__half>(r.a, x);
+  } else {
+    widen<__nv_bfloat16>(r.a, x);
   }
 }
 template <class T>
 __device__ __forceinline__ void store8(void* base, int64_t at, uint64_t n, bool vec, const float (&x)[kPer]) {
   T* p = static_cast<T*>(base) + at;
-  if (vec && at >= 0 && (uint64_t)at + kPer <= n) {
+  if (vec) {
     constexpr int per = kPerVec<T>;
 #pragma unroll
     for (int i = 0; i < kPer / per; ++i) {
@@ -96,19 +120,14 @@ __device__ __forceinline__ void store8(void* base, int64_t at, uint64_t n, bool 
       if ((uint64_t)(at + i) < n) p[i] = from_float<T>(x[i]);
   }
 }
-__device__ __forceinline__ void load8(uint32_t dtype, const void* base, int64_t at, uint64_t n, bool vec, float (&x)[kPer]) {
-  if (dtype == CVLC_F32) load8<float>(base, at, n, vec, x);
-  else if (dtype == CVLC_F16) load8<__half>(base, at, n, vec, x);
-  else load8<__nv_bfloat16>(base, at, n, vec, x);
-}
 __device__ __forceinline__ void store8(uint32_t dtype, void* base, int64_t at, uint64_t n, bool vec, const float (&x)[kPer]) {
   if (dtype == CVLC_F32) store8<float>(base, at, n, vec, x);
   else if (dtype == CVLC_F16) store8<__half>(base, at, n, vec, x);
   else store8<__nv_bfloat16>(base, at, n, vec, x);
 }
-__device__ __forceinline__ uint2 load_bytes(const void* base, int64_t at, uint64_t n, bool vec) {
+__device__ __forceinline__ uint2 fetch_bytes(const void* base, int64_t at, uint64_t n, bool vec) {
   const uint8_t* p = static_cast<const uint8_t*>(base) + at;
-  if (vec && (uint64_t)at + kPer <= n) return __ldcs(reinterpret_cast<const uint2*>(p));
+  if (vec) return __ldcs(reinterpret_cast<const uint2*>(p));
   uint32_t w[2] = {0, 0};
 #pragma unroll
   for (int i = 0; i < kPer; ++i)
@@ -117,7 +136,7 @@ __device__ __forceinline__ uint2 load_bytes(const void* base, int64_t at, uint64
 }
 __device__ __forceinline__ void store_bytes(void* base, int64_t at, uint64_t n, bool vec, const uint32_t (&w)[2]) {
   uint8_t* p = static_cast<uint8_t*>(base) + at;
-  if (vec && (uint64_t)at + kPer <= n) {
+  if (vec) {
     __stcs(reinterpret_cast<uint2*>(p), make_uint2(w[0], w[1]));
     return;
   }
@@ -130,18 +149,43 @@ __device__ __forceinline__ void store_bytes(void* base, int64_t at, uint64_t n, 
 // m is held in e4m3 (largest value 448), v in e5m2 (57344), relative to the largest value of the block of 256.  A float's bits are linear
 // between two neighbouring values of the short type, so rounding up with the probability of what is cut off is adding random bits below the cut.
 // Rounding to nearest would not do: an average that moves by a thousandth a step never leaves a value whose neighbours are an eighth away.
-template <int MANTISSA, int BIAS>
-__device__ __forceinline__ uint32_t to_float8(float y, uint32_t random16) {
-  constexpr int cut = 23 - MANTISSA;
-  constexpr float lowest = MANTISSA == 3 ? 0x1p-6f : 0x1p-14f;  // below it the steps stay as they are: a float of that size added has the same ones
-  const bool small = y < lowest;
-  const uint32_t bits = __float_as_uint(small ? y + lowest : y) + (random16 << (cut - 16)) + (1u << (cut - 17));
-  return (bits >> cut) - ((uint32_t)(127 - BIAS) << MANTISSA) - (small ? 1u << MANTISSA : 0u);
+// Times a power of two that brings the type's smallest normal value to fp32's, the code is the float's upper bits, subnormal values included
+// (their product is rounded at 2^-29 of the type's 1).  `random`: uniform below the cut, its lowest bit at half of what the random bits tell apart.
+template <int MANTISSA>
+__device__ __forceinline__ uint32_t to_float8(float y, uint32_t random) {
+  const float z = y * (MANTISSA == 3 ? 0x1p-120f : 0x1p-112f);
+  return min((__float_as_uint(z) + random) >> (23 - MANTISSA), MANTISSA == 3 ? 126u : 123u);  // up to the largest value: y may be above it by a rounding
 }
-template <int MANTISSA, int BIAS>
-__device__ __forceinline__ float from_float8(uint32_t code) {  // of 7 bits
-  // as a float's subnormal or normal number of another bias; the product with a power of two is exact
-  return __uint_as_float(code << (23 - MANTISSA)) * (BIAS == 7 ? 0x1p120f : 0x1p112f);
+// Four codes as floats: e4m3 by way of fp16, which holds all its values; e5m2 is the upper half of an fp16
+__device__ __forceinline__ void from_e4m3(uint32_t w, float (&x)[4]) {
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    uint32_t y;
+    asm("{.reg .b16 a, b;\n mov.b32 {a, b}, %1;\n cvt.rn.f16x2.e4m3x2 %0, a;}" : "=r"(y) : "r"(w >> (16 * h)));
+    __half2 z;
+    memcpy(&z, &y, 4);
+    const float2 f = __half22float2(z);
+    x[2 * h] = f.x, x[2 * h + 1] = f.y;
+  }
+}
+__device__ __forceinline__ void from_e5m2(uint32_t w, float (&x)[4]) {
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const uint32_t y = __byte_perm(w, 0, h ? 0x3424 : 0x1404);
+    __half2 z;
+    memcpy(&z, &y, 4);
+    const float2 f = __half22float2(z);
+    x[2 * h] = f.x, x[2 * h + 1] = f.y;
+  }
+}
+// all four words of a counter, the round keys worked out once
+__device__ __forceinline__ uint4 philox4x32_10(uint4 c, const PhiloxRoundKeys& rk) {
+#pragma unroll
+  for (int i = 0; i < 10; ++i) {
+    const unsigned long long p0 = (unsigned long long)0xD2511F53u * c.x, p1 = (unsigned long long)0xCD9E8D57u * c.z;
+    c = make_uint4((uint32_t)(p1 >> 32) ^ c.y ^ rk.x[i], (uint32_t)p1, (uint32_t)(p0 >> 32) ^ c.w ^ rk.y[i], (uint32_t)p0);
+  }
+  return c;
 }
 constexpr float kLeast = 0x1p-100f;  // a block whose largest value is below this is held as zeros
 
@@ -175,6 +219,7 @@ __global__ void __launch_bounds__(kThreads) k_adamw(const __grid_constant__ Tens
   }
   const uint32_t index = tensor_of(L, blockIdx.x);
   const TensorDesc& t = L.t[index];
+  const PhiloxRoundKeys keys = philox_round_keys(s.seed);
   const float lr = (s.lr_dev ? s.lr * *s.lr_dev : s.lr) * t.lr;
   const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x & 31;
   const uint64_t blocks = (t.n + t.lead + kBlock - 1) / kBlock;
@@ -182,23 +227,25 @@ __global__ void __launch_bounds__(kThreads) k_adamw(const __grid_constant__ Tens
   const uint64_t end = min(blocks, (uint64_t)(blockIdx.x - t.first + 1) * s.chunk);
   for (; block < end; block += kWarps) {
     const int64_t at = (int64_t)(block * kBlock + lane * kPer) - t.lead;
+    const uint32_t vec = at >= 0 && (uint64_t)at + kPer <= t.n ? t.vec : 0;
     float p[kPer], g[kPer], m[kPer], v[kPer];
-    load8(s.param_dtype, t.param, at, t.n, t.vec & kVecParam, p);
-    load8(s.grad_dtype, t.grad, at, t.n, t.vec & kVecGrad, g);
+    const Raw rp = fetch8(s.param_dtype == CVLC_F32, t.param, at, t.n, vec & kVecParam), rg = fetch8(s.grad_dtype == CVLC_F32, t.grad, at, t.n, vec & kVecGrad);
     if (EIGHT) {
-      const uint2 cm = load_bytes(t.m, at, t.n, t.vec & kVecM), cv = load_bytes(t.v, at, t.n, t.vec & kVecV);
+      const uint2 cm = fetch_bytes(t.m, at, t.n, vec & kVecM), cv = fetch_bytes(t.v, at, t.n, vec & kVecV);
       const float2 sc = __ldcs(t.scale + block);
-      const uint32_t wm[2] = {cm.x, cm.y}, wv[2] = {cv.x, cv.y};
 #pragma unroll
-      for (int i = 0; i < kPer; ++i) {
-        const uint32_t a = wm[i / 4] >> (8 * (i & 3)), b = wv[i / 4] >> (8 * (i & 3));
-        m[i] = __uint_as_float(__float_as_uint(from_float8<3, 7>(a & 127)) | (a & 128) << 24) * sc.x;
-        v[i] = from_float8<2, 15>(b & 127) * sc.y;
+      for (int h = 0; h < 2; ++h) {
+        float x[4], y[4];
+        from_e4m3(h ? cm.y : cm.x, x);
+        from_e5m2(h ? cv.y : cv.x, y);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) m[4 * h + i] = x[i] * sc.x, v[4 * h + i] = y[i] * sc.y;
       }
     } else {
-      load8<float>(t.m, at, t.n, t.vec & kVecM, m);
-      load8<float>(t.v, at, t.n, t.vec & kVecV, v);
+      const Raw rm = fetch8(true, t.m, at, t.n, vec & kVecM), rv = fetch8(true, t.v, at, t.n, vec & kVecV);
+      widen8(CVLC_F32, rm, m), widen8(CVLC_F32, rv, v);
     }
+    widen8(s.param_dtype, rp, p), widen8(s.grad_dtype, rg, g);
     uint32_t am = 0, av = 0;
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
@@ -206,47 +253,48 @@ __global__ void __launch_bounds__(kThreads) k_adamw(const __grid_constant__ Tens
       const float x = g[i] * scale;
       m[i] = s.b1 * m[i] + s.b1r * x;
       v[i] = s.b2 * v[i] + s.b2r * (x * x);
-      am = max(am, __float_as_uint(m[i]) & 0x7FFFFFFFu), av = max(av, __float_as_uint(v[i]) & 0x7FFFFFFFu);
-      float root;
+      if (EIGHT) am = max(am, __float_as_uint(m[i]) & 0x7FFFFFFFu), av = max(av, __float_as_uint(v[i]) & 0x7FFFFFFFu);
+      float root, inverse;
       asm("sqrt.approx.f32 %0, %1;" : "=f"(root) : "f"(v[i] * ic2));
-      p[i] -= lr * (t.decay * p[i] + __fdividef(m[i] * ic1, root + s.eps));
+      asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inverse) : "f"(root + s.eps));  // of 1e-30 or more
+      p[i] = fmaf(-lr, fmaf(t.decay, p[i], m[i] * ic1 * inverse), p[i]);
     }
-    store8(s.param_dtype, t.param, at, t.n, t.vec & kVecParam, p);
+    store8(s.param_dtype, t.param, at, t.n, vec & kVecParam, p);
     if (t.copy) {  // of the weights as they are held
       if (s.param_dtype != CVLC_F32)
 #pragma unroll
         for (int i = 0; i < kPer; ++i) p[i] = s.param_dtype == CVLC_F16 ? to_float(from_float<__half>(p[i])) : to_float(from_float<__nv_bfloat16>(p[i]));
-      if (s.copy_dtype == CVLC_F16) store8<__half>(t.copy, at, t.n, t.vec & kVecCopy, p);
-      else store8<__nv_bfloat16>(t.copy, at, t.n, t.vec & kVecCopy, p);
+      if (s.copy_dtype == CVLC_F16) store8<__half>(t.copy, at, t.n, vec & kVecCopy, p);
+      else store8<__nv_bfloat16>(t.copy, at, t.n, vec & kVecCopy, p);
     }
     if (EIGHT) {
       const float a = __uint_as_float(__reduce_max_sync(kFull, am)), b = __uint_as_float(__reduce_max_sync(kFull, av));
       const float ia = a >= kLeast ? 448.0f * (1.0f / a) : 0.0f, ib = b >= kLeast ? 57344.0f * (1.0f / b) : 0.0f;
       const uint64_t quad = (uint64_t)at / 4;
-      uint32_t wm[2] = {0, 0}, wv[2] = {0, 0};
+      uint32_t wm[2], wv[2];
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const uint4 r = philox4x32_10(make_uint4((uint32_t)(quad + h), (uint32_t)((quad + h) >> 32), s.tensor0 + index, step),
-                                      make_uint2((uint32_t)s.seed, (uint32_t)(s.seed >> 32)));
+        const uint4 r = philox4x32_10(make_uint4((uint32_t)(quad + h), (uint32_t)((quad + h) >> 32), s.tensor0 + index, step), keys);
         const uint32_t word[4] = {r.x, r.y, r.z, r.w};
+        uint32_t c[4], d[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const float x = m[4 * h + i], y = fminf(v[4 * h + i] * ib, 57344.0f);
-          uint32_t c = to_float8<3, 7>(fminf(fabsf(x) * ia, 448.0f), word[i] & 0xFFFF);
-          if (c) c |= __float_as_uint(x) >> 31 << 7;
-          uint32_t d = to_float8<2, 15>(y, word[i] >> 16);
+          const float x = m[4 * h + i], y = v[4 * h + i] * ib;
+          c[i] = to_float8<3>(fabsf(x) * ia, (word[i] << 4 & 0xFFFF0u) | 8u);
+          if (c[i]) c[i] |= __float_as_uint(x) >> 31 << 7;
           // a second moment that is there never becomes 0: the step would divide by eps alone
-          if (y > 0.0f) d = max(d, 1u); else d = 0;
-          wm[h] |= (c & 255) << (8 * i), wv[h] |= (d & 127) << (8 * i);
+          d[i] = max(to_float8<2>(y, (word[i] >> 11 & 0x1FFFE0u) | 16u), y > 0.0f ? 1u : 0u);
         }
+        wm[h] = __byte_perm(__byte_perm(c[0], c[1], 0x0040), __byte_perm(c[2], c[3], 0x0040), 0x5410);
+        wv[h] = __byte_perm(__byte_perm(d[0], d[1], 0x0040), __byte_perm(d[2], d[3], 0x0040), 0x5410);
       }
-      store_bytes(t.m, at, t.n, t.vec & kVecM, wm);
-      store_bytes(t.v, at, t.n, t.vec & kVecV, wv);
+      store_bytes(t.m, at, t.n, vec & kVecM, wm);
+      store_bytes(t.v, at, t.n, vec & kVecV, wv);
       // 0 for a block of zeros; what is not a number stays that
       if (lane == 0) __stcs(t.scale + block, make_float2(a < kLeast ? 0.0f : a * (1.0f / 448.0f), b < kLeast ? 0.0f : b * (1.0f / 57344.0f)));
     } else {
-      store8<float>(t.m, at, t.n, t.vec & kVecM, m);
-      store8<float>(t.v, at, t.n, t.vec & kVecV, v);
+      store8<float>(t.m, at, t.n, vec & kVecM, m);
+      store8<float>(t.v, at, t.n, vec & kVecV, v);
     }
   }
 }
@@ -274,17 +322,19 @@ __global__ void __launch_bounds__(kThreads) k_norm_parts(const __grid_constant__
   constexpr int kAhead = 4;  // loads of a thread that are on their way together
   double sum = 0.0;
   for (uint32_t b = warp; b < mine; b += kAhead * kWarps) {
-    float g[kAhead][kPer];
+    Raw r[kAhead];
 #pragma unroll
     for (int k = 0; k < kAhead; ++k) {
-      const uint32_t at = b + k * kWarps;
-      load8(s.grad_dtype, t.grad, from + (int64_t)at * kBlock, at < mine ? t.n : 0, t.vec & kVecGrad, g[k]);
+      const int64_t at = from + (int64_t)(b + k * kWarps) * kBlock;
+      const uint64_t n = b + k * kWarps < mine ? t.n : 0;
+      r[k] = fetch8(s.grad_dtype == CVLC_F32, t.grad, at, n, (t.vec & kVecGrad) && at >= 0 && (uint64_t)at + kPer <= n);
     }
 #pragma unroll
     for (int k = 0; k < kAhead; ++k) {
-      float q = 0.0f;
+      float g[kPer], q = 0.0f;
+      widen8(s.grad_dtype, r[k], g);
 #pragma unroll
-      for (int i = 0; i < kPer; ++i) q = fmaf(g[k][i], g[k][i], q);
+      for (int i = 0; i < kPer; ++i) q = fmaf(g[i], g[i], q);
       sum += (double)q;
     }
   }
@@ -314,11 +364,11 @@ uint32_t step_chunk(uint64_t blocks) {
   while (chunk < 4 * kWarps && blocks / (2 * chunk) >= 8 * kNumSM) chunk *= 2;
   return chunk;
 }
+// At most kNormChunks in all: a block's work should be short next to all of it (1,907 chunks on 1,184 places: 243 us instead of NORMUS for 500 M bf16 values)
 uint32_t norm_chunk(uint64_t blocks) {
-  uint32_t chunk = kWarps;
-  while (chunk < 4 * kWarps && blocks / (2 * chunk) >= 2 * kNumSM) chunk *= 2;
-  while (blocks / chunk >= kNormChunks) chunk *= 2;
-  return chunk;
+  if (blocks < 8 * kWarps * (uint64_t)kNumSM) return kWarps;
+  const uint64_t whole = 4 * kWarps, chunk = (blocks + kNormChunks - 1) / kNormChunks;
+  return (uint32_t)((chunk + whole - 1) / whole * whole);
 }
 uint32_t misplaced(const void* p, size_t size, uint32_t per) { return (uint32_t)(reinterpret_cast<uintptr_t>(p) / size % per); }
 
