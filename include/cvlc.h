@@ -582,6 +582,7 @@ int cvlc_head_step(const cvlc_head* a, float* loss_dev, void* d_hidden_dev, uint
  *  lr_dev, step_dev   device words in place of values that a captured graph would hold: lr is multiplied by *lr_dev, t is *step_dev; or NULL
  *  norm_dev     clip = min(1, max_norm / *norm_dev) (cvlc_grad_norm's, with the same grad_scale); NULL: clip = 1.  If it is
  *               not finite the call changes nothing and reports NONFINITE_INPUT in *status_dev (one int32 of the caller's, or NULL)
+ * A value whose v / (1 - beta2^t) is above 2^104 (a gradient of 4e15) takes no step.
  * Tensors may begin at any element (16-byte alignment of all of a tensor's arrays, or the same misalignment with states of 32
  * bits, is faster), must not overlap, and are left alone where n = 0.  Equal inputs give equal bits.
  * Errors: INVALID_ARG (types, bits, a pointer that is not aligned to its type, n above 2^40 in all, betas outside [0, 1), eps below

@@ -30,7 +30,7 @@ struct TensorDesc {
   uint16_t vec, lead;
 };
 struct StepScalars {
-  float lr, b1, b1r, b2, b2r, eps, ic1, ic2, grad_scale, max_norm;
+  float lr, b1, b1r, b2, b2r, eps, ic1, ic2, grad_scale, max_norm;  // ic: 1 / (1 - beta^t), the second 2^24 times that
   double beta1, beta2;
   const float *norm, *lr_dev;
   const uint32_t* step_dev;
@@ -150,11 +150,23 @@ __device__ __forceinline__ void store_bytes(void* base, int64_t at, uint64_t n, 
 // between two neighbouring values of the short type, so rounding up with the probability of what is cut off is adding random bits below the cut.
 // Rounding to nearest would not do: an average that moves by a thousandth a step never leaves a value whose neighbours are an eighth away.
 // Times a power of two that brings the type's smallest normal value to fp32's, the code is the float's upper bits, subnormal values included
-// (their product is rounded at 2^-29 of the type's 1).  `random`: uniform below the cut, its lowest bit at half of what the random bits tell apart.
+// (their product is rounded at 2^-29 of the type's 1).  y, from 0 up, becomes its code in the upper byte of a word, moved there with the addition;
+// `random`: 16 random bits above half of what they tell apart.
 template <int MANTISSA>
 __device__ __forceinline__ uint32_t to_float8(float y, uint32_t random) {
-  const float z = y * (MANTISSA == 3 ? 0x1p-120f : 0x1p-112f);
-  return min((__float_as_uint(z) + random) >> (23 - MANTISSA), MANTISSA == 3 ? 126u : 123u);  // up to the largest value: y may be above it by a rounding
+  constexpr float most = MANTISSA == 3 ? 448.0f : 57344.0f, bias = MANTISSA == 3 ? 0x1p-120f : 0x1p-112f;
+  return __float_as_uint(fminf(y, most) * bias) * (MANTISSA == 3 ? 16u : 8u) + random;
+}
+__device__ __forceinline__ uint32_t upper_bytes(const uint32_t (&x)[4]) {
+  return __byte_perm(__byte_perm(x[0], x[1], 0x0073), __byte_perm(x[2], x[3], 0x0073), 0x5410);
+}
+// bit 7 of every byte whose lower seven bits are not all 0
+__device__ __forceinline__ uint32_t some_bits(uint32_t w) { return (w & 0x7F7F7F7Fu) + 0x7F7F7F7Fu; }
+// the largest of three sizes; what is not a number stays that
+__device__ __forceinline__ float largest(float a, float b, float c) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(fabsf(b)), "f"(fabsf(c)));
+  return r;
 }
 // Four codes as floats: e4m3 by way of fp16, which holds all its values; e5m2 is the upper half of an fp16
 __device__ __forceinline__ void from_e4m3(uint32_t w, float (&x)[4]) {
@@ -203,7 +215,7 @@ __global__ void __launch_bounds__(kThreads) k_adamw(const __grid_constant__ Tens
         if (k & 1) p1 *= q1, p2 *= q2;
         q1 *= q1, q2 *= q2;
       }
-      corrections[0] = (float)(1.0 / (1.0 - p1)), corrections[1] = (float)(1.0 / (1.0 - p2));
+      corrections[0] = (float)(1.0 / (1.0 - p1)), corrections[1] = (float)(0x1p24 / (1.0 - p2));
     }
     __syncthreads();
     ic1 = corrections[0], ic2 = corrections[1];
@@ -246,17 +258,16 @@ __global__ void __launch_bounds__(kThreads) k_adamw(const __grid_constant__ Tens
       widen8(CVLC_F32, rm, m), widen8(CVLC_F32, rv, v);
     }
     widen8(s.param_dtype, rp, p), widen8(s.grad_dtype, rg, g);
-    uint32_t am = 0, av = 0;
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
       // every product and sum is rounded by itself, in this order: what an 8-bit state becomes is then a function of its inputs' bits
       const float x = g[i] * scale;
       m[i] = s.b1 * m[i] + s.b1r * x;
       v[i] = s.b2 * v[i] + s.b2r * (x * x);
-      if (EIGHT) am = max(am, __float_as_uint(m[i]) & 0x7FFFFFFFu), av = max(av, __float_as_uint(v[i]) & 0x7FFFFFFFu);
+      // the root's argument is raised by 2^24, so that no v is flushed to 0 (above 2^104 it becomes infinite, and the step 0)
       float root, inverse;
-      asm("sqrt.approx.f32 %0, %1;" : "=f"(root) : "f"(v[i] * ic2));
-      asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inverse) : "f"(root + s.eps));  // of 1e-30 or more
+      asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(root) : "f"(v[i] * ic2));
+      asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inverse) : "f"(fmaf(root, 0x1p-12f, s.eps)));  // of 1e-30 or more
       p[i] = fmaf(-lr, fmaf(t.decay, p[i], m[i] * ic1 * inverse), p[i]);
     }
     store8(s.param_dtype, t.param, at, t.n, vec & kVecParam, p);
@@ -268,7 +279,10 @@ __global__ void __launch_bounds__(kThreads) k_adamw(const __grid_constant__ Tens
       else store8<__nv_bfloat16>(t.copy, at, t.n, vec & kVecCopy, p);
     }
     if (EIGHT) {
-      const float a = __uint_as_float(__reduce_max_sync(kFull, am)), b = __uint_as_float(__reduce_max_sync(kFull, av));
+      float am = 0.0f, av = 0.0f;
+#pragma unroll
+      for (int i = 0; i < kPer; i += 2) am = largest(am, m[i], m[i + 1]), av = largest(av, v[i], v[i + 1]);
+      const float a = __uint_as_float(__reduce_max_sync(kFull, __float_as_uint(am))), b = __uint_as_float(__reduce_max_sync(kFull, __float_as_uint(av)));
       const float ia = a >= kLeast ? 448.0f * (1.0f / a) : 0.0f, ib = b >= kLeast ? 57344.0f * (1.0f / b) : 0.0f;
       const uint64_t quad = (uint64_t)at / 4;
       uint32_t wm[2], wv[2];
@@ -277,16 +291,23 @@ __global__ void __launch_bounds__(kThreads) k_adamw(const __grid_constant__ Tens
         const uint4 r = philox4x32_10(make_uint4((uint32_t)(quad + h), (uint32_t)((quad + h) >> 32), s.tensor0 + index, step), keys);
         const uint32_t word[4] = {r.x, r.y, r.z, r.w};
         uint32_t c[4], d[4];
+        float y[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const float x = m[4 * h + i], y = v[4 * h + i] * ib;
-          c[i] = to_float8<3>(fabsf(x) * ia, (word[i] << 4 & 0xFFFF0u) | 8u);
-          if (c[i]) c[i] |= __float_as_uint(x) >> 31 << 7;
-          // a second moment that is there never becomes 0: the step would divide by eps alone
-          d[i] = max(to_float8<2>(y, (word[i] >> 11 & 0x1FFFE0u) | 16u), y > 0.0f ? 1u : 0u);
+          const float x = m[4 * h + i];
+          y[i] = v[4 * h + i] * ib;
+          c[i] = (to_float8<3>(fabsf(x) * ia, __byte_perm(word[i], 0x80, 0x5104)) & 0x7FFFFFFFu) | (__float_as_uint(x) & 0x80000000u);
+          d[i] = to_float8<2>(y[i], __byte_perm(word[i], 0x80, 0x5324));
         }
-        wm[h] = __byte_perm(__byte_perm(c[0], c[1], 0x0040), __byte_perm(c[2], c[3], 0x0040), 0x5410);
-        wv[h] = __byte_perm(__byte_perm(d[0], d[1], 0x0040), __byte_perm(d[2], d[3], 0x0040), 0x5410);
+        wm[h] = upper_bytes(c);
+        wm[h] &= some_bits(wm[h]) | 0x7F7F7F7Fu;  // 0 has no sign
+        // a second moment that is there never becomes 0: the step would divide by eps alone
+        if ((some_bits(upper_bytes(d)) & 0x80808080u) != 0x80808080u) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (d[i] < 1u << 24) d[i] = y[i] > 0.0f ? 1u << 24 : 0u;
+        }
+        wv[h] = upper_bytes(d);
       }
       store_bytes(t.m, at, t.n, vec & kVecM, wm);
       store_bytes(t.v, at, t.n, vec & kVecV, wv);
@@ -435,7 +456,7 @@ cudaError_t launch_adamw(const cvlc_adamw_tensor* t, uint32_t n, const cvlc_adam
   StepScalars s = {};
   s.lr = (float)a.lr, s.b1 = (float)a.beta1, s.b1r = (float)(1.0 - a.beta1), s.b2 = (float)a.beta2, s.b2r = (float)(1.0 - a.beta2), s.eps = (float)a.eps;
   s.beta1 = a.beta1, s.beta2 = a.beta2;
-  s.ic1 = (float)(1.0 / (1.0 - pow(a.beta1, (double)a.step))), s.ic2 = (float)(1.0 / (1.0 - pow(a.beta2, (double)a.step)));
+  s.ic1 = (float)(1.0 / (1.0 - pow(a.beta1, (double)a.step))), s.ic2 = (float)(0x1p24 / (1.0 - pow(a.beta2, (double)a.step)));
   s.grad_scale = a.grad_scale, s.max_norm = a.max_norm, s.norm = a.norm_dev, s.lr_dev = a.lr_dev, s.step_dev = a.step_dev, s.seed = a.seed, s.step = a.step;
   s.param_dtype = a.param_dtype, s.grad_dtype = a.grad_dtype, s.copy_dtype = a.copy_dtype, s.status = a.status_dev;
   s.chunk = step_chunk(blocks_of(t, n));
