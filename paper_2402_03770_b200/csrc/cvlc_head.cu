@@ -60,11 +60,11 @@ __device__ __forceinline__ bool any_late(const Header* h) {  // asked by all thr
   return __syncthreads_or((int)x) != 0;
 }
 
-enum Epilogue { kStats, kKeep, kProbs, kParts, kGrad };
+enum Epilogue { kStats, kKeep, kProbs, kParts, kGrad, kBoth };  // kBoth: parts, then grad
 struct Product {
   CUtensorMap a, b;
   uint32_t m, n, k_blocks;               // rows, columns, steps of 64 of the sum
-  uint32_t tiles_m, tiles_n, splits;     // of the sum
+  uint32_t tile_n, tiles_m, tiles_n, splits;  // columns of a tile; splits of the sum
   uint32_t m_first;                      // tiles of one column of tiles follow one another, else those of a row
   uint32_t col0, token_bytes;            // stats, probs: the word of column 0
   float k2, alpha;                       // scale log2(e); factor of the output
@@ -82,6 +82,12 @@ struct Product {
   Header* header;
   int32_t* status;
   uint32_t first;                        // of the call's products
+  uint32_t early;                        // the operands are there before the kernel in front has ended
+};
+template <int EPI>
+struct Products {
+  static constexpr int count = EPI == kBoth ? 2 : 1;
+  Product p[count];
 };
 __device__ __forceinline__ bool left_out(const Product& g, uint32_t w) {
   if (!g.wild) return false;
@@ -90,14 +96,14 @@ __device__ __forceinline__ bool left_out(const Product& g, uint32_t w) {
 }
 
 struct Work {
-  uint32_t m0, n0, k_from, k_to, split;
+  uint32_t m0, n0, n_end, slot, k_from, k_to, split;
 };
 template <int CG>
 __device__ __forceinline__ Work work_of(const Product& g, uint32_t w) {
   const uint32_t tiles = g.tiles_m * g.tiles_n, split = w / tiles, t = w - split * tiles;
   const uint32_t tm = g.m_first ? t % g.tiles_m : t / g.tiles_n, tn = g.m_first ? t / g.tiles_m : t % g.tiles_n;
   Work r;
-  r.m0 = (tm * CG + pair_rank<CG>()) * kTileM, r.n0 = tn * kTileN, r.split = split;
+  r.m0 = (tm * CG + pair_rank<CG>()) * kTileM, r.n0 = tn * g.tile_n, r.n_end = min(g.n, r.n0 + g.tile_n), r.slot = 2 * tn, r.split = split;
   r.k_from = (uint32_t)((uint64_t)g.k_blocks * split / g.splits), r.k_to = (uint32_t)((uint64_t)g.k_blocks * (split + 1) / g.splits);
   return r;
 }
@@ -131,15 +137,15 @@ __device__ __forceinline__ void finish_tile(const Product& g, const Work& w, uin
     float most = -CUDART_INF_F, sum = 0.0f;
     for (int c = 0; c < 4; ++c) {
       const uint32_t col = w.n0 + half * 128 + c * 32;
-      if (col >= g.n) break;
+      if (col >= w.n_end) break;
       tensor_load(tensor + c * 32, v);
       tensor_loaded(v);
 #pragma unroll
       for (int i = 0; i < 32; ++i) v[i] = v[i] * g.k2;
-      if (g.n - col < 32) {
+      if (w.n_end - col < 32) {
 #pragma unroll
         for (int i = 0; i < 32; ++i)
-          if (col + i >= g.n) v[i] = -CUDART_INF_F;
+          if (col + i >= w.n_end) v[i] = -CUDART_INF_F;
       }
       const bool mine = target >= col && target < (int64_t)col + 32;
       if (__any_sync(kFull, mine)) {
@@ -158,7 +164,7 @@ __device__ __forceinline__ void finish_tile(const Product& g, const Work& w, uin
       sum = fmaf(sum, exp2_fast(most - from), s);
       most = m;
     }
-    if (there && w.n0 + half * 128 < g.n) g.stats[(uint64_t)(w.n0 / 128 + half) * g.stats_stride + row] = make_float2(most, sum);
+    if (there) g.stats[(uint64_t)(w.slot + half) * g.stats_stride + row] = make_float2(most, sum);
   } else if constexpr (EPI == kKeep) {
     // relative to the target's own value, known from before: what is kept needs no second look.  A row of which some word is more than 2^60 times as likely as
     // the target is wild and gets a second turn, relative to its maximum.
@@ -168,16 +174,16 @@ __device__ __forceinline__ void finish_tile(const Product& g, const Work& w, uin
     float most = -CUDART_INF_F, sum = 0.0f;
     for (int c = 0; c < 4; ++c) {
       const uint32_t col = w.n0 + half * 128 + c * 32;
-      if (col >= g.n) break;
+      if (col >= w.n_end) break;
       tensor_load(tensor + c * 32, v);
       tensor_loaded(v);
 #pragma unroll
       for (int i = 0; i < 32; ++i) v[i] = fmaf(v[i], g.k2, -from);
       const bool mine = target >= col && target < (int64_t)col + 32;
-      if (g.n - col < 32 || __any_sync(kFull, mine)) {
+      if (w.n_end - col < 32 || __any_sync(kFull, mine)) {
 #pragma unroll
         for (int i = 0; i < 32; ++i)
-          if (col + i >= g.n || (mine && target == (int64_t)col + i)) v[i] = -CUDART_INF_F;
+          if (col + i >= w.n_end || (mine && target == (int64_t)col + i)) v[i] = -CUDART_INF_F;
       }
 #pragma unroll
       for (int i = 0; i < 32; ++i) most = fmaxf(most, v[i]), v[i] = exp2_fast(v[i]);
@@ -196,7 +202,7 @@ __device__ __forceinline__ void finish_tile(const Product& g, const Work& w, uin
         }
       }
     }
-    if (there && w.n0 + half * 128 < g.n) g.stats[(uint64_t)(w.n0 / 128 + half) * g.stats_stride + row] = make_float2(most, sum);
+    if (there) g.stats[(uint64_t)(w.slot + half) * g.stats_stride + row] = make_float2(most, sum);
   } else if constexpr (EPI == kProbs) {
     // x: ln sum exp in log2, less the exponent that is added; y: the weight, 0 where the row counts for nothing; z: the target's value
     const float4 r = there ? g.row[row] : make_float4(0, 0, 0, 0);
@@ -204,7 +210,7 @@ __device__ __forceinline__ void finish_tile(const Product& g, const Work& w, uin
     T* const out = static_cast<T*>(g.out) + (uint64_t)row * g.ldo;
     for (int c = 0; c < 4; ++c) {
       const uint32_t col = w.n0 + half * 128 + c * 32;
-      if (col >= g.n) break;
+      if (col >= w.n_end) break;
       tensor_load(tensor + c * 32, v);
       tensor_loaded(v);
 #pragma unroll
@@ -229,7 +235,7 @@ __device__ __forceinline__ void finish_tile(const Product& g, const Work& w, uin
     float* const out = static_cast<float*>(g.out) + w.split * g.split_stride + (uint64_t)row * g.ldo;
     for (int c = 0; c < 4; ++c) {
       const uint32_t col = w.n0 + half * 128 + c * 32;
-      if (col >= g.n) break;
+      if (col >= w.n_end) break;
       tensor_load(tensor + c * 32, v);
       tensor_loaded(v);
       if (there) {
@@ -253,13 +259,13 @@ __device__ __forceinline__ void finish_tile(const Product& g, const Work& w, uin
     const float alpha = g.alpha_dev ? g.alpha * *g.alpha_dev : g.alpha;
     for (int c = 0; c < 4; ++c) {
       const uint32_t col = w.n0 + half * 128 + c * 32;
-      if (col >= g.n) break;
+      if (col >= w.n_end) break;
       tensor_load(tensor + c * 32, v);
       tensor_loaded(v);
       uint32_t p[16];
 #pragma unroll
       for (int i = 0; i < 16; ++i) p[i] = pack2<T>(v[2 * i] * alpha, v[2 * i + 1] * alpha);
-      if (g.wide && col + 32 <= g.n) {
+      if (g.wide && col + 32 <= w.n_end) {
         if (there) {
           store_sector(out + (uint64_t)row * g.ldo + col, p);
           store_sector(out + (uint64_t)row * g.ldo + col + 16, p + 8);
@@ -271,7 +277,7 @@ __device__ __forceinline__ void finish_tile(const Product& g, const Work& w, uin
         const uint16_t* const from = reinterpret_cast<const uint16_t*>(stage) + lane;
         uint16_t* const to = reinterpret_cast<uint16_t*>(out) + (uint64_t)(w.m0 + quarter * 32) * g.ldo + col + lane;
         const uint32_t rows = min(32u, g.m - min(g.m, w.m0 + quarter * 32));
-        if (col + lane < g.n)
+        if (col + lane < w.n_end)
           for (uint32_t r = 0; r < rows; ++r) to[r * g.ldo] = from[r * 34];
         __syncwarp();
       }
@@ -280,12 +286,13 @@ __device__ __forceinline__ void finish_tile(const Product& g, const Work& w, uin
 }
 
 template <int EPI, bool A_ROWS, bool B_ROWS, class T, int CG>
-__global__ void __launch_bounds__(kThreads, 1) k_head_product(const __grid_constant__ Product g) {
+__global__ void __launch_bounds__(kThreads, 1) k_head_product(const __grid_constant__ Products<EPI> both) {
   constexpr int stages = kStages<CG>;
+  constexpr bool turning = EPI == kGrad || EPI == kBoth;
   extern __shared__ uint8_t dynamic[];
   __shared__ uint64_t full[stages], empty[stages], made[2], taken[2], over;
   __shared__ uint32_t tensor_at, late;
-  __shared__ uint32_t turn[EPI == kGrad ? kOutWarps * 32 * 17 : 1];
+  __shared__ uint32_t turn[turning ? kOutWarps * 32 * 17 : 1];
   const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x & 31, rank = pair_rank<CG>();
   const uint32_t ring = (smem_at(dynamic) + 1023) & ~1023u;
   if (threadIdx.x == 0) {
@@ -300,26 +307,31 @@ __global__ void __launch_bounds__(kThreads, 1) k_head_product(const __grid_const
   __syncthreads();
   pair_sync<CG>();
   tensor_after();
+  const Product& g0 = both.p[0];
   const uint32_t tensor = tensor_at, first = blockIdx.x / CG, apart = gridDim.x / CG;
-  pdl_enter();
-  const uint32_t items = g.skip && *g.skip == 0 ? 0 : g.tiles_m * g.tiles_n * g.splits;
+  if (!g0.early || warp >= 4) pdl_enter();
+  const uint32_t items0 = g0.skip && *g0.skip == 0 ? 0 : g0.tiles_m * g0.tiles_n * g0.splits;
+  const uint32_t items = items0 + (EPI == kBoth ? both.p[Products<EPI>::count - 1].tiles_m * both.p[Products<EPI>::count - 1].tiles_n : 0);
   bool ok = true;
   if (warp == 0 && lane == 0) {
     uint32_t s = 0, phase = 0, issued = 0;
     for (uint32_t w = first; ok && w < items; w += apart) {
+      const bool second = EPI == kBoth && w >= items0;
+      const Product& g = both.p[second ? Products<EPI>::count - 1 : 0];
       if (left_out(g, w)) continue;
-      const Work r = work_of<CG>(g, w);
+      const Work r = work_of<CG>(g, second ? w - items0 : w);
+      const bool a_rows = EPI == kBoth ? second : A_ROWS;
       for (uint32_t k = r.k_from; k < r.k_to; ++k) {
         if (!(ok = mbar_wait(empty + s, phase ^ 1, &late))) break;
-        if (rank == 0) mbar_expect(full + s, CG * kStageBytes<CG>);
-        const uint32_t a = ring + s * kStageBytes<CG>, b = a + kBytesA, bar = leader_at<CG>(smem_at(full + s)), n0 = r.n0 + rank * (kTileN / CG);
-        if constexpr (A_ROWS) {
+        if (rank == 0) mbar_expect(full + s, CG * kBytesA + g.tile_n * kTileK * 2);
+        const uint32_t a = ring + s * kStageBytes<CG>, b = a + kBytesA, bar = leader_at<CG>(smem_at(full + s)), n0 = r.n0 + rank * (g.tile_n / CG);
+        if (a_rows) {
 #pragma unroll
           for (uint32_t i = 0; i < kTileM / 64; ++i) load_tile<CG>(g.a, a + i * kTileBytes64, bar, r.m0 + 64 * i, k * kTileK);
         } else {
           load_tile<CG>(g.a, a, bar, k * kTileK, r.m0);
         }
-        if constexpr (B_ROWS) {
+        if constexpr (B_ROWS) {  // tiles of 256 columns only
 #pragma unroll
           for (uint32_t i = 0; i < kTileN / CG / 64; ++i) load_tile<CG>(g.b, b + i * kTileBytes64, bar, n0 + 64 * i, k * kTileK);
         } else {
@@ -338,12 +350,16 @@ __global__ void __launch_bounds__(kThreads, 1) k_head_product(const __grid_const
       }
     }
   } else if (warp == 1 && lane == 0 && rank == 0) {
-    constexpr uint32_t kind = product_kind(std::is_same<T, __nv_bfloat16>::value, A_ROWS, B_ROWS, CG * kTileM, kTileN);
+    constexpr bool bf16 = std::is_same<T, __nv_bfloat16>::value;
     uint32_t s = 0, phase = 0, turn_of = 0;
     bool any = false;
     for (uint32_t w = first; ok && w < items; w += apart) {
+      const bool second = EPI == kBoth && w >= items0;
+      const Product& g = both.p[second ? Products<EPI>::count - 1 : 0];
       if (left_out(g, w)) continue;
-      const Work r = work_of<CG>(g, w);
+      const Work r = work_of<CG>(g, second ? w - items0 : w);
+      const bool a_rows = EPI == kBoth ? second : A_ROWS;
+      const uint32_t kind = product_kind(bf16, a_rows, B_ROWS, CG * kTileM, g.tile_n);
       const uint32_t half = turn_of & 1;
       if (!(ok = mbar_wait(taken + half, (turn_of / 2 & 1) ^ 1, &late))) break;
       tensor_after();
@@ -353,8 +369,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_head_product(const __grid_const
         const uint32_t a = ring + s * kStageBytes<CG>, b = a + kBytesA;
 #pragma unroll
         for (uint32_t i = 0; i < kTileK / 16; ++i)
-          multiply<CG>(tensor + half * kTileN, operand<A_ROWS>(a + i * kStepBytes<A_ROWS>), operand<B_ROWS>(b + i * kStepBytes<B_ROWS>), kind,
-                       k != r.k_from || i != 0);
+          multiply<CG>(tensor + half * kTileN, a_rows ? operand<true>(a + i * kStepBytes<true>) : operand<false>(a + i * kStepBytes<false>),
+                       operand<B_ROWS>(b + i * kStepBytes<B_ROWS>), kind, k != r.k_from || i != 0);
         commit<CG>(empty + s);
         any = true;
         if (++s == stages) s = 0, phase ^= 1;
@@ -371,12 +387,21 @@ __global__ void __launch_bounds__(kThreads, 1) k_head_product(const __grid_const
     const uint32_t half_tile = (warp - 4) / 4, quarter = warp & 3;
     uint32_t turn_of = 0;
     for (uint32_t w = first; w < items; w += apart) {
+      const bool second = EPI == kBoth && w >= items0;
+      const Product& g = both.p[second ? Products<EPI>::count - 1 : 0];
       if (left_out(g, w)) continue;
-      const Work r = work_of<CG>(g, w);
+      const Work r = work_of<CG>(g, second ? w - items0 : w);
       const uint32_t half = turn_of & 1;
       if (!(ok = __all_sync(kFull, mbar_wait(made + half, turn_of / 2 & 1, &late)))) break;
       tensor_after();
-      finish_tile<EPI, T>(g, r, tensor + half * kTileN + half_tile * 128 + (quarter * 32 << 16), half_tile, quarter, lane, turn + (EPI == kGrad ? (warp - 4) * 32 * 17 : 0));
+      const uint32_t at = tensor + half * kTileN + half_tile * 128 + (quarter * 32 << 16);
+      uint32_t* const stage = turn + (turning ? (warp - 4) * 32 * 17 : 0);
+      if constexpr (EPI == kBoth) {
+        if (second) finish_tile<kGrad, T>(g, r, at, half_tile, quarter, lane, stage);
+        else finish_tile<kParts, T>(g, r, at, half_tile, quarter, lane, stage);
+      } else {
+        finish_tile<EPI, T>(g, r, at, half_tile, quarter, lane, stage);
+      }
       tensor_before();
       __syncwarp();
       if (lane == 0) mbar_arrive_leader<CG>(taken + half);
@@ -389,12 +414,12 @@ __global__ void __launch_bounds__(kThreads, 1) k_head_product(const __grid_const
   pair_sync<CG>();
   tensor_after();
   if (warp == 2) tensor_free<CG>(tensor);
-  if (threadIdx.x == 0) {
+  if (threadIdx.x == 128) {  // of the warps that have waited for the kernel in front
     for (uint32_t i = blockIdx.x; i < kNumSM; i += gridDim.x) {
-      if (g.first) g.header->late[i] = late;  // nobody has written here
-      else if (late) g.header->late[i] = 1;
+      if (g0.first) g0.header->late[i] = late;  // nobody has written here
+      else if (late) g0.header->late[i] = 1;
     }
-    if (late && g.status) set_status(g.status, CVLC_ERR_DEVICE_TIMEOUT);
+    if (late && g0.status) set_status(g0.status, CVLC_ERR_DEVICE_TIMEOUT);
   }
 }
 
@@ -438,12 +463,21 @@ __global__ void __launch_bounds__(256) k_head_align(const uint16_t* from, uint64
     const int64_t t = target_of(targets, token_bytes, row);
     counts = t >= 0 && t < (int64_t)vocab && !(weight && weight[row] == 0.0f);
   }
-  const bool vectors = reinterpret_cast<uintptr_t>(src) % 16 == 0;
+  // rows that begin anywhere are read by the two vectors that hold eight elements
+  const uint32_t lead = (uint32_t)(reinterpret_cast<uintptr_t>(src) % 16 / 2);
+  const uint4* const vectors = reinterpret_cast<const uint4*>(src - lead);
   for (uint32_t i = lane * 8; i < dim; i += 256) {
     uint4 v = make_uint4(0, 0, 0, 0);
     if (counts) {
-      if (vectors && i + 8 <= dim) {
-        v = __ldg(reinterpret_cast<const uint4*>(src + i));
+      if (lead == 0 ? i + 8 <= dim : i >= lead && i + 16 - lead <= dim) {
+        const uint4 x = __ldg(vectors + i / 8), y = lead ? __ldg(vectors + i / 8 + 1) : x;
+        const uint32_t w[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+        const uint32_t skip = lead / 2, bits = (lead & 1) * 16;
+        uint32_t z[5];
+#pragma unroll
+        for (int k = 0; k < 5; ++k) z[k] = skip == 0 ? w[k] : skip == 1 ? w[k + 1] : skip == 2 ? w[k + 2] : w[k + 3 < 8 ? k + 3 : 7];
+        v = make_uint4(__funnelshift_r(z[0], z[1], bits), __funnelshift_r(z[1], z[2], bits), __funnelshift_r(z[2], z[3], bits),
+                       __funnelshift_r(z[3], z[4], bits));
       } else {
         uint32_t x[8];
 #pragma unroll
@@ -454,6 +488,10 @@ __global__ void __launch_bounds__(256) k_head_align(const uint16_t* from, uint64
     *reinterpret_cast<uint4*>(dst + i) = v;  // rows of the copy are filled up to eight
   }
 }
+
+// The kernel behind may be set up while this one runs: it has a block on every SM, whose first steps (barriers, tensor memory, and the operands' first tiles
+// where they do not come from here) need nothing of this one's; it waits for the rest.
+__device__ __forceinline__ void let_next_in() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 
 // z of every row's target, in log2; +inf where the row counts for nothing.  A warp a row.
 struct TargetArgs {
@@ -468,6 +506,7 @@ struct TargetArgs {
 };
 __global__ void __launch_bounds__(256) k_head_target(const TargetArgs a) {
   pdl_enter();
+  let_next_in();
   const uint64_t row = (uint64_t)blockIdx.x * 8 + threadIdx.x / 32;
   const uint32_t lane = threadIdx.x & 31;
   if (blockIdx.x == 0 && threadIdx.x == 0) a.header->wild = 0;
@@ -524,33 +563,40 @@ struct RowsArgs {
 };
 constexpr uint32_t kRowsOf = 8, kGroups = 32;  // rows of a block, threads of a row
 
-// The parts of a block's rows joined, by thread (group, row)
-__device__ __forceinline__ float2 join_parts(const RowsArgs& a, uint64_t row, uint32_t group, bool relative, float2 (*part)[kRowsOf]) {
-  float m = -CUDART_INF_F, s = 0.0f;
+// two parts of a row (maximum, sum): of sums relative to their own maxima, or of sums of the same reference
+__device__ __forceinline__ float2 join_two(float2 x, float2 y, bool relative) {
+  const float m = fmaxf(x.x, y.x), from = m == -CUDART_INF_F ? 0.0f : m;
+  return make_float2(m, relative ? x.y * exp2f(x.x - from) + y.y * exp2f(y.x - from) : x.y + y.y);
+}
+// The parts of a block's rows joined: eight threads hold what is left of each, one of a warp.
+__device__ __forceinline__ void join_parts(const RowsArgs& a, uint64_t row, uint32_t group, bool relative, float2 (*part)[kRowsOf]) {
+  float2 sum = make_float2(-CUDART_INF_F, 0.0f);
   if (row < a.rows) {
-#pragma unroll 4
-    for (uint32_t i = group; i < a.slots; i += kGroups) {
-      const float2 x = a.stats[(uint64_t)i * a.stats_stride + row];
-      const float n = fmaxf(m, x.x);
-      if (relative) {  // each to its own maximum
-        const float from = n == -CUDART_INF_F ? 0.0f : n;
-        s = s * exp2f(m - from) + x.y * exp2f(x.x - from);
-      } else {
-        s += x.y;
-      }
-      m = n;
+    const float2* const from = a.stats + row;
+    uint32_t i = group;
+    for (; i + 3 * kGroups < a.slots; i += 4 * kGroups) {
+      float2 x[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) x[k] = from[(uint64_t)(i + k * kGroups) * a.stats_stride];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) sum = join_two(sum, x[k], relative);
     }
+    for (; i < a.slots; i += kGroups) sum = join_two(sum, from[(uint64_t)i * a.stats_stride], relative);
   }
-  part[group][threadIdx.x % kRowsOf] = make_float2(m, s);
+#pragma unroll
+  for (int d = kRowsOf; d < 32; d *= 2) {
+    const float2 other = make_float2(__shfl_xor_sync(kFull, sum.x, d), __shfl_xor_sync(kFull, sum.y, d));
+    sum = join_two(sum, other, relative);
+  }
+  if ((threadIdx.x & 31) < kRowsOf) part[threadIdx.x / 32][threadIdx.x % kRowsOf] = sum;
   __syncthreads();
-  return make_float2(m, s);
 }
 
 // A row's parts joined.  Sums relative to the largest; that of the words other than the target (o) is kept apart, so that 1 - q and a small loss
 // ln(1 + o) keep their accuracy.
 __global__ void __launch_bounds__(256) k_head_rows(const RowsArgs a) {
   pdl_enter();
-  __shared__ float2 part[kGroups][kRowsOf];
+  __shared__ float2 part[8][kRowsOf];
   const uint32_t group = threadIdx.x / kRowsOf, lane = threadIdx.x % kRowsOf;
   const uint64_t row = (uint64_t)blockIdx.x * kRowsOf + lane;
   const bool late = any_late(a.header);
@@ -566,9 +612,9 @@ __global__ void __launch_bounds__(256) k_head_rows(const RowsArgs a) {
   }
   const float zt = a.at_target[row];
   float most = zt;
-  for (uint32_t i = 0; i < kGroups; ++i) most = fmaxf(most, part[i][lane].x);
+  for (uint32_t i = 0; i < 8; ++i) most = fmaxf(most, part[i][lane].x);
   double others = 0.0;
-  for (uint32_t i = 0; i < kGroups; ++i)
+  for (uint32_t i = 0; i < 8; ++i)
     if (part[i][lane].x != -CUDART_INF_F || part[i][lane].y != 0.0f) others += (double)(part[i][lane].y * exp2f(part[i][lane].x - most));
   const float o = (float)others, right = exp2f(zt - most), total = right + o;
   const float loss = most == zt ? log1pf(o) : logf(total) + (most - zt) * kLn2;
@@ -583,7 +629,8 @@ __global__ void __launch_bounds__(256) k_head_rows(const RowsArgs a) {
 // factor goes into the hidden states, row by row, and the target's own value, - o, to its place.
 __global__ void __launch_bounds__(256) k_head_rows_kept(const RowsArgs a) {
   pdl_enter();
-  __shared__ float2 part[kGroups][kRowsOf];
+  let_next_in();
+  __shared__ float2 part[8][kRowsOf];
   __shared__ float factors[kRowsOf];
   if (a.second && a.header->wild == 0) return;
   if (a.second && a.wild[(uint64_t)blockIdx.x * kRowsOf / kWildRows] == 0) return;
@@ -599,7 +646,7 @@ __global__ void __launch_bounds__(256) k_head_rows_kept(const RowsArgs a) {
     if (target >= 0 && target < (int64_t)a.vocab && weight != 0.0f) {
       float most = -CUDART_INF_F;
       double others = 0.0;
-      for (uint32_t i = 0; i < kGroups; ++i) most = fmaxf(most, part[i][lane].x), others += (double)part[i][lane].y;
+      for (uint32_t i = 0; i < 8; ++i) most = fmaxf(most, part[i][lane].x), others += (double)part[i][lane].y;
       const float o = (float)others;
       const float raised = a.second ? a.raised[row] : 0.0f, right = exp2f(-raised), total = right + o;
       loss = weight * (raised == 0.0f ? log1pf(o) : logf(total) + raised * kLn2);
@@ -661,6 +708,7 @@ __global__ void __launch_bounds__(256) k_head_join(const JoinArgs a) {
   if (row >= a.rows) return;
   const float alpha = late ? CUDART_NAN_F : a.alpha * (a.factor ? a.factor[row] : a.down ? *a.down : 1.0f);
   float4 s = make_float4(0, 0, 0, 0);
+#pragma unroll 8
   for (uint32_t k = 0; k < a.splits; ++k) {
     const float4 x = *reinterpret_cast<const float4*>(a.parts + k * a.split_stride + row * a.ldp + col);
     s.x += x.x, s.y += x.y, s.z += x.z, s.w += x.w;
@@ -680,14 +728,25 @@ uint32_t tiles(uint64_t n, uint32_t tile) { return (uint32_t)((n + tile - 1) / t
 bool by_pairs(uint64_t m) { return m > kTileM; }
 uint32_t tiles_m(uint64_t m) { return tiles(m, by_pairs(m) ? 2 * kTileM : kTileM); }
 
-// In how many parts a sum is cut: as many as leave the SMs the least to do one behind the other (a part more costs its reading and writing).
+// Rows that fit in one tile: the head is read once, by the SMs alike if its tiles come out even.
+uint32_t stats_tile(uint64_t m, uint32_t n) {
+  uint32_t best = kTileN;
+  if (by_pairs(m)) return best;
+  auto cost = [&](uint32_t t) { return (uint64_t)tiles(tiles(n, t), kNumSM) * t; };
+  for (uint32_t t = kTileN; t >= 128; t -= 32)
+    if (cost(t) < cost(best)) best = t;
+  return best;
+}
+// In how many parts a sum is cut: as many as leave the SMs the least to do one behind the other.  A step of 64 takes 0.3 us, a part more costs its
+// writing and reading.
 uint32_t splits_of(uint64_t m, uint64_t n, uint32_t k_blocks) {
   const uint64_t all = (uint64_t)tiles_m(m) * tiles(n, kTileN), at_once = by_pairs(m) ? kNumSM / 2 : kNumSM;
+  const double more = (double)(m * n) * 8 / 6.4e6 / 0.3 + 0.1;
   uint32_t best = 1;
   double cost = 1e30;
-  for (uint32_t s = 1; s <= 32 && s * 8 <= (k_blocks > 8 ? k_blocks : 8); ++s) {
-    const double c = (double)((all * s + at_once - 1) / at_once) / s * k_blocks + 2.0 * s;
-    if (c < cost * 0.98) cost = c, best = s;
+  for (uint32_t s = 1; s <= 64 && s * 8 <= (k_blocks > 8 ? k_blocks : 8); ++s) {
+    const double c = (double)((all * s + at_once - 1) / at_once) / s * k_blocks + more * s;
+    if (c < cost * 0.99) cost = c, best = s;
   }
   return best;
 }
@@ -697,7 +756,7 @@ struct HeadLayout {
   uint64_t ld;             // of copies
   uint32_t piece, pieces;  // words
   uint64_t ldg, ldp, stats_stride;
-  uint32_t splits, blocks_wild;
+  uint32_t splits, slots, blocks_wild;
   size_t off_hidden, off_head, off_scaled, off_stats, off_target, off_row, off_factor, off_raised, off_wild, off_g, off_parts, total;
 };
 HeadLayout head_layout(const cvlc_head& a, uint32_t pieces) {
@@ -716,7 +775,8 @@ HeadLayout head_layout(const cvlc_head& a, uint32_t pieces) {
   auto take = [&](size_t bytes) { const size_t from = at; at = align256(at + bytes); return from; };
   L.off_hidden = take(L.copy_hidden ? a.rows * L.ld * 2 : 0);
   L.off_head = take(L.copy_head ? a.vocab * L.ld * 2 : 0);
-  L.off_stats = take((size_t)tiles(a.vocab, 128) * L.stats_stride * 8);
+  L.slots = 2 * tiles(a.vocab, stats_tile(a.rows, a.vocab));
+  L.off_stats = take((size_t)L.slots * L.stats_stride * 8);
   L.off_target = take(a.rows * 4);
   if (pieces) {
     L.ldg = (uint64_t)tiles(L.piece, 32) * 32;
@@ -739,11 +799,10 @@ HeadLayout head_layout(const cvlc_head& a, uint32_t pieces) {
 }
 
 template <int EPI, bool A_ROWS, bool B_ROWS, class T, int CG>
-cudaError_t run_product_of(int id, Product& g, cudaStream_t st, bool overlap) {
+cudaError_t run_product_of(int id, const Products<EPI>& g, uint64_t items, cudaStream_t st, bool overlap) {
   static OncePerDevice once;
   const cudaError_t e = once_per_device(once, [] { return allow_shared(k_head_product<EPI, A_ROWS, B_ROWS, T, CG>, kGemmShared<CG>); });
   if (e != cudaSuccess) return e;
-  const uint64_t items = (uint64_t)g.tiles_m * g.tiles_n * g.splits;
   LaunchScope ls(id, st);
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((uint32_t)(items * CG < kNumSM ? items * CG : kNumSM));
@@ -757,25 +816,21 @@ cudaError_t run_product_of(int id, Product& g, cudaStream_t st, bool overlap) {
   attr[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = overlap ? 2 : 1;
-  (void)cudaLaunchKernelEx(&cfg, k_head_product<EPI, A_ROWS, B_ROWS, T, CG>, static_cast<Product>(g));
+  (void)cudaLaunchKernelEx(&cfg, k_head_product<EPI, A_ROWS, B_ROWS, T, CG>, Products<EPI>(g));
   return cudaGetLastError();
 }
 struct Operand {
   const void* at;
   uint64_t cols, rows, ld;
 };
-// D = A B^T, sums along the operands' columns, or along their rows (ROWS)
-template <int EPI, bool A_ROWS, bool B_ROWS, class T>
-cudaError_t run_product(int id, Product& g, const Operand& a, const Operand& b, cudaStream_t st, bool overlap) {
-  constexpr bool bf16 = std::is_same<T, __nv_bfloat16>::value;
-  const bool pairs = by_pairs(g.m);
-  g.tiles_m = tiles_m(g.m), g.tiles_n = tiles(g.n, kTileN);
+// D = A B^T, sums along the operands' columns, or along their rows
+bool make_product(Product& g, bool bf16, bool pairs, const Operand& a, bool a_rows, const Operand& b, bool b_rows) {
+  if (!g.tile_n) g.tile_n = kTileN;
+  g.tiles_m = tiles(g.m, pairs ? 2 * kTileM : kTileM), g.tiles_n = tiles(g.n, g.tile_n);
   // the operand with more tiles is read once, the other one's stay in the L2 cache
   g.m_first = g.tiles_m <= g.tiles_n;
-  if (!make_tensor_map(&g.a, a.at, bf16, a.cols, a.rows, a.ld, 64, A_ROWS ? kTileK : kTileM) ||
-      !make_tensor_map(&g.b, b.at, bf16, b.cols, b.rows, b.ld, 64, B_ROWS ? kTileK : kTileN / (pairs ? 2 : 1)))
-    return cudaErrorUnknown;
-  return pairs ? run_product_of<EPI, A_ROWS, B_ROWS, T, 2>(id, g, st, overlap) : run_product_of<EPI, A_ROWS, B_ROWS, T, 1>(id, g, st, overlap);
+  return make_tensor_map(&g.a, a.at, bf16, a.cols, a.rows, a.ld, 64, a_rows ? kTileK : kTileM) &&
+         make_tensor_map(&g.b, b.at, bf16, b.cols, b.rows, b.ld, 64, b_rows ? kTileK : g.tile_n / (pairs ? 2 : 1));
 }
 
 struct Gradients {
@@ -813,10 +868,20 @@ struct HeadRun {
     p.header = header, p.status = a.status_dev;
     return p;
   }
-  template <int EPI, bool A_ROWS, bool B_ROWS>
-  void multiply(int id, Product& p, const Operand& x, const Operand& y) {
-    if (error == cudaSuccess) error = run_product<EPI, A_ROWS, B_ROWS, T>(id, p, x, y, st, behind);
+  static constexpr bool bf16 = std::is_same<T, __nv_bfloat16>::value;
+  template <int EPI, bool A_ROWS, bool B_ROWS, int CG>
+  void run_product(int id, const Products<EPI>& p, bool fits) {
+    uint64_t items = 0;
+    for (const Product& x : p.p) items += (uint64_t)x.tiles_m * x.tiles_n * x.splits;
+    if (error == cudaSuccess) error = fits ? run_product_of<EPI, A_ROWS, B_ROWS, T, CG>(id, p, items, st, behind) : cudaErrorUnknown;
     behind = true;
+  }
+  // a product of hidden rows with words
+  template <int EPI>
+  void multiply(int id, Product p, const Operand& words) {
+    const bool pairs = by_pairs(a.rows), fits = make_product(p, bf16, pairs, hidden, false, words, false);
+    if (pairs) run_product<EPI, false, false, 2>(id, {{p}}, fits);
+    else run_product<EPI, false, false, 1>(id, {{p}}, fits);
   }
   void copy(Operand& x, size_t off, const void* targets) {
     launch(kKHeadAlign, k_head_align, tiles(x.rows, 8), 256, static_cast<const uint16_t*>(x.at), x.ld, at<uint16_t>(off), L.ld, x.rows, a.dim, targets,
@@ -825,7 +890,7 @@ struct HeadRun {
   }
   RowsArgs rows(float* loss) const {
     RowsArgs r = {};
-    r.stats = at<float2>(L.off_stats), r.stats_stride = L.stats_stride, r.slots = tiles(a.vocab, 128), r.token_bytes = a.token_bytes, r.vocab = a.vocab;
+    r.stats = at<float2>(L.off_stats), r.stats_stride = L.stats_stride, r.slots = L.slots, r.token_bytes = a.token_bytes, r.vocab = a.vocab;
     r.at_target = at<float>(L.off_target), r.targets = a.targets_dev, r.weight = a.row_weight_dev, r.loss = loss, r.header = header, r.rows = a.rows;
     r.status = a.status_dev;
     return r;
@@ -834,26 +899,33 @@ struct HeadRun {
 
   void logits_once(float* loss, bool graded) {
     Product p = product();
-    p.m = (uint32_t)a.rows, p.n = a.vocab, p.k_blocks = tiles(a.dim, kTileK), p.first = 1;
-    multiply<kStats, false, false>(kKHeadStats, p, hidden, head);
+    p.m = (uint32_t)a.rows, p.n = a.vocab, p.k_blocks = tiles(a.dim, kTileK), p.first = 1, p.tile_n = stats_tile(a.rows, a.vocab);
+    multiply<kStats>(kKHeadStats, p, head);
     RowsArgs r = rows(loss);
     r.row = graded ? at<float4>(L.off_row) : nullptr, r.half = std::is_same<T, __half>::value;
     launch(kKHeadRows, k_head_rows, row_blocks(), 256, r);
   }
-  // the part of a piece of the words in both gradients
+  // The part of a piece of the words in both gradients.  Up to 128 rows, where the hidden states' gradient has few tiles and the head's tiles are one step
+  // of the sum each, one launch makes both (16 x 1024 x 32000: 52 -> 30 us); by pairs, two do (8192 x 4096 x 131072: 13.7 ms, 15.2 in one).
   void gradients(uint32_t from, uint32_t words, const Operand& hidden_scaled, const Gradients& to, const float* down) {
     const Operand g = {base + L.off_g, words, a.rows, L.ldg}, piece = {static_cast<const T*>(head.at) + (uint64_t)from * head.ld, a.dim, words, head.ld};
+    const bool pairs = by_pairs(a.rows);
     Product p = product();
     p.m = (uint32_t)a.rows, p.n = a.dim, p.k_blocks = tiles(words, kTileK);
     p.splits = L.splits <= p.k_blocks ? L.splits : p.k_blocks;
     p.out = base + L.off_parts, p.ldo = L.ldp, p.split_stride = a.rows * L.ldp, p.add = from != 0;
-    multiply<kParts, false, true>(kKHeadParts, p, g, piece);
-    p = product();
-    p.m = words, p.n = a.dim, p.k_blocks = tiles(a.rows, kTileK);
+    Product q = product();
+    q.m = words, q.n = a.dim, q.k_blocks = tiles(a.rows, kTileK);
     T* const out = static_cast<T*>(to.d_head) + (uint64_t)from * to.d_head_stride;
-    p.out = out, p.ldo = to.d_head_stride, p.wide = reinterpret_cast<uintptr_t>(out) % 32 == 0 && to.d_head_stride % 16 == 0;
-    p.alpha_dev = down;
-    multiply<kGrad, true, true>(kKHeadGrad, p, g, hidden_scaled);
+    q.out = out, q.ldo = to.d_head_stride, q.wide = reinterpret_cast<uintptr_t>(out) % 32 == 0 && to.d_head_stride % 16 == 0;
+    q.alpha_dev = down;
+    const bool fits = make_product(p, bf16, pairs, g, false, piece, true) && make_product(q, bf16, pairs, g, true, hidden_scaled, true);
+    if (pairs) {
+      run_product<kParts, false, true, 2>(kKHeadParts, {{p}}, fits);
+      run_product<kGrad, true, true, 2>(kKHeadGrad, {{q}}, fits);
+    } else {
+      run_product<kBoth, false, true, 1>(kKHeadGrads, {{p, q}}, fits);
+    }
   }
   void join(const Gradients& to, const float* factor, const float* down) {
     JoinArgs j = {};
@@ -870,9 +942,9 @@ struct HeadRun {
     for (uint32_t turn = 0; turn < 2; ++turn) {
       Product p = product();
       p.m = (uint32_t)a.rows, p.n = a.vocab, p.k_blocks = tiles(a.dim, kTileK), p.first = turn == 0;
-      p.out = base + L.off_g, p.ldo = L.ldg;
+      p.out = base + L.off_g, p.ldo = L.ldg, p.tile_n = stats_tile(a.rows, a.vocab), p.early = turn == 0;
       if (turn) p.skip = &header->wild, p.wild = t.wild;
-      if constexpr (std::is_same<T, __nv_bfloat16>::value) multiply<kKeep, false, false>(kKHeadKeep, p, hidden, head);
+      if constexpr (bf16) multiply<kKeep>(kKHeadKeep, p, head);
       RowsArgs r = rows(loss);
       r.kept = at<__nv_bfloat16>(L.off_g), r.ldg = L.ldg, r.hidden = static_cast<const __nv_bfloat16*>(hidden.at), r.hidden_ld = hidden.ld;
       r.scaled = at<__nv_bfloat16>(L.off_scaled), r.scaled_ld = L.ld, r.factor = at<float>(L.off_factor), r.raised = at<float>(L.off_raised), r.wild = t.wild;
@@ -894,7 +966,7 @@ struct HeadRun {
       Product p = product();
       p.m = (uint32_t)a.rows, p.n = words, p.k_blocks = tiles(a.dim, kTileK), p.col0 = from, p.row = at<float4>(L.off_row);
       p.out = base + L.off_g, p.ldo = L.ldg;
-      multiply<kProbs, false, false>(kKHeadProbs, p, hidden, {static_cast<const T*>(head.at) + (uint64_t)from * head.ld, a.dim, words, head.ld});
+      multiply<kProbs>(kKHeadProbs, p, {static_cast<const T*>(head.at) + (uint64_t)from * head.ld, a.dim, words, head.ld});
       gradients(from, words, hidden, to, down);
     }
     join(to, nullptr, down);
