@@ -36,6 +36,10 @@ namespace {
 
 constexpr float kLog2E = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
+// The kernel behind may be set up while this one runs: the small ones fit beside a block of the products, and a block of theirs moves in as soon as an
+// SM is free; it waits for the rest before it reads or writes anything that this one does.
+__device__ __forceinline__ void let_next_in() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
 // ---- the products --------------------------------------------------------------------------
 // A block has a tile of 128 rows by 256 columns, a pair of blocks one of 256 by 256: one thread copies operands (a ring of stages of 64 values of the
 // sum), one issues the products, eight warps read a finished tile from the tensor memory while the next one is made in its other half.
@@ -309,7 +313,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_head_product(const __grid_const
   tensor_after();
   const Product& g0 = both.p[0];
   const uint32_t tensor = tensor_at, first = blockIdx.x / CG, apart = gridDim.x / CG;
-  if (!g0.early || warp >= 4) pdl_enter();
+  if (!g0.early || warp >= 4) {
+    pdl_enter();
+    let_next_in();
+  }
   const uint32_t items0 = g0.skip && *g0.skip == 0 ? 0 : g0.tiles_m * g0.tiles_n * g0.splits;
   const uint32_t items = items0 + (EPI == kBoth ? both.p[Products<EPI>::count - 1].tiles_m * both.p[Products<EPI>::count - 1].tiles_n : 0);
   bool ok = true;
@@ -428,6 +435,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_head_product(const __grid_const
 // One block, fp16 only: the power of two by which G is held.  fp16 holds 2^-24 to 2^16; G, at most the largest weight in size, is held at most 2^15.
 __global__ void __launch_bounds__(1024) k_head_begin(Header* h, const float* weight, const void* targets, uint32_t token_bytes, uint64_t rows, uint32_t vocab) {
   pdl_enter();
+  let_next_in();
   __shared__ uint32_t most;
   if (threadIdx.x == 0) most = 0;
   __syncthreads();
@@ -453,6 +461,7 @@ __global__ void __launch_bounds__(1024) k_head_begin(Header* h, const float* wei
 __global__ void __launch_bounds__(256) k_head_align(const uint16_t* from, uint64_t from_stride, uint16_t* to, uint64_t to_stride, uint64_t rows, uint32_t dim,
                                                     const void* targets, uint32_t token_bytes, uint32_t vocab, const float* weight) {
   pdl_enter();
+  let_next_in();
   const uint64_t row = (uint64_t)blockIdx.x * 8 + threadIdx.x / 32;
   const uint32_t lane = threadIdx.x & 31;
   if (row >= rows) return;
@@ -489,10 +498,6 @@ __global__ void __launch_bounds__(256) k_head_align(const uint16_t* from, uint64
   }
 }
 
-// The kernel behind may be set up while this one runs: it has a block on every SM, whose first steps (barriers, tensor memory, and the operands' first tiles
-// where they do not come from here) need nothing of this one's; it waits for the rest.
-__device__ __forceinline__ void let_next_in() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
-
 // z of every row's target, in log2; +inf where the row counts for nothing.  A warp a row.
 struct TargetArgs {
   const void *hidden, *head, *targets;
@@ -520,6 +525,7 @@ __global__ void __launch_bounds__(256) k_head_target(const TargetArgs a) {
   const __nv_bfloat16* const h = static_cast<const __nv_bfloat16*>(a.hidden) + row * a.hidden_ld;
   const __nv_bfloat16* const w = static_cast<const __nv_bfloat16*>(a.head) + (uint64_t)t * a.head_ld;
   float sum = 0.0f;
+#pragma unroll 4
   for (uint32_t i = lane * 8; i < a.dim; i += 256) {
     if (i + 8 <= a.dim) {
       float x[8], y[8];
@@ -596,6 +602,7 @@ __device__ __forceinline__ void join_parts(const RowsArgs& a, uint64_t row, uint
 // ln(1 + o) keep their accuracy.
 __global__ void __launch_bounds__(256) k_head_rows(const RowsArgs a) {
   pdl_enter();
+  if (a.row) let_next_in();  // else the last of the call
   __shared__ float2 part[8][kRowsOf];
   const uint32_t group = threadIdx.x / kRowsOf, lane = threadIdx.x % kRowsOf;
   const uint64_t row = (uint64_t)blockIdx.x * kRowsOf + lane;
@@ -698,26 +705,44 @@ struct JoinArgs {
   const Header* header;
   void* out;
 };
-template <class T>
+// The parts of the hidden states' gradient added up in their order, four columns a thread; with many parts (few rows) eight threads share them.
+template <class T, int SHARE>
 __global__ void __launch_bounds__(256) k_head_join(const JoinArgs a) {
   pdl_enter();
+  __shared__ float4 share[SHARE > 1 ? 256 : 1];
   const bool late = any_late(a.header);
-  const uint32_t per = (a.dim + 3) / 4;
-  const uint64_t i = (uint64_t)blockIdx.x * blockDim.x + threadIdx.x, row = i / per;
+  const uint32_t per = (a.dim + 3) / 4, of = 256 / SHARE, mine = threadIdx.x / of;
+  const uint64_t i = (uint64_t)blockIdx.x * of + threadIdx.x % of, row = i / per;
   const uint32_t col = (uint32_t)(i - row * per) * 4;
+  float4 s = make_float4(0, 0, 0, 0);
+  if (row < a.rows) {
+    const float* const from = a.parts + row * a.ldp + col;
+#pragma unroll 8
+    for (uint32_t k = mine; k < a.splits; k += SHARE) {
+      const float4 x = *reinterpret_cast<const float4*>(from + k * a.split_stride);
+      s.x += x.x, s.y += x.y, s.z += x.z, s.w += x.w;
+    }
+  }
+  if (SHARE > 1) {
+    share[threadIdx.x] = s;
+    __syncthreads();
+    if (mine) return;
+    for (uint32_t k = 1; k < SHARE; ++k) {
+      const float4 x = share[k * of + threadIdx.x];
+      s.x += x.x, s.y += x.y, s.z += x.z, s.w += x.w;
+    }
+  }
   if (row >= a.rows) return;
   const float alpha = late ? CUDART_NAN_F : a.alpha * (a.factor ? a.factor[row] : a.down ? *a.down : 1.0f);
-  float4 s = make_float4(0, 0, 0, 0);
-#pragma unroll 8
-  for (uint32_t k = 0; k < a.splits; ++k) {
-    const float4 x = *reinterpret_cast<const float4*>(a.parts + k * a.split_stride + row * a.ldp + col);
-    s.x += x.x, s.y += x.y, s.z += x.z, s.w += x.w;
-  }
   T* const out = static_cast<T*>(a.out) + row * a.ldo + col;
   const float v[4] = {s.x * alpha, s.y * alpha, s.z * alpha, s.w * alpha};
+  if (col + 4 <= a.dim && (reinterpret_cast<uintptr_t>(out) & 7) == 0) {
+    *reinterpret_cast<uint2*>(out) = make_uint2(pack2<T>(v[0], v[1]), pack2<T>(v[2], v[3]));
+  } else {
 #pragma unroll
-  for (int k = 0; k < 4; ++k)
-    if (col + k < a.dim) out[k] = from_float<T>(v[k]);
+    for (int k = 0; k < 4; ++k)
+      if (col + k < a.dim) out[k] = from_float<T>(v[k]);
+  }
 }
 
 // ---- layout and launching --------------------------------------------------------------------
@@ -931,7 +956,9 @@ struct HeadRun {
     JoinArgs j = {};
     j.parts = at<float>(L.off_parts), j.split_stride = a.rows * L.ldp, j.ldp = L.ldp, j.ldo = to.d_hidden_stride;
     j.splits = L.splits, j.dim = a.dim, j.rows = a.rows, j.alpha = a.scale, j.factor = factor, j.down = down, j.header = header, j.out = to.d_hidden;
-    launch(kKHeadJoin, k_head_join<T>, (uint32_t)((a.rows * ((a.dim + 3) / 4) + 255) / 256), 256, j);
+    const uint64_t quads = a.rows * ((a.dim + 3) / 4);
+    if (L.splits >= 8) launch(kKHeadJoin, k_head_join<T, 8>, (uint32_t)((quads + 31) / 32), 256, j);
+    else launch(kKHeadJoin, k_head_join<T, 1>, (uint32_t)((quads + 255) / 256), 256, j);
   }
   void run_kept(float* loss, const Gradients& to) {
     TargetArgs t = {};
