@@ -49,9 +49,10 @@ __device__ __forceinline__ void mbar_arrive_leader(uint64_t* b) {
 }
 __device__ __forceinline__ bool mbar_try(uint64_t* b, uint32_t parity) {
   uint32_t done;
-  asm volatile("{.reg .pred p;\n mbarrier.try_wait.parity.shared.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;}"
+  // suspended for up to 10 ms: threads that ask again and again take from those that work (a product of 4096 x 2048 x 50048: 604 -> 559 us)
+  asm volatile("{.reg .pred p;\n mbarrier.try_wait.parity.shared.b64 p, [%1], %2, %3;\n selp.u32 %0, 1, 0, p;}"
                : "=r"(done)
-               : "r"(smem_at(b)), "r"(parity)
+               : "r"(smem_at(b)), "r"(parity), "r"(10000000u)
                : "memory");
   return done != 0;
 }
@@ -66,9 +67,7 @@ __device__ __forceinline__ bool mbar_wait(uint64_t* b, uint32_t parity, uint32_t
   if (mbar_try(b, parity)) return true;
   const uint64_t began = now_ns();
   for (;;) {
-#pragma unroll 1
-    for (int i = 0; i < 64; ++i)
-      if (mbar_try(b, parity)) return true;
+    if (mbar_try(b, parity)) return true;
     if (*static_cast<volatile uint32_t*>(late)) return false;
     if (now_ns() - began > most) {
       *static_cast<volatile uint32_t*>(late) = 1;
