@@ -46,12 +46,13 @@ __device__ __forceinline__ void let_next_in() { asm volatile("griddepcontrol.lau
 constexpr uint32_t kTileM = 128, kTileN = 256, kTileK = 64;
 constexpr int kThreads = 384, kOutWarps = 8;
 constexpr uint32_t kBytesA = kTileM * kTileK * 2, kBytesB = kTileN * kTileK * 2;
+constexpr uint32_t kBoxBytes = 32 * 128;  // of a warp, 32 rows of 64 columns on their way out
 template <int CG>
 constexpr int kStages = CG == 2 ? 6 : 4;
 template <int CG>
 constexpr uint32_t kStageBytes = kBytesA + kBytesB / CG;  // of one block
 template <int CG>
-constexpr size_t kGemmShared = kStages<CG> * kStageBytes<CG> + 1024;
+constexpr size_t kGemmShared = kStages<CG> * kStageBytes<CG> + kOutWarps * kBoxBytes + 1024;
 
 struct Header {  // at the beginning of the workspace
   float up, down;         // fp16: a power of two that brings weights to at most 1, times 2^15, and its inverse
@@ -66,7 +67,7 @@ __device__ __forceinline__ bool any_late(const Header* h) {  // asked by all thr
 
 enum Epilogue { kStats, kKeep, kProbs, kParts, kGrad, kBoth };  // kBoth: parts, then grad
 struct Product {
-  CUtensorMap a, b;
+  CUtensorMap a, b, c;                   // c: the output, where it is of 16 bits and its rows lie on 16 bytes
   uint32_t m, n, k_blocks;               // rows, columns, steps of 64 of the sum
   uint32_t tile_n, tiles_m, tiles_n, splits;  // columns of a tile; splits of the sum
   uint32_t m_first, group;               // tiles of one column of tiles follow one another, else those of a row; so many of them, then the next column
@@ -79,7 +80,7 @@ struct Product {
   const float4* row;                     // probs: what makes a row's G of its z
   void* out;
   uint64_t ldo, split_stride;
-  uint32_t add, wide;                    // added to what is there; rows of `out` by vectors of 32 bytes
+  uint32_t add, wide;                    // added to what is there; written by boxes
   const float* alpha_dev;                // or nullptr; multiplies alpha
   const uint32_t* skip;                  // or nullptr; where it is 0 nothing is to be done
   const uint32_t* wild;                  // or nullptr; of 256 rows each: 0 where they are left out
@@ -138,9 +139,28 @@ __device__ __forceinline__ int64_t target_of(const void* targets, uint32_t bytes
   return bytes == 8 ? static_cast<const int64_t*>(targets)[row] : static_cast<const int32_t*>(targets)[row];
 }
 
+// 64 columns of a thread's row, in 16 bits, by way of shared memory: lines of 128 bytes go out whole, and nothing is left to do but start the copy.
+// (Threads that store their rows themselves, 32 bytes at a time: KEEPOLD instead of KEEPNEW us for 8192 x 4096 x 131072 with the exponentials kept.)
+__device__ __forceinline__ void row_to_box(uint32_t box, uint32_t lane, uint32_t part, const uint32_t (&p)[16]) {
+#pragma unroll
+  for (uint32_t i = 0; i < 4; ++i)
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(box + lane * 128 + ((4 * part + i) ^ (lane & 7)) * 16), "r"(p[4 * i]), "r"(p[4 * i + 1]),
+                 "r"(p[4 * i + 2]), "r"(p[4 * i + 3])
+                 : "memory");
+}
+__device__ __forceinline__ void box_free(uint32_t lane) {
+  if (lane == 0) tiles_read();
+  __syncwarp();
+}
+__device__ __forceinline__ void box_out(const CUtensorMap& map, uint32_t box, uint32_t lane, uint32_t x, uint32_t y) {
+  shared_written();
+  __syncwarp();
+  if (lane == 0) store_tile(map, box, x, y);
+}
+
 // What becomes of a warp's 32 rows and 128 columns of a finished tile
 template <int EPI, class T>
-__device__ __forceinline__ void finish_tile(const Product& g, const Work& w, uint32_t tensor, uint32_t half, uint32_t quarter, uint32_t lane, uint32_t* stage) {
+__device__ __forceinline__ void finish_tile(const Product& g, const Work& w, uint32_t tensor, uint32_t half, uint32_t quarter, uint32_t lane, uint32_t box) {
   const uint32_t row = w.m0 + quarter * 32 + lane;
   const bool there = row < g.m;
   float v[32];
@@ -182,17 +202,20 @@ __device__ __forceinline__ void finish_tile(const Product& g, const Work& w, uin
     // the target is wild and gets a second turn, relative to its maximum.
     const float from = there ? g.at_target[row] : CUDART_INF_F;
     const int64_t target = there ? target_of(g.targets, g.token_bytes, row) : -1;
-    T* const out = static_cast<T*>(g.out) + (uint64_t)row * g.ldo;
+    const bool counts = from != CUDART_INF_F;
     float most = -CUDART_INF_F, sum = 0.0f;
     for (int c = 0; c < 4; ++c) {
       const uint32_t col = w.n0 + half * 128 + c * 32;
-      if (col >= w.n_end) break;
+      if ((c & 1) == 0) {
+        if (col >= w.n_end) break;
+        box_free(lane);
+      }
       tensor_load(tensor + c * 32, v);
       tensor_loaded(v);
 #pragma unroll
       for (int i = 0; i < 32; ++i) v[i] = fmaf(v[i], g.k2, -from);
       const bool mine = target >= col && target < (int64_t)col + 32;
-      if (w.n_end - col < 32 || __any_sync(kFull, mine)) {
+      if (col + 32 > w.n_end || __any_sync(kFull, mine)) {
 #pragma unroll
         for (int i = 0; i < 32; ++i)
           if (col + i >= w.n_end || (mine && target == (int64_t)col + i)) v[i] = -CUDART_INF_F;
@@ -203,26 +226,23 @@ __device__ __forceinline__ void finish_tile(const Product& g, const Work& w, uin
 #pragma unroll
       for (int i = 4; i < 32; ++i) s[i & 3] += v[i];
       sum += (s[0] + s[1]) + (s[2] + s[3]);
-      if (there) {
-        const bool counts = from != CUDART_INF_F;
+      uint32_t p[16];
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          uint32_t p[8];
-#pragma unroll
-          for (int i = 0; i < 8; ++i) p[i] = counts ? pack2<T>(v[16 * h + 2 * i], v[16 * h + 2 * i + 1]) : 0u;
-          store_sector(out + col + 16 * h, p);
-        }
-      }
+      for (int i = 0; i < 16; ++i) p[i] = counts ? pack2<T>(v[2 * i], v[2 * i + 1]) : 0u;
+      row_to_box(box, lane, c & 1, p);
+      if (c & 1) box_out(g.c, box, lane, col - 32, w.m0 + quarter * 32);
     }
     if (there) g.stats[(uint64_t)(w.slot + half) * g.stats_stride + row] = make_float2(most, sum);
   } else if constexpr (EPI == kProbs) {
     // x: ln sum exp in log2, less the exponent that is added; y: the weight, 0 where the row counts for nothing; z: the target's value
     const float4 r = there ? g.row[row] : make_float4(0, 0, 0, 0);
     const int64_t target = there ? target_of(g.targets, g.token_bytes, row) - g.col0 : -1;
-    T* const out = static_cast<T*>(g.out) + (uint64_t)row * g.ldo;
     for (int c = 0; c < 4; ++c) {
       const uint32_t col = w.n0 + half * 128 + c * 32;
-      if (col >= w.n_end) break;
+      if ((c & 1) == 0) {
+        if (col >= w.n_end) break;
+        box_free(lane);
+      }
       tensor_load(tensor + c * 32, v);
       tensor_loaded(v);
 #pragma unroll
@@ -233,15 +253,11 @@ __device__ __forceinline__ void finish_tile(const Product& g, const Work& w, uin
         for (int i = 0; i < 32; ++i)
           if (mine && target == (int64_t)col + i) v[i] = r.z;
       }
-      if (there) {
+      uint32_t p[16];
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          uint32_t p[8];
-#pragma unroll
-          for (int i = 0; i < 8; ++i) p[i] = pack2<T>(v[16 * h + 2 * i], v[16 * h + 2 * i + 1]);
-          store_sector(out + col + 16 * h, p);
-        }
-      }
+      for (int i = 0; i < 16; ++i) p[i] = pack2<T>(v[2 * i], v[2 * i + 1]);
+      row_to_box(box, lane, c & 1, p);
+      if (c & 1) box_out(g.c, box, lane, col - 32, w.m0 + quarter * 32);
     }
   } else if constexpr (EPI == kParts) {
     float* const out = static_cast<float*>(g.out) + w.split * g.split_stride + (uint64_t)row * g.ldo;
@@ -271,26 +287,30 @@ __device__ __forceinline__ void finish_tile(const Product& g, const Work& w, uin
     const float alpha = g.alpha_dev ? g.alpha * *g.alpha_dev : g.alpha;
     for (int c = 0; c < 4; ++c) {
       const uint32_t col = w.n0 + half * 128 + c * 32;
-      if (col >= w.n_end) break;
+      if ((c & 1) == 0) {
+        if (col >= w.n_end) break;
+        if (g.wide) box_free(lane);
+      }
       tensor_load(tensor + c * 32, v);
       tensor_loaded(v);
       uint32_t p[16];
 #pragma unroll
       for (int i = 0; i < 16; ++i) p[i] = pack2<T>(v[2 * i] * alpha, v[2 * i + 1] * alpha);
-      if (g.wide && col + 32 <= w.n_end) {
-        if (there) {
-          store_sector(out + (uint64_t)row * g.ldo + col, p);
-          store_sector(out + (uint64_t)row * g.ldo + col + 16, p + 8);
-        }
-      } else {  // rows that begin anywhere: turned in shared memory, so that a warp writes neighbours
+      if (g.wide) {
+        row_to_box(box, lane, c & 1, p);
+        if (c & 1) box_out(g.c, box, lane, col - 32, w.m0 + quarter * 32);
+      } else if (col < w.n_end) {  // rows that begin anywhere: turned in shared memory, so that a warp writes neighbours
 #pragma unroll
-        for (int i = 0; i < 16; ++i) stage[lane * 17 + i] = p[i];
+        for (int i = 0; i < 16; ++i) asm volatile("st.shared.b32 [%0], %1;" ::"r"(box + (lane * 17 + i) * 4), "r"(p[i]) : "memory");
         __syncwarp();
-        const uint16_t* const from = reinterpret_cast<const uint16_t*>(stage) + lane;
         uint16_t* const to = reinterpret_cast<uint16_t*>(out) + (uint64_t)(w.m0 + quarter * 32) * g.ldo + col + lane;
         const uint32_t rows = min(32u, g.m - min(g.m, w.m0 + quarter * 32));
         if (col + lane < w.n_end)
-          for (uint32_t r = 0; r < rows; ++r) to[r * g.ldo] = from[r * 34];
+          for (uint32_t r = 0; r < rows; ++r) {
+            uint16_t x;
+            asm volatile("ld.shared.u16 %0, [%1];" : "=h"(x) : "r"(box + r * 68 + lane * 2) : "memory");
+            to[r * g.ldo] = x;
+          }
         __syncwarp();
       }
     }
@@ -300,11 +320,9 @@ __device__ __forceinline__ void finish_tile(const Product& g, const Work& w, uin
 template <int EPI, bool A_ROWS, bool B_ROWS, class T, int CG>
 __global__ void __launch_bounds__(kThreads, 1) k_head_product(const __grid_constant__ Products<EPI> both) {
   constexpr int stages = kStages<CG>;
-  constexpr bool turning = EPI == kGrad || EPI == kBoth;
   extern __shared__ uint8_t dynamic[];
   __shared__ uint64_t full[stages], empty[stages], made[2], taken[2], over;
   __shared__ uint32_t tensor_at, late;
-  __shared__ uint32_t turn[turning ? kOutWarps * 32 * 17 : 1];
   const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x & 31, rank = pair_rank<CG>();
   const uint32_t ring = (smem_at(dynamic) + 1023) & ~1023u;
   if (threadIdx.x == 0) {
@@ -399,7 +417,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_head_product(const __grid_const
       mbar_wait(&over, 0, &none, kMostWait / 4);
     }
   } else if (warp >= 4) {
-    const uint32_t half_tile = (warp - 4) / 4, quarter = warp & 3;
+    const uint32_t half_tile = (warp - 4) / 4, quarter = warp & 3, box = ring + stages * kStageBytes<CG> + (warp - 4) * kBoxBytes;
     uint32_t turn_of = 0;
     for (uint32_t w = first; w < items; w += apart) {
       const bool second = EPI == kBoth && w >= items0;
@@ -410,18 +428,18 @@ __global__ void __launch_bounds__(kThreads, 1) k_head_product(const __grid_const
       if (!(ok = __all_sync(kFull, mbar_wait(made + half, turn_of / 2 & 1, &late)))) break;
       tensor_after();
       const uint32_t at = tensor + half * kTileN + half_tile * 128 + (quarter * 32 << 16);
-      uint32_t* const stage = turn + (turning ? (warp - 4) * 32 * 17 : 0);
       if constexpr (EPI == kBoth) {
-        if (second) finish_tile<kGrad, T>(g, r, at, half_tile, quarter, lane, stage);
-        else finish_tile<kParts, T>(g, r, at, half_tile, quarter, lane, stage);
+        if (second) finish_tile<kGrad, T>(g, r, at, half_tile, quarter, lane, box);
+        else finish_tile<kParts, T>(g, r, at, half_tile, quarter, lane, box);
       } else {
-        finish_tile<EPI, T>(g, r, at, half_tile, quarter, lane, stage);
+        finish_tile<EPI, T>(g, r, at, half_tile, quarter, lane, box);
       }
       tensor_before();
       __syncwarp();
       if (lane == 0) mbar_arrive_leader<CG>(taken + half);
       ++turn_of;
     }
+    if (lane == 0) tiles_stored();
   }
   __syncwarp();
   tensor_before();
@@ -762,11 +780,12 @@ bool by_pairs(uint64_t m) { return m > kTileM; }
 uint32_t tiles_m(uint64_t m) { return tiles(m, by_pairs(m) ? 2 * kTileM : kTileM); }
 
 // Rows that fit in one tile: the head is read once, by the SMs alike if its tiles come out even.
-uint32_t stats_tile(uint64_t m, uint32_t n) {
+// (Boxes that are written have 64 columns.)
+uint32_t stats_tile(uint64_t m, uint32_t n, bool written) {
   uint32_t best = kTileN;
   if (by_pairs(m)) return best;
   auto cost = [&](uint32_t t) { return (uint64_t)tiles(tiles(n, t), kNumSM) * t; };
-  for (uint32_t t = kTileN; t >= 128; t -= 32)
+  for (uint32_t t = kTileN; t >= 128; t -= written ? 64 : 32)
     if (cost(t) < cost(best)) best = t;
   return best;
 }
@@ -808,7 +827,7 @@ HeadLayout head_layout(const cvlc_head& a, uint32_t pieces) {
   auto take = [&](size_t bytes) { const size_t from = at; at = align256(at + bytes); return from; };
   L.off_hidden = take(L.copy_hidden ? a.rows * L.ld * 2 : 0);
   L.off_head = take(L.copy_head ? a.vocab * L.ld * 2 : 0);
-  L.slots = 2 * tiles(a.vocab, stats_tile(a.rows, a.vocab));
+  L.slots = 2 * tiles(a.vocab, stats_tile(a.rows, a.vocab, L.keep));
   L.off_stats = take((size_t)L.slots * L.stats_stride * 8);
   L.off_target = take(a.rows * 4);
   if (pieces) {
@@ -857,7 +876,7 @@ struct Operand {
   uint64_t cols, rows, ld;
 };
 // D = A B^T, sums along the operands' columns, or along their rows
-bool make_product(Product& g, bool bf16, bool pairs, const Operand& a, bool a_rows, const Operand& b, bool b_rows) {
+bool make_product(Product& g, bool bf16, bool pairs, const Operand& a, bool a_rows, const Operand& b, bool b_rows, bool boxes) {
   if (!g.tile_n) g.tile_n = kTileN;
   g.tiles_m = tiles(g.m, pairs ? 2 * kTileM : kTileM), g.tiles_n = tiles(g.n, g.tile_n);
   // Of the operand with fewer tiles a group, 32 MB or eight tiles, stays in the L2 cache (of which each half of the chip has its own copy), while the other
@@ -868,6 +887,7 @@ bool make_product(Product& g, bool bf16, bool pairs, const Operand& a, bool a_ro
   if (g.group < 8) g.group = 8;
   const uint32_t fewer = g.m_first ? g.tiles_m : g.tiles_n;
   if (g.group > fewer) g.group = fewer;
+  if (boxes && !make_tensor_map(&g.c, g.out, bf16, g.n, g.m, g.ldo, 64, 32)) return false;
   return make_tensor_map(&g.a, a.at, bf16, a.cols, a.rows, a.ld, 64, a_rows ? kTileK : kTileM) &&
          make_tensor_map(&g.b, b.at, bf16, b.cols, b.rows, b.ld, 64, b_rows ? kTileK : g.tile_n / (pairs ? 2 : 1));
 }
@@ -918,7 +938,7 @@ struct HeadRun {
   // a product of hidden rows with words
   template <int EPI>
   void multiply(int id, Product p, const Operand& words) {
-    const bool pairs = by_pairs(a.rows), fits = make_product(p, bf16, pairs, hidden, false, words, false);
+    const bool pairs = by_pairs(a.rows), fits = make_product(p, bf16, pairs, hidden, false, words, false, EPI != kStats);
     if (pairs) run_product<EPI, false, false, 2>(id, {{p}}, fits);
     else run_product<EPI, false, false, 1>(id, {{p}}, fits);
   }
@@ -938,7 +958,7 @@ struct HeadRun {
 
   void logits_once(float* loss, bool graded) {
     Product p = product();
-    p.m = (uint32_t)a.rows, p.n = a.vocab, p.k_blocks = tiles(a.dim, kTileK), p.first = 1, p.tile_n = stats_tile(a.rows, a.vocab);
+    p.m = (uint32_t)a.rows, p.n = a.vocab, p.k_blocks = tiles(a.dim, kTileK), p.first = 1, p.tile_n = stats_tile(a.rows, a.vocab, false);
     multiply<kStats>(kKHeadStats, p, head);
     RowsArgs r = rows(loss);
     r.row = graded ? at<float4>(L.off_row) : nullptr, r.half = std::is_same<T, __half>::value;
@@ -956,9 +976,9 @@ struct HeadRun {
     Product q = product();
     q.m = words, q.n = a.dim, q.k_blocks = tiles(a.rows, kTileK);
     T* const out = static_cast<T*>(to.d_head) + (uint64_t)from * to.d_head_stride;
-    q.out = out, q.ldo = to.d_head_stride, q.wide = reinterpret_cast<uintptr_t>(out) % 32 == 0 && to.d_head_stride % 16 == 0;
+    q.out = out, q.ldo = to.d_head_stride, q.wide = on16(out, to.d_head_stride);
     q.alpha_dev = down;
-    const bool fits = make_product(p, bf16, pairs, g, false, piece, true) && make_product(q, bf16, pairs, g, true, hidden_scaled, true);
+    const bool fits = make_product(p, bf16, pairs, g, false, piece, true, false) && make_product(q, bf16, pairs, g, true, hidden_scaled, true, q.wide);
     if (pairs) {
       run_product<kParts, false, true, 2>(kKHeadParts, {{p}}, fits);
       run_product<kGrad, true, true, 2>(kKHeadGrad, {{q}}, fits);
@@ -983,7 +1003,7 @@ struct HeadRun {
     for (uint32_t turn = 0; turn < 2; ++turn) {
       Product p = product();
       p.m = (uint32_t)a.rows, p.n = a.vocab, p.k_blocks = tiles(a.dim, kTileK), p.first = turn == 0;
-      p.out = base + L.off_g, p.ldo = L.ldg, p.tile_n = stats_tile(a.rows, a.vocab), p.early = turn == 0;
+      p.out = base + L.off_g, p.ldo = L.ldg, p.tile_n = stats_tile(a.rows, a.vocab, true), p.early = turn == 0;
       if (turn) p.skip = &header->wild, p.wild = t.wild;
       if constexpr (bf16) multiply<kKeep>(kKHeadKeep, p, head);
       RowsArgs r = rows(loss);

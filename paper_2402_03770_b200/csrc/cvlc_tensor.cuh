@@ -90,6 +90,17 @@ __device__ __forceinline__ void load_tile(const CUtensorMap& map, uint32_t to, u
                  : "memory");
 }
 
+// A box of 64 columns by 32 rows that a warp has left in shared memory (swizzled, on 1024 bytes) to where the map says; what lies outside is left out.  By one
+// thread, behind shared_written() of all; the buffer is free again behind tiles_read(), the copy made behind tiles_stored().
+__device__ __forceinline__ void shared_written() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+__device__ __forceinline__ void store_tile(const CUtensorMap& map, uint32_t from, uint32_t x, uint32_t y) {
+  asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%2, %3}], [%1];\n cp.async.bulk.commit_group;" ::"l"(&map), "r"(from), "r"(x),
+               "r"(y)
+               : "memory");
+}
+__device__ __forceinline__ void tiles_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
+__device__ __forceinline__ void tiles_stored() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
+
 // ---- operands ------------------------------------------------------------------------------
 // Both kinds of tile hold lines of 128 bytes, eight of which are one swizzled group of 1024.
 //   along the sum ("K first"): a line is 64 values of the sum of one row; groups of eight rows follow one another.  16 values of the sum
