@@ -65,7 +65,7 @@ __device__ __forceinline__ bool any_late(const Header* h) {  // asked by all thr
   return __syncthreads_or((int)x) != 0;
 }
 
-enum Epilogue { kStats, kKeep, kProbs, kParts, kGrad, kBoth };  // kBoth: parts, then grad
+enum Epilogue { kStats, kKeep, kKeepOwn, kProbs, kParts, kGrad, kBoth };  // kBoth: parts, then grad
 struct Product {
   CUtensorMap a, b, c;                   // c: the output, where it is of 16 bits and its rows lie on 16 bytes
   uint32_t m, n, k_blocks;               // rows, columns, steps of 64 of the sum
@@ -140,7 +140,7 @@ __device__ __forceinline__ int64_t target_of(const void* targets, uint32_t bytes
 }
 
 // 64 columns of a thread's row, in 16 bits, by way of shared memory: lines of 128 bytes go out whole, and nothing is left to do but start the copy.
-// (Threads that store their rows themselves, 32 bytes at a time: KEEPOLD instead of KEEPNEW us for 8192 x 4096 x 131072 with the exponentials kept.)
+// (Threads that store their rows themselves, 32 bytes at a time, take as long; they leave four times as many requests.)
 __device__ __forceinline__ void row_to_box(uint32_t box, uint32_t lane, uint32_t part, const uint32_t (&p)[16]) {
 #pragma unroll
   for (uint32_t i = 0; i < 4; ++i)
@@ -229,6 +229,56 @@ __device__ __forceinline__ void finish_tile(const Product& g, const Work& w, uin
       uint32_t p[16];
 #pragma unroll
       for (int i = 0; i < 16; ++i) p[i] = counts ? pack2<T>(v[2 * i], v[2 * i + 1]) : 0u;
+      row_to_box(box, lane, c & 1, p);
+      if (c & 1) box_out(g.c, box, lane, col - 32, w.m0 + quarter * 32);
+    }
+    if (there) g.stats[(uint64_t)(w.slot + half) * g.stats_stride + row] = make_float2(most, sum);
+  } else if constexpr (EPI == kKeepOwn) {
+    // fp16 has no range to spare: each row of 128 columns relative to its own maximum, which takes a look of its own
+    const int64_t target = there ? target_of(g.targets, g.token_bytes, row) : -1;
+    float most = -CUDART_INF_F, sum = 0.0f;
+    for (int c = 0; c < 4; ++c) {
+      const uint32_t col = w.n0 + half * 128 + c * 32;
+      if (col >= w.n_end) break;
+      tensor_load(tensor + c * 32, v);
+      tensor_loaded(v);
+#pragma unroll
+      for (int i = 0; i < 32; ++i) v[i] = v[i] * g.k2;
+      const bool mine = target >= col && target < (int64_t)col + 32;
+      if (col + 32 > w.n_end || __any_sync(kFull, mine)) {
+#pragma unroll
+        for (int i = 0; i < 32; ++i) {
+          if (mine && target == (int64_t)col + i) g.at_target[row] = v[i], v[i] = -CUDART_INF_F;
+          if (col + i >= w.n_end) v[i] = -CUDART_INF_F;
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < 32; ++i) most = fmaxf(most, v[i]);
+    }
+    const float from = most == -CUDART_INF_F ? 0.0f : most;
+    for (int c = 0; c < 4; ++c) {
+      const uint32_t col = w.n0 + half * 128 + c * 32;
+      if ((c & 1) == 0) {
+        if (col >= w.n_end) break;
+        box_free(lane);
+      }
+      tensor_load(tensor + c * 32, v);
+      tensor_loaded(v);
+#pragma unroll
+      for (int i = 0; i < 32; ++i) v[i] = fmaf(v[i], g.k2, -from);
+      const bool mine = target >= col && target < (int64_t)col + 32;
+      if (col + 32 > w.n_end || __any_sync(kFull, mine)) {
+#pragma unroll
+        for (int i = 0; i < 32; ++i)
+          if (col + i >= w.n_end || (mine && target == (int64_t)col + i)) v[i] = -CUDART_INF_F;
+      }
+      float s[4] = {};
+#pragma unroll
+      for (int i = 0; i < 32; ++i) v[i] = exp2_fast(v[i]), s[i & 3] += v[i];
+      sum += (s[0] + s[1]) + (s[2] + s[3]);
+      uint32_t p[16];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) p[i] = pack2<T>(v[2 * i], v[2 * i + 1]);
       row_to_box(box, lane, c & 1, p);
       if (c & 1) box_out(g.c, box, lane, col - 32, w.m0 + quarter * 32);
     }
@@ -721,6 +771,41 @@ __global__ void __launch_bounds__(256) k_head_rows_kept(const RowsArgs a) {
   }
 }
 
+// Exponentials that are kept relative to the maximum of their 128 columns become G, in their place: times exp(maximum - ln sum exp) and the weight.
+// A warp a row, two times 128 columns at a time.
+struct RescaleArgs {
+  void* kept;
+  uint64_t ldg, rows, stats_stride;
+  const float2* stats;
+  const float4* row;
+  const void* targets;
+  uint32_t vocab, tile_n, token_bytes;
+};
+__global__ void __launch_bounds__(256) k_head_rescale(const RescaleArgs a) {
+  pdl_enter();
+  let_next_in();
+  const uint64_t row = (uint64_t)blockIdx.x * 8 + threadIdx.x / 32;
+  const uint32_t lane = threadIdx.x & 31;
+  if (row >= a.rows) return;
+  const float4 r = a.row[row];
+  __half* const at = static_cast<__half*>(a.kept) + row * a.ldg;
+  const int64_t target = r.y == 0.0f ? -1 : target_of(a.targets, a.token_bytes, row);
+#pragma unroll 4
+  for (uint32_t col = (blockIdx.y * 32 + lane) * 8; col < a.vocab; col += gridDim.y * 256) {
+    const uint32_t tile = col / a.tile_n, slot = 2 * tile + (col - tile * a.tile_n) / 128;
+    const uint4 raw = __ldcs(reinterpret_cast<const uint4*>(at + col));
+    const float f = exp2f(a.stats[slot * a.stats_stride + row].x - r.x) * r.y;
+    float v[8];
+    widen<__half>(raw, v);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      v[i] = r.y == 0.0f ? 0.0f : v[i] * f;
+      if (target == (int64_t)col + i) v[i] = r.z;
+    }
+    *reinterpret_cast<uint4*>(at + col) = narrow<__half>(v);
+  }
+}
+
 struct JoinArgs {
   const float* parts;
   uint64_t split_stride, ldp, ldo;
@@ -804,7 +889,7 @@ uint32_t splits_of(uint64_t m, uint64_t n, uint32_t k_blocks) {
 }
 
 struct HeadLayout {
-  bool keep, copy_hidden, copy_head;
+  bool keep, keep_own, copy_hidden, copy_head;
   uint64_t ld;             // of copies
   uint32_t piece, pieces;  // words
   uint64_t ldg, ldp, stats_stride;
@@ -818,8 +903,9 @@ HeadLayout head_layout(const cvlc_head& a, uint32_t pieces) {
     L.pieces = tiles(a.vocab, L.piece);
     if (L.pieces == 1) L.piece = a.vocab;
   }
-  // bf16 has fp32's range: the exponentials are kept from the first time.  fp16 has not, and with several pieces there is no room for them.
-  L.keep = L.pieces == 1 && a.dtype == CVLC_BF16;
+  // With room for all of them the exponentials are kept from the first time.  bf16 has fp32's range for them; fp16 has not, and they are gone over
+  // once more (777 x 1000 x 50021: 27 us; multiplying again 103).
+  L.keep = L.pieces == 1 && a.dtype == CVLC_BF16, L.keep_own = L.pieces == 1 && a.dtype == CVLC_F16;
   L.copy_hidden = (pieces && !L.keep) || !on16(a.hidden_dev, a.hidden_stride), L.copy_head = !on16(a.head_dev, a.head_stride);
   L.ld = (a.dim + 7) / 8 * 8;
   L.stats_stride = (a.rows + 31) / 32 * 32;
@@ -827,7 +913,7 @@ HeadLayout head_layout(const cvlc_head& a, uint32_t pieces) {
   auto take = [&](size_t bytes) { const size_t from = at; at = align256(at + bytes); return from; };
   L.off_hidden = take(L.copy_hidden ? a.rows * L.ld * 2 : 0);
   L.off_head = take(L.copy_head ? a.vocab * L.ld * 2 : 0);
-  L.slots = 2 * tiles(a.vocab, stats_tile(a.rows, a.vocab, L.keep));
+  L.slots = 2 * tiles(a.vocab, stats_tile(a.rows, a.vocab, L.keep || L.keep_own));
   L.off_stats = take((size_t)L.slots * L.stats_stride * 8);
   L.off_target = take(a.rows * 4);
   if (pieces) {
@@ -880,7 +966,7 @@ bool make_product(Product& g, bool bf16, bool pairs, const Operand& a, bool a_ro
   if (!g.tile_n) g.tile_n = kTileN;
   g.tiles_m = tiles(g.m, pairs ? 2 * kTileM : kTileM), g.tiles_n = tiles(g.n, g.tile_n);
   // Of the operand with fewer tiles a group, 32 MB or eight tiles, stays in the L2 cache (of which each half of the chip has its own copy), while the other
-  // one's pass by.  (All of it at once, 67 MB: 8192 x 4096 x 16384 read 1.2 GB of memory instead of READGB in each of the products.)
+  // one's pass by.  (All of it at once, 67 MB: 8192 x 4096 x 16384 read 1.2 GB of memory instead of 0.43 for the logits.)
   g.m_first = g.tiles_m <= g.tiles_n;
   const uint64_t bytes = (uint64_t)2 * kTileN * kTileK * ((g.k_blocks + g.splits - 1) / g.splits);
   g.group = (uint32_t)((32ull << 20) / bytes);
@@ -958,8 +1044,10 @@ struct HeadRun {
 
   void logits_once(float* loss, bool graded) {
     Product p = product();
-    p.m = (uint32_t)a.rows, p.n = a.vocab, p.k_blocks = tiles(a.dim, kTileK), p.first = 1, p.tile_n = stats_tile(a.rows, a.vocab, false);
-    multiply<kStats>(kKHeadStats, p, head);
+    p.m = (uint32_t)a.rows, p.n = a.vocab, p.k_blocks = tiles(a.dim, kTileK), p.first = 1, p.tile_n = stats_tile(a.rows, a.vocab, L.keep_own);
+    p.out = base + L.off_g, p.ldo = L.ldg;
+    if (!L.keep_own) multiply<kStats>(kKHeadStats, p, head);
+    else if constexpr (!bf16) multiply<kKeepOwn>(kKHeadKeep, p, head);
     RowsArgs r = rows(loss);
     r.row = graded ? at<float4>(L.off_row) : nullptr, r.half = std::is_same<T, __half>::value;
     launch(kKHeadRows, k_head_rows, row_blocks(), 256, r);
@@ -991,7 +1079,7 @@ struct HeadRun {
     j.parts = at<float>(L.off_parts), j.split_stride = a.rows * L.ldp, j.ldp = L.ldp, j.ldo = to.d_hidden_stride;
     j.splits = L.splits, j.dim = a.dim, j.rows = a.rows, j.alpha = a.scale, j.factor = factor, j.down = down, j.header = header, j.out = to.d_hidden;
     const uint64_t quads = a.rows * ((a.dim + 3) / 4);
-    if (L.splits >= 8) launch(kKHeadJoin, k_head_join<T, 8>, (uint32_t)((quads + 31) / 32), 256, j);
+    if (L.splits >= 8 && quads <= 32768) launch(kKHeadJoin, k_head_join<T, 8>, (uint32_t)((quads + 31) / 32), 256, j);
     else launch(kKHeadJoin, k_head_join<T, 1>, (uint32_t)((quads + 255) / 256), 256, j);
   }
   void run_kept(float* loss, const Gradients& to) {
@@ -1021,13 +1109,20 @@ struct HeadRun {
     copy(hidden, L.off_hidden, a.targets_dev);
     if (L.copy_head) copy(head, L.off_head, nullptr);
     logits_once(loss, true);
+    if (L.keep_own) {
+      RescaleArgs r = {};
+      r.kept = base + L.off_g, r.ldg = L.ldg, r.rows = a.rows, r.stats_stride = L.stats_stride, r.stats = at<float2>(L.off_stats), r.row = at<float4>(L.off_row);
+      r.targets = a.targets_dev, r.vocab = a.vocab, r.tile_n = stats_tile(a.rows, a.vocab, true), r.token_bytes = a.token_bytes;
+      const uint32_t blocks = tiles(a.rows, 8), along = tiles(a.vocab, 2048), most = blocks < 8 * kNumSM ? tiles(8 * kNumSM, blocks) : 1;
+      if (error == cudaSuccess) launch_kernel(kKHeadRescale, k_head_rescale, dim3(blocks, along < most ? along : most), dim3(256), 0, st, true, r);
+    }
     const float* const down = half ? &header->down : nullptr;
     for (uint32_t i = 0; i < L.pieces; ++i) {
       const uint32_t from = i * L.piece, words = i + 1 < L.pieces ? L.piece : a.vocab - from;
       Product p = product();
       p.m = (uint32_t)a.rows, p.n = words, p.k_blocks = tiles(a.dim, kTileK), p.col0 = from, p.row = at<float4>(L.off_row);
       p.out = base + L.off_g, p.ldo = L.ldg;
-      multiply<kProbs>(kKHeadProbs, p, {static_cast<const T*>(head.at) + (uint64_t)from * head.ld, a.dim, words, head.ld});
+      if (!L.keep_own) multiply<kProbs>(kKHeadProbs, p, {static_cast<const T*>(head.at) + (uint64_t)from * head.ld, a.dim, words, head.ld});
       gradients(from, words, hidden, to, down);
     }
     join(to, nullptr, down);

@@ -14,7 +14,8 @@ def sums(n, size):
 
 
 def step(hidden, head, targets, scale=1.0, weight=None, kept=False):
-    """kept: the exponentials are kept in 16 bits and their rows' factors go into the hidden states, which are rounded too for the head's gradient.
+    """kept: the exponentials are kept in 16 bits.  In bf16 their rows' factors go into the hidden states, which are rounded too for the head's
+    gradient; in fp16, where they are at most 1 in steps of 2^-24, they are multiplied and rounded once more.
     loss, d_hidden, d_head; the largest error of each before it is rounded to the operands' type, and its root mean square (the rounding of G to
     16 bits is off by a third of a half step, squared, on average)"""
     h, w = hidden.double(), head.double()
@@ -44,11 +45,13 @@ def step(hidden, head, targets, scale=1.0, weight=None, kept=False):
     cut = G.abs() * u * (1 + 2 * far)                         # the rounding to 16 bits
     if dtype == torch.float16:                                 # held at most 2^15 times the largest weight, in steps of 2^-24, and flushed below 2^-126
         cut = cut + 2.0 ** -39 * wt.abs().max() * 2
+        if kept:
+            cut = cut + G.abs() * u * 1.01 + 2.0 ** -25 * wt.abs()[:, None] * q.amax(dim=1, keepdim=True)
     cut = cut + 2.0 ** -126 * wt.abs().max()
     out = {"loss": loss, "d_hidden": G @ w * scale, "d_head": G.T @ h * scale}
     aw, ah = w.abs(), h.abs()
     tol["d_hidden"] = abs(scale) * ((off + cut) @ aw + sums(vocab, G.abs() @ aw)) + out["d_hidden"].abs() * 4 * U
-    if kept:
+    if kept and dtype == torch.bfloat16:
         cut_head, square = cut + G.abs() * u * 1.01, cut.square() + (G.abs() * u).square()
     else:
         cut_head, square = cut, cut.square()
@@ -71,7 +74,7 @@ def assert_near(got, want, tol, what="", mean=None):
 
 def check(loss, d_hidden, d_head, hidden, head, targets, scale=1.0, weight=None, pieces=1):
     vocab = head.shape[0]
-    kept = hidden.dtype == torch.bfloat16 and vocab <= (-(-vocab // pieces) + 255) // 256 * 256
+    kept = vocab <= (-(-vocab // pieces) + 255) // 256 * 256
     want, tol, mean = step(hidden, head, targets, scale, weight, kept)
     assert_near(loss, want["loss"], tol["loss"] * 1.01 + want["loss"].abs() * U, "loss")
     for name, got in (("d_hidden", d_hidden), ("d_head", d_head)):
