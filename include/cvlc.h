@@ -579,7 +579,8 @@ int cvlc_head_step(const cvlc_head* a, float* loss_dev, void* d_hidden_dev, uint
  *               key `seed`, word value % 4, the lower half for m, the upper one for v; a v above 0 stays above 0.  All zeros are the
  *               states before the first step.
  *  copy_dev     n values of copy_dtype, rounded from the new param, or NULL
- *  lr_dev, step_dev   device words in place of values that a captured graph would hold: lr is multiplied by *lr_dev, t is *step_dev; or NULL
+ *  lr_dev, step_dev   device words in place of values that a captured graph would hold: lr is multiplied by *lr_dev, t is *step_dev; or NULL.
+ *               A *step_dev of 0 changes nothing and reports INVALID_ARG in *status_dev
  *  norm_dev     clip = min(1, max_norm / *norm_dev) (cvlc_grad_norm's, with the same grad_scale); NULL: clip = 1.  If it is
  *               not finite the call changes nothing and reports NONFINITE_INPUT in *status_dev (one int32 of the caller's, or NULL)
  * A value whose v / (1 - beta2^t) is above 2^104 (a gradient of 4e15) takes no step.

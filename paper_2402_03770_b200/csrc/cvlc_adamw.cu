@@ -209,6 +209,10 @@ __global__ void __launch_bounds__(kThreads) k_adamw(const __grid_constant__ Tens
   uint32_t step = s.step;
   if (s.step_dev) {
     step = *s.step_dev;
+    if (step == 0) {  // the averages have nothing to be divided by
+      if (s.status && blockIdx.x == 0 && threadIdx.x == 0) set_status(s.status, CVLC_ERR_INVALID_ARG);
+      return;
+    }
     if (threadIdx.x == 0) {
       double p1 = 1.0, p2 = 1.0, q1 = s.beta1, q2 = s.beta2;
       for (uint32_t k = step; k; k >>= 1) {

@@ -1064,7 +1064,7 @@ struct HeadRun {
     Product q = product();
     q.m = words, q.n = a.dim, q.k_blocks = tiles(a.rows, kTileK);
     T* const out = static_cast<T*>(to.d_head) + (uint64_t)from * to.d_head_stride;
-    q.out = out, q.ldo = to.d_head_stride, q.wide = on16(out, to.d_head_stride);
+    q.out = out, q.ldo = to.d_head_stride, q.wide = on16(out, to.d_head_stride) && a.dim % 8 == 0;  // a box writes whole vectors of 16 bytes: what lies behind a row's end with them, too
     q.alpha_dev = down;
     const bool fits = make_product(p, bf16, pairs, g, false, piece, true, false) && make_product(q, bf16, pairs, g, true, hidden_scaled, true, q.wide);
     if (pairs) {

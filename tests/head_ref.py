@@ -39,8 +39,8 @@ def step(hidden, head, targets, scale=1.0, weight=None, kept=False):
     dz = sums(dim, h.abs() @ w.abs().T * abs(scale)) + 6 * U * z.abs()
     far = dz.amax(dim=1, keepdim=True)
     tol = {"loss": wt.abs() * (2 * far[:, 0] + LN) + loss.abs() * 4 * U}
-    # a loss that is small: relative to the sum of the other words' exponentials
-    tol["loss"] = torch.minimum(tol["loss"], loss.abs() * (2 * far[:, 0].expm1() + LN + 4 * U) + 2.0 ** -126)
+    # a loss that is small: relative to the sum of the other words' exponentials, of which each counts as 0 below 2^-126 of the target's
+    tol["loss"] = torch.minimum(tol["loss"], loss.abs() * (2 * far[:, 0].expm1() + LN + 4 * U) + wt.abs() * vocab * 2.0 ** -126 + 2.0 ** -126)
     off = G.abs() * (2 * far + LN + 4 * U)                     # the exponent
     cut = G.abs() * u * (1 + 2 * far)                         # the rounding to 16 bits
     if dtype == torch.float16:                                 # held at most 2^15 times the largest weight, in steps of 2^-24, and flushed below 2^-126

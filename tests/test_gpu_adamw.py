@@ -149,6 +149,37 @@ def test_no_step_behind_a_norm_that_is_not_finite(bits, norm):
         assert all(torch.equal(x, y) for x, y in zip(s[k], b))
 
 
+def test_no_step_of_number_0():
+    s = make([5000, 77], bits=8)
+    before = [[x.clone() for x in s[k]] for k in ("params", "m", "v", "scales")]
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    B.cvlc_adamw(s["list"], lr=1e-3, step=5, step_dev=torch.zeros(1, dtype=torch.int32, device="cuda"), status=status)
+    assert status.item() == B.CVLC_ERR_INVALID_ARG
+    for k, b in zip(("params", "m", "v", "scales"), before):
+        assert all(torch.equal(x, y) for x, y in zip(s[k], b))
+
+
+def test_streams_at_once():
+    """two lists in two streams, and their norms, are what they are alone"""
+    a, b = (make([300_000, 77, 4001], bits=bits, seed=bits, shift=1) for bits in (8, 32))
+    c, d = (make([300_000, 77, 4001], bits=bits, seed=bits, shift=1) for bits in (8, 32))
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    norms = [torch.zeros(1, device="cuda") for _ in range(4)]
+    ws = [B.alloc_bytes(B.cvlc_grad_norm_workspace_bytes(x["list"]), torch.device("cuda")) for x in (a, b, c, d)]
+    torch.cuda.synchronize()
+    for t in range(1, 6):
+        for x, n, w, st in zip((a, b), norms, ws, streams):
+            B.cvlc_grad_norm(x["list"], n, w, stream=st)
+            B.cvlc_adamw(x["list"], lr=1e-3, step=t, norm=n, seed=t, stream=st)
+    torch.cuda.synchronize()
+    for x, n, w in zip((c, d), norms[2:], ws[2:]):
+        for t in range(1, 6):
+            B.cvlc_grad_norm(x["list"], n, w)
+            B.cvlc_adamw(x["list"], lr=1e-3, step=t, norm=n, seed=t)
+    for x, y in ((a, c), (b, d)):
+        assert all(torch.equal(p, q) for k in ("params", "m", "v") for p, q in zip(x[k], y[k]))
+
+
 def test_nan_stays_in_its_block():
     s = make([600], bits=8)
     s["grads"][0][300] = float("nan")

@@ -100,6 +100,33 @@ def test_all_rows_count_for_nothing(dtype):
     assert not any(bool(x.any()) for x in (alone, loss, dh, dw))
 
 
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("rows,dim,pad,shift", [(200, 63, 1, 0), (100, 65, 7, 0), (300, 200, 8, 8), (40, 7, 4, 3), (130, 72, 24, 0)])
+@pytest.mark.parametrize("pieces", [1, 2])
+def test_what_lies_between_the_rows_stays(dtype, rows, dim, pad, shift, pieces):
+    hidden, head, t = make(rows, dim, 700, dtype, pad, shift)
+    room = [torch.full((x.shape[0] * (dim + pad) + shift + 64,), 7.0, dtype=dtype, device="cuda") for x in (hidden, head)]
+    dh, dw = (r[shift:shift + x.shape[0] * (dim + pad)].view(-1, dim + pad)[:, :dim] for r, x in zip(room, (hidden, head)))
+    loss = torch.full((rows + 8,), 7.0, device="cuda")
+    B.cvlc_head_step(hidden, head, t, loss[:rows], dh, dw, space(hidden, head, pieces), pieces=pieces)
+    R.check(loss[:rows], dh, dw, hidden, head, t, pieces=pieces)
+    dh.fill_(7.0), dw.fill_(7.0)
+    assert all(bool((r == 7.0).all()) for r in room) and bool((loss[rows:] == 7.0).all())
+
+
+@pytest.mark.parametrize("pieces", [1, 2])
+def test_gradients_beside_what_they_belong_to(pieces):
+    """hidden states and their gradient in rows of one matrix, and so the head"""
+    hidden, head, t = make(150, 64, 600)
+    both = [torch.zeros(x.shape[0], 128, dtype=BF, device="cuda") for x in (hidden, head)]
+    for b, x in zip(both, (hidden, head)):
+        b[:, :64] = x
+    loss = torch.zeros(150, device="cuda")
+    B.cvlc_head_step(both[0][:, :64], both[1][:, :64], t, loss, both[0][:, 64:], both[1][:, 64:], space(both[0][:, :64], both[1][:, :64], pieces), pieces=pieces)
+    R.check(loss, both[0][:, 64:], both[1][:, 64:], hidden, head, t, pieces=pieces)
+    assert torch.equal(both[0][:, :64], hidden) and torch.equal(both[1][:, :64], head)
+
+
 def test_no_rows():
     hidden, head, t = make(4, 64, 300)
     dw = torch.ones(300, 72, dtype=BF, device="cuda")
@@ -135,7 +162,7 @@ def test_far_logits(dtype, pieces):
 def test_rows_far_above_their_target(rows):
     """some word 2^60 times and more as likely as the target, in single rows, next to others of the same tiles and of others"""
     hidden, head, t = make(rows, 64, 800, width=8.0)
-    weight = torch.rand(rows, device="cuda")
+    weight = torch.rand(rows, generator=torch.Generator(device="cuda").manual_seed(48), device="cuda")
     for i in {0, rows // 2, rows - 1}:
         hidden[i] = (-25 * head[t[i]].float()).to(BF)
     loss, _, _ = check(hidden, head, t, scale=0.9, weight=weight)
