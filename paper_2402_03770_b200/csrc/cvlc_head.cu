@@ -45,14 +45,13 @@ __device__ __forceinline__ void let_next_in() { asm volatile("griddepcontrol.lau
 // sum), one issues the products, eight warps read a finished tile from the tensor memory while the next one is made in its other half.
 constexpr uint32_t kTileM = 128, kTileN = 256, kTileK = 64;
 constexpr int kThreads = 384, kOutWarps = 8;
-constexpr uint32_t kBytesA = kTileM * kTileK * 2, kBytesB = kTileN * kTileK * 2;
 constexpr uint32_t kBoxBytes = 32 * 128;  // of a warp, 32 rows of 64 columns on their way out
-template <int CG>
-constexpr int kStages = CG == 2 ? 6 : 4;
-template <int CG>
-constexpr uint32_t kStageBytes = kBytesA + kBytesB / CG;  // of one block
-template <int CG>
-constexpr size_t kGemmShared = kStages<CG> * kStageBytes<CG> + kOutWarps * kBoxBytes + 1024;
+// The ring's stages hold 64 values of the sum of a block's rows and columns.  A pair has six of 32 KB.  A block of its own with few rows copies only those: the
+// products read what follows them as rows, too, which nobody looks at, and there is room for more stages (8 x 4096 x 131072: 207 -> 171 us, the copy bandwidth).
+constexpr uint32_t kRingBytes = 192 * 1024;
+constexpr int kMostStages = 8;
+constexpr uint32_t kPairBytes = (kTileM + kTileN / 2) * kTileK * 2, kPairStages = kRingBytes / kPairBytes;
+constexpr size_t kGemmShared = kRingBytes + kOutWarps * kBoxBytes + 1024;
 
 struct Header {  // at the beginning of the workspace
   float up, down;         // fp16: a power of two that brings weights to at most 1, times 2^15, and its inverse
@@ -70,6 +69,8 @@ struct Product {
   CUtensorMap a, b, c;                   // c: the output, where it is of 16 bits and its rows lie on 16 bytes
   uint32_t m, n, k_blocks;               // rows, columns, steps of 64 of the sum
   uint32_t tile_n, tiles_m, tiles_n, splits;  // columns of a tile; splits of the sum
+  uint32_t a_bytes, b_bytes, stage_bytes, stages;  // of the ring
+  uint32_t values;                       // of the sum in a stage: 64, or what there is if that is less and both operands come rows first
   uint32_t m_first, group;               // tiles of one column of tiles follow one another, else those of a row; so many of them, then the next column
   uint32_t col0, token_bytes;            // stats, probs: the word of column 0
   float k2, alpha;                       // scale log2(e); factor of the output
@@ -369,14 +370,13 @@ __device__ __forceinline__ void finish_tile(const Product& g, const Work& w, uin
 
 template <int EPI, bool A_ROWS, bool B_ROWS, class T, int CG>
 __global__ void __launch_bounds__(kThreads, 1) k_head_product(const __grid_constant__ Products<EPI> both) {
-  constexpr int stages = kStages<CG>;
   extern __shared__ uint8_t dynamic[];
-  __shared__ uint64_t full[stages], empty[stages], made[2], taken[2], over;
+  __shared__ uint64_t full[kMostStages], empty[kMostStages], made[2], taken[2], over;
   __shared__ uint32_t tensor_at, late;
   const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x & 31, rank = pair_rank<CG>();
   const uint32_t ring = (smem_at(dynamic) + 1023) & ~1023u;
   if (threadIdx.x == 0) {
-    for (int i = 0; i < stages; ++i) mbar_init(full + i, 1), mbar_init(empty + i, 1);
+    for (int i = 0; i < kMostStages; ++i) mbar_init(full + i, 1), mbar_init(empty + i, 1);
     for (int i = 0; i < 2; ++i) mbar_init(made + i, 1), mbar_init(taken + i, CG * kOutWarps);
     mbar_init(&over, 1);
     late = 0;
@@ -388,6 +388,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_head_product(const __grid_const
   pair_sync<CG>();
   tensor_after();
   const Product& g0 = both.p[0];
+  const uint32_t stages = CG == 2 ? kPairStages : g0.stages, stage_bytes = CG == 2 ? kPairBytes : g0.stage_bytes;
   const uint32_t tensor = tensor_at, first = blockIdx.x / CG, apart = gridDim.x / CG;
   if (!g0.early || warp >= 4) {
     pdl_enter();
@@ -404,19 +405,20 @@ __global__ void __launch_bounds__(kThreads, 1) k_head_product(const __grid_const
       if (left_out(g, w)) continue;
       const Work r = work_of<CG>(g, second ? w - items0 : w);
       const bool a_rows = EPI == kBoth ? second : A_ROWS;
+      const uint32_t a_bytes = CG == 2 ? kTileM * kTileK * 2 : g.a_bytes, bytes = CG == 2 ? 2 * kPairBytes : a_bytes + g.b_bytes, values = CG == 2 ? kTileK : g.values;
       for (uint32_t k = r.k_from; k < r.k_to; ++k) {
         if (!(ok = mbar_wait(empty + s, phase ^ 1, &late))) break;
-        if (rank == 0) mbar_expect(full + s, CG * kBytesA + g.tile_n * kTileK * 2);
-        const uint32_t a = ring + s * kStageBytes<CG>, b = a + kBytesA, bar = leader_at<CG>(smem_at(full + s)), n0 = r.n0 + rank * (g.tile_n / CG);
+        if (rank == 0) mbar_expect(full + s, bytes);
+        const uint32_t a = ring + s * stage_bytes, b = a + a_bytes, bar = leader_at<CG>(smem_at(full + s)), n0 = r.n0 + rank * (g.tile_n / CG);
         if (a_rows) {
 #pragma unroll
-          for (uint32_t i = 0; i < kTileM / 64; ++i) load_tile<CG>(g.a, a + i * kTileBytes64, bar, r.m0 + 64 * i, k * kTileK);
+          for (uint32_t i = 0; i < kTileM / 64; ++i) load_tile<CG>(g.a, a + i * values * 128, bar, r.m0 + 64 * i, k * kTileK);
         } else {
           load_tile<CG>(g.a, a, bar, k * kTileK, r.m0);
         }
         if constexpr (B_ROWS) {  // tiles of 256 columns only
 #pragma unroll
-          for (uint32_t i = 0; i < kTileN / CG / 64; ++i) load_tile<CG>(g.b, b + i * kTileBytes64, bar, n0 + 64 * i, k * kTileK);
+          for (uint32_t i = 0; i < kTileN / CG / 64; ++i) load_tile<CG>(g.b, b + i * values * 128, bar, n0 + 64 * i, k * kTileK);
         } else {
           load_tile<CG>(g.b, b, bar, k * kTileK, n0);
         }
@@ -443,17 +445,20 @@ __global__ void __launch_bounds__(kThreads, 1) k_head_product(const __grid_const
       const Work r = work_of<CG>(g, second ? w - items0 : w);
       const bool a_rows = EPI == kBoth ? second : A_ROWS;
       const uint32_t kind = product_kind(bf16, a_rows, B_ROWS, CG * kTileM, g.tile_n);
+      const uint32_t a_bytes = CG == 2 ? kTileM * kTileK * 2 : g.a_bytes, values = CG == 2 ? kTileK : g.values;
       const uint32_t half = turn_of & 1;
       if (!(ok = mbar_wait(taken + half, (turn_of / 2 & 1) ^ 1, &late))) break;
       tensor_after();
       for (uint32_t k = r.k_from; k < r.k_to; ++k) {
         if (!(ok = mbar_wait(full + s, phase, &late))) break;
         tensor_after();
-        const uint32_t a = ring + s * kStageBytes<CG>, b = a + kBytesA;
+        const uint32_t a = ring + s * stage_bytes, b = a + a_bytes;
 #pragma unroll
         for (uint32_t i = 0; i < kTileK / 16; ++i)
-          multiply<CG>(tensor + half * kTileN, a_rows ? operand<true>(a + i * kStepBytes<true>) : operand<false>(a + i * kStepBytes<false>),
-                       operand<B_ROWS>(b + i * kStepBytes<B_ROWS>), kind, k != r.k_from || i != 0);
+          if (!B_ROWS || i * 16 < values)
+            multiply<CG>(tensor + half * kTileN,
+                         a_rows ? operand<true>(a + i * kStepBytes<true>, values) : operand<false>(a + i * kStepBytes<false>, values),
+                         operand<B_ROWS>(b + i * kStepBytes<B_ROWS>, values), kind, k != r.k_from || i != 0);
         commit<CG>(empty + s);
         any = true;
         if (++s == stages) s = 0, phase ^= 1;
@@ -467,7 +472,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_head_product(const __grid_const
       mbar_wait(&over, 0, &none, kMostWait / 4);
     }
   } else if (warp >= 4) {
-    const uint32_t half_tile = (warp - 4) / 4, quarter = warp & 3, box = ring + stages * kStageBytes<CG> + (warp - 4) * kBoxBytes;
+    const uint32_t half_tile = (warp - 4) / 4, quarter = warp & 3, box = ring + kRingBytes + (warp - 4) * kBoxBytes;
     uint32_t turn_of = 0;
     for (uint32_t w = first; w < items; w += apart) {
       const bool second = EPI == kBoth && w >= items0;
@@ -650,8 +655,10 @@ __device__ __forceinline__ float2 join_two(float2 x, float2 y, bool relative) {
   const float m = fmaxf(x.x, y.x), from = m == -CUDART_INF_F ? 0.0f : m;
   return make_float2(m, relative ? x.y * exp2f(x.x - from) + y.y * exp2f(y.x - from) : x.y + y.y);
 }
-// The parts of a block's rows joined: eight threads hold what is left of each, one of a warp.
-__device__ __forceinline__ void join_parts(const RowsArgs& a, uint64_t row, uint32_t group, bool relative, float2 (*part)[kRowsOf]) {
+// The parts of a block's rows joined: eight threads hold what is left of each, one of a warp.  Returns whether a block of the products has given up.
+__device__ __forceinline__ bool join_parts(const RowsArgs& a, uint64_t row, uint32_t group, bool relative, float2 (*part)[kRowsOf]) {
+  static_assert(kNumSM <= 256, "a thread for every block");
+  const uint32_t late = threadIdx.x < kNumSM ? a.header->late[threadIdx.x] : 0;
   float2 sum = make_float2(-CUDART_INF_F, 0.0f);
   if (row < a.rows) {
     const float2* const from = a.stats + row;
@@ -671,7 +678,7 @@ __device__ __forceinline__ void join_parts(const RowsArgs& a, uint64_t row, uint
     sum = join_two(sum, other, relative);
   }
   if ((threadIdx.x & 31) < kRowsOf) part[threadIdx.x / 32][threadIdx.x % kRowsOf] = sum;
-  __syncthreads();
+  return __syncthreads_or((int)late) != 0;
 }
 
 // A row's parts joined.  Sums relative to the largest; that of the words other than the target (o) is kept apart, so that 1 - q and a small loss
@@ -682,8 +689,7 @@ __global__ void __launch_bounds__(256) k_head_rows(const RowsArgs a) {
   __shared__ float2 part[8][kRowsOf];
   const uint32_t group = threadIdx.x / kRowsOf, lane = threadIdx.x % kRowsOf;
   const uint64_t row = (uint64_t)blockIdx.x * kRowsOf + lane;
-  const bool late = any_late(a.header);
-  join_parts(a, row, group, true, part);
+  const bool late = join_parts(a, row, group, true, part);
   if (group || row >= a.rows) return;
   const int64_t target = target_of(a.targets, a.token_bytes, row);
   const float weight = a.weight ? a.weight[row] : 1.0f;
@@ -719,8 +725,14 @@ __global__ void __launch_bounds__(256) k_head_rows_kept(const RowsArgs a) {
   if (a.second && a.wild[(uint64_t)blockIdx.x * kRowsOf / kWildRows] == 0) return;
   const uint32_t group = threadIdx.x / kRowsOf, lane = threadIdx.x % kRowsOf;
   const uint64_t row = (uint64_t)blockIdx.x * kRowsOf + lane;
-  const bool late = any_late(a.header);
-  join_parts(a, row, group, false, part);
+  const uint64_t row0 = (uint64_t)blockIdx.x * kRowsOf;
+  const uint32_t warp = threadIdx.x / 32, at = (threadIdx.x & 31) * 8;
+  const __nv_bfloat16* const h = a.hidden + (row0 + warp) * a.hidden_ld;
+  uint4 ahead[4];  // the beginning of the hidden states, on its way meanwhile
+#pragma unroll
+  for (int k = 0; k < 4; ++k)
+    if (row0 + warp < a.rows && at + k * 256 + 8 <= a.dim) ahead[k] = __ldg(reinterpret_cast<const uint4*>(h + at + k * 256));
+  const bool late = join_parts(a, row, group, false, part);
   if (group == 0 && row < a.rows) {
     const int64_t target = target_of(a.targets, a.token_bytes, row);
     const float weight = a.weight ? a.weight[row] : 1.0f;
@@ -749,18 +761,15 @@ __global__ void __launch_bounds__(256) k_head_rows_kept(const RowsArgs a) {
     factors[lane] = factor;
   }
   __syncthreads();
-  const uint64_t row0 = (uint64_t)blockIdx.x * kRowsOf;
-  const uint32_t warp = threadIdx.x / 32;
   if (row0 + warp >= a.rows) return;
   const float f = factors[warp];
   if ((threadIdx.x & 31) == 0) a.factor[row0 + warp] = f;
-  const __nv_bfloat16* const h = a.hidden + (row0 + warp) * a.hidden_ld;
   __nv_bfloat16* const to = a.scaled + (row0 + warp) * a.scaled_ld;
-  for (uint32_t i = (threadIdx.x & 31) * 8; i < a.dim; i += 256) {
+  auto scale = [&](uint32_t i, const uint4& raw) {
     float x[8] = {};
     if (f != 0.0f) {  // else the row may hold anything
       if (i + 8 <= a.dim) {
-        widen<__nv_bfloat16>(__ldg(reinterpret_cast<const uint4*>(h + i)), x);
+        widen<__nv_bfloat16>(raw, x);
       } else {
         for (uint32_t k = 0; i + k < a.dim; ++k) x[k] = to_float(h[i + k]);
       }
@@ -768,6 +777,17 @@ __global__ void __launch_bounds__(256) k_head_rows_kept(const RowsArgs a) {
       for (int k = 0; k < 8; ++k) x[k] *= f;
     }
     *reinterpret_cast<uint4*>(to + i) = narrow<__nv_bfloat16>(x);
+  };
+#pragma unroll
+  for (int k = 0; k < 4; ++k)
+    if (at + k * 256 < a.dim) scale(at + k * 256, ahead[k]);
+  for (uint32_t i = at + 1024; i < a.dim; i += 1024) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if (i + k * 256 + 8 <= a.dim) ahead[k] = __ldg(reinterpret_cast<const uint4*>(h + i + k * 256));
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if (i + k * 256 < a.dim) scale(i + k * 256, ahead[k]);
   }
 }
 
@@ -939,13 +959,13 @@ HeadLayout head_layout(const cvlc_head& a, uint32_t pieces) {
 template <int EPI, bool A_ROWS, bool B_ROWS, class T, int CG>
 cudaError_t run_product_of(int id, const Products<EPI>& g, uint64_t items, cudaStream_t st, bool overlap) {
   static OncePerDevice once;
-  const cudaError_t e = once_per_device(once, [] { return allow_shared(k_head_product<EPI, A_ROWS, B_ROWS, T, CG>, kGemmShared<CG>); });
+  const cudaError_t e = once_per_device(once, [] { return allow_shared(k_head_product<EPI, A_ROWS, B_ROWS, T, CG>, kGemmShared); });
   if (e != cudaSuccess) return e;
   LaunchScope ls(id, st);
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((uint32_t)(items * CG < kNumSM ? items * CG : kNumSM));
   cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = kGemmShared<CG>;
+  cfg.dynamicSmemBytes = kGemmShared;
   cfg.stream = st;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -961,6 +981,10 @@ struct Operand {
   const void* at;
   uint64_t cols, rows, ld;
 };
+void set_stages(Product& g, uint32_t stage_bytes) {
+  g.stage_bytes = stage_bytes;
+  g.stages = kRingBytes / stage_bytes < kMostStages ? kRingBytes / stage_bytes : kMostStages;
+}
 // D = A B^T, sums along the operands' columns, or along their rows
 bool make_product(Product& g, bool bf16, bool pairs, const Operand& a, bool a_rows, const Operand& b, bool b_rows, bool boxes) {
   if (!g.tile_n) g.tile_n = kTileN;
@@ -973,9 +997,14 @@ bool make_product(Product& g, bool bf16, bool pairs, const Operand& a, bool a_ro
   if (g.group < 8) g.group = 8;
   const uint32_t fewer = g.m_first ? g.tiles_m : g.tiles_n;
   if (g.group > fewer) g.group = fewer;
+  // what a block copies at a time: of the rows those that are there, of the sum (rows first) what there is
+  const uint32_t rows = !pairs && !a_rows && g.m < kTileM ? (g.m + 7) / 8 * 8 : kTileM, columns = g.tile_n / (pairs ? 2 : 1);
+  g.values = !pairs && a_rows && b_rows && a.rows < kTileK ? (uint32_t)(a.rows + 15) / 16 * 16 : kTileK;
+  g.a_bytes = rows * g.values * 2, g.b_bytes = columns * g.values * 2, g.stage_bytes = g.a_bytes + g.b_bytes;
+  set_stages(g, g.stage_bytes);
   if (boxes && !make_tensor_map(&g.c, g.out, bf16, g.n, g.m, g.ldo, 64, 32)) return false;
-  return make_tensor_map(&g.a, a.at, bf16, a.cols, a.rows, a.ld, 64, a_rows ? kTileK : kTileM) &&
-         make_tensor_map(&g.b, b.at, bf16, b.cols, b.rows, b.ld, 64, b_rows ? kTileK : g.tile_n / (pairs ? 2 : 1));
+  return make_tensor_map(&g.a, a.at, bf16, a.cols, a.rows, a.ld, 64, a_rows ? g.values : rows) &&
+         make_tensor_map(&g.b, b.at, bf16, b.cols, b.rows, b.ld, 64, b_rows ? g.values : columns);
 }
 
 struct Gradients {
@@ -1071,6 +1100,7 @@ struct HeadRun {
       run_product<kParts, false, true, 2>(kKHeadParts, {{p}}, fits);
       run_product<kGrad, true, true, 2>(kKHeadGrad, {{q}}, fits);
     } else {
+      set_stages(p, p.stage_bytes > q.stage_bytes ? p.stage_bytes : q.stage_bytes);  // one ring for both
       run_product<kBoth, false, true, 1>(kKHeadGrads, {{p, q}}, fits);
     }
   }

@@ -106,11 +106,12 @@ __device__ __forceinline__ void tiles_stored() { asm volatile("cp.async.bulk.wai
 //   along the sum ("K first"): a line is 64 values of the sum of one row; groups of eight rows follow one another.  16 values of the sum
 //   further: 32 bytes.
 //   along the rows ("rows first"): a line is 64 rows of one value of the sum; groups of eight values of the sum follow one another, 64 further rows are a
-//   tile of their own, 8192 bytes on (64 values of the sum).  16 values of the sum further: 2048 bytes.
-constexpr uint32_t kTileBytes64 = 64 * 128;
+//   tile of their own behind all values of the sum.  16 values of the sum further: 2048 bytes.
+// `values`: of the sum, in a tile of rows first
 template <bool ROWS_FIRST>
-__device__ __forceinline__ uint64_t operand(uint32_t at) {
-  constexpr uint64_t leading = ROWS_FIRST ? kTileBytes64 >> 4 : 1, stride = 1024 >> 4;
+__device__ __forceinline__ uint64_t operand(uint32_t at, uint32_t values) {
+  const uint64_t leading = ROWS_FIRST ? values * 128 >> 4 : 1;
+  constexpr uint64_t stride = 1024 >> 4;
   return (uint64_t)((at & 0x3FFFF) >> 4) | leading << 16 | stride << 32 | 1ull << 46 | 2ull << 61;
 }
 template <bool ROWS_FIRST>
