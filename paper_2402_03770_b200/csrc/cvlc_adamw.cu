@@ -201,8 +201,12 @@ __device__ __forceinline__ uint4 philox4x32_10(uint4 c, const PhiloxRoundKeys& r
 }
 constexpr float kLeast = 0x1p-100f;  // a block whose largest value is below this is held as zeros
 
+// Threads of a block: with 8-bit states a block of 128 needs fewer registers a thread (48, 61 of 256), and 40 warps share an SM (100 M values: 324 -> 299 us);
+// with 32 bits the loads alone fill it (11 M values in one vector 73 and 78).
+template <bool EIGHT>
+constexpr int kStepThreads = EIGHT ? 128 : 256;
 template <bool EIGHT, uint32_t CAP>
-__global__ void __launch_bounds__(kThreads) k_adamw(const __grid_constant__ TensorList<CAP> L) {
+__global__ void __launch_bounds__(kStepThreads<EIGHT>) k_adamw(const __grid_constant__ TensorList<CAP> L) {
   const StepScalars& s = L.s;
   __shared__ float corrections[2];
   float ic1 = s.ic1, ic2 = s.ic2;
@@ -241,7 +245,7 @@ __global__ void __launch_bounds__(kThreads) k_adamw(const __grid_constant__ Tens
   const uint64_t blocks = (t.n + t.lead + kBlock - 1) / kBlock;
   uint64_t block = (uint64_t)(blockIdx.x - t.first) * s.chunk + warp;
   const uint64_t end = min(blocks, (uint64_t)(blockIdx.x - t.first + 1) * s.chunk);
-  for (; block < end; block += kWarps) {
+  for (; block < end; block += kStepThreads<EIGHT> / 32) {
     const int64_t at = (int64_t)(block * kBlock + lane * kPer) - t.lead;
     const uint32_t vec = at >= 0 && (uint64_t)at + kPer <= t.n ? t.vec : 0;
     float p[kPer], g[kPer], m[kPer], v[kPer];
@@ -287,7 +291,8 @@ __global__ void __launch_bounds__(kThreads) k_adamw(const __grid_constant__ Tens
 #pragma unroll
       for (int i = 0; i < kPer; i += 2) am = largest(am, m[i], m[i + 1]), av = largest(av, v[i], v[i + 1]);
       const float a = __uint_as_float(__reduce_max_sync(kFull, __float_as_uint(am))), b = __uint_as_float(__reduce_max_sync(kFull, __float_as_uint(av)));
-      const float ia = a >= kLeast ? 448.0f * (1.0f / a) : 0.0f, ib = b >= kLeast ? 57344.0f * (1.0f / b) : 0.0f;
+      const float inverse = 1.0f / (lane & 16 ? b : a), of_a = __shfl_sync(kFull, inverse, 0), of_b = __shfl_sync(kFull, inverse, 16);  // one division for both
+      const float ia = a >= kLeast ? 448.0f * of_a : 0.0f, ib = b >= kLeast ? 57344.0f * of_b : 0.0f;
       const uint64_t quad = (uint64_t)at / 4;
       uint32_t wm[2], wv[2];
 #pragma unroll
@@ -377,16 +382,17 @@ __global__ void __launch_bounds__(1024) k_norm_join(const double* parts, uint32_
 
 // ---- launching -----------------------------------------------------------------------------
 
-// Blocks of values in a chunk, the work of a block of threads: short ones where there is little to do, so that all SMs have some, longer ones
-// so that finding the tensor does not count.
+// Blocks of values in a chunk, the work of a block of threads.  A step with 32-bit states has one for each warp: new blocks of threads keep more loads on their
+// way than a loop does (100 M values: one 409 us, two 419, four 426; one vector of 11 M 67, 70, 73).  With 8 bits, where there is more to do before the
+// first value (Philox's keys, the tensor), eight for each of four warps (314 us with two, 298 with four, 293), fewer where SMs would have none.
 uint64_t blocks_of(const cvlc_adamw_tensor* t, uint32_t n) {
   uint64_t blocks = 0;
   for (uint32_t i = 0; i < n; ++i) blocks += (t[i].n + kPer + kBlock - 1) / kBlock;
   return blocks;
 }
-uint32_t step_chunk(uint64_t blocks) {
+uint32_t step_chunk(uint64_t blocks, uint32_t bits) {
   uint32_t chunk = kWarps;
-  while (chunk < 4 * kWarps && blocks / (2 * chunk) >= 8 * kNumSM) chunk *= 2;
+  while (bits == 8 && chunk < 4 * kWarps && blocks / (2 * chunk) >= 8 * kNumSM) chunk *= 2;
   return chunk;
 }
 // At most kNormChunks in all: a block's work should be short next to all of it (1,907 chunks on 1,184 places: 231 us instead of 183 for 500 M bf16 values)
@@ -450,8 +456,8 @@ cudaError_t by_lists(const cvlc_adamw_tensor* t, uint32_t n, const StepScalars& 
 }
 template <uint32_t CAP>
 void run_step(const TensorList<CAP>& L, uint32_t bits, cudaStream_t st) {
-  if (bits == 8) launch_kernel(kKAdamw, k_adamw<true, CAP>, dim3(L.chunks), dim3(kThreads), 0, st, false, L);
-  else launch_kernel(kKAdamw, k_adamw<false, CAP>, dim3(L.chunks), dim3(kThreads), 0, st, false, L);
+  if (bits == 8) launch_kernel(kKAdamw, k_adamw<true, CAP>, dim3(L.chunks), dim3(kStepThreads<true>), 0, st, false, L);
+  else launch_kernel(kKAdamw, k_adamw<false, CAP>, dim3(L.chunks), dim3(kStepThreads<false>), 0, st, false, L);
 }
 
 }  // namespace
@@ -463,7 +469,7 @@ cudaError_t launch_adamw(const cvlc_adamw_tensor* t, uint32_t n, const cvlc_adam
   s.ic1 = (float)(1.0 / (1.0 - pow(a.beta1, (double)a.step))), s.ic2 = (float)(0x1p24 / (1.0 - pow(a.beta2, (double)a.step)));
   s.grad_scale = a.grad_scale, s.max_norm = a.max_norm, s.norm = a.norm_dev, s.lr_dev = a.lr_dev, s.step_dev = a.step_dev, s.seed = a.seed, s.step = a.step;
   s.param_dtype = a.param_dtype, s.grad_dtype = a.grad_dtype, s.copy_dtype = a.copy_dtype, s.status = a.status_dev;
-  s.chunk = step_chunk(blocks_of(t, n));
+  s.chunk = step_chunk(blocks_of(t, n), a.state_bits);
   return by_lists(t, n, s, a.state_bits, false, [&](const auto& L) { run_step(L, a.state_bits, st); });
 }
 
