@@ -15,7 +15,7 @@ namespace {
 constexpr int kBlock = CVLC_STATE_BLOCK;  // values of a warp at a time, and of a scale
 constexpr int kPer = kBlock / 32;         // consecutive ones of a lane
 constexpr int kThreads = 256, kWarps = kThreads / 32;
-constexpr uint32_t kNormChunks = 64 * kNumSM;  // of the norm, at most, and one more for every tensor
+constexpr uint32_t kNormChunks = 24 * kNumSM;  // of the norm, at most, and one more for every tensor
 
 // Which of a tensor's arrays can be read and written by vectors.  fp32 states have no blocks of their own, so that their tensors are cut where the
 // weights' addresses are multiples of 32 bytes: `lead` values before the first are not there.
@@ -395,7 +395,7 @@ uint32_t step_chunk(uint64_t blocks, uint32_t bits) {
   while (bits == 8 && chunk < 4 * kWarps && blocks / (2 * chunk) >= 8 * kNumSM) chunk *= 2;
   return chunk;
 }
-// At most kNormChunks in all: a block's work should be short next to all of it (1,907 chunks on 1,184 places: 231 us instead of 183 for 500 M bf16 values)
+// At most kNormChunks in all (500 M bf16 values: ten for each SM 188 us, 24 175, 64 183, 256 224): many, that blocks end together; not too many, since each has to find its tensor.
 uint32_t norm_chunk(uint64_t blocks) {
   if (blocks < 8 * kWarps * (uint64_t)kNumSM) return kWarps;
   const uint64_t whole = 4 * kWarps, chunk = (blocks + kNormChunks - 1) / kNormChunks;
