@@ -64,7 +64,7 @@ __device__ __forceinline__ bool any_late(const Header* h) {  // asked by all thr
   return __syncthreads_or((int)x) != 0;
 }
 
-enum Epilogue { kStats, kKeep, kKeepOwn, kProbs, kParts, kGrad, kBoth };  // kBoth: parts, then grad
+enum Epilogue { kStats, kKeep, kKeepOwn, kKeepWide, kProbs, kParts, kGrad, kBoth };  // kBoth: parts, then grad
 struct Product {
   CUtensorMap a, b, c;                   // c: the output, where it is of 16 bits and its rows lie on 16 bytes
   uint32_t m, n, k_blocks;               // rows, columns, steps of 64 of the sum
@@ -234,8 +234,8 @@ __device__ __forceinline__ void finish_tile(const Product& g, const Work& w, uin
       if (c & 1) box_out(g.c, box, lane, col - 32, w.m0 + quarter * 32);
     }
     if (there) g.stats[(uint64_t)(w.slot + half) * g.stats_stride + row] = make_float2(most, sum);
-  } else if constexpr (EPI == kKeepOwn) {
-    // fp16 has no range to spare: each row of 128 columns relative to its own maximum, which takes a look of its own
+  } else if constexpr (EPI == kKeepOwn || EPI == kKeepWide) {
+    // each row of 128 columns relative to its own maximum, which takes a look of its own: in fp16, which has no range to spare, and in fp32 (wide)
     const int64_t target = there ? target_of(g.targets, g.token_bytes, row) : -1;
     float most = -CUDART_INF_F, sum = 0.0f;
     for (int c = 0; c < 4; ++c) {
@@ -259,10 +259,8 @@ __device__ __forceinline__ void finish_tile(const Product& g, const Work& w, uin
     const float from = most == -CUDART_INF_F ? 0.0f : most;
     for (int c = 0; c < 4; ++c) {
       const uint32_t col = w.n0 + half * 128 + c * 32;
-      if ((c & 1) == 0) {
-        if (col >= w.n_end) break;
-        box_free(lane);
-      }
+      if (EPI == kKeepWide ? col >= w.n_end : (c & 1) == 0 && col >= w.n_end) break;
+      if (EPI == kKeepOwn && (c & 1) == 0) box_free(lane);
       tensor_load(tensor + c * 32, v);
       tensor_loaded(v);
 #pragma unroll
@@ -277,11 +275,22 @@ __device__ __forceinline__ void finish_tile(const Product& g, const Work& w, uin
 #pragma unroll
       for (int i = 0; i < 32; ++i) v[i] = exp2_fast(v[i]), s[i & 3] += v[i];
       sum += (s[0] + s[1]) + (s[2] + s[3]);
-      uint32_t p[16];
+      if constexpr (EPI == kKeepWide) {
+        float* const out = static_cast<float*>(g.out) + (uint64_t)row * g.ldo + col;
 #pragma unroll
-      for (int i = 0; i < 16; ++i) p[i] = pack2<T>(v[2 * i], v[2 * i + 1]);
-      row_to_box(box, lane, c & 1, p);
-      if (c & 1) box_out(g.c, box, lane, col - 32, w.m0 + quarter * 32);
+        for (int h = 0; h < 4; ++h) {
+          uint32_t p[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) p[i] = __float_as_uint(v[8 * h + i]);
+          if (there) store_sector(out + 8 * h, p);
+        }
+      } else {
+        uint32_t p[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) p[i] = pack2<T>(v[2 * i], v[2 * i + 1]);
+        row_to_box(box, lane, c & 1, p);
+        if (c & 1) box_out(g.c, box, lane, col - 32, w.m0 + quarter * 32);
+      }
     }
     if (there) g.stats[(uint64_t)(w.slot + half) * g.stats_stride + row] = make_float2(most, sum);
   } else if constexpr (EPI == kProbs) {
@@ -687,30 +696,52 @@ __global__ void __launch_bounds__(256) k_head_rows(const RowsArgs a) {
   pdl_enter();
   if (a.row) let_next_in();  // else the last of the call
   __shared__ float2 part[8][kRowsOf];
+  __shared__ uint32_t counts[kRowsOf];
   const uint32_t group = threadIdx.x / kRowsOf, lane = threadIdx.x % kRowsOf;
   const uint64_t row = (uint64_t)blockIdx.x * kRowsOf + lane;
   const bool late = join_parts(a, row, group, true, part);
-  if (group || row >= a.rows) return;
-  const int64_t target = target_of(a.targets, a.token_bytes, row);
-  const float weight = a.weight ? a.weight[row] : 1.0f;
-  if (target >= (int64_t)a.vocab && a.status) set_status(a.status, CVLC_ERR_INVALID_ARG);
-  if (target < 0 || target >= (int64_t)a.vocab || weight == 0.0f) {
-    a.loss[row] = late ? CUDART_NAN_F : 0.0f;
-    if (a.row) a.row[row] = make_float4(0, 0, 0, 0);
-    return;
+  if (group == 0 && row < a.rows) {
+    const int64_t target = target_of(a.targets, a.token_bytes, row);
+    const float weight = a.weight ? a.weight[row] : 1.0f;
+    if (target >= (int64_t)a.vocab && a.status) set_status(a.status, CVLC_ERR_INVALID_ARG);
+    const bool there = target >= 0 && target < (int64_t)a.vocab && weight != 0.0f;
+    counts[lane] = there;
+    float loss = 0.0f;
+    float4 r = make_float4(0, 0, 0, 0);
+    if (there) {
+      const float zt = a.at_target[row];
+      float most = zt;
+      for (uint32_t i = 0; i < 8; ++i) most = fmaxf(most, part[i][lane].x);
+      double others = 0.0;
+      for (uint32_t i = 0; i < 8; ++i)
+        if (part[i][lane].x != -CUDART_INF_F || part[i][lane].y != 0.0f) others += (double)(part[i][lane].y * exp2f(part[i][lane].x - most));
+      const float o = (float)others, right = exp2f(zt - most), total = right + o, w = a.half ? weight * a.header->up : weight;
+      loss = weight * (most == zt ? log1pf(o) : logf(total) + (most - zt) * kLn2);
+      r = make_float4(most + log2f(total), w, -(o / total) * w, 0.0f);
+    }
+    a.loss[row] = late ? CUDART_NAN_F : loss;
+    if (a.row) a.row[row] = r;
   }
-  const float zt = a.at_target[row];
-  float most = zt;
-  for (uint32_t i = 0; i < 8; ++i) most = fmaxf(most, part[i][lane].x);
-  double others = 0.0;
-  for (uint32_t i = 0; i < 8; ++i)
-    if (part[i][lane].x != -CUDART_INF_F || part[i][lane].y != 0.0f) others += (double)(part[i][lane].y * exp2f(part[i][lane].x - most));
-  const float o = (float)others, right = exp2f(zt - most), total = right + o;
-  const float loss = most == zt ? log1pf(o) : logf(total) + (most - zt) * kLn2;
-  a.loss[row] = late ? CUDART_NAN_F : weight * loss;
-  if (a.row) {
-    const float w = a.half ? weight * a.header->up : weight;
-    a.row[row] = make_float4(most + log2f(total), w, -(o / total) * w, 0.0f);
+  if (!a.scaled) return;
+  __syncthreads();
+  // the hidden states as they count: those of other rows, which may hold anything, would have a part in the head's gradient
+  const uint64_t mine = (uint64_t)blockIdx.x * kRowsOf + threadIdx.x / 32;
+  if (mine >= a.rows) return;
+  const uint16_t* const h = reinterpret_cast<const uint16_t*>(a.hidden) + mine * a.hidden_ld;
+  uint16_t* const to = reinterpret_cast<uint16_t*>(a.scaled) + mine * a.scaled_ld;
+#pragma unroll 4
+  for (uint32_t i = (threadIdx.x & 31) * 8; i < a.dim; i += 256) {
+    uint4 v = make_uint4(0, 0, 0, 0);
+    if (counts[threadIdx.x / 32]) {
+      if (i + 8 <= a.dim) {
+        v = __ldg(reinterpret_cast<const uint4*>(h + i));
+      } else {
+        uint32_t x[8] = {};
+        for (uint32_t k = 0; i + k < a.dim; ++k) x[k] = h[i + k];
+        v = make_uint4(x[0] | x[1] << 16, x[2] | x[3] << 16, x[4] | x[5] << 16, x[6] | x[7] << 16);
+      }
+    }
+    *reinterpret_cast<uint4*>(to + i) = v;
   }
 }
 
@@ -791,16 +822,18 @@ __global__ void __launch_bounds__(256) k_head_rows_kept(const RowsArgs a) {
   }
 }
 
-// Exponentials that are kept relative to the maximum of their 128 columns become G, in their place: times exp(maximum - ln sum exp) and the weight.
-// A warp a row, two times 128 columns at a time.
+// Exponentials that are kept relative to the maximum of their 128 columns become G: times exp(maximum - ln sum exp) and the weight.  In fp16 in their place; in fp32
+// (up to 128 rows, where their room is small) so that G is rounded once.  A warp a row, two times 128 columns at a time.
 struct RescaleArgs {
-  void* kept;
-  uint64_t ldg, rows, stats_stride;
+  const void* kept;
+  void* to;
+  uint64_t ld_kept, ld_to, rows, stats_stride;
   const float2* stats;
   const float4* row;
   const void* targets;
   uint32_t vocab, tile_n, token_bytes;
 };
+template <class FROM, class T>
 __global__ void __launch_bounds__(256) k_head_rescale(const RescaleArgs a) {
   pdl_enter();
   let_next_in();
@@ -808,21 +841,29 @@ __global__ void __launch_bounds__(256) k_head_rescale(const RescaleArgs a) {
   const uint32_t lane = threadIdx.x & 31;
   if (row >= a.rows) return;
   const float4 r = a.row[row];
-  __half* const at = static_cast<__half*>(a.kept) + row * a.ldg;
+  const FROM* const from = static_cast<const FROM*>(a.kept) + row * a.ld_kept;
+  T* const to = static_cast<T*>(a.to) + row * a.ld_to;
   const int64_t target = r.y == 0.0f ? -1 : target_of(a.targets, a.token_bytes, row);
 #pragma unroll 4
   for (uint32_t col = (blockIdx.y * 32 + lane) * 8; col < a.vocab; col += gridDim.y * 256) {
     const uint32_t tile = col / a.tile_n, slot = 2 * tile + (col - tile * a.tile_n) / 128;
-    const uint4 raw = __ldcs(reinterpret_cast<const uint4*>(at + col));
-    const float f = exp2f(a.stats[slot * a.stats_stride + row].x - r.x) * r.y;
     float v[8];
-    widen<__half>(raw, v);
+    if constexpr (std::is_same<FROM, float>::value) {
+      const uint4 x = *reinterpret_cast<const uint4*>(from + col), y = *reinterpret_cast<const uint4*>(from + col + 4);
+      float lo[4], hi[4];
+      widen<float>(x, lo), widen<float>(y, hi);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = lo[i], v[4 + i] = hi[i];
+    } else {
+      widen<FROM>(__ldcs(reinterpret_cast<const uint4*>(from + col)), v);
+    }
+    const float f = exp2f(a.stats[slot * a.stats_stride + row].x - r.x) * r.y;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       v[i] = r.y == 0.0f ? 0.0f : v[i] * f;
       if (target == (int64_t)col + i) v[i] = r.z;
     }
-    *reinterpret_cast<uint4*>(at + col) = narrow<__half>(v);
+    *reinterpret_cast<uint4*>(to + col) = narrow<T>(v);
   }
 }
 
@@ -885,12 +926,11 @@ bool by_pairs(uint64_t m) { return m > kTileM; }
 uint32_t tiles_m(uint64_t m) { return tiles(m, by_pairs(m) ? 2 * kTileM : kTileM); }
 
 // Rows that fit in one tile: the head is read once, by the SMs alike if its tiles come out even.
-// (Boxes that are written have 64 columns.)
-uint32_t stats_tile(uint64_t m, uint32_t n, bool written) {
+uint32_t stats_tile(uint64_t m, uint32_t n) {
   uint32_t best = kTileN;
   if (by_pairs(m)) return best;
   auto cost = [&](uint32_t t) { return (uint64_t)tiles(tiles(n, t), kNumSM) * t; };
-  for (uint32_t t = kTileN; t >= 128; t -= written ? 64 : 32)
+  for (uint32_t t = kTileN; t >= 128; t -= 32)
     if (cost(t) < cost(best)) best = t;
   return best;
 }
@@ -908,13 +948,18 @@ uint32_t splits_of(uint64_t m, uint64_t n, uint32_t k_blocks) {
   return best;
 }
 
+// What becomes of the exponentials of the first product.  Several pieces: nothing, there is no room for them.  Up to 128 rows: kept in fp32.  bf16 has fp32's
+// range, and they are relative to the target's; fp16 has not, and they are relative to the maximum of 128 columns and gone over once more (777 x 1000 x
+// 50021: 27 us; multiplying again 103).
+enum class Keep { kNot, kWide, kBf16, kFp16 };
 struct HeadLayout {
-  bool keep, keep_own, copy_hidden, copy_head;
+  Keep keep;
+  bool copy_hidden, copy_head;
   uint64_t ld;             // of copies
   uint32_t piece, pieces;  // words
   uint64_t ldg, ldp, stats_stride;
   uint32_t splits, slots, blocks_wild;
-  size_t off_hidden, off_head, off_scaled, off_stats, off_target, off_row, off_factor, off_raised, off_wild, off_g, off_parts, total;
+  size_t off_hidden, off_head, off_scaled, off_stats, off_target, off_row, off_factor, off_raised, off_wild, off_g, off_wide, off_parts, total;
 };
 HeadLayout head_layout(const cvlc_head& a, uint32_t pieces) {
   HeadLayout L = {};
@@ -923,17 +968,17 @@ HeadLayout head_layout(const cvlc_head& a, uint32_t pieces) {
     L.pieces = tiles(a.vocab, L.piece);
     if (L.pieces == 1) L.piece = a.vocab;
   }
-  // With room for all of them the exponentials are kept from the first time.  bf16 has fp32's range for them; fp16 has not, and they are gone over
-  // once more (777 x 1000 x 50021: 27 us; multiplying again 103).
-  L.keep = L.pieces == 1 && a.dtype == CVLC_BF16, L.keep_own = L.pieces == 1 && a.dtype == CVLC_F16;
-  L.copy_hidden = (pieces && !L.keep) || !on16(a.hidden_dev, a.hidden_stride), L.copy_head = !on16(a.head_dev, a.head_stride);
+  L.keep = L.pieces != 1 ? Keep::kNot : !by_pairs(a.rows) ? Keep::kWide : a.dtype == CVLC_BF16 ? Keep::kBf16 : Keep::kFp16;
+  // copied where they do not begin on 16 bytes, or where rows that count for nothing have to become zeros first
+  L.copy_hidden = !on16(a.hidden_dev, a.hidden_stride) || (pieces && (L.keep == Keep::kNot || L.keep == Keep::kFp16));
+  L.copy_head = !on16(a.head_dev, a.head_stride);
   L.ld = (a.dim + 7) / 8 * 8;
   L.stats_stride = (a.rows + 31) / 32 * 32;
   size_t at = align256(sizeof(Header));
   auto take = [&](size_t bytes) { const size_t from = at; at = align256(at + bytes); return from; };
   L.off_hidden = take(L.copy_hidden ? a.rows * L.ld * 2 : 0);
   L.off_head = take(L.copy_head ? a.vocab * L.ld * 2 : 0);
-  L.slots = 2 * tiles(a.vocab, stats_tile(a.rows, a.vocab, L.keep || L.keep_own));
+  L.slots = 2 * tiles(a.vocab, stats_tile(a.rows, a.vocab));
   L.off_stats = take((size_t)L.slots * L.stats_stride * 8);
   L.off_target = take(a.rows * 4);
   if (pieces) {
@@ -942,7 +987,7 @@ HeadLayout head_layout(const cvlc_head& a, uint32_t pieces) {
     L.splits = splits_of(a.rows, a.dim, tiles(L.piece, kTileK));
     L.off_g = take(a.rows * L.ldg * 2);
     L.off_parts = take((size_t)L.splits * a.rows * L.ldp * 4);
-    if (L.keep) {
+    if (L.keep == Keep::kBf16) {
       L.blocks_wild = tiles(a.rows, kWildRows);
       L.off_scaled = take(a.rows * L.ld * 2);
       L.off_factor = take(a.rows * 4);
@@ -950,6 +995,10 @@ HeadLayout head_layout(const cvlc_head& a, uint32_t pieces) {
       L.off_wild = take(L.blocks_wild * 4);
     } else {
       L.off_row = take(a.rows * 16);
+    }
+    if (L.keep == Keep::kWide) {
+      L.off_scaled = take(a.rows * L.ld * 2);
+      L.off_wide = take(a.rows * L.ldg * 4);
     }
   }
   L.total = at;
@@ -1053,9 +1102,11 @@ struct HeadRun {
   // a product of hidden rows with words
   template <int EPI>
   void multiply(int id, Product p, const Operand& words) {
-    const bool pairs = by_pairs(a.rows), fits = make_product(p, bf16, pairs, hidden, false, words, false, EPI != kStats);
-    if (pairs) run_product<EPI, false, false, 2>(id, {{p}}, fits);
-    else run_product<EPI, false, false, 1>(id, {{p}}, fits);
+    const bool pairs = by_pairs(a.rows), fits = make_product(p, bf16, pairs, hidden, false, words, false, EPI != kStats && EPI != kKeepWide);
+    if constexpr (EPI != kKeepWide)
+      if (pairs) run_product<EPI, false, false, 2>(id, {{p}}, fits);
+    if constexpr (EPI != kKeep && EPI != kKeepOwn)
+      if (!pairs) run_product<EPI, false, false, 1>(id, {{p}}, fits);
   }
   void copy(Operand& x, size_t off, const void* targets) {
     launch(kKHeadAlign, k_head_align, tiles(x.rows, 8), 256, static_cast<const uint16_t*>(x.at), x.ld, at<uint16_t>(off), L.ld, x.rows, a.dim, targets,
@@ -1071,15 +1122,28 @@ struct HeadRun {
   }
   uint32_t row_blocks() const { return tiles(a.rows, kRowsOf); }
 
+  // the losses, and what makes G of the logits
   void logits_once(float* loss, bool graded) {
     Product p = product();
-    p.m = (uint32_t)a.rows, p.n = a.vocab, p.k_blocks = tiles(a.dim, kTileK), p.first = 1, p.tile_n = stats_tile(a.rows, a.vocab, L.keep_own);
-    p.out = base + L.off_g, p.ldo = L.ldg;
-    if (!L.keep_own) multiply<kStats>(kKHeadStats, p, head);
+    p.m = (uint32_t)a.rows, p.n = a.vocab, p.k_blocks = tiles(a.dim, kTileK), p.first = 1, p.tile_n = stats_tile(a.rows, a.vocab);
+    p.out = base + (L.keep == Keep::kWide ? L.off_wide : L.off_g), p.ldo = L.ldg;
+    if (graded && L.keep == Keep::kWide) multiply<kKeepWide>(kKHeadKeep, p, head);
+    else if (!graded || L.keep == Keep::kNot) multiply<kStats>(kKHeadStats, p, head);
     else if constexpr (!bf16) multiply<kKeepOwn>(kKHeadKeep, p, head);
     RowsArgs r = rows(loss);
-    r.row = graded ? at<float4>(L.off_row) : nullptr, r.half = std::is_same<T, __half>::value;
+    r.row = graded ? at<float4>(L.off_row) : nullptr, r.half = !bf16;
+    if (graded && L.keep == Keep::kWide)
+      r.hidden = static_cast<const __nv_bfloat16*>(hidden.at), r.hidden_ld = hidden.ld, r.scaled = at<__nv_bfloat16>(L.off_scaled), r.scaled_ld = L.ld, r.dim = a.dim;
     launch(kKHeadRows, k_head_rows, row_blocks(), 256, r);
+  }
+  template <class FROM>
+  void rescale(size_t from) {
+    RescaleArgs r = {};
+    r.kept = base + from, r.to = base + L.off_g, r.ld_kept = r.ld_to = L.ldg, r.rows = a.rows, r.stats_stride = L.stats_stride, r.stats = at<float2>(L.off_stats);
+    r.row = at<float4>(L.off_row), r.targets = a.targets_dev, r.vocab = a.vocab, r.tile_n = stats_tile(a.rows, a.vocab), r.token_bytes = a.token_bytes;
+    const uint32_t blocks = tiles(a.rows, 8), along = tiles(a.vocab, 256), most = blocks < 8 * kNumSM ? tiles(8 * kNumSM, blocks) : 1;
+    if (error == cudaSuccess)
+      launch_kernel(kKHeadRescale, k_head_rescale<FROM, T>, dim3(blocks, along < most ? along : most), dim3(256), 0, st, true, r);
   }
   // The part of a piece of the words in both gradients.  Up to 128 rows, where the hidden states' gradient has few tiles and the head's tiles are one step
   // of the sum each, one launch makes both (16 x 1024 x 32000: 52 -> 30 us); by pairs, two do (8192 x 4096 x 131072: 13.7 ms, 15.2 in one).
@@ -1121,7 +1185,7 @@ struct HeadRun {
     for (uint32_t turn = 0; turn < 2; ++turn) {
       Product p = product();
       p.m = (uint32_t)a.rows, p.n = a.vocab, p.k_blocks = tiles(a.dim, kTileK), p.first = turn == 0;
-      p.out = base + L.off_g, p.ldo = L.ldg, p.tile_n = stats_tile(a.rows, a.vocab, true), p.early = turn == 0;
+      p.out = base + L.off_g, p.ldo = L.ldg, p.early = turn == 0;
       if (turn) p.skip = &header->wild, p.wild = t.wild;
       if constexpr (bf16) multiply<kKeep>(kKHeadKeep, p, head);
       RowsArgs r = rows(loss);
@@ -1134,36 +1198,34 @@ struct HeadRun {
     join(to, at<float>(L.off_factor), nullptr);
   }
   void run_pieces(float* loss, const Gradients& to) {
-    const bool half = std::is_same<T, __half>::value;
-    if (half) launch(kKHeadBegin, k_head_begin, 1, a.rows > 256 ? 1024 : 256, header, a.row_weight_dev, a.targets_dev, a.token_bytes, a.rows, a.vocab);
-    copy(hidden, L.off_hidden, a.targets_dev);
+    if (!bf16) launch(kKHeadBegin, k_head_begin, 1, a.rows > 256 ? 1024 : 256, header, a.row_weight_dev, a.targets_dev, a.token_bytes, a.rows, a.vocab);
+    if (L.copy_hidden) copy(hidden, L.off_hidden, L.keep == Keep::kWide ? nullptr : a.targets_dev);
     if (L.copy_head) copy(head, L.off_head, nullptr);
     logits_once(loss, true);
-    if (L.keep_own) {
-      RescaleArgs r = {};
-      r.kept = base + L.off_g, r.ldg = L.ldg, r.rows = a.rows, r.stats_stride = L.stats_stride, r.stats = at<float2>(L.off_stats), r.row = at<float4>(L.off_row);
-      r.targets = a.targets_dev, r.vocab = a.vocab, r.tile_n = stats_tile(a.rows, a.vocab, true), r.token_bytes = a.token_bytes;
-      const uint32_t blocks = tiles(a.rows, 8), along = tiles(a.vocab, 2048), most = blocks < 8 * kNumSM ? tiles(8 * kNumSM, blocks) : 1;
-      if (error == cudaSuccess) launch_kernel(kKHeadRescale, k_head_rescale, dim3(blocks, along < most ? along : most), dim3(256), 0, st, true, r);
-    }
-    const float* const down = half ? &header->down : nullptr;
+    if (L.keep == Keep::kWide) rescale<float>(L.off_wide);
+    else if constexpr (!bf16)
+      if (L.keep == Keep::kFp16) rescale<T>(L.off_g);
+    const Operand counted = L.keep == Keep::kWide ? Operand{base + L.off_scaled, a.dim, a.rows, L.ld} : hidden;
+    const float* const down = bf16 ? nullptr : &header->down;
     for (uint32_t i = 0; i < L.pieces; ++i) {
       const uint32_t from = i * L.piece, words = i + 1 < L.pieces ? L.piece : a.vocab - from;
-      Product p = product();
-      p.m = (uint32_t)a.rows, p.n = words, p.k_blocks = tiles(a.dim, kTileK), p.col0 = from, p.row = at<float4>(L.off_row);
-      p.out = base + L.off_g, p.ldo = L.ldg;
-      if (!L.keep_own) multiply<kProbs>(kKHeadProbs, p, {static_cast<const T*>(head.at) + (uint64_t)from * head.ld, a.dim, words, head.ld});
-      gradients(from, words, hidden, to, down);
+      if (L.keep == Keep::kNot) {
+        Product p = product();
+        p.m = (uint32_t)a.rows, p.n = words, p.k_blocks = tiles(a.dim, kTileK), p.col0 = from, p.row = at<float4>(L.off_row);
+        p.out = base + L.off_g, p.ldo = L.ldg;
+        multiply<kProbs>(kKHeadProbs, p, {static_cast<const T*>(head.at) + (uint64_t)from * head.ld, a.dim, words, head.ld});
+      }
+      gradients(from, words, counted, to, down);
     }
     join(to, nullptr, down);
   }
   cudaError_t run(float* loss, const Gradients* to) {
-    if (!to || L.keep) {
+    if (!to || L.keep == Keep::kBf16) {
       if (L.copy_hidden) copy(hidden, L.off_hidden, nullptr);
       if (L.copy_head) copy(head, L.off_head, nullptr);
     }
     if (!to) logits_once(loss, false);
-    else if (L.keep) run_kept(loss, *to);
+    else if (L.keep == Keep::kBf16) run_kept(loss, *to);
     else run_pieces(loss, *to);
     return error != cudaSuccess ? error : cudaGetLastError();
   }
