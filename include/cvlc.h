@@ -526,14 +526,17 @@ int cvlc_embed_grad(const void* tokens_dev, uint32_t token_bytes, uint64_t n, co
  * A target below 0 is none, and a row without one, or of weight 0, counts for nothing, whatever it holds: its loss, its gradient and
  * its part of d_head are 0.  A target >= vocab is treated as none and reported (INVALID_ARG) in *status_dev (one int32 of the caller's,
  * 0 beforehand; or NULL).  An infinite or NaN logit makes the row's loss, and what the row has a part in, not finite.
- * The products are made by the tensor cores: operands in 16 bits (CVLC_F16 or CVLC_BF16; there is no product of fp32), sums in fp32.  A logit's
- * gradient, row_weight (softmax - one for the target), is rounded to the operands' type (in fp16 times a power of two that keeps the largest row_weight at
- * 2^15), as the operand of the two products that follow; d_hidden and d_head are rounded once more.
+ * The products are made by the tensor cores: operands in 16 bits (CVLC_F16 or CVLC_BF16; there is no product of fp32), sums in fp32, in steps of 16 that
+ * may be cut off instead of rounded.  A logit's gradient, row_weight (softmax - one for the target), is rounded to the operands' type (in fp16 times a
+ * power of two that keeps the largest row_weight at 2^15), as the operand of the two products that follow, and d_hidden and d_head once more.  With more than
+ * 128 rows in one piece there is another rounding: the exponentials are kept in 16 bits; in fp16 they are multiplied later, in bf16 their rows' factors
+ * go into the hidden states for d_head, which are rounded.
  *  hidden_dev   rows x dim, hidden_stride elements apart; head_dev: vocab x dim, head_stride apart.  Rows that begin on 16 bytes are
  *               read where they are, others are copied first
  *  targets_dev  rows words of int32 or int64 (token_bytes 4 or 8);  row_weight_dev: rows fp32, or NULL: all 1
- *  pieces       cvlc_head_step makes the gradients of so many pieces of the vocabulary (or fewer: a piece has at least 256 words) one behind the other; the workspace holds rows x
- *               vocab / pieces values of 16 bits
+ *  pieces       cvlc_head_step makes the gradients of so many pieces of the vocabulary (or fewer: a piece has at least 2^22 logits) one behind the other; the workspace holds rows x
+ *               vocab / pieces values of 16 bits (up to 128 rows in one piece: of 32 bits, too).  With one piece the first product is not made
+ *               twice
  *  d_hidden_dev, d_head_dev   as hidden and head, of strides of their own; they must not overlap hidden, head or each other
  *  ws_dev       cvlc_head_workspace_bytes(a, graded) bytes (graded: 0 for cvlc_head_loss, 1 for cvlc_head_step), 256-byte aligned
  * Results do not depend on the order in which blocks run.  Waits inside the kernels are bounded (four seconds): should one run out,

@@ -951,6 +951,7 @@ uint32_t splits_of(uint64_t m, uint64_t n, uint32_t k_blocks) {
 // What becomes of the exponentials of the first product.  Several pieces: nothing, there is no room for them.  Up to 128 rows: kept in fp32.  bf16 has fp32's
 // range, and they are relative to the target's; fp16 has not, and they are relative to the maximum of 128 columns and gone over once more (777 x 1000 x
 // 50021: 27 us; multiplying again 103).
+constexpr uint64_t kLeastPiece = 1ull << 22;
 enum class Keep { kNot, kWide, kBf16, kFp16 };
 struct HeadLayout {
   Keep keep;
@@ -964,7 +965,9 @@ struct HeadLayout {
 HeadLayout head_layout(const cvlc_head& a, uint32_t pieces) {
   HeadLayout L = {};
   if (pieces) {
-    L.piece = tiles((a.vocab + pieces - 1) / pieces, kTileN) * kTileN;
+    // a piece of less than 4 M logits is not worth its launches (22 x 1533 x 2387 in five pieces 119 us, in one 46)
+    const uint64_t words = (a.vocab + pieces - 1) / pieces, least = a.rows ? (kLeastPiece + a.rows - 1) / a.rows : 1;
+    L.piece = tiles(words > least ? words : least < a.vocab ? least : a.vocab, kTileN) * kTileN;
     L.pieces = tiles(a.vocab, L.piece);
     if (L.pieces == 1) L.piece = a.vocab;
   }

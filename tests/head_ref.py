@@ -74,7 +74,7 @@ def assert_near(got, want, tol, what="", mean=None):
 
 def check(loss, d_hidden, d_head, hidden, head, targets, scale=1.0, weight=None, pieces=1):
     vocab = head.shape[0]
-    kept = vocab <= (-(-vocab // pieces) + 255) // 256 * 256 and len(targets) > 128  # up to 128 rows in 32 bits
+    kept = vocab <= (max(-(-vocab // pieces), -(-(1 << 22) // len(targets))) + 255) // 256 * 256 and len(targets) > 128  # up to 128 rows in 32 bits
     want, tol, mean = step(hidden, head, targets, scale, weight, kept)
     assert_near(loss, want["loss"], tol["loss"] * 1.01 + want["loss"].abs() * U, "loss")
     for name, got in (("d_hidden", d_hidden), ("d_head", d_head)):

@@ -77,11 +77,24 @@ def test_pieces(dtype, vocab, pieces):
 
 
 @pytest.mark.parametrize("dtype", [BF, HF])
-@pytest.mark.parametrize("pieces", [1, 3])
-def test_weights_masks_and_scale(dtype, pieces):
-    hidden, head, t = make(333, 72, 1500, dtype)
+@pytest.mark.parametrize("rows,dim,vocab,pieces", [(4200, 96, 3000, 3), (4200, 65, 2817, 2), (17000, 72, 600, 1000), (128, 64, 70000, 2), (100, 72, 90001, 2)])
+def test_pieces_of_many_logits(dtype, rows, dim, vocab, pieces):
+    hidden, head, t = make(rows, dim, vocab, dtype, pad=8 * (rows % 3), seed=rows)
+    few = B.cvlc_head_workspace_bytes(hidden, head, pieces)
+    assert few < B.cvlc_head_workspace_bytes(hidden, head, 1)
+    t[::9] = -1
+    weight = torch.rand(rows, generator=torch.Generator(device="cuda").manual_seed(2), device="cuda")
+    weight[1::7] = 0
+    hidden[1] = float("nan")
+    check(hidden, head, t, scale=1.2, weight=weight, pieces=pieces)
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("rows,pieces", [(333, 1), (333, 3), (120, 1), (4400, 2)])
+def test_weights_masks_and_scale(dtype, rows, pieces):
+    hidden, head, t = make(rows, 72, 1500, dtype)
     g = torch.Generator(device="cuda").manual_seed(5)
-    weight = torch.rand(333, generator=g, device="cuda") * 1e-3 - 2e-4
+    weight = torch.rand(rows, generator=g, device="cuda") * 1e-3 - 2e-4
     weight[::7] = 0
     t[::5] = -1
     t[3] = -(1 << 40)
@@ -148,12 +161,13 @@ def test_words_that_are_not_there_are_reported(pieces):
 
 @pytest.mark.parametrize("dtype", [BF, HF])
 @pytest.mark.parametrize("pieces", [1, 2])
-def test_far_logits(dtype, pieces):
+@pytest.mark.parametrize("rows", [256, 128, 12000])
+def test_far_logits(dtype, rows, pieces):
     """rows whose target is far below or above all others: losses of hundreds, and of next to nothing"""
-    hidden, head, t = make(256, 64, 800, dtype, width=8.0)
-    hidden[:64] = (-20 * head[t[:64]].float()).to(dtype)
+    hidden, head, t = make(rows, 64, 800, dtype, width=8.0)
+    hidden[:32] = (-20 * head[t[:32]].float()).to(dtype)
     hidden[64:128] = (3 * head[t[64:128]].float()).to(dtype)
-    hidden[128:192] *= 12
+    hidden[32:64] *= 12
     loss, _, _ = check(hidden, head, t, pieces=pieces)
     assert float(loss.max()) > 500 and 0 < float(loss[64:128].max()) and float(loss.min()) < 1e-30
 
@@ -178,12 +192,13 @@ def test_any_scale(dtype, scale):
 
 
 @pytest.mark.parametrize("dtype", [BF, HF])
-def test_not_finite(dtype):
-    hidden, head, t = make(140, 64, 500, dtype)
+@pytest.mark.parametrize("rows", [140, 100])
+def test_not_finite(dtype, rows):
+    hidden, head, t = make(rows, 64, 500, dtype)
     good = [x.clone() for x in run(hidden, head, t)]
     hidden[3, 5] = float("nan")
     alone, loss, dh, dw = run(hidden, head, t)
-    others = torch.arange(140, device="cuda") != 3
+    others = torch.arange(rows, device="cuda") != 3
     assert bool(torch.isnan(loss[3])) and bool(torch.isnan(alone[3])) and bool(torch.isnan(dh[3]).all()) and bool(torch.isnan(dw).all(dim=1).all())
     assert torch.equal(loss[others], good[1][others]) and torch.equal(dh[others], good[2][others])
 
