@@ -966,7 +966,7 @@ HeadLayout head_layout(const cvlc_head& a, uint32_t pieces) {
   HeadLayout L = {};
   if (pieces) {
     // a piece of less than 4 M logits is not worth its launches (22 x 1533 x 2387 in five pieces 119 us, in one 46)
-    const uint64_t words = (a.vocab + pieces - 1) / pieces, least = a.rows ? (kLeastPiece + a.rows - 1) / a.rows : 1;
+    const uint64_t words = ((uint64_t)a.vocab + pieces - 1) / pieces, least = a.rows ? (kLeastPiece + a.rows - 1) / a.rows : 1;
     L.piece = tiles(words > least ? words : least < a.vocab ? least : a.vocab, kTileN) * kTileN;
     L.pieces = tiles(a.vocab, L.piece);
     if (L.pieces == 1) L.piece = a.vocab;
