@@ -724,8 +724,8 @@ def cvlc_head_step(hidden: torch.Tensor, head: torch.Tensor, targets: torch.Tens
 
 class AdamwTensors:
     """The tensors of cvlc_adamw and cvlc_grad_norm, made once for all steps: gradients, and for the step weights, states and, with states of
-    8 bits (m in e4m3, v in e5m2, uint8 or those types), scales of shape (blocks of STATE_BLOCK values, 2).  Tensors are contiguous and stay where
-    they are.  lr (a multiple of the call's) and weight_decay: one number, or one for each."""
+    8 bits (m in e4m3, v in e5m2, uint8 or those types), scales of shape (blocks of STATE_BLOCK values, 2).  Tensors are contiguous, stay where
+    they are and do not overlap, but for gradients.  lr (a multiple of the call's) and weight_decay: one number, or one for each."""
 
     def __init__(self, grads: Sequence[torch.Tensor], params: Optional[Sequence[torch.Tensor]] = None, m: Optional[Sequence[torch.Tensor]] = None,
                  v: Optional[Sequence[torch.Tensor]] = None, scales: Optional[Sequence[torch.Tensor]] = None,
@@ -764,6 +764,17 @@ class AdamwTensors:
                     t.scale_dev = at(scales[i], 2 * ((size + STATE_BLOCK - 1) // STATE_BLOCK), CVLC_F32)
                 if copies is not None:
                     t.copy_dev = at(copies[i], size, self.copy_dtype)
+        # what the step writes has no byte in common with anything else of it: a weight that is there twice, as one that two layers share, would be moved twice at once
+        parts = []
+        for i in range(n if self.step else 0):
+            for k, x in enumerate((grads[i], params[i], m[i], v[i], scales and scales[i], copies and copies[i])):
+                if x is not None and x.numel():
+                    parts.append((x.data_ptr(), x.data_ptr() + x.numel() * x.element_size(), k > 0))
+        parts.sort()
+        last = last_written = 0
+        for begin, end, written in parts:
+            assert begin >= (last if written else last_written), "tensors of a step overlap"
+            last, last_written = max(last, end), max(last_written, end if written else 0)
 
 
 def cvlc_adamw(tensors: AdamwTensors, *, lr: float, step: int, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8, grad_scale: float = 1.0,

@@ -3,6 +3,7 @@ import ctypes as C
 import math
 
 import pytest
+import torch
 
 from paper_2402_03770_b200 import binding as B
 
@@ -71,3 +72,20 @@ def test_norm_workspace():
     t = tensor(grad_dev=AT + 2)
     assert B.lib().cvlc_grad_norm(C.byref(t), 1, 0, 1.0, AT, AT, need, None) == BAD
     assert C.sizeof(B.CvlcAdamwTensor) == 64 and C.sizeof(B.CvlcAdamwArgs) == 104
+
+
+def test_binding_refuses_what_overlaps():
+    p, q, g, m, v, w, x, c = (torch.zeros(300) for _ in range(8))
+    half = torch.zeros(300, dtype=torch.bfloat16)
+    B.AdamwTensors([g, g], [p, q], [m, w], [v, x], copies=[half, None])  # gradients alone may be shared
+    B.AdamwTensors([g, g])
+    byte, scales = torch.zeros(4, 300, dtype=torch.uint8), torch.zeros(2, 2, 2)
+    B.AdamwTensors([g[:0], g], [p[:0], p], [byte[0][:0], byte[1]], [byte[2][:0], byte[3]], scales=[scales[0][:0], scales[1]])
+    for how in (([g, c], [p, p], [m, w], [v, x]), ([g, c], [g, q], [m, w], [v, x]), ([g, c], [p, q], [m, m], [v, x]), ([g, c], [p, q], [m, w], [w, x]), ([g, p], [p, q], [m, w], [v, x]),
+                ([g[:100], c[:100]], [p[:100], p[99:199]], [m[:100], w[:100]], [v[:100], x[:100]])):
+        with pytest.raises(AssertionError, match="overlap"):
+            B.AdamwTensors(*how)
+    with pytest.raises(AssertionError, match="overlap"):
+        B.AdamwTensors([g, c], [p, q], [m, w], [v, x], copies=[half, half])
+    with pytest.raises(AssertionError, match="overlap"):
+        B.AdamwTensors([g, c], [p, q], [byte[0], byte[1]], [byte[2], byte[3]], scales=[scales[0], scales[0]])
