@@ -148,6 +148,49 @@ def test_no_rows():
     assert not bool(dw[:, :64].any()) and bool((dw[:, 64:] == 1).all())
 
 
+@pytest.mark.parametrize("rows", [0, 1, 3])
+@pytest.mark.parametrize("stride", [(1 << 30) - 8, (1 << 30) + 8, (1 << 30) + 3])
+def test_rows_far_apart(rows, stride):
+    """strides in bytes beyond 31 bits, and offsets of rows beyond 32"""
+    hidden, head, t = make(rows, 40, 3)
+    h, w, dh, dw = (torch.empty((len(x) - 1) * stride + 40 if len(x) else 0, dtype=BF, device="cuda").as_strided(x.shape, (stride, 1)) for x in (hidden, head) * 2)
+    h.copy_(hidden), w.copy_(head), dh.fill_(7.0), dw.fill_(7.0)
+    loss = torch.zeros(rows, device="cuda")
+    B.cvlc_head_step(h, w, t, loss, dh, dw, space(h, w, 1))
+    if rows:
+        R.check(loss, dh, dw, hidden, head, t)
+    else:
+        assert not bool(dw.any())
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+def test_more_logits_than_32_bits_count(dtype):
+    """the exponentials' offsets pass 2^32; the oracle goes over them in rows of 2048"""
+    hidden, head, t = make(16500, 24, 260500, dtype)
+    assert hidden.shape[0] * head.shape[0] > 1 << 32
+    loss, dh, dw = torch.empty(16500, device="cuda"), torch.empty_like(hidden), torch.empty_like(head)
+    B.cvlc_head_step(hidden, head, t, loss, dh, dw, space(hidden, head, 1))
+    w, total, size = head.double(), torch.zeros(head.shape, dtype=torch.float64, device="cuda"), torch.zeros(head.shape, dtype=torch.float64, device="cuda")
+    u = torch.finfo(dtype).eps / 2
+    for i in range(0, 16500, 2048):
+        h, at = hidden[i:i + 2048].double(), t[i:i + 2048, None]
+        G = h @ w.T
+        far = R.sums(24, h.norm(dim=1).amax() * w.norm(dim=1).amax()) + 6 * R.U * G.abs().amax() + R.LN
+        lse = torch.logsumexp(G, dim=1)
+        want = lse - G.gather(1, at)[:, 0]
+        R.assert_near(loss[i:i + 2048], want, 2 * far + want.abs() * 8 * R.U, "loss")
+        G = G.sub_(lse[:, None]).exp_()
+        least = 2.0 ** -25 * G.amax(dim=1, keepdim=True) + 2.0 ** -38 if dtype == HF else 0.0  # half steps of what is kept, and of G times 2^15
+        G.scatter_add_(1, at, torch.full_like(want, -1.0)[:, None])
+        total.addmm_(G.T, h)
+        want, G = G @ w, G.abs_()
+        # G is rounded twice, and in bf16 the hidden states for the head's gradient; its exponent and the sums (of 260500, 16 at a time)
+        each = G.mul_(2.1 * u + 4 * float(far)).add_(least)
+        R.assert_near(dh[i:i + 2048], want, each @ w.abs() + R.sums(260500, each @ w.abs() / (2 * u)) + want.abs() * u + 2.0 ** -25, "d_hidden")
+        size.addmm_(each.T, h.abs())
+    R.assert_near(dw, total, size + R.sums(16500, size / (2 * u)) + total.abs() * u + 2.0 ** -25, "d_head")
+
+
 @pytest.mark.parametrize("pieces", [1, 2])
 def test_words_that_are_not_there_are_reported(pieces):
     hidden, head, t = make(200, 64, 600)
