@@ -525,7 +525,8 @@ int cvlc_embed_grad(const void* tokens_dev, uint32_t token_bytes, uint64_t n, co
  * and, for cvlc_head_step, the gradients of the sum of all losses, d_hidden and d_head, in the operands' type.
  * A target below 0 is none, and a row without one, or of weight 0, counts for nothing, whatever it holds: its loss, its gradient and
  * its part of d_head are 0.  A target >= vocab is treated as none and reported (INVALID_ARG) in *status_dev (one int32 of the caller's,
- * 0 beforehand; or NULL).  An infinite or NaN logit makes the row's loss, and what the row has a part in, not finite.
+ * 0 beforehand; or NULL).  A NaN or +infinite logit makes the row's loss, and what the row has a part in, not finite (one of
+ * -infinity the loss of its own word, and the gradients).
  * The products are made by the tensor cores: operands in 16 bits (CVLC_F16 or CVLC_BF16; there is no product of fp32), sums in fp32, in steps of 16 that
  * may be cut off instead of rounded.  A logit's gradient, row_weight (softmax - one for the target), is rounded to the operands' type (in fp16 times a
  * power of two that keeps the largest row_weight at 2^15), as the operand of the two products that follow, and d_hidden and d_head once more.  With more than
