@@ -530,13 +530,13 @@ int cvlc_embed_grad(const void* tokens_dev, uint32_t token_bytes, uint64_t n, co
  * The products are made by the tensor cores: operands in 16 bits (CVLC_F16 or CVLC_BF16; there is no product of fp32), sums in fp32, in steps of 16 that
  * may be cut off instead of rounded.  A logit's gradient, row_weight (softmax - one for the target), is rounded to the operands' type (in fp16 times a
  * power of two that keeps the largest row_weight at 2^15), as the operand of the two products that follow, and d_hidden and d_head once more.  With more than
- * 128 rows in one piece there is another rounding: the exponentials are kept in 16 bits; in fp16 they are multiplied later, in bf16 their rows' factors
- * go into the hidden states for d_head, which are rounded.
+ * 128 rows in one piece, and more than 2^22 logits or 8192 words, there is another rounding: the exponentials are kept in 16 bits; in fp16 they are multiplied later,
+ * in bf16 their rows' factors go into the hidden states for d_head, which are rounded.
  *  hidden_dev   rows x dim, hidden_stride elements apart; head_dev: vocab x dim, head_stride apart.  Rows that begin on 16 bytes are
  *               read where they are, others are copied first
  *  targets_dev  rows words of int32 or int64 (token_bytes 4 or 8);  row_weight_dev: rows fp32, or NULL: all 1
  *  pieces       cvlc_head_step makes the gradients of so many pieces of the vocabulary (or fewer: a piece has at least 2^22 logits) one behind the other; the workspace holds rows x
- *               vocab / pieces values of 16 bits (up to 128 rows in one piece: of 32 bits, too).  With one piece the first product is not made
+ *               vocab / pieces values of 16 bits (up to 128 rows in one piece, or 2^22 logits: of 32 bits, too).  With one piece the first product is not made
  *               twice
  *  d_hidden_dev, d_head_dev   as hidden and head, of strides of their own; they must not overlap hidden, head or each other
  *  ws_dev       cvlc_head_workspace_bytes(a, graded) bytes (graded: 0 for cvlc_head_loss, 1 for cvlc_head_step), 256-byte aligned
@@ -672,7 +672,7 @@ int cvlc_selftest_ring(const float* row_dev, uint32_t stages, int give_back, uin
  * k_noalloc_publish_status, k_selftest, k_hist_check, k_apply, k_plan_literal, k_ec_accumulate, k_pack_unframed, k_decode_unframed,
  * k_top_logits, k_distill_loss, k_distill_grad, k_distill_step, k_embed, k_token_sort, k_embed_sum, k_embed_join,
  * k_adamw, k_norm_parts, k_norm_join,
- * k_head_begin, k_head_align, k_head_target, k_head_keep, k_head_stats, k_head_rows, k_head_probs, k_head_rescale, k_head_parts, k_head_grad, k_head_grads, k_head_join. */
+ * k_head_begin, k_head_align, k_head_logits, k_head_softmax, k_head_target, k_head_keep, k_head_stats, k_head_rows, k_head_probs, k_head_rescale, k_head_parts, k_head_grad, k_head_grads, k_head_join. */
 unsigned long long cvlc_launch_count(const char* kernel_name);
 /* Optional kernel timing: after cvlc_profile_select(name, n) the next n launches of that kernel
  * ("*" = of every kernel) are bracketed by a CUDA event pair on their own stream;

@@ -369,7 +369,7 @@ enum KernelId {
   kKRankRest, kKSort, kKPack, kKDecodePrepare, kKFillZero, kKPrefetchL2, kKDecode, kKNoallocStatus, kKSelftest, kKHistCheck, kKApply,
   kKPlanLiteral, kKEcAccumulate, kKPackUnframed, kKDecodeUnframed, kKTopLogits, kKDistillLoss,
   kKDistillGrad, kKDistillStep, kKEmbed, kKTokenSort, kKEmbedSum, kKEmbedJoin, kKAdamw, kKNormParts, kKNormJoin,
-  kKHeadBegin, kKHeadAlign, kKHeadTarget, kKHeadKeep, kKHeadStats, kKHeadRows, kKHeadProbs, kKHeadRescale, kKHeadParts, kKHeadGrad, kKHeadGrads, kKHeadJoin, kNumKernelIds
+  kKHeadBegin, kKHeadAlign, kKHeadLogits, kKHeadSoftmax, kKHeadTarget, kKHeadKeep, kKHeadStats, kKHeadRows, kKHeadProbs, kKHeadRescale, kKHeadParts, kKHeadGrad, kKHeadGrads, kKHeadJoin, kNumKernelIds
 };
 
 // Called around every kernel launch.  Counts launches; when a kernel has been selected with

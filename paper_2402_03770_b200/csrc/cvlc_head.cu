@@ -6,7 +6,8 @@
 // Three products of rows x vocab x dim each.  The first one's values never leave the tensor memory: a tile of them becomes, per row, its maximum
 // and its sum of exponentials (k_head_stats), which are joined to the row's loss and ln sum exp (k_head_rows).  For the gradients a piece of the
 // vocabulary at a time is multiplied again and becomes G, rounded to the type of the operands (k_head_probs), from which come the piece of the head's
-// gradient (k_head_grad) and the piece's part of the hidden states' (k_head_parts, in fp32, joined by k_head_join).
+// gradient (k_head_grad) and the piece's part of the hidden states' (k_head_parts, in fp32, joined by k_head_join).  In one piece the exponentials are kept
+// (k_head_keep); few logits are kept themselves (k_head_logits, k_head_softmax).
 #include <math.h>
 
 #include "cvlc_tensor.cuh"
@@ -404,7 +405,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_head_product(const __grid_const
     let_next_in();
   }
   const uint32_t items0 = g0.skip && *g0.skip == 0 ? 0 : g0.tiles_m * g0.tiles_n * g0.splits;
-  const uint32_t items = items0 + (EPI == kBoth ? both.p[Products<EPI>::count - 1].tiles_m * both.p[Products<EPI>::count - 1].tiles_n : 0);
+  const Product& last = both.p[Products<EPI>::count - 1];
+  const uint32_t items = items0 + (EPI == kBoth ? last.tiles_m * last.tiles_n * last.splits : 0);
   bool ok = true;
   if (warp == 0 && lane == 0) {
     uint32_t s = 0, phase = 0, issued = 0;
@@ -493,7 +495,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_head_product(const __grid_const
       tensor_after();
       const uint32_t at = tensor + half * kTileN + half_tile * 128 + (quarter * 32 << 16);
       if constexpr (EPI == kBoth) {
-        if (second) finish_tile<kGrad, T>(g, r, at, half_tile, quarter, lane, box);
+        if (second && g.splits == 1) finish_tile<kGrad, T>(g, r, at, half_tile, quarter, lane, box);
         else finish_tile<kParts, T>(g, r, at, half_tile, quarter, lane, box);
       } else {
         finish_tile<EPI, T>(g, r, at, half_tile, quarter, lane, box);
@@ -690,6 +692,24 @@ __device__ __forceinline__ bool join_parts(const RowsArgs& a, uint64_t row, uint
   return __syncthreads_or((int)late) != 0;
 }
 
+// A row of hidden states as it counts: others, which may hold anything, would have a part in the head's gradient
+__device__ __forceinline__ void masked_row(const uint16_t* h, uint16_t* to, uint32_t dim, bool counts, uint32_t thread, uint32_t threads) {
+#pragma unroll 4
+  for (uint32_t i = thread * 8; i < dim; i += threads * 8) {
+    uint4 v = make_uint4(0, 0, 0, 0);
+    if (counts) {
+      if (i + 8 <= dim) {
+        v = __ldg(reinterpret_cast<const uint4*>(h + i));
+      } else {
+        uint32_t x[8] = {};
+        for (uint32_t k = 0; i + k < dim; ++k) x[k] = h[i + k];
+        v = make_uint4(x[0] | x[1] << 16, x[2] | x[3] << 16, x[4] | x[5] << 16, x[6] | x[7] << 16);
+      }
+    }
+    *reinterpret_cast<uint4*>(to + i) = v;
+  }
+}
+
 // A row's parts joined.  Sums relative to the largest; that of the words other than the target (o) is kept apart, so that 1 - q and a small loss
 // ln(1 + o) keep their accuracy.
 __global__ void __launch_bounds__(256) k_head_rows(const RowsArgs a) {
@@ -724,25 +744,10 @@ __global__ void __launch_bounds__(256) k_head_rows(const RowsArgs a) {
   }
   if (!a.scaled) return;
   __syncthreads();
-  // the hidden states as they count: those of other rows, which may hold anything, would have a part in the head's gradient
   const uint64_t mine = (uint64_t)blockIdx.x * kRowsOf + threadIdx.x / 32;
   if (mine >= a.rows) return;
-  const uint16_t* const h = reinterpret_cast<const uint16_t*>(a.hidden) + mine * a.hidden_ld;
-  uint16_t* const to = reinterpret_cast<uint16_t*>(a.scaled) + mine * a.scaled_ld;
-#pragma unroll 4
-  for (uint32_t i = (threadIdx.x & 31) * 8; i < a.dim; i += 256) {
-    uint4 v = make_uint4(0, 0, 0, 0);
-    if (counts[threadIdx.x / 32]) {
-      if (i + 8 <= a.dim) {
-        v = __ldg(reinterpret_cast<const uint4*>(h + i));
-      } else {
-        uint32_t x[8] = {};
-        for (uint32_t k = 0; i + k < a.dim; ++k) x[k] = h[i + k];
-        v = make_uint4(x[0] | x[1] << 16, x[2] | x[3] << 16, x[4] | x[5] << 16, x[6] | x[7] << 16);
-      }
-    }
-    *reinterpret_cast<uint4*>(to + i) = v;
-  }
+  masked_row(reinterpret_cast<const uint16_t*>(a.hidden) + mine * a.hidden_ld, reinterpret_cast<uint16_t*>(a.scaled) + mine * a.scaled_ld, a.dim,
+             counts[threadIdx.x / 32], threadIdx.x & 31, 32);
 }
 
 // The same where the exponentials are kept, relative to the target's (to the row's maximum in a second turn): of G = weight exp(z - from) / total the
@@ -822,6 +827,116 @@ __global__ void __launch_bounds__(256) k_head_rows_kept(const RowsArgs a) {
   }
 }
 
+// Few logits: they are there themselves, in parts of their sums, and a row's loss and G are made at once by THREADS threads, of which each holds up to 32 of them.
+// A warp up to 1024 words (557 x 184 x 379: 9.6 us, 12.3 by eight warps), eight up to 8192 (183 x 426 x 3796: 32 us, 40 by 32 warps).
+struct SoftmaxArgs {
+  const float* parts;
+  uint64_t split_stride, ldz, rows, ldg, hidden_ld, scaled_ld;
+  uint32_t splits, vocab, token_bytes, dim;
+  const void* targets;
+  const float* weight;
+  const float* up;  // fp16: multiplies the weight; or nullptr
+  float k2;
+  float* loss;
+  void* to;  // G; or nullptr: the loss alone
+  const uint16_t* hidden;
+  uint16_t* scaled;
+  const Header* header;
+  int32_t* status;
+};
+constexpr uint32_t kHeld = 8;  // times four logits of a thread
+constexpr uint32_t kMostHeld = 256 * 4 * kHeld;
+template <int THREADS, bool MAX>
+__device__ __forceinline__ float over_row(float x, float* shared) {
+#pragma unroll
+  for (int d = 16; d; d /= 2) {
+    const float y = __shfl_xor_sync(kFull, x, d);
+    x = MAX ? fmaxf(x, y) : x + y;
+  }
+  if constexpr (THREADS > 32) {
+    if ((threadIdx.x & 31) == 0) shared[threadIdx.x / 32] = x;
+    __syncthreads();
+    x = shared[threadIdx.x % (THREADS / 32)];
+#pragma unroll
+    for (int d = THREADS / 64; d; d /= 2) {
+      const float y = __shfl_xor_sync(kFull, x, d);
+      x = MAX ? fmaxf(x, y) : x + y;
+    }
+  }
+  return x;
+}
+template <class T, int THREADS>
+__global__ void __launch_bounds__(256) k_head_softmax(const SoftmaxArgs a) {
+  pdl_enter();
+  if (a.to) let_next_in();  // else the last of the call
+  __shared__ float shared[2][8], at_target;
+  const uint64_t row = THREADS == 32 ? (uint64_t)blockIdx.x * 8 + threadIdx.x / 32 : blockIdx.x;
+  const uint32_t mine = threadIdx.x % THREADS;
+  if (row >= a.rows) return;
+  const int64_t word = target_of(a.targets, a.token_bytes, row);
+  const float weight = a.weight ? a.weight[row] : 1.0f;
+  uint32_t late = 0;
+  if (mine < 32)
+    for (uint32_t i = mine; i < kNumSM; i += 32) late |= a.header->late[i];
+  float z[kHeld][4] = {};
+  const float* const from = a.parts + row * a.ldz + mine * 4;
+  for (uint32_t k = 0; k < a.splits; ++k)
+#pragma unroll
+    for (uint32_t i = 0; i < kHeld; ++i) {
+      if (i * THREADS * 4 >= a.vocab) break;
+      if ((i * THREADS + mine) * 4 < a.vocab) {
+        const float4 x = *reinterpret_cast<const float4*>(from + k * a.split_stride + i * THREADS * 4);
+        z[i][0] += x.x, z[i][1] += x.y, z[i][2] += x.z, z[i][3] += x.w;
+      }
+    }
+  if (word >= (int64_t)a.vocab && a.status && mine == 0) set_status(a.status, CVLC_ERR_INVALID_ARG);
+  const bool there = word >= 0 && word < (int64_t)a.vocab && weight != 0.0f;
+  const uint32_t target = there ? (uint32_t)word : 0;
+  float most = -CUDART_INF_F, zt = 0.0f, o = 0.0f;
+#pragma unroll
+  for (uint32_t i = 0; i < kHeld; ++i) {
+    if (i * THREADS * 4 >= a.vocab) break;
+#pragma unroll
+    for (uint32_t k = 0; k < 4; ++k) {
+      const uint32_t col = (i * THREADS + mine) * 4 + k;
+      z[i][k] = col < a.vocab ? z[i][k] * a.k2 : -CUDART_INF_F;
+      most = fmaxf(most, z[i][k]);
+      if (col == target) zt = z[i][k], z[i][k] = -CUDART_INF_F;
+    }
+  }
+  if (THREADS > 32 && target / 4 % THREADS == mine) at_target = zt;
+  most = over_row<THREADS, true>(most, shared[0]);
+  zt = THREADS > 32 ? at_target : __shfl_sync(kFull, zt, target / 4 % 32);
+#pragma unroll
+  for (uint32_t i = 0; i < kHeld; ++i) {
+    if (i * THREADS * 4 >= a.vocab) break;
+#pragma unroll
+    for (uint32_t k = 0; k < 4; ++k) {
+      z[i][k] = exp2_fast(z[i][k] - most);
+      o += z[i][k];
+    }
+  }
+  o = over_row<THREADS, false>(o, shared[1]);
+  const float right = exp2f(zt - most), total = right + o, w = a.up ? weight * *a.up : weight, f = w / total, of_target = -(o / total) * w;
+  if (mine < 32 && __any_sync(kFull, late)) {
+    if (mine == 0) a.loss[row] = CUDART_NAN_F;
+  } else if (mine == 0) {
+    a.loss[row] = !there ? 0.0f : weight * (most == zt ? log1pf(o) : logf(total) + (most - zt) * kLn2);
+  }
+  if (!a.to) return;
+  T* const to = static_cast<T*>(a.to) + row * a.ldg + mine * 4;
+#pragma unroll
+  for (uint32_t i = 0; i < kHeld; ++i) {
+    if (i * THREADS * 4 >= a.vocab) break;
+    const uint32_t col = (i * THREADS + mine) * 4;
+    float g[4];
+#pragma unroll
+    for (uint32_t k = 0; k < 4; ++k) g[k] = !there ? 0.0f : col + k == target ? of_target : z[i][k] * f;
+    if (col < a.vocab) *reinterpret_cast<uint2*>(to + i * THREADS * 4) = make_uint2(pack2<T>(g[0], g[1]), pack2<T>(g[2], g[3]));
+  }
+  masked_row(a.hidden + row * a.hidden_ld, a.scaled + row * a.scaled_ld, a.dim, there, mine, THREADS);
+}
+
 // Exponentials that are kept relative to the maximum of their 128 columns become G: times exp(maximum - ln sum exp) and the weight.  In fp16 in their place; in fp32
 // (up to 128 rows, where their room is small) so that G is rounded once.  A warp a row, two times 128 columns at a time.
 struct RescaleArgs {
@@ -867,24 +982,30 @@ __global__ void __launch_bounds__(256) k_head_rescale(const RescaleArgs a) {
   }
 }
 
-struct JoinArgs {
+struct JoinJob {
   const float* parts;
   uint64_t split_stride, ldp, ldo;
   uint32_t splits, dim;
   uint64_t rows;
   float alpha;
   const float *factor, *down;  // of a row; of all; or nullptr
-  const Header* header;
   void* out;
 };
-// The parts of the hidden states' gradient added up in their order, four columns a thread; with many parts (few rows) eight threads share them.
+struct JoinArgs {
+  JoinJob of[2];
+  uint32_t blocks;  // of the first
+  const Header* header;
+};
+// The parts of the hidden states' gradient, and of the head's where it comes in parts, added up in their order, four columns a thread; with many parts (few rows) eight threads share them.
 template <class T, int SHARE>
-__global__ void __launch_bounds__(256) k_head_join(const JoinArgs a) {
+__global__ void __launch_bounds__(256) k_head_join(const JoinArgs all) {
   pdl_enter();
   __shared__ float4 share[SHARE > 1 ? 256 : 1];
-  const bool late = any_late(a.header);
+  const bool late = any_late(all.header);
+  const bool second = blockIdx.x >= all.blocks;
+  const JoinJob& a = all.of[second];
   const uint32_t per = (a.dim + 3) / 4, of = 256 / SHARE, mine = threadIdx.x / of;
-  const uint64_t i = (uint64_t)blockIdx.x * of + threadIdx.x % of, row = i / per;
+  const uint64_t i = (uint64_t)(blockIdx.x - (second ? all.blocks : 0)) * of + threadIdx.x % of, row = i / per;
   const uint32_t col = (uint32_t)(i - row * per) * 4;
   float4 s = make_float4(0, 0, 0, 0);
   if (row < a.rows) {
@@ -923,7 +1044,6 @@ bool on16(const void* p, uint64_t stride) { return reinterpret_cast<uintptr_t>(p
 uint32_t tiles(uint64_t n, uint32_t tile) { return (uint32_t)((n + tile - 1) / tile); }
 // Up to 128 rows a block has them all; above, a pair of blocks reads half as much of the other operand.
 bool by_pairs(uint64_t m) { return m > kTileM; }
-uint32_t tiles_m(uint64_t m) { return tiles(m, by_pairs(m) ? 2 * kTileM : kTileM); }
 
 // Rows that fit in one tile: the head is read once, by the SMs alike if its tiles come out even.
 uint32_t stats_tile(uint64_t m, uint32_t n) {
@@ -936,8 +1056,8 @@ uint32_t stats_tile(uint64_t m, uint32_t n) {
 }
 // In how many parts a sum is cut: as many as leave the SMs the least to do one behind the other.  A step of 64 takes 0.3 us, a part more costs its
 // writing and reading.
-uint32_t splits_of(uint64_t m, uint64_t n, uint32_t k_blocks) {
-  const uint64_t all = (uint64_t)tiles_m(m) * tiles(n, kTileN), at_once = by_pairs(m) ? kNumSM / 2 : kNumSM;
+uint32_t splits_of(uint64_t m, uint64_t n, uint32_t k_blocks, bool pairs) {
+  const uint64_t all = (uint64_t)tiles(m, pairs ? 2 * kTileM : kTileM) * tiles(n, kTileN), at_once = pairs ? kNumSM / 2 : kNumSM;
   const double more = (double)(m * n) * 8 / 6.4e6 / 0.3 + 0.1;
   uint32_t best = 1;
   double cost = 1e30;
@@ -948,19 +1068,38 @@ uint32_t splits_of(uint64_t m, uint64_t n, uint32_t k_blocks) {
   return best;
 }
 
+// Few logits, of which single blocks make tiles of any width: both at once.  A step takes 0.08 us and what it copies, a tile its reading and writing.
+void cut_few(uint64_t m, uint64_t n, uint32_t k_blocks, uint32_t* tile_n, uint32_t* splits) {
+  double cost = 1e30;
+  for (uint32_t t = kTileN; t >= 32; t -= 32)
+    for (uint32_t s = 1; s <= 32 && s <= k_blocks; ++s) {
+      const uint64_t waves = ((uint64_t)tiles(m, kTileM) * tiles(n, t) * s + kNumSM - 1) / kNumSM;
+      const double step = 0.08 + 0.0006 * ((m < kTileM ? m : kTileM) + t);
+      const double c = (double)waves * (((k_blocks + s - 1) / s) * step + 0.5 + 0.004 * t) + s * (0.05 + (double)(m * n) * 8 / 6.4e6);
+      if (c < cost * 0.99) cost = c, *tile_n = t, *splits = s;
+    }
+}
+
 // What becomes of the exponentials of the first product.  Several pieces: nothing, there is no room for them.  Up to 128 rows: kept in fp32.  bf16 has fp32's
 // range, and they are relative to the target's; fp16 has not, and they are relative to the maximum of 128 columns and gone over once more (777 x 1000 x
 // 50021: 27 us; multiplying again 103).
 constexpr uint64_t kLeastPiece = 1ull << 22;
-enum class Keep { kNot, kWide, kBf16, kFp16 };
+// Few logits go through the memory in 32 bits: nothing has to be known of a row before its logits are there, none gets a second turn, and sums are cut
+// wherever SMs are idle.  A step takes four launches instead of five (up to 128 rows) or eight: 149 x 624 x 56 39 -> 20 us, 5579 x 104 x 117 69 -> 25, 1518 x 1328 x
+// 3047 even; a loss two as before: 3420 x 3856 x 101 30 -> 15, even at a million logits, 2252 x 94 x 3405 21 -> 29.
+constexpr uint64_t kFewLogits = kLeastPiece, kFewOfLoss = 1ull << 20;
+enum class Keep { kNot, kFew, kWide, kBf16, kFp16 };
 struct HeadLayout {
   Keep keep;
+  bool pairs;              // in the gradients' products
   bool copy_hidden, copy_head;
   uint64_t ld;             // of copies
   uint32_t piece, pieces;  // words
   uint64_t ldg, ldp, stats_stride;
   uint32_t splits, slots, blocks_wild;
-  size_t off_hidden, off_head, off_scaled, off_stats, off_target, off_row, off_factor, off_raised, off_wild, off_g, off_wide, off_parts, total;
+  uint64_t ldz;  // few logits
+  uint32_t tile_z, splits_z, splits_head;
+  size_t off_z, off_head_parts, off_hidden, off_head, off_scaled, off_stats, off_target, off_row, off_factor, off_raised, off_wild, off_g, off_wide, off_parts, total;
 };
 HeadLayout head_layout(const cvlc_head& a, uint32_t pieces) {
   HeadLayout L = {};
@@ -971,7 +1110,9 @@ HeadLayout head_layout(const cvlc_head& a, uint32_t pieces) {
     L.pieces = tiles(a.vocab, L.piece);
     if (L.pieces == 1) L.piece = a.vocab;
   }
-  L.keep = L.pieces != 1 ? Keep::kNot : !by_pairs(a.rows) ? Keep::kWide : a.dtype == CVLC_BF16 ? Keep::kBf16 : Keep::kFp16;
+  const bool few = L.pieces <= 1 && a.vocab <= kMostHeld && a.rows * a.vocab <= (pieces ? kFewLogits : kFewOfLoss);
+  L.keep = few ? Keep::kFew : L.pieces != 1 ? Keep::kNot : !by_pairs(a.rows) ? Keep::kWide : a.dtype == CVLC_BF16 ? Keep::kBf16 : Keep::kFp16;
+  L.pairs = !few && by_pairs(a.rows);
   // copied where they do not begin on 16 bytes, or where rows that count for nothing have to become zeros first
   L.copy_hidden = !on16(a.hidden_dev, a.hidden_stride) || (pieces && (L.keep == Keep::kNot || L.keep == Keep::kFp16));
   L.copy_head = !on16(a.head_dev, a.head_stride);
@@ -981,13 +1122,22 @@ HeadLayout head_layout(const cvlc_head& a, uint32_t pieces) {
   auto take = [&](size_t bytes) { const size_t from = at; at = align256(at + bytes); return from; };
   L.off_hidden = take(L.copy_hidden ? a.rows * L.ld * 2 : 0);
   L.off_head = take(L.copy_head ? a.vocab * L.ld * 2 : 0);
-  L.slots = 2 * tiles(a.vocab, stats_tile(a.rows, a.vocab));
-  L.off_stats = take((size_t)L.slots * L.stats_stride * 8);
-  L.off_target = take(a.rows * 4);
+  if (few) {
+    L.ldz = (uint64_t)tiles(a.vocab, 32) * 32;
+    cut_few(a.rows, a.vocab, tiles(a.dim, kTileK), &L.tile_z, &L.splits_z);
+    L.off_z = take((size_t)L.splits_z * a.rows * L.ldz * 4);
+  } else {
+    L.slots = 2 * tiles(a.vocab, stats_tile(a.rows, a.vocab));
+    L.off_stats = take((size_t)L.slots * L.stats_stride * 8);
+    L.off_target = take(a.rows * 4);
+  }
   if (pieces) {
     L.ldg = (uint64_t)tiles(L.piece, 32) * 32;
     L.ldp = (a.dim + 31) / 32 * 32;
-    L.splits = splits_of(a.rows, a.dim, tiles(L.piece, kTileK));
+    L.splits = splits_of(a.rows, a.dim, tiles(L.piece, kTileK), L.pairs);
+    // of few words and many rows the head's gradient has few tiles and long sums (7094 x 144 x 83: 79 -> 34 us)
+    L.splits_head = few ? splits_of(a.vocab, a.dim, tiles(a.rows, kTileK), false) : 1;
+    if (L.splits_head > 1) L.off_head_parts = take((size_t)L.splits_head * a.vocab * L.ldp * 4);
     L.off_g = take(a.rows * L.ldg * 2);
     L.off_parts = take((size_t)L.splits * a.rows * L.ldp * 4);
     if (L.keep == Keep::kBf16) {
@@ -996,13 +1146,11 @@ HeadLayout head_layout(const cvlc_head& a, uint32_t pieces) {
       L.off_factor = take(a.rows * 4);
       L.off_raised = take(a.rows * 4);
       L.off_wild = take(L.blocks_wild * 4);
-    } else {
+    } else if (!few) {
       L.off_row = take(a.rows * 16);
     }
-    if (L.keep == Keep::kWide) {
-      L.off_scaled = take(a.rows * L.ld * 2);
-      L.off_wide = take(a.rows * L.ldg * 4);
-    }
+    if (few || L.keep == Keep::kWide) L.off_scaled = take(a.rows * L.ld * 2);
+    if (L.keep == Keep::kWide) L.off_wide = take(a.rows * L.ldg * 4);
   }
   L.total = at;
   return L;
@@ -1152,16 +1300,17 @@ struct HeadRun {
   // of the sum each, one launch makes both (16 x 1024 x 32000: 52 -> 30 us); by pairs, two do (8192 x 4096 x 131072: 13.7 ms, 15.2 in one).
   void gradients(uint32_t from, uint32_t words, const Operand& hidden_scaled, const Gradients& to, const float* down) {
     const Operand g = {base + L.off_g, words, a.rows, L.ldg}, piece = {static_cast<const T*>(head.at) + (uint64_t)from * head.ld, a.dim, words, head.ld};
-    const bool pairs = by_pairs(a.rows);
+    const bool pairs = L.pairs;
     Product p = product();
     p.m = (uint32_t)a.rows, p.n = a.dim, p.k_blocks = tiles(words, kTileK);
     p.splits = L.splits <= p.k_blocks ? L.splits : p.k_blocks;
     p.out = base + L.off_parts, p.ldo = L.ldp, p.split_stride = a.rows * L.ldp, p.add = from != 0;
     Product q = product();
-    q.m = words, q.n = a.dim, q.k_blocks = tiles(a.rows, kTileK);
+    q.m = words, q.n = a.dim, q.k_blocks = tiles(a.rows, kTileK), q.splits = L.splits_head;
     T* const out = static_cast<T*>(to.d_head) + (uint64_t)from * to.d_head_stride;
     q.out = out, q.ldo = to.d_head_stride, q.wide = on16(out, to.d_head_stride) && a.dim % 8 == 0;  // a box writes whole vectors of 16 bytes: what lies behind a row's end with them, too
     q.alpha_dev = down;
+    if (q.splits > 1) q.out = base + L.off_head_parts, q.ldo = L.ldp, q.split_stride = words * L.ldp, q.wide = 0;
     const bool fits = make_product(p, bf16, pairs, g, false, piece, true, false) && make_product(q, bf16, pairs, g, true, hidden_scaled, true, q.wide);
     if (pairs) {
       run_product<kParts, false, true, 2>(kKHeadParts, {{p}}, fits);
@@ -1173,11 +1322,43 @@ struct HeadRun {
   }
   void join(const Gradients& to, const float* factor, const float* down) {
     JoinArgs j = {};
-    j.parts = at<float>(L.off_parts), j.split_stride = a.rows * L.ldp, j.ldp = L.ldp, j.ldo = to.d_hidden_stride;
-    j.splits = L.splits, j.dim = a.dim, j.rows = a.rows, j.alpha = a.scale, j.factor = factor, j.down = down, j.header = header, j.out = to.d_hidden;
-    const uint64_t quads = a.rows * ((a.dim + 3) / 4);
-    if (L.splits >= 8 && quads <= 32768) launch(kKHeadJoin, k_head_join<T, 8>, (uint32_t)((quads + 31) / 32), 256, j);
-    else launch(kKHeadJoin, k_head_join<T, 1>, (uint32_t)((quads + 255) / 256), 256, j);
+    uint64_t quads[2] = {};
+    auto add = [&](uint32_t i, size_t parts, uint32_t splits, uint64_t rows, void* out, uint64_t stride) {
+      JoinJob& x = j.of[i];
+      x.parts = at<float>(parts), x.split_stride = rows * L.ldp, x.ldp = L.ldp, x.ldo = stride, x.splits = splits, x.dim = a.dim, x.rows = rows, x.alpha = a.scale;
+      x.factor = factor, x.down = down, x.out = out, quads[i] = rows * ((a.dim + 3) / 4);
+    };
+    add(0, L.off_parts, L.splits, a.rows, to.d_hidden, to.d_hidden_stride);
+    if (L.splits_head > 1) add(1, L.off_head_parts, L.splits_head, a.vocab, to.d_head, to.d_head_stride);
+    j.header = header;
+    const bool shared = (L.splits >= 8 || L.splits_head >= 8) && quads[0] + quads[1] <= 32768;
+    const uint32_t of = shared ? 32 : 256;
+    j.blocks = (uint32_t)((quads[0] + of - 1) / of);
+    const uint32_t blocks = j.blocks + (uint32_t)((quads[1] + of - 1) / of);
+    if (shared) launch(kKHeadJoin, k_head_join<T, 8>, blocks, 256, j);
+    else launch(kKHeadJoin, k_head_join<T, 1>, blocks, 256, j);
+  }
+  void begin() {
+    launch(kKHeadBegin, k_head_begin, 1, a.rows > 256 ? 1024 : 256, header, a.row_weight_dev, a.targets_dev, a.token_bytes, a.rows, a.vocab);
+  }
+  void run_few(float* loss, const Gradients* to) {
+    if (to && !bf16) begin();
+    Product p = product();
+    p.m = (uint32_t)a.rows, p.n = a.vocab, p.k_blocks = tiles(a.dim, kTileK), p.first = 1, p.tile_n = L.tile_z, p.splits = L.splits_z;
+    p.out = base + L.off_z, p.ldo = L.ldz, p.split_stride = a.rows * L.ldz;
+    const bool fits = make_product(p, bf16, false, hidden, false, head, false, false);
+    run_product<kParts, false, false, 1>(kKHeadLogits, {{p}}, fits);
+    SoftmaxArgs r = {};
+    r.parts = at<float>(L.off_z), r.split_stride = p.split_stride, r.ldz = L.ldz, r.rows = a.rows, r.ldg = L.ldg, r.hidden_ld = hidden.ld, r.scaled_ld = L.ld;
+    r.splits = L.splits_z, r.vocab = a.vocab, r.token_bytes = a.token_bytes, r.dim = a.dim, r.targets = a.targets_dev, r.weight = a.row_weight_dev;
+    r.up = to && !bf16 ? &header->up : nullptr, r.k2 = p.k2, r.loss = loss, r.to = to ? base + L.off_g : nullptr;
+    r.hidden = static_cast<const uint16_t*>(hidden.at), r.scaled = at<uint16_t>(L.off_scaled), r.header = header, r.status = a.status_dev;
+    if (a.vocab <= 1024) launch(kKHeadSoftmax, k_head_softmax<T, 32>, tiles(a.rows, 8), 256, r);
+    else launch(kKHeadSoftmax, k_head_softmax<T, 256>, (uint32_t)a.rows, 256, r);
+    if (!to) return;
+    const float* const down = bf16 ? nullptr : &header->down;
+    gradients(0, a.vocab, {base + L.off_scaled, a.dim, a.rows, L.ld}, *to, down);
+    join(*to, nullptr, down);
   }
   void run_kept(float* loss, const Gradients& to) {
     TargetArgs t = {};
@@ -1201,7 +1382,7 @@ struct HeadRun {
     join(to, at<float>(L.off_factor), nullptr);
   }
   void run_pieces(float* loss, const Gradients& to) {
-    if (!bf16) launch(kKHeadBegin, k_head_begin, 1, a.rows > 256 ? 1024 : 256, header, a.row_weight_dev, a.targets_dev, a.token_bytes, a.rows, a.vocab);
+    if (!bf16) begin();
     if (L.copy_hidden) copy(hidden, L.off_hidden, L.keep == Keep::kWide ? nullptr : a.targets_dev);
     if (L.copy_head) copy(head, L.off_head, nullptr);
     logits_once(loss, true);
@@ -1223,11 +1404,12 @@ struct HeadRun {
     join(to, nullptr, down);
   }
   cudaError_t run(float* loss, const Gradients* to) {
-    if (!to || L.keep == Keep::kBf16) {
+    if (!to || L.keep == Keep::kBf16 || L.keep == Keep::kFew) {
       if (L.copy_hidden) copy(hidden, L.off_hidden, nullptr);
       if (L.copy_head) copy(head, L.off_head, nullptr);
     }
-    if (!to) logits_once(loss, false);
+    if (L.keep == Keep::kFew) run_few(loss, to);
+    else if (!to) logits_once(loss, false);
     else if (L.keep == Keep::kBf16) run_kept(loss, *to);
     else run_pieces(loss, *to);
     return error != cudaSuccess ? error : cudaGetLastError();

@@ -13,7 +13,7 @@ const char* const kKernelNames[kNumKernelIds] = {
     "k_selftest", "k_hist_check", "k_apply", "k_plan_literal", "k_ec_accumulate", "k_pack_unframed", "k_decode_unframed",
     "k_top_logits", "k_distill_loss", "k_distill_grad", "k_distill_step", "k_embed", "k_token_sort", "k_embed_sum", "k_embed_join",
     "k_adamw", "k_norm_parts", "k_norm_join",
-    "k_head_begin", "k_head_align", "k_head_target", "k_head_keep", "k_head_stats", "k_head_rows", "k_head_probs", "k_head_rescale", "k_head_parts", "k_head_grad", "k_head_grads", "k_head_join"};
+    "k_head_begin", "k_head_align", "k_head_logits", "k_head_softmax", "k_head_target", "k_head_keep", "k_head_stats", "k_head_rows", "k_head_probs", "k_head_rescale", "k_head_parts", "k_head_grad", "k_head_grads", "k_head_join"};
 
 std::atomic<unsigned long long> g_launches[kNumKernelIds];
 std::atomic<int> g_prof_kernel{-1};  // kernel id being timed; kNumKernelIds = every kernel; -1 = off

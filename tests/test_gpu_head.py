@@ -305,3 +305,103 @@ def test_gradients_by_differences():
         name = "d_hidden" if x is hidden else "d_head"
         left_out = float((e["loss"] - f["loss"]).sum() - (moved * (e[name] + f[name]) / 2).sum())
         assert abs(float(a[1].double().sum() - b[1].double().sum()) - predicted - left_out) <= 2.0 ** -8 * float(terms.norm()) * 3
+
+
+# ---- more than 8192 words: the logits are not held, whatever their number ----
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("rows", [1, 2, 16, 127, 129, 257])
+@pytest.mark.parametrize("dim,vocab,pad,shift", [(1, 8193, 0, 0), (8, 8448, 8, 0), (63, 8449, 1, 0), (65, 8703, 0, 3), (264, 9003, 0, 8), (200, 8200, 5, 3)])
+def test_many_words(dtype, rows, dim, vocab, pad, shift):
+    check(*make(rows, dim, vocab, dtype, pad, shift, wide=rows % 2 == 0), pad=pad, shift=shift)
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("rows", [120, 333])
+def test_many_words_weights_masks_and_scale(dtype, rows):
+    hidden, head, t = make(rows, 96, 8300, dtype, pad=8)
+    g = torch.Generator(device="cuda").manual_seed(7)
+    weight = torch.rand(rows, generator=g, device="cuda") * 1e-3 - 2e-4
+    weight[::7] = 0
+    t[::5] = -1
+    hidden[0], hidden[5] = float("nan"), float("inf")
+    loss, dh, _ = check(hidden, head, t, scale=0.7, weight=weight)
+    assert not bool(loss[::7].any()) and not bool(dh[::5].any())
+    loss, dh, _ = check(hidden, head, t, scale=-0.7, weight=weight)
+    weight[:] = 0
+    _, loss, dh, dw = run(hidden, head, t, weight=weight)
+    assert not any(bool(x.any()) for x in (loss, dh, dw))
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("rows", [3, 128, 129, 700])
+def test_many_words_far_logits(dtype, rows):
+    """some word 2^60 times and more as likely as the target, in single rows, next to others of the same tiles and of others"""
+    hidden, head, t = make(rows, 64, 8200, dtype, width=8.0)
+    weight = torch.rand(rows, generator=torch.Generator(device="cuda").manual_seed(48), device="cuda")
+    for i in {0, rows // 2, rows - 1}:
+        hidden[i] = (-25 * head[t[i]].float()).to(dtype)
+    hidden[1] = (3 * head[t[1]].float()).to(dtype)
+    loss, _, _ = check(hidden, head, t, scale=0.9, weight=weight)
+    assert int((loss > 60 * weight).sum()) >= 1
+    t[0] = -1
+    check(hidden, head, t, scale=0.9, weight=weight)
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("rows", [140, 100])
+def test_many_words_not_finite(dtype, rows):
+    hidden, head, t = make(rows, 64, 8300, dtype)
+    good = [x.clone() for x in run(hidden, head, t)]
+    hidden[3, 5] = float("nan")
+    alone, loss, dh, dw = run(hidden, head, t)
+    others = torch.arange(rows, device="cuda") != 3
+    assert bool(torch.isnan(loss[3])) and bool(torch.isnan(alone[3])) and bool(torch.isnan(dh[3]).all()) and bool(torch.isnan(dw).all(dim=1).all())
+    assert torch.equal(loss[others], good[1][others]) and torch.equal(dh[others], good[2][others])
+
+
+@pytest.mark.parametrize("rows", [100, 200])
+def test_many_words_in_a_graph(rows):
+    hidden, head, t = make(rows, 64, 8300)
+    loss, dh, dw, ws = torch.zeros(rows, device="cuda"), torch.zeros_like(hidden), torch.zeros_like(head), space(hidden, head, 1)
+    stream, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        B.cvlc_head_step(hidden, head, t, loss, dh, dw, ws, stream=stream)
+    for seed in (3, 4):
+        for x, y in zip((hidden, head, t), make(rows, 64, 8300, seed=seed)):
+            x.copy_(y)
+        graph.replay()
+        torch.cuda.synchronize()
+        want = run(hidden, head, t)
+        assert torch.equal(loss, want[1]) and torch.equal(dh, want[2]) and torch.equal(dw, want[3])
+
+
+# ---- few logits: where warps, blocks, parts of sums and what is held end ----
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("rows,dim,vocab", [(1, 5000, 3), (7, 4096, 32), (129, 2049, 33), (40, 640, 127), (9, 72, 1023), (9, 72, 1024), (9, 72, 1025), (3, 640, 2049),
+                                            (500, 64, 8191), (512, 64, 8192), (513, 64, 8192), (127, 64, 8193), (4096, 72, 1024), (4097, 72, 1024), (1024, 64, 1024),
+                                            (1025, 64, 1024), (30000, 24, 10), (65000, 16, 64), (2000, 2048, 70), (700, 1000, 1000)])
+def test_few_logits(dtype, rows, dim, vocab):
+    check(*make(rows, dim, vocab, dtype, seed=rows))
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("rows,dim,vocab", [(5000, 40, 12), (300, 88, 2000)])
+def test_few_logits_weights_masks_and_strides(dtype, rows, dim, vocab):
+    hidden, head, t = make(rows, dim, vocab, dtype, pad=11, shift=3)
+    weight = torch.rand(rows, generator=torch.Generator(device="cuda").manual_seed(5), device="cuda") * 8 - 2
+    weight[::6], t[::5] = 0, -7
+    hidden[0], hidden[6] = float("nan"), float("-inf")
+    loss, dh, _ = check(hidden, head, t, scale=1.3, weight=weight, pad=11, shift=3)
+    assert not bool(loss[::5].any()) and not bool(dh[::6].any())
+
+
+@pytest.mark.parametrize("rows,dim,vocab,pad", [(5000, 41, 12, 7), (5000, 40, 12, 8), (60, 33, 700, 1)])
+def test_few_logits_leave_what_lies_between_the_rows(rows, dim, vocab, pad):
+    hidden, head, t = make(rows, dim, vocab, pad=pad)
+    room = [torch.full((x.shape[0], dim + pad), 7.0, dtype=BF, device="cuda") for x in (hidden, head)]
+    loss = torch.full((rows + 8,), 7.0, device="cuda")
+    B.cvlc_head_step(hidden, head, t, loss[:rows], room[0][:, :dim], room[1][:, :dim], space(hidden, head, 1))
+    R.check(loss[:rows], room[0][:, :dim], room[1][:, :dim], hidden, head, t)
+    assert all(bool((r[:, dim:] == 7.0).all()) for r in room) and bool((loss[rows:] == 7.0).all())
