@@ -550,19 +550,32 @@ __global__ void __launch_bounds__(1024) k_head_begin(Header* h, const float* wei
 
 // Rows of any alignment, copied to rows on 16 bytes, a warp each.  Rows that count for nothing become zeros: their values, which may be no numbers, have a part
 // in the products of others' gradients.
-__global__ void __launch_bounds__(256) k_head_align(const uint16_t* from, uint64_t from_stride, uint16_t* to, uint64_t to_stride, uint64_t rows, uint32_t dim,
-                                                    const void* targets, uint32_t token_bytes, uint32_t vocab, const float* weight) {
+struct AlignJob {
+  const uint16_t* from;
+  uint16_t* to;
+  uint64_t from_stride, to_stride, rows;
+  const void* targets;  // or nullptr: all rows count
+};
+struct AlignArgs {
+  AlignJob of[2];
+  uint32_t blocks;  // of the first
+  uint32_t dim, token_bytes, vocab;
+  const float* weight;
+};
+__global__ void __launch_bounds__(256) k_head_align(const __grid_constant__ AlignArgs all) {
   pdl_enter();
   let_next_in();
-  const uint64_t row = (uint64_t)blockIdx.x * 8 + threadIdx.x / 32;
-  const uint32_t lane = threadIdx.x & 31;
-  if (row >= rows) return;
-  const uint16_t* const src = from + row * from_stride;
-  uint16_t* const dst = to + row * to_stride;
+  const bool second = blockIdx.x >= all.blocks;
+  const AlignJob& a = all.of[second];
+  const uint64_t row = (uint64_t)(blockIdx.x - (second ? all.blocks : 0)) * 8 + threadIdx.x / 32;
+  const uint32_t lane = threadIdx.x & 31, dim = all.dim;
+  if (row >= a.rows) return;
+  const uint16_t* const src = a.from + row * a.from_stride;
+  uint16_t* const dst = a.to + row * a.to_stride;
   bool counts = true;
-  if (targets) {
-    const int64_t t = target_of(targets, token_bytes, row);
-    counts = t >= 0 && t < (int64_t)vocab && !(weight && weight[row] == 0.0f);
+  if (a.targets) {
+    const int64_t t = target_of(a.targets, all.token_bytes, row);
+    counts = t >= 0 && t < (int64_t)all.vocab && !(all.weight && all.weight[row] == 0.0f);
   }
   // rows that begin anywhere are read by the two vectors that hold eight elements
   const uint32_t lead = (uint32_t)(reinterpret_cast<uintptr_t>(src) % 16 / 2);
@@ -998,7 +1011,7 @@ struct JoinArgs {
 };
 // The parts of the hidden states' gradient, and of the head's where it comes in parts, added up in their order, four columns a thread; with many parts (few rows) eight threads share them.
 template <class T, int SHARE>
-__global__ void __launch_bounds__(256) k_head_join(const JoinArgs all) {
+__global__ void __launch_bounds__(256) k_head_join(const __grid_constant__ JoinArgs all) {
   pdl_enter();
   __shared__ float4 share[SHARE > 1 ? 256 : 1];
   const bool late = any_late(all.header);
@@ -1259,10 +1272,20 @@ struct HeadRun {
     if constexpr (EPI != kKeep && EPI != kKeepOwn)
       if (!pairs) run_product<EPI, false, false, 1>(id, {{p}}, fits);
   }
-  void copy(Operand& x, size_t off, const void* targets) {
-    launch(kKHeadAlign, k_head_align, tiles(x.rows, 8), 256, static_cast<const uint16_t*>(x.at), x.ld, at<uint16_t>(off), L.ld, x.rows, a.dim, targets,
-           a.token_bytes, a.vocab, a.row_weight_dev);
-    x.at = base + off, x.ld = L.ld;
+  // the copies of rows that do not lie on 16 bytes, or (targets) of those that may not count
+  void copies(const void* targets) {
+    AlignArgs r = {};
+    uint32_t n = 0, blocks = 0;
+    auto add = [&](Operand& x, size_t off, const void* t) {
+      r.of[n++] = {static_cast<const uint16_t*>(x.at), at<uint16_t>(off), x.ld, L.ld, x.rows, t};
+      if (n == 1) r.blocks = tiles(x.rows, 8);
+      blocks += tiles(x.rows, 8);
+      x.at = base + off, x.ld = L.ld;
+    };
+    if (L.copy_hidden) add(hidden, L.off_hidden, targets);
+    if (L.copy_head) add(head, L.off_head, nullptr);
+    r.dim = a.dim, r.token_bytes = a.token_bytes, r.vocab = a.vocab, r.weight = a.row_weight_dev;
+    if (n) launch(kKHeadAlign, k_head_align, blocks, 256, r);
   }
   RowsArgs rows(float* loss) const {
     RowsArgs r = {};
@@ -1383,8 +1406,7 @@ struct HeadRun {
   }
   void run_pieces(float* loss, const Gradients& to) {
     if (!bf16) begin();
-    if (L.copy_hidden) copy(hidden, L.off_hidden, L.keep == Keep::kWide ? nullptr : a.targets_dev);
-    if (L.copy_head) copy(head, L.off_head, nullptr);
+    copies(L.keep == Keep::kWide ? nullptr : a.targets_dev);
     logits_once(loss, true);
     if (L.keep == Keep::kWide) rescale<float>(L.off_wide);
     else if constexpr (!bf16)
@@ -1404,10 +1426,7 @@ struct HeadRun {
     join(to, nullptr, down);
   }
   cudaError_t run(float* loss, const Gradients* to) {
-    if (!to || L.keep == Keep::kBf16 || L.keep == Keep::kFew) {
-      if (L.copy_hidden) copy(hidden, L.off_hidden, nullptr);
-      if (L.copy_head) copy(head, L.off_head, nullptr);
-    }
+    if (!to || L.keep == Keep::kBf16 || L.keep == Keep::kFew) copies(nullptr);
     if (L.keep == Keep::kFew) run_few(loss, to);
     else if (!to) logits_once(loss, false);
     else if (L.keep == Keep::kBf16) run_kept(loss, *to);
