@@ -524,7 +524,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_head_product(const __grid_const
 
 // ---- what is around them -------------------------------------------------------------------
 
-// One block, fp16 only: the power of two by which G is held.  fp16 holds 2^-24 to 2^16; G, at most the largest weight in size, is held at most 2^15.
+// One block, fp16 with weights only: the power of two by which G is held.  fp16 holds 2^-24 to 2^16; G, at most the largest weight in size, is held at most 2^15.
 __global__ void __launch_bounds__(1024) k_head_begin(Header* h, const float* weight, const void* targets, uint32_t token_bytes, uint64_t rows, uint32_t vocab) {
   pdl_enter();
   let_next_in();
@@ -532,18 +532,16 @@ __global__ void __launch_bounds__(1024) k_head_begin(Header* h, const float* wei
   if (threadIdx.x == 0) most = 0;
   __syncthreads();
   uint32_t m = 0;
-  if (weight) {
-    for (uint64_t i = threadIdx.x; i < rows; i += blockDim.x) {
-      const int64_t t = target_of(targets, token_bytes, i);
-      const uint32_t w = __float_as_uint(weight[i]) & 0x7FFFFFFFu;
-      if (t >= 0 && t < (int64_t)vocab && w < 0x7F800000u) m = max(m, w);
-    }
-    m = __reduce_max_sync(kFull, m);
-    if ((threadIdx.x & 31) == 0) atomicMax(&most, m);
-    __syncthreads();
+  for (uint64_t i = threadIdx.x; i < rows; i += blockDim.x) {
+    const int64_t t = target_of(targets, token_bytes, i);
+    const uint32_t w = __float_as_uint(weight[i]) & 0x7FFFFFFFu;
+    if (t >= 0 && t < (int64_t)vocab && w < 0x7F800000u) m = max(m, w);
   }
+  m = __reduce_max_sync(kFull, m);
+  if ((threadIdx.x & 31) == 0) atomicMax(&most, m);
+  __syncthreads();
   if (threadIdx.x == 0) {
-    const int e = (weight && most ? min(max((int)(most >> 23) - 126, -100), 100) : 0) - 15;
+    const int e = (most ? min(max((int)(most >> 23) - 126, -100), 100) : 0) - 15;
     h->up = exp2f((float)-e), h->down = exp2f((float)e);
   }
 }
@@ -662,7 +660,8 @@ struct RowsArgs {
   Header* header;
   uint64_t rows;
   int32_t* status;
-  uint32_t half;  // fp16
+  const float* up;  // multiplies the weight, or nullptr: up_by does
+  float up_by;
   // where the exponentials are kept:
   __nv_bfloat16* kept;
   uint64_t ldg, hidden_ld, scaled_ld;
@@ -748,7 +747,7 @@ __global__ void __launch_bounds__(256) k_head_rows(const RowsArgs a) {
       double others = 0.0;
       for (uint32_t i = 0; i < 8; ++i)
         if (part[i][lane].x != -CUDART_INF_F || part[i][lane].y != 0.0f) others += (double)(part[i][lane].y * exp2f(part[i][lane].x - most));
-      const float o = (float)others, right = exp2f(zt - most), total = right + o, w = a.half ? weight * a.header->up : weight;
+      const float o = (float)others, right = exp2f(zt - most), total = right + o, w = weight * (a.up ? *a.up : a.up_by);
       loss = weight * (most == zt ? log1pf(o) : logf(total) + (most - zt) * kLn2);
       r = make_float4(most + log2f(total), w, -(o / total) * w, 0.0f);
     }
@@ -848,8 +847,8 @@ struct SoftmaxArgs {
   uint32_t splits, vocab, token_bytes, dim;
   const void* targets;
   const float* weight;
-  const float* up;  // fp16: multiplies the weight; or nullptr
-  float k2;
+  const float* up;  // multiplies the weight, or nullptr: up_by does
+  float up_by, k2;
   float* loss;
   void* to;  // G; or nullptr: the loss alone
   const uint16_t* hidden;
@@ -930,7 +929,7 @@ __global__ void __launch_bounds__(256) k_head_softmax(const SoftmaxArgs a) {
     }
   }
   o = over_row<THREADS, false>(o, shared[1]);
-  const float right = exp2f(zt - most), total = right + o, w = a.up ? weight * *a.up : weight, f = w / total, of_target = -(o / total) * w;
+  const float right = exp2f(zt - most), total = right + o, w = weight * (a.up ? *a.up : a.up_by), f = w / total, of_target = -(o / total) * w;
   if (mine < 32 && __any_sync(kFull, late)) {
     if (mine == 0) a.loss[row] = CUDART_NAN_F;
   } else if (mine == 0) {
@@ -1305,7 +1304,7 @@ struct HeadRun {
     else if (!graded || L.keep == Keep::kNot) multiply<kStats>(kKHeadStats, p, head);
     else if constexpr (!bf16) multiply<kKeepOwn>(kKHeadKeep, p, head);
     RowsArgs r = rows(loss);
-    r.row = graded ? at<float4>(L.off_row) : nullptr, r.half = !bf16;
+    r.row = graded ? at<float4>(L.off_row) : nullptr, r.up = graded ? up() : nullptr, r.up_by = up_by();
     if (graded && L.keep == Keep::kWide)
       r.hidden = static_cast<const __nv_bfloat16*>(hidden.at), r.hidden_ld = hidden.ld, r.scaled = at<__nv_bfloat16>(L.off_scaled), r.scaled_ld = L.ld, r.dim = a.dim;
     launch(kKHeadRows, k_head_rows, row_blocks(), 256, r);
@@ -1321,7 +1320,7 @@ struct HeadRun {
   }
   // The part of a piece of the words in both gradients.  Up to 128 rows, where the hidden states' gradient has few tiles and the head's tiles are one step
   // of the sum each, one launch makes both (16 x 1024 x 32000: 52 -> 30 us); by pairs, two do (8192 x 4096 x 131072: 13.7 ms, 15.2 in one).
-  void gradients(uint32_t from, uint32_t words, const Operand& hidden_scaled, const Gradients& to, const float* down) {
+  void gradients(uint32_t from, uint32_t words, const Operand& hidden_scaled, const Gradients& to) {
     const Operand g = {base + L.off_g, words, a.rows, L.ldg}, piece = {static_cast<const T*>(head.at) + (uint64_t)from * head.ld, a.dim, words, head.ld};
     const bool pairs = L.pairs;
     Product p = product();
@@ -1332,7 +1331,7 @@ struct HeadRun {
     q.m = words, q.n = a.dim, q.k_blocks = tiles(a.rows, kTileK), q.splits = L.splits_head;
     T* const out = static_cast<T*>(to.d_head) + (uint64_t)from * to.d_head_stride;
     q.out = out, q.ldo = to.d_head_stride, q.wide = on16(out, to.d_head_stride) && a.dim % 8 == 0;  // a box writes whole vectors of 16 bytes: what lies behind a row's end with them, too
-    q.alpha_dev = down;
+    q.alpha = a.scale * down_by(), q.alpha_dev = down();
     if (q.splits > 1) q.out = base + L.off_head_parts, q.ldo = L.ldp, q.split_stride = words * L.ldp, q.wide = 0;
     const bool fits = make_product(p, bf16, pairs, g, false, piece, true, false) && make_product(q, bf16, pairs, g, true, hidden_scaled, true, q.wide);
     if (pairs) {
@@ -1343,13 +1342,13 @@ struct HeadRun {
       run_product<kBoth, false, true, 1>(kKHeadGrads, {{p, q}}, fits);
     }
   }
-  void join(const Gradients& to, const float* factor, const float* down) {
+  void join(const Gradients& to, const float* factor) {
     JoinArgs j = {};
     uint64_t quads[2] = {};
     auto add = [&](uint32_t i, size_t parts, uint32_t splits, uint64_t rows, void* out, uint64_t stride) {
       JoinJob& x = j.of[i];
-      x.parts = at<float>(parts), x.split_stride = rows * L.ldp, x.ldp = L.ldp, x.ldo = stride, x.splits = splits, x.dim = a.dim, x.rows = rows, x.alpha = a.scale;
-      x.factor = factor, x.down = down, x.out = out, quads[i] = rows * ((a.dim + 3) / 4);
+      x.parts = at<float>(parts), x.split_stride = rows * L.ldp, x.ldp = L.ldp, x.ldo = stride, x.splits = splits, x.dim = a.dim, x.rows = rows, x.alpha = a.scale * down_by();
+      x.factor = factor, x.down = down(), x.out = out, quads[i] = rows * ((a.dim + 3) / 4);
     };
     add(0, L.off_parts, L.splits, a.rows, to.d_hidden, to.d_hidden_stride);
     if (L.splits_head > 1) add(1, L.off_head_parts, L.splits_head, a.vocab, to.d_head, to.d_head_stride);
@@ -1361,11 +1360,17 @@ struct HeadRun {
     if (shared) launch(kKHeadJoin, k_head_join<T, 8>, blocks, 256, j);
     else launch(kKHeadJoin, k_head_join<T, 1>, blocks, 256, j);
   }
+  // fp16: by how much G is raised, known beforehand where no row has a weight
+  bool weighed() const { return !bf16 && a.row_weight_dev; }
+  const float* up() const { return weighed() ? &header->up : nullptr; }
+  const float* down() const { return weighed() ? &header->down : nullptr; }
+  static constexpr float up_by() { return bf16 ? 1.0f : 0x1p15f; }
+  float down_by() const { return bf16 || weighed() ? 1.0f : 0x1p-15f; }
   void begin() {
-    launch(kKHeadBegin, k_head_begin, 1, a.rows > 256 ? 1024 : 256, header, a.row_weight_dev, a.targets_dev, a.token_bytes, a.rows, a.vocab);
+    if (weighed()) launch(kKHeadBegin, k_head_begin, 1, a.rows > 256 ? 1024 : 256, header, a.row_weight_dev, a.targets_dev, a.token_bytes, a.rows, a.vocab);
   }
   void run_few(float* loss, const Gradients* to) {
-    if (to && !bf16) begin();
+    if (to) begin();
     Product p = product();
     p.m = (uint32_t)a.rows, p.n = a.vocab, p.k_blocks = tiles(a.dim, kTileK), p.first = 1, p.tile_n = L.tile_z, p.splits = L.splits_z;
     p.out = base + L.off_z, p.ldo = L.ldz, p.split_stride = a.rows * L.ldz;
@@ -1374,14 +1379,13 @@ struct HeadRun {
     SoftmaxArgs r = {};
     r.parts = at<float>(L.off_z), r.split_stride = p.split_stride, r.ldz = L.ldz, r.rows = a.rows, r.ldg = L.ldg, r.hidden_ld = hidden.ld, r.scaled_ld = L.ld;
     r.splits = L.splits_z, r.vocab = a.vocab, r.token_bytes = a.token_bytes, r.dim = a.dim, r.targets = a.targets_dev, r.weight = a.row_weight_dev;
-    r.up = to && !bf16 ? &header->up : nullptr, r.k2 = p.k2, r.loss = loss, r.to = to ? base + L.off_g : nullptr;
+    r.up = to ? up() : nullptr, r.up_by = up_by(), r.k2 = p.k2, r.loss = loss, r.to = to ? base + L.off_g : nullptr;
     r.hidden = static_cast<const uint16_t*>(hidden.at), r.scaled = at<uint16_t>(L.off_scaled), r.header = header, r.status = a.status_dev;
     if (a.vocab <= 1024) launch(kKHeadSoftmax, k_head_softmax<T, 32>, tiles(a.rows, 8), 256, r);
     else launch(kKHeadSoftmax, k_head_softmax<T, 256>, (uint32_t)a.rows, 256, r);
     if (!to) return;
-    const float* const down = bf16 ? nullptr : &header->down;
-    gradients(0, a.vocab, {base + L.off_scaled, a.dim, a.rows, L.ld}, *to, down);
-    join(*to, nullptr, down);
+    gradients(0, a.vocab, {base + L.off_scaled, a.dim, a.rows, L.ld}, *to);
+    join(*to, nullptr);
   }
   void run_kept(float* loss, const Gradients& to) {
     TargetArgs t = {};
@@ -1401,18 +1405,17 @@ struct HeadRun {
       r.dim = a.dim, r.second = turn;
       launch(kKHeadRows, k_head_rows_kept, row_blocks(), 256, r);
     }
-    gradients(0, a.vocab, {base + L.off_scaled, a.dim, a.rows, L.ld}, to, nullptr);
-    join(to, at<float>(L.off_factor), nullptr);
+    gradients(0, a.vocab, {base + L.off_scaled, a.dim, a.rows, L.ld}, to);
+    join(to, at<float>(L.off_factor));
   }
   void run_pieces(float* loss, const Gradients& to) {
-    if (!bf16) begin();
+    begin();
     copies(L.keep == Keep::kWide ? nullptr : a.targets_dev);
     logits_once(loss, true);
     if (L.keep == Keep::kWide) rescale<float>(L.off_wide);
     else if constexpr (!bf16)
       if (L.keep == Keep::kFp16) rescale<T>(L.off_g);
     const Operand counted = L.keep == Keep::kWide ? Operand{base + L.off_scaled, a.dim, a.rows, L.ld} : hidden;
-    const float* const down = bf16 ? nullptr : &header->down;
     for (uint32_t i = 0; i < L.pieces; ++i) {
       const uint32_t from = i * L.piece, words = i + 1 < L.pieces ? L.piece : a.vocab - from;
       if (L.keep == Keep::kNot) {
@@ -1421,9 +1424,9 @@ struct HeadRun {
         p.out = base + L.off_g, p.ldo = L.ldg;
         multiply<kProbs>(kKHeadProbs, p, {static_cast<const T*>(head.at) + (uint64_t)from * head.ld, a.dim, words, head.ld});
       }
-      gradients(from, words, counted, to, down);
+      gradients(from, words, counted, to);
     }
-    join(to, nullptr, down);
+    join(to, nullptr);
   }
   cudaError_t run(float* loss, const Gradients* to) {
     if (!to || L.keep == Keep::kBf16 || L.keep == Keep::kFew) copies(nullptr);
