@@ -541,7 +541,7 @@ int cvlc_embed_grad(const void* tokens_dev, uint32_t token_bytes, uint64_t n, co
  *  d_hidden_dev, d_head_dev   as hidden and head, of strides of their own; they must not overlap hidden, head or each other
  *  ws_dev       cvlc_head_workspace_bytes(a, graded) bytes (graded: 0 for cvlc_head_loss, 1 for cvlc_head_step), 256-byte aligned
  * Results do not depend on the order in which blocks run.  Waits inside the kernels are bounded (four seconds): should one run out,
- * CVLC_ERR_DEVICE_TIMEOUT goes to *status_dev, and losses and d_hidden are NaN, d_head undefined.
+ * CVLC_ERR_DEVICE_TIMEOUT goes to *status_dev, and what it had a part in of losses and d_hidden is NaN, d_head undefined.
  * Errors: INVALID_ARG (dtype, vocab from 1 to CVLC_MAX_VOCAB, dim from 1 to 65536, rows above 2^24, a stride below dim or above 2^32, a scale that
  * is not finite, pieces of 0, alignment, overlap), WORKSPACE_TOO_SMALL.  rows = 0 writes zeros to d_head.
  */

@@ -83,6 +83,7 @@ struct Product {
   void* out;
   uint64_t ldo, split_stride;
   uint32_t add, wide;                    // added to what is there; written by boxes
+  uint32_t whole;                        // both: a gradient itself, not a part of it
   const float* alpha_dev;                // or nullptr; multiplies alpha
   const uint32_t* skip;                  // or nullptr; where it is 0 nothing is to be done
   const uint32_t* wild;                  // or nullptr; of 256 rows each: 0 where they are left out
@@ -484,8 +485,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_head_product(const __grid_const
     }
   } else if (warp >= 4) {
     const uint32_t half_tile = (warp - 4) / 4, quarter = warp & 3, box = ring + kRingBytes + (warp - 4) * kBoxBytes;
-    uint32_t turn_of = 0;
-    for (uint32_t w = first; w < items; w += apart) {
+    uint32_t turn_of = 0, w = first;
+    for (; w < items; w += apart) {
       const bool second = EPI == kBoth && w >= items0;
       const Product& g = both.p[second ? Products<EPI>::count - 1 : 0];
       if (left_out(g, w)) continue;
@@ -495,7 +496,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_head_product(const __grid_const
       tensor_after();
       const uint32_t at = tensor + half * kTileN + half_tile * 128 + (quarter * 32 << 16);
       if constexpr (EPI == kBoth) {
-        if (second && g.splits == 1) finish_tile<kGrad, T>(g, r, at, half_tile, quarter, lane, box);
+        if (g.whole) finish_tile<kGrad, T>(g, r, at, half_tile, quarter, lane, box);
         else finish_tile<kParts, T>(g, r, at, half_tile, quarter, lane, box);
       } else {
         finish_tile<EPI, T>(g, r, at, half_tile, quarter, lane, box);
@@ -505,6 +506,13 @@ __global__ void __launch_bounds__(kThreads, 1) k_head_product(const __grid_const
       if (lane == 0) mbar_arrive_leader<CG>(taken + half);
       ++turn_of;
     }
+    if (EPI == kBoth && !ok && g0.whole)  // no kernel follows that would say it: what is missing of the hidden states' gradient is NaN
+      for (; w < items0; w += apart) {
+        const Work r = work_of<CG>(g0, w);
+        const uint32_t row = r.m0 + quarter * 32 + lane, from = r.n0 + half_tile * 128;
+        if (row < g0.m)
+          for (uint32_t col = from; col < min(r.n_end, from + 128); ++col) static_cast<T*>(g0.out)[row * g0.ldo + col] = from_float<T>(CUDART_NAN_F);
+      }
     if (lane == 0) tiles_stored();
   }
   __syncwarp();
@@ -888,8 +896,7 @@ __global__ void __launch_bounds__(256) k_head_softmax(const SoftmaxArgs a) {
   const int64_t word = target_of(a.targets, a.token_bytes, row);
   const float weight = a.weight ? a.weight[row] : 1.0f;
   uint32_t late = 0;
-  if (mine < 32)
-    for (uint32_t i = mine; i < kNumSM; i += 32) late |= a.header->late[i];
+  for (uint32_t i = threadIdx.x & 31; i < kNumSM; i += 32) late |= a.header->late[i];
   float z[kHeld][4] = {};
   const float* const from = a.parts + row * a.ldz + mine * 4;
   for (uint32_t k = 0; k < a.splits; ++k)
@@ -929,12 +936,10 @@ __global__ void __launch_bounds__(256) k_head_softmax(const SoftmaxArgs a) {
     }
   }
   o = over_row<THREADS, false>(o, shared[1]);
-  const float right = exp2f(zt - most), total = right + o, w = weight * (a.up ? *a.up : a.up_by), f = w / total, of_target = -(o / total) * w;
-  if (mine < 32 && __any_sync(kFull, late)) {
-    if (mine == 0) a.loss[row] = CUDART_NAN_F;
-  } else if (mine == 0) {
-    a.loss[row] = !there ? 0.0f : weight * (most == zt ? log1pf(o) : logf(total) + (most - zt) * kLn2);
-  }
+  const bool gone = __any_sync(kFull, late);
+  const float right = exp2f(zt - most), total = right + o, w = gone ? CUDART_NAN_F : weight * (a.up ? *a.up : a.up_by);
+  const float f = w / total, of_target = -(o / total) * w;
+  if (mine == 0) a.loss[row] = gone ? CUDART_NAN_F : !there ? 0.0f : weight * (most == zt ? log1pf(o) : logf(total) + (most - zt) * kLn2);
   if (!a.to) return;
   T* const to = static_cast<T*>(a.to) + row * a.ldg + mine * 4;
 #pragma unroll
@@ -1104,6 +1109,7 @@ enum class Keep { kNot, kFew, kWide, kBf16, kFp16 };
 struct HeadLayout {
   Keep keep;
   bool pairs;              // in the gradients' products
+  bool whole;              // d_hidden is made in one part and needs no joining
   bool copy_hidden, copy_head;
   uint64_t ld;             // of copies
   uint32_t piece, pieces;  // words
@@ -1149,9 +1155,10 @@ HeadLayout head_layout(const cvlc_head& a, uint32_t pieces) {
     L.splits = splits_of(a.rows, a.dim, tiles(L.piece, kTileK), L.pairs);
     // of few words and many rows the head's gradient has few tiles and long sums (7094 x 144 x 83: 79 -> 34 us)
     L.splits_head = few ? splits_of(a.vocab, a.dim, tiles(a.rows, kTileK), false) : 1;
+    L.whole = few && L.splits == 1;
     if (L.splits_head > 1) L.off_head_parts = take((size_t)L.splits_head * a.vocab * L.ldp * 4);
     L.off_g = take(a.rows * L.ldg * 2);
-    L.off_parts = take((size_t)L.splits * a.rows * L.ldp * 4);
+    if (!L.whole) L.off_parts = take((size_t)L.splits * a.rows * L.ldp * 4);
     if (L.keep == Keep::kBf16) {
       L.blocks_wild = tiles(a.rows, kWildRows);
       L.off_scaled = take(a.rows * L.ld * 2);
@@ -1332,8 +1339,11 @@ struct HeadRun {
     T* const out = static_cast<T*>(to.d_head) + (uint64_t)from * to.d_head_stride;
     q.out = out, q.ldo = to.d_head_stride, q.wide = on16(out, to.d_head_stride) && a.dim % 8 == 0;  // a box writes whole vectors of 16 bytes: what lies behind a row's end with them, too
     q.alpha = a.scale * down_by(), q.alpha_dev = down();
+    q.whole = q.splits == 1;
+    if (L.whole)
+      p.whole = 1, p.out = to.d_hidden, p.ldo = to.d_hidden_stride, p.wide = on16(to.d_hidden, to.d_hidden_stride) && a.dim % 8 == 0, p.alpha = q.alpha, p.alpha_dev = q.alpha_dev;
     if (q.splits > 1) q.out = base + L.off_head_parts, q.ldo = L.ldp, q.split_stride = words * L.ldp, q.wide = 0;
-    const bool fits = make_product(p, bf16, pairs, g, false, piece, true, false) && make_product(q, bf16, pairs, g, true, hidden_scaled, true, q.wide);
+    const bool fits = make_product(p, bf16, pairs, g, false, piece, true, p.wide) && make_product(q, bf16, pairs, g, true, hidden_scaled, true, q.wide);
     if (pairs) {
       run_product<kParts, false, true, 2>(kKHeadParts, {{p}}, fits);
       run_product<kGrad, true, true, 2>(kKHeadGrad, {{q}}, fits);
@@ -1345,13 +1355,15 @@ struct HeadRun {
   void join(const Gradients& to, const float* factor) {
     JoinArgs j = {};
     uint64_t quads[2] = {};
-    auto add = [&](uint32_t i, size_t parts, uint32_t splits, uint64_t rows, void* out, uint64_t stride) {
-      JoinJob& x = j.of[i];
+    uint32_t n = 0;
+    auto add = [&](size_t parts, uint32_t splits, uint64_t rows, void* out, uint64_t stride) {
+      JoinJob& x = j.of[n];
       x.parts = at<float>(parts), x.split_stride = rows * L.ldp, x.ldp = L.ldp, x.ldo = stride, x.splits = splits, x.dim = a.dim, x.rows = rows, x.alpha = a.scale * down_by();
-      x.factor = factor, x.down = down(), x.out = out, quads[i] = rows * ((a.dim + 3) / 4);
+      x.factor = factor, x.down = down(), x.out = out, quads[n++] = rows * ((a.dim + 3) / 4);
     };
-    add(0, L.off_parts, L.splits, a.rows, to.d_hidden, to.d_hidden_stride);
-    if (L.splits_head > 1) add(1, L.off_head_parts, L.splits_head, a.vocab, to.d_head, to.d_head_stride);
+    if (!L.whole) add(L.off_parts, L.splits, a.rows, to.d_hidden, to.d_hidden_stride);
+    if (L.splits_head > 1) add(L.off_head_parts, L.splits_head, a.vocab, to.d_head, to.d_head_stride);
+    if (!n) return;
     j.header = header;
     const bool shared = (L.splits >= 8 || L.splits_head >= 8) && quads[0] + quads[1] <= 32768;
     const uint32_t of = shared ? 32 : 256;

@@ -405,3 +405,15 @@ def test_few_logits_leave_what_lies_between_the_rows(rows, dim, vocab, pad):
     B.cvlc_head_step(hidden, head, t, loss[:rows], room[0][:, :dim], room[1][:, :dim], space(hidden, head, 1))
     R.check(loss[:rows], room[0][:, :dim], room[1][:, :dim], hidden, head, t)
     assert all(bool((r[:, dim:] == 7.0).all()) for r in room) and bool((loss[rows:] == 7.0).all())
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+def test_few_logits_ignored_rows_of_any_weight(dtype):
+    hidden, head, t = make(50, 64, 40, dtype)
+    weight = torch.ones(50, device="cuda")
+    weight[::5], t[::5] = float("nan"), -1
+    _, loss, dh, dw = run(hidden, head, t, weight=weight)
+    live = torch.arange(50, device="cuda") % 5 != 0
+    assert not bool(loss[~live].any()) and not bool(dh[~live].any())
+    weight[::5] = 0
+    R.check(loss, dh, dw, hidden, head, t, 1.0, weight)
