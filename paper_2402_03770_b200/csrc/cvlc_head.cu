@@ -239,15 +239,24 @@ __device__ __forceinline__ void finish_tile(const Product& g, const Work& w, uin
   } else if constexpr (EPI == kKeepOwn || EPI == kKeepWide) {
     // each row of 128 columns relative to its own maximum, which takes a look of its own: in fp16, which has no range to spare, and in fp32 (wide)
     const int64_t target = there ? target_of(g.targets, g.token_bytes, row) : -1;
-    float most = -CUDART_INF_F, sum = 0.0f;
+    // (by pairs, all 128 columns are held meanwhile)
+    constexpr bool held = EPI == kKeepOwn;
+    constexpr int unrolled = held ? 4 : 1;
+    float z[held ? 4 : 1][32], most = -CUDART_INF_F, sum = 0.0f;
+    if (held) {
+#pragma unroll
+      for (int c = 0; c < 4; ++c) tensor_load(tensor + c * 32, z[held ? c : 0]);
+    }
+#pragma unroll unrolled
     for (int c = 0; c < 4; ++c) {
       const uint32_t col = w.n0 + half * 128 + c * 32;
-      if (col >= w.n_end) break;
-      tensor_load(tensor + c * 32, v);
+      if (!held && col >= w.n_end) break;
+      float (&v)[32] = z[held ? c : 0];
+      if (!held) tensor_load(tensor + c * 32, v);
       tensor_loaded(v);
 #pragma unroll
       for (int i = 0; i < 32; ++i) v[i] = v[i] * g.k2;
-      const bool mine = target >= col && target < (int64_t)col + 32;
+      const bool mine = target >= col && target < (int64_t)min(col + 32, w.n_end);
       if (col + 32 > w.n_end || __any_sync(kFull, mine)) {
 #pragma unroll
         for (int i = 0; i < 32; ++i) {
@@ -259,19 +268,26 @@ __device__ __forceinline__ void finish_tile(const Product& g, const Work& w, uin
       for (int i = 0; i < 32; ++i) most = fmaxf(most, v[i]);
     }
     const float from = most == -CUDART_INF_F ? 0.0f : most;
+#pragma unroll unrolled
     for (int c = 0; c < 4; ++c) {
       const uint32_t col = w.n0 + half * 128 + c * 32;
       if (EPI == kKeepWide ? col >= w.n_end : (c & 1) == 0 && col >= w.n_end) break;
       if (EPI == kKeepOwn && (c & 1) == 0) box_free(lane);
-      tensor_load(tensor + c * 32, v);
-      tensor_loaded(v);
+      float (&v)[32] = z[held ? c : 0];
+      if (held) {
 #pragma unroll
-      for (int i = 0; i < 32; ++i) v[i] = fmaf(v[i], g.k2, -from);
-      const bool mine = target >= col && target < (int64_t)col + 32;
-      if (col + 32 > w.n_end || __any_sync(kFull, mine)) {
+        for (int i = 0; i < 32; ++i) v[i] -= from;
+      } else {
+        tensor_load(tensor + c * 32, v);
+        tensor_loaded(v);
 #pragma unroll
-        for (int i = 0; i < 32; ++i)
-          if (col + i >= w.n_end || (mine && target == (int64_t)col + i)) v[i] = -CUDART_INF_F;
+        for (int i = 0; i < 32; ++i) v[i] = fmaf(v[i], g.k2, -from);
+        const bool mine = target >= col && target < (int64_t)col + 32;
+        if (col + 32 > w.n_end || __any_sync(kFull, mine)) {
+#pragma unroll
+          for (int i = 0; i < 32; ++i)
+            if (col + i >= w.n_end || (mine && target == (int64_t)col + i)) v[i] = -CUDART_INF_F;
+        }
       }
       float s[4] = {};
 #pragma unroll

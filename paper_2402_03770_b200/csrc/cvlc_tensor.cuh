@@ -42,10 +42,12 @@ __device__ __forceinline__ void mbar_expect(uint64_t* b, uint32_t bytes) {
   asm volatile("mbarrier.arrive.expect_tx.shared.b64 _, [%0], %1;" ::"r"(smem_at(b)), "r"(bytes) : "memory");
 }
 __device__ __forceinline__ void mbar_arrive(uint64_t* b) { asm volatile("mbarrier.arrive.shared.b64 _, [%0];" ::"r"(smem_at(b)) : "memory"); }
+// The tensor memory has been read (tensor_loaded() has waited for it), and nothing else is handed over: an arrival that released would wait for the stores of all that
+// the thread has written (4096 x 256 x 50048, the logits' statistics: 137 -> 119 us).
 template <int CG>
 __device__ __forceinline__ void mbar_arrive_leader(uint64_t* b) {
   if constexpr (CG == 1) mbar_arrive(b);
-  else asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(leader_at<CG>(smem_at(b))) : "memory");
+  else asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(leader_at<CG>(smem_at(b))) : "memory");
 }
 __device__ __forceinline__ bool mbar_try(uint64_t* b, uint32_t parity) {
   uint32_t done;
