@@ -417,3 +417,30 @@ def test_few_logits_ignored_rows_of_any_weight(dtype):
     assert not bool(loss[~live].any()) and not bool(dh[~live].any())
     weight[::5] = 0
     R.check(loss, dh, dw, hidden, head, t, 1.0, weight)
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("pieces", [1, 2])
+def test_many_rows_in_graphs_of_two_streams(dtype, pieces):
+    """two captured steps of sizes of their own, replayed at once, again and again with other inputs"""
+    sizes = ((4200, 64, 2100), (2300, 72, 4000))
+    cases = [[*make(*n, dtype, seed=1)] for n in sizes]
+    outs = [(torch.zeros(h.shape[0], device="cuda"), torch.zeros_like(h), torch.zeros_like(w), space(h, w, pieces)) for h, w, _ in cases]
+    graphs, streams = [], [torch.cuda.Stream() for _ in sizes]
+    for (h, w, t), (loss, dh, dw, ws), stream in zip(cases, outs, streams):
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1], stream=stream):
+            B.cvlc_head_step(h, w, t, loss, dh, dw, ws, pieces=pieces, stream=stream)
+    for seed in (3, 4):
+        for case, n in zip(cases, sizes):
+            for x, y in zip(case, make(*n, dtype, seed=seed)):
+                x.copy_(y)
+        torch.cuda.synchronize()
+        for _ in range(3):
+            for graph, stream in zip(graphs, streams):
+                with torch.cuda.stream(stream):
+                    graph.replay()
+        torch.cuda.synchronize()
+        for (h, w, t), out in zip(cases, outs):
+            want = run(h, w, t, pieces=pieces)
+            assert all(torch.equal(x, y) for x, y in zip(out[:3], want[1:]))
