@@ -738,7 +738,7 @@ class AdamwTensors:
         self.grad_dtype = _DTYPES[grads[0].dtype] if n else CVLC_F32
         self.param_dtype = _DTYPES[params[0].dtype] if n and self.step else CVLC_F32
         self.state_bits = 32 if scales is None else 8
-        self.copy_dtype = next((_DTYPES[x.dtype] for x in copies or () if x is not None), CVLC_BF16)
+        self.copy_dtype = next((_DTYPES[x.dtype] for x in (() if copies is None else copies) if x is not None), CVLC_BF16)
 
         def at(x: Optional[torch.Tensor], size: int, dtype: int) -> Optional[int]:
             if x is None:
@@ -767,7 +767,7 @@ class AdamwTensors:
         # what the step writes has no byte in common with anything else of it: a weight that is there twice, as one that two layers share, would be moved twice at once
         parts = []
         for i in range(n if self.step else 0):
-            for k, x in enumerate((grads[i], params[i], m[i], v[i], scales and scales[i], copies and copies[i])):
+            for k, x in enumerate((grads[i], params[i], m[i], v[i], None if scales is None else scales[i], None if copies is None else copies[i])):
                 if x is not None and x.numel():
                     parts.append((x.data_ptr(), x.data_ptr() + x.numel() * x.element_size(), k > 0))
         parts.sort()

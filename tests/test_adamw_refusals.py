@@ -89,3 +89,11 @@ def test_binding_refuses_what_overlaps():
         B.AdamwTensors([g, c], [p, q], [m, w], [v, x], copies=[half, half])
     with pytest.raises(AssertionError, match="overlap"):
         B.AdamwTensors([g, c], [p, q], [byte[0], byte[1]], [byte[2], byte[3]], scales=[scales[0], scales[0]])
+
+
+def test_binding_takes_rows_of_one_tensor():
+    g, p, m, v = torch.zeros(4, 3, 512).unbind()
+    byte, copies = torch.zeros(2, 3, 512, dtype=torch.uint8), torch.zeros(3, 512, dtype=torch.bfloat16)
+    t = B.AdamwTensors(g, p, byte[0], byte[1], scales=torch.zeros(3, 2, 2), copies=copies)
+    assert t.n == 3 and t.array[1].copy_dev == copies[1].data_ptr() and t.array[2].m_dev == byte[0, 2].data_ptr()
+    assert B.AdamwTensors(g, p, m, v).array[1].v_dev == v[1].data_ptr()
