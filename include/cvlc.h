@@ -520,7 +520,7 @@ int cvlc_embed_grad(const void* tokens_dev, uint32_t token_bytes, uint64_t n, co
 
 /*
  * The training loss of such a model: softmax cross entropy of hidden states against the head, the matrix whose rows are the words (the
- * embedding table itself, or one of its own), without ever holding the logits.  With z = scale hidden_t . head_v,
+ * embedding table itself, or one of its own), without ever holding more than 2^22 logits.  With z = scale hidden_t . head_v,
  *   loss_t = row_weight_t (ln sum_v exp(z_tv) - z_t,target)
  * and, for cvlc_head_step, the gradients of the sum of all losses, d_hidden and d_head, in the operands' type.
  * A target below 0 is none, and a row without one, or of weight 0, counts for nothing, whatever it holds: its loss, its gradient and
@@ -528,7 +528,7 @@ int cvlc_embed_grad(const void* tokens_dev, uint32_t token_bytes, uint64_t n, co
  * 0 beforehand; or NULL).  A NaN or +infinite logit makes the row's loss, and what the row has a part in, not finite (one of
  * -infinity the loss of its own word, and the gradients).
  * The products are made by the tensor cores: operands in 16 bits (CVLC_F16 or CVLC_BF16; there is no product of fp32), sums in fp32, in steps of 16 that
- * may be cut off instead of rounded.  A logit's gradient, row_weight (softmax - one for the target), is rounded to the operands' type (in fp16 times a
+ * are cut off instead of rounded (what that takes from a logit on average is put back).  A logit's gradient, row_weight (softmax - one for the target), is rounded to the operands' type (in fp16 times a
  * power of two that keeps the largest row_weight at 2^15), as the operand of the two products that follow, and d_hidden and d_head once more.  With more than
  * 128 rows in one piece, and more than 2^22 logits or 8192 words, there is another rounding: the exponentials are kept in 16 bits; in fp16 they are multiplied later,
  * in bf16 their rows' factors go into the hidden states for d_head, which are rounded.
