@@ -729,9 +729,9 @@ __device__ __forceinline__ bool join_parts(const RowsArgs& a, uint64_t row, uint
 }
 
 // A row of hidden states as it counts: others, which may hold anything, would have a part in the head's gradient
-__device__ __forceinline__ void masked_row(const uint16_t* h, uint16_t* to, uint32_t dim, bool counts, uint32_t thread, uint32_t threads) {
+__device__ __forceinline__ void masked_row(const uint16_t* h, uint16_t* to, uint32_t dim, bool counts, uint32_t from, uint32_t threads) {
 #pragma unroll 4
-  for (uint32_t i = thread * 8; i < dim; i += threads * 8) {
+  for (uint32_t i = from; i < dim; i += threads * 8) {
     uint4 v = make_uint4(0, 0, 0, 0);
     if (counts) {
       if (i + 8 <= dim) {
@@ -783,7 +783,7 @@ __global__ void __launch_bounds__(256) k_head_rows(const RowsArgs a) {
   const uint64_t mine = (uint64_t)blockIdx.x * kRowsOf + threadIdx.x / 32;
   if (mine >= a.rows) return;
   masked_row(reinterpret_cast<const uint16_t*>(a.hidden) + mine * a.hidden_ld, reinterpret_cast<uint16_t*>(a.scaled) + mine * a.scaled_ld, a.dim,
-             counts[threadIdx.x / 32], threadIdx.x & 31, 32);
+             counts[threadIdx.x / 32], (threadIdx.x & 31) * 8, 32);
 }
 
 // The same where the exponentials are kept, relative to the target's (to the row's maximum in a second turn): of G = weight exp(z - from) / total the
@@ -864,7 +864,6 @@ __global__ void __launch_bounds__(256) k_head_rows_kept(const RowsArgs a) {
 }
 
 // Few logits: they are there themselves, in parts of their sums, and a row's loss and G are made at once by THREADS threads, of which each holds up to 32 of them.
-// A warp up to 1024 words (557 x 184 x 379: 9.6 us, 12.3 by eight warps), eight up to 8192 (183 x 426 x 3796: 32 us, 40 by 32 warps).
 struct SoftmaxArgs {
   const float* parts;
   uint64_t split_stride, ldz, rows, ldg, hidden_ld, scaled_ld;
@@ -902,7 +901,7 @@ __device__ __forceinline__ float over_row(float x, float* shared) {
   return x;
 }
 template <class T, int THREADS>
-__global__ void __launch_bounds__(256) k_head_softmax(const SoftmaxArgs a) {
+__global__ void __launch_bounds__(256, 3) k_head_softmax(const SoftmaxArgs a) {
   pdl_enter();
   if (a.to) let_next_in();  // else the last of the call
   __shared__ float shared[2][8], at_target;
@@ -913,17 +912,37 @@ __global__ void __launch_bounds__(256) k_head_softmax(const SoftmaxArgs a) {
   const float weight = a.weight ? a.weight[row] : 1.0f;
   uint32_t late = 0;
   for (uint32_t i = threadIdx.x & 31; i < kNumSM; i += 32) late |= a.header->late[i];
+  constexpr uint32_t kAhead = THREADS == 32 ? 4 : 2;
+  uint4 ahead[kAhead];  // the beginning of the hidden states, on its way meanwhile
+  const uint16_t* const h = a.hidden + row * a.hidden_ld;
+  if (a.to) {
+#pragma unroll
+    for (uint32_t k = 0; k < kAhead; ++k)
+      if ((k * THREADS + mine) * 8 + 8 <= a.dim) ahead[k] = __ldg(reinterpret_cast<const uint4*>(h + (k * THREADS + mine) * 8));
+  }
   float z[kHeld][4] = {};
   const float* const from = a.parts + row * a.ldz + mine * 4;
-  for (uint32_t k = 0; k < a.splits; ++k)
+  auto part = [&](uint32_t i, uint32_t k) {
+    return (i * THREADS + mine) * 4 < a.vocab && k < a.splits ? *reinterpret_cast<const float4*>(from + k * a.split_stride + i * THREADS * 4) : make_float4(0, 0, 0, 0);
+  };
+  auto add = [&](uint32_t i, const float4& x) { z[i][0] += x.x, z[i][1] += x.y, z[i][2] += x.z, z[i][3] += x.w; };
+  if (a.splits >= 4) {  // many parts of few logits, or few of many: four or eight loads on their way
 #pragma unroll
     for (uint32_t i = 0; i < kHeld; ++i) {
       if (i * THREADS * 4 >= a.vocab) break;
-      if ((i * THREADS + mine) * 4 < a.vocab) {
-        const float4 x = *reinterpret_cast<const float4*>(from + k * a.split_stride + i * THREADS * 4);
-        z[i][0] += x.x, z[i][1] += x.y, z[i][2] += x.z, z[i][3] += x.w;
+      for (uint32_t k = 0; k < a.splits; k += 4) {
+        const float4 x0 = part(i, k), x1 = part(i, k + 1), x2 = part(i, k + 2), x3 = part(i, k + 3);
+        add(i, x0), add(i, x1), add(i, x2), add(i, x3);
       }
     }
+  } else {
+    for (uint32_t k = 0; k < a.splits; ++k)
+#pragma unroll
+      for (uint32_t i = 0; i < kHeld; ++i) {
+        if (i * THREADS * 4 >= a.vocab) break;
+        if ((i * THREADS + mine) * 4 < a.vocab) add(i, *reinterpret_cast<const float4*>(from + k * a.split_stride + i * THREADS * 4));
+      }
+  }
   if (word >= (int64_t)a.vocab && a.status && mine == 0) set_status(a.status, CVLC_ERR_INVALID_ARG);
   const bool there = word >= 0 && word < (int64_t)a.vocab && weight != 0.0f;
   const uint32_t target = there ? (uint32_t)word : 0;
@@ -967,7 +986,15 @@ __global__ void __launch_bounds__(256) k_head_softmax(const SoftmaxArgs a) {
     for (uint32_t k = 0; k < 4; ++k) g[k] = !there ? 0.0f : col + k == target ? of_target : z[i][k] * f;
     if (col < a.vocab) *reinterpret_cast<uint2*>(to + i * THREADS * 4) = make_uint2(pack2<T>(g[0], g[1]), pack2<T>(g[2], g[3]));
   }
-  masked_row(a.hidden + row * a.hidden_ld, a.scaled + row * a.scaled_ld, a.dim, there, mine, THREADS);
+  uint16_t* const scaled = a.scaled + row * a.scaled_ld;
+  uint32_t col = mine * 8;
+#pragma unroll
+  for (uint32_t k = 0; k < kAhead; ++k)
+    if (col + 8 <= a.dim) {
+      *reinterpret_cast<uint4*>(scaled + col) = there ? ahead[k] : make_uint4(0, 0, 0, 0);
+      col += THREADS * 8;
+    }
+  masked_row(h, scaled, a.dim, there, col, THREADS);
 }
 
 // Exponentials that are kept relative to the maximum of their 128 columns become G: times exp(maximum - ln sum exp) and the weight.  In fp16 in their place; in fp32
@@ -1416,7 +1443,14 @@ struct HeadRun {
     r.splits = L.splits_z, r.vocab = a.vocab, r.token_bytes = a.token_bytes, r.dim = a.dim, r.targets = a.targets_dev, r.weight = a.row_weight_dev;
     r.up = to ? up() : nullptr, r.up_by = up_by(), r.k2 = p.k2, r.loss = loss, r.to = to ? base + L.off_g : nullptr;
     r.hidden = static_cast<const uint16_t*>(hidden.at), r.scaled = at<uint16_t>(L.off_scaled), r.header = header, r.status = a.status_dev;
-    if (a.vocab <= 1024) launch(kKHeadSoftmax, k_head_softmax<T, 32>, tiles(a.rows, 8), 256, r);
+    // as many threads a row as hold it, and more while there is work for them and all rows' are resident (50 x 768 x 1000: 29 us by 32, 20 by 256; 700 x 700 x 300: 28, 26 by 128, 29 by 256;
+    // 7094 x 144 x 83: 25 by 32, 47 by 256)
+    uint32_t threads = 32;
+    const uint32_t work = to && a.dim / 2 > a.vocab ? a.dim / 2 : a.vocab;  // logits or, at 16 bytes a thread, hidden states
+    while (threads < 256 && (a.vocab > threads * 4 * kHeld || (work > threads * 4 && a.rows * threads * 2 <= kNumSM * 1024))) threads *= 2;
+    if (threads == 32) launch(kKHeadSoftmax, k_head_softmax<T, 32>, tiles(a.rows, 8), 256, r);
+    else if (threads == 64) launch(kKHeadSoftmax, k_head_softmax<T, 64>, (uint32_t)a.rows, 64, r);
+    else if (threads == 128) launch(kKHeadSoftmax, k_head_softmax<T, 128>, (uint32_t)a.rows, 128, r);
     else launch(kKHeadSoftmax, k_head_softmax<T, 256>, (uint32_t)a.rows, 256, r);
     if (!to) return;
     gradients(0, a.vocab, {base + L.off_scaled, a.dim, a.rows, L.ld}, *to);
