@@ -367,7 +367,7 @@ __device__ __forceinline__ void finish_tile(const Product& g, const Work& w, uin
       const uint32_t col = w.n0 + half * 128 + c * 32;
       if ((c & 1) == 0) {
         if (col >= w.n_end) break;
-        if (g.wide) box_free(lane);
+        box_free(lane);  // in either form: the tile before this one may have been the launch's other product's, on its way from this box
       }
       tensor_load(tensor + c * 32, v);
       tensor_loaded(v);
