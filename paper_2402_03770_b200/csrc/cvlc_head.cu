@@ -625,6 +625,9 @@ __global__ void __launch_bounds__(256) k_head_align(const __grid_constant__ Alig
   }
 }
 
+// The target's logit as the loss is made of it.  +infinity would be a loss of 0: all others' exponentials relative to it are 0.
+__device__ __forceinline__ float known(float zt) { return zt < CUDART_INF_F ? zt : CUDART_NAN_F; }
+
 // z of every row's target, in log2; +inf where the row counts for nothing.  A warp a row.
 struct TargetArgs {
   const void *hidden, *head, *targets;
@@ -667,7 +670,7 @@ __global__ void __launch_bounds__(256) k_head_target(const TargetArgs a) {
 #pragma unroll
   for (int d = 16; d; d /= 2) sum += __shfl_xor_sync(kFull, sum, d);
   sum *= a.k2;
-  if (lane == 0) a.at_target[row] = sum < CUDART_INF_F ? sum : CUDART_NAN_F;
+  if (lane == 0) a.at_target[row] = known(sum);
 }
 
 constexpr float kWild = 60.0f;
@@ -765,7 +768,7 @@ __global__ void __launch_bounds__(256) k_head_rows(const RowsArgs a) {
     float loss = 0.0f;
     float4 r = make_float4(0, 0, 0, 0);
     if (there) {
-      const float zt = a.at_target[row];
+      const float zt = known(a.at_target[row]);
       float most = zt;
       for (uint32_t i = 0; i < 8; ++i) most = fmaxf(most, part[i][lane].x);
       double others = 0.0;
@@ -960,7 +963,7 @@ __global__ void __launch_bounds__(256, 3) k_head_softmax(const SoftmaxArgs a) {
   }
   if (THREADS > 32 && target / 4 % THREADS == mine) at_target = zt;
   most = over_row<THREADS, true>(most, shared[0]);
-  zt = THREADS > 32 ? at_target : __shfl_sync(kFull, zt, target / 4 % 32);
+  zt = known(THREADS > 32 ? at_target : __shfl_sync(kFull, zt, target / 4 % 32));
 #pragma unroll
   for (uint32_t i = 0; i < kHeld; ++i) {
     if (i * THREADS * 4 >= a.vocab) break;
