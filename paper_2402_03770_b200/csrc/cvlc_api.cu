@@ -781,6 +781,7 @@ int cvlc_head_step(const cvlc_head* a, float* loss_dev, void* d_hidden_dev, uint
   if (!a || !head_ok(*a) || !rows_ok(d_head_dev, 2, a->dim, d_head_stride)) return CVLC_ERR_INVALID_ARG;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   const uint64_t row = (uint64_t)a->dim * 2;
+  if (!rows_apart(a->head_dev, a->vocab, a->head_stride * 2, d_head_dev, a->vocab, d_head_stride * 2, row)) return CVLC_ERR_INVALID_ARG;
   if (a->rows == 0) {
     if (d_head_stride * 2 <= INT32_MAX) return cudaMemset2DAsync(d_head_dev, d_head_stride * 2, 0, row, a->vocab, st) == cudaSuccess ? CVLC_OK : CVLC_ERR_CUDA;
     for (uint64_t v = 0; v < a->vocab; ++v)  // rows that are further apart than a fill in two dimensions may leave
@@ -791,7 +792,6 @@ int cvlc_head_step(const cvlc_head* a, float* loss_dev, void* d_hidden_dev, uint
   if (!rows_apart(a->hidden_dev, a->rows, a->hidden_stride * 2, d_hidden_dev, a->rows, d_hidden_stride * 2, row) ||
       !rows_apart(a->hidden_dev, a->rows, a->hidden_stride * 2, d_head_dev, a->vocab, d_head_stride * 2, row) ||
       !rows_apart(a->head_dev, a->vocab, a->head_stride * 2, d_hidden_dev, a->rows, d_hidden_stride * 2, row) ||
-      !rows_apart(a->head_dev, a->vocab, a->head_stride * 2, d_head_dev, a->vocab, d_head_stride * 2, row) ||
       !rows_apart(d_hidden_dev, a->rows, d_hidden_stride * 2, d_head_dev, a->vocab, d_head_stride * 2, row))
     return CVLC_ERR_INVALID_ARG;
   if (ws_bytes < head_ws_bytes(*a, a->pieces)) return CVLC_ERR_WORKSPACE_TOO_SMALL;
