@@ -310,11 +310,11 @@ __global__ void __launch_bounds__(kStepThreads<EIGHT>) k_adamw(const __grid_cons
         }
         wm[h] = upper_bytes(c);
         wm[h] &= some_bits(wm[h]) | 0x7F7F7F7Fu;  // 0 has no sign
-        // a second moment that is there never becomes 0: the step would divide by eps alone
+        // a second moment that is there never becomes 0: the step would divide by eps alone (asked of v itself: next to one 2^166 times as large y is 0)
         if ((some_bits(upper_bytes(d)) & 0x80808080u) != 0x80808080u) {
 #pragma unroll
           for (int i = 0; i < 4; ++i)
-            if (d[i] < 1u << 24) d[i] = y[i] > 0.0f ? 1u << 24 : 0u;
+            if (d[i] < 1u << 24) d[i] = v[4 * h + i] > 0.0f && ib > 0.0f ? 1u << 24 : 0u;
         }
         wv[h] = upper_bytes(d);
       }
