@@ -665,6 +665,14 @@ int cvlc_selftest_wait(uint64_t* word_dev, int32_t* status_dev, uint32_t max_pol
 int cvlc_selftest_ring(const float* row_dev, uint32_t stages, int give_back, uint32_t limit_us, int32_t* status_dev, float* seen_dev,
                        void* cuda_stream);
 
+/* The bounded waits inside the products of cvlc_head_step (of cvlc_head_loss, where d_head_dev is NULL): the call with a fault in its product-th launch of products,
+ * counted from 0 (one that the call does not have: none), whose waits have a limit of limit_us (up to a second).  lost_copy: the tile of a block, counted from 0, from which on it
+ * copies no operands, so that who waits for them gives up; lost_tile: the tile at which its readers give up, as if their limit had run out while
+ * all the rest is still at work; UINT32_MAX: none.  Blocks that have so many report CVLC_ERR_DEVICE_TIMEOUT in *status_dev, end what they have begun and leave;
+ * what becomes of the results is said above.  Nothing hangs. */
+int cvlc_selftest_head(const cvlc_head* a, float* loss_dev, void* d_hidden_dev, uint64_t d_hidden_stride, void* d_head_dev, uint64_t d_head_stride,
+                       uint32_t product, uint32_t lost_copy, uint32_t lost_tile, uint32_t limit_us, void* ws_dev, size_t ws_bytes, void* cuda_stream);
+
 /* Launch accounting: number of kernels this library has launched in this process
  * (all kernels when kernel_name is NULL or "", else the named one, e.g. "k_hist").  Kernel names: k_zero_words,
  * k_hist, k_plan_threshold, k_plan_fit, k_plan_tune, k_encode_init, k_select, k_select_lookback, k_rank_split, k_rank, k_rank_rest, k_sort,

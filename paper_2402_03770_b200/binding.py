@@ -55,7 +55,7 @@ EXPORTS = [
     "cvlc_plan", "cvlc_plan_fixed", "cvlc_encode", "cvlc_plan_batch_workspace_bytes",
     "cvlc_encode_batch_workspace_bytes", "cvlc_plan_batch", "cvlc_encode_batch", "cvlc_decode_aggregate", "cvlc_read_status",
     "cvlc_selftest_philox", "cvlc_selftest_math", "cvlc_histogram_batch", "cvlc_plan_from_histogram_batch", "cvlc_decode_apply",
-    "cvlc_decode_aggregate_noalloc", "cvlc_compress_batch", "cvlc_selftest_wait", "cvlc_selftest_ring", "cvlc_plan_literal",
+    "cvlc_decode_aggregate_noalloc", "cvlc_compress_batch", "cvlc_selftest_wait", "cvlc_selftest_ring", "cvlc_selftest_head", "cvlc_plan_literal",
     "cvlc_plan_literal_workspace_bytes", "cvlc_ec_accumulate_batch", "cvlc_encode_batch_ec",
     "cvlc_unframed_stream_capacity", "cvlc_unframed_workspace_bytes", "cvlc_encode_unframed_batch", "cvlc_decode_aggregate_unframed",
     "cvlc_top_logits", "cvlc_distill_loss", "cvlc_distill_grad", "cvlc_distill_step", "cvlc_embed", "cvlc_embed_grad_workspace_bytes",
@@ -225,6 +225,8 @@ def lib() -> C.CDLL:
     L.cvlc_head_loss.argtypes = [PH, vp, vp, sz, vp]
     L.cvlc_head_step.restype = C.c_int
     L.cvlc_head_step.argtypes = [PH, vp, vp, u64, vp, u64, vp, sz, vp]
+    L.cvlc_selftest_head.restype = C.c_int
+    L.cvlc_selftest_head.argtypes = [PH, vp, vp, u64, vp, u64, u32, u32, u32, u32, vp, sz, vp]
     PT = C.POINTER(CvlcAdamwTensor)
     L.cvlc_adamw.restype = C.c_int
     L.cvlc_adamw.argtypes = [PT, u32, C.POINTER(CvlcAdamwArgs), vp]
@@ -720,6 +722,20 @@ def cvlc_head_step(hidden: torch.Tensor, head: torch.Tensor, targets: torch.Tens
     (dh, dh_stride), (dw, dw_stride) = _rows(d_hidden, device), _rows(d_head, device)
     _check(lib().cvlc_head_step(C.byref(a), _here(loss, torch.float32, (a.rows,), device), dh, dh_stride, dw, dw_stride, _ptr(ws), _nbytes(ws),
                                 _stream_on(stream, device)), "cvlc_head_step")
+
+
+def cvlc_selftest_head(hidden: torch.Tensor, head: torch.Tensor, targets: torch.Tensor, loss: torch.Tensor, d_hidden: Optional[torch.Tensor],
+                       d_head: Optional[torch.Tensor], ws: torch.Tensor, *, product: int = 0, lost_copy: Optional[int] = None, lost_tile: Optional[int] = None,
+                       limit_us: int = 1000, pieces: int = 1, status: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> None:
+    """cvlc_head_step (without d_head cvlc_head_loss) with a fault in one of its launches of products."""
+    device = _device()
+    a = _head(hidden, head, targets, 1.0, None, pieces, status, device)
+    assert ws.get_device() == device and (d_hidden is None) == (d_head is None)
+    none = 0xFFFFFFFF
+    (dh, dh_stride), (dw, dw_stride) = ((None, 0), (None, 0)) if d_head is None else (_rows(d_hidden, device), _rows(d_head, device))
+    _check(lib().cvlc_selftest_head(C.byref(a), _here(loss, torch.float32, (a.rows,), device), dh, dh_stride, dw, dw_stride, product,
+                                    none if lost_copy is None else lost_copy, none if lost_tile is None else lost_tile, limit_us, _ptr(ws), _nbytes(ws),
+                                    _stream_on(stream, device)), "cvlc_selftest_head")
 
 
 class AdamwTensors:

@@ -227,6 +227,35 @@ bool rows_apart(const void* p, uint64_t p_rows, uint64_t p_stride, const void* q
   return p_stride == q_stride && between >= row && p_stride - between >= row;
 }
 
+int head_loss(const cvlc_head* a, float* loss_dev, void* ws_dev, size_t ws_bytes, cudaStream_t st, const HeadFault* fault) {
+  if (!a || !head_ok(*a)) return CVLC_ERR_INVALID_ARG;
+  if (a->rows == 0) return CVLC_OK;
+  if (!aligned(loss_dev, 4) || !aligned(ws_dev, 256)) return CVLC_ERR_INVALID_ARG;
+  if (ws_bytes < head_ws_bytes(*a, 0)) return CVLC_ERR_WORKSPACE_TOO_SMALL;
+  return launch_head(*a, 0, loss_dev, nullptr, 0, nullptr, 0, ws_dev, st, fault) == cudaSuccess ? CVLC_OK : CVLC_ERR_CUDA;
+}
+
+int head_step(const cvlc_head* a, float* loss_dev, void* d_hidden_dev, uint64_t d_hidden_stride, void* d_head_dev, uint64_t d_head_stride, void* ws_dev,
+              size_t ws_bytes, cudaStream_t st, const HeadFault* fault) {
+  if (!a || !head_ok(*a) || !rows_ok(d_head_dev, 2, a->dim, d_head_stride)) return CVLC_ERR_INVALID_ARG;
+  const uint64_t row = (uint64_t)a->dim * 2;
+  if (!rows_apart(a->head_dev, a->vocab, a->head_stride * 2, d_head_dev, a->vocab, d_head_stride * 2, row)) return CVLC_ERR_INVALID_ARG;
+  if (a->rows == 0) {
+    if (d_head_stride * 2 <= INT32_MAX) return cudaMemset2DAsync(d_head_dev, d_head_stride * 2, 0, row, a->vocab, st) == cudaSuccess ? CVLC_OK : CVLC_ERR_CUDA;
+    for (uint64_t v = 0; v < a->vocab; ++v)  // rows that are further apart than a fill in two dimensions may leave
+      if (cudaMemsetAsync(static_cast<uint16_t*>(d_head_dev) + v * d_head_stride, 0, row, st) != cudaSuccess) return CVLC_ERR_CUDA;
+    return CVLC_OK;
+  }
+  if (!rows_ok(d_hidden_dev, 2, a->dim, d_hidden_stride) || !aligned(loss_dev, 4) || !aligned(ws_dev, 256)) return CVLC_ERR_INVALID_ARG;
+  if (!rows_apart(a->hidden_dev, a->rows, a->hidden_stride * 2, d_hidden_dev, a->rows, d_hidden_stride * 2, row) ||
+      !rows_apart(a->hidden_dev, a->rows, a->hidden_stride * 2, d_head_dev, a->vocab, d_head_stride * 2, row) ||
+      !rows_apart(a->head_dev, a->vocab, a->head_stride * 2, d_hidden_dev, a->rows, d_hidden_stride * 2, row) ||
+      !rows_apart(d_hidden_dev, a->rows, d_hidden_stride * 2, d_head_dev, a->vocab, d_head_stride * 2, row))
+    return CVLC_ERR_INVALID_ARG;
+  if (ws_bytes < head_ws_bytes(*a, a->pieces)) return CVLC_ERR_WORKSPACE_TOO_SMALL;
+  return launch_head(*a, a->pieces, loss_dev, d_hidden_dev, d_hidden_stride, d_head_dev, d_head_stride, ws_dev, st, fault) == cudaSuccess ? CVLC_OK : CVLC_ERR_CUDA;
+}
+
 constexpr uint64_t kMostValues = 1ull << 40;  // of all tensors of a call
 bool add_values(uint64_t n, uint64_t* total) {
   if (n > kMostValues || *total + n > kMostValues) return false;
@@ -769,33 +798,12 @@ size_t cvlc_head_workspace_bytes(const cvlc_head* a, int graded) {
 }
 
 int cvlc_head_loss(const cvlc_head* a, float* loss_dev, void* ws_dev, size_t ws_bytes, void* cuda_stream) {
-  if (!a || !head_ok(*a)) return CVLC_ERR_INVALID_ARG;
-  if (a->rows == 0) return CVLC_OK;
-  if (!aligned(loss_dev, 4) || !aligned(ws_dev, 256)) return CVLC_ERR_INVALID_ARG;
-  if (ws_bytes < head_ws_bytes(*a, 0)) return CVLC_ERR_WORKSPACE_TOO_SMALL;
-  return launch_head(*a, 0, loss_dev, nullptr, 0, nullptr, 0, ws_dev, static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess ? CVLC_OK : CVLC_ERR_CUDA;
+  return head_loss(a, loss_dev, ws_dev, ws_bytes, static_cast<cudaStream_t>(cuda_stream), nullptr);
 }
 
 int cvlc_head_step(const cvlc_head* a, float* loss_dev, void* d_hidden_dev, uint64_t d_hidden_stride, void* d_head_dev,
                    uint64_t d_head_stride, void* ws_dev, size_t ws_bytes, void* cuda_stream) {
-  if (!a || !head_ok(*a) || !rows_ok(d_head_dev, 2, a->dim, d_head_stride)) return CVLC_ERR_INVALID_ARG;
-  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-  const uint64_t row = (uint64_t)a->dim * 2;
-  if (!rows_apart(a->head_dev, a->vocab, a->head_stride * 2, d_head_dev, a->vocab, d_head_stride * 2, row)) return CVLC_ERR_INVALID_ARG;
-  if (a->rows == 0) {
-    if (d_head_stride * 2 <= INT32_MAX) return cudaMemset2DAsync(d_head_dev, d_head_stride * 2, 0, row, a->vocab, st) == cudaSuccess ? CVLC_OK : CVLC_ERR_CUDA;
-    for (uint64_t v = 0; v < a->vocab; ++v)  // rows that are further apart than a fill in two dimensions may leave
-      if (cudaMemsetAsync(static_cast<uint16_t*>(d_head_dev) + v * d_head_stride, 0, row, st) != cudaSuccess) return CVLC_ERR_CUDA;
-    return CVLC_OK;
-  }
-  if (!rows_ok(d_hidden_dev, 2, a->dim, d_hidden_stride) || !aligned(loss_dev, 4) || !aligned(ws_dev, 256)) return CVLC_ERR_INVALID_ARG;
-  if (!rows_apart(a->hidden_dev, a->rows, a->hidden_stride * 2, d_hidden_dev, a->rows, d_hidden_stride * 2, row) ||
-      !rows_apart(a->hidden_dev, a->rows, a->hidden_stride * 2, d_head_dev, a->vocab, d_head_stride * 2, row) ||
-      !rows_apart(a->head_dev, a->vocab, a->head_stride * 2, d_hidden_dev, a->rows, d_hidden_stride * 2, row) ||
-      !rows_apart(d_hidden_dev, a->rows, d_hidden_stride * 2, d_head_dev, a->vocab, d_head_stride * 2, row))
-    return CVLC_ERR_INVALID_ARG;
-  if (ws_bytes < head_ws_bytes(*a, a->pieces)) return CVLC_ERR_WORKSPACE_TOO_SMALL;
-  return launch_head(*a, a->pieces, loss_dev, d_hidden_dev, d_hidden_stride, d_head_dev, d_head_stride, ws_dev, st) == cudaSuccess ? CVLC_OK : CVLC_ERR_CUDA;
+  return head_step(a, loss_dev, d_hidden_dev, d_hidden_stride, d_head_dev, d_head_stride, ws_dev, ws_bytes, static_cast<cudaStream_t>(cuda_stream), nullptr);
 }
 
 int cvlc_adamw(const cvlc_adamw_tensor* tensors, uint32_t n_tensors, const cvlc_adamw_args* a, void* cuda_stream) {
@@ -836,6 +844,15 @@ int cvlc_selftest_wait(uint64_t* word_dev, int32_t* status_dev, uint32_t max_pol
                               static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess
              ? CVLC_OK
              : CVLC_ERR_CUDA;
+}
+
+int cvlc_selftest_head(const cvlc_head* a, float* loss_dev, void* d_hidden_dev, uint64_t d_hidden_stride, void* d_head_dev, uint64_t d_head_stride,
+                       uint32_t product, uint32_t lost_copy, uint32_t lost_tile, uint32_t limit_us, void* ws_dev, size_t ws_bytes, void* cuda_stream) {
+  if (limit_us > 1000000u) return CVLC_ERR_INVALID_ARG;
+  const HeadFault fault = {product, lost_copy, lost_tile, (uint64_t)limit_us * 1000};
+  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  if (!d_head_dev) return head_loss(a, loss_dev, ws_dev, ws_bytes, st, &fault);
+  return head_step(a, loss_dev, d_hidden_dev, d_hidden_stride, d_head_dev, d_head_stride, ws_dev, ws_bytes, st, &fault);
 }
 
 int cvlc_selftest_ring(const float* row_dev, uint32_t stages, int give_back, uint32_t limit_us, int32_t* status_dev, float* seen_dev,

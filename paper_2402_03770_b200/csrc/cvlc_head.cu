@@ -91,6 +91,8 @@ struct Product {
   int32_t* status;
   uint32_t first;                        // of the call's products
   uint32_t early;                        // the operands are there before the kernel in front has ended
+  uint32_t lost_copy, lost_tile;         // self-test: the tiles of a block from which on nothing is copied, its readers give up
+  uint64_t most;                         // nanoseconds, of every wait
 };
 template <int EPI>
 struct Products {
@@ -395,18 +397,23 @@ __device__ __forceinline__ void finish_tile(const Product& g, const Work& w, uin
   }
 }
 
+// where a block's first n tiles end
+__device__ __forceinline__ uint32_t first_tiles(uint32_t n, uint32_t first, uint32_t apart, uint32_t items) {
+  return (uint32_t)min((uint64_t)items, first + (uint64_t)n * apart);
+}
+
 template <int EPI, bool A_ROWS, bool B_ROWS, class T, int CG>
 __global__ void __launch_bounds__(kThreads, 1) k_head_product(const __grid_constant__ Products<EPI> both) {
   extern __shared__ uint8_t dynamic[];
   __shared__ uint64_t full[kMostStages], empty[kMostStages], made[2], taken[2], over;
-  __shared__ uint32_t tensor_at, late;
+  __shared__ uint32_t tensor_at, late, other_late, copies;  // late: somebody of this block has given up; of the pair's other one; stages whose copies this one has begun
   const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x & 31, rank = pair_rank<CG>();
   const uint32_t ring = (smem_at(dynamic) + 1023) & ~1023u;
   if (threadIdx.x == 0) {
     for (int i = 0; i < kMostStages; ++i) mbar_init(full + i, 1), mbar_init(empty + i, 1);
     for (int i = 0; i < 2; ++i) mbar_init(made + i, 1), mbar_init(taken + i, CG * kOutWarps);
     mbar_init(&over, 1);
-    late = 0;
+    late = other_late = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == 2) tensor_alloc<CG>(&tensor_at);
@@ -424,10 +431,11 @@ __global__ void __launch_bounds__(kThreads, 1) k_head_product(const __grid_const
   const uint32_t items0 = g0.skip && *g0.skip == 0 ? 0 : g0.tiles_m * g0.tiles_n * g0.splits;
   const Product& last = both.p[Products<EPI>::count - 1];
   const uint32_t items = items0 + (EPI == kBoth ? last.tiles_m * last.tiles_n * last.splits : 0);
-  bool ok = true;
+  bool ok = true, multiplied = false;
   if (warp == 0 && lane == 0) {
     uint32_t s = 0, phase = 0, issued = 0;
-    for (uint32_t w = first; ok && w < items; w += apart) {
+    const uint32_t end = first_tiles(g0.lost_copy, first, apart, items);
+    for (uint32_t w = first; ok && w < end; w += apart) {
       const bool second = EPI == kBoth && w >= items0;
       const Product& g = both.p[second ? Products<EPI>::count - 1 : 0];
       if (left_out(g, w)) continue;
@@ -435,7 +443,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_head_product(const __grid_const
       const bool a_rows = EPI == kBoth ? second : A_ROWS;
       const uint32_t a_bytes = CG == 2 ? kTileM * kTileK * 2 : g.a_bytes, bytes = CG == 2 ? 2 * kPairBytes : a_bytes + g.b_bytes, values = CG == 2 ? kTileK : g.values;
       for (uint32_t k = r.k_from; k < r.k_to; ++k) {
-        if (!(ok = mbar_wait(empty + s, phase ^ 1, &late))) break;
+        if (!(ok = mbar_wait(empty + s, phase ^ 1, &late, g0.most))) break;
         if (rank == 0) mbar_expect(full + s, bytes);
         const uint32_t a = ring + s * stage_bytes, b = a + a_bytes, bar = leader_at<CG>(smem_at(full + s)), n0 = r.n0 + rank * (g.tile_n / CG);
         if (a_rows) {
@@ -454,18 +462,12 @@ __global__ void __launch_bounds__(kThreads, 1) k_head_product(const __grid_const
         if (++s == stages) s = 0, phase ^= 1;
       }
     }
-    if (!ok && rank == 0) {  // copies that are on their way, the other block's among them, end before the blocks do
-      uint32_t none = 0;
-      for (uint32_t i = 0; i < (issued < stages ? issued : stages); ++i) {
-        if (s == 0) s = stages, phase ^= 1;
-        --s;
-        mbar_wait(full + s, phase, &none, kMostWait / 4);
-      }
-    }
+    copies = issued;
+    // what the products report of the last stages reaches this block before it leaves
+    for (uint32_t i = issued - min(issued, stages); ok && i < issued; ++i) ok = mbar_wait(empty + i % stages, i / stages & 1, &late, g0.most);
   } else if (warp == 1 && lane == 0 && rank == 0) {
     constexpr bool bf16 = std::is_same<T, __nv_bfloat16>::value;
     uint32_t s = 0, phase = 0, turn_of = 0;
-    bool any = false;
     for (uint32_t w = first; ok && w < items; w += apart) {
       const bool second = EPI == kBoth && w >= items0;
       const Product& g = both.p[second ? Products<EPI>::count - 1 : 0];
@@ -475,10 +477,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_head_product(const __grid_const
       const uint32_t kind = product_kind(bf16, a_rows, B_ROWS, CG * kTileM, g.tile_n);
       const uint32_t a_bytes = CG == 2 ? kTileM * kTileK * 2 : g.a_bytes, values = CG == 2 ? kTileK : g.values;
       const uint32_t half = turn_of & 1;
-      if (!(ok = mbar_wait(taken + half, (turn_of / 2 & 1) ^ 1, &late))) break;
+      if (!(ok = mbar_wait(taken + half, (turn_of / 2 & 1) ^ 1, &late, g0.most))) break;
       tensor_after();
       for (uint32_t k = r.k_from; k < r.k_to; ++k) {
-        if (!(ok = mbar_wait(full + s, phase, &late))) break;
+        if (!(ok = mbar_wait(full + s, phase, &late, g0.most))) break;
         tensor_after();
         const uint32_t a = ring + s * stage_bytes, b = a + a_bytes;
 #pragma unroll
@@ -488,27 +490,23 @@ __global__ void __launch_bounds__(kThreads, 1) k_head_product(const __grid_const
                          a_rows ? operand<true>(a + i * kStepBytes<true>, values) : operand<false>(a + i * kStepBytes<false>, values),
                          operand<B_ROWS>(b + i * kStepBytes<B_ROWS>, values), kind, k != r.k_from || i != 0);
         commit<CG>(empty + s);
-        any = true;
+        multiplied = true;
         if (++s == stages) s = 0, phase ^= 1;
       }
       if (ok) commit<CG>(made + half);
       ++turn_of;
     }
-    if (!ok && any) {
-      uint32_t none = 0;
-      commit<CG>(&over);
-      mbar_wait(&over, 0, &none, kMostWait / 4);
-    }
   } else if (warp >= 4) {
     const uint32_t half_tile = (warp - 4) / 4, quarter = warp & 3, box = ring + kRingBytes + (warp - 4) * kBoxBytes;
+    const uint32_t end = first_tiles(g0.lost_tile, first, apart, items);
     uint32_t turn_of = 0, w = first;
-    for (; w < items; w += apart) {
+    for (; w < end; w += apart) {
       const bool second = EPI == kBoth && w >= items0;
       const Product& g = both.p[second ? Products<EPI>::count - 1 : 0];
       if (left_out(g, w)) continue;
       const Work r = work_of<CG>(g, second ? w - items0 : w);
       const uint32_t half = turn_of & 1;
-      if (!(ok = __all_sync(kFull, mbar_wait(made + half, turn_of / 2 & 1, &late)))) break;
+      if (!(ok = __all_sync(kFull, mbar_wait(made + half, turn_of / 2 & 1, &late, g0.most)))) break;
       tensor_after();
       const uint32_t at = tensor + half * kTileN + half_tile * 128 + (quarter * 32 << 16);
       if constexpr (EPI == kBoth) {
@@ -522,6 +520,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_head_product(const __grid_const
       if (lane == 0) mbar_arrive_leader<CG>(taken + half);
       ++turn_of;
     }
+    if (w < items && ok) ok = false, *static_cast<volatile uint32_t*>(&late) = 1;
     if (EPI == kBoth && !ok && g0.whole)  // no kernel follows that would say it: what is missing of the hidden states' gradient is NaN
       for (; w < items0; w += apart) {
         const Work r = work_of<CG>(g0, w);
@@ -534,8 +533,30 @@ __global__ void __launch_bounds__(kThreads, 1) k_head_product(const __grid_const
   __syncwarp();
   tensor_before();
   __syncthreads();
+  if (CG == 2 && threadIdx.x == 0 && late) shared_store(other_at(smem_at(&other_late)), 1);
   pair_sync<CG>();
   tensor_after();
+  if (late || (CG == 2 && other_late)) {  // alike for both blocks of a pair.  What they have begun ends before they leave:
+    if (threadIdx.x == 0 && rank == 0) {  // the copies of the last stages, of both,
+      const uint32_t others = CG == 2 ? shared_load(other_at(smem_at(&copies))) : copies, most = max(copies, others);
+      for (uint32_t i = most - min(most, stages); i < most; ++i) {
+        uint32_t none = 0;
+        uint64_t* const b = full + i % stages;
+        if (i >= copies) mbar_expect(b, kPairBytes);  // begun by the other block alone
+        if (i >= others) mbar_came(b, kPairBytes);    // expected of it, and not begun
+        mbar_wait(b, i / stages & 1, &none, g0.most / 4);
+      }
+    }
+    if (multiplied) {  // and the products, where all are issued, too, and readers alone have given up
+      uint32_t none = 0;
+      commit<CG>(&over);
+      mbar_wait(&over, 0, &none, g0.most / 4);
+    }
+    __syncwarp();
+    tensor_before();
+    pair_sync<CG>();
+    tensor_after();
+  }
   if (warp == 2) tensor_free<CG>(tensor);
   if (threadIdx.x == 128) {  // of the warps that have waited for the kernel in front
     for (uint32_t i = blockIdx.x; i < kNumSM; i += gridDim.x) {
@@ -1287,12 +1308,14 @@ struct HeadRun {
   const cudaStream_t st;
   Header* const header;
   Operand hidden, head;
+  const HeadFault* const fault;
   bool behind = false;  // some kernel of the call is in front
+  uint32_t products = 0;  // launched so far
   cudaError_t error = cudaSuccess;
 
-  HeadRun(const cvlc_head& a_, uint32_t pieces, void* ws, cudaStream_t st_)
+  HeadRun(const cvlc_head& a_, uint32_t pieces, void* ws, cudaStream_t st_, const HeadFault* fault_)
       : a(a_), L(head_layout(a_, pieces)), base(static_cast<uint8_t*>(ws)), st(st_), header(static_cast<Header*>(ws)),
-        hidden{a_.hidden_dev, a_.dim, a_.rows, a_.hidden_stride}, head{a_.head_dev, a_.dim, a_.vocab, a_.head_stride} {}
+        hidden{a_.hidden_dev, a_.dim, a_.rows, a_.hidden_stride}, head{a_.head_dev, a_.dim, a_.vocab, a_.head_stride}, fault(fault_) {}
   template <class P>
   P* at(size_t off) const { return reinterpret_cast<P*>(base + off); }
   template <class... Params, class... Args>
@@ -1311,12 +1334,14 @@ struct HeadRun {
     Product p = {};
     p.splits = 1, p.alpha = a.scale, p.k2 = logit_scale(), p.targets = a.targets_dev, p.token_bytes = a.token_bytes;
     p.stats = at<float2>(L.off_stats), p.stats_stride = L.stats_stride, p.at_target = at<float>(L.off_target);
-    p.header = header, p.status = a.status_dev;
+    p.header = header, p.status = a.status_dev, p.lost_copy = p.lost_tile = ~0u, p.most = kMostWait;
     return p;
   }
   static constexpr bool bf16 = std::is_same<T, __nv_bfloat16>::value;
   template <int EPI, bool A_ROWS, bool B_ROWS, int CG>
-  void run_product(int id, const Products<EPI>& p, bool fits) {
+  void run_product(int id, Products<EPI> p, bool fits) {
+    if (fault && products == fault->product) p.p[0].lost_copy = fault->copy, p.p[0].lost_tile = fault->tile, p.p[0].most = fault->most;
+    ++products;
     uint64_t items = 0;
     for (const Product& x : p.p) items += (uint64_t)x.tiles_m * x.tiles_n * x.splits;
     if (error == cudaSuccess) error = fits ? run_product_of<EPI, A_ROWS, B_ROWS, T, CG>(id, p, items, st, behind) : cudaErrorUnknown;
@@ -1515,10 +1540,10 @@ struct HeadRun {
 size_t head_ws_bytes(const cvlc_head& a, uint32_t pieces) { return head_layout(a, pieces).total; }
 
 cudaError_t launch_head(const cvlc_head& a, uint32_t pieces, float* loss, void* d_hidden, uint64_t d_hidden_stride, void* d_head, uint64_t d_head_stride, void* ws,
-                        cudaStream_t st) {
+                        cudaStream_t st, const HeadFault* fault) {
   const Gradients g = {d_hidden, d_hidden_stride, d_head, d_head_stride};
-  if (a.dtype == CVLC_F16) return HeadRun<__half>(a, pieces, ws, st).run(loss, pieces ? &g : nullptr);
-  return HeadRun<__nv_bfloat16>(a, pieces, ws, st).run(loss, pieces ? &g : nullptr);
+  if (a.dtype == CVLC_F16) return HeadRun<__half>(a, pieces, ws, st, fault).run(loss, pieces ? &g : nullptr);
+  return HeadRun<__nv_bfloat16>(a, pieces, ws, st, fault).run(loss, pieces ? &g : nullptr);
 }
 
 }  // namespace cvlc

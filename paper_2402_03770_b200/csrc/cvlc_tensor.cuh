@@ -37,9 +37,26 @@ __device__ __forceinline__ void pair_sync() {  // of all threads
   else asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
+// A word in the shared memory of a pair's other block
+__device__ __forceinline__ uint32_t other_at(uint32_t at) {
+  uint32_t r;
+  asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(at), "r"(pair_rank<2>() ^ 1));
+  return r;
+}
+__device__ __forceinline__ void shared_store(uint32_t at, uint32_t x) { asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(at), "r"(x) : "memory"); }
+__device__ __forceinline__ uint32_t shared_load(uint32_t at) {
+  uint32_t x;
+  asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(x) : "r"(at) : "memory");
+  return x;
+}
+
 __device__ __forceinline__ void mbar_init(uint64_t* b, uint32_t n) { asm volatile("mbarrier.init.shared.b64 [%0], %1;" ::"r"(smem_at(b)), "r"(n)); }
 __device__ __forceinline__ void mbar_expect(uint64_t* b, uint32_t bytes) {
   asm volatile("mbarrier.arrive.expect_tx.shared.b64 _, [%0], %1;" ::"r"(smem_at(b)), "r"(bytes) : "memory");
+}
+// bytes that are expected and will not come count as come
+__device__ __forceinline__ void mbar_came(uint64_t* b, uint32_t bytes) {
+  asm volatile("mbarrier.complete_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(smem_at(b)), "r"(bytes) : "memory");
 }
 __device__ __forceinline__ void mbar_arrive(uint64_t* b) { asm volatile("mbarrier.arrive.shared.b64 _, [%0];" ::"r"(smem_at(b)) : "memory"); }
 // The tensor memory has been read (tensor_loaded() has waited for it), and nothing else is handed over: an arrival that released would wait for the stores of all that

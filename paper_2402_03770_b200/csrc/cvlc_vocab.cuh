@@ -70,9 +70,14 @@ struct EmbedGradArgs {
 cudaError_t launch_embed_grad(const EmbedGradArgs& a, uint32_t dtype, cudaStream_t st);
 size_t embed_grad_ws_bytes(uint64_t n, uint32_t dim);
 
+// A fault for the self-test, in one of a call's products: the tile of every block from which on it copies nothing, the one at which its readers give up, the limit of waits
+struct HeadFault {
+  uint32_t product, copy, tile;
+  uint64_t most;
+};
 size_t head_ws_bytes(const cvlc_head& a, uint32_t pieces);
 cudaError_t launch_head(const cvlc_head& a, uint32_t pieces, float* loss, void* d_hidden, uint64_t d_hidden_stride, void* d_head, uint64_t d_head_stride, void* ws,
-                        cudaStream_t st);  // pieces = 0: the loss alone
+                        cudaStream_t st, const HeadFault* fault = nullptr);  // pieces = 0: the loss alone
 
 cudaError_t launch_adamw(const cvlc_adamw_tensor* tensors, uint32_t n, const cvlc_adamw_args& a, cudaStream_t st);
 size_t norm_ws_bytes(uint32_t n);
