@@ -520,15 +520,18 @@ int cvlc_embed_grad(const void* tokens_dev, uint32_t token_bytes, uint64_t n, co
 
 /*
  * The training loss of such a model: softmax cross entropy of hidden states against the head, the matrix whose rows are the words (the
- * embedding table itself, or one of its own), without ever holding more than 2^22 logits.  With z = scale hidden_t . head_v,
+ * embedding table itself, or one of its own).  Up to 2^22 logits (the loss alone: 2^20) of up to 8192 words are held; of more, the loss alone
+ * holds none, and a step their exponentials, or with several pieces a piece's gradients (see pieces).  With z = scale hidden_t . head_v,
  *   loss_t = row_weight_t (ln sum_v exp(z_tv) - z_t,target)
  * and, for cvlc_head_step, the gradients of the sum of all losses, d_hidden and d_head, in the operands' type.
  * A target below 0 is none, and a row without one, or of weight 0, counts for nothing, whatever it holds: its loss, its gradient and
- * its part of d_head are 0.  A target >= vocab is treated as none and reported (INVALID_ARG) in *status_dev (one int32 of the caller's,
- * 0 beforehand; or NULL).  A NaN or +infinite logit makes the row's loss, and what the row has a part in, not finite (one of
+ * its part of d_head are 0 (but for d_hidden in columns where some word of the head is not finite: 0 times that is no number).
+ * A target >= vocab is treated as none and reported (INVALID_ARG) in *status_dev (one int32 of the caller's, 0 beforehand; or NULL).  A NaN or +infinite logit makes the row's loss, and what the row has a part in, not finite (one of
  * -infinity the loss of its own word, and the gradients).
  * The products are made by the tensor cores: operands in 16 bits (CVLC_F16 or CVLC_BF16; there is no product of fp32), sums in fp32, in steps of 16 that
- * are cut off instead of rounded (what that takes from a logit on average is put back).  A logit's gradient, row_weight (softmax - one for the target), is rounded to the operands' type (in fp16 times a
+ * are cut off instead of rounded.  What that takes from a logit on average, dim / 64 units of 2^-24 of it, is put back: at dim 4096 losses of sums that
+ * grow evenly are 0.8e-6 off instead of 2.2e-6, of one that lies all in its first values 2.8e-6 instead of 6.6e-6, but of one all in its last
+ * values 3.7e-6 instead of 0.1e-6.  A logit's gradient, row_weight (softmax - one for the target), is rounded to the operands' type (in fp16 times a
  * power of two that keeps the largest row_weight at 2^15), as the operand of the two products that follow, and d_hidden and d_head once more.  With more than
  * 128 rows in one piece, and more than 2^22 logits or 8192 words, there is another rounding: the exponentials are kept in 16 bits; in fp16 they are multiplied later,
  * in bf16 their rows' factors go into the hidden states for d_head, which are rounded.
@@ -539,9 +542,10 @@ int cvlc_embed_grad(const void* tokens_dev, uint32_t token_bytes, uint64_t n, co
  *               vocab / pieces values of 16 bits (up to 128 rows in one piece, or 2^22 logits: of 32 bits, too).  With one piece the first product is not made
  *               twice
  *  d_hidden_dev, d_head_dev   as hidden and head, of strides of their own; they must not overlap hidden, head or each other
- *  ws_dev       cvlc_head_workspace_bytes(a, graded) bytes (graded: 0 for cvlc_head_loss, 1 for cvlc_head_step), 256-byte aligned
+ *  ws_dev       cvlc_head_workspace_bytes(a, graded) bytes (graded: 0 for cvlc_head_loss, 1 for cvlc_head_step), 256-byte aligned; they depend on sizes, type, pieces and on
+ *               whether hidden's and head's rows begin on 16 bytes
  * Results do not depend on the order in which blocks run.  Waits inside the kernels are bounded (four seconds): should one run out,
- * CVLC_ERR_DEVICE_TIMEOUT goes to *status_dev, and what it had a part in of losses and d_hidden is NaN, d_head undefined.
+ * CVLC_ERR_DEVICE_TIMEOUT goes to *status_dev, and what it had a part in of losses and d_hidden is NaN, d_head undefined (cvlc_selftest_head).
  * Errors: INVALID_ARG (dtype, vocab from 1 to CVLC_MAX_VOCAB, dim from 1 to 65536, rows above 2^24, a stride below dim or above 2^32, a scale that
  * is not finite, pieces of 0, alignment, overlap), WORKSPACE_TOO_SMALL.  rows = 0 writes zeros to d_head.
  */
@@ -587,7 +591,7 @@ int cvlc_head_step(const cvlc_head* a, float* loss_dev, void* d_hidden_dev, uint
  *               A *step_dev of 0 changes nothing and reports INVALID_ARG in *status_dev
  *  norm_dev     clip = min(1, max_norm / *norm_dev) (cvlc_grad_norm's, with the same grad_scale); NULL: clip = 1.  If it is
  *               not finite the call changes nothing and reports NONFINITE_INPUT in *status_dev (one int32 of the caller's, or NULL)
- * A value whose v / (1 - beta2^t) is above 2^104 (a gradient of 4e15) takes no step.
+ * A value whose v / (1 - beta2^t) is above 2^104 (a gradient of 4e15) takes no step but its decay's.
  * Tensors may begin at any element (16-byte alignment of all of a tensor's arrays, or the same misalignment with states of 32
  * bits, is faster), must not overlap, and are left alone where n = 0.  Equal inputs give equal bits.
  * Errors: INVALID_ARG (types, bits, a pointer that is not aligned to its type, n above 2^40 in all, betas outside [0, 1), eps below

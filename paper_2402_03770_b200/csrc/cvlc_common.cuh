@@ -410,9 +410,10 @@ inline cudaError_t allow_shared(K kernel, size_t bytes) {
 // Every kernel of the plan / encode / decode path but the first of a call is launched with programmatic stream serialization: it is
 // set up while the kernel before it drains, and pdl_enter(), the first thing every thread does, waits until that kernel is complete and its
 // writes are visible.  Nothing is read or written before that.  This takes about 2 us off every kernel boundary (one small
-// client, 12 kernels: 101 -> 78 us a pass; 100 ResNet-18 clients: 3.89 -> 3.87 ms).  No kernel lets its successor in before
+// client, 12 kernels: 101 -> 78 us a pass; 100 ResNet-18 clients: 3.89 -> 3.87 ms).  No kernel of that path lets its successor in before
 // its own blocks have left (griddepcontrol.launch_dependents): blocks that move in early gather on the SMs that happen to be
 // free, and the successor then runs on part of the chip (error compensation 314 -> 361 us, the large round 3.87 -> 4.00 ms).
+// The kernels of a head do, and one of them reads before its wait, by a rule of their own (let_next_in() in cvlc_head.cu).
 // The attribute leaves the order behind the kernel before it on the stream to pdl_enter(), and waiting for that kernel alone is enough
 // only where it has waited for its own predecessor.  Ours have.  What precedes the first kernel of a call is the caller's: a kernel
 // launched in the same way that does not wait may end before the work in front of it.  So the first kernel of a call is an ordinary

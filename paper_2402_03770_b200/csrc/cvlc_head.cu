@@ -1,4 +1,4 @@
-// Softmax cross entropy of hidden states against a head matrix, and its gradients, without the logits.
+// Softmax cross entropy of hidden states against a head matrix, and its gradients, without holding the logits, but where they are few.
 //
 // z_tv = scale h_t . w_v;  loss_t = weight_t (ln sum_v exp(z_tv) - z_t,target);  G_tv = weight_t (q_tv - [v = target]);
 // dh_t = scale sum_v G_tv w_v;  dw_v = scale sum_t G_tv h_t
@@ -38,7 +38,9 @@ namespace {
 constexpr float kLog2E = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 // The kernel behind may be set up while this one runs: the small ones fit beside a block of the products, and a block of theirs moves in as soon as an
-// SM is free; it waits for the rest before it reads or writes anything that this one does.
+// SM is free; it waits for the rest before it reads or writes anything that this one does.  The rule: a kernel first waits for the one in front (pdl_enter()), then lets
+// the next one in.  So when a kernel starts, all kernels of the call but the one directly in front are complete, and so is what the caller has in front of the call, whose
+// first kernel is an ordinary launch.  What they have written, and the one in front does not write, may be read ahead of the wait (`early`).
 __device__ __forceinline__ void let_next_in() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 
 // ---- the products --------------------------------------------------------------------------
@@ -314,7 +316,7 @@ __device__ __forceinline__ void finish_tile(const Product& g, const Work& w, uin
     }
     if (there) g.stats[(uint64_t)(w.slot + half) * g.stats_stride + row] = make_float2(most, sum);
   } else if constexpr (EPI == kProbs) {
-    // x: ln sum exp in log2, less the exponent that is added; y: the weight, 0 where the row counts for nothing; z: the target's value
+    // x: ln sum exp in log2; y: the weight, times the power of two by which G is raised, 0 where the row counts for nothing; z: the target's G
     const float4 r = there ? g.row[row] : make_float4(0, 0, 0, 0);
     const int64_t target = there ? target_of(g.targets, g.token_bytes, row) - g.col0 : -1;
     for (int c = 0; c < 4; ++c) {
@@ -1493,7 +1495,8 @@ struct HeadRun {
     for (uint32_t turn = 0; turn < 2; ++turn) {
       Product p = product();
       p.m = (uint32_t)a.rows, p.n = a.vocab, p.k_blocks = tiles(a.dim, kTileK), p.first = turn == 0;
-      p.out = base + L.off_g, p.ldo = L.ldg, p.early = turn == 0;
+      p.out = base + L.off_g, p.ldo = L.ldg;
+      p.early = turn == 0;  // k_head_target, in front, writes none of the operands, and the copies of rows, if any, are complete: it has waited for them
       if (turn) p.skip = &header->wild, p.wild = t.wild;
       if constexpr (bf16) multiply<kKeep>(kKHeadKeep, p, head);
       RowsArgs r = rows(loss);
